@@ -13,6 +13,8 @@
  *   fs_solve_bounds       conservative / optimistic allocations and Gamma_t
  *   fs_set_floors         critical classes' fulfilment floors (tier 1)
  *   fs_reveal, fs_certificate, fs_replay            the profiling loop
+ *   fs_kv_append, fs_kv_attend                      a rank's share of the serving step that
+ *                                                   a cell's measurement runs
  *
  * Notation (paper, Section 3): class i has demand lambda_i (req/s) and an SLO
  * L_i (s) on its binding tail metric. A configuration is a TP degree
@@ -482,6 +484,153 @@ int fs_timing_read(fs_model *m, double *kernel_ms, int32_t *launches, double *ph
  * [1, 1000] or a null output.
  */
 int fs_draw_floor(int32_t mode, int32_t w, int64_t calls, int32_t reps, double *ms, int64_t *calls_done);
+
+/*
+ * ---- The serving step of one rank: a paged 8-bit cache and its attention ----
+ *
+ * A cell's measurement (Section 5) runs a replica of tau GPUs on batches of
+ * requests. What one GPU of the replica does per layer beside its matrix products
+ * is: put the new tokens' keys and values into the cache (fs_kv_append), and let
+ * their queries attend to it (fs_kv_attend). Timed on the GPU at hand, these bound a
+ * cell before it is measured: no replica is faster than its attention alone
+ * (paper_2608_19659_gb300/probe.py tightens a model's optimistic bounds so). The
+ * paper's replica serves in FP8; the cache holds e4m3 codes with one scale per
+ * (page, key head).
+ *
+ * Both calls take device pointers, enqueue their work on cuda_stream and return;
+ * they allocate nothing and can be captured into a CUDA graph. fs_kv_check waits
+ * and reports device-side errors.
+ *
+ * fs_kv_cache: pages of page_tokens tokens (16, 32, 64 or 128), `heads` key heads
+ * of `dim` (64 or 128) dimensions. k and v hold e4m3 codes; the code of token slot
+ * t, dimension d of (page, head) is at page * page_stride + head * head_stride +
+ * t * token_stride + d (bytes; strides multiples of 16, k and v 16-byte aligned).
+ * k_scale, v_scale: [pages][heads] floats >= 0; a code stands for its value times
+ * its (page, head)'s scale. Slots that hold no token may hold any bytes. A slot
+ * that holds a token must not hold a NaN code (fs_kv_append writes none).
+ */
+typedef struct {
+    int32_t pages;
+    int32_t heads;
+    int32_t page_tokens;
+    int32_t dim;
+    void *k;
+    void *v;
+    float *k_scale;
+    float *v_scale;
+    int64_t page_stride;
+    int64_t head_stride;
+    int64_t token_stride;
+} fs_kv_cache;
+
+/*
+ * fs_kv_batch: sequence b has length[b] tokens in the cache once the call's new ones
+ * are in, and its new tokens, the last of them, are rows q_start[b] .. q_start[b + 1]
+ * of the call's arrays (none: a slot without a request, or one that only waits).
+ * Token position p of sequence b is in page page_table[b * table_stride +
+ * p / page_tokens], slot p mod page_tokens; entries beyond a sequence's tokens are
+ * not read. A row whose position would be negative (more new tokens than length) is
+ * not appended and attends to nothing. Host values: tokens = q_start[batch],
+ * max_new >= every sequence's new tokens, max_length >= every length (bounds: what
+ * launches are sized by). The device arrays are not checked before the call; the
+ * kernels check them, skip a sequence that breaks a bound, and set KV status bits
+ * (fs_kv_check: FS_EDEVICE). Limits: batch <= 65535, tokens * query heads <= 2^31 - 1,
+ * heads <= 1024, max_length <= 2^30.
+ */
+typedef struct {
+    int32_t batch;
+    int32_t tokens;
+    int32_t max_new;
+    int32_t max_length;
+    int32_t table_stride;
+    int32_t reserved;
+    const int32_t *page_table;
+    const int32_t *length;
+    const int32_t *q_start;
+} fs_kv_batch;
+
+#define FS_KV_BF16 0
+#define FS_KV_FP16 1
+
+/* Rows of 16-bit floats: (token, head) at data + token * token_stride + head *
+ * head_stride (elements, multiples of 8; data 16-byte aligned), dim contiguous. */
+typedef struct {
+    void *data;
+    int64_t token_stride;
+    int64_t head_stride;
+} fs_kv_rows;
+
+/*
+ * The workspace of both calls: device memory of at least the bytes that
+ * fs_kv_workspace_bytes gives for the largest cache, batch and q_heads that will
+ * use it, 256-byte aligned, zero-filled once before its first use. It holds the
+ * status word and parts of results; calls that share one run one after the other.
+ */
+int fs_kv_workspace_bytes(const fs_kv_cache *cache, const fs_kv_batch *batch, int32_t q_heads,
+                          int64_t *bytes);
+
+/*
+ * fs_kv_append -- new keys and values into the cache, rotated by position on the way.
+ *   dtype      FS_KV_BF16 or FS_KV_FP16, of every fs_kv_rows of the call
+ *   k, v       [tokens][cache->heads][dim]
+ *   cos, sin   [angle_rows][rot / 2] floats, row = position; NULL with rot = 0: no
+ *              rotation. rot: rotated dimensions, a multiple of 8, <= dim. With
+ *              interleaved = 0 dimension i < rot / 2 pairs with i + rot / 2, else 2 i
+ *              with 2 i + 1; (a, b) becomes (a c - b s, b c + a s), every step rounded
+ *              to float. Values are not rotated.
+ *   q, q_out   optional [tokens][q_heads][dim] queries, rotated alike and rounded once
+ *              to dtype (q_out may be q); NULL data: none.
+ * The scale of a (page, head) that the call writes to becomes the larger of its old
+ * one (0 if the call writes slot 0: a fresh page) and the least power of two s >=
+ * 2^-126 with |x| <= 448 s for the call's finite values x there (0 if they are all 0).
+ * Where it grows, codes of earlier tokens of the page are rescaled (a power of two:
+ * exact unless they leave e4m3's normal range). Codes are x / scale rounded to
+ * nearest even. Infinities become +-448 times the scale; a NaN becomes 0 and sets a
+ * status bit. Pages that a batch writes to belong to one sequence each.
+ */
+typedef struct {
+    int32_t dtype;
+    int32_t q_heads;
+    int32_t rot;
+    int32_t interleaved;
+    int32_t angle_rows;
+    int32_t reserved;
+    fs_kv_rows k;
+    fs_kv_rows v;
+    fs_kv_rows q;
+    fs_kv_rows q_out;
+    const float *cos;
+    const float *sin;
+} fs_kv_new;
+
+int fs_kv_append(const fs_kv_cache *cache, const fs_kv_batch *batch, const fs_kv_new *rows,
+                 void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/*
+ * fs_kv_attend -- out = softmax(scale q k^T) v for every new token over the cached
+ * tokens of its sequence up to its own position, or with window > 0 over the last
+ * `window` of those. q_heads is a multiple of cache->heads; query head h reads key
+ * head h / (q_heads / heads). Sums, softmax statistics and the accumulators are
+ * floats; probabilities are rounded to half precision relative to the row's largest,
+ * the result once to dtype. A row that sees no token becomes 0. Rows of out that
+ * belong to a sequence skipped for a broken bound are left as they are.
+ */
+typedef struct {
+    int32_t dtype;
+    int32_t q_heads;
+    float scale;
+    int32_t window;
+    fs_kv_rows q;
+    fs_kv_rows out;
+} fs_kv_query;
+
+int fs_kv_attend(const fs_kv_cache *cache, const fs_kv_batch *batch, const fs_kv_query *query,
+                 void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/* Waits for cuda_stream and reports what the calls on this workspace met since the last
+ * check (FS_EDEVICE, FS_ETIMEOUT); clears the status word and, after an error, the
+ * workspace's tickets. */
+int fs_kv_check(void *workspace, void *cuda_stream);
 
 /* Kernels this library has launched since it was loaded (all models). */
 uint64_t fs_launch_count(void);

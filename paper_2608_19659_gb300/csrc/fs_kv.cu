@@ -1,0 +1,531 @@
+// The cache operators' entry points, and appending to the cache.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <climits>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+
+#include "fs_kv.cuh"
+
+namespace fs {
+
+int record_error(int code, const char* msg);
+
+namespace {
+
+int say(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return record_error(code, buf);
+}
+
+int cuda_say(cudaError_t e, const char* what) { return say(FS_ECUDA, "%s: %s", what, cudaGetErrorString(e)); }
+
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+int log2_page(int p) { return p == 16 ? 4 : p == 32 ? 5 : p == 64 ? 6 : p == 128 ? 7 : -1; }
+
+int check_cache(const fs_kv_cache* c) {
+  if (!c) return say(FS_EINVAL, "cache is NULL");
+  if (c->pages < 1) return say(FS_EINVAL, "cache pages = %d < 1", c->pages);
+  if (c->heads < 1 || c->heads > 1024) return say(FS_EINVAL, "cache heads = %d outside [1, 1024]", c->heads);
+  if (log2_page(c->page_tokens) < 0) return say(FS_EINVAL, "page_tokens = %d is not 16, 32, 64 or 128", c->page_tokens);
+  if (c->dim != 64 && c->dim != 128) return say(FS_EINVAL, "dim = %d is not 64 or 128", c->dim);
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale) return say(FS_EINVAL, "a cache pointer is NULL");
+  if (!aligned(c->k, 16) || !aligned(c->v, 16)) return say(FS_EINVAL, "cache k / v are not 16-byte aligned");
+  if (!aligned(c->k_scale, 4) || !aligned(c->v_scale, 4)) return say(FS_EINVAL, "cache scales are not 4-byte aligned");
+  const int64_t st[3] = {c->page_stride, c->head_stride, c->token_stride};
+  for (int64_t s : st)
+    if (s < 16 || s % 16 || s >= (1ll << 40)) return say(FS_EINVAL, "cache strides must be multiples of 16 in [16, 2^40)");
+  if (c->token_stride < c->dim) return say(FS_EINVAL, "cache token_stride is less than dim");
+  return FS_OK;
+}
+
+int check_batch(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads) {
+  if (!b) return say(FS_EINVAL, "batch is NULL");
+  if (b->batch < 0 || b->batch > 65535) return say(FS_EINVAL, "batch = %d outside [0, 65535]", b->batch);
+  if (b->tokens < 0 || b->max_new < 0 || b->max_new > b->tokens)
+    return say(FS_EINVAL, "tokens = %d, max_new = %d: want 0 <= max_new <= tokens", b->tokens, b->max_new);
+  if (b->max_length < 0 || b->max_length > (1 << 30))
+    return say(FS_EINVAL, "max_length = %d outside [0, 2^30]", b->max_length);
+  if (b->table_stride < 0 || (int64_t)b->table_stride * c->page_tokens < b->max_length)
+    return say(FS_EINVAL, "table_stride = %d pages are fewer than max_length = %d tokens need", b->table_stride,
+               b->max_length);
+  if ((int64_t)b->table_stride * c->page_tokens > INT_MAX) return say(FS_EINVAL, "table_stride = %d is too large", b->table_stride);
+  if (q_heads < 1 || q_heads > 65535) return say(FS_EINVAL, "q_heads = %d outside [1, 65535]", q_heads);
+  if ((int64_t)b->tokens * q_heads > INT_MAX) return say(FS_EINVAL, "tokens * q_heads exceeds 2^31 - 1");
+  if (b->batch && b->tokens && (!b->page_table || !b->length || !b->q_start))
+    return say(FS_EINVAL, "page_table / length / q_start is NULL");
+  return FS_OK;
+}
+
+int check_rows(const fs_kv_rows& r, const char* name) {
+  if (!r.data) return say(FS_EINVAL, "%s is NULL", name);
+  if (!aligned(r.data, 16)) return say(FS_EINVAL, "%s is not 16-byte aligned", name);
+  if (r.token_stride % 8 || r.head_stride % 8 || r.token_stride < 0 || r.head_stride < 0)
+    return say(FS_EINVAL, "%s: strides must be multiples of 8 elements, >= 0", name);
+  return FS_OK;
+}
+
+KvView view_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, void* ws) {
+  KvView v{};
+  v.pages = c->pages;
+  v.heads = c->heads;
+  v.log_page = log2_page(c->page_tokens);
+  v.batch = b->batch;
+  v.tokens = b->tokens;
+  v.max_new = b->max_new;
+  v.table_stride = b->table_stride;
+  v.group = q_heads / c->heads;
+  v.k_scale = c->k_scale;
+  v.v_scale = c->v_scale;
+  v.page_table = b->page_table;
+  v.length = b->length;
+  v.q_start = b->q_start;
+  v.status = static_cast<uint32_t*>(ws);
+  return v;
+}
+
+// ---------------------------------------------------------------- append
+
+struct KvAppendArgs {
+  KvView v;
+  uint8_t *kc, *vc;
+  long long page_stride, head_stride, token_stride;
+  const void *k, *vals, *q;
+  void* q_out;
+  long long k_token, k_head, v_token, v_head, q_token, q_head, o_token, o_head;
+  const float *cos, *sin;
+  int rot, angle_rows, interleaved, q_heads;
+};
+
+// Four dimensions from d0 on of a row, rotated for position `pos`; x: the row's own
+// four, row: the row (for the other half of a pair).
+template <typename T>
+__device__ __forceinline__ void rotate4(float (&x)[4], const T* row, int d0, const KvAppendArgs& a, int pos) {
+  if (d0 >= a.rot) return;
+  const int half = a.rot >> 1;
+  const float* ct = a.cos + (long long)pos * half;
+  const float* st = a.sin + (long long)pos * half;
+  if (a.interleaved) {
+    const float2 c = *reinterpret_cast<const float2*>(ct + (d0 >> 1));
+    const float2 s = *reinterpret_cast<const float2*>(st + (d0 >> 1));
+    const float y0 = __fsub_rn(__fmul_rn(x[0], c.x), __fmul_rn(x[1], s.x));
+    const float y1 = __fadd_rn(__fmul_rn(x[1], c.x), __fmul_rn(x[0], s.x));
+    const float y2 = __fsub_rn(__fmul_rn(x[2], c.y), __fmul_rn(x[3], s.y));
+    const float y3 = __fadd_rn(__fmul_rn(x[3], c.y), __fmul_rn(x[2], s.y));
+    x[0] = y0, x[1] = y1, x[2] = y2, x[3] = y3;
+    return;
+  }
+  const bool low = d0 < half;
+  const int i0 = low ? d0 : d0 - half;
+  const uint2 w = *reinterpret_cast<const uint2*>(row + (low ? d0 + half : d0 - half));
+  const float2 p01 = Elem<T>::two(w.x), p23 = Elem<T>::two(w.y);
+  const float4 c = *reinterpret_cast<const float4*>(ct + i0), s = *reinterpret_cast<const float4*>(st + i0);
+  const float p[4] = {p01.x, p01.y, p23.x, p23.y}, cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float m = __fmul_rn(x[i], cc[i]), n = __fmul_rn(p[i], ss[i]);
+    x[i] = low ? __fsub_rn(m, n) : __fadd_rn(m, n);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void load4(float (&x)[4], const T* p) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  const float2 a = Elem<T>::two(w.x), b = Elem<T>::two(w.y);
+  x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+}
+
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// The least power of two s >= 2^-126 with amax <= 448 s; 0 for 0. amax finite.
+__device__ __forceinline__ float scale_for(float amax) {
+  if (!(amax > 0.f)) return 0.f;
+  const uint32_t b = __float_as_uint(amax);
+  const int e = (int)(b >> 23) - 127;  // subnormals: -127, and the bound below holds
+  const int p = e - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);  // 448 = 1.75 * 2^8
+  return exp2_int(max(p, -126));
+}
+
+// One unit of D / 8 lanes appends the new tokens of one (sequence, page) for one head
+// of keys or values, or rotates one query head over them. Its lanes hold dimensions
+// 4 l .. 4 l + 3 of each half. Two passes over the tokens: the largest magnitude,
+// then the codes.
+template <int D, typename T>
+__global__ void __launch_bounds__(128) k_kv_append(const KvAppendArgs a) {
+  constexpr int kLanes = D / 8, kUnits = 128 / kLanes;
+  const int b = blockIdx.z, piece = blockIdx.x;
+  const int unit = threadIdx.x / kLanes, l = threadIdx.x % kLanes;
+  const int job = blockIdx.y * kUnits + unit;  // [0, heads) keys, [heads, 2 heads) values, then queries
+  KvSeq s;
+  if (!kv_seq(a.v, b, s)) {
+    if (threadIdx.x == 0) kv_flag(a.v, KV_ST_BATCH);
+    return;
+  }
+  const int P = 1 << a.v.log_page;
+  const int p0 = max(s.len - s.count, 0);  // first position that is appended
+  const int pg = (p0 >> a.v.log_page) + piece;
+  const int lo = max(p0, pg << a.v.log_page), hi = min(s.len, (pg + 1) << a.v.log_page);
+  if (lo >= hi || s.count == 0) return;
+  const int H = a.v.heads;
+  if (job >= 2 * H + (a.q ? a.q_heads : 0)) return;
+  const long long row0 = (long long)s.first - (s.len - s.count);  // + position: the token's row
+  if (a.rot && hi > a.angle_rows) {
+    if (l == 0) kv_flag(a.v, KV_ST_ANGLE);
+    return;
+  }
+  const int dA = 4 * l, dB = D / 2 + 4 * l;
+  const uint32_t mask = (kLanes == 16 ? 0xffffu : 0xffu) << (threadIdx.x % 32 / kLanes * kLanes);  // the unit's lanes
+
+  // Tokens go by fours: their loads are all under way before the first store.
+  if (job >= 2 * H) {
+    const int h = job - 2 * H;
+    for (int p = lo; p < hi; p += 4) {
+      const int n = min(4, hi - p);
+      float x[4][4], y[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < n) {
+          const T* row = static_cast<const T*>(a.q) + (row0 + p + i) * a.q_token + h * a.q_head;
+          load4(x[i], row + dA);
+          load4(y[i], row + dB);
+          rotate4(x[i], row, dA, a, p + i);
+          rotate4(y[i], row, dB, a, p + i);
+        }
+      __syncwarp(mask);  // q_out may be q: every lane of a row has read before one writes
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < n) {
+          T* to = static_cast<T*>(a.q_out) + (row0 + p + i) * a.o_token + h * a.o_head;
+          *reinterpret_cast<uint2*>(to + dA) = make_uint2(Elem<T>::pack(x[i][0], x[i][1]), Elem<T>::pack(x[i][2], x[i][3]));
+          *reinterpret_cast<uint2*>(to + dB) = make_uint2(Elem<T>::pack(y[i][0], y[i][1]), Elem<T>::pack(y[i][2], y[i][3]));
+        }
+    }
+    return;
+  }
+
+  const bool is_k = job < H;
+  const int h = is_k ? job : job - H;
+  const T* src = is_k ? static_cast<const T*>(a.k) + row0 * a.k_token + h * a.k_head
+                      : static_cast<const T*>(a.vals) + row0 * a.v_token + h * a.v_head;
+  const long long src_token = is_k ? a.k_token : a.v_token;
+  const int g = kv_page(a.v, b, pg);
+  uint8_t* page = (is_k ? a.kc : a.vc) + g * a.page_stride + h * a.head_stride;
+  float* scale_at = const_cast<float*>(is_k ? a.v.k_scale : a.v.v_scale) + (long long)g * H + h;
+  const int slot0 = lo & (P - 1);
+  const float old = slot0 ? *scale_at : 0.f;
+
+  float amax = 0.f;
+  bool nan = false;
+#pragma unroll 4
+  for (int p = lo; p < hi; ++p) {
+    const T* row = src + p * src_token;
+    float x[4], y[4];
+    load4(x, row + dA);
+    load4(y, row + dB);
+    if (is_k) {
+      rotate4(x, row, dA, a, p);
+      rotate4(y, row, dB, a, p);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float u = fabsf(x[i]), w = fabsf(y[i]);
+      if (u < INFINITY) amax = fmaxf(amax, u);
+      if (w < INFINITY) amax = fmaxf(amax, w);
+      nan |= u != u || w != w;
+    }
+  }
+  if (nan) kv_flag(a.v, KV_ST_VALUE);
+#pragma unroll
+  for (int o = kLanes / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(mask, amax, o));
+  const float now = fmaxf(old, scale_for(amax));
+  if (slot0 && now > old) {
+    // the page's earlier tokens, 8 codes a lane
+    const float f = __fdiv_rn(old, now);
+    uint8_t* at = page + 8 * l;
+#pragma unroll 4
+    for (int t = 0; t < slot0; ++t) {
+      uint2* w = reinterpret_cast<uint2*>(at + t * a.token_stride);
+      const uint2 c = *w;
+      uint32_t r[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t u = i ? c.y : c.x;
+        const float2 lo2 = Elem<__half>::two(e4m3x2_to_f16x2(u)), hi2 = Elem<__half>::two(e4m3x2_to_f16x2_hi(u));
+        r[i] = e4m3x2(__fmul_rn(lo2.x, f), __fmul_rn(lo2.y, f)) | e4m3x2(__fmul_rn(hi2.x, f), __fmul_rn(hi2.y, f)) << 16;
+      }
+      *w = make_uint2(r[0], r[1]);
+    }
+  }
+  if (l == 0) *scale_at = now;
+
+  const float inv = now > 0.f ? __fdiv_rn(1.f, now) : 0.f;
+  for (int p = lo; p < hi; p += 4) {
+    const int n = min(4, hi - p);
+    float x[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) {
+        const T* row = src + (p + i) * src_token;
+        float u[4], w[4];
+        load4(u, row + dA);
+        load4(w, row + dB);
+        if (is_k) {
+          rotate4(u, row, dA, a, p + i);
+          rotate4(w, row, dB, a, p + i);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[i][j] = u[j], x[i][4 + j] = w[j];
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float u = x[i][j];
+          // (an infinity times 0 would be NaN; the conversion saturates)
+          x[i][j] = u != u ? 0.f : fabsf(u) < INFINITY ? __fmul_rn(u, inv) : u;
+        }
+        uint8_t* to = page + (long long)((p + i) & (P - 1)) * a.token_stride;
+        *reinterpret_cast<uint32_t*>(to + dA) = e4m3x2(x[i][0], x[i][1]) | e4m3x2(x[i][2], x[i][3]) << 16;
+        *reinterpret_cast<uint32_t*>(to + dB) = e4m3x2(x[i][4], x[i][5]) | e4m3x2(x[i][6], x[i][7]) << 16;
+      }
+  }
+}
+
+template <int D, typename T>
+cudaError_t launch_append(const KvAppendArgs& a, int pieces, cudaStream_t s) {
+  constexpr int kUnits = 128 / (D / 8);
+  const int jobs = 2 * a.v.heads + (a.q ? a.q_heads : 0);
+  k_kv_append<D, T><<<dim3(pieces, (jobs + kUnits - 1) / kUnits, a.v.batch), 128, 0, s>>>(a);
+  note_launch();
+  return cudaGetLastError();
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder, looked up once (the library does not link libcuda).
+EncodeTiled encode_tiled() {
+  static const EncodeTiled f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+        r != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiled>(p);
+  }();
+  return f;
+}
+
+int sm_count_of(int dev) {
+  static std::atomic<int> known[64];
+  if (dev < 0 || dev >= 64) return 0;
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (!n && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess)
+    known[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+// How an attend call is cut up (see k_kv_decode): rows of a (sequence, key head) in tiles
+// of row_tile, the cache axis in parts of `split` tokens.
+struct KvPlan {
+  int row_tile, row_blocks, split, splits;
+  size_t part_floats;
+};
+
+constexpr int kMinSplit = 256, kMaxSplit = 4096;
+
+KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int sms) {
+  KvPlan p{};
+  const int rows = std::max(1, b->max_new) * (q_heads / c->heads);
+  p.row_tile = rows <= 8 ? 8 : 16;
+  p.row_blocks = (rows + p.row_tile - 1) / p.row_tile;
+  const long long items = (long long)std::max(1, b->batch) * c->heads * p.row_blocks;
+  const int len = std::max(1, b->max_length);
+  if (items > kKvTickets) {
+    p.split = (len + 127) / 128 * 128;
+    p.splits = 1;
+  } else {
+    const long long want = std::max(1ll, (4ll * sms + items - 1) / items);
+    p.split = std::clamp((int)((len + want - 1) / want + 127) / 128 * 128, kMinSplit, kMaxSplit);
+    p.splits = (len + p.split - 1) / p.split;
+  }
+  p.part_floats = p.splits > 1 ? (size_t)items * p.splits * p.row_tile * (c->dim + 2) : 0;
+  return p;
+}
+
+// At least plan_of's part_floats, and nondecreasing in the batch's sizes: items * splits
+// is at most 4 sms + 2 items where the items alone set the parts' length, items *
+// ceil(len / kMaxSplit) where that does.
+size_t part_floats_bound(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int sms) {
+  const long long rows = (long long)std::max(1, b->max_new) * (q_heads / c->heads);
+  const long long items = std::min<long long>(kKvTickets, (long long)std::max(1, b->batch) * c->heads * ((rows + 7) / 8));
+  const long long len = std::max(1, b->max_length);
+  return (size_t)(std::max(4ll * sms + 2 * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2));
+}
+
+int device_sms(int* sms) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_say(e, "cudaGetDevice");
+  *sms = sm_count_of(dev);
+  return *sms ? FS_OK : say(FS_ECUDA, "device query failed");
+}
+
+int check_workspace(const void* ws, int64_t bytes, int64_t need) {
+  if (!ws) return say(FS_EINVAL, "workspace is NULL");
+  if (!aligned(ws, 256)) return say(FS_EINVAL, "workspace is not 256-byte aligned");
+  if (bytes < need)
+    return say(FS_EINVAL, "workspace of %lld bytes is less than the %lld this call needs", (long long)bytes,
+               (long long)need);
+  return FS_OK;
+}
+
+}  // namespace
+
+int kv_tensor_map(CUtensorMap* m, const fs_kv_cache& c, const void* base, int rows) {
+  const EncodeTiled enc = encode_tiled();
+  if (!enc) return say(FS_ECUDA, "the driver has no cuTensorMapEncodeTiled");
+  const cuuint64_t dims[4] = {(cuuint64_t)c.dim, (cuuint64_t)c.page_tokens, (cuuint64_t)c.heads, (cuuint64_t)c.pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)c.token_stride, (cuuint64_t)c.head_stride, (cuuint64_t)c.page_stride};
+  const cuuint32_t box[4] = {(cuuint32_t)c.dim, (cuuint32_t)rows, 1, 1}, step[4] = {1, 1, 1, 1};
+  const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box, step,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         c.dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? FS_OK : say(FS_ECUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+}
+
+}  // namespace fs
+
+using namespace fs;
+
+extern "C" int fs_kv_workspace_bytes(const fs_kv_cache* cache, const fs_kv_batch* batch, int32_t q_heads,
+                                     int64_t* bytes) {
+  if (!bytes) return say(FS_EINVAL, "bytes is NULL");
+  if (int rc = check_cache(cache)) return rc;
+  fs_kv_batch b{};
+  if (!batch) return say(FS_EINVAL, "batch is NULL");
+  b = *batch;
+  b.page_table = b.length = b.q_start = reinterpret_cast<const int32_t*>(16);  // (sizes alone are looked at)
+  if (int rc = check_batch(cache, &b, q_heads)) return rc;
+  if (q_heads % cache->heads) return say(FS_EINVAL, "q_heads = %d is not a multiple of %d heads", q_heads, cache->heads);
+  int sms = 0;
+  if (int rc = device_sms(&sms)) return rc;
+  *bytes = (int64_t)(kKvPartAt + 4 * part_floats_bound(cache, &b, q_heads, sms));
+  return FS_OK;
+}
+
+extern "C" int fs_kv_append(const fs_kv_cache* cache, const fs_kv_batch* batch, const fs_kv_new* in, void* workspace,
+                            int64_t workspace_bytes, void* cuda_stream) {
+  if (int rc = check_cache(cache)) return rc;
+  if (!in) return say(FS_EINVAL, "rows is NULL");
+  const bool with_q = in->q.data || in->q_out.data;
+  if (int rc = check_batch(cache, batch, with_q ? in->q_heads : 1)) return rc;
+  if (in->dtype != FS_KV_BF16 && in->dtype != FS_KV_FP16) return say(FS_EINVAL, "dtype = %d is not FS_KV_BF16 or FS_KV_FP16", in->dtype);
+  if (in->rot < 0 || in->rot % 8 || in->rot > cache->dim)
+    return say(FS_EINVAL, "rot = %d must be a multiple of 8 in [0, %d]", in->rot, cache->dim);
+  if (in->interleaved != 0 && in->interleaved != 1) return say(FS_EINVAL, "interleaved = %d is not 0 or 1", in->interleaved);
+  if (int rc = check_workspace(workspace, workspace_bytes, kKvPartAt)) return rc;
+  if (batch->batch == 0 || batch->tokens == 0 || batch->max_new == 0) return FS_OK;
+  if (in->rot) {
+    if (!in->cos || !in->sin) return say(FS_EINVAL, "cos / sin is NULL with rot = %d", in->rot);
+    if (!aligned(in->cos, 16) || !aligned(in->sin, 16)) return say(FS_EINVAL, "cos / sin are not 16-byte aligned");
+    if (in->angle_rows < 1) return say(FS_EINVAL, "angle_rows = %d < 1", in->angle_rows);
+  }
+  if (int rc = check_rows(in->k, "k")) return rc;
+  if (int rc = check_rows(in->v, "v")) return rc;
+  if (with_q) {
+    if (int rc = check_rows(in->q, "q")) return rc;
+    if (int rc = check_rows(in->q_out, "q_out")) return rc;
+  }
+  KvAppendArgs a{};
+  a.v = view_of(cache, batch, cache->heads, workspace);
+  a.kc = static_cast<uint8_t*>(cache->k);
+  a.vc = static_cast<uint8_t*>(cache->v);
+  a.page_stride = cache->page_stride;
+  a.head_stride = cache->head_stride;
+  a.token_stride = cache->token_stride;
+  a.k = in->k.data, a.k_token = in->k.token_stride, a.k_head = in->k.head_stride;
+  a.vals = in->v.data, a.v_token = in->v.token_stride, a.v_head = in->v.head_stride;
+  a.q = with_q ? in->q.data : nullptr, a.q_token = in->q.token_stride, a.q_head = in->q.head_stride;
+  a.q_out = in->q_out.data, a.o_token = in->q_out.token_stride, a.o_head = in->q_out.head_stride;
+  a.cos = in->cos, a.sin = in->sin;
+  a.rot = in->rot, a.angle_rows = in->angle_rows, a.interleaved = in->interleaved, a.q_heads = in->q_heads;
+  const int P = cache->page_tokens;
+  const int pieces = (batch->max_new + P - 2) / P + 1;  // pages that max_new tokens can touch
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const bool h = in->dtype == FS_KV_FP16;
+  const cudaError_t e = cache->dim == 128 ? (h ? launch_append<128, __half>(a, pieces, s) : launch_append<128, __nv_bfloat16>(a, pieces, s))
+                                          : (h ? launch_append<64, __half>(a, pieces, s) : launch_append<64, __nv_bfloat16>(a, pieces, s));
+  return e == cudaSuccess ? FS_OK : cuda_say(e, "launch (fs_kv_append)");
+}
+
+extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, const fs_kv_query* qu, void* workspace,
+                            int64_t workspace_bytes, void* cuda_stream) {
+  if (int rc = check_cache(cache)) return rc;
+  if (!qu) return say(FS_EINVAL, "query is NULL");
+  if (int rc = check_batch(cache, batch, qu->q_heads)) return rc;
+  if (qu->q_heads % cache->heads) return say(FS_EINVAL, "q_heads = %d is not a multiple of %d heads", qu->q_heads, cache->heads);
+  if (qu->dtype != FS_KV_BF16 && qu->dtype != FS_KV_FP16) return say(FS_EINVAL, "dtype = %d is not FS_KV_BF16 or FS_KV_FP16", qu->dtype);
+  if (!(std::fabs(qu->scale) < INFINITY)) return say(FS_EINVAL, "scale is not finite");
+  if (qu->window < 0) return say(FS_EINVAL, "window = %d < 0", qu->window);
+  if (batch->batch == 0 || batch->tokens == 0 || batch->max_new == 0) return check_workspace(workspace, workspace_bytes, kKvPartAt);
+  if (int rc = check_rows(qu->q, "q")) return rc;
+  if (int rc = check_rows(qu->out, "out")) return rc;
+  int sms = 0;
+  if (int rc = device_sms(&sms)) return rc;
+  const KvPlan p = plan_of(cache, batch, qu->q_heads, sms);
+  if (int rc = check_workspace(workspace, workspace_bytes, (int64_t)(kKvPartAt + 4 * p.part_floats))) return rc;
+  if ((long long)p.row_blocks * cache->heads > 65535)
+    return say(FS_EINVAL, "max_new = %d: too many rows for one call", batch->max_new);
+
+  KvAttendArgs a{};
+  a.v = view_of(cache, batch, qu->q_heads, workspace);
+  a.q = qu->q.data, a.q_token = qu->q.token_stride, a.q_head = qu->q.head_stride;
+  a.out = qu->out.data, a.out_token = qu->out.token_stride, a.out_head = qu->out.head_stride;
+  a.scale_log2 = qu->scale * 1.44269504f;
+  a.window = qu->window;
+  a.split = p.split;
+  a.min_rows = 0, a.max_rows = INT_MAX;
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kKvPartAt);
+  a.ticket = reinterpret_cast<unsigned*>(static_cast<char*>(workspace) + kKvTicketAt);
+  CUtensorMap mk, mv;
+  const int box = std::min(32, cache->page_tokens);
+  if (int rc = kv_tensor_map(&mk, *cache, cache->k, box)) return rc;
+  if (int rc = kv_tensor_map(&mv, *cache, cache->v, box)) return rc;
+  const cudaError_t e = launch_kv_decode(mk, mv, a, cache->dim, qu->dtype, p.row_tile, p.row_blocks, p.splits,
+                                         static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? FS_OK : cuda_say(e, "launch (fs_kv_attend)");
+}
+
+extern "C" int fs_kv_check(void* workspace, void* cuda_stream) {
+  if (int rc = check_workspace(workspace, kKvPartAt, kKvPartAt)) return rc;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  uint32_t st = 0;
+  cudaError_t e = cudaMemcpyAsync(&st, workspace, 4, cudaMemcpyDeviceToHost, s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e != cudaSuccess) return cuda_say(e, "synchronize (fs_kv_check)");
+  if (!st) return FS_OK;
+  e = cudaMemsetAsync(workspace, 0, kKvPartAt, s);  // a wait that ran out leaves tickets behind
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e != cudaSuccess) return cuda_say(e, "clear (fs_kv_check)");
+  if (st & ST_TIMEOUT) return say(FS_ETIMEOUT, "a device wait timed out (status 0x%x)", st);
+  return say(FS_EDEVICE, "%s%s%s%s(status 0x%x)", st & KV_ST_PAGE ? "a page id outside the cache; " : "",
+             st & KV_ST_BATCH ? "length or q_start out of the batch's bounds; " : "",
+             st & KV_ST_VALUE ? "a NaN in keys or values; " : "",
+             st & KV_ST_ANGLE ? "a position beyond the rows of cos / sin; " : "", st);
+}

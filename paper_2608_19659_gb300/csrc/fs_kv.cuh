@@ -1,0 +1,135 @@
+// Shared parts of the cache operators (fs_kv.cu, fs_kv_decode.cu, fs_kv_chunk.cu).
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "fs_internal.cuh"
+
+namespace fs {
+
+// Bits of a cache workspace's status word besides ST_TIMEOUT.
+enum : uint32_t {
+  KV_ST_PAGE = 0x100u,    // a page id outside the cache
+  KV_ST_BATCH = 0x200u,   // q_start or length out of order, or beyond the batch's bounds
+  KV_ST_VALUE = 0x400u,   // a NaN among the keys or values of an append (stored as 0)
+  KV_ST_ANGLE = 0x800u,   // a position beyond the rows of cos / sin
+};
+
+// The workspace: status word, tickets (zero between calls), partial results.
+constexpr int kKvTickets = 8192;
+constexpr size_t kKvTicketAt = 256;
+constexpr size_t kKvPartAt = kKvTicketAt + 4 * (size_t)kKvTickets;
+
+// What every kernel reads of the cache and the batch.
+struct KvView {
+  int pages, heads, log_page, batch, tokens, max_new, table_stride, group;  // group: query heads per key head
+  const float *k_scale, *v_scale;
+  const int *page_table, *length, *q_start;
+  uint32_t* status;
+};
+
+struct KvAttendArgs {
+  KvView v;
+  const void* q;
+  void* out;
+  long long q_token, q_head, out_token, out_head;  // strides, elements
+  float scale_log2;  // scale * log2(e)
+  int window;        // 0: none
+  int split;         // tokens per part of the cache axis
+  int min_rows, max_rows;  // sequences with rows outside (min_rows, max_rows] are another kernel's
+  float* part;       // partial results
+  unsigned* ticket;
+};
+
+// One sequence of the batch as a kernel may use it: ranges checked, so that no
+// later index leaves its array whatever the batch's device arrays hold.
+struct KvSeq {
+  int len, first, count;  // tokens cached, first row of q, rows of q
+};
+
+__device__ __forceinline__ bool kv_seq(const KvView& v, int b, KvSeq& s) {
+  s.len = v.length[b];
+  s.first = v.q_start[b];
+  s.count = v.q_start[b + 1] - s.first;
+  const bool ok = s.len >= 0 && (long long)s.len <= ((long long)v.table_stride << v.log_page) && s.first >= 0 &&
+                  s.count >= 0 && s.count <= v.max_new && s.first <= v.tokens - s.count;
+  return ok;
+}
+
+__device__ __forceinline__ void kv_flag(const KvView& v, uint32_t bit) { atomicOr(v.status, bit); }
+
+// Page id `i` of sequence b, or 0 (flagged) where the table holds none of the cache's.
+__device__ __forceinline__ int kv_page(const KvView& v, int b, int i) {
+  const int g = v.page_table[(long long)b * v.table_stride + i];
+  if ((unsigned)g < (unsigned)v.pages) return g;
+  kv_flag(v, KV_ST_PAGE);
+  return 0;
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Two e4m3 codes (the low or high half of w) as two halves; exact.
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t w) {
+  uint32_t r;
+  asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %1;\n cvt.rn.f16x2.e4m3x2 %0, lo;\n}" : "=r"(r) : "r"(w));
+  return r;
+}
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2_hi(uint32_t w) {
+  uint32_t r;
+  asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %1;\n cvt.rn.f16x2.e4m3x2 %0, hi;\n}" : "=r"(r) : "r"(w));
+  return r;
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+template <typename T>
+struct Elem;
+template <>
+struct Elem<__nv_bfloat16> {
+  static __device__ __forceinline__ float2 two(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+  }
+};
+template <>
+struct Elem<__half> {
+  static __device__ __forceinline__ float2 two(uint32_t w) {
+    __half2 h;
+    memcpy(&h, &w, 4);
+    return __half22float2(h);
+  }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) { return pack_f16(a, b); }
+};
+
+// A row's power of two: 2^-e with e the exponent of its largest magnitude, so that the
+// row times it lies in [-2, 2] and rounds to half precision without overflow. (A bf16
+// row's values keep their 8 bits there unless they are under 2^-14 of its largest.)
+__device__ __forceinline__ int row_exponent(float amax) {
+  const int e = (int)((__float_as_uint(amax) >> 23) & 255u) - 127;
+  return min(max(e, -126), 126);
+}
+__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126..127
+
+// A tensor map of a cache tensor: [pages][heads][page tokens][dim] bytes in tiles of
+// `rows` tokens of one (page, head), swizzled over its rows.
+int kv_tensor_map(CUtensorMap* m, const fs_kv_cache& c, const void* base, int rows);
+
+cudaError_t launch_kv_decode(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int dim, int dtype,
+                             int row_tile, int row_blocks, int splits, cudaStream_t s);
+
+}  // namespace fs

@@ -1,0 +1,485 @@
+// Attention of a few rows over the paged 8-bit cache (single tokens, proposals).
+//
+// With at most 16 rows a key head (new tokens x query heads of its group) the call
+// is bound by reading the cache: 2 dim bytes a token and key head. The work is cut into
+// items (sequence, key head, tile of rows) and each item's cache axis into parts, one
+// block each; the last block of an item to finish joins its parts (fixed order: results
+// do not depend on which that is).
+//
+// A warp of the block takes every fourth tile of 32 tokens. Its lane 0 keeps kStages
+// tiles of keys and values on their way into the warp's own ring (tensor-map copies of
+// 16 or 32 tokens of one page, swizzled, so that the reads below meet no bank twice);
+// no block-wide barrier is met before the end. Per 16 tokens:
+//   S^T [16 tokens x rows]  = K [16 x dim] Q^T          (the codes, exact in half precision)
+//   O^T [dim x rows]       += V^T [dim x 16] P^T         (P rounded to half precision)
+// with m16n8k16 products: tokens and dimensions fill the 16 rows of the instruction, the
+// attention rows its 8 columns, so one query head costs no more padding than eight.
+// tcgen05 has nothing to add here: its smallest tile is 128 rows high, and its operands
+// would have to pass through shared memory once more after the conversion.
+// The scale of a page's keys multiplies S, that of its values P (relative to the largest
+// met so far, v_ref, so that half precision holds the product).
+#include "fs_kv.cuh"
+
+namespace fs {
+namespace {
+
+constexpr int kWarps = 4, kStages = 3, kTile = 32;
+constexpr float kUp = 16384.f;  // probability * page scale / v_ref, <= 1, times this: 28 binades of normal halves
+
+__device__ __forceinline__ void tma_tile(void* dst, const CUtensorMap* m, int token, int head, int page, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+          smem_u32(dst)),
+      "l"(m), "r"(0), "r"(token), "r"(head), "r"(page), "r"(smem_u32(bar))
+      : "memory");
+}
+
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+// Shared memory: the warps' rings of (keys, values) tiles; after the last tile the same
+// bytes hold the warps' results.
+template <int D>
+constexpr size_t decode_smem() {
+  return (size_t)kWarps * kStages * 2 * kTile * D + 1024;
+}
+
+template <int D, int NT, typename T>
+__global__ void __launch_bounds__(kWarps * 32)
+    k_kv_decode(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const KvAttendArgs a) {
+  constexpr int kRows = 8 * NT;
+  constexpr int kSteps = D / 16;   // products along the dimensions of a key
+  constexpr int kMt = D / 16;      // 16-dimension tiles of O^T
+  constexpr int kChunk = D / 8;    // dimensions of a value that one lane group holds
+  constexpr int kTileBytes = kTile * D;
+  extern __shared__ unsigned char raw[];
+  unsigned char* ring = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+  __shared__ uint64_t bars[kWarps][kStages];
+  __shared__ float sm_m[kWarps][kRows], sm_l[kWarps][kRows];
+  __shared__ unsigned sm_last;
+
+  const KvView& v = a.v;
+  const int part = blockIdx.x, b = blockIdx.z;
+  const int row_blocks = gridDim.y / v.heads;
+  const int h = blockIdx.y / row_blocks, rb = blockIdx.y % row_blocks;
+  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tid = lane & 3;
+
+  KvSeq s;
+  if (!kv_seq(v, b, s)) {
+    if (threadIdx.x == 0 && part == 0) kv_flag(v, KV_ST_BATCH);
+    return;
+  }
+  const int rows = s.count * v.group;
+  const int r0 = rb * kRows;
+  if (r0 >= rows || rows <= a.min_rows || rows > a.max_rows) return;
+  const int r_end = min(rows, r0 + kRows);
+  // keys that some row of the tile sees: [kv_lo, kv_hi)
+  const int pos0 = s.len - s.count + r0 / v.group, pos1 = s.len - s.count + (r_end - 1) / v.group;
+  const int kv_hi = max(pos1 + 1, 0);
+  const int kv_lo = a.window ? max(pos0 - a.window + 1, 0) : 0;
+  const int begin = kv_lo & ~(kTile - 1);
+  const int n_parts = max(1, (kv_hi - begin + a.split - 1) / a.split);
+  if (n_parts > (int)gridDim.x) {  // a length beyond max_length
+    if (threadIdx.x == 0 && part == 0) kv_flag(v, KV_ST_BATCH);
+    return;
+  }
+  if (part >= n_parts) return;
+  const int c0 = begin + part * a.split, c1 = min(c0 + a.split, kv_hi);
+  const int n_tiles = max(0, (c1 - c0 + kTile - 1) / kTile);
+  const int my_tiles = w < n_tiles ? (n_tiles - w + kWarps - 1) / kWarps : 0;
+
+  if (lane == 0)
+    for (int i = 0; i < kStages; ++i) mbar_init(&bars[w][i], 1);
+  __syncwarp();
+
+  unsigned char* my_ring = ring + w * (kStages * 2 * kTileBytes);
+  // pages and scales of this warp's tiles, 32 tiles at a time, a tile a lane
+  int pg0 = 0, pg1 = 0;
+  float ks0 = 0.f, ks1 = 0.f, vs0 = 0.f, vs1 = 0.f;
+  const bool half_tiles = v.log_page == 4;
+  auto load_pages = [&](int i0) {
+    const int i = i0 + lane;
+    pg0 = pg1 = 0;
+    ks0 = ks1 = vs0 = vs1 = 0.f;
+    if (i < my_tiles) {
+      const int t = c0 + (w + i * kWarps) * kTile;
+      pg0 = pg1 = kv_page(v, b, t >> v.log_page);
+      if (half_tiles && t + 16 < s.len) pg1 = kv_page(v, b, (t + 16) >> v.log_page);
+    }
+  };
+  auto load_scales = [&](int i0) {
+    if (i0 + lane < my_tiles) {
+      const long long at0 = (long long)pg0 * v.heads + h, at1 = (long long)pg1 * v.heads + h;
+      ks0 = v.k_scale[at0], vs0 = v.v_scale[at0];
+      ks1 = ks0, vs1 = vs0;
+      if (pg1 != pg0) ks1 = v.k_scale[at1], vs1 = v.v_scale[at1];
+    }
+  };
+  auto issue = [&](int i, int p0, int p1) {  // lane 0: tile i into its stage
+    const int st = i % kStages, t = c0 + (w + i * kWarps) * kTile, slot = t & ((1 << v.log_page) - 1);
+    unsigned char* kd = my_ring + st * (2 * kTileBytes);
+    uint64_t* bar = &bars[w][st];
+    mbar_expect_tx(bar, 2 * kTileBytes);
+    tma_tile(kd, &mk, slot, h, p0, bar);
+    tma_tile(kd + kTileBytes, &mv, slot, h, p0, bar);
+    if (half_tiles) {
+      tma_tile(kd + kTileBytes / 2, &mk, 0, h, p1, bar);
+      tma_tile(kd + kTileBytes + kTileBytes / 2, &mv, 0, h, p1, bar);
+    }
+  };
+
+  load_pages(0);
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) {
+    const int p0 = __shfl_sync(~0u, pg0, i), p1 = __shfl_sync(~0u, pg1, i);
+    if (lane == 0 && i < my_tiles) issue(i, p0, p1);
+  }
+  load_scales(0);
+
+  // queries: row gid of each tile of 8 rows, in the order that the codes come in
+  uint32_t qf[NT][kSteps][2];
+  float cq[NT][2];  // of rows 2 tid, 2 tid + 1: the row's power of two, the scale, log2(e)
+  int hi_lim[NT][2], lo_lim[NT][2];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int r = r0 + n * 8 + gid;
+    float f[kSteps * 4];
+    float amax = 0.f;
+    if (r < r_end) {
+      const T* q = static_cast<const T*>(a.q) + (long long)(s.first + r / v.group) * a.q_token +
+                   (h * v.group + r % v.group) * a.q_head;
+#pragma unroll
+      for (int c = 0; c < kSteps / 4; ++c) {
+        const uint4* at = reinterpret_cast<const uint4*>(q + (tid * (kSteps / 4) + c) * 16);
+        const uint4 x = at[0], y = at[1];
+        const uint32_t u[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 z = Elem<T>::two(u[i]);
+          f[c * 16 + 2 * i] = z.x, f[c * 16 + 2 * i + 1] = z.y;
+          amax = fmaxf(amax, fmaxf(fabsf(z.x), fabsf(z.y)));
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kSteps * 4; ++i) f[i] = 0.f;
+    }
+    amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
+    amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 2));
+    const int e = row_exponent(amax);
+    const float down = exp2_int(-e);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      qf[n][i][0] = pack_f16(f[4 * i] * down, f[4 * i + 1] * down);
+      qf[n][i][1] = pack_f16(f[4 * i + 2] * down, f[4 * i + 3] * down);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      cq[n][j] = a.scale_log2 * exp2_int(__shfl_sync(~0u, e, (2 * tid + j) * 4));
+      const int rj = r0 + n * 8 + 2 * tid + j;
+      const int pos = s.len - s.count + rj / v.group;
+      hi_lim[n][j] = rj < r_end ? pos : -1;
+      lo_lim[n][j] = a.window ? pos - a.window + 1 : 0;
+    }
+  }
+  // tiles inside [full_lo, full_hi) are seen whole by every row
+  const int full_hi = pos0 + 1;
+  const int full_lo = a.window ? pos1 - a.window + 1 : 0;
+
+  float o[kMt][NT][4];
+  float m[NT][2], l[NT][2], v_ref = 0.f;
+#pragma unroll
+  for (int j = 0; j < kMt; ++j)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[j][n][i] = 0.f;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) m[n][0] = m[n][1] = -INFINITY, l[n][0] = l[n][1] = 0.f;
+
+  bool ok = true;
+  int done = 0;
+  for (int i = 0; i < my_tiles; done = ++i) {
+    if ((i & 31) == 0) {
+      if (i) {
+        // (tiles already under way took their pages from the lists of the round before)
+        load_pages(i);
+        load_scales(i);
+      }
+      float top = fmaxf(vs0, vs1);
+#pragma unroll
+      for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+      if (top > v_ref) {
+        const float f = v_ref / top;
+        v_ref = top;
+#pragma unroll
+        for (int j = 0; j < kMt; ++j)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[j][n][k] *= f;
+      }
+    }
+    const int st = i % kStages, t0 = c0 + (w + i * kWarps) * kTile;
+    const float inv_ref = v_ref > 0.f ? kUp / v_ref : 0.f;
+    const float ks[2] = {__shfl_sync(~0u, ks0, i & 31), __shfl_sync(~0u, ks1, i & 31)};
+    const float vs[2] = {__shfl_sync(~0u, vs0, i & 31) * inv_ref, __shfl_sync(~0u, vs1, i & 31) * inv_ref};
+    ok = mbar_wait(&bars[w][st], (i / kStages) & 1, kWaitLimitNs);
+    if (!__all_sync(~0u, ok)) break;
+    const unsigned char* kt = my_ring + st * (2 * kTileBytes);
+    const unsigned char* vt = kt + kTileBytes;
+
+    float sc[2][NT][4];
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sc[mt][n][k] = 0.f;
+#pragma unroll
+      for (int c = 0; c < kSteps / 4; ++c) {
+        // 16 codes of tokens gid and gid + 8
+        const int chunk = D == 128 ? (2 * tid + c) ^ gid : tid ^ (gid >> 1);
+        const unsigned char* at = kt + (mt * 16 + gid) * D + chunk * 16;
+        const uint4 x = *reinterpret_cast<const uint4*>(at), y = *reinterpret_cast<const uint4*>(at + 8 * D);
+        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t a0 = e4m3x2_to_f16x2(xs[k]), a2 = e4m3x2_to_f16x2_hi(xs[k]);
+          const uint32_t a1 = e4m3x2_to_f16x2(ys[k]), a3 = e4m3x2_to_f16x2_hi(ys[k]);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma16816(sc[mt][n], a0, a1, a2, a3, qf[n][c * 4 + k][0], qf[n][c * 4 + k][1]);
+        }
+      }
+    }
+    const bool whole = t0 >= full_lo && t0 + kTile <= full_hi;
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float x = sc[mt][n][k] * (ks[mt] * cq[n][k & 1]);
+          if (!whole) {
+            const int t = t0 + mt * 16 + gid + (k >> 1) * 8;
+            if (t > hi_lim[n][k & 1] || t < lo_lim[n][k & 1]) x = -INFINITY;
+          }
+          sc[mt][n][k] = x;
+        }
+    // running maximum and sum; a row without a key yet keeps -infinity, and 0 in its place
+    uint32_t pf[2][NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float mx[2], corr[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float x = fmaxf(fmaxf(sc[0][n][j], sc[0][n][j + 2]), fmaxf(sc[1][n][j], sc[1][n][j + 2]));
+        x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+        x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
+        x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
+        const float m_new = fmaxf(m[n][j], x);
+        mx[j] = m_new == -INFINITY ? 0.f : m_new;
+        corr[j] = ex2(m[n][j] - mx[j]);
+        m[n][j] = m_new;
+        l[n][j] *= corr[j];
+      }
+      if (__any_sync(~0u, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+        for (int j = 0; j < kMt; ++j) {
+          o[j][n][0] *= corr[0], o[j][n][2] *= corr[0];
+          o[j][n][1] *= corr[1], o[j][n][3] *= corr[1];
+        }
+      }
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float p0 = ex2(sc[mt][n][2 * k] - mx[0]), p1 = ex2(sc[mt][n][2 * k + 1] - mx[1]);
+          l[n][0] += p0, l[n][1] += p1;
+          pf[mt][n][k] = transpose8x8(pack_f16(p0 * vs[mt], p1 * vs[mt]));
+        }
+    }
+    const bool tail = t0 + kTile > s.len;
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+      // codes of tokens 2 tid, 2 tid + 1, 2 tid + 8, 2 tid + 9: kChunk dimensions from gid * kChunk on
+      uint32_t vw[4][kChunk / 4];
+#pragma unroll
+      for (int i2 = 0; i2 < 4; ++i2) {
+        const int t = mt * 16 + 2 * tid + (i2 & 1) + (i2 >> 1) * 8;
+        if constexpr (D == 128) {
+          const uint4 x = *reinterpret_cast<const uint4*>(vt + t * D + ((gid ^ (t & 7)) * 16));
+          vw[i2][0] = x.x, vw[i2][1] = x.y, vw[i2][2] = x.z, vw[i2][3] = x.w;
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(vt + t * D + (((gid >> 1) ^ ((t >> 1) & 3)) * 16) + (gid & 1) * 8);
+          vw[i2][0] = x.x, vw[i2][1] = x.y;
+        }
+        if (tail && t0 + t >= s.len) {  // slots without a token may hold NaN codes
+#pragma unroll
+          for (int k = 0; k < kChunk / 4; ++k) vw[i2][k] = 0;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kChunk / 4; ++k) {
+        const uint32_t u0 = __byte_perm(vw[0][k], vw[1][k], 0x5140), u1 = __byte_perm(vw[0][k], vw[1][k], 0x7362);
+        const uint32_t x0 = __byte_perm(vw[2][k], vw[3][k], 0x5140), x1 = __byte_perm(vw[2][k], vw[3][k], 0x7362);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          mma16816(o[2 * k][n], e4m3x2_to_f16x2(u0), e4m3x2_to_f16x2_hi(u0), e4m3x2_to_f16x2(x0), e4m3x2_to_f16x2_hi(x0),
+                   pf[mt][n][0], pf[mt][n][1]);
+          mma16816(o[2 * k + 1][n], e4m3x2_to_f16x2(u1), e4m3x2_to_f16x2_hi(u1), e4m3x2_to_f16x2(x1),
+                   e4m3x2_to_f16x2_hi(x1), pf[mt][n][0], pf[mt][n][1]);
+        }
+      }
+    }
+    __syncwarp();  // every lane has read the stage
+    // the next tile of this stage; its pages are in the lists of its round of 32
+    const int nx = i + kStages;
+    int p0 = __shfl_sync(~0u, pg0, nx & 31), p1 = __shfl_sync(~0u, pg1, nx & 31);
+    if (lane == 0 && nx < my_tiles) {
+      if ((nx & ~31) != (i & ~31)) {
+        const int t = c0 + (w + nx * kWarps) * kTile;
+        p0 = p1 = kv_page(v, b, t >> v.log_page);
+        if (half_tiles && t + 16 < s.len) p1 = kv_page(v, b, (t + 16) >> v.log_page);
+      }
+      issue(nx, p0, p1);
+    }
+  }
+  if (!__all_sync(~0u, ok)) {
+    // give up: say so, and wait (with the same limit) for the copies still under way
+    if (lane == 0) kv_flag(v, ST_TIMEOUT);
+    for (int i = done; i < min(done + kStages, my_tiles); ++i)
+      mbar_wait(&bars[w][i % kStages], (i / kStages) & 1, kWaitLimitNs);
+  }
+
+  // ---- join the warps
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) l[n][j] += __shfl_xor_sync(~0u, l[n][j], d);
+      if (gid == 0) sm_m[w][n * 8 + 2 * tid + j] = m[n][j], sm_l[w][n * 8 + 2 * tid + j] = l[n][j];
+    }
+  __syncthreads();  // every warp has left its ring
+  float* ow = reinterpret_cast<float*>(ring);  // [kWarps][kRows][D]
+  const float down = v_ref * (1.f / kUp);
+#pragma unroll
+  for (int j = 0; j < kMt; ++j)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        // rows gid, gid + 8 of tile j are dimensions gid * kChunk + 2 j, + 1
+        const int r = n * 8 + 2 * tid + k;
+        *reinterpret_cast<float2*>(ow + ((w * kRows + r) * D + gid * kChunk + 2 * j)) =
+            make_float2(o[j][n][k] * down, o[j][n][k + 2] * down);
+      }
+  __syncthreads();
+
+  const int n_rows = r_end - r0;
+  const long long item = ((long long)b * gridDim.y + blockIdx.y);
+  float* part_o = a.part + (item * gridDim.x + part) * (kRows * (D + 2));
+  float* part_ml = part_o + kRows * D;
+  auto write_out = [&](int r, int d, float4 x, float lsum) {
+    const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+    const int rr = r0 + r;
+    T* to = static_cast<T*>(a.out) + (long long)(s.first + rr / v.group) * a.out_token +
+            (h * v.group + rr % v.group) * a.out_head + d;
+    *reinterpret_cast<uint2*>(to) = make_uint2(Elem<T>::pack(x.x * inv, x.y * inv), Elem<T>::pack(x.z * inv, x.w * inv));
+  };
+  for (int u = threadIdx.x; u < n_rows * (D / 4); u += kWarps * 32) {
+    const int r = u / (D / 4), d = u % (D / 4) * 4;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) top = fmaxf(top, sm_m[i][r]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    float lsum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const float f = ex2(sm_m[i][r] - base);
+      const float4 y = *reinterpret_cast<const float4*>(ow + (i * kRows + r) * D + d);
+      lsum = fmaf(sm_l[i][r], f, lsum);
+      x.x = fmaf(y.x, f, x.x), x.y = fmaf(y.y, f, x.y), x.z = fmaf(y.z, f, x.z), x.w = fmaf(y.w, f, x.w);
+    }
+    if (n_parts == 1) {
+      write_out(r, d, x, lsum);
+    } else {
+      *reinterpret_cast<float4*>(part_o + r * D + d) = x;
+      if (d == 0) *reinterpret_cast<float2*>(part_ml + 2 * r) = make_float2(top, lsum);
+    }
+  }
+  if (n_parts == 1) return;
+
+  // ---- join the parts: the block that takes the last ticket
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const unsigned t = atomicAdd(a.ticket + item, 1u);
+    sm_last = t == (unsigned)n_parts - 1;
+    if (sm_last) a.ticket[item] = 0;  // as it was found
+  }
+  __syncthreads();
+  if (!sm_last) return;
+  __threadfence();
+  const float* parts = a.part + item * gridDim.x * (kRows * (D + 2));
+  for (int u = threadIdx.x; u < n_rows * (D / 4); u += kWarps * 32) {
+    const int r = u / (D / 4), d = u % (D / 4) * 4;
+    float top = -INFINITY, lsum = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < n_parts; ++i) {
+      const float* at = parts + (long long)i * (kRows * (D + 2));
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(at + kRows * D + 2 * r));
+      const float4 y = __ldcg(reinterpret_cast<const float4*>(at + r * D + d));
+      const float m_new = fmaxf(top, ml.x), base = m_new == -INFINITY ? 0.f : m_new;
+      const float f0 = ex2(top - base), f1 = ex2(ml.x - base);
+      top = m_new;
+      lsum = fmaf(lsum, f0, ml.y * f1);
+      x.x = fmaf(x.x, f0, y.x * f1), x.y = fmaf(x.y, f0, y.y * f1);
+      x.z = fmaf(x.z, f0, y.z * f1), x.w = fmaf(x.w, f0, y.w * f1);
+    }
+    write_out(r, d, x, lsum);
+  }
+}
+
+template <int D, int NT, typename T>
+cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int row_blocks, int splits,
+                   cudaStream_t s) {
+  static const cudaError_t limit = raise_smem_limit(reinterpret_cast<const void*>(k_kv_decode<D, NT, T>), decode_smem<D>());
+  if (limit != cudaSuccess) return limit;
+  k_kv_decode<D, NT, T><<<dim3(splits, a.v.heads * row_blocks, a.v.batch), kWarps * 32, decode_smem<D>(), s>>>(mk, mv, a);
+  note_launch();
+  return cudaGetLastError();
+}
+
+template <int D, typename T>
+cudaError_t launch_rows(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int row_tile,
+                        int row_blocks, int splits, cudaStream_t s) {
+  return row_tile == 8 ? launch<D, 1, T>(mk, mv, a, row_blocks, splits, s) : launch<D, 2, T>(mk, mv, a, row_blocks, splits, s);
+}
+
+}  // namespace
+
+cudaError_t launch_kv_decode(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int dim, int dtype,
+                             int row_tile, int row_blocks, int splits, cudaStream_t s) {
+  const bool h = dtype == FS_KV_FP16;
+  if (dim == 128)
+    return h ? launch_rows<128, __half>(mk, mv, a, row_tile, row_blocks, splits, s)
+             : launch_rows<128, __nv_bfloat16>(mk, mv, a, row_tile, row_blocks, splits, s);
+  return h ? launch_rows<64, __half>(mk, mv, a, row_tile, row_blocks, splits, s)
+           : launch_rows<64, __nv_bfloat16>(mk, mv, a, row_tile, row_blocks, splits, s);
+}
+
+}  // namespace fs

@@ -27,7 +27,9 @@ EXPORTS = ("fs_load_model", "fs_update_bounds", "fs_set_floors", "fs_dump_stride
            "fs_certificate", "fs_replay", "fs_check", "fs_launch_count",
            "fs_watchdog_selftest", "fs_free_model", "fs_last_error", "fs_score_candidates_noalloc",
            "fs_timing_enable",
-           "fs_timing_read", "fs_draw_floor")
+           "fs_timing_read", "fs_draw_floor", "fs_kv_workspace_bytes", "fs_kv_append", "fs_kv_attend",
+           "fs_kv_check")
+FS_KV_BF16, FS_KV_FP16 = 0, 1
 
 
 class FleetSieveError(RuntimeError):
@@ -62,6 +64,35 @@ class fs_replay_spec(C.Structure):
                 ("O", C.c_int32), ("S", C.c_int32), ("max_rounds", C.c_int32),
                 ("policy", C.c_int32), ("seed", C.c_uint64), ("truth_cap", C.POINTER(C.c_float)),
                 ("truth_tail", C.POINTER(C.c_float)), ("perm", C.POINTER(C.c_int32))]
+
+
+class fs_kv_cache(C.Structure):
+    _fields_ = [("pages", C.c_int32), ("heads", C.c_int32), ("page_tokens", C.c_int32),
+                ("dim", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("token_stride", C.c_int64)]
+
+
+class fs_kv_batch(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("tokens", C.c_int32), ("max_new", C.c_int32),
+                ("max_length", C.c_int32), ("table_stride", C.c_int32), ("reserved", C.c_int32),
+                ("page_table", C.c_void_p), ("length", C.c_void_p), ("q_start", C.c_void_p)]
+
+
+class fs_kv_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class fs_kv_new(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("q_heads", C.c_int32), ("rot", C.c_int32),
+                ("interleaved", C.c_int32), ("angle_rows", C.c_int32), ("reserved", C.c_int32),
+                ("k", fs_kv_rows), ("v", fs_kv_rows), ("q", fs_kv_rows), ("q_out", fs_kv_rows),
+                ("cos", C.c_void_p), ("sin", C.c_void_p)]
+
+
+class fs_kv_query(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("q_heads", C.c_int32), ("scale", C.c_float),
+                ("window", C.c_int32), ("q", fs_kv_rows), ("out", fs_kv_rows)]
 
 
 ALLOC_DTYPE = np.dtype({"names": ["t_star", "total_gpus", "has_option_mask", "ok", "floors_met",
@@ -119,6 +150,13 @@ def lib():
         L.fs_watchdog_selftest.argtypes = [C.c_int64]
         L.fs_draw_floor.argtypes = [C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.POINTER(C.c_double),
                                     C.POINTER(C.c_int64)]
+        L.fs_kv_workspace_bytes.argtypes = [C.POINTER(fs_kv_cache), C.POINTER(fs_kv_batch), C.c_int32,
+                                            C.POINTER(C.c_int64)]
+        L.fs_kv_append.argtypes = [C.POINTER(fs_kv_cache), C.POINTER(fs_kv_batch), C.POINTER(fs_kv_new),
+                                   C.c_void_p, C.c_int64, C.c_void_p]
+        L.fs_kv_attend.argtypes = [C.POINTER(fs_kv_cache), C.POINTER(fs_kv_batch), C.POINTER(fs_kv_query),
+                                   C.c_void_p, C.c_int64, C.c_void_p]
+        L.fs_kv_check.argtypes = [C.c_void_p, C.c_void_p]
         L.fs_free_model.argtypes = [C.c_void_p]
         L.fs_free_model.restype = None
         L.fs_last_error.restype = C.c_char_p
@@ -486,6 +524,138 @@ def fs_free_model(m: Model) -> None:
 
 def fs_last_error() -> str:
     return lib().fs_last_error().decode(errors="replace")
+
+
+# ---- the serving step of one rank: a paged 8-bit cache and its attention
+
+class KvCache:
+    """A paged cache of keys and values in e4m3 codes, described by the caller's CUDA tensors.
+
+    k, v: [pages, heads, page_tokens, dim] of ``torch.float8_e4m3fn`` (or its bytes, uint8), the
+    last dimension contiguous, both with the same strides (a ``transpose(1, 2)`` view of a cache
+    laid out by token is as good); k_scale, v_scale: contiguous [pages, heads] float32.
+    """
+
+    def __init__(self, k, v, k_scale, v_scale):
+        import torch
+
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
+            raise ValueError("k and v are [pages, heads, page_tokens, dim] with equal strides, the last one 1")
+        for t, name in ((k, "k"), (v, "v")):
+            if t.dtype not in (torch.float8_e4m3fn, torch.uint8):
+                raise ValueError(f"{name} is {t.dtype}, not float8_e4m3fn or uint8")
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t.dtype != torch.float32 or tuple(t.shape) != tuple(k.shape[:2]) or not t.is_contiguous():
+                raise ValueError(f"{name} is a contiguous float32 [pages, heads]")
+        if not k.is_cuda or any(t.device != k.device for t in (v, k_scale, v_scale)):
+            raise ValueError("the cache's tensors are on one CUDA device")
+        self.tensors = (k, v, k_scale, v_scale)
+        self.device, self.heads, self.dim = k.device, k.shape[1], k.shape[3]
+        self.struct = fs_kv_cache(k.shape[0], k.shape[1], k.shape[2], k.shape[3], k.data_ptr(), v.data_ptr(),
+                                  k_scale.data_ptr(), v_scale.data_ptr(), k.stride(0), k.stride(1), k.stride(2))
+
+
+class KvBatch:
+    """The sequences of a call (see fs_kv_batch): page_table [batch, width] (rows contiguous), length
+    [batch] and q_start [batch + 1] int32 CUDA tensors; tokens = q_start[batch], max_new and max_length
+    bounds known on the host. The tensors' contents may change between calls; their storage may not."""
+
+    def __init__(self, page_table, length, q_start, tokens: int, max_new: int, max_length: int):
+        import torch
+
+        n = length.shape[0]
+        if (page_table.dim() != 2 or page_table.shape[0] != n or length.dim() != 1 or q_start.dim() != 1
+                or q_start.shape[0] != n + 1):
+            raise ValueError("page_table [batch, width], length [batch], q_start [batch + 1]")
+        for t, name in ((page_table, "page_table"), (length, "length"), (q_start, "q_start")):
+            if t.dtype != torch.int32 or not t.is_cuda or t.device != length.device or not t.is_contiguous():
+                raise ValueError(f"{name} is a contiguous int32 CUDA tensor, on one device with the others")
+        self.tensors = (page_table, length, q_start)
+        self.device, self.tokens = length.device, int(tokens)
+        self.struct = fs_kv_batch(n, self.tokens, int(max_new), int(max_length), page_table.shape[1], 0,
+                                  page_table.data_ptr(), length.data_ptr(), q_start.data_ptr())
+
+
+class KvWorkspace:
+    """Device memory for calls with this cache and batch, or smaller ones, one after the other."""
+
+    def __init__(self, cache: KvCache, batch: KvBatch, q_heads: int):
+        import torch
+
+        n = C.c_int64()
+        _check(lib().fs_kv_workspace_bytes(C.byref(cache.struct), C.byref(batch.struct), int(q_heads), C.byref(n)))
+        self.tensor = torch.zeros(n.value, dtype=torch.uint8, device=cache.device)
+        self.address, self.bytes = self.tensor.data_ptr(), n.value
+
+
+def _kv_dtype(t) -> int:
+    import torch
+
+    if t.dtype == torch.bfloat16:
+        return FS_KV_BF16
+    if t.dtype == torch.float16:
+        return FS_KV_FP16
+    raise ValueError(f"rows are bfloat16 or float16, not {t.dtype}")
+
+
+def _kv_rows(t, name: str, like, cache: KvCache, batch: KvBatch, heads: int | None) -> fs_kv_rows:
+    if t.dim() != 3 or t.shape[0] != batch.tokens or t.shape[2] != cache.dim or (heads and t.shape[1] != heads):
+        raise ValueError(f"{name} is [tokens = {batch.tokens}, {heads or 'heads'}, {cache.dim}], not {tuple(t.shape)}")
+    if t.dtype != like.dtype or t.device != cache.device or (t.stride(2) != 1 and t.numel()):
+        raise ValueError(f"{name}: want {like.dtype} on {cache.device}, the last dimension contiguous")
+    return fs_kv_rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _kv_stream(stream, device):
+    if stream is not None:
+        return _stream(stream)
+    import torch
+
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def fs_kv_append(cache: KvCache, batch: KvBatch, k, v, cos=None, sin=None, q=None, q_out=None,
+                 interleaved: bool = False, *, workspace: KvWorkspace, stream=None) -> None:
+    """New keys and values [tokens, heads, dim] into the cache, the keys rotated by cos, sin
+    [positions, rot / 2] (None: not rotated); q [tokens, q_heads, dim] rotated alike into q_out.
+    Enqueued on ``stream`` (default: torch's current one)."""
+    a = fs_kv_new(_kv_dtype(k), 0, 0, 1 if interleaved else 0)
+    a.k = _kv_rows(k, "k", k, cache, batch, cache.heads)
+    a.v = _kv_rows(v, "v", k, cache, batch, cache.heads)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if q is not None:
+        a.q = _kv_rows(q, "q", k, cache, batch, None)
+        a.q_out = _kv_rows(q_out, "q_out", k, cache, batch, q.shape[1])
+        a.q_heads = q.shape[1]
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin go together")
+    if cos is not None:
+        if (cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != sin.dtype or "float32" not in str(cos.dtype)
+                or cos.device != cache.device or sin.device != cache.device or not cos.is_contiguous()
+                or not sin.is_contiguous()):
+            raise ValueError("cos and sin are contiguous float32 [positions, rot / 2] on the cache's device")
+        a.rot, a.angle_rows, a.cos, a.sin = 2 * cos.shape[1], cos.shape[0], cos.data_ptr(), sin.data_ptr()
+    _check(lib().fs_kv_append(C.byref(cache.struct), C.byref(batch.struct), C.byref(a), workspace.address,
+                              workspace.bytes, _kv_stream(stream, cache.device)))
+
+
+def fs_kv_attend(cache: KvCache, batch: KvBatch, q, out, scale: float, window: int = 0, *,
+                 workspace: KvWorkspace, stream=None):
+    """out [tokens, q_heads, dim] = attention of the batch's new tokens over their sequences' cached
+    tokens up to their own (the last ``window`` of them; 0: all). Enqueued on ``stream`` (default:
+    torch's current one); returns out."""
+    a = fs_kv_query(_kv_dtype(q), q.shape[1] if q.dim() == 3 else 0, float(scale), int(window),
+                    _kv_rows(q, "q", q, cache, batch, None))
+    a.out = _kv_rows(out, "out", q, cache, batch, q.shape[1])
+    _check(lib().fs_kv_attend(C.byref(cache.struct), C.byref(batch.struct), C.byref(a), workspace.address,
+                              workspace.bytes, _kv_stream(stream, cache.device)))
+    return out
+
+
+def fs_kv_check(workspace: KvWorkspace, stream=None) -> None:
+    """Waits for the stream and raises what the workspace's calls met on the device."""
+    _check(lib().fs_kv_check(workspace.address, _kv_stream(stream, workspace.tensor.device)))
 
 
 def dump_dtype(K: int) -> np.dtype:

@@ -1,0 +1,225 @@
+"""fs_kv_attend against attention in 64 bits over the same codes.
+
+Tolerance, per element: a row's probabilities are rounded to half precision (2^-11 each) and
+carry the rounding of their scores (fp32 sums of dim exact products: 2^-20 of sum |q k| scale, in
+nats, also covers the exponential), so the weighted sum is off by at most
+(2^-10 + 2^-19 sum |q k| scale) sum p |v|; then the result is rounded once to its type."""
+
+import numpy as np
+import pytest
+
+import kv_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"bf16": 2.0**-8, "fp16": 2.0**-11}
+
+
+def on_gpu(torch, fsb, d, hq, dtype, qf, by_token=False):
+    """The inputs on the GPU: caches, batch, queries (float32 values of qf rounded to dtype)."""
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float16
+
+    def codes(x):
+        t = torch.from_numpy(x).cuda()
+        return t.transpose(1, 2).contiguous().transpose(1, 2) if by_token else t
+
+    cache = fsb.KvCache(codes(d["k"]), codes(d["v"]), torch.from_numpy(d["k_scale"]).cuda(),
+                        torch.from_numpy(d["v_scale"]).cuda())
+    T = int(d["q_start"][-1])
+    new = np.diff(d["q_start"])
+    batch = fsb.KvBatch(torch.from_numpy(d["table"]).cuda(), torch.from_numpy(d["length"]).cuda(),
+                        torch.from_numpy(d["q_start"]).cuda(), T, int(new.max()), int(d["length"].max()))
+    q = torch.from_numpy(qf).to(dt).cuda()
+    return cache, batch, q, fsb.KvWorkspace(cache, batch, hq)
+
+
+def check(out, want, mag, dots, eps):
+    tol = (2.0**-10 + 2.0**-19 * dots) * mag + eps * np.abs(want) + 1e-30
+    err = np.abs(out.float().cpu().numpy() - want)
+    assert np.isfinite(out.float().cpu().numpy()).all()
+    assert (err <= tol).all(), float((err / tol).max())
+
+
+def run(torch, fsb, seed, lens, heads, group, dim, page, dtype="bf16", window=0, by_token=False, q_gain=2.0, change=None,
+        garbage=True):
+    rng = np.random.default_rng(seed)
+    d = ref.make(rng, lens, heads, dim, page)
+    if garbage:  # slots without a token hold NaN codes
+        for b, (l, _) in enumerate(lens):
+            if l % page:
+                g = d["table"][b, l // page]
+                d["k"][g, :, l % page:] = 0x7F
+                d["v"][g, :, l % page:] = 0xFF
+    if change:
+        change(d)
+    T, hq = int(d["q_start"][-1]), heads * group
+    cache, batch, q, ws = on_gpu(torch, fsb, d, hq, dtype, (q_gain * rng.standard_normal((T, hq, dim))).astype(np.float32),
+                                 by_token)
+    out = torch.full((T, hq, dim), float("nan"), dtype=q.dtype, device="cuda")
+    scale = dim**-0.5
+    n0 = fsb.fs_launch_count()
+    fsb.fs_kv_attend(cache, batch, q, out, scale, window=window, workspace=ws)
+    fsb.fs_kv_check(ws)
+    assert fsb.fs_launch_count() > n0
+    want, mag, dots = ref.attend(q.float().cpu().numpy(), d["k"], d["v"], d["k_scale"], d["v_scale"], d["table"],
+                                 d["length"], d["q_start"], scale, window)
+    check(out, want, mag, dots, DTYPES[dtype])
+    return out, (cache, batch, q, ws)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim,page", [(128, 16), (128, 64), (64, 16), (64, 32), (128, 128), (64, 128)])
+def test_single_tokens_of_every_length(fsb, cuda, dim, page, dtype):
+    """Lengths at the edges of tiles and pages, an empty slot, all in one batch."""
+    lens = [(l, 1) for l in (1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300)] + [(0, 0), (77, 0), (5, 1)]
+    run(cuda, fsb, 1, lens, 2, 4, dim, page, dtype)
+
+
+@pytest.mark.parametrize("group", [1, 3, 5, 8, 16])
+def test_groups(fsb, cuda, group):
+    run(cuda, fsb, 2, [(200, 1), (1, 1), (513, 1)], 3, group, 128, 32)
+
+
+@pytest.mark.parametrize("new,group", [(2, 4), (5, 8), (9, 1), (17, 3), (40, 8)])
+@pytest.mark.parametrize("window", [0, 1, 7, 100])
+def test_several_tokens_and_windows(fsb, cuda, new, group, window):
+    lens = [(new, new), (new + 1, new), (333, new), (0, 0), (97, max(1, new - 1)), (64 + new, new)]
+    run(cuda, fsb, 3, lens, 2, group, 128, 16, window=window)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("new,length", [(128, 128), (129, 200), (300, 300), (257, 1000), (64, 700)])
+@pytest.mark.parametrize("window", [0, 150])
+def test_chunks(fsb, cuda, dim, new, length, window):
+    lens = [(length, new), (new // 2 + 3, new // 2 + 3), (5, 1), (0, 0), (400, 0)]
+    run(cuda, fsb, 4, lens, 2, 3, dim, 64, window=window)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_chunks_over_every_page_size(fsb, cuda, page, dtype):
+    run(cuda, fsb, 5, [(391, 211), (1030, 97), (140, 140)], 1, 8, 128, page, dtype)
+
+
+def test_one_long_sequence(fsb, cuda):
+    """Many parts of one sequence's cache axis, joined by the last block."""
+    run(cuda, fsb, 6, [(20011, 1)], 1, 8, 128, 64)
+    run(cuda, fsb, 7, [(9000, 3), (17, 2)], 2, 4, 64, 16, window=5000)
+
+
+def test_cache_laid_out_by_token(fsb, cuda):
+    run(cuda, fsb, 8, [(200, 1), (70, 3)], 4, 2, 128, 32, by_token=True)
+    run(cuda, fsb, 8, [(300, 150), (70, 3)], 4, 2, 64, 32, by_token=True)
+
+
+@pytest.mark.parametrize("new", [1, 150])
+def test_strided_rows(fsb, cuda, new):
+    """Queries cut out of a wider projection, results into every other row block."""
+    torch = cuda
+    rng = np.random.default_rng(9)
+    d = ref.make(rng, [(201, new), (new, new)], 2, 128, 32)
+    T, hq = int(d["q_start"][-1]), 6
+    qf = rng.standard_normal((T, hq, 128)).astype(np.float32)
+    cache, batch, q, ws = on_gpu(torch, fsb, d, hq, "bf16", qf)
+    wide = torch.randn(T, hq + 4, 128, device="cuda").to(q.dtype)
+    wide[:, 2:2 + hq] = q
+    held = torch.full((2 * T, hq, 128), 7.0, dtype=q.dtype, device="cuda")
+    fsb.fs_kv_attend(cache, batch, wide[:, 2:2 + hq], held[::2], 0.1, workspace=ws)
+    plain = torch.empty(T, hq, 128, dtype=q.dtype, device="cuda")
+    fsb.fs_kv_attend(cache, batch, q, plain, 0.1, workspace=ws)
+    fsb.fs_kv_check(ws)
+    assert torch.equal(held[::2], plain) and bool((held[1::2] == 7).all())
+    want, mag, dots = ref.attend(q.float().cpu().numpy(), d["k"], d["v"], d["k_scale"], d["v_scale"], d["table"],
+                                 d["length"], d["q_start"], 0.1, 0)
+    check(plain, want, mag, dots, DTYPES["bf16"])
+
+
+@pytest.mark.parametrize("new", [1, 140])
+def test_scales_far_apart(fsb, cuda, new):
+    """Pages whose scales differ by 2^14 either way, some of them 0; values of a page with scale 0 are 0."""
+
+    def change(d):
+        rng = np.random.default_rng(10)
+        for n in ("k_scale", "v_scale"):
+            d[n] *= np.exp2(rng.integers(-7, 8, d[n].shape)).astype(np.float32)
+            d[n][rng.random(d[n].shape) < 0.1] = 0.0
+        d["k_scale"] *= np.float32(2.0**-6)  # (scores that do not pick a single key)
+
+    run(cuda, fsb, 11, [(700, new), (new, new)], 2, 4, 128, 16, change=change)
+
+
+@pytest.mark.parametrize("new", [1, 140])
+@pytest.mark.parametrize("gain", [0.0, 1e-30, 30.0])
+def test_query_magnitudes(fsb, cuda, new, gain):
+    """Zero queries (the mean of the values), tiny ones, and scores of hundreds (a single key counts)."""
+    run(cuda, fsb, 12, [(300, new), (new, new)], 2, 4, 128, 32, q_gain=gain)
+
+
+def test_rows_before_the_first_token_are_zero(fsb, cuda):
+    """More new tokens than length: rows at negative positions see nothing and become 0."""
+    torch = cuda
+    rng = np.random.default_rng(13)
+    for new in (4, 200):
+        d = ref.make(rng, [(3, 3), (50, 1)], 2, 128, 16)
+        d["q_start"] = np.array([0, new, new + 1], np.int32)  # sequence 0: `new` rows, 3 tokens
+        cache, batch, q, ws = on_gpu(torch, fsb, d, 8, "bf16", rng.standard_normal((new + 1, 8, 128)).astype(np.float32))
+        out = torch.full_like(q, float("nan"))
+        fsb.fs_kv_attend(cache, batch, q, out, 0.1, workspace=ws)
+        fsb.fs_kv_check(ws)
+        assert bool((out[: new - 3] == 0).all()) and bool(torch.isfinite(out.float()).all())
+        assert bool((out[new - 3:].float().abs().amax((1, 2)) > 0).all())
+
+
+def test_same_bits_every_time_and_under_a_graph(fsb, cuda):
+    torch = cuda
+    out, (cache, batch, q, ws) = run(torch, fsb, 14, [(5000, 1), (700, 1), (3, 1)], 2, 8, 128, 64)
+    again = torch.empty_like(out)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        fsb.fs_kv_attend(cache, batch, q, again, 128**-0.5, workspace=ws)
+    for _ in range(3):
+        again.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, again)
+
+
+def test_another_stream(fsb, cuda):
+    torch = cuda
+    out, (cache, batch, q, ws) = run(torch, fsb, 15, [(900, 1), (30, 1)], 2, 4, 128, 64)
+    s = torch.cuda.Stream()
+    q2, out2 = torch.empty_like(q), torch.empty_like(out)
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        q2.copy_(q)
+        fsb.fs_kv_attend(cache, batch, q2, out2, 128**-0.5, workspace=ws)
+    fsb.fs_kv_check(ws, s)
+    assert torch.equal(out, out2)
+    fsb.fs_kv_attend(cache, batch, q2, out2.zero_(), 128**-0.5, workspace=ws, stream=torch.cuda.current_stream())
+    fsb.fs_kv_check(ws)
+    assert torch.equal(out, out2)
+
+
+def test_broken_batches_are_reported(fsb, cuda):
+    """Device arrays that break the batch's bounds: the sequence is skipped (or page 0 read in the
+    place of a page the cache does not have), a status is reported, the next call is right."""
+    torch = cuda
+    rng = np.random.default_rng(16)
+    d = ref.make(rng, [(100, 1), (40, 1)], 2, 128, 16)
+    cache, batch, q, ws = on_gpu(torch, fsb, d, 4, "bf16", rng.standard_normal((2, 4, 128)).astype(np.float32))
+    table, length, q_start = batch.tensors
+    out = torch.zeros_like(q)
+    for t, at, bad, word in ((length, 0, 200, "bounds"), (length, 1, -1, "bounds"), (q_start, 1, 7, "bounds"),
+                             (table, (0, 2), d["pages"], "page"), (table, (1, 0), -5, "page")):
+        keep = t[at].clone()
+        t[at] = bad
+        fsb.fs_kv_attend(cache, batch, q, out, 0.1, workspace=ws)
+        with pytest.raises(fsb.FleetSieveError) as ei:
+            fsb.fs_kv_check(ws)
+        assert ei.value.code == fsb.FS_EDEVICE and word in str(ei.value)
+        t[at] = keep
+    fsb.fs_kv_attend(cache, batch, q, out, 0.1, workspace=ws)
+    fsb.fs_kv_check(ws)
+    want, mag, dots = ref.attend(q.float().cpu().numpy(), d["k"], d["v"], d["k_scale"], d["v_scale"], d["table"],
+                                 d["length"], d["q_start"], 0.1, 0)
+    check(out, want, mag, dots, DTYPES["bf16"])
