@@ -343,14 +343,24 @@ int sm_count_of(int dev) {
 // of row_tile, the cache axis in parts of `split` tokens.
 struct KvPlan {
   int row_tile, row_blocks, split, splits;
+  int chunk_tiles;  // blocks of k_kv_chunk a (sequence, key head); 0: no sequence has that many rows
+  int decode;       // whether some sequence can have few rows
   size_t part_floats;
 };
+
+// Sequences with more rows (new tokens x query heads of a key head) than this go to
+// k_kv_chunk.
+constexpr int kFewRows = 64;
 
 constexpr int kMinSplit = 256, kMaxSplit = 4096;
 
 KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int sms) {
   KvPlan p{};
-  const int rows = std::max(1, b->max_new) * (q_heads / c->heads);
+  const long long all = (long long)std::max(1, b->max_new) * (q_heads / c->heads);
+  const int rows = (int)std::min<long long>(all, kFewRows);
+  p.chunk_tiles = all > kFewRows ? (int)((all + kKvChunkRows - 1) / kKvChunkRows) : 0;
+  // (every sequence has max_new new tokens: all have the same rows)
+  p.decode = !p.chunk_tiles || (long long)b->batch * b->max_new != b->tokens;
   p.row_tile = rows <= 8 ? 8 : 16;
   p.row_blocks = (rows + p.row_tile - 1) / p.row_tile;
   const long long items = (long long)std::max(1, b->batch) * c->heads * p.row_blocks;
@@ -363,7 +373,7 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int sms)
     p.split = std::clamp((int)((len + want - 1) / want + 127) / 128 * 128, kMinSplit, kMaxSplit);
     p.splits = (len + p.split - 1) / p.split;
   }
-  p.part_floats = p.splits > 1 ? (size_t)items * p.splits * p.row_tile * (c->dim + 2) : 0;
+  p.part_floats = p.decode && p.splits > 1 ? (size_t)items * p.splits * p.row_tile * (c->dim + 2) : 0;
   return p;
 }
 
@@ -371,7 +381,7 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int sms)
 // is at most 4 sms + 2 items where the items alone set the parts' length, items *
 // ceil(len / kMaxSplit) where that does.
 size_t part_floats_bound(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int sms) {
-  const long long rows = (long long)std::max(1, b->max_new) * (q_heads / c->heads);
+  const long long rows = std::min<long long>(kFewRows, (long long)std::max(1, b->max_new) * (q_heads / c->heads));
   const long long items = std::min<long long>(kKvTickets, (long long)std::max(1, b->batch) * c->heads * ((rows + 7) / 8));
   const long long len = std::max(1, b->max_length);
   return (size_t)(std::max(4ll * sms + 2 * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2));
@@ -490,8 +500,7 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   if (int rc = device_sms(&sms)) return rc;
   const KvPlan p = plan_of(cache, batch, qu->q_heads, sms);
   if (int rc = check_workspace(workspace, workspace_bytes, (int64_t)(kKvPartAt + 4 * p.part_floats))) return rc;
-  if ((long long)p.row_blocks * cache->heads > 65535)
-    return say(FS_EINVAL, "max_new = %d: too many rows for one call", batch->max_new);
+  if (p.chunk_tiles > 65535) return say(FS_EINVAL, "max_new = %d: too many rows for one call", batch->max_new);
 
   KvAttendArgs a{};
   a.v = view_of(cache, batch, qu->q_heads, workspace);
@@ -500,16 +509,28 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   a.scale_log2 = qu->scale * 1.44269504f;
   a.window = qu->window;
   a.split = p.split;
-  a.min_rows = 0, a.max_rows = INT_MAX;
   a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kKvPartAt);
   a.ticket = reinterpret_cast<unsigned*>(static_cast<char*>(workspace) + kKvTicketAt);
-  CUtensorMap mk, mv;
-  const int box = std::min(32, cache->page_tokens);
-  if (int rc = kv_tensor_map(&mk, *cache, cache->k, box)) return rc;
-  if (int rc = kv_tensor_map(&mv, *cache, cache->v, box)) return rc;
-  const cudaError_t e = launch_kv_decode(mk, mv, a, cache->dim, qu->dtype, p.row_tile, p.row_blocks, p.splits,
-                                         static_cast<cudaStream_t>(cuda_stream));
-  return e == cudaSuccess ? FS_OK : cuda_say(e, "launch (fs_kv_attend)");
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (p.chunk_tiles) {
+    KvChunkArgs ca{};
+    ca.a = a;
+    ca.a.min_rows = kFewRows, ca.a.max_rows = INT_MAX;
+    ca.kc = static_cast<const uint8_t*>(cache->k), ca.vc = static_cast<const uint8_t*>(cache->v);
+    ca.page_stride = cache->page_stride, ca.head_stride = cache->head_stride, ca.token_stride = cache->token_stride;
+    const cudaError_t e = launch_kv_chunk(ca, cache->dim, qu->dtype, p.chunk_tiles, st);
+    if (e != cudaSuccess) return cuda_say(e, "launch (fs_kv_attend, chunks)");
+  }
+  if (p.decode) {
+    a.min_rows = 0, a.max_rows = kFewRows;
+    CUtensorMap mk, mv;
+    const int box = std::min(32, cache->page_tokens);
+    if (int rc = kv_tensor_map(&mk, *cache, cache->k, box)) return rc;
+    if (int rc = kv_tensor_map(&mv, *cache, cache->v, box)) return rc;
+    const cudaError_t e = launch_kv_decode(mk, mv, a, cache->dim, qu->dtype, p.row_tile, p.row_blocks, p.splits, st);
+    if (e != cudaSuccess) return cuda_say(e, "launch (fs_kv_attend)");
+  }
+  return FS_OK;
 }
 
 extern "C" int fs_kv_check(void* workspace, void* cuda_stream) {
@@ -524,8 +545,9 @@ extern "C" int fs_kv_check(void* workspace, void* cuda_stream) {
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   if (e != cudaSuccess) return cuda_say(e, "clear (fs_kv_check)");
   if (st & ST_TIMEOUT) return say(FS_ETIMEOUT, "a device wait timed out (status 0x%x)", st);
-  return say(FS_EDEVICE, "%s%s%s%s(status 0x%x)", st & KV_ST_PAGE ? "a page id outside the cache; " : "",
+  return say(FS_EDEVICE, "%s%s%s%s%s(status 0x%x)", st & KV_ST_PAGE ? "a page id outside the cache; " : "",
              st & KV_ST_BATCH ? "length or q_start out of the batch's bounds; " : "",
              st & KV_ST_VALUE ? "a NaN in keys or values; " : "",
-             st & KV_ST_ANGLE ? "a position beyond the rows of cos / sin; " : "", st);
+             st & KV_ST_ANGLE ? "a position beyond the rows of cos / sin; " : "",
+             st & KV_ST_SCALE ? "a scale that is neither a power of two nor 0; " : "", st);
 }

@@ -16,6 +16,7 @@ enum : uint32_t {
   KV_ST_BATCH = 0x200u,   // q_start or length out of order, or beyond the batch's bounds
   KV_ST_VALUE = 0x400u,   // a NaN among the keys or values of an append (stored as 0)
   KV_ST_ANGLE = 0x800u,   // a position beyond the rows of cos / sin
+  KV_ST_SCALE = 0x1000u,  // a scale that is neither a power of two nor 0
 };
 
 // The workspace: status word, tickets (zero between calls), partial results.
@@ -44,6 +45,12 @@ struct KvAttendArgs {
   unsigned* ticket;
 };
 
+struct KvChunkArgs {
+  KvAttendArgs a;
+  const uint8_t *kc, *vc;
+  long long page_stride, head_stride, token_stride;
+};
+
 // One sequence of the batch as a kernel may use it: ranges checked, so that no
 // later index leaves its array whatever the batch's device arrays hold.
 struct KvSeq {
@@ -67,6 +74,16 @@ __device__ __forceinline__ int kv_page(const KvView& v, int b, int i) {
   if ((unsigned)g < (unsigned)v.pages) return g;
   kv_flag(v, KV_ST_PAGE);
   return 0;
+}
+
+// Scales are powers of two or 0, so that a code times a quotient of scales is exact in
+// half precision; others are reported.
+__device__ __forceinline__ bool kv_scale_ok(float s) {
+  const uint32_t x = __float_as_uint(s);
+  return x == 0 || ((x & 0x807fffffu) == 0 && x != 0x7f800000u);
+}
+__device__ __forceinline__ void kv_scales(const KvView& v, float ks, float vs) {
+  if (!kv_scale_ok(ks) || !kv_scale_ok(vs)) kv_flag(v, KV_ST_SCALE);
 }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -131,5 +148,7 @@ int kv_tensor_map(CUtensorMap* m, const fs_kv_cache& c, const void* base, int ro
 
 cudaError_t launch_kv_decode(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int dim, int dtype,
                              int row_tile, int row_blocks, int splits, cudaStream_t s);
+constexpr int kKvChunkRows = 256;  // rows of a block
+cudaError_t launch_kv_chunk(const KvChunkArgs& a, int dim, int dtype, int tiles, cudaStream_t s);
 
 }  // namespace fs

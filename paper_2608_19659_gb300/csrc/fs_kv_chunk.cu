@@ -1,0 +1,489 @@
+// Attention of many rows over the paged 8-bit cache (chunks of prompts): tcgen05.
+//
+// A block takes two tiles of 128 rows (new token, query head) of one (sequence, key head)
+// and walks over the cache in tiles of 128 tokens:
+//   S [128 x 128] = Q K^T,  P = exp2(c S - m),  O [128 x dim] += P V
+// with both products on the tensor cores in half precision (the codes are exact in it, a
+// bf16 query too once its row is scaled by a power of two; P keeps 11 bits) and S, P, O in
+// tensor memory: S_t in 128 columns, P_t in the first 64 of the same ones (a row's thread
+// writes a column only after it has read it), O_t in dim.
+//
+// Roles of the 13 warps:
+//   0-3, 4-7  softmax of tile 0 / 1, a row a thread: the maximum in one pass over S, P and the
+//             row's sum in a second. P holds a token's weight times the scale of its page's values
+//             (a power of two: an addend of the exponent), m is the largest of those, so that half
+//             precision's step is relative to what counts most; the sum of weights is taken without
+//             the scales. O is rescaled only when m has grown by more than 2^8 (P, times 2^7,
+//             stays under 65504), so almost never after the first tiles
+//   8-11      codes to halves: 16-byte loads of the next tile are under way while this one is
+//             converted and stored swizzled. Keys are scaled by their page's scale over the largest
+//             (times 2^7: 448 * 2^7 < 65504 leaves small pages the most room)
+//   12        one thread issues every product. While tile 0's rows are in softmax the tensor
+//             cores work on tile 1, and the other way round.
+// Bound by the tensor cores: 4 dim operations per (row, token) at the bf16 rate.
+#include "fs_kv.cuh"
+
+namespace fs {
+namespace {
+
+constexpr int kThreads = 13 * 32, kTok = 128, kTileRows = 128;
+constexpr float kUp = 7.f;  // halves hold 2^(kUp + 8) of a row's largest weight, and 2^kUp of a code
+
+template <int D>
+struct Cfg {
+  static constexpr int kStages = D == 128 ? 5 : 8;
+  static constexpr int kSlot = kTok * D * 2;              // bytes of a tile of keys or values
+  static constexpr int kQ = 2 * kTileRows * D * 2;
+  static constexpr size_t kSmem = 1024 + kQ + (size_t)kStages * kSlot + 1024;
+};
+
+struct Bars {
+  uint64_t full[8], empty[8], s_full[2], p_full[2], pv_done[2], end;
+  float2 v_scale[8][8];  // per tile (mod 8) and 16 tokens: log2 of the values' scale, and its reciprocal
+  float k_ref, v_ref;
+  uint32_t tmem;
+};
+static_assert(sizeof(Bars) <= 1024, "the barriers' share of shared memory");
+
+__device__ __forceinline__ void st_shared16(uint32_t a, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// Matrix descriptor of a 128-byte swizzled tile: `stride` bytes between groups of 8 rows,
+// `lead` between 64-dimension blocks where the dimensions are not the reduced ones.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint32_t stride) {
+  return (uint64_t)((addr >> 4) & 0x3fff) | (uint64_t)((lead >> 4) & 0x3fff) << 16 | (uint64_t)((stride >> 4) & 0x3fff) << 32 |
+         1ull << 46 | 2ull << 61;
+}
+
+// half x half -> float products of 128 rows and n columns; b_mn: B's columns are contiguous
+__host__ __device__ constexpr uint32_t instr_desc(int n, bool b_mn) {
+  return 1u << 4 | (b_mn ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(128 >> 4) << 24;
+}
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void tmem_ld32(uint32_t (&r)[32], uint32_t a) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+      "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(a)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t a, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+      "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(a),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+      "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+      "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(a),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+// A wait that says so when it runs out; the caller leaves its loop.
+__device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, const KvView& v) {
+  if (mbar_wait(bar, parity, kWaitLimitNs)) return true;
+  kv_flag(v, ST_TIMEOUT);
+  return false;
+}
+
+template <int D, typename T>
+__global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) {
+  using C = Cfg<D>;
+  extern __shared__ unsigned char raw[];
+  const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
+  const uint32_t q_at = smem, ring_at = smem + C::kQ;
+  Bars& bars = *reinterpret_cast<Bars*>(raw + (smem - smem_u32(raw)) + C::kQ + (size_t)C::kStages * C::kSlot);
+  const KvAttendArgs& a = ca.a;
+  const KvView& v = a.v;
+  const int tile = gridDim.y - 1 - blockIdx.y;  // the longest walks first
+  const int h = blockIdx.x % v.heads, b = blockIdx.x / v.heads;
+  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  KvSeq s;
+  if (!kv_seq(v, b, s)) {
+    if (threadIdx.x == 0 && tile == 0) kv_flag(v, KV_ST_BATCH);
+    return;
+  }
+  const int rows = s.count * v.group, r0 = tile * (2 * kTileRows);
+  if (r0 >= rows || rows <= a.min_rows || rows > a.max_rows) return;
+  const int r_end = min(rows, r0 + 2 * kTileRows);
+  const int n_sub = r_end - r0 > kTileRows ? 2 : 1;
+  const int base = s.len - s.count;  // position of the sequence's first new token
+  const int pos0 = base + r0 / v.group, pos1 = base + (r_end - 1) / v.group;
+  const int kv_hi = max(pos1 + 1, 0), kv_lo = a.window ? max(pos0 - a.window + 1, 0) : 0;
+  const int begin = kv_lo & ~(kTok - 1);
+  const int n = (kv_hi - begin + kTok - 1) / kTok;  // tiles of the cache; 0: no row sees a token
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::kStages; ++i) mbar_init(&bars.full[i], 128), mbar_init(&bars.empty[i], 1);
+    for (int t = 0; t < 2; ++t) mbar_init(&bars.s_full[t], 1), mbar_init(&bars.p_full[t], 128), mbar_init(&bars.pv_done[t], 1);
+    mbar_init(&bars.end, 1);
+    bars.k_ref = bars.v_ref = 0.f;
+  }
+  if (w == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  __syncthreads();
+
+  // the largest scales of the pages that are walked
+  {
+    float km = 0.f, vm = 0.f;
+    const int g0 = begin >> v.log_page, g1 = (kv_hi + (1 << v.log_page) - 1) >> v.log_page;
+    for (int g = g0 + threadIdx.x; g < g1; g += kThreads) {
+      const long long at = (long long)kv_page(v, b, g) * v.heads + h;
+      const float ks = v.k_scale[at], vs = v.v_scale[at];
+      kv_scales(v, ks, vs);
+      km = fmaxf(km, ks), vm = fmaxf(vm, vs);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) km = fmaxf(km, __shfl_xor_sync(~0u, km, d)), vm = fmaxf(vm, __shfl_xor_sync(~0u, vm, d));
+    if (lane == 0) {  // (nonnegative floats order as their bits do)
+      atomicMax(reinterpret_cast<int*>(&bars.k_ref), __float_as_int(km));
+      atomicMax(reinterpret_cast<int*>(&bars.v_ref), __float_as_int(vm));
+    }
+  }
+  // queries: a row a thread, scaled into [-2, 2] by a power of two (and by the scale's sign)
+  int q_exp = 0;
+  if (w < 8) {
+    const int r = r0 + threadIdx.x;
+    uint32_t x[D / 2];
+    if (r < r_end) {
+      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (long long)(s.first + r / v.group) * a.q_token +
+                                                      (h * v.group + r % v.group) * a.q_head);
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) {
+        const uint4 u = q[i];
+        x[4 * i] = u.x, x[4 * i + 1] = u.y, x[4 * i + 2] = u.z, x[4 * i + 3] = u.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < D / 2; ++i) x[i] = 0;
+    }
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 2; ++i) {
+      const float2 z = Elem<T>::two(x[i]);
+      amax = fmaxf(amax, fmaxf(fabsf(z.x), fabsf(z.y)));
+    }
+    q_exp = row_exponent(amax);
+    const float down = a.scale_log2 < 0.f ? -exp2_int(-q_exp) : exp2_int(-q_exp);
+    const int t = threadIdx.x >> 7, rr = threadIdx.x & 127;
+    const uint32_t row = q_at + t * (kTileRows * D * 2) + rr * 128;
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+      uint32_t y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 z = Elem<T>::two(x[4 * i + k]);
+        y[k] = pack_f16(z.x * down, z.y * down);
+      }
+      st_shared16(row + (i >> 3) * (kTileRows * 128) + (((i & 7) ^ (rr & 7)) << 4), make_uint4(y[0], y[1], y[2], y[3]));
+    }
+    fence_proxy_async();
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = bars.tmem;
+
+  if (w < 8) {
+    // ---------------------------------------------------------------- softmax
+    const int t = w >> 2;
+    const int r = r0 + threadIdx.x;
+    if (t < n_sub) {
+      const uint32_t lanes = (uint32_t)(w & 3) << 21;  // 32 lanes a warp, in bits 16 and up
+      const uint32_t s_at = tmem + lanes + t * 128, o_at = tmem + lanes + 256 + t * 128;
+      const float c = fabsf(a.scale_log2) * exp2_int(q_exp) * (bars.k_ref * (1.f / 128.f));
+      const int pos = base + r / v.group;
+      const int hi = r < r_end ? pos : -1, lo = a.window ? pos - a.window + 1 : 0;
+      // tiles inside [all_lo, all_hi) are seen whole by every row of this tile
+      const int t_r0 = r0 + t * kTileRows, t_r1 = min(r_end, t_r0 + kTileRows) - 1;
+      const int all_hi = base + t_r0 / v.group + 1, all_lo = a.window ? base + t_r1 / v.group - a.window + 1 : 0;
+      float m = -INFINITY, l = 0.f;
+      bool ok = true;
+      int j = 0;
+      for (; j < n; ++j) {
+        const int t0 = begin + j * kTok;
+        const bool whole = t0 >= all_lo && t0 + kTok <= all_hi;
+        const int c_hi = hi - t0, c_lo = lo - t0;  // columns [c_lo, c_hi] count
+        ok = wait_bar(&bars.s_full[t], j & 1, v);
+        if (!__all_sync(~0u, ok)) break;
+        fence_after();
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t x[32];
+          tmem_ld32(x, s_at + 32 * k);
+          wait_ld();
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            float most = -INFINITY;
+#pragma unroll
+            for (int i = 16 * g; i < 16 * g + 16; ++i)
+              if (whole || (32 * k + i <= c_hi && 32 * k + i >= c_lo)) most = fmaxf(most, __uint_as_float(x[i]));
+            if (most > -INFINITY) top = fmaxf(top, fmaf(most, c, bars.v_scale[j & 7][2 * k + g].x));
+          }
+        }
+        const bool grow = top > m + 8.f || (m == -INFINITY && top > m);
+        if (__any_sync(~0u, grow)) {
+          const float f = grow ? ex2(m - top) : 1.f;
+          if (grow) m = top;
+          l *= f;
+          if (j > 0) {  // (the first product overwrites O)
+            ok = wait_bar(&bars.pv_done[t], (j - 1) & 1, v);
+            if (!__all_sync(~0u, ok)) break;
+            fence_after();
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) {
+              uint32_t x[32];
+              tmem_ld32(x, o_at + 32 * k);
+              wait_ld();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
+              tmem_st32(o_at + 32 * k, x);
+            }
+          }
+        }
+        const float off = m == -INFINITY ? 0.f : m;  // (m: log2 of weight times scale, without kUp)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t x[32], p[16];
+          tmem_ld32(x, s_at + 32 * k);
+          wait_ld();
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const float2 vs = bars.v_scale[j & 7][2 * k + g];
+            const float off_g = vs.x + kUp - off;
+            float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+            for (int i = 8 * g; i < 8 * g + 8; ++i) {
+              float y0 = ex2(fmaf(__uint_as_float(x[2 * i]), c, off_g)), y1 = ex2(fmaf(__uint_as_float(x[2 * i + 1]), c, off_g));
+              if (!whole) {
+                const int col = 32 * k + 2 * i;
+                y0 = col <= c_hi && col >= c_lo ? y0 : 0.f;
+                y1 = col + 1 <= c_hi && col + 1 >= c_lo ? y1 : 0.f;
+              }
+              l0 += y0, l1 += y1;
+              p[i] = pack_f16(y0, y1);
+            }
+            l = fmaf(l0 + l1, vs.y * (1.f / 128.f), l);
+          }
+          tmem_st16(s_at + 16 * k, p);
+        }
+        wait_st();
+        fence_before();
+        mbar_arrive(&bars.p_full[t]);
+      }
+      // ------------------------------------------------------------ result
+      if (ok && n > 0) {
+        ok = wait_bar(&bars.pv_done[t], (n - 1) & 1, v);
+        fence_after();
+      }
+      ok = __all_sync(~0u, ok);
+      const float inv = l > 0.f ? bars.v_ref * (1.f / 128.f) / l : 0.f;
+      T* to = static_cast<T*>(a.out) + (long long)(s.first + r / v.group) * a.out_token + (h * v.group + r % v.group) * a.out_head;
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) {
+        uint32_t x[32];
+        if (n > 0) {
+          tmem_ld32(x, o_at + 32 * k);
+          wait_ld();
+        }
+        if (ok && r < r_end) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t y[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              y[u] = l > 0.f ? Elem<T>::pack(__uint_as_float(x[8 * i + 2 * u]) * inv, __uint_as_float(x[8 * i + 2 * u + 1]) * inv) : 0u;
+            *reinterpret_cast<uint4*>(to + 32 * k + 8 * i) = make_uint4(y[0], y[1], y[2], y[3]);
+          }
+        }
+      }
+    }
+  } else if (w < 12) {
+    // ---------------------------------------------------------------- codes to halves
+    constexpr int kLanes = D / 16;               // lanes a token, 16 codes each
+    constexpr int kPer = 128 / kLanes;           // tokens a pass
+    constexpr int kPasses = kTok / kPer;         // 8 (dim 128) or 4 (dim 64)
+    const int id = threadIdx.x - 256, cl = id % kLanes, tk = id / kLanes;
+    const float inv_k = bars.k_ref > 0.f ? 128.f / bars.k_ref : 0.f;
+    const int v_exp = __float_as_int(bars.v_ref) >> 23;
+    // lane g of every warp knows the page of the tile's g-th 16 tokens
+    int page = 0;
+    float fk = 0.f, vs = 0.f;
+    auto load_pages = [&](int j) {
+      const int t = begin + j * kTok + (lane & 7) * 16;
+      page = 0, fk = vs = 0.f;
+      if (j < n && t < kv_hi) {
+        page = kv_page(v, b, t >> v.log_page);
+        const long long at = (long long)page * v.heads + h;
+        fk = v.k_scale[at] * inv_k, vs = v.v_scale[at];
+      }
+    };
+    uint4 cur[kPasses], nxt[kPasses];
+    float cur_f[kPasses], nxt_f[kPasses];
+    auto load = [&](int i, uint4(&x)[kPasses], float(&f)[kPasses]) {  // tile i / 2's keys (even i) or values
+      const uint8_t* from = (i & 1) ? ca.vc : ca.kc;
+#pragma unroll
+      for (int p = 0; p < kPasses; ++p) {
+        const int tl = p * kPer + tk;
+        const int g = __shfl_sync(~0u, page, tl >> 4);
+        f[p] = __shfl_sync(~0u, (i & 1) ? vs : fk, tl >> 4);
+        const int t = begin + (i >> 1) * kTok + tl;
+        x[p] = make_uint4(0, 0, 0, 0);
+        if (i < 2 * n && t < kv_hi && f[p] != 0.f)  // (beyond: not seen, and slots without a token may hold NaN codes)
+          x[p] = __ldg(reinterpret_cast<const uint4*>(from + g * ca.page_stride + h * ca.head_stride +
+                                                      (t & ((1 << v.log_page) - 1)) * ca.token_stride + cl * 16));
+      }
+    };
+    load_pages(0);
+    load(0, cur, cur_f);
+    for (int i = 0; i < 2 * n; ++i) {
+      const int st = i % C::kStages;
+      // (before the lists move on) the scales of values over each 16 tokens of this tile, relative to
+      // the largest; a scale of 0 counts as one too small to matter, and its values are stored as 0
+      float2 ps = make_float2(0.f, 0.f);
+      if (!(i & 1)) {
+        const int e = vs != 0.f ? max((__float_as_int(vs) >> 23) - v_exp, -100) : -100;
+        ps = make_float2((float)e, exp2_int(-e));
+      }
+      if (i & 1) load_pages((i + 1) >> 1);
+      load(i + 1, nxt, nxt_f);
+      if (!wait_bar(&bars.empty[st], ((i / C::kStages) & 1) ^ 1, v)) break;
+      // (this far ahead of softmax the entry of eight tiles ago has been read)
+      if (!(i & 1) && id < 8) bars.v_scale[(i >> 1) & 7][id] = ps;
+      const uint32_t slot = ring_at + st * C::kSlot;
+#pragma unroll
+      for (int p = 0; p < kPasses; ++p) {
+        const int tl = p * kPer + tk;
+        const float f = (i & 1) ? 1.f : cur_f[p];  // (the values' scale is in P)
+        const uint32_t f2 = pack_f16(f, f);
+        const uint32_t ws[4] = {cur[p].x, cur[p].y, cur[p].z, cur[p].w};
+        uint32_t y[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t e0 = e4m3x2_to_f16x2(ws[k]), e1 = e4m3x2_to_f16x2_hi(ws[k]);
+          asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(y[2 * k]) : "r"(e0), "r"(f2));
+          asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(y[2 * k + 1]) : "r"(e1), "r"(f2));
+        }
+        // 16-byte chunks 2 (cl mod 4) and + 1 of the token's row in block cl / 4; lanes of the second
+        // block begin with the other one, so that a row's lanes meet every bank once
+        const uint32_t row = slot + (cl >> 2) * (kTok * 128) + tl * 128;
+        const int sw = D == 128 ? cl >> 2 : 0;
+        const uint32_t c0 = (((cl & 3) * 2 + sw) ^ (tl & 7)) << 4, c1 = (((cl & 3) * 2 + (sw ^ 1)) ^ (tl & 7)) << 4;
+        const uint4 y0 = make_uint4(y[0], y[1], y[2], y[3]), y1 = make_uint4(y[4], y[5], y[6], y[7]);
+        st_shared16(row + c0, sw ? y1 : y0);
+        st_shared16(row + c1, sw ? y0 : y1);
+      }
+      fence_proxy_async();
+      mbar_arrive(&bars.full[st]);
+#pragma unroll
+      for (int p = 0; p < kPasses; ++p) cur[p] = nxt[p], cur_f[p] = nxt_f[p];
+    }
+  } else if (lane == 0 && n > 0) {
+    // ---------------------------------------------------------------- products
+    constexpr uint32_t kIdS = instr_desc(kTok, false), kIdO = instr_desc(D, true);
+    auto qk = [&](int t, int slot) {
+      const uint32_t q = q_at + t * (kTileRows * D * 2), k = ring_at + slot * C::kSlot;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+        mma_ss(tmem + t * 128, smem_desc(q + (i >> 2) * (kTileRows * 128) + (i & 3) * 32, 16, 1024),
+               smem_desc(k + (i >> 2) * (kTok * 128) + (i & 3) * 32, 16, 1024), kIdS, i > 0);
+    };
+    auto pv = [&](int t, int slot, bool add) {
+      const uint32_t vv = ring_at + slot * C::kSlot;
+#pragma unroll
+      for (int i = 0; i < kTok / 16; ++i)
+        mma_ts(tmem + 256 + t * 128, tmem + t * 128 + i * 8, smem_desc(vv + i * 2048, kTok * 128, 1024), kIdO, add || i > 0);
+    };
+    bool ok = wait_bar(&bars.full[0], 0, v);
+    if (ok) {
+      fence_after();
+      for (int t = 0; t < n_sub; ++t) {
+        qk(t, 0);
+        commit(&bars.s_full[t]);
+      }
+      commit(&bars.empty[0]);
+      for (int j = 0; ok && j < n; ++j) {
+        const int vi = 2 * j + 1, ki = 2 * j + 2, vs = vi % C::kStages, ks = ki % C::kStages;
+        ok = wait_bar(&bars.full[vs], (vi / C::kStages) & 1, v);
+        for (int t = 0; ok && t < n_sub; ++t) {
+          ok = wait_bar(&bars.p_full[t], j & 1, v);
+          if (!ok) break;
+          fence_after();
+          pv(t, vs, j > 0);
+          commit(&bars.pv_done[t]);
+          if (j + 1 < n) {
+            if (t == 0) ok = wait_bar(&bars.full[ks], (ki / C::kStages) & 1, v);
+            if (!ok) break;
+            fence_after();
+            qk(t, ks);
+            commit(&bars.s_full[t]);
+          }
+        }
+        commit(&bars.empty[vs]);
+        if (j + 1 < n) commit(&bars.empty[ks]);
+      }
+    }
+    // nothing of this block's is under way once this has arrived
+    commit(&bars.end);
+    wait_bar(&bars.end, 0, v);
+  }
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (w == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+
+template <int D, typename T>
+cudaError_t launch(const KvChunkArgs& a, int tiles, cudaStream_t s) {
+  static const cudaError_t limit = raise_smem_limit(reinterpret_cast<const void*>(k_kv_chunk<D, T>), Cfg<D>::kSmem);
+  if (limit != cudaSuccess) return limit;
+  k_kv_chunk<D, T><<<dim3(a.a.v.heads * a.a.v.batch, tiles), kThreads, Cfg<D>::kSmem, s>>>(a);
+  note_launch();
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_kv_chunk(const KvChunkArgs& a, int dim, int dtype, int tiles, cudaStream_t s) {
+  const bool h = dtype == FS_KV_FP16;
+  if (dim == 128) return h ? launch<128, __half>(a, tiles, s) : launch<128, __nv_bfloat16>(a, tiles, s);
+  return h ? launch<64, __half>(a, tiles, s) : launch<64, __nv_bfloat16>(a, tiles, s);
+}
+
+}  // namespace fs

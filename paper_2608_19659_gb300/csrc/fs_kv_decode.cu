@@ -16,15 +16,17 @@
 // attention rows its 8 columns, so one query head costs no more padding than eight.
 // tcgen05 has nothing to add here: its smallest tile is 128 rows high, and its operands
 // would have to pass through shared memory once more after the conversion.
-// The scale of a page's keys multiplies S, that of its values P (relative to the largest
-// met so far, v_ref, so that half precision holds the product).
+// The scale of a page's keys multiplies S. That of its values, a power of two relative to the
+// largest met so far (v_ref), goes into P as an addend of the exponent, and m is the largest
+// weight times scale: half precision's step is relative to what counts most, however far the
+// scales are apart. The sum of weights is taken without it.
 #include "fs_kv.cuh"
 
 namespace fs {
 namespace {
 
 constexpr int kWarps = 4, kStages = 3, kTile = 32;
-constexpr float kUp = 16384.f;  // probability * page scale / v_ref, <= 1, times this: 28 binades of normal halves
+constexpr float kUp = 15.f;  // log2 of the largest weight: near the top of half precision
 
 __device__ __forceinline__ void tma_tile(void* dst, const CUtensorMap* m, int token, int head, int page, uint64_t* bar) {
   asm volatile(
@@ -124,6 +126,8 @@ __global__ void __launch_bounds__(kWarps * 32)
       ks0 = v.k_scale[at0], vs0 = v.v_scale[at0];
       ks1 = ks0, vs1 = vs0;
       if (pg1 != pg0) ks1 = v.k_scale[at1], vs1 = v.v_scale[at1];
+      kv_scales(v, ks0, vs0);
+      kv_scales(v, ks1, vs1);
     }
   };
   auto issue = [&](int i, int p0, int p1) {  // lane 0: tile i into its stage
@@ -221,20 +225,26 @@ __global__ void __launch_bounds__(kWarps * 32)
 #pragma unroll
       for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
       if (top > v_ref) {
-        const float f = v_ref / top;
-        v_ref = top;
-#pragma unroll
-        for (int j = 0; j < kMt; ++j)
+        // weights times scales, and their maxima, are relative to v_ref; the sums of weights are not
+        if (v_ref > 0.f) {
+          const int up = min((__float_as_int(top) >> 23) - (__float_as_int(v_ref) >> 23), 100);
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) o[j][n][k] *= f;
+            for (int k = 0; k < 2; ++k) m[n][k] -= (float)up, l[n][k] = fminf(l[n][k] * exp2_int(up), 0x1p120f);
+        }
+        v_ref = top;
       }
     }
     const int st = i % kStages, t0 = c0 + (w + i * kWarps) * kTile;
-    const float inv_ref = v_ref > 0.f ? kUp / v_ref : 0.f;
     const float ks[2] = {__shfl_sync(~0u, ks0, i & 31), __shfl_sync(~0u, ks1, i & 31)};
-    const float vs[2] = {__shfl_sync(~0u, vs0, i & 31) * inv_ref, __shfl_sync(~0u, vs1, i & 31) * inv_ref};
+    // log2 of the values' scale over the largest so far; a scale of 0 counts as one too small to
+    // matter, and its values as 0
+    const float vs[2] = {__shfl_sync(~0u, vs0, i & 31), __shfl_sync(~0u, vs1, i & 31)};
+    int ve[2];
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+      ve[mt] = vs[mt] != 0.f ? max((__float_as_int(vs[mt]) >> 23) - (__float_as_int(v_ref) >> 23), -100) : -100;
     ok = mbar_wait(&bars[w][st], (i / kStages) & 1, kWaitLimitNs);
     if (!__all_sync(~0u, ok)) break;
     const unsigned char* kt = my_ring + st * (2 * kTileBytes);
@@ -270,7 +280,7 @@ __global__ void __launch_bounds__(kWarps * 32)
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          float x = sc[mt][n][k] * (ks[mt] * cq[n][k & 1]);
+          float x = fmaf(sc[mt][n][k], ks[mt] * cq[n][k & 1], (float)ve[mt]);
           if (!whole) {
             const int t = t0 + mt * 16 + gid + (k >> 1) * 8;
             if (t > hi_lim[n][k & 1] || t < lo_lim[n][k & 1]) x = -INFINITY;
@@ -281,7 +291,7 @@ __global__ void __launch_bounds__(kWarps * 32)
     uint32_t pf[2][NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float mx[2], corr[2];
+      float up[2], corr[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         float x = fmaxf(fmaxf(sc[0][n][j], sc[0][n][j + 2]), fmaxf(sc[1][n][j], sc[1][n][j + 2]));
@@ -289,8 +299,9 @@ __global__ void __launch_bounds__(kWarps * 32)
         x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
         x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
         const float m_new = fmaxf(m[n][j], x);
-        mx[j] = m_new == -INFINITY ? 0.f : m_new;
-        corr[j] = ex2(m[n][j] - mx[j]);
+        const float mx = m_new == -INFINITY ? 0.f : m_new;
+        up[j] = mx - kUp;
+        corr[j] = ex2(m[n][j] - mx);
         m[n][j] = m_new;
         l[n][j] *= corr[j];
       }
@@ -305,9 +316,9 @@ __global__ void __launch_bounds__(kWarps * 32)
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const float p0 = ex2(sc[mt][n][2 * k] - mx[0]), p1 = ex2(sc[mt][n][2 * k + 1] - mx[1]);
-          l[n][0] += p0, l[n][1] += p1;
-          pf[mt][n][k] = transpose8x8(pack_f16(p0 * vs[mt], p1 * vs[mt]));
+          const float p0 = ex2(sc[mt][n][2 * k] - up[0]), p1 = ex2(sc[mt][n][2 * k + 1] - up[1]);
+          l[n][0] = fmaf(p0, exp2_int(-ve[mt]), l[n][0]), l[n][1] = fmaf(p1, exp2_int(-ve[mt]), l[n][1]);
+          pf[mt][n][k] = transpose8x8(pack_f16(p0, p1));
         }
     }
     const bool tail = t0 + kTile > s.len;
@@ -325,7 +336,7 @@ __global__ void __launch_bounds__(kWarps * 32)
           const uint2 x = *reinterpret_cast<const uint2*>(vt + t * D + (((gid >> 1) ^ ((t >> 1) & 3)) * 16) + (gid & 1) * 8);
           vw[i2][0] = x.x, vw[i2][1] = x.y;
         }
-        if (tail && t0 + t >= s.len) {  // slots without a token may hold NaN codes
+        if ((tail && t0 + t >= s.len) || vs[mt] == 0.f) {  // slots without a token may hold NaN codes
 #pragma unroll
           for (int k = 0; k < kChunk / 4; ++k) vw[i2][k] = 0;
         }
@@ -374,7 +385,6 @@ __global__ void __launch_bounds__(kWarps * 32)
     }
   __syncthreads();  // every warp has left its ring
   float* ow = reinterpret_cast<float*>(ring);  // [kWarps][kRows][D]
-  const float down = v_ref * (1.f / kUp);
 #pragma unroll
   for (int j = 0; j < kMt; ++j)
 #pragma unroll
@@ -384,7 +394,7 @@ __global__ void __launch_bounds__(kWarps * 32)
         // rows gid, gid + 8 of tile j are dimensions gid * kChunk + 2 j, + 1
         const int r = n * 8 + 2 * tid + k;
         *reinterpret_cast<float2*>(ow + ((w * kRows + r) * D + gid * kChunk + 2 * j)) =
-            make_float2(o[j][n][k] * down, o[j][n][k + 2] * down);
+            make_float2(o[j][n][k] * v_ref, o[j][n][k + 2] * v_ref);
       }
   __syncthreads();
 

@@ -210,7 +210,9 @@ def test_broken_batches_are_reported(fsb, cuda):
     table, length, q_start = batch.tensors
     out = torch.zeros_like(q)
     for t, at, bad, word in ((length, 0, 200, "bounds"), (length, 1, -1, "bounds"), (q_start, 1, 7, "bounds"),
-                             (table, (0, 2), d["pages"], "page"), (table, (1, 0), -5, "page")):
+                             (table, (0, 2), d["pages"], "page"), (table, (1, 0), -5, "page"),
+                             (cache.tensors[2], (int(d["table"][0, 1]), 1), 0.3, "power of two"),
+                             (cache.tensors[3], (int(d["table"][1, 0]), 0), -1.0, "power of two")):
         keep = t[at].clone()
         t[at] = bad
         fsb.fs_kv_attend(cache, batch, q, out, 0.1, workspace=ws)
