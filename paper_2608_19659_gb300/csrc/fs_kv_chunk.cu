@@ -117,6 +117,61 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, const K
   return false;
 }
 
+// A row's largest log2 weight (times its value scale) among columns [lo, hi] of S (all of them
+// with kWhole), into top. The walk over 32 columns at a time is a loop: unrolled whole, the
+// two passes overflow the instruction cache.
+template <bool kWhole>
+__device__ __forceinline__ void row_top(float& top, uint32_t s_at, float c, const float2* v_scale, int lo, int hi) {
+#pragma unroll 1
+  for (int k = 0; k < 4; ++k) {
+    uint32_t x[32];
+    tmem_ld32(x, s_at + 32 * k);
+    wait_ld();
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float most = -INFINITY;
+#pragma unroll
+      for (int i = 16 * g; i < 16 * g + 16; ++i) {
+        const float y = __uint_as_float(x[i]);
+        most = fmaxf(most, kWhole || (32 * k + i <= hi && 32 * k + i >= lo) ? y : -INFINITY);
+      }
+      if (kWhole || most > -INFINITY) top = fmaxf(top, fmaf(most, c, v_scale[2 * k + g].x));
+    }
+  }
+}
+
+// P = 2^(c S + log2 of the value scale - off) in half precision over S, and the row's sum of
+// weights (without the scales) added to l.
+template <bool kWhole>
+__device__ __forceinline__ void row_weights(float& l, uint32_t s_at, float c, float off, const float2* v_scale, int lo,
+                                            int hi) {
+#pragma unroll 1
+  for (int k = 0; k < 4; ++k) {
+    uint32_t x[32], p[16];
+    tmem_ld32(x, s_at + 32 * k);
+    wait_ld();
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const float2 vs = v_scale[2 * k + g];
+      const float off_g = vs.x + kUp - off;
+      float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+      for (int i = 8 * g; i < 8 * g + 8; ++i) {
+        float y0 = ex2(fmaf(__uint_as_float(x[2 * i]), c, off_g)), y1 = ex2(fmaf(__uint_as_float(x[2 * i + 1]), c, off_g));
+        if (!kWhole) {
+          const int col = 32 * k + 2 * i;
+          y0 = col <= hi && col >= lo ? y0 : 0.f;
+          y1 = col + 1 <= hi && col + 1 >= lo ? y1 : 0.f;
+        }
+        l0 += y0, l1 += y1;
+        p[i] = pack_f16(y0, y1);
+      }
+      l = fmaf(l0 + l1, vs.y * (1.f / 128.f), l);
+    }
+    tmem_st16(s_at + 16 * k, p);
+  }
+}
+
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) {
   using C = Cfg<D>;
@@ -178,35 +233,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) 
   int q_exp = 0;
   if (w < 8) {
     const int r = r0 + threadIdx.x;
-    uint32_t x[D / 2];
+    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (long long)(s.first + r / v.group) * a.q_token +
+                                                    (h * v.group + r % v.group) * a.q_head);
+    float amax = 0.f;
     if (r < r_end) {
-      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (long long)(s.first + r / v.group) * a.q_token +
-                                                      (h * v.group + r % v.group) * a.q_head);
-#pragma unroll
+#pragma unroll 4
       for (int i = 0; i < D / 8; ++i) {
         const uint4 u = q[i];
-        x[4 * i] = u.x, x[4 * i + 1] = u.y, x[4 * i + 2] = u.z, x[4 * i + 3] = u.w;
+        const float2 z0 = Elem<T>::two(u.x), z1 = Elem<T>::two(u.y), z2 = Elem<T>::two(u.z), z3 = Elem<T>::two(u.w);
+        amax = fmaxf(amax, fmaxf(fmaxf(fmaxf(fabsf(z0.x), fabsf(z0.y)), fmaxf(fabsf(z1.x), fabsf(z1.y))),
+                                 fmaxf(fmaxf(fabsf(z2.x), fabsf(z2.y)), fmaxf(fabsf(z3.x), fabsf(z3.y)))));
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < D / 2; ++i) x[i] = 0;
-    }
-    float amax = 0.f;
-#pragma unroll
-    for (int i = 0; i < D / 2; ++i) {
-      const float2 z = Elem<T>::two(x[i]);
-      amax = fmaxf(amax, fmaxf(fabsf(z.x), fabsf(z.y)));
     }
     q_exp = row_exponent(amax);
     const float down = a.scale_log2 < 0.f ? -exp2_int(-q_exp) : exp2_int(-q_exp);
     const int t = threadIdx.x >> 7, rr = threadIdx.x & 127;
     const uint32_t row = q_at + t * (kTileRows * D * 2) + rr * 128;
-#pragma unroll
+#pragma unroll 4
     for (int i = 0; i < D / 8; ++i) {
-      uint32_t y[4];
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (r < r_end) u = q[i];
+      uint32_t y[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float2 z = Elem<T>::two(x[4 * i + k]);
+        const float2 z = Elem<T>::two(y[k]);
         y[k] = pack_f16(z.x * down, z.y * down);
       }
       st_shared16(row + (i >> 3) * (kTileRows * 128) + (((i & 7) ^ (rr & 7)) << 4), make_uint4(y[0], y[1], y[2], y[3]));
@@ -242,20 +292,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) 
         if (!__all_sync(~0u, ok)) break;
         fence_after();
         float top = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t x[32];
-          tmem_ld32(x, s_at + 32 * k);
-          wait_ld();
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            float most = -INFINITY;
-#pragma unroll
-            for (int i = 16 * g; i < 16 * g + 16; ++i)
-              if (whole || (32 * k + i <= c_hi && 32 * k + i >= c_lo)) most = fmaxf(most, __uint_as_float(x[i]));
-            if (most > -INFINITY) top = fmaxf(top, fmaf(most, c, bars.v_scale[j & 7][2 * k + g].x));
-          }
-        }
+        if (whole)
+          row_top<true>(top, s_at, c, bars.v_scale[j & 7], 0, 0);
+        else
+          row_top<false>(top, s_at, c, bars.v_scale[j & 7], c_lo, c_hi);
         const bool grow = top > m + 8.f || (m == -INFINITY && top > m);
         if (__any_sync(~0u, grow)) {
           const float f = grow ? ex2(m - top) : 1.f;
@@ -277,31 +317,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) 
           }
         }
         const float off = m == -INFINITY ? 0.f : m;  // (m: log2 of weight times scale, without kUp)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t x[32], p[16];
-          tmem_ld32(x, s_at + 32 * k);
-          wait_ld();
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const float2 vs = bars.v_scale[j & 7][2 * k + g];
-            const float off_g = vs.x + kUp - off;
-            float l0 = 0.f, l1 = 0.f;
-#pragma unroll
-            for (int i = 8 * g; i < 8 * g + 8; ++i) {
-              float y0 = ex2(fmaf(__uint_as_float(x[2 * i]), c, off_g)), y1 = ex2(fmaf(__uint_as_float(x[2 * i + 1]), c, off_g));
-              if (!whole) {
-                const int col = 32 * k + 2 * i;
-                y0 = col <= c_hi && col >= c_lo ? y0 : 0.f;
-                y1 = col + 1 <= c_hi && col + 1 >= c_lo ? y1 : 0.f;
-              }
-              l0 += y0, l1 += y1;
-              p[i] = pack_f16(y0, y1);
-            }
-            l = fmaf(l0 + l1, vs.y * (1.f / 128.f), l);
-          }
-          tmem_st16(s_at + 16 * k, p);
-        }
+        if (whole)
+          row_weights<true>(l, s_at, c, off, bars.v_scale[j & 7], 0, 0);
+        else
+          row_weights<false>(l, s_at, c, off, bars.v_scale[j & 7], c_lo, c_hi);
         wait_st();
         fence_before();
         mbar_arrive(&bars.p_full[t]);
