@@ -68,13 +68,17 @@ __device__ __forceinline__ bool kv_seq(const KvView& v, int b, KvSeq& s) {
 
 __device__ __forceinline__ void kv_flag(const KvView& v, uint32_t bit) { atomicOr(v.status, bit); }
 
-// Page id `i` of sequence b, or 0 (flagged) where the table holds none of the cache's.
-__device__ __forceinline__ int kv_page(const KvView& v, int b, int i) {
-  const int g = v.page_table[(long long)b * v.table_stride + i];
+// Page id `i` of sequence b, or 0 (flagged) where the table holds none of the cache's. The
+// check waits for the load: kv_page_raw and kv_page_ok apart let other work come between.
+__device__ __forceinline__ int kv_page_raw(const KvView& v, int b, int i) {
+  return v.page_table[(long long)b * v.table_stride + i];
+}
+__device__ __forceinline__ int kv_page_ok(const KvView& v, int g) {
   if ((unsigned)g < (unsigned)v.pages) return g;
   kv_flag(v, KV_ST_PAGE);
   return 0;
 }
+__device__ __forceinline__ int kv_page(const KvView& v, int b, int i) { return kv_page_ok(v, kv_page_raw(v, b, i)); }
 
 // Scales are powers of two or 0, so that a code times a quotient of scales is exact in
 // half precision; others are reported.

@@ -73,6 +73,11 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
       "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
       : "memory");
 }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
+  return r != 0;
+}
 __device__ __forceinline__ void commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
@@ -360,36 +365,43 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) 
     const int id = threadIdx.x - 256, cl = id % kLanes, tk = id / kLanes;
     const float inv_k = bars.k_ref > 0.f ? 128.f / bars.k_ref : 0.f;
     const int v_exp = __float_as_int(bars.v_ref) >> 23;
-    // lane g of every warp knows the page of the tile's g-th 16 tokens
-    int page = 0;
-    float fk = 0.f, vs = 0.f;
-    auto load_pages = [&](int j) {
+    // Lane g of every warp knows the page of the tile's g-th 16 tokens. A tile's page ids are
+    // asked for two tiles ahead and their scales one, so that no load of codes waits for either.
+    int page_k = -1, page_v = -1, page1 = 0, page2 = 0;  // (-1: zeros, nothing to load)
+    bool held2 = false;
+    float fk = 0.f, vs = 0.f, ks1 = 0.f, vs1 = 0.f;
+    auto ask_pages = [&](int j) {
       const int t = begin + j * kTok + (lane & 7) * 16;
-      page = 0, fk = vs = 0.f;
-      if (j < n && t < kv_hi) {
-        page = kv_page(v, b, t >> v.log_page);
-        const long long at = (long long)page * v.heads + h;
-        fk = v.k_scale[at] * inv_k, vs = v.v_scale[at];
+      held2 = j < n && t < kv_hi;
+      if (held2) page2 = kv_page_raw(v, b, t >> v.log_page);
+    };
+    auto ask_scales = [&] {
+      ks1 = vs1 = 0.f;
+      if (held2) {
+        page1 = kv_page_ok(v, page2);
+        const long long at = (long long)page1 * v.heads + h;
+        ks1 = v.k_scale[at], vs1 = v.v_scale[at];
       }
     };
+    auto take_pages = [&] { fk = ks1 * inv_k, vs = vs1, page_k = fk != 0.f ? page1 : -1, page_v = vs != 0.f ? page1 : -1; };
     uint4 cur[kPasses], nxt[kPasses];
-    float cur_f[kPasses], nxt_f[kPasses];
-    auto load = [&](int i, uint4(&x)[kPasses], float(&f)[kPasses]) {  // tile i / 2's keys (even i) or values
-      const uint8_t* from = (i & 1) ? ca.vc : ca.kc;
+    auto load = [&](int i, uint4(&x)[kPasses]) {  // tile i / 2's keys (even i) or values
+      const uint8_t* from = ((i & 1) ? ca.vc : ca.kc) + h * ca.head_stride + cl * 16;
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
         const int tl = p * kPer + tk;
-        const int g = __shfl_sync(~0u, page, tl >> 4);
-        f[p] = __shfl_sync(~0u, (i & 1) ? vs : fk, tl >> 4);
+        const int g = __shfl_sync(~0u, (i & 1) ? page_v : page_k, tl >> 4);
         const int t = begin + (i >> 1) * kTok + tl;
         x[p] = make_uint4(0, 0, 0, 0);
-        if (i < 2 * n && t < kv_hi && f[p] != 0.f)  // (beyond: not seen, and slots without a token may hold NaN codes)
-          x[p] = __ldg(reinterpret_cast<const uint4*>(from + g * ca.page_stride + h * ca.head_stride +
-                                                      (t & ((1 << v.log_page) - 1)) * ca.token_stride + cl * 16));
+        if (i < 2 * n && t < kv_hi && g >= 0)  // (beyond: not seen, and slots without a token may hold NaN codes)
+          x[p] = __ldg(reinterpret_cast<const uint4*>(from + g * ca.page_stride + (t & ((1 << v.log_page) - 1)) * ca.token_stride));
       }
     };
-    load_pages(0);
-    load(0, cur, cur_f);
+    ask_pages(0);
+    ask_scales();
+    ask_pages(1);
+    take_pages();
+    load(0, cur);
     for (int i = 0; i < 2 * n; ++i) {
       const int st = i % C::kStages;
       // (before the lists move on) the scales of values over each 16 tokens of this tile, relative to
@@ -399,8 +411,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) 
         const int e = vs != 0.f ? max((__float_as_int(vs) >> 23) - v_exp, -100) : -100;
         ps = make_float2((float)e, exp2_int(-e));
       }
-      if (i & 1) load_pages((i + 1) >> 1);
-      load(i + 1, nxt, nxt_f);
+      const float f_now = (i & 1) ? 1.f : fk;  // (the values' scale is in P)
+      if (i & 1)
+        take_pages();
+      else
+        ask_scales(), ask_pages((i >> 1) + 2);
+      load(i + 1, nxt);
       if (!wait_bar(&bars.empty[st], ((i / C::kStages) & 1) ^ 1, v)) break;
       // (this far ahead of softmax the entry of eight tiles ago has been read)
       if (!(i & 1) && id < 8) bars.v_scale[(i >> 1) & 7][id] = ps;
@@ -408,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) 
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
         const int tl = p * kPer + tk;
-        const float f = (i & 1) ? 1.f : cur_f[p];  // (the values' scale is in P)
+        const float f = __shfl_sync(~0u, f_now, tl >> 4);
         const uint32_t f2 = pack_f16(f, f);
         const uint32_t ws[4] = {cur[p].x, cur[p].y, cur[p].z, cur[p].w};
         uint32_t y[8];
@@ -430,55 +446,71 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) 
       fence_proxy_async();
       mbar_arrive(&bars.full[st]);
 #pragma unroll
-      for (int p = 0; p < kPasses; ++p) cur[p] = nxt[p], cur_f[p] = nxt_f[p];
+      for (int p = 0; p < kPasses; ++p) cur[p] = nxt[p];
     }
-  } else if (lane == 0 && n > 0) {
+  } else if (n > 0) {
     // ---------------------------------------------------------------- products
+    // The whole warp walks, so that addresses and descriptors stay in uniform registers; one
+    // lane, always the same, issues.
     constexpr uint32_t kIdS = instr_desc(kTok, false), kIdO = instr_desc(D, true);
+    const uint64_t q_desc = smem_desc(q_at, 16, 1024), k_desc = smem_desc(ring_at, 16, 1024),
+                   v_desc = smem_desc(ring_at, kTok * 128, 1024);
     auto qk = [&](int t, int slot) {
-      const uint32_t q = q_at + t * (kTileRows * D * 2), k = ring_at + slot * C::kSlot;
+      const uint64_t q = q_desc + (uint32_t)(t * (kTileRows * D * 2 / 16)), k = k_desc + (uint32_t)(slot * (C::kSlot / 16));
+      const uint32_t d = tmem + t * 128;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
-        mma_ss(tmem + t * 128, smem_desc(q + (i >> 2) * (kTileRows * 128) + (i & 3) * 32, 16, 1024),
-               smem_desc(k + (i >> 2) * (kTok * 128) + (i & 3) * 32, 16, 1024), kIdS, i > 0);
+        mma_ss(d, q + ((i >> 2) * (kTileRows * 8) + (i & 3) * 2), k + ((i >> 2) * (kTok * 8) + (i & 3) * 2), kIdS, i > 0);
     };
     auto pv = [&](int t, int slot, bool add) {
-      const uint32_t vv = ring_at + slot * C::kSlot;
+      const uint64_t vv = v_desc + (uint32_t)(slot * (C::kSlot / 16));
+      const uint32_t d = tmem + 256 + t * 128, p = tmem + t * 128;
 #pragma unroll
-      for (int i = 0; i < kTok / 16; ++i)
-        mma_ts(tmem + 256 + t * 128, tmem + t * 128 + i * 8, smem_desc(vv + i * 2048, kTok * 128, 1024), kIdO, add || i > 0);
+      for (int i = 0; i < kTok / 16; ++i) mma_ts(d, p + i * 8, vv + i * 128, kIdO, add || i > 0);
     };
+    const bool one = elect_one();
     bool ok = wait_bar(&bars.full[0], 0, v);
-    if (ok) {
-      fence_after();
+    fence_after();
+    if (ok && one) {
       for (int t = 0; t < n_sub; ++t) {
         qk(t, 0);
         commit(&bars.s_full[t]);
       }
       commit(&bars.empty[0]);
-      for (int j = 0; ok && j < n; ++j) {
-        const int vi = 2 * j + 1, ki = 2 * j + 2, vs = vi % C::kStages, ks = ki % C::kStages;
-        ok = wait_bar(&bars.full[vs], (vi / C::kStages) & 1, v);
-        for (int t = 0; ok && t < n_sub; ++t) {
-          ok = wait_bar(&bars.p_full[t], j & 1, v);
-          if (!ok) break;
-          fence_after();
+    }
+    int vs = 1, ks = 2;
+    uint32_t v_par = 0, k_par = 0;  // parities of the slots' rounds
+    for (int j = 0; ok && j < n; ++j) {
+      ok = wait_bar(&bars.full[vs], v_par, v);
+      for (int t = 0; ok && t < n_sub; ++t) {
+        ok = wait_bar(&bars.p_full[t], j & 1, v);
+        if (!ok) break;
+        fence_after();
+        if (one) {
           pv(t, vs, j > 0);
           commit(&bars.pv_done[t]);
-          if (j + 1 < n) {
-            if (t == 0) ok = wait_bar(&bars.full[ks], (ki / C::kStages) & 1, v);
-            if (!ok) break;
-            fence_after();
+        }
+        if (j + 1 < n) {
+          if (t == 0) ok = wait_bar(&bars.full[ks], k_par, v);
+          if (!ok) break;
+          fence_after();
+          if (one) {
             qk(t, ks);
             commit(&bars.s_full[t]);
           }
         }
+      }
+      if (one) {
         commit(&bars.empty[vs]);
         if (j + 1 < n) commit(&bars.empty[ks]);
       }
+      vs += 2;
+      if (vs >= C::kStages) vs -= C::kStages, v_par ^= 1;
+      ks += 2;
+      if (ks >= C::kStages) ks -= C::kStages, k_par ^= 1;
     }
     // nothing of this block's is under way once this has arrived
-    commit(&bars.end);
+    if (one) commit(&bars.end);
     wait_bar(&bars.end, 0, v);
   }
   __syncwarp();
