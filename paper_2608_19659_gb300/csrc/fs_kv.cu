@@ -406,7 +406,7 @@ int check_workspace(const void* ws, int64_t bytes, int64_t need) {
 
 }  // namespace
 
-int kv_tensor_map(CUtensorMap* m, const fs_kv_cache& c, const void* base, int rows) {
+int kv_tensor_map(CUtensorMap* m, const fs_kv_cache& c, const void* base, int rows, bool swizzled) {
   const EncodeTiled enc = encode_tiled();
   if (!enc) return say(FS_ECUDA, "the driver has no cuTensorMapEncodeTiled");
   const cuuint64_t dims[4] = {(cuuint64_t)c.dim, (cuuint64_t)c.page_tokens, (cuuint64_t)c.heads, (cuuint64_t)c.pages};
@@ -414,7 +414,8 @@ int kv_tensor_map(CUtensorMap* m, const fs_kv_cache& c, const void* base, int ro
   const cuuint32_t box[4] = {(cuuint32_t)c.dim, (cuuint32_t)rows, 1, 1}, step[4] = {1, 1, 1, 1};
   const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box, step,
                          CU_TENSOR_MAP_INTERLEAVE_NONE,
-                         c.dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                         !swizzled ? CU_TENSOR_MAP_SWIZZLE_NONE
+                         : c.dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? FS_OK : say(FS_ECUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }
@@ -512,21 +513,20 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kKvPartAt);
   a.ticket = reinterpret_cast<unsigned*>(static_cast<char*>(workspace) + kKvTicketAt);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  CUtensorMap mk, mv;
   if (p.chunk_tiles) {
-    KvChunkArgs ca{};
-    ca.a = a;
-    ca.a.min_rows = kFewRows, ca.a.max_rows = INT_MAX;
-    ca.kc = static_cast<const uint8_t*>(cache->k), ca.vc = static_cast<const uint8_t*>(cache->v);
-    ca.page_stride = cache->page_stride, ca.head_stride = cache->head_stride, ca.token_stride = cache->token_stride;
-    const cudaError_t e = launch_kv_chunk(ca, cache->dim, qu->dtype, p.chunk_tiles, st);
+    KvAttendArgs ca = a;
+    ca.min_rows = kFewRows, ca.max_rows = INT_MAX;
+    if (int rc = kv_tensor_map(&mk, *cache, cache->k, cache->page_tokens, false)) return rc;
+    if (int rc = kv_tensor_map(&mv, *cache, cache->v, cache->page_tokens, false)) return rc;
+    const cudaError_t e = launch_kv_chunk(mk, mv, ca, cache->dim, qu->dtype, p.chunk_tiles, st);
     if (e != cudaSuccess) return cuda_say(e, "launch (fs_kv_attend, chunks)");
   }
   if (p.decode) {
     a.min_rows = 0, a.max_rows = kFewRows;
-    CUtensorMap mk, mv;
     const int box = std::min(32, cache->page_tokens);
-    if (int rc = kv_tensor_map(&mk, *cache, cache->k, box)) return rc;
-    if (int rc = kv_tensor_map(&mv, *cache, cache->v, box)) return rc;
+    if (int rc = kv_tensor_map(&mk, *cache, cache->k, box, true)) return rc;
+    if (int rc = kv_tensor_map(&mv, *cache, cache->v, box, true)) return rc;
     const cudaError_t e = launch_kv_decode(mk, mv, a, cache->dim, qu->dtype, p.row_tile, p.row_blocks, p.splits, st);
     if (e != cudaSuccess) return cuda_say(e, "launch (fs_kv_attend)");
   }

@@ -45,12 +45,6 @@ struct KvAttendArgs {
   unsigned* ticket;
 };
 
-struct KvChunkArgs {
-  KvAttendArgs a;
-  const uint8_t *kc, *vc;
-  long long page_stride, head_stride, token_stride;
-};
-
 // One sequence of the batch as a kernel may use it: ranges checked, so that no
 // later index leaves its array whatever the batch's device arrays hold.
 struct KvSeq {
@@ -114,6 +108,14 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   return r;
 }
 
+// One tile of the cache into shared memory: from token slot `token` of (page, head) on.
+__device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap* m, int token, int head, int page, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(m), "r"(0), "r"(token), "r"(head), "r"(page), "r"(smem_u32(bar))
+      : "memory");
+}
+
 template <typename T>
 struct Elem;
 template <>
@@ -147,12 +149,13 @@ __device__ __forceinline__ int row_exponent(float amax) {
 __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126..127
 
 // A tensor map of a cache tensor: [pages][heads][page tokens][dim] bytes in tiles of
-// `rows` tokens of one (page, head), swizzled over its rows.
-int kv_tensor_map(CUtensorMap* m, const fs_kv_cache& c, const void* base, int rows);
+// `rows` tokens of one (page, head), its 16-byte pieces swizzled over the rows or in order.
+int kv_tensor_map(CUtensorMap* m, const fs_kv_cache& c, const void* base, int rows, bool swizzled);
 
 cudaError_t launch_kv_decode(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int dim, int dtype,
                              int row_tile, int row_blocks, int splits, cudaStream_t s);
 constexpr int kKvChunkRows = 256;  // rows of a block
-cudaError_t launch_kv_chunk(const KvChunkArgs& a, int dim, int dtype, int tiles, cudaStream_t s);
+cudaError_t launch_kv_chunk(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int dim, int dtype,
+                            int tiles, cudaStream_t s);
 
 }  // namespace fs

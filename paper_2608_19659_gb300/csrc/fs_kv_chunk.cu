@@ -8,45 +8,54 @@
 // tensor memory: S_t in 128 columns, P_t in the first 64 of the same ones (a row's thread
 // writes a column only after it has read it), O_t in dim.
 //
-// Roles of the 13 warps:
+// Roles of the 14 warps:
 //   0-3, 4-7  softmax of tile 0 / 1, a row a thread: the maximum in one pass over S, P and the
 //             row's sum in a second. P holds a token's weight times the scale of its page's values
 //             (a power of two: an addend of the exponent), m is the largest of those, so that half
 //             precision's step is relative to what counts most; the sum of weights is taken without
 //             the scales. O is rescaled only when m has grown by more than 2^8 (P, times 2^7,
 //             stays under 65504), so almost never after the first tiles
-//   8-11      codes to halves: 16-byte loads of the next tile are under way while this one is
-//             converted and stored swizzled. Keys are scaled by their page's scale over the largest
-//             (times 2^7: 448 * 2^7 < 65504 leaves small pages the most room)
+//   8-11      codes to halves, from the tiles as they came to swizzled ones. Keys are scaled by
+//             their page's scale over the largest (times 2^7: 448 * 2^7 < 65504 leaves small
+//             pages the most room)
 //   12        one thread issues every product. While tile 0's rows are in softmax the tensor
 //             cores work on tile 1, and the other way round.
+//   13        keeps tiles of codes on their way (tensor-map copies, a page each at most)
 // Bound by the tensor cores: 4 dim operations per (row, token) at the bf16 rate.
 #include "fs_kv.cuh"
 
 namespace fs {
 namespace {
 
-constexpr int kThreads = 13 * 32, kTok = 128, kTileRows = 128;
+constexpr int kThreads = 14 * 32, kTok = 128, kTileRows = 128;
 constexpr float kUp = 7.f;  // halves hold 2^(kUp + 8) of a row's largest weight, and 2^kUp of a code
 
 template <int D>
 struct Cfg {
-  static constexpr int kStages = D == 128 ? 5 : 8;
-  static constexpr int kSlot = kTok * D * 2;              // bytes of a tile of keys or values
+  static constexpr int kStages = D == 128 ? 4 : 8;        // tiles of halves
+  static constexpr int kRaw = D == 128 ? 2 : 4;           // tiles of codes
+  static constexpr int kSlot = kTok * D * 2, kRawSlot = kTok * D;
   static constexpr int kQ = 2 * kTileRows * D * 2;
-  static constexpr size_t kSmem = 1024 + kQ + (size_t)kStages * kSlot + 1024;
+  static constexpr size_t kSmem = 1024 + kQ + (size_t)kStages * kSlot + kRaw * kRawSlot + 1280;
 };
 
 struct Bars {
-  uint64_t full[8], empty[8], s_full[2], p_full[2], pv_done[2], end;
+  uint64_t full[8], empty[8], raw_full[4], raw_empty[4], s_full[2], p_full[2], pv_done[2], end;
+  float2 scale[4][8];    // per tile of codes: its own scales, and the values' scales, of its 16-token groups
   float2 v_scale[8][8];  // per tile (mod 8) and 16 tokens: log2 of the values' scale, and its reciprocal
   float k_ref, v_ref;
   uint32_t tmem;
 };
-static_assert(sizeof(Bars) <= 1024, "the barriers' share of shared memory");
+static_assert(sizeof(Bars) <= 1280, "the barriers' share of shared memory");
 
 __device__ __forceinline__ void st_shared16(uint32_t a, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+__device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
 }
 
 // Matrix descriptor of a 128-byte swizzled tile: `stride` bytes between groups of 8 rows,
@@ -178,13 +187,14 @@ __device__ __forceinline__ void row_weights(float& l, uint32_t s_at, float c, fl
 }
 
 template <int D, typename T>
-__global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) {
+__global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant__ CUtensorMap mk,
+                                                             const __grid_constant__ CUtensorMap mv, const KvAttendArgs a) {
   using C = Cfg<D>;
   extern __shared__ unsigned char raw[];
   const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
-  const uint32_t q_at = smem, ring_at = smem + C::kQ;
-  Bars& bars = *reinterpret_cast<Bars*>(raw + (smem - smem_u32(raw)) + C::kQ + (size_t)C::kStages * C::kSlot);
-  const KvAttendArgs& a = ca.a;
+  const uint32_t q_at = smem, ring_at = smem + C::kQ, raw_at = ring_at + C::kStages * C::kSlot;
+  Bars& bars = *reinterpret_cast<Bars*>(raw + (smem - smem_u32(raw)) + C::kQ + (size_t)C::kStages * C::kSlot +
+                                        C::kRaw * C::kRawSlot);
   const KvView& v = a.v;
   const int tile = gridDim.y - 1 - blockIdx.y;  // the longest walks first
   const int h = blockIdx.x % v.heads, b = blockIdx.x / v.heads;
@@ -207,6 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) 
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kStages; ++i) mbar_init(&bars.full[i], 128), mbar_init(&bars.empty[i], 1);
+    for (int i = 0; i < C::kRaw; ++i) mbar_init(&bars.raw_full[i], 1), mbar_init(&bars.raw_empty[i], 128);
     for (int t = 0; t < 2; ++t) mbar_init(&bars.s_full[t], 1), mbar_init(&bars.p_full[t], 128), mbar_init(&bars.pv_done[t], 1);
     mbar_init(&bars.end, 1);
     bars.k_ref = bars.v_ref = 0.f;
@@ -365,68 +376,36 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) 
     const int id = threadIdx.x - 256, cl = id % kLanes, tk = id / kLanes;
     const float inv_k = bars.k_ref > 0.f ? 128.f / bars.k_ref : 0.f;
     const int v_exp = __float_as_int(bars.v_ref) >> 23;
-    // Lane g of every warp knows the page of the tile's g-th 16 tokens. A tile's page ids are
-    // asked for two tiles ahead and their scales one, so that no load of codes waits for either.
-    int page_k = -1, page_v = -1, page1 = 0, page2 = 0;  // (-1: zeros, nothing to load)
-    bool held2 = false;
-    float fk = 0.f, vs = 0.f, ks1 = 0.f, vs1 = 0.f;
-    auto ask_pages = [&](int j) {
-      const int t = begin + j * kTok + (lane & 7) * 16;
-      held2 = j < n && t < kv_hi;
-      if (held2) page2 = kv_page_raw(v, b, t >> v.log_page);
-    };
-    auto ask_scales = [&] {
-      ks1 = vs1 = 0.f;
-      if (held2) {
-        page1 = kv_page_ok(v, page2);
-        const long long at = (long long)page1 * v.heads + h;
-        ks1 = v.k_scale[at], vs1 = v.v_scale[at];
-      }
-    };
-    auto take_pages = [&] { fk = ks1 * inv_k, vs = vs1, page_k = fk != 0.f ? page1 : -1, page_v = vs != 0.f ? page1 : -1; };
-    uint4 cur[kPasses], nxt[kPasses];
-    auto load = [&](int i, uint4(&x)[kPasses]) {  // tile i / 2's keys (even i) or values
-      const uint8_t* from = ((i & 1) ? ca.vc : ca.kc) + h * ca.head_stride + cl * 16;
+    for (int i = 0; i < 2 * n; ++i) {
+      const int st = i % C::kStages, rs = i % C::kRaw;
+      if (!wait_bar(&bars.raw_full[rs], (i / C::kRaw) & 1, v)) break;
+      uint4 x[kPasses];
+      float f[kPasses];
+      const bool values = i & 1;
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
         const int tl = p * kPer + tk;
-        const int g = __shfl_sync(~0u, (i & 1) ? page_v : page_k, tl >> 4);
-        const int t = begin + (i >> 1) * kTok + tl;
-        x[p] = make_uint4(0, 0, 0, 0);
-        if (i < 2 * n && t < kv_hi && g >= 0)  // (beyond: not seen, and slots without a token may hold NaN codes)
-          x[p] = __ldg(reinterpret_cast<const uint4*>(from + g * ca.page_stride + (t & ((1 << v.log_page) - 1)) * ca.token_stride));
+        const float sc = bars.scale[rs][tl >> 4].x;
+        f[p] = values ? 1.f : sc * inv_k;  // (the values' scale is in P)
+        x[p] = ld_shared16(raw_at + rs * C::kRawSlot + tl * D + cl * 16);
+        // beyond kv_hi nothing is seen, and slots without a token may hold NaN codes
+        if (begin + (i >> 1) * kTok + tl >= kv_hi || sc == 0.f) x[p] = make_uint4(0, 0, 0, 0);
       }
-    };
-    ask_pages(0);
-    ask_scales();
-    ask_pages(1);
-    take_pages();
-    load(0, cur);
-    for (int i = 0; i < 2 * n; ++i) {
-      const int st = i % C::kStages;
-      // (before the lists move on) the scales of values over each 16 tokens of this tile, relative to
-      // the largest; a scale of 0 counts as one too small to matter, and its values are stored as 0
-      float2 ps = make_float2(0.f, 0.f);
-      if (!(i & 1)) {
+      // log2 of the scales of values over each 16 tokens of a tile, relative to the largest; a scale
+      // of 0 counts as one too small to matter
+      if (!values && id < 8) {
+        const float vs = bars.scale[rs][id].y;
         const int e = vs != 0.f ? max((__float_as_int(vs) >> 23) - v_exp, -100) : -100;
-        ps = make_float2((float)e, exp2_int(-e));
+        bars.v_scale[(i >> 1) & 7][id] = make_float2((float)e, exp2_int(-e));
       }
-      const float f_now = (i & 1) ? 1.f : fk;  // (the values' scale is in P)
-      if (i & 1)
-        take_pages();
-      else
-        ask_scales(), ask_pages((i >> 1) + 2);
-      load(i + 1, nxt);
+      mbar_arrive(&bars.raw_empty[rs]);
       if (!wait_bar(&bars.empty[st], ((i / C::kStages) & 1) ^ 1, v)) break;
-      // (this far ahead of softmax the entry of eight tiles ago has been read)
-      if (!(i & 1) && id < 8) bars.v_scale[(i >> 1) & 7][id] = ps;
       const uint32_t slot = ring_at + st * C::kSlot;
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
         const int tl = p * kPer + tk;
-        const float f = __shfl_sync(~0u, f_now, tl >> 4);
-        const uint32_t f2 = pack_f16(f, f);
-        const uint32_t ws[4] = {cur[p].x, cur[p].y, cur[p].z, cur[p].w};
+        const uint32_t f2 = pack_f16(f[p], f[p]);
+        const uint32_t ws[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
         uint32_t y[8];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -445,9 +424,52 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) 
       }
       fence_proxy_async();
       mbar_arrive(&bars.full[st]);
-#pragma unroll
-      for (int p = 0; p < kPasses; ++p) cur[p] = nxt[p];
     }
+  } else if (w == 13) {
+    // ---------------------------------------------------------------- codes from the cache
+    // Lane g holds the page of a tile's g-th box of a page's tokens. Page ids are asked for two tiles
+    // ahead and their scales one, so that no copy waits for either.
+    const int log_p = v.log_page, boxes = kTok >> log_p;
+    int page0 = 0, page1 = 0, page2 = 0;
+    bool held0 = false, held1 = false, held2 = false;
+    float ks0 = 0.f, vs0 = 0.f, ks1 = 0.f, vs1 = 0.f;
+    auto ask_pages = [&](int j) {
+      const int t = begin + j * kTok + (lane << log_p);
+      held2 = j < n && lane < boxes && t < kv_hi;
+      if (held2) page2 = kv_page_raw(v, b, t >> log_p);
+    };
+    auto ask_scales = [&] {
+      held1 = held2, ks1 = vs1 = 0.f;
+      if (held1) {
+        page1 = kv_page_ok(v, page2);
+        const long long at = (long long)page1 * v.heads + h;
+        ks1 = v.k_scale[at], vs1 = v.v_scale[at];
+      }
+    };
+    ask_pages(0);
+    ask_scales();
+    ask_pages(1);
+    int i = 0;
+    for (; i < 2 * n; ++i) {
+      const int rs = i % C::kRaw;
+      if (!(i & 1)) {
+        held0 = held1, page0 = page1, ks0 = ks1, vs0 = vs1;
+        ask_scales();
+        ask_pages((i >> 1) + 2);
+      }
+      bool ok = wait_bar(&bars.raw_empty[rs], ((i / C::kRaw) & 1) ^ 1, v);
+      if (!__all_sync(~0u, ok)) break;
+      const uint32_t held = __ballot_sync(~0u, held0);
+      const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p), ks = __shfl_sync(~0u, ks0, (lane << 4) >> log_p);
+      if (lane < 8) bars.scale[rs][lane] = make_float2((i & 1) ? vs : ks, vs);
+      __syncwarp();
+      if (lane == 0) mbar_expect_tx(&bars.raw_full[rs], (uint32_t)(__popc(held) * D) << log_p);
+      __syncwarp();
+      if (held0)
+        tma_tile(raw_at + rs * C::kRawSlot + ((lane * D) << log_p), (i & 1) ? &mv : &mk, 0, h, page0, &bars.raw_full[rs]);
+    }
+    if (i < 2 * n)  // a wait ran out: the copies under way first (with the same limit)
+      for (int k = max(0, i - C::kRaw); k < i; ++k) mbar_wait(&bars.raw_full[k % C::kRaw], (k / C::kRaw) & 1, kWaitLimitNs);
   } else if (n > 0) {
     // ---------------------------------------------------------------- products
     // The whole warp walks, so that addresses and descriptors stay in uniform registers; one
@@ -521,20 +543,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const KvChunkArgs ca) 
 }
 
 template <int D, typename T>
-cudaError_t launch(const KvChunkArgs& a, int tiles, cudaStream_t s) {
+cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int tiles, cudaStream_t s) {
   static const cudaError_t limit = raise_smem_limit(reinterpret_cast<const void*>(k_kv_chunk<D, T>), Cfg<D>::kSmem);
   if (limit != cudaSuccess) return limit;
-  k_kv_chunk<D, T><<<dim3(a.a.v.heads * a.a.v.batch, tiles), kThreads, Cfg<D>::kSmem, s>>>(a);
+  k_kv_chunk<D, T><<<dim3(a.v.heads * a.v.batch, tiles), kThreads, Cfg<D>::kSmem, s>>>(mk, mv, a);
   note_launch();
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_kv_chunk(const KvChunkArgs& a, int dim, int dtype, int tiles, cudaStream_t s) {
+cudaError_t launch_kv_chunk(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int dim, int dtype,
+                            int tiles, cudaStream_t s) {
   const bool h = dtype == FS_KV_FP16;
-  if (dim == 128) return h ? launch<128, __half>(a, tiles, s) : launch<128, __nv_bfloat16>(a, tiles, s);
-  return h ? launch<64, __half>(a, tiles, s) : launch<64, __nv_bfloat16>(a, tiles, s);
+  if (dim == 128) return h ? launch<128, __half>(mk, mv, a, tiles, s) : launch<128, __nv_bfloat16>(mk, mv, a, tiles, s);
+  return h ? launch<64, __half>(mk, mv, a, tiles, s) : launch<64, __nv_bfloat16>(mk, mv, a, tiles, s);
 }
 
 }  // namespace fs

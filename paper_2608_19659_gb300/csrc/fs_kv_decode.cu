@@ -28,14 +28,6 @@ namespace {
 constexpr int kWarps = 4, kStages = 3, kTile = 32;
 constexpr float kUp = 15.f;  // log2 of the largest weight: near the top of half precision
 
-__device__ __forceinline__ void tma_tile(void* dst, const CUtensorMap* m, int token, int head, int page, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-          smem_u32(dst)),
-      "l"(m), "r"(0), "r"(token), "r"(head), "r"(page), "r"(smem_u32(bar))
-      : "memory");
-}
-
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
   asm(
@@ -132,7 +124,7 @@ __global__ void __launch_bounds__(kWarps * 32)
   };
   auto issue = [&](int i, int p0, int p1) {  // lane 0: tile i into its stage
     const int st = i % kStages, t = c0 + (w + i * kWarps) * kTile, slot = t & ((1 << v.log_page) - 1);
-    unsigned char* kd = my_ring + st * (2 * kTileBytes);
+    const uint32_t kd = smem_u32(my_ring) + st * (2 * kTileBytes);
     uint64_t* bar = &bars[w][st];
     mbar_expect_tx(bar, 2 * kTileBytes);
     tma_tile(kd, &mk, slot, h, p0, bar);
