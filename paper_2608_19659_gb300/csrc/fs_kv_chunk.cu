@@ -27,7 +27,7 @@
 namespace fs {
 namespace {
 
-constexpr int kThreads = 14 * 32, kTok = 128, kTileRows = 128;
+constexpr int kThreads = 16 * 32, kTok = 128, kTileRows = 128;
 constexpr float kUp = 7.f;  // halves hold 2^(kUp + 8) of a row's largest weight, and 2^kUp of a code
 
 template <int D>
@@ -41,7 +41,8 @@ struct Cfg {
 
 struct Bars {
   uint64_t full[8], empty[8], raw_full[4], raw_empty[4], s_full[2], p_full[2], pv_done[2], end;
-  float2 scale[4][8];    // per tile of codes: its own scales, and the values' scales, of its 16-token groups
+  float2 scale[4][8];    // per tile of codes and 16 tokens: what keys are multiplied by (two halves), the values' scale
+  uint32_t cut[4];       // per tile of codes: some tokens' values are to be 0
   float2 v_scale[8][8];  // per tile (mod 8) and 16 tokens: log2 of the values' scale, and its reciprocal
   float k_ref, v_ref;
   uint32_t tmem;
@@ -52,10 +53,32 @@ __device__ __forceinline__ void st_shared16(uint32_t a, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
-__device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+__device__ __forceinline__ float2 ld_shared8(uint32_t a) {
+  float2 v;
+  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
   return v;
+}
+
+// Two floats at a time (one instruction each).
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
+      " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
 // Matrix descriptor of a 128-byte swizzled tile: `stride` bytes between groups of 8 rows,
@@ -106,14 +129,12 @@ __device__ __forceinline__ void tmem_ld32(uint32_t (&r)[32], uint32_t a) {
       : "r"(a)
       : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t a, const uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_ld16(uint32_t (&r)[16], uint32_t a) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
-      "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(a),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-      "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
-      "r"(r[30]), "r"(r[31])
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(a)
       : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t (&r)[16]) {
@@ -131,59 +152,24 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, const K
   return false;
 }
 
-// A row's largest log2 weight (times its value scale) among columns [lo, hi] of S (all of them
-// with kWhole), into top. The walk over 32 columns at a time is a loop: unrolled whole, the
-// two passes overflow the instruction cache.
+// A row of S: its largest log2 weight (times its value scale) among columns [lo, hi] (all of
+// them with kWhole); masked columns become -infinity.
 template <bool kWhole>
-__device__ __forceinline__ void row_top(float& top, uint32_t s_at, float c, const float2* v_scale, int lo, int hi) {
-#pragma unroll 1
-  for (int k = 0; k < 4; ++k) {
-    uint32_t x[32];
-    tmem_ld32(x, s_at + 32 * k);
-    wait_ld();
+__device__ __forceinline__ float row_top(float (&x)[kTok], float c, const float2* v_scale, int lo, int hi) {
+  float top = -INFINITY;
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      float most = -INFINITY;
+  for (int g = 0; g < kTok / 16; ++g) {
+    if (!kWhole) {
 #pragma unroll
-      for (int i = 16 * g; i < 16 * g + 16; ++i) {
-        const float y = __uint_as_float(x[i]);
-        most = fmaxf(most, kWhole || (32 * k + i <= hi && 32 * k + i >= lo) ? y : -INFINITY);
-      }
-      if (kWhole || most > -INFINITY) top = fmaxf(top, fmaf(most, c, v_scale[2 * k + g].x));
+      for (int i = 16 * g; i < 16 * g + 16; ++i)
+        if (i > hi || i < lo) x[i] = -INFINITY;
     }
+    const float* y = x + 16 * g;
+    const float m0 = max3(max3(max3(y[0], y[1], y[2]), max3(y[3], y[4], y[5]), max3(y[6], y[7], y[8])),
+                          max3(y[9], y[10], y[11]), max3(max3(y[12], y[13], y[14]), y[15], y[15]));
+    if (kWhole || m0 > -INFINITY) top = fmaxf(top, fmaf(m0, c, v_scale[g].x));
   }
-}
-
-// P = 2^(c S + log2 of the value scale - off) in half precision over S, and the row's sum of
-// weights (without the scales) added to l.
-template <bool kWhole>
-__device__ __forceinline__ void row_weights(float& l, uint32_t s_at, float c, float off, const float2* v_scale, int lo,
-                                            int hi) {
-#pragma unroll 1
-  for (int k = 0; k < 4; ++k) {
-    uint32_t x[32], p[16];
-    tmem_ld32(x, s_at + 32 * k);
-    wait_ld();
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const float2 vs = v_scale[2 * k + g];
-      const float off_g = vs.x + kUp - off;
-      float l0 = 0.f, l1 = 0.f;
-#pragma unroll
-      for (int i = 8 * g; i < 8 * g + 8; ++i) {
-        float y0 = ex2(fmaf(__uint_as_float(x[2 * i]), c, off_g)), y1 = ex2(fmaf(__uint_as_float(x[2 * i + 1]), c, off_g));
-        if (!kWhole) {
-          const int col = 32 * k + 2 * i;
-          y0 = col <= hi && col >= lo ? y0 : 0.f;
-          y1 = col + 1 <= hi && col + 1 >= lo ? y1 : 0.f;
-        }
-        l0 += y0, l1 += y1;
-        p[i] = pack_f16(y0, y1);
-      }
-      l = fmaf(l0 + l1, vs.y * (1.f / 128.f), l);
-    }
-    tmem_st16(s_at + 16 * k, p);
-  }
+  return top;
 }
 
 template <int D, typename T>
@@ -284,8 +270,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
   fence_after();
   const uint32_t tmem = bars.tmem;
 
+  // Registers: 512 threads x 128 at launch; 128 x (192 + 192 + 80 + 48) from here on.
   if (w < 8) {
     // ---------------------------------------------------------------- softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
     const int t = w >> 2;
     const int r = r0 + threadIdx.x;
     if (t < n_sub) {
@@ -307,11 +295,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
         ok = wait_bar(&bars.s_full[t], j & 1, v);
         if (!__all_sync(~0u, ok)) break;
         fence_after();
-        float top = -INFINITY;
-        if (whole)
-          row_top<true>(top, s_at, c, bars.v_scale[j & 7], 0, 0);
-        else
-          row_top<false>(top, s_at, c, bars.v_scale[j & 7], c_lo, c_hi);
+        float x[kTok];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) tmem_ld32(reinterpret_cast<uint32_t(&)[32]>(x[32 * k]), s_at + 32 * k);
+        wait_ld();
+        const float2* v_scale = bars.v_scale[j & 7];
+        const float top = whole ? row_top<true>(x, c, v_scale, 0, 0) : row_top<false>(x, c, v_scale, c_lo, c_hi);
         const bool grow = top > m + 8.f || (m == -INFINITY && top > m);
         if (__any_sync(~0u, grow)) {
           const float f = grow ? ex2(m - top) : 1.f;
@@ -321,22 +310,40 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
             ok = wait_bar(&bars.pv_done[t], (j - 1) & 1, v);
             if (!__all_sync(~0u, ok)) break;
             fence_after();
-#pragma unroll
-            for (int k = 0; k < D / 32; ++k) {
-              uint32_t x[32];
-              tmem_ld32(x, o_at + 32 * k);
+#pragma unroll 1
+            for (int k = 0; k < D / 16; ++k) {
+              uint32_t y[16];
+              tmem_ld16(y, o_at + 16 * k);
               wait_ld();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
-              tmem_st32(o_at + 32 * k, x);
+              for (int i = 0; i < 16; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * f);
+              tmem_st16(o_at + 16 * k, y);
             }
           }
         }
         const float off = m == -INFINITY ? 0.f : m;  // (m: log2 of weight times scale, without kUp)
-        if (whole)
-          row_weights<true>(l, s_at, c, off, bars.v_scale[j & 7], 0, 0);
-        else
-          row_weights<false>(l, s_at, c, off, bars.v_scale[j & 7], c_lo, c_hi);
+        // P = 2^(c S + log2 of the value scale - m), and the row's sum of weights without the scales
+        // (a masked column: c * -infinity, but c may be 0)
+        const float cc = whole ? c : fmaxf(c, 0x1p-126f);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t p[16];
+#pragma unroll
+          for (int g = 2 * k; g < 2 * k + 2; ++g) {
+            const float2 vs = v_scale[g];
+            const float off_g = vs.x + kUp - off;
+            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int i = 16 * g; i < 16 * g + 16; i += 2) {
+              float2 y = fma2(make_float2(x[i], x[i + 1]), make_float2(cc, cc), make_float2(off_g, off_g));
+              y.x = ex2(y.x), y.y = ex2(y.y);
+              sum = add2(sum, y);
+              p[(i - 32 * k) / 2] = pack_f16(y.x, y.y);
+            }
+            l = fmaf(sum.x + sum.y, vs.y * (1.f / 128.f), l);
+          }
+          tmem_st16(s_at + 16 * k, p);
+        }
         wait_st();
         fence_before();
         mbar_arrive(&bars.p_full[t]);
@@ -347,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
         fence_after();
       }
       ok = __all_sync(~0u, ok);
-      const float inv = l > 0.f ? bars.v_ref * (1.f / 128.f) / l : 0.f;
+      const float inv = bars.v_ref * (1.f / 128.f) / l;
       T* to = static_cast<T*>(a.out) + (long long)(s.first + r / v.group) * a.out_token + (h * v.group + r % v.group) * a.out_head;
 #pragma unroll
       for (int k = 0; k < D / 32; ++k) {
@@ -362,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
             uint32_t y[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-              y[u] = l > 0.f ? Elem<T>::pack(__uint_as_float(x[8 * i + 2 * u]) * inv, __uint_as_float(x[8 * i + 2 * u + 1]) * inv) : 0u;
+              y[u] = l != 0.f ? Elem<T>::pack(__uint_as_float(x[8 * i + 2 * u]) * inv, __uint_as_float(x[8 * i + 2 * u + 1]) * inv) : 0u;
             *reinterpret_cast<uint4*>(to + 32 * k + 8 * i) = make_uint4(y[0], y[1], y[2], y[3]);
           }
         }
@@ -370,66 +377,73 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
     }
   } else if (w < 12) {
     // ---------------------------------------------------------------- codes to halves
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     constexpr int kLanes = D / 16;               // lanes a token, 16 codes each
     constexpr int kPer = 128 / kLanes;           // tokens a pass
     constexpr int kPasses = kTok / kPer;         // 8 (dim 128) or 4 (dim 64)
     const int id = threadIdx.x - 256, cl = id % kLanes, tk = id / kLanes;
-    const float inv_k = bars.k_ref > 0.f ? 128.f / bars.k_ref : 0.f;
     const int v_exp = __float_as_int(bars.v_ref) >> 23;
+    // A lane's 16 codes become the 16-byte chunks 2 (cl mod 4) and + 1 of the token's row in block
+    // cl / 4; lanes of the second block begin with the other one, so that a row's lanes meet every
+    // bank once.
+    const int sw = D == 128 ? cl >> 2 : 0;
+    const uint32_t from = raw_at + tk * D + cl * 16, to = (cl >> 2) * (kTok * 128) + tk * 128;
+    const uint32_t c0 = (((cl & 3) * 2 + sw) ^ (tk & 7)) << 4, c1 = (((cl & 3) * 2 + (sw ^ 1)) ^ (tk & 7)) << 4;
     for (int i = 0; i < 2 * n; ++i) {
       const int st = i % C::kStages, rs = i % C::kRaw;
       if (!wait_bar(&bars.raw_full[rs], (i / C::kRaw) & 1, v)) break;
-      uint4 x[kPasses];
-      float f[kPasses];
+      uint32_t x[kPasses][4], f2[kPasses];
       const bool values = i & 1;
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
-        const int tl = p * kPer + tk;
-        const float sc = bars.scale[rs][tl >> 4].x;
-        f[p] = values ? 1.f : sc * inv_k;  // (the values' scale is in P)
-        x[p] = ld_shared16(raw_at + rs * C::kRawSlot + tl * D + cl * 16);
-        // beyond kv_hi nothing is seen, and slots without a token may hold NaN codes
-        if (begin + (i >> 1) * kTok + tl >= kv_hi || sc == 0.f) x[p] = make_uint4(0, 0, 0, 0);
+        const uint32_t at = from + rs * C::kRawSlot + p * (kPer * D);
+        const float2 u = ld_shared8(at + 8 * sw), z = ld_shared8(at + 8 * (sw ^ 1));
+        x[p][0] = __float_as_uint(u.x), x[p][1] = __float_as_uint(u.y);
+        x[p][2] = __float_as_uint(z.x), x[p][3] = __float_as_uint(z.y);
+        if (!values) f2[p] = __float_as_uint(bars.scale[rs][(p * kPer + tk) >> 4].x);
       }
-      // log2 of the scales of values over each 16 tokens of a tile, relative to the largest; a scale
-      // of 0 counts as one too small to matter
-      if (!values && id < 8) {
+      if (values) {
+        // tokens that no row sees (their slots may hold NaN codes), and values whose scale is 0
+        if (bars.cut[rs]) {
+#pragma unroll
+          for (int p = 0; p < kPasses; ++p) {
+            const int tl = p * kPer + tk;
+            if (begin + (i >> 1) * kTok + tl >= kv_hi || bars.scale[rs][tl >> 4].y == 0.f) x[p][0] = x[p][1] = x[p][2] = x[p][3] = 0;
+          }
+        }
+      } else if (id < 8) {
+        // log2 of the scales of values over each 16 tokens of the tile, relative to the largest; a
+        // scale of 0 counts as one too small to matter
         const float vs = bars.scale[rs][id].y;
         const int e = vs != 0.f ? max((__float_as_int(vs) >> 23) - v_exp, -100) : -100;
         bars.v_scale[(i >> 1) & 7][id] = make_float2((float)e, exp2_int(-e));
       }
       mbar_arrive(&bars.raw_empty[rs]);
       if (!wait_bar(&bars.empty[st], ((i / C::kStages) & 1) ^ 1, v)) break;
-      const uint32_t slot = ring_at + st * C::kSlot;
+      const uint32_t row = ring_at + st * C::kSlot + to;
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
-        const int tl = p * kPer + tk;
-        const uint32_t f2 = pack_f16(f[p], f[p]);
-        const uint32_t ws[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
         uint32_t y[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t e0 = e4m3x2_to_f16x2(ws[k]), e1 = e4m3x2_to_f16x2_hi(ws[k]);
-          asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(y[2 * k]) : "r"(e0), "r"(f2));
-          asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(y[2 * k + 1]) : "r"(e1), "r"(f2));
+        for (int k = 0; k < 4; ++k) y[2 * k] = e4m3x2_to_f16x2(x[p][k]), y[2 * k + 1] = e4m3x2_to_f16x2_hi(x[p][k]);
+        if (!values) {  // (the values' scale is in P)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(y[k]) : "r"(f2[p]));
         }
-        // 16-byte chunks 2 (cl mod 4) and + 1 of the token's row in block cl / 4; lanes of the second
-        // block begin with the other one, so that a row's lanes meet every bank once
-        const uint32_t row = slot + (cl >> 2) * (kTok * 128) + tl * 128;
-        const int sw = D == 128 ? cl >> 2 : 0;
-        const uint32_t c0 = (((cl & 3) * 2 + sw) ^ (tl & 7)) << 4, c1 = (((cl & 3) * 2 + (sw ^ 1)) ^ (tl & 7)) << 4;
-        const uint4 y0 = make_uint4(y[0], y[1], y[2], y[3]), y1 = make_uint4(y[4], y[5], y[6], y[7]);
-        st_shared16(row + c0, sw ? y1 : y0);
-        st_shared16(row + c1, sw ? y0 : y1);
+        st_shared16(row + p * (kPer * 128) + c0, make_uint4(y[0], y[1], y[2], y[3]));
+        st_shared16(row + p * (kPer * 128) + c1, make_uint4(y[4], y[5], y[6], y[7]));
       }
       fence_proxy_async();
       mbar_arrive(&bars.full[st]);
     }
-  } else if (w == 13) {
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (w == 13) {
     // ---------------------------------------------------------------- codes from the cache
     // Lane g holds the page of a tile's g-th box of a page's tokens. Page ids are asked for two tiles
     // ahead and their scales one, so that no copy waits for either.
     const int log_p = v.log_page, boxes = kTok >> log_p;
+    const float inv_k = bars.k_ref > 0.f ? 128.f / bars.k_ref : 0.f;
     int page0 = 0, page1 = 0, page2 = 0;
     bool held0 = false, held1 = false, held2 = false;
     float ks0 = 0.f, vs0 = 0.f, ks1 = 0.f, vs1 = 0.f;
@@ -461,7 +475,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
       if (!__all_sync(~0u, ok)) break;
       const uint32_t held = __ballot_sync(~0u, held0);
       const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p), ks = __shfl_sync(~0u, ks0, (lane << 4) >> log_p);
-      if (lane < 8) bars.scale[rs][lane] = make_float2((i & 1) ? vs : ks, vs);
+      if (lane < 8) bars.scale[rs][lane] = make_float2(__uint_as_float(pack_f16(ks * inv_k, ks * inv_k)), vs);
+      // (a group beyond kv_hi has the scale 0 too)
+      const bool cut = __any_sync(~0u, lane < 8 && vs == 0.f) || begin + ((i >> 1) + 1) * kTok > kv_hi;
+      if (lane == 0) bars.cut[rs] = cut;
       __syncwarp();
       if (lane == 0) mbar_expect_tx(&bars.raw_full[rs], (uint32_t)(__popc(held) * D) << log_p);
       __syncwarp();
@@ -470,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
     }
     if (i < 2 * n)  // a wait ran out: the copies under way first (with the same limit)
       for (int k = max(0, i - C::kRaw); k < i; ++k) mbar_wait(&bars.raw_full[k % C::kRaw], (k / C::kRaw) & 1, kWaitLimitNs);
-  } else if (n > 0) {
+    } else if (w == 12 && n > 0) {
     // ---------------------------------------------------------------- products
     // The whole warp walks, so that addresses and descriptors stay in uniform registers; one
     // lane, always the same, issues.
@@ -534,6 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
     // nothing of this block's is under way once this has arrived
     if (one) commit(&bars.end);
     wait_bar(&bars.end, 0, v);
+  }
   }
   __syncwarp();
   fence_before();
