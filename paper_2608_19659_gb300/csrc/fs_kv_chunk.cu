@@ -268,7 +268,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
   fence_before();
   __syncthreads();
   fence_after();
-  const uint32_t tmem = bars.tmem;
+  // (the whole of tensor memory is this block's: its columns begin at 0)
+  constexpr uint32_t tmem = 0;
 
   // Registers: 512 threads x 128 at launch; 128 x (192 + 192 + 80 + 48) from here on.
   if (w < 8) {
@@ -489,29 +490,32 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
       for (int k = max(0, i - C::kRaw); k < i; ++k) mbar_wait(&bars.raw_full[k % C::kRaw], (k / C::kRaw) & 1, kWaitLimitNs);
     } else if (w == 12 && n > 0) {
     // ---------------------------------------------------------------- products
-    // The whole warp walks, so that addresses and descriptors stay in uniform registers; one
-    // lane, always the same, issues.
+    // The whole warp walks, with values and conditions that are the same in every lane, so that
+    // addresses and descriptors stay in uniform registers: beside eight busy softmax warps every
+    // instruction between two products shows. One lane, always the same, issues.
+    const int n_u = __shfl_sync(~0u, n, 0), n_sub_u = __shfl_sync(~0u, n_sub, 0);
+    auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, wait_bar(bar, parity, v)) != 0; };
     constexpr uint32_t kIdS = instr_desc(kTok, false), kIdO = instr_desc(D, true);
     const uint64_t q_desc = smem_desc(q_at, 16, 1024), k_desc = smem_desc(ring_at, 16, 1024),
                    v_desc = smem_desc(ring_at, kTok * 128, 1024);
     auto qk = [&](int t, int slot) {
       const uint64_t q = q_desc + (uint32_t)(t * (kTileRows * D * 2 / 16)), k = k_desc + (uint32_t)(slot * (C::kSlot / 16));
-      const uint32_t d = tmem + t * 128;
+      const uint32_t d = t * 128;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
         mma_ss(d, q + ((i >> 2) * (kTileRows * 8) + (i & 3) * 2), k + ((i >> 2) * (kTok * 8) + (i & 3) * 2), kIdS, i > 0);
     };
     auto pv = [&](int t, int slot, bool add) {
       const uint64_t vv = v_desc + (uint32_t)(slot * (C::kSlot / 16));
-      const uint32_t d = tmem + 256 + t * 128, p = tmem + t * 128;
+      const uint32_t d = 256 + t * 128, p = t * 128;
 #pragma unroll
       for (int i = 0; i < kTok / 16; ++i) mma_ts(d, p + i * 8, vv + i * 128, kIdO, add || i > 0);
     };
     const bool one = elect_one();
-    bool ok = wait_bar(&bars.full[0], 0, v);
+    bool ok = wait_all(&bars.full[0], 0);
     fence_after();
     if (ok && one) {
-      for (int t = 0; t < n_sub; ++t) {
+      for (int t = 0; t < n_sub_u; ++t) {
         qk(t, 0);
         commit(&bars.s_full[t]);
       }
@@ -519,18 +523,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
     }
     int vs = 1, ks = 2;
     uint32_t v_par = 0, k_par = 0;  // parities of the slots' rounds
-    for (int j = 0; ok && j < n; ++j) {
-      ok = wait_bar(&bars.full[vs], v_par, v);
-      for (int t = 0; ok && t < n_sub; ++t) {
-        ok = wait_bar(&bars.p_full[t], j & 1, v);
+    for (int j = 0; ok && j < n_u; ++j) {
+      ok = wait_all(&bars.full[vs], v_par);
+      for (int t = 0; ok && t < n_sub_u; ++t) {
+        ok = wait_all(&bars.p_full[t], j & 1);
         if (!ok) break;
         fence_after();
         if (one) {
           pv(t, vs, j > 0);
           commit(&bars.pv_done[t]);
         }
-        if (j + 1 < n) {
-          if (t == 0) ok = wait_bar(&bars.full[ks], k_par, v);
+        if (j + 1 < n_u) {
+          if (t == 0) ok = wait_all(&bars.full[ks], k_par);
           if (!ok) break;
           fence_after();
           if (one) {
@@ -541,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
       }
       if (one) {
         commit(&bars.empty[vs]);
-        if (j + 1 < n) commit(&bars.empty[ks]);
+        if (j + 1 < n_u) commit(&bars.empty[ks]);
       }
       vs += 2;
       if (vs >= C::kStages) vs -= C::kStages, v_par ^= 1;
