@@ -40,7 +40,7 @@ struct Cfg {
 };
 
 struct Bars {
-  uint64_t full[8], empty[8], raw_full[4], raw_empty[4], s_full[2], p_full[2], pv_done[2], end;
+  uint64_t full[8], empty[8], raw_full[4], raw_empty[4], s_full[2], p_full[2][2], pv_done[2], end;
   float2 scale[4][8];    // per tile of codes and 16 tokens: what keys are multiplied by (two halves), the values' scale
   uint32_t cut[4];       // per tile of codes: some tokens' values are to be 0
   float2 v_scale[8][8];  // per tile (mod 8) and 16 tokens: log2 of the values' scale, and its reciprocal
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kStages; ++i) mbar_init(&bars.full[i], 128), mbar_init(&bars.empty[i], 1);
     for (int i = 0; i < C::kRaw; ++i) mbar_init(&bars.raw_full[i], 1), mbar_init(&bars.raw_empty[i], 128);
-    for (int t = 0; t < 2; ++t) mbar_init(&bars.s_full[t], 1), mbar_init(&bars.p_full[t], 128), mbar_init(&bars.pv_done[t], 1);
+    for (int t = 0; t < 2; ++t) mbar_init(&bars.s_full[t], 1), mbar_init(&bars.p_full[t][0], 128), mbar_init(&bars.p_full[t][1], 128), mbar_init(&bars.pv_done[t], 1);
     mbar_init(&bars.end, 1);
     bars.k_ref = bars.v_ref = 0.f;
   }
@@ -344,10 +344,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
             l = fmaf(sum.x + sum.y, vs.y * (1.f / 128.f), l);
           }
           tmem_st16(s_at + 16 * k, p);
+          if (k & 1) {  // half of P: its product begins while the other half is computed
+            wait_st();
+            fence_before();
+            mbar_arrive(&bars.p_full[t][k >> 1]);
+          }
         }
-        wait_st();
-        fence_before();
-        mbar_arrive(&bars.p_full[t]);
       }
       // ------------------------------------------------------------ result
       if (ok && n > 0) {
@@ -505,11 +507,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
       for (int i = 0; i < D / 16; ++i)
         mma_ss(d, q + ((i >> 2) * (kTileRows * 8) + (i & 3) * 2), k + ((i >> 2) * (kTok * 8) + (i & 3) * 2), kIdS, i > 0);
     };
-    auto pv = [&](int t, int slot, bool add) {
+    auto pv = [&](int t, int slot, int half, bool add) {
       const uint64_t vv = v_desc + (uint32_t)(slot * (C::kSlot / 16));
       const uint32_t d = 256 + t * 128, p = t * 128;
 #pragma unroll
-      for (int i = 0; i < kTok / 16; ++i) mma_ts(d, p + i * 8, vv + i * 128, kIdO, add || i > 0);
+      for (int i = 0; i < kTok / 32; ++i)
+        mma_ts(d, p + (half * (kTok / 32) + i) * 8, vv + (half * (kTok / 32) + i) * 128, kIdO, add || half || i > 0);
     };
     const bool one = elect_one();
     bool ok = wait_all(&bars.full[0], 0);
@@ -526,13 +529,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
     for (int j = 0; ok && j < n_u; ++j) {
       ok = wait_all(&bars.full[vs], v_par);
       for (int t = 0; ok && t < n_sub_u; ++t) {
-        ok = wait_all(&bars.p_full[t], j & 1);
-        if (!ok) break;
-        fence_after();
-        if (one) {
-          pv(t, vs, j > 0);
-          commit(&bars.pv_done[t]);
+        for (int half = 0; ok && half < 2; ++half) {
+          ok = wait_all(&bars.p_full[t][half], j & 1);
+          fence_after();
+          if (ok && one) pv(t, vs, half, j > 0);
         }
+        if (!ok) break;
+        if (one) commit(&bars.pv_done[t]);
         if (j + 1 < n_u) {
           if (t == 0) ok = wait_all(&bars.full[ks], k_par);
           if (!ok) break;
