@@ -342,7 +342,7 @@ int sm_count_of(int dev) {
 // How an attend call is cut up (see k_kv_decode): rows of a (sequence, key head) in tiles
 // of row_tile, the cache axis in parts of `split` tokens.
 struct KvPlan {
-  int row_tile, row_blocks, split, splits;
+  int row_tile, row_blocks, split, splits, tickets;
   int chunk_tiles;  // blocks of k_kv_chunk a (sequence, key head); 0: no sequence has that many rows
   int decode;       // whether some sequence can have few rows
   size_t part_floats;
@@ -354,7 +354,7 @@ constexpr int kFewRows = 64;
 
 constexpr int kMinSplit = 256, kMaxSplit = 4096;
 
-KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int sms) {
+KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int window, int sms) {
   KvPlan p{};
   const long long all = (long long)std::max(1, b->max_new) * (q_heads / c->heads);
   const int rows = (int)std::min<long long>(all, kFewRows);
@@ -364,14 +364,20 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int sms)
   p.row_tile = rows <= 8 ? 8 : 16;
   p.row_blocks = (rows + p.row_tile - 1) / p.row_tile;
   const long long items = (long long)std::max(1, b->batch) * c->heads * p.row_blocks;
-  const int len = std::max(1, b->max_length);
+  // (a window's tiles may begin up to 31 tokens early)
+  const int len = std::max(1, window ? (int)std::min<long long>(b->max_length, (long long)window + b->max_new + 30) : b->max_length);
+  p.tickets = 1;
   if (items > kKvTickets) {
     p.split = (len + 127) / 128 * 128;
     p.splits = 1;
   } else {
-    const long long want = std::max(1ll, (4ll * sms + items - 1) / items);
+    // a part for every block that is resident at once; more of them while they are few an item,
+    // because sequences differ in length
+    const long long want = std::max(1ll, ((items < sms ? 2ll : 4ll) * sms + items - 1) / items);
     p.split = std::clamp((int)((len + want - 1) / want + 127) / 128 * 128, kMinSplit, kMaxSplit);
     p.splits = (len + p.split - 1) / p.split;
+    const int groups = (p.splits + kKvFan - 1) / kKvFan;
+    if (groups > 1 && items * (1 + groups) <= kKvTickets) p.tickets = 1 + groups;
   }
   p.part_floats = p.decode && p.splits > 1 ? (size_t)items * p.splits * p.row_tile * (c->dim + 2) : 0;
   return p;
@@ -499,7 +505,7 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   if (int rc = check_rows(qu->out, "out")) return rc;
   int sms = 0;
   if (int rc = device_sms(&sms)) return rc;
-  const KvPlan p = plan_of(cache, batch, qu->q_heads, sms);
+  const KvPlan p = plan_of(cache, batch, qu->q_heads, qu->window, sms);
   if (int rc = check_workspace(workspace, workspace_bytes, (int64_t)(kKvPartAt + 4 * p.part_floats))) return rc;
   if (p.chunk_tiles > 65535) return say(FS_EINVAL, "max_new = %d: too many rows for one call", batch->max_new);
 
@@ -510,6 +516,7 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   a.scale_log2 = qu->scale * 1.44269504f;
   a.window = qu->window;
   a.split = p.split;
+  a.tickets = p.tickets;
   a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kKvPartAt);
   a.ticket = reinterpret_cast<unsigned*>(static_cast<char*>(workspace) + kKvTicketAt);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

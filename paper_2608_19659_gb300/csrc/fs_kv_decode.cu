@@ -57,10 +57,13 @@ __global__ void __launch_bounds__(kWarps * 32)
   constexpr int kMt = D / 16;      // 16-dimension tiles of O^T
   constexpr int kChunk = D / 8;    // dimensions of a value that one lane group holds
   constexpr int kTileBytes = kTile * D;
+  constexpr int kPart = kRows * (D + 2);                      // floats of a partial result
+  constexpr int kUnits = kRows * (D / 4) / (kWarps * 32);     // groups of 4 dimensions a thread joins
   extern __shared__ unsigned char raw[];
   unsigned char* ring = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
   __shared__ uint64_t bars[kWarps][kStages];
   __shared__ float sm_m[kWarps][kRows], sm_l[kWarps][kRows];
+  __shared__ float2 sm_ml[kRows][kKvFan];
   __shared__ unsigned sm_last;
 
   const KvView& v = a.v;
@@ -392,7 +395,7 @@ __global__ void __launch_bounds__(kWarps * 32)
 
   const int n_rows = r_end - r0;
   const long long item = ((long long)b * gridDim.y + blockIdx.y);
-  float* part_o = a.part + (item * gridDim.x + part) * (kRows * (D + 2));
+  float* part_o = a.part + (item * gridDim.x + part) * kPart;
   float* part_ml = part_o + kRows * D;
   auto write_out = [&](int r, int d, float4 x, float lsum) {
     const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
@@ -425,34 +428,78 @@ __global__ void __launch_bounds__(kWarps * 32)
   }
   if (n_parts == 1) return;
 
-  // ---- join the parts: the block that takes the last ticket
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    const unsigned t = atomicAdd(a.ticket + item, 1u);
-    sm_last = t == (unsigned)n_parts - 1;
-    if (sm_last) a.ticket[item] = 0;  // as it was found
-  }
-  __syncthreads();
-  if (!sm_last) return;
-  __threadfence();
-  const float* parts = a.part + item * gridDim.x * (kRows * (D + 2));
-  for (int u = threadIdx.x; u < n_rows * (D / 4); u += kWarps * 32) {
-    const int r = u / (D / 4), d = u % (D / 4) * 4;
-    float top = -INFINITY, lsum = 0.f;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = 0; i < n_parts; ++i) {
-      const float* at = parts + (long long)i * (kRows * (D + 2));
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(at + kRows * D + 2 * r));
-      const float4 y = __ldcg(reinterpret_cast<const float4*>(at + r * D + d));
-      const float m_new = fmaxf(top, ml.x), base = m_new == -INFINITY ? 0.f : m_new;
-      const float f0 = ex2(top - base), f1 = ex2(ml.x - base);
-      top = m_new;
-      lsum = fmaf(lsum, f0, ml.y * f1);
-      x.x = fmaf(x.x, f0, y.x * f1), x.y = fmaf(x.y, f0, y.y * f1);
-      x.z = fmaf(x.z, f0, y.z * f1), x.w = fmaf(x.w, f0, y.w * f1);
+  // ---- join the parts: the last block of every kKvFan, then the last of those
+  float* parts = a.part + item * gridDim.x * kPart;
+  int me = part, count = n_parts, step = 1;  // of `count` results, `step` parts apart, mine is the `me`-th
+  unsigned* ticket = a.ticket + item * a.tickets;
+  for (bool first = a.tickets > 1;; first = false) {
+    const int g = first ? me / kKvFan : 0, g0 = first ? g * kKvFan : 0, g_n = first ? min(kKvFan, count - g0) : count;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      unsigned* at = ticket + (first ? 1 + g : 0);
+      const unsigned t = atomicAdd(at, 1u);
+      sm_last = t == (unsigned)g_n - 1;
+      if (sm_last) *at = 0;  // as it was found
     }
-    write_out(r, d, x, lsum);
+    __syncthreads();
+    if (!sm_last) return;
+    __threadfence();
+    const bool done = g_n == count;  // nothing is left to join with
+    float* from = parts + (long long)(g0 * step) * kPart;
+    // sixteen results at a time: their weights first, then their sums with every load under way at once
+    float4 acc[kUnits];
+    float lsum[kUnits], top[kUnits];
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f), lsum[i] = 0.f, top[i] = -INFINITY;
+    for (int i0 = 0; i0 < g_n; i0 += kKvFan) {
+      const int m_n = min(kKvFan, g_n - i0);
+      __syncthreads();
+      for (int u = threadIdx.x; u < kRows * kKvFan; u += kWarps * 32) {
+        const int r = u / kKvFan, i = u % kKvFan;
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (i < m_n && r < n_rows)
+          ml = __ldcg(reinterpret_cast<const float2*>(from + (long long)((i0 + i) * step) * kPart + kRows * D + 2 * r));
+        sm_ml[r][i] = ml;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kUnits; ++k) {
+        const int u = threadIdx.x + k * kWarps * 32, r = u / (D / 4), d = u % (D / 4) * 4;
+        if (r >= n_rows) continue;
+        float m_new = top[k];
+#pragma unroll
+        for (int i = 0; i < kKvFan; ++i) m_new = fmaxf(m_new, sm_ml[r][i].x);
+        const float base = m_new == -INFINITY ? 0.f : m_new, f0 = ex2(top[k] - base);
+        top[k] = m_new, lsum[k] *= f0;
+        acc[k].x *= f0, acc[k].y *= f0, acc[k].z *= f0, acc[k].w *= f0;
+        float4 y[kKvFan];
+#pragma unroll
+        for (int i = 0; i < kKvFan; ++i)
+          if (i < m_n) y[i] = __ldcg(reinterpret_cast<const float4*>(from + (long long)((i0 + i) * step) * kPart + r * D + d));
+#pragma unroll
+        for (int i = 0; i < kKvFan; ++i)
+          if (i < m_n) {
+            const float f = ex2(sm_ml[r][i].x - base);
+            lsum[k] = fmaf(sm_ml[r][i].y, f, lsum[k]);
+            acc[k].x = fmaf(y[i].x, f, acc[k].x), acc[k].y = fmaf(y[i].y, f, acc[k].y);
+            acc[k].z = fmaf(y[i].z, f, acc[k].z), acc[k].w = fmaf(y[i].w, f, acc[k].w);
+          }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) {
+      const int u = threadIdx.x + k * kWarps * 32, r = u / (D / 4), d = u % (D / 4) * 4;
+      if (r >= n_rows) continue;
+      if (done) {
+        write_out(r, d, acc[k], lsum[k]);
+      } else {  // in the place of the first of them (every maximum and sum there has been read)
+        *reinterpret_cast<float4*>(from + r * D + d) = acc[k];
+        if (d == 0) *reinterpret_cast<float2*>(from + kRows * D + 2 * r) = make_float2(top[k], lsum[k]);
+      }
+    }
+    if (done) return;
+    me = g, count = (count + kKvFan - 1) / kKvFan, step = kKvFan;
   }
 }
 
