@@ -528,8 +528,8 @@ typedef struct {
  * are in, and its new tokens, the last of them, are rows q_start[b] .. q_start[b + 1]
  * of the call's arrays (none: a slot without a request, or one that only waits).
  * Token position p of sequence b is in page page_table[b * table_stride +
- * p / page_tokens], slot p mod page_tokens; entries beyond a sequence's tokens are
- * not read. A row whose position would be negative (more new tokens than length) is
+ * p / page_tokens], slot p mod page_tokens; entries beyond a sequence's tokens may
+ * hold anything. A row whose position would be negative (more new tokens than length) is
  * not appended and attends to nothing. Host values: tokens = q_start[batch],
  * max_new >= every sequence's new tokens, max_length >= every length (bounds: what
  * launches are sized by). The device arrays are not checked before the call; the

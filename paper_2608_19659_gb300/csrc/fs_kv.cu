@@ -371,9 +371,10 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
     p.split = (len + 127) / 128 * 128;
     p.splits = 1;
   } else {
-    // a part for every block that is resident at once; more of them while they are few an item,
-    // because sequences differ in length
-    const long long want = std::max(1ll, ((items < sms ? 2ll : 4ll) * sms + items - 1) / items);
+    // a part for every block that is resident at once; parts for two such waves where they are few
+    // an item, because sequences differ in length
+    const long long slots = (long long)sms * (c->dim == 128 ? 2 : 4);
+    const long long want = 2 * items <= slots ? slots / items : (2 * slots + items - 1) / items;
     p.split = std::clamp((int)((len + want - 1) / want + 127) / 128 * 128, kMinSplit, kMaxSplit);
     p.splits = (len + p.split - 1) / p.split;
     const int groups = (p.splits + kKvFan - 1) / kKvFan;
@@ -384,13 +385,13 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
 }
 
 // At least plan_of's part_floats, and nondecreasing in the batch's sizes: items * splits
-// is at most 4 sms + 2 items where the items alone set the parts' length, items *
+// is at most 8 sms + 2 items where the items alone set the parts' length, items *
 // ceil(len / kMaxSplit) where that does.
 size_t part_floats_bound(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int sms) {
   const long long rows = std::min<long long>(kFewRows, (long long)std::max(1, b->max_new) * (q_heads / c->heads));
   const long long items = std::min<long long>(kKvTickets, (long long)std::max(1, b->batch) * c->heads * ((rows + 7) / 8));
   const long long len = std::max(1, b->max_length);
-  return (size_t)(std::max(4ll * sms + 2 * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2));
+  return (size_t)(std::max(8ll * sms + 2 * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2));
 }
 
 int device_sms(int* sms) {

@@ -26,7 +26,7 @@ namespace fs {
 namespace {
 
 constexpr int kWarps = 4, kStages = 3, kTile = 32;
-constexpr float kUp = 15.f;  // log2 of the largest weight: near the top of half precision
+constexpr float kUp = 7.f, kSlack = 8.f;  // log2: weights are scaled by 2^kUp, and m may lag behind by kSlack: 2^15 at most
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kWarps * 32)
   constexpr int kChunk = D / 8;    // dimensions of a value that one lane group holds
   constexpr int kTileBytes = kTile * D;
   constexpr int kPart = kRows * (D + 2);                      // floats of a partial result
-  constexpr int kUnits = kRows * (D / 4) / (kWarps * 32);     // groups of 4 dimensions a thread joins
+  constexpr int kUnits = (kRows * (D / 4) + kWarps * 32 - 1) / (kWarps * 32);  // groups of 4 dimensions a thread joins
   extern __shared__ unsigned char raw[];
   unsigned char* ring = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
   __shared__ uint64_t bars[kWarps][kStages];
@@ -72,6 +72,17 @@ __global__ void __launch_bounds__(kWarps * 32)
   const int h = blockIdx.y / row_blocks, rb = blockIdx.y % row_blocks;
   const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tid = lane & 3;
 
+  if (threadIdx.x < 2)  // (the copies' descriptions)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(threadIdx.x ? &mv : &mk) : "memory");
+  // the page of this lane's first tile, asked for before the sequence's length is known: without a
+  // window the tile's place does not depend on it (entries beyond the sequence are read, not used)
+  const int early_at = (part * a.split + (w + lane * kWarps) * kTile) >> v.log_page;
+  int early = 0;
+  if (!a.window && early_at < v.table_stride)
+    asm volatile("ld.global.s32 %0, [%1];" : "=r"(early) : "l"(v.page_table + (long long)b * v.table_stride + early_at));
+  if (lane == 0)
+    for (int i = 0; i < kStages; ++i) mbar_init(&bars[w][i], 1);
+  __syncwarp();
   KvSeq s;
   if (!kv_seq(v, b, s)) {
     if (threadIdx.x == 0 && part == 0) kv_flag(v, KV_ST_BATCH);
@@ -96,10 +107,6 @@ __global__ void __launch_bounds__(kWarps * 32)
   const int n_tiles = max(0, (c1 - c0 + kTile - 1) / kTile);
   const int my_tiles = w < n_tiles ? (n_tiles - w + kWarps - 1) / kWarps : 0;
 
-  if (lane == 0)
-    for (int i = 0; i < kStages; ++i) mbar_init(&bars[w][i], 1);
-  __syncwarp();
-
   unsigned char* my_ring = ring + w * (kStages * 2 * kTileBytes);
   // pages and scales of this warp's tiles, 32 tiles at a time, a tile a lane
   int pg0 = 0, pg1 = 0;
@@ -111,7 +118,7 @@ __global__ void __launch_bounds__(kWarps * 32)
     ks0 = ks1 = vs0 = vs1 = 0.f;
     if (i < my_tiles) {
       const int t = c0 + (w + i * kWarps) * kTile;
-      pg0 = pg1 = kv_page(v, b, t >> v.log_page);
+      pg0 = pg1 = !a.window && i0 == 0 ? kv_page_ok(v, early) : kv_page(v, b, t >> v.log_page);
       if (half_tiles && t + 16 < s.len) pg1 = kv_page(v, b, (t + 16) >> v.log_page);
     }
   };
@@ -121,28 +128,40 @@ __global__ void __launch_bounds__(kWarps * 32)
       ks0 = v.k_scale[at0], vs0 = v.v_scale[at0];
       ks1 = ks0, vs1 = vs0;
       if (pg1 != pg0) ks1 = v.k_scale[at1], vs1 = v.v_scale[at1];
-      kv_scales(v, ks0, vs0);
-      kv_scales(v, ks1, vs1);
     }
   };
-  auto issue = [&](int i, int p0, int p1) {  // lane 0: tile i into its stage
+  // one of a tile's copies into its stage: keys, values, and those of the second page
+  auto copy = [&](int i, int which, int p0, int p1) {
     const int st = i % kStages, t = c0 + (w + i * kWarps) * kTile, slot = t & ((1 << v.log_page) - 1);
-    const uint32_t kd = smem_u32(my_ring) + st * (2 * kTileBytes);
-    uint64_t* bar = &bars[w][st];
-    mbar_expect_tx(bar, 2 * kTileBytes);
-    tma_tile(kd, &mk, slot, h, p0, bar);
-    tma_tile(kd + kTileBytes, &mv, slot, h, p0, bar);
-    if (half_tiles) {
-      tma_tile(kd + kTileBytes / 2, &mk, 0, h, p1, bar);
-      tma_tile(kd + kTileBytes + kTileBytes / 2, &mv, 0, h, p1, bar);
-    }
+    tma_tile(smem_u32(my_ring) + st * (2 * kTileBytes) + (which & 1) * kTileBytes + (which >> 1) * (kTileBytes / 2),
+             which & 1 ? &mv : &mk, half_tiles ? 0 : slot, h, which >> 1 ? p1 : p0, &bars[w][st]);
+  };
+  auto issue = [&](int i, int p0, int p1) {
+    if (lane == 0) mbar_expect_tx(&bars[w][i % kStages], 2 * kTileBytes);
+    __syncwarp();
+    if (lane < (half_tiles ? 4 : 2)) copy(i, lane, p0, p1);
   };
 
-  load_pages(0);
+  // queries' loads first, then the first copies: the lanes of a stage issue its own
+  uint4 qraw[NT][kSteps / 4][2];
 #pragma unroll
-  for (int i = 0; i < kStages; ++i) {
-    const int p0 = __shfl_sync(~0u, pg0, i), p1 = __shfl_sync(~0u, pg1, i);
-    if (lane == 0 && i < my_tiles) issue(i, p0, p1);
+  for (int n = 0; n < NT; ++n) {
+    const int r = r0 + n * 8 + gid;
+    const T* q = static_cast<const T*>(a.q) + (long long)(s.first + r / v.group) * a.q_token +
+                 (h * v.group + r % v.group) * a.q_head;
+#pragma unroll
+    for (int c = 0; c < kSteps / 4; ++c)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        qraw[n][c][k] = r < r_end ? *reinterpret_cast<const uint4*>(q + (tid * (kSteps / 4) + c) * 16 + 8 * k) : make_uint4(0, 0, 0, 0);
+  }
+  load_pages(0);
+  {
+    const int i = lane >> 2, p0 = __shfl_sync(~0u, pg0, i), p1 = __shfl_sync(~0u, pg1, i);
+    const bool mine = i < kStages && i < my_tiles;
+    if (mine && (lane & 3) == 0) mbar_expect_tx(&bars[w][i], 2 * kTileBytes);
+    __syncwarp();
+    if (mine && (lane & 3) < (half_tiles ? 4 : 2)) copy(i, lane & 3, p0, p1);
   }
   load_scales(0);
 
@@ -152,27 +171,18 @@ __global__ void __launch_bounds__(kWarps * 32)
   int hi_lim[NT][2], lo_lim[NT][2];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int r = r0 + n * 8 + gid;
     float f[kSteps * 4];
     float amax = 0.f;
-    if (r < r_end) {
-      const T* q = static_cast<const T*>(a.q) + (long long)(s.first + r / v.group) * a.q_token +
-                   (h * v.group + r % v.group) * a.q_head;
 #pragma unroll
-      for (int c = 0; c < kSteps / 4; ++c) {
-        const uint4* at = reinterpret_cast<const uint4*>(q + (tid * (kSteps / 4) + c) * 16);
-        const uint4 x = at[0], y = at[1];
-        const uint32_t u[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    for (int c = 0; c < kSteps / 4; ++c) {
+      const uint4 x = qraw[n][c][0], y = qraw[n][c][1];
+      const uint32_t u[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float2 z = Elem<T>::two(u[i]);
-          f[c * 16 + 2 * i] = z.x, f[c * 16 + 2 * i + 1] = z.y;
-          amax = fmaxf(amax, fmaxf(fabsf(z.x), fabsf(z.y)));
-        }
+      for (int i = 0; i < 8; ++i) {
+        const float2 z = Elem<T>::two(u[i]);
+        f[c * 16 + 2 * i] = z.x, f[c * 16 + 2 * i + 1] = z.y;
+        amax = fmaxf(amax, fmaxf(fabsf(z.x), fabsf(z.y)));
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kSteps * 4; ++i) f[i] = 0.f;
     }
     amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
     amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 2));
@@ -216,6 +226,8 @@ __global__ void __launch_bounds__(kWarps * 32)
         load_pages(i);
         load_scales(i);
       }
+      kv_scales(v, ks0, vs0);
+      kv_scales(v, ks1, vs1);
       float top = fmaxf(vs0, vs1);
 #pragma unroll
       for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
@@ -248,10 +260,11 @@ __global__ void __launch_bounds__(kWarps * 32)
     float sc[2][NT][4];
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
+      float sc1[NT][4];  // (two chains of products: half the latency)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sc[mt][n][k] = 0.f;
+        for (int k = 0; k < 4; ++k) sc[mt][n][k] = sc1[n][k] = 0.f;
 #pragma unroll
       for (int c = 0; c < kSteps / 4; ++c) {
         // 16 codes of tokens gid and gid + 8
@@ -264,9 +277,13 @@ __global__ void __launch_bounds__(kWarps * 32)
           const uint32_t a0 = e4m3x2_to_f16x2(xs[k]), a2 = e4m3x2_to_f16x2_hi(xs[k]);
           const uint32_t a1 = e4m3x2_to_f16x2(ys[k]), a3 = e4m3x2_to_f16x2_hi(ys[k]);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma16816(sc[mt][n], a0, a1, a2, a3, qf[n][c * 4 + k][0], qf[n][c * 4 + k][1]);
+          for (int n = 0; n < NT; ++n) mma16816(k & 1 ? sc1[n] : sc[mt][n], a0, a1, a2, a3, qf[n][c * 4 + k][0], qf[n][c * 4 + k][1]);
         }
       }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sc[mt][n][k] += sc1[n][k];
     }
     const bool whole = t0 >= full_lo && t0 + kTile <= full_hi;
 #pragma unroll
@@ -282,31 +299,44 @@ __global__ void __launch_bounds__(kWarps * 32)
           }
           sc[mt][n][k] = x;
         }
-    // running maximum and sum; a row without a key yet keeps -infinity, and 0 in its place
-    uint32_t pf[2][NT][2];
+    // m, the reference of the weights, follows the rows' maxima only when one of them has grown by
+    // more than 2^kSlack: most tiles need no exchange between lanes. A row without a key yet keeps
+    // -infinity, and 0 in its place.
+    float lm[NT][2];
+    bool grow = false;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      float up[2], corr[2];
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        float x = fmaxf(fmaxf(sc[0][n][j], sc[0][n][j + 2]), fmaxf(sc[1][n][j], sc[1][n][j + 2]));
-        x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
-        x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
-        x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
-        const float m_new = fmaxf(m[n][j], x);
-        const float mx = m_new == -INFINITY ? 0.f : m_new;
-        up[j] = mx - kUp;
-        corr[j] = ex2(m[n][j] - mx);
-        m[n][j] = m_new;
-        l[n][j] *= corr[j];
+        lm[n][j] = fmaxf(fmaxf(sc[0][n][j], sc[0][n][j + 2]), fmaxf(sc[1][n][j], sc[1][n][j + 2]));
+        grow |= lm[n][j] > m[n][j] + kSlack || (m[n][j] == -INFINITY && lm[n][j] > m[n][j]);
       }
-      if (__any_sync(~0u, corr[0] != 1.f || corr[1] != 1.f)) {
+    if (__any_sync(~0u, grow)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float corr[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float x = lm[n][j];
+          x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+          x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
+          x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
+          const float m_new = fmaxf(m[n][j], x);
+          corr[j] = ex2(m[n][j] - (m_new == -INFINITY ? 0.f : m_new));
+          m[n][j] = m_new;
+          l[n][j] *= corr[j];
+        }
 #pragma unroll
         for (int j = 0; j < kMt; ++j) {
           o[j][n][0] *= corr[0], o[j][n][2] *= corr[0];
           o[j][n][1] *= corr[1], o[j][n][3] *= corr[1];
         }
       }
+    }
+    uint32_t pf[2][NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float up[2] = {(m[n][0] == -INFINITY ? 0.f : m[n][0]) - kUp, (m[n][1] == -INFINITY ? 0.f : m[n][1]) - kUp};
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
@@ -352,9 +382,11 @@ __global__ void __launch_bounds__(kWarps * 32)
     __syncwarp();  // every lane has read the stage
     // the next tile of this stage; its pages are in the lists of its round of 32
     const int nx = i + kStages;
-    int p0 = __shfl_sync(~0u, pg0, nx & 31), p1 = __shfl_sync(~0u, pg1, nx & 31);
-    if (lane == 0 && nx < my_tiles) {
-      if ((nx & ~31) != (i & ~31)) {
+    if (nx < my_tiles) {
+      int p0, p1;
+      if ((nx & ~31) == (i & ~31)) {
+        p0 = __shfl_sync(~0u, pg0, nx & 31), p1 = __shfl_sync(~0u, pg1, nx & 31);
+      } else {
         const int t = c0 + (w + nx * kWarps) * kTile;
         p0 = p1 = kv_page(v, b, t >> v.log_page);
         if (half_tiles && t + 16 < s.len) p1 = kv_page(v, b, (t + 16) >> v.log_page);
