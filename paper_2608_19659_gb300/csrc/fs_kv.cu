@@ -105,42 +105,81 @@ struct KvAppendArgs {
   int rot, angle_rows, interleaved, q_heads;
 };
 
-// Four dimensions from d0 on of a row, rotated for position `pos`; x: the row's own
-// four, row: the row (for the other half of a pair).
 template <typename T>
-__device__ __forceinline__ void rotate4(float (&x)[4], const T* row, int d0, const KvAppendArgs& a, int pos) {
-  if (d0 >= a.rot) return;
+__device__ __forceinline__ void unpack4(float (&x)[4], uint2 w) {
+  const float2 a = Elem<T>::two(w.x), b = Elem<T>::two(w.y);
+  x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+}
+
+// The angles of the four dimensions from d0 on at position `pos`: one a pair (interleaved:
+// two of each), or one a dimension.
+struct Angles {
+  float4 c, s;
+};
+__device__ __forceinline__ Angles angles_of(const KvAppendArgs& a, int pos, int d0) {
+  Angles r{};
+  if (d0 >= a.rot) return r;
   const int half = a.rot >> 1;
   const float* ct = a.cos + (long long)pos * half;
   const float* st = a.sin + (long long)pos * half;
   if (a.interleaved) {
-    const float2 c = *reinterpret_cast<const float2*>(ct + (d0 >> 1));
-    const float2 s = *reinterpret_cast<const float2*>(st + (d0 >> 1));
-    const float y0 = __fsub_rn(__fmul_rn(x[0], c.x), __fmul_rn(x[1], s.x));
-    const float y1 = __fadd_rn(__fmul_rn(x[1], c.x), __fmul_rn(x[0], s.x));
-    const float y2 = __fsub_rn(__fmul_rn(x[2], c.y), __fmul_rn(x[3], s.y));
-    const float y3 = __fadd_rn(__fmul_rn(x[3], c.y), __fmul_rn(x[2], s.y));
-    x[0] = y0, x[1] = y1, x[2] = y2, x[3] = y3;
-    return;
+    const float2 c = *reinterpret_cast<const float2*>(ct + (d0 >> 1)), s = *reinterpret_cast<const float2*>(st + (d0 >> 1));
+    r.c = make_float4(c.x, c.x, c.y, c.y), r.s = make_float4(s.x, s.x, s.y, s.y);
+  } else {
+    const int i0 = d0 < half ? d0 : d0 - half;
+    r.c = *reinterpret_cast<const float4*>(ct + i0), r.s = *reinterpret_cast<const float4*>(st + i0);
   }
-  const bool low = d0 < half;
-  const int i0 = low ? d0 : d0 - half;
-  const uint2 w = *reinterpret_cast<const uint2*>(row + (low ? d0 + half : d0 - half));
-  const float2 p01 = Elem<T>::two(w.x), p23 = Elem<T>::two(w.y);
-  const float4 c = *reinterpret_cast<const float4*>(ct + i0), s = *reinterpret_cast<const float4*>(st + i0);
-  const float p[4] = {p01.x, p01.y, p23.x, p23.y}, cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+  return r;
+}
+
+// What the dimensions from dA and from dB on are paired with: each other where the whole row is
+// rotated in halves, their neighbours where pairs are interleaved, else what the row holds half
+// the rotated dimensions away.
+template <typename T>
+__device__ __forceinline__ void partners(float (&pa)[4], float (&pb)[4], const float (&xa)[4], const float (&xb)[4],
+                                         const T* row, int dA, int dB, const KvAppendArgs& a, int dim) {
+  if (a.interleaved) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) pa[i] = xa[i ^ 1], pb[i] = xb[i ^ 1];
+  } else if (a.rot == dim) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) pa[i] = xb[i], pb[i] = xa[i];
+  } else {
+    const int half = a.rot >> 1;
+    uint2 wa = make_uint2(0, 0), wb = wa;
+    if (dA < a.rot) wa = *reinterpret_cast<const uint2*>(row + (dA < half ? dA + half : dA - half));
+    if (dB < a.rot) wb = *reinterpret_cast<const uint2*>(row + (dB < half ? dB + half : dB - half));
+    unpack4<T>(pa, wa);
+    unpack4<T>(pb, wb);
+  }
+}
+
+// x rotated: x c - p s for the first of a pair, x c + p s for the second.
+__device__ __forceinline__ void turn4(float (&x)[4], const float (&p)[4], int d0, const Angles& an, const KvAppendArgs& a) {
+  if (d0 >= a.rot) return;
+  const float c[4] = {an.c.x, an.c.y, an.c.z, an.c.w}, s[4] = {an.s.x, an.s.y, an.s.z, an.s.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float m = __fmul_rn(x[i], cc[i]), n = __fmul_rn(p[i], ss[i]);
-    x[i] = low ? __fsub_rn(m, n) : __fadd_rn(m, n);
+    const float m = __fmul_rn(x[i], c[i]), n = __fmul_rn(p[i], s[i]);
+    const bool first = a.interleaved ? !(i & 1) : d0 < (a.rot >> 1);
+    x[i] = first ? __fsub_rn(m, n) : __fadd_rn(m, n);
   }
+}
+
+// Both groups of four dimensions of a row, rotated.
+template <typename T>
+__device__ __forceinline__ void rotate8(float (&x)[4], float (&y)[4], const T* row, int dA, int dB, const KvAppendArgs& a,
+                                        int pos, int dim) {
+  if (!a.rot) return;
+  float px[4], py[4];
+  partners<T>(px, py, x, y, row, dA, dB, a, dim);
+  turn4(x, px, dA, angles_of(a, pos, dA), a);
+  turn4(y, py, dB, angles_of(a, pos, dB), a);
 }
 
 template <typename T>
 __device__ __forceinline__ void load4(float (&x)[4], const T* p) {
-  const uint2 w = *reinterpret_cast<const uint2*>(p);
-  const float2 a = Elem<T>::two(w.x), b = Elem<T>::two(w.y);
-  x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+  unpack4<T>(x, *reinterpret_cast<const uint2*>(p));
 }
 
 __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
@@ -158,12 +197,35 @@ __device__ __forceinline__ float scale_for(float amax) {
   return exp2_int(max(p, -126));
 }
 
+// Four values as codes: x / scale (the scale's reciprocal is exact), infinities saturated (an
+// infinity times 0 would be NaN; the conversion saturates), NaN as 0.
+__device__ __forceinline__ uint32_t codes4(const float (&x)[4], float inv) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = x[i] != x[i] ? 0.f : fabsf(x[i]) < INFINITY ? __fmul_rn(x[i], inv) : x[i];
+  return e4m3x2(y[0], y[1]) | e4m3x2(y[2], y[3]) << 16;
+}
+
+// Eight codes under a scale that has grown: times f = old scale / new one.
+__device__ __forceinline__ void rescale8(uint8_t* at, float f) {
+  uint2* w = reinterpret_cast<uint2*>(at);
+  const uint2 c = *w;
+  uint32_t r[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t u = i ? c.y : c.x;
+    const float2 lo = Elem<__half>::two(e4m3x2_to_f16x2(u)), hi = Elem<__half>::two(e4m3x2_to_f16x2_hi(u));
+    r[i] = e4m3x2(__fmul_rn(lo.x, f), __fmul_rn(lo.y, f)) | e4m3x2(__fmul_rn(hi.x, f), __fmul_rn(hi.y, f)) << 16;
+  }
+  *w = make_uint2(r[0], r[1]);
+}
+
 // One unit of D / 8 lanes appends the new tokens of one (sequence, page) for one head
 // of keys or values, or rotates one query head over them. Its lanes hold dimensions
 // 4 l .. 4 l + 3 of each half. Two passes over the tokens: the largest magnitude,
 // then the codes.
 template <int D, typename T>
-__global__ void __launch_bounds__(128) k_kv_append(const KvAppendArgs a) {
+__global__ void __launch_bounds__(128, 6) k_kv_append(const KvAppendArgs a) {
   constexpr int kLanes = D / 8, kUnits = 128 / kLanes;
   const int b = blockIdx.z, piece = blockIdx.x;
   const int unit = threadIdx.x / kLanes, l = threadIdx.x % kLanes;
@@ -188,24 +250,23 @@ __global__ void __launch_bounds__(128) k_kv_append(const KvAppendArgs a) {
   const int dA = 4 * l, dB = D / 2 + 4 * l;
   const uint32_t mask = (kLanes == 16 ? 0xffffu : 0xffu) << (threadIdx.x % 32 / kLanes * kLanes);  // the unit's lanes
 
-  // Tokens go by fours: their loads are all under way before the first store.
+  // Tokens go by twos: their loads are under way before the first store.
   if (job >= 2 * H) {
     const int h = job - 2 * H;
-    for (int p = lo; p < hi; p += 4) {
-      const int n = min(4, hi - p);
-      float x[4][4], y[4][4];
+    for (int p = lo; p < hi; p += 2) {
+      const int n = min(2, hi - p);
+      float x[2][4], y[2][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 2; ++i)
         if (i < n) {
           const T* row = static_cast<const T*>(a.q) + (row0 + p + i) * a.q_token + h * a.q_head;
           load4(x[i], row + dA);
           load4(y[i], row + dB);
-          rotate4(x[i], row, dA, a, p + i);
-          rotate4(y[i], row, dB, a, p + i);
+          rotate8<T>(x[i], y[i], row, dA, dB, a, p + i, D);
         }
       __syncwarp(mask);  // q_out may be q: every lane of a row has read before one writes
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 2; ++i)
         if (i < n) {
           T* to = static_cast<T*>(a.q_out) + (row0 + p + i) * a.o_token + h * a.o_head;
           *reinterpret_cast<uint2*>(to + dA) = make_uint2(Elem<T>::pack(x[i][0], x[i][1]), Elem<T>::pack(x[i][2], x[i][3]));
@@ -228,16 +289,13 @@ __global__ void __launch_bounds__(128) k_kv_append(const KvAppendArgs a) {
 
   float amax = 0.f;
   bool nan = false;
-#pragma unroll 4
+#pragma unroll 2
   for (int p = lo; p < hi; ++p) {
     const T* row = src + p * src_token;
     float x[4], y[4];
     load4(x, row + dA);
     load4(y, row + dB);
-    if (is_k) {
-      rotate4(x, row, dA, a, p);
-      rotate4(y, row, dB, a, p);
-    }
+    if (is_k) rotate8<T>(x, y, row, dA, dB, a, p, D);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float u = fabsf(x[i]), w = fabsf(y[i]);
@@ -253,62 +311,269 @@ __global__ void __launch_bounds__(128) k_kv_append(const KvAppendArgs a) {
   if (slot0 && now > old) {
     // the page's earlier tokens, 8 codes a lane
     const float f = __fdiv_rn(old, now);
-    uint8_t* at = page + 8 * l;
 #pragma unroll 4
-    for (int t = 0; t < slot0; ++t) {
-      uint2* w = reinterpret_cast<uint2*>(at + t * a.token_stride);
-      const uint2 c = *w;
-      uint32_t r[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint32_t u = i ? c.y : c.x;
-        const float2 lo2 = Elem<__half>::two(e4m3x2_to_f16x2(u)), hi2 = Elem<__half>::two(e4m3x2_to_f16x2_hi(u));
-        r[i] = e4m3x2(__fmul_rn(lo2.x, f), __fmul_rn(lo2.y, f)) | e4m3x2(__fmul_rn(hi2.x, f), __fmul_rn(hi2.y, f)) << 16;
-      }
-      *w = make_uint2(r[0], r[1]);
-    }
+    for (int t = 0; t < slot0; ++t) rescale8(page + t * a.token_stride + 8 * l, f);
   }
   if (l == 0) *scale_at = now;
 
   const float inv = now > 0.f ? __fdiv_rn(1.f, now) : 0.f;
-  for (int p = lo; p < hi; p += 4) {
-    const int n = min(4, hi - p);
-    float x[4][8];
+  for (int p = lo; p < hi; p += 2) {
+    const int n = min(2, hi - p);
+    float x[2][4], y[2][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
       if (i < n) {
         const T* row = src + (p + i) * src_token;
         float u[4], w[4];
         load4(u, row + dA);
         load4(w, row + dB);
-        if (is_k) {
-          rotate4(u, row, dA, a, p + i);
-          rotate4(w, row, dB, a, p + i);
-        }
+        if (is_k) rotate8<T>(u, w, row, dA, dB, a, p + i, D);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[i][j] = u[j], x[i][4 + j] = w[j];
+        for (int j = 0; j < 4; ++j) x[i][j] = u[j], y[i][j] = w[j];
       }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
       if (i < n) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float u = x[i][j];
-          // (an infinity times 0 would be NaN; the conversion saturates)
-          x[i][j] = u != u ? 0.f : fabsf(u) < INFINITY ? __fmul_rn(u, inv) : u;
-        }
         uint8_t* to = page + (long long)((p + i) & (P - 1)) * a.token_stride;
-        *reinterpret_cast<uint32_t*>(to + dA) = e4m3x2(x[i][0], x[i][1]) | e4m3x2(x[i][2], x[i][3]) << 16;
-        *reinterpret_cast<uint32_t*>(to + dB) = e4m3x2(x[i][4], x[i][5]) | e4m3x2(x[i][6], x[i][7]) << 16;
+        *reinterpret_cast<uint32_t*>(to + dA) = codes4(x[i], inv);
+        *reinterpret_cast<uint32_t*>(to + dB) = codes4(y[i], inv);
       }
   }
 }
 
+// The same for one new token a sequence at most: every load that does not need another's
+// answer is under way at once, and few registers leave room for many units.
 template <int D, typename T>
-cudaError_t launch_append(const KvAppendArgs& a, int pieces, cudaStream_t s) {
+__global__ void __launch_bounds__(128, 8) k_kv_append_one(const KvAppendArgs a) {
+  constexpr int kLanes = D / 8, kUnits = 128 / kLanes;
+  const int b = blockIdx.y, unit = threadIdx.x / kLanes, l = threadIdx.x % kLanes;
+  const int job = blockIdx.x * kUnits + unit, H = a.v.heads;
+  KvSeq s;
+  if (!kv_seq(a.v, b, s)) {
+    if (threadIdx.x == 0) kv_flag(a.v, KV_ST_BATCH);
+    return;
+  }
+  const int p = s.len - 1;
+  if (s.count == 0 || p < 0 || job >= 2 * H + (a.q ? a.q_heads : 0)) return;
+  if (a.rot && p >= a.angle_rows) {
+    if (l == 0) kv_flag(a.v, KV_ST_ANGLE);
+    return;
+  }
+  const int dA = 4 * l, dB = D / 2 + 4 * l;
+  const uint32_t mask = (kLanes == 16 ? 0xffffu : 0xffu) << (threadIdx.x % 32 / kLanes * kLanes);  // the unit's lanes
+  const bool is_q = job >= 2 * H, is_k = job < H;
+  const int h = is_q ? job - 2 * H : is_k ? job : job - H;
+  const T* row = is_q   ? static_cast<const T*>(a.q) + s.first * a.q_token + h * a.q_head
+                 : is_k ? static_cast<const T*>(a.k) + s.first * a.k_token + h * a.k_head
+                        : static_cast<const T*>(a.vals) + s.first * a.v_token + h * a.v_head;
+  const int g_raw = is_q ? 0 : kv_page_raw(a.v, b, p >> a.v.log_page);
+  float x[4], y[4];
+  load4(x, row + dA);
+  load4(y, row + dB);
+  if (is_q || is_k) rotate8<T>(x, y, row, dA, dB, a, p, D);
+  if (is_q) {
+    __syncwarp(mask);  // q_out may be q: every lane of a row has read before one writes
+    T* to = static_cast<T*>(a.q_out) + s.first * a.o_token + h * a.o_head;
+    *reinterpret_cast<uint2*>(to + dA) = make_uint2(Elem<T>::pack(x[0], x[1]), Elem<T>::pack(x[2], x[3]));
+    *reinterpret_cast<uint2*>(to + dB) = make_uint2(Elem<T>::pack(y[0], y[1]), Elem<T>::pack(y[2], y[3]));
+    return;
+  }
+  const int g = kv_page_ok(a.v, g_raw), slot = p & ((1 << a.v.log_page) - 1);
+  float* scale_at = const_cast<float*>(is_k ? a.v.k_scale : a.v.v_scale) + (long long)g * H + h;
+  const float old = slot ? *scale_at : 0.f;
+  float amax = 0.f;
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float u = fabsf(x[i]), w = fabsf(y[i]);
+    if (u < INFINITY) amax = fmaxf(amax, u);
+    if (w < INFINITY) amax = fmaxf(amax, w);
+    nan |= u != u || w != w;
+  }
+  if (nan) kv_flag(a.v, KV_ST_VALUE);
+#pragma unroll
+  for (int o = kLanes / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(mask, amax, o));
+  const float now = fmaxf(old, scale_for(amax));
+  uint8_t* page = (is_k ? a.kc : a.vc) + g * a.page_stride + h * a.head_stride;
+  if (slot && now > old) {
+    const float f = __fdiv_rn(old, now);
+#pragma unroll 4
+    for (int t = 0; t < slot; ++t) rescale8(page + t * a.token_stride + 8 * l, f);
+  }
+  if (l == 0) *scale_at = now;
+  const float inv = now > 0.f ? __fdiv_rn(1.f, now) : 0.f;
+  uint8_t* to = page + slot * a.token_stride;
+  *reinterpret_cast<uint32_t*>(to + dA) = codes4(x, inv);
+  *reinterpret_cast<uint32_t*>(to + dB) = codes4(y, inv);
+}
+
+// The same for many new tokens: a block per (page, head of keys or values) holds the page's
+// tokens in registers, kIt of them a unit, so that they are read once and all at once; for
+// queries a block per page's tokens and kQHeads heads, whose rows share the angles. A unit a
+// page, as above, keeps too few loads under way: 8 prompts of 4096 tokens took XXX us with it.
+constexpr int kQHeads = 8;
+constexpr int kFewTokens = 8;  // up to so many new tokens a sequence, k_kv_append
+
+template <int D, typename T, int kIt, int kThreads>
+__global__ void __launch_bounds__(kThreads, 768 / kThreads) k_kv_append_many(const KvAppendArgs a) {
+  constexpr int kLanes = D / 8, kUnits = kThreads / kLanes;
+  __shared__ float sm_amax[kThreads / 32];
+  const int b = blockIdx.z, piece = blockIdx.x;
+  const int unit = threadIdx.x / kLanes, l = threadIdx.x % kLanes;
+  KvSeq s;
+  if (!kv_seq(a.v, b, s)) {
+    if (threadIdx.x == 0) kv_flag(a.v, KV_ST_BATCH);
+    return;
+  }
+  const int P = 1 << a.v.log_page, H = a.v.heads;
+  const int p0 = max(s.len - s.count, 0);
+  const int pg = (p0 >> a.v.log_page) + piece;
+  const int lo = max(p0, pg << a.v.log_page), hi = min(s.len, (pg + 1) << a.v.log_page);
+  if (lo >= hi || s.count == 0) return;
+  const long long row0 = (long long)s.first - (s.len - s.count);
+  if (a.rot && hi > a.angle_rows) {
+    if (threadIdx.x == 0) kv_flag(a.v, KV_ST_ANGLE);
+    return;
+  }
+  const int dA = 4 * l, dB = D / 2 + 4 * l;
+
+  if ((int)blockIdx.y >= 2 * H) {
+    const int h0 = (blockIdx.y - 2 * H) * kQHeads, h_n = min(kQHeads, a.q_heads - h0);
+    const uint32_t mask = (kLanes == 16 ? 0xffffu : 0xffu) << (threadIdx.x % 32 / kLanes * kLanes);
+    for (int p = lo + unit; p < hi; p += kUnits) {
+      const Angles an = angles_of(a, p, dA), bn = angles_of(a, p, dB);
+#pragma unroll 1
+      for (int hg = 0; hg < h_n; hg += 4) {  // four heads' loads under way at a time
+        const T* from = static_cast<const T*>(a.q) + (row0 + p) * a.q_token + (h0 + hg) * a.q_head;
+        T* to = static_cast<T*>(a.q_out) + (row0 + p) * a.o_token + (h0 + hg) * a.o_head;
+        uint2 x[4], y[4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+          if (hg + h < h_n) {
+            x[h] = *reinterpret_cast<const uint2*>(from + h * a.q_head + dA);
+            y[h] = *reinterpret_cast<const uint2*>(from + h * a.q_head + dB);
+          }
+        if (a.rot) {
+#pragma unroll
+          for (int h = 0; h < 4; ++h)
+            if (hg + h < h_n) {
+              float u[4], w[4], pu[4], pw[4];
+              unpack4<T>(u, x[h]);
+              unpack4<T>(w, y[h]);
+              partners<T>(pu, pw, u, w, from + h * a.q_head, dA, dB, a, D);
+              turn4(u, pu, dA, an, a);
+              turn4(w, pw, dB, bn, a);
+              x[h] = make_uint2(Elem<T>::pack(u[0], u[1]), Elem<T>::pack(u[2], u[3]));
+              y[h] = make_uint2(Elem<T>::pack(w[0], w[1]), Elem<T>::pack(w[2], w[3]));
+            }
+        }
+        __syncwarp(mask);  // q_out may be q: every lane of a row has read before one writes
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+          if (hg + h < h_n) {
+            *reinterpret_cast<uint2*>(to + h * a.o_head + dA) = x[h];
+            *reinterpret_cast<uint2*>(to + h * a.o_head + dB) = y[h];
+          }
+      }
+    }
+    return;
+  }
+
+  const bool is_k = (int)blockIdx.y < H;
+  const int h = is_k ? blockIdx.y : blockIdx.y - H;
+  const T* src = is_k ? static_cast<const T*>(a.k) + row0 * a.k_token + h * a.k_head
+                      : static_cast<const T*>(a.vals) + row0 * a.v_token + h * a.v_head;
+  const long long src_token = is_k ? a.k_token : a.v_token;
+  const int g_raw = kv_page_raw(a.v, b, pg);
+  float x[kIt][4], y[kIt][4];
+  {
+    uint2 xr[kIt], yr[kIt];
+#pragma unroll
+    for (int i = 0; i < kIt; ++i) {
+      const int p = lo + unit + i * kUnits;
+      xr[i] = yr[i] = make_uint2(0, 0);
+      if (p < hi) {
+        xr[i] = *reinterpret_cast<const uint2*>(src + p * src_token + dA);
+        yr[i] = *reinterpret_cast<const uint2*>(src + p * src_token + dB);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kIt; ++i) unpack4<T>(x[i], xr[i]), unpack4<T>(y[i], yr[i]);
+  }
+  if (is_k && a.rot) {
+#pragma unroll
+    for (int i = 0; i < kIt; ++i) {
+      const int p = lo + unit + i * kUnits;
+      if (p < hi) {
+        float pu[4], pw[4];
+        partners<T>(pu, pw, x[i], y[i], src + p * src_token, dA, dB, a, D);
+        turn4(x[i], pu, dA, angles_of(a, p, dA), a);
+        turn4(y[i], pw, dB, angles_of(a, p, dB), a);
+      }
+    }
+  }
+  float amax = 0.f;
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < kIt; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float u = fabsf(x[i][j]), w = fabsf(y[i][j]);
+      if (u < INFINITY) amax = fmaxf(amax, u);
+      if (w < INFINITY) amax = fmaxf(amax, w);
+      nan |= u != u || w != w;
+    }
+  if (nan) kv_flag(a.v, KV_ST_VALUE);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, o));
+  if (threadIdx.x % 32 == 0) sm_amax[threadIdx.x / 32] = amax;
+  const int g = kv_page_ok(a.v, g_raw);
+  float* scale_at = const_cast<float*>(is_k ? a.v.k_scale : a.v.v_scale) + (long long)g * H + h;
+  const int slot0 = lo & (P - 1);
+  const float old = slot0 ? *scale_at : 0.f;
+  __syncthreads();  // (every thread has the old scale, too)
+#pragma unroll
+  for (int i = 0; i < kThreads / 32; ++i) amax = fmaxf(amax, sm_amax[i]);
+  const float now = fmaxf(old, scale_for(amax));
+  uint8_t* page = (is_k ? a.kc : a.vc) + g * a.page_stride + h * a.head_stride;
+  if (slot0 && now > old) {
+    const float f = __fdiv_rn(old, now);
+    for (int t = unit; t < slot0; t += kUnits) rescale8(page + t * a.token_stride + 8 * l, f);
+  }
+  if (threadIdx.x == 0) *scale_at = now;
+  const float inv = now > 0.f ? __fdiv_rn(1.f, now) : 0.f;
+#pragma unroll
+  for (int i = 0; i < kIt; ++i) {
+    const int p = lo + unit + i * kUnits;
+    if (p < hi) {
+      uint8_t* to = page + (long long)(p & (P - 1)) * a.token_stride;
+      *reinterpret_cast<uint32_t*>(to + dA) = codes4(x[i], inv);
+      *reinterpret_cast<uint32_t*>(to + dB) = codes4(y[i], inv);
+    }
+  }
+}
+
+template <int D, typename T>
+cudaError_t launch_append(const KvAppendArgs& a, int pieces, bool many, cudaStream_t s) {
+  const int q_heads = a.q ? a.q_heads : 0;
   constexpr int kUnits = 128 / (D / 8);
-  const int jobs = 2 * a.v.heads + (a.q ? a.q_heads : 0);
-  k_kv_append<D, T><<<dim3(pieces, (jobs + kUnits - 1) / kUnits, a.v.batch), 128, 0, s>>>(a);
+  const int unit_blocks = (2 * a.v.heads + q_heads + kUnits - 1) / kUnits;
+  if (a.v.max_new == 1) {
+    k_kv_append_one<D, T><<<dim3(unit_blocks, a.v.batch), 128, 0, s>>>(a);
+  } else if (!many) {
+    k_kv_append<D, T><<<dim3(pieces, unit_blocks, a.v.batch), 128, 0, s>>>(a);
+  } else {
+    const dim3 grid(pieces, 2 * a.v.heads + (q_heads + kQHeads - 1) / kQHeads, a.v.batch);
+    const int its = (D / 8 << a.v.log_page) / 128;  // rows a unit of a block of 128
+    if (its <= 2)
+      k_kv_append_many<D, T, 2, 128><<<grid, 128, 0, s>>>(a);
+    else if (its == 4)
+      k_kv_append_many<D, T, 4, 128><<<grid, 128, 0, s>>>(a);
+    else if (its == 8)
+      k_kv_append_many<D, T, 4, 256><<<grid, 256, 0, s>>>(a);
+    else
+      k_kv_append_many<D, T, 4, 512><<<grid, 512, 0, s>>>(a);
+  }
   note_launch();
   return cudaGetLastError();
 }
@@ -487,8 +752,9 @@ extern "C" int fs_kv_append(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   const int pieces = (batch->max_new + P - 2) / P + 1;  // pages that max_new tokens can touch
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const bool h = in->dtype == FS_KV_FP16;
-  const cudaError_t e = cache->dim == 128 ? (h ? launch_append<128, __half>(a, pieces, s) : launch_append<128, __nv_bfloat16>(a, pieces, s))
-                                          : (h ? launch_append<64, __half>(a, pieces, s) : launch_append<64, __nv_bfloat16>(a, pieces, s));
+  const bool many = batch->max_new > kFewTokens;
+  const cudaError_t e = cache->dim == 128 ? (h ? launch_append<128, __half>(a, pieces, many, s) : launch_append<128, __nv_bfloat16>(a, pieces, many, s))
+                                          : (h ? launch_append<64, __half>(a, pieces, many, s) : launch_append<64, __nv_bfloat16>(a, pieces, many, s));
   return e == cudaSuccess ? FS_OK : cuda_say(e, "launch (fs_kv_append)");
 }
 
