@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes as C
 import dataclasses
 import os
+import struct
 
 import numpy as np
 
@@ -152,9 +153,9 @@ def lib():
                                     C.POINTER(C.c_int64)]
         L.fs_kv_workspace_bytes.argtypes = [C.POINTER(fs_kv_cache), C.POINTER(fs_kv_batch), C.c_int32,
                                             C.POINTER(C.c_int64)]
-        L.fs_kv_append.argtypes = [C.POINTER(fs_kv_cache), C.POINTER(fs_kv_batch), C.POINTER(fs_kv_new),
+        L.fs_kv_append.argtypes = [C.POINTER(fs_kv_cache), C.POINTER(fs_kv_batch), C.c_void_p,
                                    C.c_void_p, C.c_int64, C.c_void_p]
-        L.fs_kv_attend.argtypes = [C.POINTER(fs_kv_cache), C.POINTER(fs_kv_batch), C.POINTER(fs_kv_query),
+        L.fs_kv_attend.argtypes = [C.POINTER(fs_kv_cache), C.POINTER(fs_kv_batch), C.c_void_p,
                                    C.c_void_p, C.c_int64, C.c_void_p]
         L.fs_kv_check.argtypes = [C.c_void_p, C.c_void_p]
         L.fs_free_model.argtypes = [C.c_void_p]
@@ -553,6 +554,7 @@ class KvCache:
         self.device, self.heads, self.dim = k.device, k.shape[1], k.shape[3]
         self.struct = fs_kv_cache(k.shape[0], k.shape[1], k.shape[2], k.shape[3], k.data_ptr(), v.data_ptr(),
                                   k_scale.data_ptr(), v_scale.data_ptr(), k.stride(0), k.stride(1), k.stride(2))
+        self.ref = C.byref(self.struct)
 
 
 class KvBatch:
@@ -574,6 +576,7 @@ class KvBatch:
         self.device, self.tokens = length.device, int(tokens)
         self.struct = fs_kv_batch(n, self.tokens, int(max_new), int(max_length), page_table.shape[1], 0,
                                   page_table.data_ptr(), length.data_ptr(), q_start.data_ptr())
+        self.ref = C.byref(self.struct)
 
 
 class KvWorkspace:
@@ -588,30 +591,50 @@ class KvWorkspace:
         self.address, self.bytes = self.tensor.data_ptr(), n.value
 
 
+_kv_kinds = {}  # torch dtype -> FS_KV_*
+
+
 def _kv_dtype(t) -> int:
-    import torch
+    if not _kv_kinds:
+        import torch
 
-    if t.dtype == torch.bfloat16:
-        return FS_KV_BF16
-    if t.dtype == torch.float16:
-        return FS_KV_FP16
-    raise ValueError(f"rows are bfloat16 or float16, not {t.dtype}")
-
-
-def _kv_rows(t, name: str, like, cache: KvCache, batch: KvBatch, heads: int | None) -> fs_kv_rows:
-    if t.dim() != 3 or t.shape[0] != batch.tokens or t.shape[2] != cache.dim or (heads and t.shape[1] != heads):
-        raise ValueError(f"{name} is [tokens = {batch.tokens}, {heads or 'heads'}, {cache.dim}], not {tuple(t.shape)}")
-    if t.dtype != like.dtype or t.device != cache.device or (t.stride(2) != 1 and t.numel()):
-        raise ValueError(f"{name}: want {like.dtype} on {cache.device}, the last dimension contiguous")
-    return fs_kv_rows(t.data_ptr(), t.stride(0), t.stride(1))
+        _kv_kinds.update({torch.bfloat16: FS_KV_BF16, torch.float16: FS_KV_FP16})
+    kind = _kv_kinds.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"rows are bfloat16 or float16, not {t.dtype}")
+    return kind
 
 
-def _kv_stream(stream, device):
+def _kv_rows(t, name: str, dtype, cache: KvCache, tokens: int, heads: int | None) -> tuple[int, int, int]:
+    """(address, token stride, head stride) of rows [tokens, heads, dim]."""
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != cache.dim or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{name} is [tokens = {tokens}, {heads or 'heads'}, {cache.dim}], not {tuple(shape)}")
+    s0, s1, s2 = t.stride()
+    if t.dtype is not dtype or t.get_device() != cache.device.index or (s2 != 1 and t.numel()):
+        raise ValueError(f"{name}: want {dtype} on {cache.device}, the last dimension contiguous")
+    return t.data_ptr(), s0, s1
+
+
+_current_stream = None  # torch's current stream of a device index, as an address
+
+
+def _kv_stream(stream, device) -> int:
+    global _current_stream
     if stream is not None:
-        return _stream(stream)
-    import torch
+        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if _current_stream is None:
+        import torch
 
-    return torch.cuda.current_stream(device).cuda_stream
+        # (without a torch.cuda.Stream object around the address, whose making takes 2 us of a 10 us call)
+        _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return _current_stream(device.index)
+
+
+# the layouts of fs_kv_new and fs_kv_query (packing is a third of the cost of filling nested structures)
+_KV_NEW = struct.Struct("=6i12q2Q")
+_KV_QUERY = struct.Struct("=2ifi6q")
 
 
 def fs_kv_append(cache: KvCache, batch: KvBatch, k, v, cos=None, sin=None, q=None, q_out=None,
@@ -619,25 +642,33 @@ def fs_kv_append(cache: KvCache, batch: KvBatch, k, v, cos=None, sin=None, q=Non
     """New keys and values [tokens, heads, dim] into the cache, the keys rotated by cos, sin
     [positions, rot / 2] (None: not rotated); q [tokens, q_heads, dim] rotated alike into q_out.
     Enqueued on ``stream`` (default: torch's current one)."""
-    a = fs_kv_new(_kv_dtype(k), 0, 0, 1 if interleaved else 0)
-    a.k = _kv_rows(k, "k", k, cache, batch, cache.heads)
-    a.v = _kv_rows(v, "v", k, cache, batch, cache.heads)
+    dtype, tokens = k.dtype, batch.tokens
+    kind = _kv_dtype(k)
+    kr = _kv_rows(k, "k", dtype, cache, tokens, cache.heads)
+    vr = _kv_rows(v, "v", dtype, cache, tokens, cache.heads)
+    qr = qo = (0, 0, 0)
+    q_heads = 0
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
     if q is not None:
-        a.q = _kv_rows(q, "q", k, cache, batch, None)
-        a.q_out = _kv_rows(q_out, "q_out", k, cache, batch, q.shape[1])
-        a.q_heads = q.shape[1]
+        qr = _kv_rows(q, "q", dtype, cache, tokens, None)
+        q_heads = q.shape[1]
+        qo = _kv_rows(q_out, "q_out", dtype, cache, tokens, q_heads)
+    rot = rows = c_at = s_at = 0
     if (cos is None) != (sin is None):
         raise ValueError("cos and sin go together")
     if cos is not None:
-        if (cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != sin.dtype or "float32" not in str(cos.dtype)
-                or cos.device != cache.device or sin.device != cache.device or not cos.is_contiguous()
-                or not sin.is_contiguous()):
+        index, shape = cache.device.index, cos.shape
+        if (len(shape) != 2 or sin.shape != shape or cos.element_size() != 4 or not cos.is_floating_point()
+                or sin.dtype is not cos.dtype or cos.get_device() != index or sin.get_device() != index
+                or not cos.is_contiguous() or not sin.is_contiguous()):
             raise ValueError("cos and sin are contiguous float32 [positions, rot / 2] on the cache's device")
-        a.rot, a.angle_rows, a.cos, a.sin = 2 * cos.shape[1], cos.shape[0], cos.data_ptr(), sin.data_ptr()
-    _check(lib().fs_kv_append(C.byref(cache.struct), C.byref(batch.struct), C.byref(a), workspace.address,
-                              workspace.bytes, _kv_stream(stream, cache.device)))
+        rows, rot = shape
+        rot, c_at, s_at = 2 * rot, cos.data_ptr(), sin.data_ptr()
+    a = _KV_NEW.pack(kind, q_heads, rot, 1 if interleaved else 0, rows, 0, *kr, *vr, *qr, *qo, c_at, s_at)
+    rc = lib().fs_kv_append(cache.ref, batch.ref, a, workspace.address, workspace.bytes, _kv_stream(stream, cache.device))
+    if rc:
+        _check(rc)
 
 
 def fs_kv_attend(cache: KvCache, batch: KvBatch, q, out, scale: float, window: int = 0, *,
@@ -645,11 +676,15 @@ def fs_kv_attend(cache: KvCache, batch: KvBatch, q, out, scale: float, window: i
     """out [tokens, q_heads, dim] = attention of the batch's new tokens over their sequences' cached
     tokens up to their own (the last ``window`` of them; 0: all). Enqueued on ``stream`` (default:
     torch's current one); returns out."""
-    a = fs_kv_query(_kv_dtype(q), q.shape[1] if q.dim() == 3 else 0, float(scale), int(window),
-                    _kv_rows(q, "q", q, cache, batch, None))
-    a.out = _kv_rows(out, "out", q, cache, batch, q.shape[1])
-    _check(lib().fs_kv_attend(C.byref(cache.struct), C.byref(batch.struct), C.byref(a), workspace.address,
-                              workspace.bytes, _kv_stream(stream, cache.device)))
+    dtype, tokens = q.dtype, batch.tokens
+    kind = _kv_dtype(q)
+    qr = _kv_rows(q, "q", dtype, cache, tokens, None)
+    heads = q.shape[1]
+    o = _kv_rows(out, "out", dtype, cache, tokens, heads)
+    a = _KV_QUERY.pack(kind, heads, scale, window, *qr, *o)
+    rc = lib().fs_kv_attend(cache.ref, batch.ref, a, workspace.address, workspace.bytes, _kv_stream(stream, cache.device))
+    if rc:
+        _check(rc)
     return out
 
 
