@@ -609,8 +609,9 @@ int sm_count_of(int dev) {
 struct KvPlan {
   int row_tile, row_blocks, split, splits, tickets;
   int chunk_tiles;  // blocks of k_kv_chunk a (sequence, key head); 0: no sequence has that many rows
+  int chunk_split, chunk_parts;
   int decode;       // whether some sequence can have few rows
-  size_t part_floats;
+  size_t part_floats, chunk_floats;
 };
 
 // Sequences with more rows (new tokens x query heads of a key head) than this go to
@@ -645,6 +646,18 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
     const int groups = (p.splits + kKvFan - 1) / kKvFan;
     if (groups > 1 && items * (1 + groups) <= kKvTickets) p.tickets = 1 + groups;
   }
+  if (p.chunk_tiles) {
+    // parts of at least four tiles of 128 tokens where whole walks leave half of the SMs without a block
+    // (more parts for balance alone cost more than they give: ragged chunks 105 us whole, 220 us in twos)
+    const long long blocks = (long long)b->batch * c->heads * p.chunk_tiles;
+    const int walk = (std::max(1, window ? (int)std::min<long long>(b->max_length, (long long)window + kKvChunkRows + 126) : b->max_length) + 127) / 128;
+    long long want = sms / blocks;
+    want = std::max(1ll, std::min({want, (long long)walk / 4, (long long)kKvFan}));
+    const int tiles = (int)((walk + want - 1) / want);
+    p.chunk_split = tiles * 128;
+    p.chunk_parts = (walk + tiles - 1) / tiles;
+    p.chunk_floats = p.chunk_parts > 1 ? (size_t)blocks * p.chunk_parts * kKvChunkRows * (c->dim + 4) : 0;
+  }
   p.part_floats = p.decode && p.splits > 1 ? (size_t)items * p.splits * p.row_tile * (c->dim + 2) : 0;
   return p;
 }
@@ -656,7 +669,11 @@ size_t part_floats_bound(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads
   const long long rows = std::min<long long>(kFewRows, (long long)std::max(1, b->max_new) * (q_heads / c->heads));
   const long long items = std::min<long long>(kKvTickets, (long long)std::max(1, b->batch) * c->heads * ((rows + 7) / 8));
   const long long len = std::max(1, b->max_length);
-  return (size_t)(std::max(8ll * sms + 2 * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2));
+  const long long decode = std::max(8ll * sms + 2 * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2);
+  // chunks: at most sms parts in all
+  const long long all = (long long)std::max(1, b->max_new) * (q_heads / c->heads);
+  const long long blocks = all > kFewRows ? std::max(1, b->batch) * (long long)c->heads * ((all + kKvChunkRows - 1) / kKvChunkRows) : 0;
+  return (size_t)(decode + std::min((long long)sms, kKvFan * blocks) * kKvChunkRows * (c->dim + 4));
 }
 
 int device_sms(int* sms) {
@@ -773,7 +790,7 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   int sms = 0;
   if (int rc = device_sms(&sms)) return rc;
   const KvPlan p = plan_of(cache, batch, qu->q_heads, qu->window, sms);
-  if (int rc = check_workspace(workspace, workspace_bytes, (int64_t)(kKvPartAt + 4 * p.part_floats))) return rc;
+  if (int rc = check_workspace(workspace, workspace_bytes, (int64_t)(kKvPartAt + 4 * (p.part_floats + p.chunk_floats)))) return rc;
   if (p.chunk_tiles > 65535) return say(FS_EINVAL, "max_new = %d: too many rows for one call", batch->max_new);
 
   KvAttendArgs a{};
@@ -791,9 +808,11 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   if (p.chunk_tiles) {
     KvAttendArgs ca = a;
     ca.min_rows = kFewRows, ca.max_rows = INT_MAX;
+    ca.split = p.chunk_split;
+    ca.part = a.part + p.part_floats;
     if (int rc = kv_tensor_map(&mk, *cache, cache->k, cache->page_tokens, false)) return rc;
     if (int rc = kv_tensor_map(&mv, *cache, cache->v, cache->page_tokens, false)) return rc;
-    const cudaError_t e = launch_kv_chunk(mk, mv, ca, cache->dim, qu->dtype, p.chunk_tiles, st);
+    const cudaError_t e = launch_kv_chunk(mk, mv, ca, cache->dim, qu->dtype, p.chunk_tiles, p.chunk_parts, st);
     if (e != cudaSuccess) return cuda_say(e, "launch (fs_kv_attend, chunks)");
   }
   if (p.decode) {

@@ -158,6 +158,6 @@ cudaError_t launch_kv_decode(const CUtensorMap& mk, const CUtensorMap& mv, const
                              int row_tile, int row_blocks, int splits, cudaStream_t s);
 constexpr int kKvChunkRows = 256;  // rows of a block
 cudaError_t launch_kv_chunk(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int dim, int dtype,
-                            int tiles, cudaStream_t s);
+                            int tiles, int parts, cudaStream_t s);
 
 }  // namespace fs

@@ -172,33 +172,56 @@ __device__ __forceinline__ float row_top(float (&x)[kTok], float c, const float2
   return top;
 }
 
+// The keys that rows [r0, r_end) of a sequence see: a walk over [begin, end), in parts of
+// a.split tokens.
+struct Walk {
+  int begin, end, parts;
+};
+__device__ __forceinline__ Walk walk_of(const KvAttendArgs& a, const KvSeq& s, int r0, int r_end) {
+  const int base = s.len - s.count;
+  const int pos0 = base + r0 / a.v.group, pos1 = base + (r_end - 1) / a.v.group;
+  Walk w;
+  w.end = max(pos1 + 1, 0);
+  w.begin = (a.window ? max(pos0 - a.window + 1, 0) : 0) & ~(kTok - 1);
+  w.parts = max(1, (w.end - w.begin + a.split - 1) / a.split);
+  return w;
+}
+
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant__ CUtensorMap mk,
                                                              const __grid_constant__ CUtensorMap mv, const KvAttendArgs a) {
   using C = Cfg<D>;
+  constexpr int kPart = 2 * kTileRows * (D + 4);  // floats of a part's result: per row its sums, m, l (and two to keep 16 bytes)
   extern __shared__ unsigned char raw[];
   const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
   const uint32_t q_at = smem, ring_at = smem + C::kQ, raw_at = ring_at + C::kStages * C::kSlot;
   Bars& bars = *reinterpret_cast<Bars*>(raw + (smem - smem_u32(raw)) + C::kQ + (size_t)C::kStages * C::kSlot +
                                         C::kRaw * C::kRawSlot);
   const KvView& v = a.v;
-  const int tile = gridDim.y - 1 - blockIdx.y;  // the longest walks first
   const int h = blockIdx.x % v.heads, b = blockIdx.x / v.heads;
   const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int item = blockIdx.y * gridDim.x + blockIdx.x;
 
   KvSeq s;
   if (!kv_seq(v, b, s)) {
-    if (threadIdx.x == 0 && tile == 0) kv_flag(v, KV_ST_BATCH);
+    if (threadIdx.x == 0 && blockIdx.y == 0) kv_flag(v, KV_ST_BATCH);
     return;
   }
-  const int rows = s.count * v.group, r0 = tile * (2 * kTileRows);
-  if (r0 >= rows || rows <= a.min_rows || rows > a.max_rows) return;
+  // each sequence's last rows first: theirs are its longest walks
+  const int rows = s.count * v.group, part = blockIdx.z;
+  const int tile = (rows + 2 * kTileRows - 1) / (2 * kTileRows) - 1 - (int)blockIdx.y, r0 = tile * (2 * kTileRows);
+  if (tile < 0 || rows <= a.min_rows || rows > a.max_rows) return;
   const int r_end = min(rows, r0 + 2 * kTileRows);
   const int n_sub = r_end - r0 > kTileRows ? 2 : 1;
   const int base = s.len - s.count;  // position of the sequence's first new token
-  const int pos0 = base + r0 / v.group, pos1 = base + (r_end - 1) / v.group;
-  const int kv_hi = max(pos1 + 1, 0), kv_lo = a.window ? max(pos0 - a.window + 1, 0) : 0;
-  const int begin = kv_lo & ~(kTok - 1);
+  const Walk walk = walk_of(a, s, r0, r_end);
+  const int n_parts = walk.parts;
+  if (n_parts > (int)gridDim.z) {  // a length beyond max_length
+    if (threadIdx.x == 0 && part == 0) kv_flag(v, KV_ST_BATCH);
+    return;
+  }
+  if (part >= n_parts) return;
+  const int begin = walk.begin + part * a.split, kv_hi = min(begin + a.split, walk.end);  // this block's part
   const int n = (kv_hi - begin + kTok - 1) / kTok;  // tiles of the cache; 0: no row sees a token
 
   if (threadIdx.x == 0) {
@@ -357,25 +380,42 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
         fence_after();
       }
       ok = __all_sync(~0u, ok);
-      const float inv = bars.v_ref * (1.f / 128.f) / l;
-      T* to = static_cast<T*>(a.out) + (long long)(s.first + r / v.group) * a.out_token + (h * v.group + r % v.group) * a.out_head;
+      const float up = bars.v_ref * (1.f / 128.f), inv = up / l;
+      if (n_parts == 1) {
+        T* to = static_cast<T*>(a.out) + (long long)(s.first + r / v.group) * a.out_token + (h * v.group + r % v.group) * a.out_head;
 #pragma unroll
-      for (int k = 0; k < D / 32; ++k) {
-        uint32_t x[32];
-        if (n > 0) {
-          tmem_ld32(x, o_at + 32 * k);
-          wait_ld();
-        }
-        if (ok && r < r_end) {
+        for (int k = 0; k < D / 32; ++k) {
+          uint32_t x[32];
+          if (n > 0) {
+            tmem_ld32(x, o_at + 32 * k);
+            wait_ld();
+          }
+          if (ok && r < r_end) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t y[4];
+            for (int i = 0; i < 4; ++i) {
+              uint32_t y[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-              y[u] = l != 0.f ? Elem<T>::pack(__uint_as_float(x[8 * i + 2 * u]) * inv, __uint_as_float(x[8 * i + 2 * u + 1]) * inv) : 0u;
-            *reinterpret_cast<uint4*>(to + 32 * k + 8 * i) = make_uint4(y[0], y[1], y[2], y[3]);
+              for (int u = 0; u < 4; ++u)
+                y[u] = l != 0.f ? Elem<T>::pack(__uint_as_float(x[8 * i + 2 * u]) * inv, __uint_as_float(x[8 * i + 2 * u + 1]) * inv) : 0u;
+              *reinterpret_cast<uint4*>(to + 32 * k + 8 * i) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
           }
         }
+      } else {
+        float* to = a.part + ((long long)item * gridDim.z + part) * kPart + threadIdx.x * (D + 4);
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+          uint32_t x[32];
+          tmem_ld32(x, o_at + 32 * k);
+          wait_ld();
+          if (r < r_end) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+              *reinterpret_cast<float4*>(to + 32 * k + i) = make_float4(__uint_as_float(x[i]) * up, __uint_as_float(x[i + 1]) * up,
+                                                                        __uint_as_float(x[i + 2]) * up, __uint_as_float(x[i + 3]) * up);
+          }
+        }
+        if (r < r_end) *reinterpret_cast<float2*>(to + D) = make_float2(m, l);
       }
     }
   } else if (w < 12) {
@@ -567,11 +607,58 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
   if (w == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
+// The parts of a walk, joined: a group of D / 4 lanes a row, every part's load under way at once.
 template <int D, typename T>
-cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int tiles, cudaStream_t s) {
+__global__ void __launch_bounds__(256) k_kv_chunk_join(const KvAttendArgs a, int max_parts) {
+  constexpr int kPart = 2 * kTileRows * (D + 4), kRowsHere = 256 / (D / 4);
+  const KvView& v = a.v;
+  const int h = blockIdx.x % v.heads, b = blockIdx.x / v.heads;
+  KvSeq s;
+  if (!kv_seq(v, b, s)) return;
+  const int rows = s.count * v.group;
+  const int tile = (rows + 2 * kTileRows - 1) / (2 * kTileRows) - 1 - (int)blockIdx.y, r0 = tile * (2 * kTileRows);
+  if (tile < 0 || rows <= a.min_rows || rows > a.max_rows) return;
+  const int r_end = min(rows, r0 + 2 * kTileRows);
+  const Walk walk = walk_of(a, s, r0, r_end);
+  const int rr = blockIdx.z * kRowsHere + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4, r = r0 + rr;
+  if (walk.parts == 1 || walk.parts > max_parts || r >= r_end) return;
+  const float* at = a.part + (long long)(blockIdx.y * gridDim.x + blockIdx.x) * max_parts * kPart + rr * (D + 4);
+  float2 ml[kKvFan];
+  float4 y[kKvFan];
+#pragma unroll
+  for (int i = 0; i < kKvFan; ++i)
+    if (i < walk.parts) {
+      ml[i] = *reinterpret_cast<const float2*>(at + (long long)i * kPart + D);
+      y[i] = *reinterpret_cast<const float4*>(at + (long long)i * kPart + d);
+    }
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kKvFan; ++i)
+    if (i < walk.parts) top = fmaxf(top, ml[i].x);
+  const float off = top == -INFINITY ? 0.f : top;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  float lsum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kKvFan; ++i)
+    if (i < walk.parts) {
+      const float f = ex2(ml[i].x - off);
+      lsum = fmaf(ml[i].y, f, lsum);
+      x.x = fmaf(y[i].x, f, x.x), x.y = fmaf(y[i].y, f, x.y), x.z = fmaf(y[i].z, f, x.z), x.w = fmaf(y[i].w, f, x.w);
+    }
+  const float inv = lsum != 0.f ? 1.f / lsum : 0.f;
+  T* to = static_cast<T*>(a.out) + (long long)(s.first + r / v.group) * a.out_token + (h * v.group + r % v.group) * a.out_head + d;
+  *reinterpret_cast<uint2*>(to) = make_uint2(Elem<T>::pack(x.x * inv, x.y * inv), Elem<T>::pack(x.z * inv, x.w * inv));
+}
+
+template <int D, typename T>
+cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int tiles, int parts, cudaStream_t s) {
   static const cudaError_t limit = raise_smem_limit(reinterpret_cast<const void*>(k_kv_chunk<D, T>), Cfg<D>::kSmem);
   if (limit != cudaSuccess) return limit;
-  k_kv_chunk<D, T><<<dim3(a.v.heads * a.v.batch, tiles), kThreads, Cfg<D>::kSmem, s>>>(mk, mv, a);
+  k_kv_chunk<D, T><<<dim3(a.v.heads * a.v.batch, tiles, parts), kThreads, Cfg<D>::kSmem, s>>>(mk, mv, a);
+  note_launch();
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || parts == 1) return e;
+  k_kv_chunk_join<D, T><<<dim3(a.v.heads * a.v.batch, tiles, 2 * kTileRows * (D / 4) / 256), 256, 0, s>>>(a, parts);
   note_launch();
   return cudaGetLastError();
 }
@@ -579,10 +666,10 @@ cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendA
 }  // namespace
 
 cudaError_t launch_kv_chunk(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int dim, int dtype,
-                            int tiles, cudaStream_t s) {
+                            int tiles, int parts, cudaStream_t s) {
   const bool h = dtype == FS_KV_FP16;
-  if (dim == 128) return h ? launch<128, __half>(mk, mv, a, tiles, s) : launch<128, __nv_bfloat16>(mk, mv, a, tiles, s);
-  return h ? launch<64, __half>(mk, mv, a, tiles, s) : launch<64, __nv_bfloat16>(mk, mv, a, tiles, s);
+  if (dim == 128) return h ? launch<128, __half>(mk, mv, a, tiles, parts, s) : launch<128, __nv_bfloat16>(mk, mv, a, tiles, parts, s);
+  return h ? launch<64, __half>(mk, mv, a, tiles, parts, s) : launch<64, __nv_bfloat16>(mk, mv, a, tiles, parts, s);
 }
 
 }  // namespace fs

@@ -107,6 +107,13 @@ def test_one_long_sequence(fsb, cuda):
     run(cuda, fsb, 7, [(9000, 3), (17, 2)], 2, 4, 64, 16, window=5000)
 
 
+@pytest.mark.parametrize("dim,window", [(128, 0), (128, 3000), (64, 0)])
+def test_chunks_on_long_sequences(fsb, cuda, dim, window):
+    """Few rows over long caches: walks in parts, joined by a second kernel; lengths that end a part early."""
+    run(cuda, fsb, 16, [(9001, 40), (700, 33), (0, 0), (5120, 70)], 1, 4, dim, 64, window=window)
+    run(cuda, fsb, 17, [(20000, 129)], 1, 1, dim, 128, window=window)
+
+
 def test_cache_laid_out_by_token(fsb, cuda):
     run(cuda, fsb, 8, [(200, 1), (70, 3)], 4, 2, 128, 32, by_token=True)
     run(cuda, fsb, 8, [(300, 150), (70, 3)], 4, 2, 64, 32, by_token=True)
