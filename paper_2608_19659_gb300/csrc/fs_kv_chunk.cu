@@ -39,8 +39,11 @@ struct Cfg {
   static constexpr size_t kSmem = 1024 + kQ + (size_t)kStages * kSlot + kRaw * kRawSlot + 1280;
 };
 
+// (a wait must not find its barrier two phases on: a phase comes round in no less than the ring)
+constexpr int kUsed = 8;
+
 struct Bars {
-  uint64_t full[8], empty[8], raw_full[4], raw_empty[4], s_full[2], p_full[2][2], pv_done[2], end;
+  uint64_t full[8], used[kUsed], raw_full[4], raw_empty[4], s_full[2], p_full[2][2], pv_done[2], end;
   float2 scale[4][8];    // per tile of codes and 16 tokens: what keys are multiplied by (two halves), the values' scale
   uint32_t cut[4];       // per tile of codes: some tokens' values are to be 0
   float2 v_scale[8][8];  // per tile (mod 8) and 16 tokens: log2 of the values' scale, and its reciprocal
@@ -225,7 +228,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
   const int n = (kv_hi - begin + kTok - 1) / kTok;  // tiles of the cache; 0: no row sees a token
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < C::kStages; ++i) mbar_init(&bars.full[i], 128), mbar_init(&bars.empty[i], 1);
+    for (int i = 0; i < C::kStages; ++i) mbar_init(&bars.full[i], 128);
+    for (int i = 0; i < kUsed; ++i) mbar_init(&bars.used[i], 1);
     for (int i = 0; i < C::kRaw; ++i) mbar_init(&bars.raw_full[i], 1), mbar_init(&bars.raw_empty[i], 128);
     for (int t = 0; t < 2; ++t) mbar_init(&bars.s_full[t], 1), mbar_init(&bars.p_full[t][0], 128), mbar_init(&bars.p_full[t][1], 128), mbar_init(&bars.pv_done[t], 1);
     mbar_init(&bars.end, 1);
@@ -330,10 +334,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
           const float f = grow ? ex2(m - top) : 1.f;
           if (grow) m = top;
           l *= f;
-          if (j > 0) {  // (the first product overwrites O)
-            ok = wait_bar(&bars.pv_done[t], (j - 1) & 1, v);
-            if (!__all_sync(~0u, ok)) break;
-            fence_after();
+          if (j > 0) {  // (the first product overwrites O; those before this S have ended with it)
 #pragma unroll 1
             for (int k = 0; k < D / 16; ++k) {
               uint32_t y[16];
@@ -376,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
       }
       // ------------------------------------------------------------ result
       if (ok && n > 0) {
-        ok = wait_bar(&bars.pv_done[t], (n - 1) & 1, v);
+        ok = wait_bar(&bars.pv_done[t], 0, v);
         fence_after();
       }
       ok = __all_sync(~0u, ok);
@@ -462,7 +463,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
         bars.v_scale[(i >> 1) & 7][id] = make_float2((float)e, exp2_int(-e));
       }
       mbar_arrive(&bars.raw_empty[rs]);
-      if (!wait_bar(&bars.empty[st], ((i / C::kStages) & 1) ^ 1, v)) break;
+      // the slot's last tile, kStages / 2 of the cache's tiles ago: keys' products go with the tile before
+      const int use = (i >> 1) - C::kStages / 2 - (values ? 0 : 1);
+      if (use >= 0 && !wait_bar(&bars.used[use % kUsed], (use / kUsed) & 1, v)) break;
       const uint32_t row = ring_at + st * C::kSlot + to;
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
@@ -562,7 +565,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
         qk(t, 0);
         commit(&bars.s_full[t]);
       }
-      commit(&bars.empty[0]);
     }
     int vs = 1, ks = 2;
     uint32_t v_par = 0, k_par = 0;  // parities of the slots' rounds
@@ -575,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
           if (ok && one) pv(t, vs, half, j > 0);
         }
         if (!ok) break;
-        if (one) commit(&bars.pv_done[t]);
+        if (one && j + 1 == n_u) commit(&bars.pv_done[t]);
         if (j + 1 < n_u) {
           if (t == 0) ok = wait_all(&bars.full[ks], k_par);
           if (!ok) break;
@@ -586,10 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
           }
         }
       }
-      if (one) {
-        commit(&bars.empty[vs]);
-        if (j + 1 < n_u) commit(&bars.empty[ks]);
-      }
+      if (one) commit(&bars.used[j % kUsed]);  // tile j's values and the keys of the next
       vs += 2;
       if (vs >= C::kStages) vs -= C::kStages, v_par ^= 1;
       ks += 2;
