@@ -230,6 +230,8 @@ __global__ void __launch_bounds__(128, 6) k_kv_append(const KvAppendArgs a) {
   const int b = blockIdx.z, piece = blockIdx.x;
   const int unit = threadIdx.x / kLanes, l = threadIdx.x % kLanes;
   const int job = blockIdx.y * kUnits + unit;  // [0, heads) keys, [heads, 2 heads) values, then queries
+  pdl_trigger();
+  pdl_wait();
   KvSeq s;
   if (!kv_seq(a.v, b, s)) {
     if (threadIdx.x == 0) kv_flag(a.v, KV_ST_BATCH);
@@ -348,6 +350,8 @@ __global__ void __launch_bounds__(128, 8) k_kv_append_one(const KvAppendArgs a) 
   constexpr int kLanes = D / 8, kUnits = 128 / kLanes;
   const int b = blockIdx.y, unit = threadIdx.x / kLanes, l = threadIdx.x % kLanes;
   const int job = blockIdx.x * kUnits + unit, H = a.v.heads;
+  pdl_trigger();
+  pdl_wait();
   KvSeq s;
   if (!kv_seq(a.v, b, s)) {
     if (threadIdx.x == 0) kv_flag(a.v, KV_ST_BATCH);
@@ -420,6 +424,8 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) k_kv_append_many(con
   __shared__ float sm_amax[kThreads / 32];
   const int b = blockIdx.z, piece = blockIdx.x;
   const int unit = threadIdx.x / kLanes, l = threadIdx.x % kLanes;
+  pdl_trigger();
+  pdl_wait();
   KvSeq s;
   if (!kv_seq(a.v, b, s)) {
     if (threadIdx.x == 0) kv_flag(a.v, KV_ST_BATCH);
@@ -558,24 +564,14 @@ cudaError_t launch_append(const KvAppendArgs& a, int pieces, bool many, cudaStre
   const int q_heads = a.q ? a.q_heads : 0;
   constexpr int kUnits = 128 / (D / 8);
   const int unit_blocks = (2 * a.v.heads + q_heads + kUnits - 1) / kUnits;
-  if (a.v.max_new == 1) {
-    k_kv_append_one<D, T><<<dim3(unit_blocks, a.v.batch), 128, 0, s>>>(a);
-  } else if (!many) {
-    k_kv_append<D, T><<<dim3(pieces, unit_blocks, a.v.batch), 128, 0, s>>>(a);
-  } else {
-    const dim3 grid(pieces, 2 * a.v.heads + (q_heads + kQHeads - 1) / kQHeads, a.v.batch);
-    const int its = (D / 8 << a.v.log_page) / 128;  // rows a unit of a block of 128
-    if (its <= 2)
-      k_kv_append_many<D, T, 2, 128><<<grid, 128, 0, s>>>(a);
-    else if (its == 4)
-      k_kv_append_many<D, T, 4, 128><<<grid, 128, 0, s>>>(a);
-    else if (its == 8)
-      k_kv_append_many<D, T, 4, 256><<<grid, 256, 0, s>>>(a);
-    else
-      k_kv_append_many<D, T, 4, 512><<<grid, 512, 0, s>>>(a);
-  }
-  note_launch();
-  return cudaGetLastError();
+  if (a.v.max_new == 1) return launch_pdl(k_kv_append_one<D, T>, dim3(unit_blocks, a.v.batch), dim3(128), 0, s, a);
+  if (!many) return launch_pdl(k_kv_append<D, T>, dim3(pieces, unit_blocks, a.v.batch), dim3(128), 0, s, a);
+  const dim3 grid(pieces, 2 * a.v.heads + (q_heads + kQHeads - 1) / kQHeads, a.v.batch);
+  const int its = (D / 8 << a.v.log_page) / 128;  // rows a unit of a block of 128
+  if (its <= 2) return launch_pdl(k_kv_append_many<D, T, 2, 128>, grid, dim3(128), 0, s, a);
+  if (its == 4) return launch_pdl(k_kv_append_many<D, T, 4, 128>, grid, dim3(128), 0, s, a);
+  if (its == 8) return launch_pdl(k_kv_append_many<D, T, 4, 256>, grid, dim3(256), 0, s, a);
+  return launch_pdl(k_kv_append_many<D, T, 4, 512>, grid, dim3(512), 0, s, a);
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -639,7 +635,7 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
   } else {
     // a part for every block that is resident at once; parts for two such waves where they are few
     // an item, because sequences differ in length
-    const long long slots = (long long)sms * (c->dim == 128 ? 2 : 4);
+    const long long slots = (long long)sms * (c->dim == 128 ? 3 : 6);
     const long long want = 2 * items <= slots ? slots / items : (2 * slots + items - 1) / items;
     p.split = std::clamp((int)((len + want - 1) / want + 127) / 128 * 128, kMinSplit, kMaxSplit);
     p.splits = (len + p.split - 1) / p.split;
@@ -663,13 +659,13 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
 }
 
 // At least plan_of's part_floats, and nondecreasing in the batch's sizes: items * splits
-// is at most 8 sms + 2 items where the items alone set the parts' length, items *
+// is at most 12 sms + 2 items where the items alone set the parts' length, items *
 // ceil(len / kMaxSplit) where that does.
 size_t part_floats_bound(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int sms) {
   const long long rows = std::min<long long>(kFewRows, (long long)std::max(1, b->max_new) * (q_heads / c->heads));
   const long long items = std::min<long long>(kKvTickets, (long long)std::max(1, b->batch) * c->heads * ((rows + 7) / 8));
   const long long len = std::max(1, b->max_length);
-  const long long decode = std::max(8ll * sms + 2 * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2);
+  const long long decode = std::max(12ll * sms + 2 * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2);
   // chunks: at most sms parts in all
   const long long all = (long long)std::max(1, b->max_new) * (q_heads / c->heads);
   const long long blocks = all > kFewRows ? std::max(1, b->batch) * (long long)c->heads * ((all + kKvChunkRows - 1) / kKvChunkRows) : 0;

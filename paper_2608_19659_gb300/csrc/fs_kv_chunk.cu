@@ -205,6 +205,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
   const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int item = blockIdx.y * gridDim.x + blockIdx.x;
 
+  pdl_trigger();
+  pdl_wait();
   KvSeq s;
   if (!kv_seq(v, b, s)) {
     if (threadIdx.x == 0 && blockIdx.y == 0) kv_flag(v, KV_ST_BATCH);
@@ -612,6 +614,8 @@ __global__ void __launch_bounds__(256) k_kv_chunk_join(const KvAttendArgs a, int
   constexpr int kPart = 2 * kTileRows * (D + 4), kRowsHere = 256 / (D / 4);
   const KvView& v = a.v;
   const int h = blockIdx.x % v.heads, b = blockIdx.x / v.heads;
+  pdl_trigger();
+  pdl_wait();
   KvSeq s;
   if (!kv_seq(v, b, s)) return;
   const int rows = s.count * v.group;
@@ -653,13 +657,9 @@ template <int D, typename T>
 cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int tiles, int parts, cudaStream_t s) {
   static const cudaError_t limit = raise_smem_limit(reinterpret_cast<const void*>(k_kv_chunk<D, T>), Cfg<D>::kSmem);
   if (limit != cudaSuccess) return limit;
-  k_kv_chunk<D, T><<<dim3(a.v.heads * a.v.batch, tiles, parts), kThreads, Cfg<D>::kSmem, s>>>(mk, mv, a);
-  note_launch();
-  cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_pdl(k_kv_chunk<D, T>, dim3(a.v.heads * a.v.batch, tiles, parts), dim3(kThreads), Cfg<D>::kSmem, s, mk, mv, a);
   if (e != cudaSuccess || parts == 1) return e;
-  k_kv_chunk_join<D, T><<<dim3(a.v.heads * a.v.batch, tiles, 2 * kTileRows * (D / 4) / 256), 256, 0, s>>>(a, parts);
-  note_launch();
-  return cudaGetLastError();
+  return launch_pdl(k_kv_chunk_join<D, T>, dim3(a.v.heads * a.v.batch, tiles, 2 * kTileRows * (D / 4) / 256), dim3(256), 0, s, a, parts);
 }
 
 }  // namespace

@@ -25,7 +25,7 @@
 namespace fs {
 namespace {
 
-constexpr int kWarps = 4, kStages = 3, kTile = 32;
+constexpr int kWarps = 4, kStages = 2, kTile = 32;
 constexpr float kUp = 7.f, kSlack = 8.f;  // log2: weights are scaled by 2^kUp, and m may lag behind by kSlack: 2^15 at most
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -72,17 +72,20 @@ __global__ void __launch_bounds__(kWarps * 32)
   const int h = blockIdx.y / row_blocks, rb = blockIdx.y % row_blocks;
   const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tid = lane & 3;
 
+  // before the kernel ahead in the stream has ended: nothing that it may write
+  pdl_trigger();
   if (threadIdx.x < 2)  // (the copies' descriptions)
     asm volatile("prefetch.tensormap [%0];" ::"l"(threadIdx.x ? &mv : &mk) : "memory");
+  if (lane == 0)
+    for (int i = 0; i < kStages; ++i) mbar_init(&bars[w][i], 1);
+  __syncwarp();
+  pdl_wait();
   // the page of this lane's first tile, asked for before the sequence's length is known: without a
   // window the tile's place does not depend on it (entries beyond the sequence are read, not used)
   const int early_at = (part * a.split + (w + lane * kWarps) * kTile) >> v.log_page;
   int early = 0;
   if (!a.window && early_at < v.table_stride)
     asm volatile("ld.global.s32 %0, [%1];" : "=r"(early) : "l"(v.page_table + (long long)b * v.table_stride + early_at));
-  if (lane == 0)
-    for (int i = 0; i < kStages; ++i) mbar_init(&bars[w][i], 1);
-  __syncwarp();
   KvSeq s;
   if (!kv_seq(v, b, s)) {
     if (threadIdx.x == 0 && part == 0) kv_flag(v, KV_ST_BATCH);
@@ -540,9 +543,8 @@ cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendA
                    cudaStream_t s) {
   static const cudaError_t limit = raise_smem_limit(reinterpret_cast<const void*>(k_kv_decode<D, NT, T>), decode_smem<D>());
   if (limit != cudaSuccess) return limit;
-  k_kv_decode<D, NT, T><<<dim3(splits, a.v.heads * row_blocks, a.v.batch), kWarps * 32, decode_smem<D>(), s>>>(mk, mv, a);
-  note_launch();
-  return cudaGetLastError();
+  return launch_pdl(k_kv_decode<D, NT, T>, dim3(splits, a.v.heads * row_blocks, a.v.batch), dim3(kWarps * 32), decode_smem<D>(), s,
+                    mk, mv, a);
 }
 
 template <int D, typename T>
