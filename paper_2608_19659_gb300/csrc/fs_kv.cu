@@ -633,10 +633,10 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
     p.split = (len + 127) / 128 * 128;
     p.splits = 1;
   } else {
-    // a part for every block that is resident at once; parts for two such waves where they are few
-    // an item, because sequences differ in length
+    // a part for every block that is resident at once; parts for three such waves where they are
+    // few an item, because sequences differ in length (64 of up to 8192 tokens: 67 us with two)
     const long long slots = (long long)sms * (c->dim == 128 ? 3 : 6);
-    const long long want = 2 * items <= slots ? slots / items : (2 * slots + items - 1) / items;
+    const long long want = 2 * items <= slots ? slots / items : (3 * slots + items - 1) / items;
     p.split = std::clamp((int)((len + want - 1) / want + 127) / 128 * 128, kMinSplit, kMaxSplit);
     p.splits = (len + p.split - 1) / p.split;
     const int groups = (p.splits + kKvFan - 1) / kKvFan;
@@ -659,13 +659,13 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
 }
 
 // At least plan_of's part_floats, and nondecreasing in the batch's sizes: items * splits
-// is at most 12 sms + 2 items where the items alone set the parts' length, items *
+// is at most 18 sms + 2 items where the items alone set the parts' length, items *
 // ceil(len / kMaxSplit) where that does.
 size_t part_floats_bound(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int sms) {
   const long long rows = std::min<long long>(kFewRows, (long long)std::max(1, b->max_new) * (q_heads / c->heads));
   const long long items = std::min<long long>(kKvTickets, (long long)std::max(1, b->batch) * c->heads * ((rows + 7) / 8));
   const long long len = std::max(1, b->max_length);
-  const long long decode = std::max(12ll * sms + 2 * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2);
+  const long long decode = std::max(18ll * sms + 2 * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2);
   // chunks: at most sms parts in all
   const long long all = (long long)std::max(1, b->max_new) * (q_heads / c->heads);
   const long long blocks = all > kFewRows ? std::max(1, b->batch) * (long long)c->heads * ((all + kKvChunkRows - 1) / kKvChunkRows) : 0;

@@ -469,27 +469,37 @@ __global__ void __launch_bounds__(kWarps * 32)
   unsigned* ticket = a.ticket + item * a.tickets;
   for (bool first = a.tickets > 1;; first = false) {
     const int g = first ? me / kKvFan : 0, g0 = first ? g * kKvFan : 0, g_n = first ? min(kKvFan, count - g0) : count;
-    __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) {
+      __threadfence();  // (the block's results, ordered before by the barrier, become visible with the ticket)
       unsigned* at = ticket + (first ? 1 + g : 0);
       const unsigned t = atomicAdd(at, 1u);
       sm_last = t == (unsigned)g_n - 1;
       if (sm_last) *at = 0;  // as it was found
+      __threadfence();
     }
     __syncthreads();
     if (!sm_last) return;
-    __threadfence();
     const bool done = g_n == count;  // nothing is left to join with
     float* from = parts + (long long)(g0 * step) * kPart;
-    // sixteen results at a time: their weights first, then their sums with every load under way at once
+    // sixteen results at a time, every load of a unit under way at once, the first unit's beside
+    // those of the weights
     float4 acc[kUnits];
     float lsum[kUnits], top[kUnits];
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f), lsum[i] = 0.f, top[i] = -INFINITY;
     for (int i0 = 0; i0 < g_n; i0 += kKvFan) {
       const int m_n = min(kKvFan, g_n - i0);
-      __syncthreads();
+      float4 y[kKvFan];
+      auto load = [&](int k) {
+        const int u = threadIdx.x + k * kWarps * 32, r = u / (D / 4), d = u % (D / 4) * 4;
+#pragma unroll
+        for (int i = 0; i < kKvFan; ++i)
+          if (i < m_n && r < n_rows)
+            y[i] = __ldcg(reinterpret_cast<const float4*>(from + (long long)((i0 + i) * step) * kPart + r * D + d));
+      };
+      load(0);
+      if (i0) __syncthreads();
       for (int u = threadIdx.x; u < kRows * kKvFan; u += kWarps * 32) {
         const int r = u / kKvFan, i = u % kKvFan;
         float2 ml = make_float2(-INFINITY, 0.f);
@@ -500,7 +510,8 @@ __global__ void __launch_bounds__(kWarps * 32)
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < kUnits; ++k) {
-        const int u = threadIdx.x + k * kWarps * 32, r = u / (D / 4), d = u % (D / 4) * 4;
+        const int u = threadIdx.x + k * kWarps * 32, r = u / (D / 4);
+        if (k) load(k);
         if (r >= n_rows) continue;
         float m_new = top[k];
 #pragma unroll
@@ -508,10 +519,6 @@ __global__ void __launch_bounds__(kWarps * 32)
         const float base = m_new == -INFINITY ? 0.f : m_new, f0 = ex2(top[k] - base);
         top[k] = m_new, lsum[k] *= f0;
         acc[k].x *= f0, acc[k].y *= f0, acc[k].z *= f0, acc[k].w *= f0;
-        float4 y[kKvFan];
-#pragma unroll
-        for (int i = 0; i < kKvFan; ++i)
-          if (i < m_n) y[i] = __ldcg(reinterpret_cast<const float4*>(from + (long long)((i0 + i) * step) * kPart + r * D + d));
 #pragma unroll
         for (int i = 0; i < kKvFan; ++i)
           if (i < m_n) {
@@ -522,13 +529,14 @@ __global__ void __launch_bounds__(kWarps * 32)
           }
       }
     }
+    if (!done) __syncthreads();  // (every maximum and sum has been read)
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
       const int u = threadIdx.x + k * kWarps * 32, r = u / (D / 4), d = u % (D / 4) * 4;
       if (r >= n_rows) continue;
       if (done) {
         write_out(r, d, acc[k], lsum[k]);
-      } else {  // in the place of the first of them (every maximum and sum there has been read)
+      } else {  // in the place of the first of them
         *reinterpret_cast<float4*>(from + r * D + d) = acc[k];
         if (d == 0) *reinterpret_cast<float2*>(from + kRows * D + 2 * r) = make_float2(top[k], lsum[k]);
       }
