@@ -603,7 +603,7 @@ int sm_count_of(int dev) {
 // How an attend call is cut up (see k_kv_decode): rows of a (sequence, key head) in tiles
 // of row_tile, the cache axis in parts of `split` tokens.
 struct KvPlan {
-  int row_tile, row_blocks, split, splits, tickets;
+  int row_tile, row_blocks, split, splits, cluster, tickets;
   int chunk_tiles;  // blocks of k_kv_chunk a (sequence, key head); 0: no sequence has that many rows
   int chunk_split, chunk_parts;
   int decode;       // whether some sequence can have few rows
@@ -614,7 +614,7 @@ struct KvPlan {
 // k_kv_chunk.
 constexpr int kFewRows = 64;
 
-constexpr int kMinSplit = 256, kMaxSplit = 4096;
+constexpr int kMinSplit = 128, kMaxSplit = 4096;
 
 KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int window, int sms) {
   KvPlan p{};
@@ -628,7 +628,7 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
   const long long items = (long long)std::max(1, b->batch) * c->heads * p.row_blocks;
   // (a window's tiles may begin up to 31 tokens early)
   const int len = std::max(1, window ? (int)std::min<long long>(b->max_length, (long long)window + b->max_new + 30) : b->max_length);
-  p.tickets = 1;
+  p.tickets = p.cluster = 1;
   if (items > kKvTickets) {
     p.split = (len + 127) / 128 * 128;
     p.splits = 1;
@@ -639,7 +639,12 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
     const long long want = 2 * items <= slots ? slots / items : (3 * slots + items - 1) / items;
     p.split = std::clamp((int)((len + want - 1) / want + 127) / 128 * 128, kMinSplit, kMaxSplit);
     p.splits = (len + p.split - 1) / p.split;
-    const int groups = (p.splits + kKvFan - 1) / kKvFan;
+    // clusters where blocks are few (one token of 1000: 8.0 us without): where they are many, their
+    // need of free places side by side costs more (33 ragged requests 17 us without, 24 us with)
+    if (items * p.splits <= sms)
+      while (p.cluster < kKvCluster && p.cluster < p.splits) p.cluster *= 2;
+    p.splits = (p.splits + p.cluster - 1) / p.cluster * p.cluster;
+    const int groups = (p.splits / p.cluster + kKvFan - 1) / kKvFan;
     if (groups > 1 && items * (1 + groups) <= kKvTickets) p.tickets = 1 + groups;
   }
   if (p.chunk_tiles) {
@@ -659,13 +664,13 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
 }
 
 // At least plan_of's part_floats, and nondecreasing in the batch's sizes: items * splits
-// is at most 18 sms + 2 items where the items alone set the parts' length, items *
+// is at most 18 sms + 9 items (with whole clusters) where the items alone set the parts' length, items *
 // ceil(len / kMaxSplit) where that does.
 size_t part_floats_bound(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int sms) {
   const long long rows = std::min<long long>(kFewRows, (long long)std::max(1, b->max_new) * (q_heads / c->heads));
   const long long items = std::min<long long>(kKvTickets, (long long)std::max(1, b->batch) * c->heads * ((rows + 7) / 8));
   const long long len = std::max(1, b->max_length);
-  const long long decode = std::max(18ll * sms + 2 * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2);
+  const long long decode = std::max(18ll * sms + (1 + kKvCluster) * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2);
   // chunks: at most sms parts in all
   const long long all = (long long)std::max(1, b->max_new) * (q_heads / c->heads);
   const long long blocks = all > kFewRows ? std::max(1, b->batch) * (long long)c->heads * ((all + kKvChunkRows - 1) / kKvChunkRows) : 0;
@@ -797,6 +802,7 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   a.window = qu->window;
   a.split = p.split;
   a.tickets = p.tickets;
+  a.cluster = p.cluster;
   a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kKvPartAt);
   a.ticket = reinterpret_cast<unsigned*>(static_cast<char*>(workspace) + kKvTicketAt);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

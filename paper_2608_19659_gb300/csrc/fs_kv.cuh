@@ -22,6 +22,7 @@ enum : uint32_t {
 // The workspace: status word, tickets (zero between calls), partial results.
 constexpr int kKvTickets = 8192;
 constexpr int kKvFan = 16;  // results that are joined at a time
+constexpr int kKvCluster = 8;
 constexpr size_t kKvTicketAt = 256;
 constexpr size_t kKvPartAt = kKvTicketAt + 4 * (size_t)kKvTickets;
 
@@ -44,7 +45,8 @@ struct KvAttendArgs {
   int min_rows, max_rows;  // sequences with rows outside (min_rows, max_rows] are another kernel's
   float* part;       // partial results
   unsigned* ticket;
-  int tickets;       // of an item: 1, or 1 and one for every kKvFan parts
+  int cluster;       // blocks of a cluster: consecutive parts of one item
+  int tickets;       // of an item: 1, or 1 and one for every kKvFan clusters
 };
 
 // One sequence of the batch as a kernel may use it: ranges checked, so that no

@@ -3,8 +3,9 @@
 // With at most 16 rows a key head (new tokens x query heads of its group) the call
 // is bound by reading the cache: 2 dim bytes a token and key head. The work is cut into
 // items (sequence, key head, tile of rows) and each item's cache axis into parts, one
-// block each; the last block of an item to finish joins its parts (fixed order: results
-// do not depend on which that is).
+// block each; the blocks of a cluster join their parts through shared memory, and the last
+// blocks to finish join the clusters' results (fixed order: results do not depend on which
+// block is last).
 //
 // A warp of the block takes every fourth tile of 32 tokens. Its lane 0 keeps kStages
 // tiles of keys and values on their way into the warp's own ring (tensor-map copies of
@@ -42,10 +43,33 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   return y;
 }
 
+// All blocks of the cluster that have not left (those without tokens have).
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Shared memory of the cluster's block `rank`, at this block's address a.
+__device__ __forceinline__ float4 ld_cluster16(uint32_t a, int rank) {
+  float4 v;
+  asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %4, %5;\n ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [r];\n}"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(a), "r"(rank)
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 ld_cluster8(uint32_t a, int rank) {
+  float2 v;
+  asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %2, %3;\n ld.shared::cluster.v2.f32 {%0, %1}, [r];\n}"
+               : "=f"(v.x), "=f"(v.y)
+               : "r"(a), "r"(rank)
+               : "memory");
+  return v;
+}
+
 // Shared memory: the warps' rings of (keys, values) tiles; after the last tile the same
 // bytes hold the warps' results.
 template <int D>
 constexpr size_t decode_smem() {
+  static_assert((kWarps + 1) * 16 * D * 4 + 128 <= kWarps * kStages * 2 * kTile * D, "results fit the rings");
   return (size_t)kWarps * kStages * 2 * kTile * D + 1024;
 }
 
@@ -430,8 +454,10 @@ __global__ void __launch_bounds__(kWarps * 32)
 
   const int n_rows = r_end - r0;
   const long long item = ((long long)b * gridDim.y + blockIdx.y);
-  float* part_o = a.part + (item * gridDim.x + part) * kPart;
-  float* part_ml = part_o + kRows * D;
+  // the blocks of a cluster hold consecutive parts of one item; `active` of them have tokens
+  const int rank = part % a.cluster, active = min(a.cluster, n_parts - (part - rank));
+  float* part_o = a.part + (item * gridDim.x + (part - rank)) * kPart;  // the cluster's result
+  float* res = ow + kWarps * kRows * D;                                 // this block's, for its cluster
   auto write_out = [&](int r, int d, float4 x, float lsum) {
     const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
     const int rr = r0 + r;
@@ -456,16 +482,58 @@ __global__ void __launch_bounds__(kWarps * 32)
     }
     if (n_parts == 1) {
       write_out(r, d, x, lsum);
+    } else if (active > 1) {
+      *reinterpret_cast<float4*>(res + r * D + d) = x;
+      if (d == 0) *reinterpret_cast<float2*>(res + kRows * D + 2 * r) = make_float2(top, lsum);
     } else {
       *reinterpret_cast<float4*>(part_o + r * D + d) = x;
-      if (d == 0) *reinterpret_cast<float2*>(part_ml + 2 * r) = make_float2(top, lsum);
+      if (d == 0) *reinterpret_cast<float2*>(part_o + kRows * D + 2 * r) = make_float2(top, lsum);
     }
   }
   if (n_parts == 1) return;
 
-  // ---- join the parts: the last block of every kKvFan, then the last of those
+  // ---- join the cluster's parts, each of its blocks a share of the rows' dimensions
+  if (active > 1) {
+    cluster_sync();
+    const uint32_t res_at = smem_u32(res);
+    for (int u = rank * kWarps * 32 + threadIdx.x; u < n_rows * (D / 4); u += active * kWarps * 32) {
+      const int r = u / (D / 4), d = u % (D / 4) * 4;
+      float2 ml[kKvCluster];
+      float4 y[kKvCluster];
+#pragma unroll
+      for (int i = 0; i < kKvCluster; ++i)
+        if (i < active) {
+          ml[i] = ld_cluster8(res_at + 4 * (kRows * D + 2 * r), i);
+          y[i] = ld_cluster16(res_at + 4 * (r * D + d), i);
+        }
+      float top = -INFINITY, lsum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kKvCluster; ++i)
+        if (i < active) top = fmaxf(top, ml[i].x);
+      const float base = top == -INFINITY ? 0.f : top;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kKvCluster; ++i)
+        if (i < active) {
+          const float f = ex2(ml[i].x - base);
+          lsum = fmaf(ml[i].y, f, lsum);
+          x.x = fmaf(y[i].x, f, x.x), x.y = fmaf(y[i].y, f, x.y), x.z = fmaf(y[i].z, f, x.z), x.w = fmaf(y[i].w, f, x.w);
+        }
+      if (active == n_parts) {
+        write_out(r, d, x, lsum);
+      } else {
+        *reinterpret_cast<float4*>(part_o + r * D + d) = x;
+        if (d == 0) *reinterpret_cast<float2*>(part_o + kRows * D + 2 * r) = make_float2(top, lsum);
+      }
+    }
+    cluster_sync();  // no block leaves while another reads its shared memory
+    if (active == n_parts || rank) return;
+  }
+
+  // ---- join the clusters' results: the last block of every kKvFan, then the last of those
   float* parts = a.part + item * gridDim.x * kPart;
-  int me = part, count = n_parts, step = 1;  // of `count` results, `step` parts apart, mine is the `me`-th
+  // of `count` results, `step` parts apart, mine is the `me`-th
+  int me = part / a.cluster, count = (n_parts + a.cluster - 1) / a.cluster, step = a.cluster;
   unsigned* ticket = a.ticket + item * a.tickets;
   for (bool first = a.tickets > 1;; first = false) {
     const int g = first ? me / kKvFan : 0, g0 = first ? g * kKvFan : 0, g_n = first ? min(kKvFan, count - g0) : count;
@@ -542,7 +610,7 @@ __global__ void __launch_bounds__(kWarps * 32)
       }
     }
     if (done) return;
-    me = g, count = (count + kKvFan - 1) / kKvFan, step = kKvFan;
+    me = g, count = (count + kKvFan - 1) / kKvFan, step *= kKvFan;
   }
 }
 
@@ -551,8 +619,20 @@ cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendA
                    cudaStream_t s) {
   static const cudaError_t limit = raise_smem_limit(reinterpret_cast<const void*>(k_kv_decode<D, NT, T>), decode_smem<D>());
   if (limit != cudaSuccess) return limit;
-  return launch_pdl(k_kv_decode<D, NT, T>, dim3(splits, a.v.heads * row_blocks, a.v.batch), dim3(kWarps * 32), decode_smem<D>(), s,
-                    mk, mv, a);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((splits + a.cluster - 1) / a.cluster * a.cluster, a.v.heads * row_blocks, a.v.batch);
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = decode_smem<D>();
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {(unsigned)a.cluster, 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = a.cluster > 1 ? 2 : 1;
+  note_launch();
+  return cudaLaunchKernelEx(&cfg, k_kv_decode<D, NT, T>, mk, mv, a);
 }
 
 template <int D, typename T>
