@@ -74,7 +74,7 @@ constexpr size_t decode_smem() {
 }
 
 template <int D, int NT, typename T>
-__global__ void __launch_bounds__(kWarps * 32)
+__global__ void __launch_bounds__(kWarps * 32, D == 128 && NT == 1 ? 3 : 1)
     k_kv_decode(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const KvAttendArgs a) {
   constexpr int kRows = 8 * NT;
   constexpr int kSteps = D / 16;   // products along the dimensions of a key
