@@ -606,13 +606,26 @@ struct KvPlan {
   int row_tile, row_blocks, split, splits, cluster, tickets;
   int chunk_tiles;  // blocks of k_kv_chunk a (sequence, key head); 0: no sequence has that many rows
   int chunk_split, chunk_parts;
+  int wide_tiles;   // tiles of a sequence that k_kv_expand writes; 0: the walks convert for themselves
   int decode;       // whether some sequence can have few rows
-  size_t part_floats, chunk_floats;
+  size_t part_floats, chunk_floats, wide_bytes;
 };
 
 // Sequences with more rows (new tokens x query heads of a key head) than this go to
 // k_kv_chunk.
 constexpr int kFewRows = 64;
+
+// Where at least kWideFrom blocks can walk over a sequence's tokens, and the batch's tokens as
+// halves take no more than kWideBytes, they are converted once.
+constexpr int kWideFrom = 4;
+constexpr long long kWideBytes = 1ll << 30;
+void wide_of(const fs_kv_cache* c, const fs_kv_batch* b, int tiles, int* wide_tiles, size_t* bytes) {
+  const long long per = (std::max(1, b->max_length) + 127) / 128;
+  const long long all = per * b->batch * c->heads * (2ll * 128 * c->dim * 2);
+  const bool wide = tiles >= kWideFrom && all <= kWideBytes;
+  *wide_tiles = wide ? (int)per : 0;
+  *bytes = wide ? (size_t)all : 0;
+}
 
 constexpr int kMinSplit = 128, kMaxSplit = 4096;
 
@@ -657,6 +670,8 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
     const int tiles = (int)((walk + want - 1) / want);
     p.chunk_split = tiles * 128;
     p.chunk_parts = (walk + tiles - 1) / tiles;
+    wide_of(c, b, p.chunk_tiles, &p.wide_tiles, &p.wide_bytes);
+    if (p.chunk_parts > 1) p.wide_tiles = 0, p.wide_bytes = 0;
     p.chunk_floats = p.chunk_parts > 1 ? (size_t)blocks * p.chunk_parts * kKvChunkRows * (c->dim + 4) : 0;
   }
   p.part_floats = p.decode && p.splits > 1 ? (size_t)items * p.splits * p.row_tile * (c->dim + 2) : 0;
@@ -674,7 +689,10 @@ size_t part_floats_bound(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads
   // chunks: at most sms parts in all
   const long long all = (long long)std::max(1, b->max_new) * (q_heads / c->heads);
   const long long blocks = all > kFewRows ? std::max(1, b->batch) * (long long)c->heads * ((all + kKvChunkRows - 1) / kKvChunkRows) : 0;
-  return (size_t)(decode + std::min((long long)sms, kKvFan * blocks) * kKvChunkRows * (c->dim + 4));
+  // the tokens as halves: a smaller batch may have them where a larger one's are too many
+  const long long tokens = ((len + 127) / 128) * std::max(1, b->batch) * c->heads * (2ll * 128 * c->dim * 2);
+  return (size_t)(decode + std::min((long long)sms, kKvFan * blocks) * kKvChunkRows * (c->dim + 4) +
+                  (blocks ? std::min(tokens, kWideBytes) / 4 + 32 : 0));
 }
 
 int device_sms(int* sms) {
@@ -791,7 +809,7 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   int sms = 0;
   if (int rc = device_sms(&sms)) return rc;
   const KvPlan p = plan_of(cache, batch, qu->q_heads, qu->window, sms);
-  if (int rc = check_workspace(workspace, workspace_bytes, (int64_t)(kKvPartAt + 4 * (p.part_floats + p.chunk_floats)))) return rc;
+  if (int rc = check_workspace(workspace, workspace_bytes, (int64_t)(kKvPartAt + 4 * (p.part_floats + p.chunk_floats) + (p.wide_bytes ? p.wide_bytes + 128 : 0)))) return rc;
   if (p.chunk_tiles > 65535) return say(FS_EINVAL, "max_new = %d: too many rows for one call", batch->max_new);
 
   KvAttendArgs a{};
@@ -812,9 +830,12 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
     ca.min_rows = kFewRows, ca.max_rows = INT_MAX;
     ca.split = p.chunk_split;
     ca.part = a.part + p.part_floats;
+    ca.wide_tiles = p.wide_tiles;
+    if (p.wide_tiles)
+      ca.wide = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(ca.part + p.chunk_floats) + 127) & ~(uintptr_t)127);
     if (int rc = kv_tensor_map(&mk, *cache, cache->k, cache->page_tokens, false)) return rc;
     if (int rc = kv_tensor_map(&mv, *cache, cache->v, cache->page_tokens, false)) return rc;
-    const cudaError_t e = launch_kv_chunk(mk, mv, ca, cache->dim, qu->dtype, p.chunk_tiles, p.chunk_parts, st);
+    const cudaError_t e = launch_kv_chunk(mk, mv, ca, *cache, qu->dtype, p.chunk_tiles, p.chunk_parts, st);
     if (e != cudaSuccess) return cuda_say(e, "launch (fs_kv_attend, chunks)");
   }
   if (p.decode) {

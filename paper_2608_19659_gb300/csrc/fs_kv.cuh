@@ -44,6 +44,8 @@ struct KvAttendArgs {
   int split;         // tokens per part of the cache axis
   int min_rows, max_rows;  // sequences with rows outside (min_rows, max_rows] are another kernel's
   float* part;       // partial results
+  char* wide;        // k_kv_chunk: the walked tokens as halves (k_kv_expand), or null
+  int wide_tiles;    // tiles of 128 tokens there, of a sequence
   unsigned* ticket;
   int cluster;       // blocks of a cluster: consecutive parts of one item
   int tickets;       // of an item: 1, or 1 and one for every kKvFan clusters
@@ -159,7 +161,7 @@ int kv_tensor_map(CUtensorMap* m, const fs_kv_cache& c, const void* base, int ro
 cudaError_t launch_kv_decode(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int dim, int dtype,
                              int row_tile, int row_blocks, int splits, cudaStream_t s);
 constexpr int kKvChunkRows = 256;  // rows of a block
-cudaError_t launch_kv_chunk(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int dim, int dtype,
-                            int tiles, int parts, cudaStream_t s);
+cudaError_t launch_kv_chunk(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, const fs_kv_cache& c,
+                            int dtype, int tiles, int parts, cudaStream_t s);
 
 }  // namespace fs

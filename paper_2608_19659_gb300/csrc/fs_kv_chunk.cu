@@ -27,13 +27,15 @@
 namespace fs {
 namespace {
 
-constexpr int kThreads = 16 * 32, kTok = 128, kTileRows = 128;
-constexpr float kUp = 7.f;  // halves hold 2^(kUp + 8) of a row's largest weight, and 2^kUp of a code
+constexpr int kTok = 128, kTileRows = 128;
+constexpr float kUp = 7.f;  // halves hold 2^(kUp + 8) of a row's largest weight
 
-template <int D>
+template <int D, bool kWide>
 struct Cfg {
+  static constexpr int kThreads = kWide ? 12 * 32 : 16 * 32;
+  static constexpr int kIssuer = kWide ? 8 : 12;          // the warp that issues the products, and the next one that copies
   static constexpr int kStages = D == 128 ? 4 : 8;        // tiles of halves
-  static constexpr int kRaw = D == 128 ? 2 : 4;           // tiles of codes
+  static constexpr int kRaw = kWide ? 0 : D == 128 ? 2 : 4;  // tiles of codes
   static constexpr int kSlot = kTok * D * 2, kRawSlot = kTok * D;
   static constexpr int kQ = 2 * kTileRows * D * 2;
   static constexpr size_t kSmem = 1024 + kQ + (size_t)kStages * kSlot + kRaw * kRawSlot + 1280;
@@ -44,10 +46,10 @@ constexpr int kUsed = 8;
 
 struct Bars {
   uint64_t full[8], used[kUsed], raw_full[4], raw_empty[4], s_full[2], p_full[2][2], pv_done[2], end;
-  float2 scale[4][8];    // per tile of codes and 16 tokens: what keys are multiplied by (two halves), the values' scale
+  float vs[4][8];        // per tile of codes and 16 tokens: the values' scale
   uint32_t cut[4];       // per tile of codes: some tokens' values are to be 0
-  float2 v_scale[8][8];  // per tile (mod 8) and 16 tokens: log2 of the values' scale, and its reciprocal
-  float k_ref, v_ref;
+  float2 scale[8][8];    // per tile (mod 8) and 16 tokens: the keys' scale, log2 of the values' over the largest
+  float v_ref;
   uint32_t tmem;
 };
 static_assert(sizeof(Bars) <= 1280, "the barriers' share of shared memory");
@@ -148,6 +150,13 @@ __device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t (&r)[16]) {
       : "memory");
 }
 
+// Global -> shared copy of a contiguous tile.
+__device__ __forceinline__ void bulk_g2s_at(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+
 // A wait that says so when it runs out; the caller leaves its loop.
 __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, const KvView& v) {
   if (mbar_wait(bar, parity, kWaitLimitNs)) return true;
@@ -158,7 +167,7 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, const K
 // A row of S: its largest log2 weight (times its value scale) among columns [lo, hi] (all of
 // them with kWhole); masked columns become -infinity.
 template <bool kWhole>
-__device__ __forceinline__ float row_top(float (&x)[kTok], float c, const float2* v_scale, int lo, int hi) {
+__device__ __forceinline__ float row_top(float (&x)[kTok], float c, const float2* scale, int lo, int hi) {
   float top = -INFINITY;
 #pragma unroll
   for (int g = 0; g < kTok / 16; ++g) {
@@ -170,7 +179,7 @@ __device__ __forceinline__ float row_top(float (&x)[kTok], float c, const float2
     const float* y = x + 16 * g;
     const float m0 = max3(max3(max3(y[0], y[1], y[2]), max3(y[3], y[4], y[5]), max3(y[6], y[7], y[8])),
                           max3(y[9], y[10], y[11]), max3(max3(y[12], y[13], y[14]), y[15], y[15]));
-    if (kWhole || m0 > -INFINITY) top = fmaxf(top, fmaf(m0, c, v_scale[g].x));
+    if (kWhole || m0 > -INFINITY) top = fmaxf(top, fmaf(m0, c * scale[g].x, scale[g].y));
   }
   return top;
 }
@@ -190,10 +199,10 @@ __device__ __forceinline__ Walk walk_of(const KvAttendArgs& a, const KvSeq& s, i
   return w;
 }
 
-template <int D, typename T>
-__global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant__ CUtensorMap mk,
+template <int D, typename T, bool kWide>
+__global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const __grid_constant__ CUtensorMap mk,
                                                              const __grid_constant__ CUtensorMap mv, const KvAttendArgs a) {
-  using C = Cfg<D>;
+  using C = Cfg<D, kWide>;
   constexpr int kPart = 2 * kTileRows * (D + 4);  // floats of a part's result: per row its sums, m, l (and two to keep 16 bytes)
   extern __shared__ unsigned char raw[];
   const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
@@ -230,35 +239,32 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
   const int n = (kv_hi - begin + kTok - 1) / kTok;  // tiles of the cache; 0: no row sees a token
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < C::kStages; ++i) mbar_init(&bars.full[i], 128);
+    for (int i = 0; i < C::kStages; ++i) mbar_init(&bars.full[i], kWide ? 1 : 128);
     for (int i = 0; i < kUsed; ++i) mbar_init(&bars.used[i], 1);
     for (int i = 0; i < C::kRaw; ++i) mbar_init(&bars.raw_full[i], 1), mbar_init(&bars.raw_empty[i], 128);
     for (int t = 0; t < 2; ++t) mbar_init(&bars.s_full[t], 1), mbar_init(&bars.p_full[t][0], 128), mbar_init(&bars.p_full[t][1], 128), mbar_init(&bars.pv_done[t], 1);
     mbar_init(&bars.end, 1);
-    bars.k_ref = bars.v_ref = 0.f;
+    bars.v_ref = 0.f;
   }
-  if (w == 12) {
+  if (w == C::kIssuer) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars.tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
   __syncthreads();
 
-  // the largest scales of the pages that are walked
+  // the largest scale of values of the pages that are walked
   {
-    float km = 0.f, vm = 0.f;
+    float vm = 0.f;
     const int g0 = begin >> v.log_page, g1 = (kv_hi + (1 << v.log_page) - 1) >> v.log_page;
-    for (int g = g0 + threadIdx.x; g < g1; g += kThreads) {
+    for (int g = g0 + threadIdx.x; g < g1; g += C::kThreads) {
       const long long at = (long long)kv_page(v, b, g) * v.heads + h;
       const float ks = v.k_scale[at], vs = v.v_scale[at];
       kv_scales(v, ks, vs);
-      km = fmaxf(km, ks), vm = fmaxf(vm, vs);
+      vm = fmaxf(vm, vs);
     }
 #pragma unroll
-    for (int d = 16; d; d >>= 1) km = fmaxf(km, __shfl_xor_sync(~0u, km, d)), vm = fmaxf(vm, __shfl_xor_sync(~0u, vm, d));
-    if (lane == 0) {  // (nonnegative floats order as their bits do)
-      atomicMax(reinterpret_cast<int*>(&bars.k_ref), __float_as_int(km));
-      atomicMax(reinterpret_cast<int*>(&bars.v_ref), __float_as_int(vm));
-    }
+    for (int d = 16; d; d >>= 1) vm = fmaxf(vm, __shfl_xor_sync(~0u, vm, d));
+    if (lane == 0) atomicMax(reinterpret_cast<int*>(&bars.v_ref), __float_as_int(vm));  // (nonnegative floats order as their bits do)
   }
   // queries: a row a thread, scaled into [-2, 2] by a power of two (and by the scale's sign)
   int q_exp = 0;
@@ -300,7 +306,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
   // (the whole of tensor memory is this block's: its columns begin at 0)
   constexpr uint32_t tmem = 0;
 
-  // Registers: 512 threads x 128 at launch; 128 x (192 + 192 + 80 + 48) from here on.
+  // Registers at launch: 512 threads x 128 (384 x 168); from here on 128 x (192 + 192 + 80 + 48)
+  // (128 x (192 + 192 + 120)).
   if (w < 8) {
     // ---------------------------------------------------------------- softmax
     asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
@@ -309,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
     if (t < n_sub) {
       const uint32_t lanes = (uint32_t)(w & 3) << 21;  // 32 lanes a warp, in bits 16 and up
       const uint32_t s_at = tmem + lanes + t * 128, o_at = tmem + lanes + 256 + t * 128;
-      const float c = fabsf(a.scale_log2) * exp2_int(q_exp) * (bars.k_ref * (1.f / 128.f));
+      const float c = fabsf(a.scale_log2) * exp2_int(q_exp);
       const int pos = base + r / v.group;
       const int hi = r < r_end ? pos : -1, lo = a.window ? pos - a.window + 1 : 0;
       // tiles inside [all_lo, all_hi) are seen whole by every row of this tile
@@ -329,8 +336,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
 #pragma unroll
         for (int k = 0; k < 4; ++k) tmem_ld32(reinterpret_cast<uint32_t(&)[32]>(x[32 * k]), s_at + 32 * k);
         wait_ld();
-        const float2* v_scale = bars.v_scale[j & 7];
-        const float top = whole ? row_top<true>(x, c, v_scale, 0, 0) : row_top<false>(x, c, v_scale, c_lo, c_hi);
+        const float2* scale = bars.scale[j & 7];
+        const float top = whole ? row_top<true>(x, c, scale, 0, 0) : row_top<false>(x, c, scale, c_lo, c_hi);
         const bool grow = top > m + 8.f || (m == -INFINITY && top > m);
         if (__any_sync(~0u, grow)) {
           const float f = grow ? ex2(m - top) : 1.f;
@@ -350,24 +357,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
         }
         const float off = m == -INFINITY ? 0.f : m;  // (m: log2 of weight times scale, without kUp)
         // P = 2^(c S + log2 of the value scale - m), and the row's sum of weights without the scales
-        // (a masked column: c * -infinity, but c may be 0)
-        const float cc = whole ? c : fmaxf(c, 0x1p-126f);
+        // (a masked column: c times -infinity, but c may be 0)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           uint32_t p[16];
 #pragma unroll
           for (int g = 2 * k; g < 2 * k + 2; ++g) {
-            const float2 vs = v_scale[g];
-            const float off_g = vs.x + kUp - off;
+            const float ve = scale[g].y, off_g = ve + kUp - off;
+            const float cg = whole ? c * scale[g].x : fmaxf(c * scale[g].x, 0x1p-126f);
             float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
             for (int i = 16 * g; i < 16 * g + 16; i += 2) {
-              float2 y = fma2(make_float2(x[i], x[i + 1]), make_float2(cc, cc), make_float2(off_g, off_g));
+              float2 y = fma2(make_float2(x[i], x[i + 1]), make_float2(cg, cg), make_float2(off_g, off_g));
               y.x = ex2(y.x), y.y = ex2(y.y);
               sum = add2(sum, y);
               p[(i - 32 * k) / 2] = pack_f16(y.x, y.y);
             }
-            l = fmaf(sum.x + sum.y, vs.y * (1.f / 128.f), l);
+            l = fmaf(sum.x + sum.y, exp2_int(-(int)ve - 7), l);
           }
           tmem_st16(s_at + 16 * k, p);
           if (k & 1) {  // half of P: its product begins while the other half is computed
@@ -421,14 +427,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
         if (r < r_end) *reinterpret_cast<float2*>(to + D) = make_float2(m, l);
       }
     }
-  } else if (w < 12) {
+  } else if (!kWide && w < 12) {
     // ---------------------------------------------------------------- codes to halves
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     constexpr int kLanes = D / 16;               // lanes a token, 16 codes each
     constexpr int kPer = 128 / kLanes;           // tokens a pass
     constexpr int kPasses = kTok / kPer;         // 8 (dim 128) or 4 (dim 64)
+    constexpr int kRaw = C::kRaw > 0 ? C::kRaw : 1;
     const int id = threadIdx.x - 256, cl = id % kLanes, tk = id / kLanes;
-    const int v_exp = __float_as_int(bars.v_ref) >> 23;
     // A lane's 16 codes become the 16-byte chunks 2 (cl mod 4) and + 1 of the token's row in block
     // cl / 4; lanes of the second block begin with the other one, so that a row's lanes meet every
     // bank once.
@@ -436,9 +442,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
     const uint32_t from = raw_at + tk * D + cl * 16, to = (cl >> 2) * (kTok * 128) + tk * 128;
     const uint32_t c0 = (((cl & 3) * 2 + sw) ^ (tk & 7)) << 4, c1 = (((cl & 3) * 2 + (sw ^ 1)) ^ (tk & 7)) << 4;
     for (int i = 0; i < 2 * n; ++i) {
-      const int st = i % C::kStages, rs = i % C::kRaw;
-      if (!wait_bar(&bars.raw_full[rs], (i / C::kRaw) & 1, v)) break;
-      uint32_t x[kPasses][4], f2[kPasses];
+      const int st = i % C::kStages, rs = i % kRaw;
+      if (!wait_bar(&bars.raw_full[rs], (i / kRaw) & 1, v)) break;
+      uint32_t x[kPasses][4];
       const bool values = i & 1;
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
@@ -446,38 +452,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
         const float2 u = ld_shared8(at + 8 * sw), z = ld_shared8(at + 8 * (sw ^ 1));
         x[p][0] = __float_as_uint(u.x), x[p][1] = __float_as_uint(u.y);
         x[p][2] = __float_as_uint(z.x), x[p][3] = __float_as_uint(z.y);
-        if (!values) f2[p] = __float_as_uint(bars.scale[rs][(p * kPer + tk) >> 4].x);
       }
-      if (values) {
+      if (values && bars.cut[rs]) {
         // tokens that no row sees (their slots may hold NaN codes), and values whose scale is 0
-        if (bars.cut[rs]) {
 #pragma unroll
-          for (int p = 0; p < kPasses; ++p) {
-            const int tl = p * kPer + tk;
-            if (begin + (i >> 1) * kTok + tl >= kv_hi || bars.scale[rs][tl >> 4].y == 0.f) x[p][0] = x[p][1] = x[p][2] = x[p][3] = 0;
-          }
+        for (int p = 0; p < kPasses; ++p) {
+          const int tl = p * kPer + tk;
+          if (begin + (i >> 1) * kTok + tl >= kv_hi || bars.vs[rs][tl >> 4] == 0.f) x[p][0] = x[p][1] = x[p][2] = x[p][3] = 0;
         }
-      } else if (id < 8) {
-        // log2 of the scales of values over each 16 tokens of the tile, relative to the largest; a
-        // scale of 0 counts as one too small to matter
-        const float vs = bars.scale[rs][id].y;
-        const int e = vs != 0.f ? max((__float_as_int(vs) >> 23) - v_exp, -100) : -100;
-        bars.v_scale[(i >> 1) & 7][id] = make_float2((float)e, exp2_int(-e));
       }
       mbar_arrive(&bars.raw_empty[rs]);
-      // the slot's last tile, kStages / 2 of the cache's tiles ago: keys' products go with the tile before
-      const int use = (i >> 1) - C::kStages / 2 - (values ? 0 : 1);
-      if (use >= 0 && !wait_bar(&bars.used[use % kUsed], (use / kUsed) & 1, v)) break;
+      // the slot's last tile, kStages / 2 of the cache's tiles ago (used[j] follows the products over the
+      // keys of tile j and the values of the one before)
+      const int use = (i >> 1) - C::kStages / 2 + (values ? 1 : 0);
+      if ((i >> 1) >= C::kStages / 2 && !wait_bar(&bars.used[use % kUsed], (use / kUsed) & 1, v)) break;
       const uint32_t row = ring_at + st * C::kSlot + to;
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
         uint32_t y[8];
 #pragma unroll
         for (int k = 0; k < 4; ++k) y[2 * k] = e4m3x2_to_f16x2(x[p][k]), y[2 * k + 1] = e4m3x2_to_f16x2_hi(x[p][k]);
-        if (!values) {  // (the values' scale is in P)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(y[k]) : "r"(f2[p]));
-        }
         st_shared16(row + p * (kPer * 128) + c0, make_uint4(y[0], y[1], y[2], y[3]));
         st_shared16(row + p * (kPer * 128) + c1, make_uint4(y[4], y[5], y[6], y[7]));
       }
@@ -485,13 +479,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
       mbar_arrive(&bars.full[st]);
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    if (w == 13) {
-    // ---------------------------------------------------------------- codes from the cache
+    if (kWide)
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
+    else
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (w == C::kIssuer + 1) {
+    // ---------------------------------------------------------------- tiles from the cache
     // Lane g holds the page of a tile's g-th box of a page's tokens. Page ids are asked for two tiles
     // ahead and their scales one, so that no copy waits for either.
+    constexpr int kRaw = C::kRaw > 0 ? C::kRaw : 1;
     const int log_p = v.log_page, boxes = kTok >> log_p;
-    const float inv_k = bars.k_ref > 0.f ? 128.f / bars.k_ref : 0.f;
+    const int v_exp = __float_as_int(bars.v_ref) >> 23;
     int page0 = 0, page1 = 0, page2 = 0;
     bool held0 = false, held1 = false, held2 = false;
     float ks0 = 0.f, vs0 = 0.f, ks1 = 0.f, vs1 = 0.f;
@@ -508,34 +506,64 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
         ks1 = v.k_scale[at], vs1 = v.v_scale[at];
       }
     };
+    const char* wide = kWide ? a.wide + ((long long)(b * v.heads + h) * a.wide_tiles + begin / kTok) * (2 * C::kSlot) : nullptr;
     ask_pages(0);
     ask_scales();
     ask_pages(1);
     int i = 0;
     for (; i < 2 * n; ++i) {
-      const int rs = i % C::kRaw;
-      if (!(i & 1)) {
+      const int j = i >> 1;
+      const bool values = i & 1;
+      if (!values) {
         held0 = held1, page0 = page1, ks0 = ks1, vs0 = vs1;
         ask_scales();
-        ask_pages((i >> 1) + 2);
+        ask_pages(j + 2);
       }
-      bool ok = wait_bar(&bars.raw_empty[rs], ((i / C::kRaw) & 1) ^ 1, v);
+      bool ok = true;
+      if constexpr (kWide) {
+        const int use = j - C::kStages / 2 + (values ? 1 : 0);  // (as for the converters)
+        if (j >= C::kStages / 2) ok = wait_bar(&bars.used[use % kUsed], (use / kUsed) & 1, v);
+      } else {
+        ok = wait_bar(&bars.raw_empty[i % kRaw], ((i / kRaw) & 1) ^ 1, v);
+      }
       if (!__all_sync(~0u, ok)) break;
-      const uint32_t held = __ballot_sync(~0u, held0);
-      const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p), ks = __shfl_sync(~0u, ks0, (lane << 4) >> log_p);
-      if (lane < 8) bars.scale[rs][lane] = make_float2(__uint_as_float(pack_f16(ks * inv_k, ks * inv_k)), vs);
-      // (a group beyond kv_hi has the scale 0 too)
-      const bool cut = __any_sync(~0u, lane < 8 && vs == 0.f) || begin + ((i >> 1) + 1) * kTok > kv_hi;
-      if (lane == 0) bars.cut[rs] = cut;
-      __syncwarp();
-      if (lane == 0) mbar_expect_tx(&bars.raw_full[rs], (uint32_t)(__popc(held) * D) << log_p);
-      __syncwarp();
-      if (held0)
-        tma_tile(raw_at + rs * C::kRawSlot + ((lane * D) << log_p), (i & 1) ? &mv : &mk, 0, h, page0, &bars.raw_full[rs]);
+      if (!values) {
+        // (this far ahead of softmax the entry of eight tiles ago has been read) a scale of 0 counts as
+        // one too small to matter
+        const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p), ks = __shfl_sync(~0u, ks0, (lane << 4) >> log_p);
+        const int e = vs != 0.f ? max((__float_as_int(vs) >> 23) - v_exp, -100) : -100;
+        if (lane < 8) bars.scale[j & 7][lane] = make_float2(ks, (float)e);
+      }
+      if constexpr (kWide) {
+        const int st = i % C::kStages;
+        __syncwarp();
+        if (lane == 0) {
+          mbar_expect_tx(&bars.full[st], C::kSlot);
+          bulk_g2s_at(ring_at + st * C::kSlot, wide + (long long)i * C::kSlot, C::kSlot, &bars.full[st]);
+        }
+      } else {
+        const int rs = i % kRaw;
+        const uint32_t held = __ballot_sync(~0u, held0);
+        if (values) {
+          const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p);
+          if (lane < 8) bars.vs[rs][lane] = vs;
+          // (a group beyond kv_hi has the scale 0 too)
+          const bool cut = __any_sync(~0u, lane < 8 && vs == 0.f) || begin + (j + 1) * kTok > kv_hi;
+          if (lane == 0) bars.cut[rs] = cut;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_expect_tx(&bars.raw_full[rs], (uint32_t)(__popc(held) * D) << log_p);
+        __syncwarp();
+        if (held0)
+          tma_tile(raw_at + rs * C::kRawSlot + ((lane * D) << log_p), values ? &mv : &mk, 0, h, page0, &bars.raw_full[rs]);
+      }
     }
-    if (i < 2 * n)  // a wait ran out: the copies under way first (with the same limit)
-      for (int k = max(0, i - C::kRaw); k < i; ++k) mbar_wait(&bars.raw_full[k % C::kRaw], (k / C::kRaw) & 1, kWaitLimitNs);
-    } else if (w == 12 && n > 0) {
+    if (i < 2 * n) {  // a wait ran out: the copies under way first (with the same limit)
+      constexpr int kAhead = kWide ? C::kStages : kRaw;
+      uint64_t* bar = kWide ? bars.full : bars.raw_full;
+      for (int k = max(0, i - kAhead); k < i; ++k) mbar_wait(&bar[k % kAhead], (k / kAhead) & 1, kWaitLimitNs);
+    }
+    } else if (w == C::kIssuer && n > 0) {
     // ---------------------------------------------------------------- products
     // The whole warp walks, with values and conditions that are the same in every lane, so that
     // addresses and descriptors stay in uniform registers: beside eight busy softmax warps every
@@ -567,6 +595,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
         qk(t, 0);
         commit(&bars.s_full[t]);
       }
+      commit(&bars.used[0]);
     }
     int vs = 1, ks = 2;
     uint32_t v_par = 0, k_par = 0;  // parities of the slots' rounds
@@ -590,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
           }
         }
       }
-      if (one) commit(&bars.used[j % kUsed]);  // tile j's values and the keys of the next
+      if (one) commit(&bars.used[(j + 1) % kUsed]);  // tile j's values and the keys of the next
       vs += 2;
       if (vs >= C::kStages) vs -= C::kStages, v_par ^= 1;
       ks += 2;
@@ -605,7 +634,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_chunk(const __grid_constant_
   fence_before();
   __syncthreads();
   fence_after();
-  if (w == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  if (w == C::kIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
 // The parts of a walk, joined: a group of D / 4 lanes a row, every part's load under way at once.
@@ -653,22 +682,83 @@ __global__ void __launch_bounds__(256) k_kv_chunk_join(const KvAttendArgs a, int
   *reinterpret_cast<uint2*>(to) = make_uint2(Elem<T>::pack(x.x * inv, x.y * inv), Elem<T>::pack(x.z * inv, x.w * inv));
 }
 
-template <int D, typename T>
+// The codes of whole sequences as halves, in the order and swizzle that the products read
+// them in: [sequence][head][tile of 128 tokens][keys, values][block of 64 dimensions][token][64].
+// Where many blocks walk over the same tokens, each tile is then converted once instead of by every
+// one of them (8192 tokens' prompt XXX us with conversion in every walk). Tokens beyond a sequence's
+// and values whose scale is 0 become 0.
+template <int D>
+__global__ void __launch_bounds__(256) k_kv_expand(const KvAttendArgs a, const uint8_t* kc, const uint8_t* vc,
+                                                   long long page_stride, long long head_stride, long long token_stride) {
+  constexpr int kLanes = D / 16, kPer = 256 / kLanes, kPasses = kTok / kPer, kSlot = kTok * D * 2;
+  pdl_trigger();
+  pdl_wait();
+  const KvView& v = a.v;
+  const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x;
+  KvSeq s;
+  if (!kv_seq(v, b, s)) return;  // (the walks' kernel reports it)
+  const int rows = s.count * v.group, t0 = tile * kTok;
+  const int lo = a.window ? s.len - s.count - a.window + 1 : 0;  // the first token that a row sees
+  if (rows <= a.min_rows || rows > a.max_rows || t0 >= s.len || t0 + kTok <= lo || tile >= a.wide_tiles) return;
+  const int cl = threadIdx.x % kLanes, tk = threadIdx.x / kLanes;
+  uint4 x[2][kPasses];
+#pragma unroll
+  for (int p = 0; p < kPasses; ++p) {
+    const int t = t0 + p * kPer + tk;
+    x[0][p] = x[1][p] = make_uint4(0, 0, 0, 0);
+    if (t < s.len) {
+      const int g = kv_page(v, b, t >> v.log_page);
+      const long long at = g * page_stride + h * head_stride + (t & ((1 << v.log_page) - 1)) * token_stride + cl * 16;
+      x[0][p] = __ldg(reinterpret_cast<const uint4*>(kc + at));
+      if (v.v_scale[(long long)g * v.heads + h] != 0.f) x[1][p] = __ldg(reinterpret_cast<const uint4*>(vc + at));
+    }
+  }
+  char* out = a.wide + ((long long)(b * v.heads + h) * a.wide_tiles + tile) * (2 * kSlot);
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      const int tl = p * kPer + tk;
+      const uint32_t ws[4] = {x[k][p].x, x[k][p].y, x[k][p].z, x[k][p].w};
+      uint32_t y[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[2 * i] = e4m3x2_to_f16x2(ws[i]), y[2 * i + 1] = e4m3x2_to_f16x2_hi(ws[i]);
+      char* row = out + k * kSlot + (cl >> 2) * (kTok * 128) + tl * 128;
+      *reinterpret_cast<uint4*>(row + ((((cl & 3) * 2) ^ (tl & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+      *reinterpret_cast<uint4*>(row + ((((cl & 3) * 2 + 1) ^ (tl & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+    }
+}
+
+template <int D, typename T, bool kWide>
 cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int tiles, int parts, cudaStream_t s) {
-  static const cudaError_t limit = raise_smem_limit(reinterpret_cast<const void*>(k_kv_chunk<D, T>), Cfg<D>::kSmem);
+  using C = Cfg<D, kWide>;
+  static const cudaError_t limit = raise_smem_limit(reinterpret_cast<const void*>(k_kv_chunk<D, T, kWide>), C::kSmem);
   if (limit != cudaSuccess) return limit;
-  const cudaError_t e = launch_pdl(k_kv_chunk<D, T>, dim3(a.v.heads * a.v.batch, tiles, parts), dim3(kThreads), Cfg<D>::kSmem, s, mk, mv, a);
+  return launch_pdl(k_kv_chunk<D, T, kWide>, dim3(a.v.heads * a.v.batch, tiles, parts), dim3(C::kThreads), C::kSmem, s, mk, mv, a);
+}
+
+template <int D, typename T>
+cudaError_t launch_all(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, const fs_kv_cache& c, int tiles,
+                       int parts, cudaStream_t s) {
+  if (a.wide) {
+    const cudaError_t e = launch_pdl(k_kv_expand<D>, dim3(a.wide_tiles, a.v.heads, a.v.batch), dim3(256), 0, s, a,
+                                     static_cast<const uint8_t*>(c.k), static_cast<const uint8_t*>(c.v), (long long)c.page_stride,
+                                     (long long)c.head_stride, (long long)c.token_stride);
+    return e != cudaSuccess ? e : launch<D, T, true>(mk, mv, a, tiles, parts, s);
+  }
+  const cudaError_t e = launch<D, T, false>(mk, mv, a, tiles, parts, s);
   if (e != cudaSuccess || parts == 1) return e;
   return launch_pdl(k_kv_chunk_join<D, T>, dim3(a.v.heads * a.v.batch, tiles, 2 * kTileRows * (D / 4) / 256), dim3(256), 0, s, a, parts);
 }
 
 }  // namespace
 
-cudaError_t launch_kv_chunk(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int dim, int dtype,
-                            int tiles, int parts, cudaStream_t s) {
+cudaError_t launch_kv_chunk(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, const fs_kv_cache& c,
+                            int dtype, int tiles, int parts, cudaStream_t s) {
   const bool h = dtype == FS_KV_FP16;
-  if (dim == 128) return h ? launch<128, __half>(mk, mv, a, tiles, parts, s) : launch<128, __nv_bfloat16>(mk, mv, a, tiles, parts, s);
-  return h ? launch<64, __half>(mk, mv, a, tiles, parts, s) : launch<64, __nv_bfloat16>(mk, mv, a, tiles, parts, s);
+  if (c.dim == 128)
+    return h ? launch_all<128, __half>(mk, mv, a, c, tiles, parts, s) : launch_all<128, __nv_bfloat16>(mk, mv, a, c, tiles, parts, s);
+  return h ? launch_all<64, __half>(mk, mv, a, c, tiles, parts, s) : launch_all<64, __nv_bfloat16>(mk, mv, a, c, tiles, parts, s);
 }
 
 }  // namespace fs
