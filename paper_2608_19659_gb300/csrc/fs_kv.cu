@@ -446,6 +446,63 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) k_kv_append_many(con
   if ((int)blockIdx.y >= 2 * H) {
     const int h0 = (blockIdx.y - 2 * H) * kQHeads, h_n = min(kQHeads, a.q_heads - h0);
     const uint32_t mask = (kLanes == 16 ? 0xffffu : 0xffu) << (threadIdx.x % 32 / kLanes * kLanes);
+    const int half = a.rot >> 1;
+    if (a.interleaved || !(half & 7)) {
+      // 16 bytes a lane: dimensions 8 l on; what they are paired with is in the lane itself, or in the one
+      // that holds the dimensions half the rotated ones away
+      const int d0 = 8 * l;
+      const bool turns = d0 < a.rot, first = d0 < half;
+      const int other = !turns || a.interleaved ? l : first ? l + (half >> 3) : l - (half >> 3);
+      const int src = (threadIdx.x % 32 / kLanes) * kLanes + other;
+      for (int p = lo + unit; p < hi; p += kUnits) {
+        const T* from = static_cast<const T*>(a.q) + (row0 + p) * a.q_token + h0 * a.q_head + d0;
+        T* to = static_cast<T*>(a.q_out) + (row0 + p) * a.o_token + h0 * a.o_head + d0;
+        uint4 x[kQHeads];
+#pragma unroll
+        for (int h = 0; h < kQHeads; ++h)
+          if (h < h_n) x[h] = *reinterpret_cast<const uint4*>(from + h * a.q_head);
+        float c[8], sn[8];  // of each dimension (of pairs, twice); the sine negative for the first of a pair
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = 1.f, sn[i] = 0.f;
+        if (turns) {
+          const long long at = (long long)p * half + (a.interleaved ? d0 >> 1 : first ? d0 : d0 - half);
+          const float4 c0 = *reinterpret_cast<const float4*>(a.cos + at), s0 = *reinterpret_cast<const float4*>(a.sin + at);
+          if (a.interleaved) {
+            const float cs[4] = {c0.x, c0.y, c0.z, c0.w}, ss[4] = {s0.x, s0.y, s0.z, s0.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c[2 * i] = c[2 * i + 1] = cs[i], sn[2 * i] = -ss[i], sn[2 * i + 1] = ss[i];
+          } else {
+            const float4 c1 = *reinterpret_cast<const float4*>(a.cos + at + 4), s1 = *reinterpret_cast<const float4*>(a.sin + at + 4);
+            const float cs[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w}, ss[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[i] = cs[i], sn[i] = first ? -ss[i] : ss[i];
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < kQHeads; ++h) {
+          if (h >= h_n) break;
+          const uint32_t w[4] = {x[h].x, x[h].y, x[h].z, x[h].w};
+          uint32_t y[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 u = Elem<T>::two(w[i]);
+            const uint32_t pw = a.interleaved ? w[i] : __shfl_sync(mask, w[i], src);
+            const float2 z = Elem<T>::two(pw);
+            const float q0 = a.interleaved ? z.y : z.x, q1 = a.interleaved ? z.x : z.y;
+            // (x c + p (-s) rounds as x c - p s does)
+            const float r0 = __fadd_rn(__fmul_rn(u.x, c[2 * i]), __fmul_rn(q0, sn[2 * i]));
+            const float r1 = __fadd_rn(__fmul_rn(u.y, c[2 * i + 1]), __fmul_rn(q1, sn[2 * i + 1]));
+            y[i] = turns ? Elem<T>::pack(r0, r1) : w[i];
+          }
+          x[h] = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+        __syncwarp(mask);  // q_out may be q: every lane of a row has read before one writes
+#pragma unroll
+        for (int h = 0; h < kQHeads; ++h)
+          if (h < h_n) *reinterpret_cast<uint4*>(to + h * a.o_head) = x[h];
+      }
+      return;
+    }
     for (int p = lo + unit; p < hi; p += kUnits) {
       const Angles an = angles_of(a, p, dA), bn = angles_of(a, p, dB);
 #pragma unroll 1
