@@ -419,7 +419,7 @@ constexpr int kQHeads = 8;
 constexpr int kFewTokens = 8;  // up to so many new tokens a sequence, k_kv_append
 
 template <int D, typename T, int kIt, int kThreads>
-__global__ void __launch_bounds__(kThreads, 768 / kThreads) k_kv_append_many(const KvAppendArgs a) {
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_kv_append_many(const KvAppendArgs a) {
   constexpr int kLanes = D / 8, kUnits = kThreads / kLanes;
   __shared__ float sm_amax[kThreads / 32];
   const int b = blockIdx.z, piece = blockIdx.x;
@@ -457,10 +457,6 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) k_kv_append_many(con
       for (int p = lo + unit; p < hi; p += kUnits) {
         const T* from = static_cast<const T*>(a.q) + (row0 + p) * a.q_token + h0 * a.q_head + d0;
         T* to = static_cast<T*>(a.q_out) + (row0 + p) * a.o_token + h0 * a.o_head + d0;
-        uint4 x[kQHeads];
-#pragma unroll
-        for (int h = 0; h < kQHeads; ++h)
-          if (h < h_n) x[h] = *reinterpret_cast<const uint4*>(from + h * a.q_head);
         float c[8], sn[8];  // of each dimension (of pairs, twice); the sine negative for the first of a pair
 #pragma unroll
         for (int i = 0; i < 8; ++i) c[i] = 1.f, sn[i] = 0.f;
@@ -478,9 +474,15 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) k_kv_append_many(con
             for (int i = 0; i < 8; ++i) c[i] = cs[i], sn[i] = first ? -ss[i] : ss[i];
           }
         }
+#pragma unroll 1
+        for (int hg = 0; hg < h_n; hg += 4, from += 4 * a.q_head, to += 4 * a.o_head) {  // four heads under way at a time
+          uint4 x[4];
 #pragma unroll
-        for (int h = 0; h < kQHeads; ++h) {
-          if (h >= h_n) break;
+          for (int h = 0; h < 4; ++h)
+            if (hg + h < h_n) x[h] = *reinterpret_cast<const uint4*>(from + h * a.q_head);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          if (hg + h >= h_n) break;
           const uint32_t w[4] = {x[h].x, x[h].y, x[h].z, x[h].w};
           uint32_t y[4];
 #pragma unroll
@@ -498,8 +500,9 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) k_kv_append_many(con
         }
         __syncwarp(mask);  // q_out may be q: every lane of a row has read before one writes
 #pragma unroll
-        for (int h = 0; h < kQHeads; ++h)
-          if (h < h_n) *reinterpret_cast<uint4*>(to + h * a.o_head) = x[h];
+        for (int h = 0; h < 4; ++h)
+          if (hg + h < h_n) *reinterpret_cast<uint4*>(to + h * a.o_head) = x[h];
+        }
       }
       return;
     }
