@@ -534,8 +534,8 @@ typedef struct {
  * max_new >= every sequence's new tokens, max_length >= every length (bounds: what
  * launches are sized by). The device arrays are not checked before the call; the
  * kernels check them, skip a sequence that breaks a bound, and set KV status bits
- * (fs_kv_check: FS_EDEVICE). Limits: batch <= 65535, tokens * query heads <= 2^31 - 1,
- * heads <= 1024, max_length <= 2^30.
+ * (fs_kv_check: FS_EDEVICE). Limits: batch <= 65535, tokens <= batch * max_new unless batch is 0, tokens *
+ * query heads <= 2^30, heads <= 1024, max_length <= 2^30.
  */
 typedef struct {
     int32_t batch;

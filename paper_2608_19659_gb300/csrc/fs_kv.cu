@@ -52,14 +52,16 @@ int check_batch(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads) {
   if (b->batch < 0 || b->batch > 65535) return say(FS_EINVAL, "batch = %d outside [0, 65535]", b->batch);
   if (b->tokens < 0 || b->max_new < 0 || b->max_new > b->tokens)
     return say(FS_EINVAL, "tokens = %d, max_new = %d: want 0 <= max_new <= tokens", b->tokens, b->max_new);
+  if (b->batch && (int64_t)b->batch * b->max_new < b->tokens)
+    return say(FS_EINVAL, "tokens = %d are more than batch * max_new = %d * %d", b->tokens, b->batch, b->max_new);
   if (b->max_length < 0 || b->max_length > (1 << 30))
     return say(FS_EINVAL, "max_length = %d outside [0, 2^30]", b->max_length);
   if (b->table_stride < 0 || (int64_t)b->table_stride * c->page_tokens < b->max_length)
     return say(FS_EINVAL, "table_stride = %d pages are fewer than max_length = %d tokens need", b->table_stride,
                b->max_length);
-  if ((int64_t)b->table_stride * c->page_tokens > INT_MAX) return say(FS_EINVAL, "table_stride = %d is too large", b->table_stride);
+  if ((int64_t)b->table_stride * c->page_tokens > INT_MAX - 128) return say(FS_EINVAL, "table_stride = %d is too large", b->table_stride);
   if (q_heads < 1 || q_heads > 65535) return say(FS_EINVAL, "q_heads = %d outside [1, 65535]", q_heads);
-  if ((int64_t)b->tokens * q_heads > INT_MAX) return say(FS_EINVAL, "tokens * q_heads exceeds 2^31 - 1");
+  if ((int64_t)b->tokens * q_heads > (1 << 30)) return say(FS_EINVAL, "tokens * q_heads exceeds 2^30");
   if (b->batch && b->tokens && (!b->page_table || !b->length || !b->q_start))
     return say(FS_EINVAL, "page_table / length / q_start is NULL");
   return FS_OK;
@@ -868,7 +870,8 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   if (int rc = check_rows(qu->out, "out")) return rc;
   int sms = 0;
   if (int rc = device_sms(&sms)) return rc;
-  const KvPlan p = plan_of(cache, batch, qu->q_heads, qu->window, sms);
+  const int window = qu->window < batch->max_length ? qu->window : 0;  // (a window over everything is none)
+  const KvPlan p = plan_of(cache, batch, qu->q_heads, window, sms);
   if (int rc = check_workspace(workspace, workspace_bytes, (int64_t)(kKvPartAt + 4 * (p.part_floats + p.chunk_floats) + (p.wide_bytes ? p.wide_bytes + 128 : 0)))) return rc;
   if (p.chunk_tiles > 65535) return say(FS_EINVAL, "max_new = %d: too many rows for one call", batch->max_new);
 
@@ -877,7 +880,7 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   a.q = qu->q.data, a.q_token = qu->q.token_stride, a.q_head = qu->q.head_stride;
   a.out = qu->out.data, a.out_token = qu->out.token_stride, a.out_head = qu->out.head_stride;
   a.scale_log2 = qu->scale * 1.44269504f;
-  a.window = qu->window;
+  a.window = window;
   a.split = p.split;
   a.tickets = p.tickets;
   a.cluster = p.cluster;

@@ -6,6 +6,8 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 #include "fs_internal.cuh"
 
 namespace fs {
@@ -153,6 +155,18 @@ __device__ __forceinline__ int row_exponent(float amax) {
   return min(max(e, -126), 126);
 }
 __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126..127
+
+// Raises a kernel's shared memory limit once on each device (seen: a bit a device, one word a kernel).
+inline cudaError_t smem_limit_once(std::atomic<uint64_t>& seen, const void* kernel, size_t bytes) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (seen.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  e = raise_smem_limit(kernel, bytes);
+  if (e == cudaSuccess && dev < 64) seen.fetch_or(bit, std::memory_order_release);
+  return e;
+}
 
 // A tensor map of a cache tensor: [pages][heads][page tokens][dim] bytes in tiles of
 // `rows` tokens of one (page, head), its 16-byte pieces swizzled over the rows or in order.

@@ -732,7 +732,8 @@ __global__ void __launch_bounds__(256) k_kv_expand(const KvAttendArgs a, const u
 template <int D, typename T, bool kWide>
 cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int tiles, int parts, cudaStream_t s) {
   using C = Cfg<D, kWide>;
-  static const cudaError_t limit = raise_smem_limit(reinterpret_cast<const void*>(k_kv_chunk<D, T, kWide>), C::kSmem);
+  static std::atomic<uint64_t> seen{0};
+  const cudaError_t limit = smem_limit_once(seen, reinterpret_cast<const void*>(k_kv_chunk<D, T, kWide>), C::kSmem);
   if (limit != cudaSuccess) return limit;
   return launch_pdl(k_kv_chunk<D, T, kWide>, dim3(a.v.heads * a.v.batch, tiles, parts), dim3(C::kThreads), C::kSmem, s, mk, mv, a);
 }

@@ -617,7 +617,8 @@ __global__ void __launch_bounds__(kWarps * 32, D == 128 && NT == 1 ? 3 : 1)
 template <int D, int NT, typename T>
 cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, int row_blocks, int splits,
                    cudaStream_t s) {
-  static const cudaError_t limit = raise_smem_limit(reinterpret_cast<const void*>(k_kv_decode<D, NT, T>), decode_smem<D>());
+  static std::atomic<uint64_t> seen{0};
+  const cudaError_t limit = smem_limit_once(seen, reinterpret_cast<const void*>(k_kv_decode<D, NT, T>), decode_smem<D>());
   if (limit != cudaSuccess) return limit;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((splits + a.cluster - 1) / a.cluster * a.cluster, a.v.heads * row_blocks, a.v.batch);

@@ -232,3 +232,74 @@ def test_broken_batches_are_reported(fsb, cuda):
     want, mag, dots = ref.attend(q.float().cpu().numpy(), d["k"], d["v"], d["k_scale"], d["v_scale"], d["table"],
                                  d["length"], d["q_start"], 0.1, 0)
     check(out, want, mag, dots, DTYPES["bf16"])
+
+
+def test_a_workspace_serves_smaller_batches(fsb, cuda):
+    """A workspace made for the largest batch, cache and queries is enough for any smaller ones (the cut into
+    parts differs), and what one call leaves in it does not show in the next."""
+    torch = cuda
+    rng = np.random.default_rng(18)
+    big = ref.make(rng, [(6000, 300)] + [(3000, 40)] * 11, 2, 64, 16)
+    cache, batch, q, ws = on_gpu(torch, fsb, big, 8, "bf16", rng.standard_normal((740, 8, 64)).astype(np.float32))
+    for lens in ([(6000, 1)], [(2999, 9), (17, 3)], [(6000, 300)], [(1, 1)] * 12, [(4097, 70)] * 3, [(5000, 1)] * 12):
+        need = [-(-l // 16) for l, _ in lens]
+        table = np.stack([np.resize(big["table"][0], 375) for _ in lens])
+        d = dict(big, table=table, length=np.array([l for l, _ in lens], np.int32),
+                 q_start=np.concatenate([[0], np.cumsum([n for _, n in lens])]).astype(np.int32))
+        assert max(need) <= 375
+        T = int(d["q_start"][-1])
+        b = fsb.KvBatch(torch.from_numpy(table).cuda(), torch.from_numpy(d["length"]).cuda(), torch.from_numpy(d["q_start"]).cuda(),
+                        T, max(n for _, n in lens), max(l for l, _ in lens))
+        qq = torch.from_numpy(rng.standard_normal((T, 8, 64)).astype(np.float32)).to(torch.bfloat16).cuda()
+        out = torch.full_like(qq, float("nan"))
+        fsb.fs_kv_attend(cache, b, qq, out, 0.125, workspace=ws)
+        fsb.fs_kv_check(ws)
+        want, mag, dots = ref.attend(qq.float().cpu().numpy(), d["k"], d["v"], d["k_scale"], d["v_scale"], table, d["length"],
+                                     d["q_start"], 0.125, 0)
+        check(out, want, mag, dots, DTYPES["bf16"])
+
+
+@pytest.mark.parametrize("new", [1, 20, 200])
+def test_negative_and_zero_scales_of_scores(fsb, cuda, new):
+    torch = cuda
+    rng = np.random.default_rng(19)
+    d = ref.make(rng, [(330, new), (new, new)], 2, 128, 32)
+    cache, batch, q, ws = on_gpu(torch, fsb, d, 8, "fp16", rng.standard_normal((2 * new, 8, 128)).astype(np.float32))
+    for scale in (-0.1, 0.0):
+        out = torch.empty_like(q)
+        fsb.fs_kv_attend(cache, batch, q, out, scale, workspace=ws)
+        fsb.fs_kv_check(ws)
+        want, mag, dots = ref.attend(q.float().cpu().numpy(), d["k"], d["v"], d["k_scale"], d["v_scale"], d["table"],
+                                     d["length"], d["q_start"], scale, 0)
+        check(out, want, mag, dots, DTYPES["fp16"])
+
+
+@pytest.mark.parametrize("new", [1, 100])
+def test_windows_as_wide_as_an_int(fsb, cuda, new):
+    """A window that holds everything is no window, however wide."""
+    torch = cuda
+    rng = np.random.default_rng(20)
+    d = ref.make(rng, [(330, new), (new, new)], 1, 64, 16)
+    cache, batch, q, ws = on_gpu(torch, fsb, d, 4, "bf16", rng.standard_normal((2 * new, 4, 64)).astype(np.float32))
+    outs = []
+    for window in (0, 330, 2**31 - 1):
+        outs.append(fsb.fs_kv_attend(cache, batch, q, torch.empty_like(q), 0.125, window=window, workspace=ws))
+    fsb.fs_kv_check(ws)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("new", [1, 40, 300])
+def test_nan_queries_stay_in_their_rows(fsb, cuda, new):
+    torch = cuda
+    rng = np.random.default_rng(21)
+    d = ref.make(rng, [(400, new), (new, new)], 2, 128, 64)
+    cache, batch, q, ws = on_gpu(torch, fsb, d, 8, "bf16", rng.standard_normal((2 * new, 8, 128)).astype(np.float32))
+    clean = fsb.fs_kv_attend(cache, batch, q, torch.empty_like(q), 0.1, workspace=ws).clone()
+    bad = q.clone()
+    bad[new - 1, 3, 17] = float("nan")
+    bad[new, 6, 0] = float("inf")
+    out = fsb.fs_kv_attend(cache, batch, bad, torch.empty_like(q), 0.1, workspace=ws)
+    fsb.fs_kv_check(ws)
+    hit = torch.zeros(out.shape[:2], dtype=torch.bool, device="cuda")
+    hit[new - 1, 3] = hit[new, 6] = True
+    assert bool(torch.isnan(out[hit].float()).all()) and torch.equal(out[~hit], clean[~hit])

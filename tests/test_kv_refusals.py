@@ -126,3 +126,11 @@ def test_the_binding_checks_tensors(fsb):
         fsb.KvBatch(torch.zeros(3, 4, dtype=torch.int64), i, torch.zeros(4, dtype=torch.int32), 0, 0, 0)
     with pytest.raises(ValueError, match="bfloat16 or float16"):
         fsb._kv_dtype(s)
+
+
+def test_more_tokens_than_sequences_can_hold(fsb):
+    cache, batch, new, query = good(fsb)
+    batch.tokens = 7  # three sequences of at most two new tokens
+    refused(fsb, fsb.lib().fs_kv_append(C.byref(cache), C.byref(batch), C.byref(new), P16, 1 << 40, None))
+    batch.tokens, batch.max_new = 1 << 29, 1 << 29  # times four query heads
+    refused(fsb, fsb.lib().fs_kv_attend(C.byref(cache), C.byref(batch), C.byref(query), P16, 1 << 40, None))
