@@ -506,8 +506,9 @@ int fs_draw_floor(int32_t mode, int32_t w, int64_t calls, int32_t reps, double *
  * t, dimension d of (page, head) is at page * page_stride + head * head_stride +
  * t * token_stride + d (bytes; strides multiples of 16, k and v 16-byte aligned).
  * k_scale, v_scale: [pages][heads] floats, powers of two or 0 (others set a status
- * bit); a code stands for its value times its (page, head)'s scale. Slots that hold no token may hold any bytes. A slot
- * that holds a token must not hold a NaN code (fs_kv_append writes none).
+ * bit, as may scales of a sequence's values more than 2^100 apart); a code stands for
+ * its value times its (page, head)'s scale. Slots that hold no token may hold any bytes.
+ * A slot that holds a token must not hold a NaN code (fs_kv_append writes none).
  */
 typedef struct {
     int32_t pages;

@@ -928,5 +928,5 @@ extern "C" int fs_kv_check(void* workspace, void* cuda_stream) {
              st & KV_ST_BATCH ? "length or q_start out of the batch's bounds; " : "",
              st & KV_ST_VALUE ? "a NaN in keys or values; " : "",
              st & KV_ST_ANGLE ? "a position beyond the rows of cos / sin; " : "",
-             st & KV_ST_SCALE ? "a scale that is neither a power of two nor 0; " : "", st);
+             st & KV_ST_SCALE ? "a scale that is neither a power of two nor 0, or scales of values of a sequence 2^100 apart; " : "", st);
 }

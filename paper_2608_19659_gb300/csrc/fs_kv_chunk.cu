@@ -48,7 +48,7 @@ struct Bars {
   uint64_t full[8], used[kUsed], raw_full[4], raw_empty[4], s_full[2], p_full[2][2], pv_done[2], end;
   float vs[4][8];        // per tile of codes and 16 tokens: the values' scale
   uint32_t cut[4];       // per tile of codes: some tokens' values are to be 0
-  float2 scale[8][8];    // per tile (mod 8) and 16 tokens: the keys' scale, log2 of the values' over the largest
+  float2 scale[8][8];    // per tile (mod 8) and 16 tokens: the keys' scale, log2 of the values' over the first page's
   float v_ref;
   uint32_t tmem;
 };
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
     for (int i = 0; i < C::kRaw; ++i) mbar_init(&bars.raw_full[i], 1), mbar_init(&bars.raw_empty[i], 128);
     for (int t = 0; t < 2; ++t) mbar_init(&bars.s_full[t], 1), mbar_init(&bars.p_full[t][0], 128), mbar_init(&bars.p_full[t][1], 128), mbar_init(&bars.pv_done[t], 1);
     mbar_init(&bars.end, 1);
-    bars.v_ref = 0.f;
+    bars.v_ref = 1.f;
   }
   if (w == C::kIssuer) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars.tmem)) : "memory");
@@ -252,20 +252,6 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
   }
   __syncthreads();
 
-  // the largest scale of values of the pages that are walked
-  {
-    float vm = 0.f;
-    const int g0 = begin >> v.log_page, g1 = (kv_hi + (1 << v.log_page) - 1) >> v.log_page;
-    for (int g = g0 + threadIdx.x; g < g1; g += C::kThreads) {
-      const long long at = (long long)kv_page(v, b, g) * v.heads + h;
-      const float ks = v.k_scale[at], vs = v.v_scale[at];
-      kv_scales(v, ks, vs);
-      vm = fmaxf(vm, vs);
-    }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) vm = fmaxf(vm, __shfl_xor_sync(~0u, vm, d));
-    if (lane == 0) atomicMax(reinterpret_cast<int*>(&bars.v_ref), __float_as_int(vm));  // (nonnegative floats order as their bits do)
-  }
   // queries: a row a thread, scaled into [-2, 2] by a power of two (and by the scale's sign)
   int q_exp = 0;
   if (w < 8) {
@@ -300,9 +286,13 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
     }
     fence_proxy_async();
   }
-  fence_before();
-  __syncthreads();
-  fence_after();
+  // Queries are in place: only the warps that stored them and the one that issues products wait for
+  // that; tiles of the cache are on their way meanwhile.
+  if (w < 8 || w == C::kIssuer) {
+    fence_before();
+    asm volatile("bar.sync 1, 288;" ::: "memory");
+    fence_after();
+  }
   // (the whole of tensor memory is this block's: its columns begin at 0)
   constexpr uint32_t tmem = 0;
 
@@ -489,7 +479,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
     // ahead and their scales one, so that no copy waits for either.
     constexpr int kRaw = C::kRaw > 0 ? C::kRaw : 1;
     const int log_p = v.log_page, boxes = kTok >> log_p;
-    const int v_exp = __float_as_int(bars.v_ref) >> 23;
+    int v_exp = 127;  // exponent of the scale that those of values are relative to: the first page's
     int page0 = 0, page1 = 0, page2 = 0;
     bool held0 = false, held1 = false, held2 = false;
     float ks0 = 0.f, vs0 = 0.f, ks1 = 0.f, vs1 = 0.f;
@@ -518,6 +508,12 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
         held0 = held1, page0 = page1, ks0 = ks1, vs0 = vs1;
         ask_scales();
         ask_pages(j + 2);
+        if (j == 0) {
+          const float ref = __shfl_sync(~0u, vs0, 0);
+          if (ref > 0.f) v_exp = __float_as_int(ref) >> 23 & 255;
+          if (lane == 0) bars.v_ref = exp2_int(v_exp - 127);
+        }
+        kv_scales(v, ks0, vs0);
       }
       bool ok = true;
       if constexpr (kWide) {
@@ -531,7 +527,8 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
         // (this far ahead of softmax the entry of eight tiles ago has been read) a scale of 0 counts as
         // one too small to matter
         const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p), ks = __shfl_sync(~0u, ks0, (lane << 4) >> log_p);
-        const int e = vs != 0.f ? max((__float_as_int(vs) >> 23) - v_exp, -100) : -100;
+        const int d = (__float_as_int(vs) >> 23) - v_exp, e = vs != 0.f ? min(max(d, -100), 100) : -100;
+        if (vs != 0.f && d != e) kv_flag(v, KV_ST_SCALE);
         if (lane < 8) bars.scale[j & 7][lane] = make_float2(ks, (float)e);
       }
       if constexpr (kWide) {
