@@ -500,65 +500,80 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
     ask_pages(0);
     ask_scales();
     ask_pages(1);
+    // the next tile's lists become the current ones, and its scales go to the softmax warps (far enough
+    // ahead of them that the entry of eight tiles ago has been read); a scale of 0 counts as one too
+    // small to matter
+    auto take = [&](int j) {
+      held0 = held1, page0 = page1, ks0 = ks1, vs0 = vs1;
+      ask_scales();
+      ask_pages(j + 2);
+      if (j == 0) {
+        const float ref = __shfl_sync(~0u, vs0, 0);
+        if (ref > 0.f) v_exp = __float_as_int(ref) >> 23 & 255;
+        if (lane == 0) bars.v_ref = exp2_int(v_exp - 127);
+      }
+      kv_scales(v, ks0, vs0);
+    };
+    auto tell = [&](int j) {
+      const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p), ks = __shfl_sync(~0u, ks0, (lane << 4) >> log_p);
+      const int d = (__float_as_int(vs) >> 23) - v_exp, e = vs != 0.f ? min(max(d, -100), 100) : -100;
+      if (vs != 0.f && d != e) kv_flag(v, KV_ST_SCALE);
+      if (lane < 8) bars.scale[j & 7][lane] = make_float2(ks, (float)e);
+      __syncwarp();
+    };
+    if constexpr (kWide) {
+      // the first keys, then values j and keys j + 1 on one barrier: both slots are free after the same products
+      constexpr int kHalf = C::kStages / 2;
+      auto copy = [&](int i, uint64_t* bar) {
+        bulk_g2s_at(ring_at + i % C::kStages * C::kSlot, wide + (long long)i * C::kSlot, C::kSlot, bar);
+      };
+      int j = -1;
+      if (n > 0) {
+        take(0);
+        tell(0);
+        if (lane == 0) mbar_expect_tx(&bars.full[0], C::kSlot), copy(0, &bars.full[0]);
+        for (j = 0; j < n; ++j) {
+          const bool next = j + 1 < n;
+          if (next) take(j + 1);
+          const int use = j - kHalf + 1;
+          const bool ok = use < 0 || wait_bar(&bars.used[use % kUsed], (use / kUsed) & 1, v);
+          if (!__all_sync(~0u, ok)) break;
+          if (next) tell(j + 1);
+          uint64_t* bar = &bars.full[1 + j % kHalf];
+          if (lane == 0) {
+            mbar_expect_tx(bar, (next ? 2 : 1) * C::kSlot);
+            copy(2 * j + 1, bar);
+            if (next) copy(2 * j + 2, bar);
+          }
+        }
+        if (j < n)  // a wait ran out: the copies under way first (with the same limit)
+          for (int k = max(0, j - kHalf); k < j; ++k) mbar_wait(&bars.full[1 + k % kHalf], (k / kHalf) & 1, kWaitLimitNs);
+      }
+    } else {
     int i = 0;
     for (; i < 2 * n; ++i) {
-      const int j = i >> 1;
+      const int j = i >> 1, rs = i % kRaw;
       const bool values = i & 1;
-      if (!values) {
-        held0 = held1, page0 = page1, ks0 = ks1, vs0 = vs1;
-        ask_scales();
-        ask_pages(j + 2);
-        if (j == 0) {
-          const float ref = __shfl_sync(~0u, vs0, 0);
-          if (ref > 0.f) v_exp = __float_as_int(ref) >> 23 & 255;
-          if (lane == 0) bars.v_ref = exp2_int(v_exp - 127);
-        }
-        kv_scales(v, ks0, vs0);
-      }
-      bool ok = true;
-      if constexpr (kWide) {
-        const int use = j - C::kStages / 2 + (values ? 1 : 0);  // (as for the converters)
-        if (j >= C::kStages / 2) ok = wait_bar(&bars.used[use % kUsed], (use / kUsed) & 1, v);
-      } else {
-        ok = wait_bar(&bars.raw_empty[i % kRaw], ((i / kRaw) & 1) ^ 1, v);
-      }
+      if (!values) take(j);
+      const bool ok = wait_bar(&bars.raw_empty[rs], ((i / kRaw) & 1) ^ 1, v);
       if (!__all_sync(~0u, ok)) break;
-      if (!values) {
-        // (this far ahead of softmax the entry of eight tiles ago has been read) a scale of 0 counts as
-        // one too small to matter
-        const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p), ks = __shfl_sync(~0u, ks0, (lane << 4) >> log_p);
-        const int d = (__float_as_int(vs) >> 23) - v_exp, e = vs != 0.f ? min(max(d, -100), 100) : -100;
-        if (vs != 0.f && d != e) kv_flag(v, KV_ST_SCALE);
-        if (lane < 8) bars.scale[j & 7][lane] = make_float2(ks, (float)e);
+      if (!values) tell(j);
+      const uint32_t held = __ballot_sync(~0u, held0);
+      if (values) {
+        const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p);
+        if (lane < 8) bars.vs[rs][lane] = vs;
+        // (a group beyond kv_hi has the scale 0 too)
+        const bool cut = __any_sync(~0u, lane < 8 && vs == 0.f) || begin + (j + 1) * kTok > kv_hi;
+        if (lane == 0) bars.cut[rs] = cut;
       }
-      if constexpr (kWide) {
-        const int st = i % C::kStages;
-        __syncwarp();
-        if (lane == 0) {
-          mbar_expect_tx(&bars.full[st], C::kSlot);
-          bulk_g2s_at(ring_at + st * C::kSlot, wide + (long long)i * C::kSlot, C::kSlot, &bars.full[st]);
-        }
-      } else {
-        const int rs = i % kRaw;
-        const uint32_t held = __ballot_sync(~0u, held0);
-        if (values) {
-          const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p);
-          if (lane < 8) bars.vs[rs][lane] = vs;
-          // (a group beyond kv_hi has the scale 0 too)
-          const bool cut = __any_sync(~0u, lane < 8 && vs == 0.f) || begin + (j + 1) * kTok > kv_hi;
-          if (lane == 0) bars.cut[rs] = cut;
-        }
-        __syncwarp();
-        if (lane == 0) mbar_expect_tx(&bars.raw_full[rs], (uint32_t)(__popc(held) * D) << log_p);
-        __syncwarp();
-        if (held0)
-          tma_tile(raw_at + rs * C::kRawSlot + ((lane * D) << log_p), values ? &mv : &mk, 0, h, page0, &bars.raw_full[rs]);
-      }
+      __syncwarp();
+      if (lane == 0) mbar_expect_tx(&bars.raw_full[rs], (uint32_t)(__popc(held) * D) << log_p);
+      __syncwarp();
+      if (held0)
+        tma_tile(raw_at + rs * C::kRawSlot + ((lane * D) << log_p), values ? &mv : &mk, 0, h, page0, &bars.raw_full[rs]);
     }
-    if (i < 2 * n) {  // a wait ran out: the copies under way first (with the same limit)
-      constexpr int kAhead = kWide ? C::kStages : kRaw;
-      uint64_t* bar = kWide ? bars.full : bars.raw_full;
-      for (int k = max(0, i - kAhead); k < i; ++k) mbar_wait(&bar[k % kAhead], (k / kAhead) & 1, kWaitLimitNs);
+    if (i < 2 * n)  // a wait ran out: the copies under way first (with the same limit)
+      for (int k = max(0, i - kRaw); k < i; ++k) mbar_wait(&bars.raw_full[k % kRaw], (k / kRaw) & 1, kWaitLimitNs);
     }
     } else if (w == C::kIssuer && n > 0) {
     // ---------------------------------------------------------------- products
@@ -597,7 +612,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
     int vs = 1, ks = 2;
     uint32_t v_par = 0, k_par = 0;  // parities of the slots' rounds
     for (int j = 0; ok && j < n_u; ++j) {
-      ok = wait_all(&bars.full[vs], v_par);
+      ok = kWide ? wait_all(&bars.full[1 + j % (C::kStages / 2)], (j / (C::kStages / 2)) & 1) : wait_all(&bars.full[vs], v_par);
       for (int t = 0; ok && t < n_sub_u; ++t) {
         for (int half = 0; ok && half < 2; ++half) {
           ok = wait_all(&bars.p_full[t][half], j & 1);
@@ -607,9 +622,9 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
         if (!ok) break;
         if (one && j + 1 == n_u) commit(&bars.pv_done[t]);
         if (j + 1 < n_u) {
-          if (t == 0) ok = wait_all(&bars.full[ks], k_par);
+          if (!kWide && t == 0) ok = wait_all(&bars.full[ks], k_par);
           if (!ok) break;
-          fence_after();
+          if (!kWide) fence_after();
           if (one) {
             qk(t, ks);
             commit(&bars.s_full[t]);
