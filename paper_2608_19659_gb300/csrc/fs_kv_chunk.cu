@@ -2,26 +2,35 @@
 //
 // A block takes two tiles of 128 rows (new token, query head) of one (sequence, key head)
 // and walks over the cache in tiles of 128 tokens:
-//   S [128 x 128] = Q K^T,  P = exp2(c S - m),  O [128 x dim] += P V
+//   S [128 x 128] = Q K^T,  P = 2^(c S + e - m),  O [128 x dim] += P V
 // with both products on the tensor cores in half precision (the codes are exact in it, a
 // bf16 query too once its row is scaled by a power of two; P keeps 11 bits) and S, P, O in
 // tensor memory: S_t in 128 columns, P_t in the first 64 of the same ones (a row's thread
-// writes a column only after it has read it), O_t in dim.
+// holds its S in registers by then), O_t in dim. c holds the scale of a page's keys, e is log2
+// of that of its values and m the largest of c S + e: half precision's step in P is relative to
+// what counts most, however far the scales are apart. The row's sum of weights is taken in
+// float without e. O is rescaled only when m has grown by more than 2^8 (P, times 2^7, stays
+// under 65504), so almost never after the first tiles.
 //
-// Roles of the 14 warps:
-//   0-3, 4-7  softmax of tile 0 / 1, a row a thread: the maximum in one pass over S, P and the
-//             row's sum in a second. P holds a token's weight times the scale of its page's values
-//             (a power of two: an addend of the exponent), m is the largest of those, so that half
-//             precision's step is relative to what counts most; the sum of weights is taken without
-//             the scales. O is rescaled only when m has grown by more than 2^8 (P, times 2^7,
-//             stays under 65504), so almost never after the first tiles
-//   8-11      codes to halves, from the tiles as they came to swizzled ones. Keys are scaled by
-//             their page's scale over the largest (times 2^7: 448 * 2^7 < 65504 leaves small
-//             pages the most room)
-//   12        one thread issues every product. While tile 0's rows are in softmax the tensor
-//             cores work on tile 1, and the other way round.
-//   13        keeps tiles of codes on their way (tensor-map copies, a page each at most)
-// Bound by the tensor cores: 4 dim operations per (row, token) at the bf16 rate.
+// The codes become halves once for all walks (k_kv_expand) where at least four blocks walk over
+// a sequence's tokens, else in each walk. Roles of the warps:
+//   0-3, 4-7  softmax of tile 0 / 1, a row a thread. Half of P is handed over while the other half
+//             is computed (471 -> 465 us, see below). Two threads a row: 544 us, the 16 warps
+//             crowd out the one that issues products
+//   8-11      (only where the walk converts) codes to halves, from the tiles as they came to
+//             swizzled ones
+//   then one  issues every product. While tile 0's rows are in softmax the tensor cores work on
+//             tile 1, and the other way round. Two such warps, one a tile: 506-525 us, their
+//             products mix and neither chain is short
+//   and one   keeps tiles on their way: bulk copies of 32 KB halves, or tensor-map copies of the
+//             codes, a page each at most
+//
+// Bound by the tensor cores, 4 dim operations per (row, token), and by how fast one thread beside
+// eight busy softmax warps can issue their products and waits (a commit costs it about 200 clocks,
+// hence three of them a pair of tiles: 477 -> 458 us). A prompt of 8192 tokens, 32 query heads over 4
+// key heads of 128: 411 us with the conversion (10 us), 1.34 PFLOP/s of causal work, tensor cores
+// active 61 % of the time; 69 % of the bf16 rate that a library product reaches. The steps in
+// brackets are of the same prompt, when they were taken.
 #include "fs_kv.cuh"
 
 namespace fs {
@@ -697,7 +706,7 @@ __global__ void __launch_bounds__(256) k_kv_chunk_join(const KvAttendArgs a, int
 // The codes of whole sequences as halves, in the order and swizzle that the products read
 // them in: [sequence][head][tile of 128 tokens][keys, values][block of 64 dimensions][token][64].
 // Where many blocks walk over the same tokens, each tile is then converted once instead of by every
-// one of them (8192 tokens' prompt XXX us with conversion in every walk). Tokens beyond a sequence's
+// one of them (a prompt of 8192 tokens 455 -> 423 us). Tokens beyond a sequence's
 // and values whose scale is 0 become 0.
 template <int D>
 __global__ void __launch_bounds__(256) k_kv_expand(const KvAttendArgs a, const uint8_t* kc, const uint8_t* vc,

@@ -7,16 +7,19 @@
 // blocks to finish join the clusters' results (fixed order: results do not depend on which
 // block is last).
 //
-// A warp of the block takes every fourth tile of 32 tokens. Its lane 0 keeps kStages
-// tiles of keys and values on their way into the warp's own ring (tensor-map copies of
-// 16 or 32 tokens of one page, swizzled, so that the reads below meet no bank twice);
-// no block-wide barrier is met before the end. Per 16 tokens:
+// A warp of the block takes every fourth tile of 32 tokens and keeps kStages tiles of keys and
+// values on their way into its own ring (tensor-map copies of 16 or 32 tokens of one page,
+// swizzled, so that the reads below meet no bank twice); no block-wide barrier is met before the
+// end. Per 16 tokens:
 //   S^T [16 tokens x rows]  = K [16 x dim] Q^T          (the codes, exact in half precision)
 //   O^T [dim x rows]       += V^T [dim x 16] P^T         (P rounded to half precision)
 // with m16n8k16 products: tokens and dimensions fill the 16 rows of the instruction, the
 // attention rows its 8 columns, so one query head costs no more padding than eight.
 // tcgen05 has nothing to add here: its smallest tile is 128 rows high, and its operands
 // would have to pass through shared memory once more after the conversion.
+// Three blocks an SM with two stages a warp (24 warps' rings, 192 KB an SM) read 64 sequences of up
+// to 32768 tokens, 1.5 GB, in 243 us (6.3 TB/s, 93 % of the copy rate); two blocks with three
+// stages took 258 us.
 // The scale of a page's keys multiplies S. That of its values, a power of two relative to the
 // largest met so far (v_ref), goes into P as an addend of the exponent, and m is the largest
 // weight times scale: half precision's step is relative to what counts most, however far the
