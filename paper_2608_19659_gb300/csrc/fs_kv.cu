@@ -762,9 +762,10 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
     const long long want = 2 * items <= slots ? slots / items : (3 * slots + items - 1) / items;
     p.split = std::clamp((int)((len + want - 1) / want + 127) / 128 * 128, kMinSplit, kMaxSplit);
     p.splits = (len + p.split - 1) / p.split;
-    // clusters where blocks are few (one token of 1000: 8.0 us without): where they are many, their
-    // need of free places side by side costs more (33 ragged requests 17 us without, 24 us with)
-    if (items * p.splits <= sms)
+    // clusters where blocks are few (one token of 1000: 8.0 us without) or of few items (131072 tokens
+    // of one head: 19.9 us without, 18.8 with): elsewhere sequences' parts differ in number, and the need
+    // of free places side by side costs more (33 ragged requests 17 us without, 24 us with)
+    if (items * p.splits <= (items <= 8 ? slots : sms))
       while (p.cluster < kKvCluster && p.cluster < p.splits) p.cluster *= 2;
     p.splits = (p.splits + p.cluster - 1) / p.cluster * p.cluster;
     const int groups = (p.splits / p.cluster + kKvFan - 1) / kKvFan;
