@@ -531,12 +531,13 @@ typedef struct {
  * Token position p of sequence b is in page page_table[b * table_stride +
  * p / page_tokens], slot p mod page_tokens; entries beyond a sequence's tokens may
  * hold anything. A row whose position would be negative (more new tokens than length) is
- * not appended and attends to nothing. Host values: tokens = q_start[batch],
- * max_new >= every sequence's new tokens, max_length >= every length (bounds: what
- * launches are sized by). The device arrays are not checked before the call; the
- * kernels check them, skip a sequence that breaks a bound, and set KV status bits
- * (fs_kv_check: FS_EDEVICE). Limits: batch <= 65535, tokens <= batch * max_new unless batch is 0, tokens *
- * query heads <= 2^30, heads <= 1024, max_length <= 2^30.
+ * not appended, its query not rotated (its row of q_out is left), and it attends to
+ * nothing. Host values: tokens = q_start[batch], max_new >= every sequence's new tokens,
+ * max_length >= every length (bounds: what launches are sized by). The device arrays
+ * are not checked before the call; the kernels check them, skip a sequence that breaks a
+ * bound, and set status bits (fs_kv_check: FS_EDEVICE). Limits: batch <= 65535,
+ * tokens <= batch * max_new unless batch is 0, tokens * query heads <= 2^30, heads <= 1024,
+ * max_length <= 2^30.
  */
 typedef struct {
     int32_t batch;

@@ -83,6 +83,7 @@ KvView view_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, void* ws
   v.batch = b->batch;
   v.tokens = b->tokens;
   v.max_new = b->max_new;
+  v.max_length = b->max_length;
   v.table_stride = b->table_stride;
   v.group = q_heads / c->heads;
   v.k_scale = c->k_scale;

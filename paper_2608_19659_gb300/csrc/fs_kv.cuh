@@ -30,7 +30,7 @@ constexpr size_t kKvPartAt = kKvTicketAt + 4 * (size_t)kKvTickets;
 
 // What every kernel reads of the cache and the batch.
 struct KvView {
-  int pages, heads, log_page, batch, tokens, max_new, table_stride, group;  // group: query heads per key head
+  int pages, heads, log_page, batch, tokens, max_new, max_length, table_stride, group;  // group: query heads per key head
   const float *k_scale, *v_scale;
   const int *page_table, *length, *q_start;
   uint32_t* status;
@@ -54,7 +54,8 @@ struct KvAttendArgs {
 };
 
 // One sequence of the batch as a kernel may use it: ranges checked, so that no
-// later index leaves its array whatever the batch's device arrays hold.
+// later index leaves its array whatever the batch's device arrays hold (the host has
+// checked that a page table's row holds max_length tokens).
 struct KvSeq {
   int len, first, count;  // tokens cached, first row of q, rows of q
 };
@@ -63,8 +64,7 @@ __device__ __forceinline__ bool kv_seq(const KvView& v, int b, KvSeq& s) {
   s.len = v.length[b];
   s.first = v.q_start[b];
   s.count = v.q_start[b + 1] - s.first;
-  const bool ok = s.len >= 0 && (long long)s.len <= ((long long)v.table_stride << v.log_page) && s.first >= 0 &&
-                  s.count >= 0 && s.count <= v.max_new && s.first <= v.tokens - s.count;
+  const bool ok = s.len >= 0 && s.len <= v.max_length && s.first >= 0 && s.count >= 0 && s.count <= v.max_new && s.first <= v.tokens - s.count;
   return ok;
 }
 

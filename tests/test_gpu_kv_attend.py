@@ -303,3 +303,75 @@ def test_nan_queries_stay_in_their_rows(fsb, cuda, new):
     hit = torch.zeros(out.shape[:2], dtype=torch.bool, device="cuda")
     hit[new - 1, 3] = hit[new, 6] = True
     assert bool(torch.isnan(out[hit].float()).all()) and torch.equal(out[~hit], clean[~hit])
+
+
+def test_a_length_beyond_the_bound_is_reported(fsb, cuda):
+    """Room in the page table, but a length beyond max_length, with every kind of walk: skipped and reported."""
+    torch = cuda
+    rng = np.random.default_rng(22)
+    for new, window in ((1, 0), (3, 100), (300, 0), (300, 100), (70, 0)):
+        d = ref.make(rng, [(4000, new), (4000, new)], 1, 64, 16)
+        cache, _, q, ws = on_gpu(torch, fsb, d, 4, "bf16", rng.standard_normal((2 * new, 4, 64)).astype(np.float32))
+        length = torch.tensor([500, 4000], dtype=torch.int32, device="cuda")
+        batch = fsb.KvBatch(torch.from_numpy(d["table"]).cuda(), length, torch.from_numpy(d["q_start"]).cuda(), 2 * new, new, 500)
+        work = fsb.KvWorkspace(cache, batch, 4)
+        out = torch.full_like(q, 7.0)
+        fsb.fs_kv_attend(cache, batch, q, out, 0.1, window=window, workspace=work)
+        with pytest.raises(fsb.FleetSieveError) as ei:
+            fsb.fs_kv_check(work)
+        assert ei.value.code == fsb.FS_EDEVICE and "bounds" in str(ei.value)
+        assert bool((out[new:] == 7).all())
+        want, mag, dots = ref.attend(q[:new].float().cpu().numpy(), d["k"], d["v"], d["k_scale"], d["v_scale"], d["table"][:1],
+                                     [500], [0, new], 0.1, window)
+        check(out[:new], want, mag, dots, DTYPES["bf16"])
+
+
+def test_chunks_give_the_same_bits_every_time_and_under_a_graph(fsb, cuda):
+    torch = cuda
+    for lens, heads in (([(700, 300), (130, 130), (90, 2)], 2), ([(6000, 40)], 1)):
+        out, (cache, batch, q, ws) = run(torch, fsb, 23, lens, heads, 8, 128, 32)
+        again = torch.empty_like(out)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            fsb.fs_kv_attend(cache, batch, q, again, 128**-0.5, workspace=ws)
+        for _ in range(3):
+            again.fill_(float("nan"))
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, again)
+
+
+def test_append_and_attend_in_a_row(fsb, cuda):
+    """A prompt in chunks, then single tokens, each step's append and attention queued without a wait between
+    them: every step's outputs are those of the same step alone."""
+    torch = cuda
+    rng = np.random.default_rng(24)
+    steps, hk, hq, D, P = [130, 1, 1, 64, 1, 257, 2], 2, 8, 128, 32
+    total = sum(steps)
+    pages = -(-total // P) + 1
+    x = torch.from_numpy(rng.standard_normal((total, hq + 2 * hk, D)).astype(np.float32)).to(torch.bfloat16).cuda()
+    table = torch.randperm(pages, device="cuda")[None].to(torch.int32).contiguous()
+
+    def go(wait):
+        cache = fsb.KvCache(*(torch.full((pages, hk, P, D), 0x7F, dtype=torch.uint8, device="cuda") for _ in range(2)),
+                            *(torch.full((pages, hk), 3.0, device="cuda") for _ in range(2)))
+        outs, at, keep = [], 0, []
+        for n in steps:
+            batch = fsb.KvBatch(table, torch.tensor([at + n], dtype=torch.int32, device="cuda"),
+                                torch.tensor([0, n], dtype=torch.int32, device="cuda"), n, n, total)
+            ws = fsb.KvWorkspace(cache, batch, hq)
+            row = x[at:at + n]
+            out = torch.empty(n, hq, D, dtype=x.dtype, device="cuda")
+            fsb.fs_kv_append(cache, batch, row[:, hq:hq + hk], row[:, hq + hk:], workspace=ws)
+            fsb.fs_kv_attend(cache, batch, row[:, :hq], out, 0.1, workspace=ws)
+            if wait:
+                fsb.fs_kv_check(ws)
+            keep.append(ws)
+            outs.append(out)
+            at += n
+        for ws in keep:
+            fsb.fs_kv_check(ws)
+        return outs
+
+    a, b = go(True), go(False)
+    assert all(torch.equal(p, q) and bool(torch.isfinite(p.float()).all()) for p, q in zip(a, b))
