@@ -50,11 +50,12 @@ struct Cfg {
   static constexpr size_t kSmem = 1024 + kQ + (size_t)kStages * kSlot + kRaw * kRawSlot + 1280;
 };
 
-// (a wait must not find its barrier two phases on: a phase comes round in no less than the ring)
-constexpr int kUsed = 8;
+// S of tile j of the cache is told on barrier j mod kRound. (Whoever refills a slot waits for the S
+// after the products that read it, up to four tiles late: a barrier must not be two phases on by then.)
+constexpr int kRound = 4;
 
 struct Bars {
-  uint64_t full[8], used[kUsed], raw_full[4], raw_empty[4], s_full[2], p_full[2][2], pv_done[2], end;
+  uint64_t full[8], raw_full[4], raw_empty[4], s_full[2][kRound], p_full[2][2], pv_done[2], end;
   float vs[4][8];        // per tile of codes and 16 tokens: the values' scale
   uint32_t cut[4];       // per tile of codes: some tokens' values are to be 0
   float2 scale[8][8];    // per tile (mod 8) and 16 tokens: the keys' scale, log2 of the values' over the first page's
@@ -249,9 +250,11 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kStages; ++i) mbar_init(&bars.full[i], kWide ? 1 : 128);
-    for (int i = 0; i < kUsed; ++i) mbar_init(&bars.used[i], 1);
     for (int i = 0; i < C::kRaw; ++i) mbar_init(&bars.raw_full[i], 1), mbar_init(&bars.raw_empty[i], 128);
-    for (int t = 0; t < 2; ++t) mbar_init(&bars.s_full[t], 1), mbar_init(&bars.p_full[t][0], 128), mbar_init(&bars.p_full[t][1], 128), mbar_init(&bars.pv_done[t], 1);
+    for (int t = 0; t < 2; ++t) {
+      for (int i = 0; i < kRound; ++i) mbar_init(&bars.s_full[t][i], 1);
+      mbar_init(&bars.p_full[t][0], 128), mbar_init(&bars.p_full[t][1], 128), mbar_init(&bars.pv_done[t], 1);
+    }
     mbar_init(&bars.end, 1);
     bars.v_ref = 1.f;
   }
@@ -328,7 +331,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
         const int t0 = begin + j * kTok;
         const bool whole = t0 >= all_lo && t0 + kTok <= all_hi;
         const int c_hi = hi - t0, c_lo = lo - t0;  // columns [c_lo, c_hi] count
-        ok = wait_bar(&bars.s_full[t], j & 1, v);
+        ok = wait_bar(&bars.s_full[t][j % kRound], (j / kRound) & 1, v);
         if (!__all_sync(~0u, ok)) break;
         fence_after();
         float x[kTok];
@@ -461,10 +464,10 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
         }
       }
       mbar_arrive(&bars.raw_empty[rs]);
-      // the slot's last tile, kStages / 2 of the cache's tiles ago (used[j] follows the products over the
-      // keys of tile j and the values of the one before)
+      // the slot's last tile, kStages / 2 of the cache's tiles ago (the last S of tile j follows the
+      // products over its keys and over the values of the tile before)
       const int use = (i >> 1) - C::kStages / 2 + (values ? 1 : 0);
-      if ((i >> 1) >= C::kStages / 2 && !wait_bar(&bars.used[use % kUsed], (use / kUsed) & 1, v)) break;
+      if ((i >> 1) >= C::kStages / 2 && !wait_bar(&bars.s_full[n_sub - 1][use % kRound], (use / kRound) & 1, v)) break;
       const uint32_t row = ring_at + st * C::kSlot + to;
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
@@ -545,7 +548,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
           const bool next = j + 1 < n;
           if (next) take(j + 1);
           const int use = j - kHalf + 1;
-          const bool ok = use < 0 || wait_bar(&bars.used[use % kUsed], (use / kUsed) & 1, v);
+          const bool ok = use < 0 || wait_bar(&bars.s_full[n_sub - 1][use % kRound], (use / kRound) & 1, v);
           if (!__all_sync(~0u, ok)) break;
           if (next) tell(j + 1);
           uint64_t* bar = &bars.full[1 + j % kHalf];
@@ -614,9 +617,8 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
     if (ok && one) {
       for (int t = 0; t < n_sub_u; ++t) {
         qk(t, 0);
-        commit(&bars.s_full[t]);
+        commit(&bars.s_full[t][0]);
       }
-      commit(&bars.used[0]);
     }
     int vs = 1, ks = 2;
     uint32_t v_par = 0, k_par = 0;  // parities of the slots' rounds
@@ -636,11 +638,10 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
           if (!kWide) fence_after();
           if (one) {
             qk(t, ks);
-            commit(&bars.s_full[t]);
+            commit(&bars.s_full[t][(j + 1) % kRound]);
           }
         }
       }
-      if (one) commit(&bars.used[(j + 1) % kUsed]);  // tile j's values and the keys of the next
       vs += 2;
       if (vs >= C::kStages) vs -= C::kStages, v_par ^= 1;
       ks += 2;
