@@ -486,171 +486,171 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
     else
       asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (w == C::kIssuer + 1) {
-    // ---------------------------------------------------------------- tiles from the cache
-    // Lane g holds the page of a tile's g-th box of a page's tokens. Page ids are asked for two tiles
-    // ahead and their scales one, so that no copy waits for either.
-    constexpr int kRaw = C::kRaw > 0 ? C::kRaw : 1;
-    const int log_p = v.log_page, boxes = kTok >> log_p;
-    int v_exp = 127;  // exponent of the scale that those of values are relative to: the first page's
-    int page0 = 0, page1 = 0, page2 = 0;
-    bool held0 = false, held1 = false, held2 = false;
-    float ks0 = 0.f, vs0 = 0.f, ks1 = 0.f, vs1 = 0.f;
-    auto ask_pages = [&](int j) {
-      const int t = begin + j * kTok + (lane << log_p);
-      held2 = j < n && lane < boxes && t < kv_hi;
-      if (held2) page2 = kv_page_raw(v, b, t >> log_p);
-    };
-    auto ask_scales = [&] {
-      held1 = held2, ks1 = vs1 = 0.f;
-      if (held1) {
-        page1 = kv_page_ok(v, page2);
-        const long long at = (long long)page1 * v.heads + h;
-        ks1 = v.k_scale[at], vs1 = v.v_scale[at];
-      }
-    };
-    const char* wide = kWide ? a.wide + ((long long)(b * v.heads + h) * a.wide_tiles + begin / kTok) * (2 * C::kSlot) : nullptr;
-    ask_pages(0);
-    ask_scales();
-    ask_pages(1);
-    // the next tile's lists become the current ones, and its scales go to the softmax warps (far enough
-    // ahead of them that the entry of eight tiles ago has been read); a scale of 0 counts as one too
-    // small to matter
-    auto take = [&](int j) {
-      held0 = held1, page0 = page1, ks0 = ks1, vs0 = vs1;
-      ask_scales();
-      ask_pages(j + 2);
-      if (j == 0) {
-        const float ref = __shfl_sync(~0u, vs0, 0);
-        if (ref > 0.f) v_exp = __float_as_int(ref) >> 23 & 255;
-        if (lane == 0) bars.v_ref = exp2_int(v_exp - 127);
-      }
-      kv_scales(v, ks0, vs0);
-    };
-    auto tell = [&](int j) {
-      const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p), ks = __shfl_sync(~0u, ks0, (lane << 4) >> log_p);
-      const int d = (__float_as_int(vs) >> 23) - v_exp, e = vs != 0.f ? min(max(d, -100), 100) : -100;
-      if (vs != 0.f && d != e) kv_flag(v, KV_ST_SCALE);
-      if (lane < 8) bars.scale[j & 7][lane] = make_float2(ks, (float)e);
-      __syncwarp();
-    };
-    if constexpr (kWide) {
-      // the first keys, then values j and keys j + 1 on one barrier: both slots are free after the same products
-      constexpr int kHalf = C::kStages / 2;
-      auto copy = [&](int i, uint64_t* bar) {
-        bulk_g2s_at(ring_at + i % C::kStages * C::kSlot, wide + (long long)i * C::kSlot, C::kSlot, bar);
+      // ---------------------------------------------------------------- tiles from the cache
+      // Lane g holds the page of a tile's g-th box of a page's tokens. Page ids are asked for two tiles
+      // ahead and their scales one, so that no copy waits for either.
+      constexpr int kRaw = C::kRaw > 0 ? C::kRaw : 1;
+      const int log_p = v.log_page, boxes = kTok >> log_p;
+      int v_exp = 127;  // exponent of the scale that those of values are relative to: the first page's
+      int page0 = 0, page1 = 0, page2 = 0;
+      bool held0 = false, held1 = false, held2 = false;
+      float ks0 = 0.f, vs0 = 0.f, ks1 = 0.f, vs1 = 0.f;
+      auto ask_pages = [&](int j) {
+        const int t = begin + j * kTok + (lane << log_p);
+        held2 = j < n && lane < boxes && t < kv_hi;
+        if (held2) page2 = kv_page_raw(v, b, t >> log_p);
       };
-      int j = -1;
-      if (n > 0) {
-        take(0);
-        tell(0);
-        if (lane == 0) mbar_expect_tx(&bars.full[0], C::kSlot), copy(0, &bars.full[0]);
-        for (j = 0; j < n; ++j) {
-          const bool next = j + 1 < n;
-          if (next) take(j + 1);
-          const int use = j - kHalf + 1;
-          const bool ok = use < 0 || wait_bar(&bars.s_full[n_sub - 1][use % kRound], (use / kRound) & 1, v);
+      auto ask_scales = [&] {
+        held1 = held2, ks1 = vs1 = 0.f;
+        if (held1) {
+          page1 = kv_page_ok(v, page2);
+          const long long at = (long long)page1 * v.heads + h;
+          ks1 = v.k_scale[at], vs1 = v.v_scale[at];
+        }
+      };
+      const char* wide = kWide ? a.wide + ((long long)(b * v.heads + h) * a.wide_tiles + begin / kTok) * (2 * C::kSlot) : nullptr;
+      ask_pages(0);
+      ask_scales();
+      ask_pages(1);
+      // the next tile's lists become the current ones, and its scales go to the softmax warps (far enough
+      // ahead of them that the entry of eight tiles ago has been read); a scale of 0 counts as one too
+      // small to matter
+      auto take = [&](int j) {
+        held0 = held1, page0 = page1, ks0 = ks1, vs0 = vs1;
+        ask_scales();
+        ask_pages(j + 2);
+        if (j == 0) {
+          const float ref = __shfl_sync(~0u, vs0, 0);
+          if (ref > 0.f) v_exp = __float_as_int(ref) >> 23 & 255;
+          if (lane == 0) bars.v_ref = exp2_int(v_exp - 127);
+        }
+        kv_scales(v, ks0, vs0);
+      };
+      auto tell = [&](int j) {
+        const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p), ks = __shfl_sync(~0u, ks0, (lane << 4) >> log_p);
+        const int d = (__float_as_int(vs) >> 23) - v_exp, e = vs != 0.f ? min(max(d, -100), 100) : -100;
+        if (vs != 0.f && d != e) kv_flag(v, KV_ST_SCALE);
+        if (lane < 8) bars.scale[j & 7][lane] = make_float2(ks, (float)e);
+        __syncwarp();
+      };
+      if constexpr (kWide) {
+        // the first keys, then values j and keys j + 1 on one barrier: both slots are free after the same products
+        constexpr int kHalf = C::kStages / 2;
+        auto copy = [&](int i, uint64_t* bar) {
+          bulk_g2s_at(ring_at + i % C::kStages * C::kSlot, wide + (long long)i * C::kSlot, C::kSlot, bar);
+        };
+        int j = -1;
+        if (n > 0) {
+          take(0);
+          tell(0);
+          if (lane == 0) mbar_expect_tx(&bars.full[0], C::kSlot), copy(0, &bars.full[0]);
+          for (j = 0; j < n; ++j) {
+            const bool next = j + 1 < n;
+            if (next) take(j + 1);
+            const int use = j - kHalf + 1;
+            const bool ok = use < 0 || wait_bar(&bars.s_full[n_sub - 1][use % kRound], (use / kRound) & 1, v);
+            if (!__all_sync(~0u, ok)) break;
+            if (next) tell(j + 1);
+            uint64_t* bar = &bars.full[1 + j % kHalf];
+            if (lane == 0) {
+              mbar_expect_tx(bar, (next ? 2 : 1) * C::kSlot);
+              copy(2 * j + 1, bar);
+              if (next) copy(2 * j + 2, bar);
+            }
+          }
+          if (j < n)  // a wait ran out: the copies under way first (with the same limit)
+            for (int k = max(0, j - kHalf); k < j; ++k) mbar_wait(&bars.full[1 + k % kHalf], (k / kHalf) & 1, kWaitLimitNs);
+        }
+      } else {
+        int i = 0;
+        for (; i < 2 * n; ++i) {
+          const int j = i >> 1, rs = i % kRaw;
+          const bool values = i & 1;
+          if (!values) take(j);
+          const bool ok = wait_bar(&bars.raw_empty[rs], ((i / kRaw) & 1) ^ 1, v);
           if (!__all_sync(~0u, ok)) break;
-          if (next) tell(j + 1);
-          uint64_t* bar = &bars.full[1 + j % kHalf];
-          if (lane == 0) {
-            mbar_expect_tx(bar, (next ? 2 : 1) * C::kSlot);
-            copy(2 * j + 1, bar);
-            if (next) copy(2 * j + 2, bar);
+          if (!values) tell(j);
+          const uint32_t held = __ballot_sync(~0u, held0);
+          if (values) {
+            const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p);
+            if (lane < 8) bars.vs[rs][lane] = vs;
+            // (a group beyond kv_hi has the scale 0 too)
+            const bool cut = __any_sync(~0u, lane < 8 && vs == 0.f) || begin + (j + 1) * kTok > kv_hi;
+            if (lane == 0) bars.cut[rs] = cut;
           }
+          __syncwarp();
+          if (lane == 0) mbar_expect_tx(&bars.raw_full[rs], (uint32_t)(__popc(held) * D) << log_p);
+          __syncwarp();
+          if (held0)
+            tma_tile(raw_at + rs * C::kRawSlot + ((lane * D) << log_p), values ? &mv : &mk, 0, h, page0, &bars.raw_full[rs]);
         }
-        if (j < n)  // a wait ran out: the copies under way first (with the same limit)
-          for (int k = max(0, j - kHalf); k < j; ++k) mbar_wait(&bars.full[1 + k % kHalf], (k / kHalf) & 1, kWaitLimitNs);
+        if (i < 2 * n)  // a wait ran out: the copies under way first (with the same limit)
+          for (int k = max(0, i - kRaw); k < i; ++k) mbar_wait(&bars.raw_full[k % kRaw], (k / kRaw) & 1, kWaitLimitNs);
       }
-    } else {
-    int i = 0;
-    for (; i < 2 * n; ++i) {
-      const int j = i >> 1, rs = i % kRaw;
-      const bool values = i & 1;
-      if (!values) take(j);
-      const bool ok = wait_bar(&bars.raw_empty[rs], ((i / kRaw) & 1) ^ 1, v);
-      if (!__all_sync(~0u, ok)) break;
-      if (!values) tell(j);
-      const uint32_t held = __ballot_sync(~0u, held0);
-      if (values) {
-        const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p);
-        if (lane < 8) bars.vs[rs][lane] = vs;
-        // (a group beyond kv_hi has the scale 0 too)
-        const bool cut = __any_sync(~0u, lane < 8 && vs == 0.f) || begin + (j + 1) * kTok > kv_hi;
-        if (lane == 0) bars.cut[rs] = cut;
-      }
-      __syncwarp();
-      if (lane == 0) mbar_expect_tx(&bars.raw_full[rs], (uint32_t)(__popc(held) * D) << log_p);
-      __syncwarp();
-      if (held0)
-        tma_tile(raw_at + rs * C::kRawSlot + ((lane * D) << log_p), values ? &mv : &mk, 0, h, page0, &bars.raw_full[rs]);
-    }
-    if (i < 2 * n)  // a wait ran out: the copies under way first (with the same limit)
-      for (int k = max(0, i - kRaw); k < i; ++k) mbar_wait(&bars.raw_full[k % kRaw], (k / kRaw) & 1, kWaitLimitNs);
-    }
     } else if (w == C::kIssuer && n > 0) {
-    // ---------------------------------------------------------------- products
-    // The whole warp walks, with values and conditions that are the same in every lane, so that
-    // addresses and descriptors stay in uniform registers: beside eight busy softmax warps every
-    // instruction between two products shows. One lane, always the same, issues.
-    const int n_u = __shfl_sync(~0u, n, 0), n_sub_u = __shfl_sync(~0u, n_sub, 0);
-    auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, wait_bar(bar, parity, v)) != 0; };
-    constexpr uint32_t kIdS = instr_desc(kTok, false), kIdO = instr_desc(D, true);
-    const uint64_t q_desc = smem_desc(q_at, 16, 1024), k_desc = smem_desc(ring_at, 16, 1024),
-                   v_desc = smem_desc(ring_at, kTok * 128, 1024);
-    auto qk = [&](int t, int slot) {
-      const uint64_t q = q_desc + (uint32_t)(t * (kTileRows * D * 2 / 16)), k = k_desc + (uint32_t)(slot * (C::kSlot / 16));
-      const uint32_t d = t * 128;
+      // ---------------------------------------------------------------- products
+      // The whole warp walks, with values and conditions that are the same in every lane, so that
+      // addresses and descriptors stay in uniform registers: beside eight busy softmax warps every
+      // instruction between two products shows. One lane, always the same, issues.
+      const int n_u = __shfl_sync(~0u, n, 0), n_sub_u = __shfl_sync(~0u, n_sub, 0);
+      auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, wait_bar(bar, parity, v)) != 0; };
+      constexpr uint32_t kIdS = instr_desc(kTok, false), kIdO = instr_desc(D, true);
+      const uint64_t q_desc = smem_desc(q_at, 16, 1024), k_desc = smem_desc(ring_at, 16, 1024),
+                     v_desc = smem_desc(ring_at, kTok * 128, 1024);
+      auto qk = [&](int t, int slot) {
+        const uint64_t q = q_desc + (uint32_t)(t * (kTileRows * D * 2 / 16)), k = k_desc + (uint32_t)(slot * (C::kSlot / 16));
+        const uint32_t d = t * 128;
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i)
-        mma_ss(d, q + ((i >> 2) * (kTileRows * 8) + (i & 3) * 2), k + ((i >> 2) * (kTok * 8) + (i & 3) * 2), kIdS, i > 0);
-    };
-    auto pv = [&](int t, int slot, int half, bool add) {
-      const uint64_t vv = v_desc + (uint32_t)(slot * (C::kSlot / 16));
-      const uint32_t d = 256 + t * 128, p = t * 128;
+        for (int i = 0; i < D / 16; ++i)
+          mma_ss(d, q + ((i >> 2) * (kTileRows * 8) + (i & 3) * 2), k + ((i >> 2) * (kTok * 8) + (i & 3) * 2), kIdS, i > 0);
+      };
+      auto pv = [&](int t, int slot, int half, bool add) {
+        const uint64_t vv = v_desc + (uint32_t)(slot * (C::kSlot / 16));
+        const uint32_t d = 256 + t * 128, p = t * 128;
 #pragma unroll
-      for (int i = 0; i < kTok / 32; ++i)
-        mma_ts(d, p + (half * (kTok / 32) + i) * 8, vv + (half * (kTok / 32) + i) * 128, kIdO, add || half || i > 0);
-    };
-    const bool one = elect_one();
-    bool ok = wait_all(&bars.full[0], 0);
-    fence_after();
-    if (ok && one) {
-      for (int t = 0; t < n_sub_u; ++t) {
-        qk(t, 0);
-        commit(&bars.s_full[t][0]);
-      }
-    }
-    int vs = 1, ks = 2;
-    uint32_t v_par = 0, k_par = 0;  // parities of the slots' rounds
-    for (int j = 0; ok && j < n_u; ++j) {
-      ok = kWide ? wait_all(&bars.full[1 + j % (C::kStages / 2)], (j / (C::kStages / 2)) & 1) : wait_all(&bars.full[vs], v_par);
-      for (int t = 0; ok && t < n_sub_u; ++t) {
-        for (int half = 0; ok && half < 2; ++half) {
-          ok = wait_all(&bars.p_full[t][half], j & 1);
-          fence_after();
-          if (ok && one) pv(t, vs, half, j > 0);
+        for (int i = 0; i < kTok / 32; ++i)
+          mma_ts(d, p + (half * (kTok / 32) + i) * 8, vv + (half * (kTok / 32) + i) * 128, kIdO, add || half || i > 0);
+      };
+      const bool one = elect_one();
+      bool ok = wait_all(&bars.full[0], 0);
+      fence_after();
+      if (ok && one) {
+        for (int t = 0; t < n_sub_u; ++t) {
+          qk(t, 0);
+          commit(&bars.s_full[t][0]);
         }
-        if (!ok) break;
-        if (one && j + 1 == n_u) commit(&bars.pv_done[t]);
-        if (j + 1 < n_u) {
-          if (!kWide && t == 0) ok = wait_all(&bars.full[ks], k_par);
+      }
+      int vs = 1, ks = 2;
+      uint32_t v_par = 0, k_par = 0;  // parities of the slots' rounds
+      for (int j = 0; ok && j < n_u; ++j) {
+        ok = kWide ? wait_all(&bars.full[1 + j % (C::kStages / 2)], (j / (C::kStages / 2)) & 1) : wait_all(&bars.full[vs], v_par);
+        for (int t = 0; ok && t < n_sub_u; ++t) {
+          for (int half = 0; ok && half < 2; ++half) {
+            ok = wait_all(&bars.p_full[t][half], j & 1);
+            fence_after();
+            if (ok && one) pv(t, vs, half, j > 0);
+          }
           if (!ok) break;
-          if (!kWide) fence_after();
-          if (one) {
-            qk(t, ks);
-            commit(&bars.s_full[t][(j + 1) % kRound]);
+          if (one && j + 1 == n_u) commit(&bars.pv_done[t]);
+          if (j + 1 < n_u) {
+            if (!kWide && t == 0) ok = wait_all(&bars.full[ks], k_par);
+            if (!ok) break;
+            if (!kWide) fence_after();
+            if (one) {
+              qk(t, ks);
+              commit(&bars.s_full[t][(j + 1) % kRound]);
+            }
           }
         }
+        vs += 2;
+        if (vs >= C::kStages) vs -= C::kStages, v_par ^= 1;
+        ks += 2;
+        if (ks >= C::kStages) ks -= C::kStages, k_par ^= 1;
       }
-      vs += 2;
-      if (vs >= C::kStages) vs -= C::kStages, v_par ^= 1;
-      ks += 2;
-      if (ks >= C::kStages) ks -= C::kStages, k_par ^= 1;
+      // nothing of this block's is under way once this has arrived
+      if (one) commit(&bars.end);
+      wait_bar(&bars.end, 0, v);
     }
-    // nothing of this block's is under way once this has arrived
-    if (one) commit(&bars.end);
-    wait_bar(&bars.end, 0, v);
-  }
   }
   __syncwarp();
   fence_before();
