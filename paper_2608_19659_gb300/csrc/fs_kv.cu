@@ -717,14 +717,19 @@ struct KvPlan {
   int row_tile, row_blocks, split, splits, cluster, tickets;
   int chunk_tiles;  // blocks of k_kv_chunk a (sequence, key head); 0: no sequence has that many rows
   int chunk_split, chunk_parts;
+  int few;          // sequences with more rows than this go to k_kv_chunk
   int wide_tiles;   // tiles of a sequence that k_kv_expand writes; 0: the walks convert for themselves
   int decode;       // whether some sequence can have few rows
   size_t part_floats, chunk_floats, wide_bytes;
 };
 
-// Sequences with more rows (new tokens x query heads of a key head) than this go to
-// k_kv_chunk.
-constexpr int kFewRows = 64;
+// Sequences with more rows (new tokens x query heads of a key head) than kFewRows go to k_kv_chunk.
+// With heads of 128, where k_kv_decode needs three passes over the codes (more than kMidRows) and
+// k_kv_chunk's blocks fill at least half of the SMs, they go there too: 40 rows over 5 sequences of up to 40000
+// tokens 106 -> 64 us, 64 rows over 48 of up to 6000 120 -> 84, 48 rows under a window of 4096 37 -> 24 (40
+// rows: 25 either way). With 32 rows it is 55 against 68, with heads of 64 54 against 62, with one long
+// sequence (16 blocks) 33 against 46.
+constexpr int kMidRows = 32, kFewRows = 64;
 
 // Where at least kWideFrom blocks can walk over a sequence's tokens, and the batch's tokens as
 // halves take no more than kWideBytes, they are converted once.
@@ -743,8 +748,26 @@ constexpr int kMinSplit = 128, kMaxSplit = 4096;
 KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int window, int sms) {
   KvPlan p{};
   const long long all = (long long)std::max(1, b->max_new) * (q_heads / c->heads);
-  const int rows = (int)std::min<long long>(all, kFewRows);
-  p.chunk_tiles = all > kFewRows ? (int)((all + kKvChunkRows - 1) / kKvChunkRows) : 0;
+  p.few = kFewRows;
+  if (all > kMidRows) {
+    // parts of at least four tiles of 128 tokens where whole walks leave half of the SMs without a block
+    // (more parts for balance alone cost more than they give: ragged chunks 105 us whole, 220 us in twos)
+    p.chunk_tiles = (int)((all + kKvChunkRows - 1) / kKvChunkRows);
+    const long long blocks = std::max(1, b->batch) * (long long)c->heads * p.chunk_tiles;
+    const int walk = (std::max(1, window ? (int)std::min<long long>(b->max_length, (long long)window + kKvChunkRows + 126) : b->max_length) + 127) / 128;
+    const long long want = std::max(1ll, std::min({sms / blocks, (long long)walk / 4, (long long)kKvFan}));
+    const int tiles = (int)((walk + want - 1) / want);
+    p.chunk_split = tiles * 128;
+    p.chunk_parts = (walk + tiles - 1) / tiles;
+    if (c->dim == 128 && 2 * blocks * p.chunk_parts >= sms) p.few = kMidRows;
+    if (all <= p.few) p.chunk_tiles = 0;
+  }
+  if (p.chunk_tiles) {
+    wide_of(c, b, p.chunk_tiles, &p.wide_tiles, &p.wide_bytes);
+    if (p.chunk_parts > 1) p.wide_tiles = 0, p.wide_bytes = 0;
+    p.chunk_floats = p.chunk_parts > 1 ? (size_t)b->batch * c->heads * p.chunk_tiles * p.chunk_parts * kKvChunkRows * (c->dim + 4) : 0;
+  }
+  const int rows = (int)std::min<long long>(all, p.few);
   // (every sequence has max_new new tokens: all have the same rows)
   p.decode = !p.chunk_tiles || (long long)b->batch * b->max_new != b->tokens;
   p.row_tile = rows <= 8 ? 8 : 16;
@@ -772,20 +795,6 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
     const int groups = (p.splits / p.cluster + kKvFan - 1) / kKvFan;
     if (groups > 1 && items * (1 + groups) <= kKvTickets) p.tickets = 1 + groups;
   }
-  if (p.chunk_tiles) {
-    // parts of at least four tiles of 128 tokens where whole walks leave half of the SMs without a block
-    // (more parts for balance alone cost more than they give: ragged chunks 105 us whole, 220 us in twos)
-    const long long blocks = (long long)b->batch * c->heads * p.chunk_tiles;
-    const int walk = (std::max(1, window ? (int)std::min<long long>(b->max_length, (long long)window + kKvChunkRows + 126) : b->max_length) + 127) / 128;
-    long long want = sms / blocks;
-    want = std::max(1ll, std::min({want, (long long)walk / 4, (long long)kKvFan}));
-    const int tiles = (int)((walk + want - 1) / want);
-    p.chunk_split = tiles * 128;
-    p.chunk_parts = (walk + tiles - 1) / tiles;
-    wide_of(c, b, p.chunk_tiles, &p.wide_tiles, &p.wide_bytes);
-    if (p.chunk_parts > 1) p.wide_tiles = 0, p.wide_bytes = 0;
-    p.chunk_floats = p.chunk_parts > 1 ? (size_t)blocks * p.chunk_parts * kKvChunkRows * (c->dim + 4) : 0;
-  }
   p.part_floats = p.decode && p.splits > 1 ? (size_t)items * p.splits * p.row_tile * (c->dim + 2) : 0;
   return p;
 }
@@ -800,7 +809,7 @@ size_t part_floats_bound(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads
   const long long decode = std::max(18ll * sms + (1 + kKvCluster) * items, items * ((len + kMaxSplit - 1) / kMaxSplit)) * 16 * (c->dim + 2);
   // chunks: at most sms parts in all
   const long long all = (long long)std::max(1, b->max_new) * (q_heads / c->heads);
-  const long long blocks = all > kFewRows ? std::max(1, b->batch) * (long long)c->heads * ((all + kKvChunkRows - 1) / kKvChunkRows) : 0;
+  const long long blocks = all > kMidRows ? std::max(1, b->batch) * (long long)c->heads * ((all + kKvChunkRows - 1) / kKvChunkRows) : 0;
   // the tokens as halves: a smaller batch may have them where a larger one's are too many
   const long long tokens = ((len + 127) / 128) * std::max(1, b->batch) * c->heads * (2ll * 128 * c->dim * 2);
   return (size_t)(decode + std::min((long long)sms, kKvFan * blocks) * kKvChunkRows * (c->dim + 4) +
@@ -940,7 +949,7 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   CUtensorMap mk, mv;
   if (p.chunk_tiles) {
     KvAttendArgs ca = a;
-    ca.min_rows = kFewRows, ca.max_rows = INT_MAX;
+    ca.min_rows = p.few, ca.max_rows = INT_MAX;
     ca.split = p.chunk_split;
     ca.part = a.part + p.part_floats;
     ca.wide_tiles = p.wide_tiles;
@@ -952,7 +961,7 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
     if (e != cudaSuccess) return cuda_say(e, "launch (fs_kv_attend, chunks)");
   }
   if (p.decode) {
-    a.min_rows = 0, a.max_rows = kFewRows;
+    a.min_rows = 0, a.max_rows = p.few;
     const int box = std::min(32, cache->page_tokens);
     if (int rc = kv_tensor_map(&mk, *cache, cache->k, box, true)) return rc;
     if (int rc = kv_tensor_map(&mv, *cache, cache->v, box, true)) return rc;

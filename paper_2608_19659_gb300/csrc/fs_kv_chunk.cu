@@ -18,19 +18,24 @@
 //             is computed (471 -> 465 us, see below). Two threads a row: 544 us, the 16 warps
 //             crowd out the one that issues products
 //   8-11      (only where the walk converts) codes to halves, from the tiles as they came to
-//             swizzled ones
+//             swizzled ones; two warps for the keys, two for the values
 //   then one  issues every product. While tile 0's rows are in softmax the tensor cores work on
 //             tile 1, and the other way round. Two such warps, one a tile: 506-525 us, their
 //             products mix and neither chain is short
 //   and one   keeps tiles on their way: bulk copies of 32 KB halves, or tensor-map copies of the
-//             codes, a page each at most
+//             codes, a page each at most: of the keys, and one more warp of the values (one for both
+//             took 2900 clocks a tile beside the other warps, longer than anything else)
+//
+// Where the rows end in the first tile, the second's warps and tensor memory take every second tile of
+// the cache for the same rows, and both results are joined at the end (with the warps for keys and values:
+// 64 rows over 48 sequences of up to 6000 tokens 96 -> 80 us).
 //
 // Bound by the tensor cores, 4 dim operations per (row, token), and by how fast one thread beside
 // eight busy softmax warps can issue their products and waits (a commit costs it about 200 clocks,
-// hence three of them a pair of tiles: 477 -> 458 us). A prompt of 8192 tokens, 32 query heads over 4
-// key heads of 128: 411 us with the conversion (10 us), 1.34 PFLOP/s of causal work, tensor cores
-// active 61 % of the time; 69 % of the bf16 rate that a library product reaches. The steps in
-// brackets are of the same prompt, when they were taken.
+// so a slot is refilled after the S that follows its products and there are only the two of S a pair
+// of tiles: 477 -> 458 us with three, 411 -> 407 with two). A prompt of 8192 tokens, 32 query heads over 4
+// key heads of 128: 404 us with the conversion (10 us), 1.36 PFLOP/s of causal work; 70 % of the bf16 rate
+// that a library product reaches. The steps in brackets are of the same prompt, when they were taken.
 #include "fs_kv.cuh"
 
 namespace fs {
@@ -47,7 +52,7 @@ struct Cfg {
   static constexpr int kRaw = kWide ? 0 : D == 128 ? 2 : 4;  // tiles of codes
   static constexpr int kSlot = kTok * D * 2, kRawSlot = kTok * D;
   static constexpr int kQ = 2 * kTileRows * D * 2;
-  static constexpr size_t kSmem = 1024 + kQ + (size_t)kStages * kSlot + kRaw * kRawSlot + 1280;
+  static constexpr size_t kSmem = 1024 + kQ + (size_t)kStages * kSlot + kRaw * kRawSlot + 1792;
 };
 
 // S of tile j of the cache is told on barrier j mod kRound. (Whoever refills a slot waits for the S
@@ -58,14 +63,20 @@ struct Bars {
   uint64_t full[8], raw_full[4], raw_empty[4], s_full[2][kRound], p_full[2][2], pv_done[2], end;
   float vs[4][8];        // per tile of codes and 16 tokens: the values' scale
   uint32_t cut[4];       // per tile of codes: some tokens' values are to be 0
-  float2 scale[8][8];    // per tile (mod 8) and 16 tokens: the keys' scale, log2 of the values' over the first page's
+  float2 scale[16][8];   // per tile (mod 16) and 16 tokens: the keys' scale, log2 of the values' over the first page's
   float v_ref;
   uint32_t tmem;
 };
-static_assert(sizeof(Bars) <= 1280, "the barriers' share of shared memory");
+static_assert(sizeof(Bars) <= 1792, "the barriers' share of shared memory");
 
 __device__ __forceinline__ void st_shared16(uint32_t a, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+__device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
 }
 
 __device__ __forceinline__ float2 ld_shared8(uint32_t a) {
@@ -247,10 +258,17 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
   if (part >= n_parts) return;
   const int begin = walk.begin + part * a.split, kv_hi = min(begin + a.split, walk.end);  // this block's part
   const int n = (kv_hi - begin + kTok - 1) / kTok;  // tiles of the cache; 0: no row sees a token
+  // With one tile of rows, each half of the block (softmax warps, S, O) takes every second tile of the
+  // cache, and the halves' results are joined at the end.
+  const bool two = !kWide && n_sub == 1 && n > 1;
+  const int n_act = two ? 2 : n_sub;
+  // (where the second tile's queries would be are then two more tiles of codes)
+  const int n_raw = D == 128 && two ? 4 : C::kRaw;
+  auto raw_slot = [&](int rs) { return rs < C::kRaw ? raw_at + rs * C::kRawSlot : q_at + kTileRows * D * 2 + (rs - C::kRaw) * C::kRawSlot; };
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < C::kStages; ++i) mbar_init(&bars.full[i], kWide ? 1 : 128);
-    for (int i = 0; i < C::kRaw; ++i) mbar_init(&bars.raw_full[i], 1), mbar_init(&bars.raw_empty[i], 128);
+    for (int i = 0; i < C::kStages; ++i) mbar_init(&bars.full[i], kWide ? 1 : 64);
+    for (int i = 0; i < n_raw; ++i) mbar_init(&bars.raw_full[i], 1), mbar_init(&bars.raw_empty[i], 64);
     for (int t = 0; t < 2; ++t) {
       for (int i = 0; i < kRound; ++i) mbar_init(&bars.s_full[t][i], 1);
       mbar_init(&bars.p_full[t][0], 128), mbar_init(&bars.p_full[t][1], 128), mbar_init(&bars.pv_done[t], 1);
@@ -267,7 +285,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
   // queries: a row a thread, scaled into [-2, 2] by a power of two (and by the scale's sign)
   int q_exp = 0;
   if (w < 8) {
-    const int r = r0 + threadIdx.x;
+    const int r = r0 + (two ? threadIdx.x & 127 : threadIdx.x);
     const uint4* q = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (long long)(s.first + r / v.group) * a.q_token +
                                                     (h * v.group + r % v.group) * a.q_head);
     float amax = 0.f;
@@ -285,7 +303,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
     const int t = threadIdx.x >> 7, rr = threadIdx.x & 127;
     const uint32_t row = q_at + t * (kTileRows * D * 2) + rr * 128;
 #pragma unroll 4
-    for (int i = 0; i < D / 8; ++i) {
+    for (int i = 0; i < (two && t ? 0 : D / 8); ++i) {
       uint4 u = make_uint4(0, 0, 0, 0);
       if (r < r_end) u = q[i];
       uint32_t y[4] = {u.x, u.y, u.z, u.w};
@@ -314,20 +332,20 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
     // ---------------------------------------------------------------- softmax
     asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
     const int t = w >> 2;
-    const int r = r0 + threadIdx.x;
-    if (t < n_sub) {
+    const int r = r0 + (two ? threadIdx.x & 127 : threadIdx.x);
+    if (t < n_act) {
       const uint32_t lanes = (uint32_t)(w & 3) << 21;  // 32 lanes a warp, in bits 16 and up
       const uint32_t s_at = tmem + lanes + t * 128, o_at = tmem + lanes + 256 + t * 128;
       const float c = fabsf(a.scale_log2) * exp2_int(q_exp);
       const int pos = base + r / v.group;
       const int hi = r < r_end ? pos : -1, lo = a.window ? pos - a.window + 1 : 0;
       // tiles inside [all_lo, all_hi) are seen whole by every row of this tile
-      const int t_r0 = r0 + t * kTileRows, t_r1 = min(r_end, t_r0 + kTileRows) - 1;
+      const int t_r0 = two ? r0 : r0 + t * kTileRows, t_r1 = min(r_end, t_r0 + kTileRows) - 1;
       const int all_hi = base + t_r0 / v.group + 1, all_lo = a.window ? base + t_r1 / v.group - a.window + 1 : 0;
       float m = -INFINITY, l = 0.f;
       bool ok = true;
-      int j = 0;
-      for (; j < n; ++j) {
+      const int first = two ? t : 0, step = two ? 2 : 1;
+      for (int j = first; j < n; j += step) {
         const int t0 = begin + j * kTok;
         const bool whole = t0 >= all_lo && t0 + kTok <= all_hi;
         const int c_hi = hi - t0, c_lo = lo - t0;  // columns [c_lo, c_hi] count
@@ -338,14 +356,14 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
 #pragma unroll
         for (int k = 0; k < 4; ++k) tmem_ld32(reinterpret_cast<uint32_t(&)[32]>(x[32 * k]), s_at + 32 * k);
         wait_ld();
-        const float2* scale = bars.scale[j & 7];
+        const float2* scale = bars.scale[j & 15];
         const float top = whole ? row_top<true>(x, c, scale, 0, 0) : row_top<false>(x, c, scale, c_lo, c_hi);
         const bool grow = top > m + 8.f || (m == -INFINITY && top > m);
         if (__any_sync(~0u, grow)) {
           const float f = grow ? ex2(m - top) : 1.f;
           if (grow) m = top;
           l *= f;
-          if (j > 0) {  // (the first product overwrites O; those before this S have ended with it)
+          if (j > first) {  // (the first product overwrites O; those before this S have ended with it)
 #pragma unroll 1
             for (int k = 0; k < D / 16; ++k) {
               uint32_t y[16];
@@ -391,16 +409,54 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
         fence_after();
       }
       ok = __all_sync(~0u, ok);
+      // the halves' results: the second's through shared memory (the tiles' slots, which nothing uses
+      // once both halves' products have ended)
+      float f0 = 1.f, f1 = 0.f;
+      const uint32_t mine = ring_at + (threadIdx.x & 127) * ((D + 4) * 4);
+      if (two) {
+        asm volatile("bar.sync 2, 256;" ::: "memory");
+        if (t == 1) {
+#pragma unroll 1
+          for (int k = 0; k < D / 16; ++k) {
+            uint32_t x[16];
+            tmem_ld16(x, o_at + 16 * k);
+            wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) st_shared16(mine + (16 * k + i) * 4, make_uint4(x[i], x[i + 1], x[i + 2], x[i + 3]));
+          }
+          st_shared16(mine + D * 4, make_uint4(__float_as_uint(m), __float_as_uint(l), ok, 0));
+        }
+        asm volatile("bar.sync 2, 256;" ::: "memory");
+        if (t == 0) {
+          const uint4 other = ld_shared16(mine + D * 4);
+          const float m1 = __uint_as_float(other.x), top = fmaxf(m, m1), off = top == -INFINITY ? 0.f : top;
+          f0 = ex2(m - off), f1 = ex2(m1 - off);
+          m = top, l = fmaf(__uint_as_float(other.y), f1, l * f0);
+          ok = __all_sync(~0u, ok && other.z);
+        }
+      }
+      auto result = [&](uint32_t(&x)[32], int k) {
+        tmem_ld32(x, o_at + 32 * k);
+        wait_ld();
+        if (two) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const uint4 y = ld_shared16(mine + (32 * k + i) * 4);
+            const uint32_t ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[i + u] = __float_as_uint(fmaf(__uint_as_float(ys[u]), f1, __uint_as_float(x[i + u]) * f0));
+          }
+        }
+      };
       const float up = bars.v_ref * (1.f / 128.f), inv = up / l;
-      if (n_parts == 1) {
+      if (two && t == 1) {
+        // (its result is the first half's)
+      } else if (n_parts == 1) {
         T* to = static_cast<T*>(a.out) + (long long)(s.first + r / v.group) * a.out_token + (h * v.group + r % v.group) * a.out_head;
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
           uint32_t x[32];
-          if (n > 0) {
-            tmem_ld32(x, o_at + 32 * k);
-            wait_ld();
-          }
+          if (n > 0) result(x, k);
           if (ok && r < r_end) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -417,8 +473,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
           uint32_t x[32];
-          tmem_ld32(x, o_at + 32 * k);
-          wait_ld();
+          result(x, k);
           if (r < r_end) {
 #pragma unroll
             for (int i = 0; i < 32; i += 4)
@@ -432,64 +487,77 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
   } else if (!kWide && w < 12) {
     // ---------------------------------------------------------------- codes to halves
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    // Two warps for the keys, two for the values: while one pair waits for its tile the other converts.
     constexpr int kLanes = D / 16;               // lanes a token, 16 codes each
-    constexpr int kPer = 128 / kLanes;           // tokens a pass
-    constexpr int kPasses = kTok / kPer;         // 8 (dim 128) or 4 (dim 64)
-    constexpr int kRaw = C::kRaw > 0 ? C::kRaw : 1;
-    const int id = threadIdx.x - 256, cl = id % kLanes, tk = id / kLanes;
+    constexpr int kPer = 64 / kLanes;            // tokens a pass
+    constexpr int kPasses = 8, kBatches = kTok / kPer / kPasses;  // (2 of 8 passes with dim 128)
+    const bool values = w >= 10;
+    const int id = threadIdx.x & 63, cl = id % kLanes, tk = id / kLanes;
     // A lane's 16 codes become the 16-byte chunks 2 (cl mod 4) and + 1 of the token's row in block
     // cl / 4; lanes of the second block begin with the other one, so that a row's lanes meet every
     // bank once.
     const int sw = D == 128 ? cl >> 2 : 0;
-    const uint32_t from = raw_at + tk * D + cl * 16, to = (cl >> 2) * (kTok * 128) + tk * 128;
+    const uint32_t from = tk * D + cl * 16, to = (cl >> 2) * (kTok * 128) + tk * 128;
     const uint32_t c0 = (((cl & 3) * 2 + sw) ^ (tk & 7)) << 4, c1 = (((cl & 3) * 2 + (sw ^ 1)) ^ (tk & 7)) << 4;
-    for (int i = 0; i < 2 * n; ++i) {
-      const int st = i % C::kStages, rs = i % kRaw;
-      if (!wait_bar(&bars.raw_full[rs], (i / kRaw) & 1, v)) break;
-      uint32_t x[kPasses][4];
-      const bool values = i & 1;
+    int rs = values, st = values;
+    uint32_t rs_par = 0;
+    for (int j = 0; j < n; ++j) {
+      bool ok = wait_bar(&bars.raw_full[rs], rs_par, v);
+      if (!ok) break;
+      const bool cut = values && bars.cut[rs];
+      const uint32_t slot = raw_slot(rs) + from, row = ring_at + st * C::kSlot + to;
 #pragma unroll
-      for (int p = 0; p < kPasses; ++p) {
-        const uint32_t at = from + rs * C::kRawSlot + p * (kPer * D);
-        const float2 u = ld_shared8(at + 8 * sw), z = ld_shared8(at + 8 * (sw ^ 1));
-        x[p][0] = __float_as_uint(u.x), x[p][1] = __float_as_uint(u.y);
-        x[p][2] = __float_as_uint(z.x), x[p][3] = __float_as_uint(z.y);
-      }
-      if (values && bars.cut[rs]) {
-        // tokens that no row sees (their slots may hold NaN codes), and values whose scale is 0
+      for (int q = 0; q < kBatches; ++q) {
+        uint32_t x[kPasses][4];
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
-          const int tl = p * kPer + tk;
-          if (begin + (i >> 1) * kTok + tl >= kv_hi || bars.vs[rs][tl >> 4] == 0.f) x[p][0] = x[p][1] = x[p][2] = x[p][3] = 0;
+          const uint32_t at = slot + (q * kPasses + p) * (kPer * D);
+          const float2 u = ld_shared8(at + 8 * sw), z = ld_shared8(at + 8 * (sw ^ 1));
+          x[p][0] = __float_as_uint(u.x), x[p][1] = __float_as_uint(u.y);
+          x[p][2] = __float_as_uint(z.x), x[p][3] = __float_as_uint(z.y);
+        }
+        if (cut) {
+          // tokens that no row sees (their slots may hold NaN codes), and values whose scale is 0
+#pragma unroll
+          for (int p = 0; p < kPasses; ++p) {
+            const int tl = (q * kPasses + p) * kPer + tk;
+            if (begin + j * kTok + tl >= kv_hi || bars.vs[rs][tl >> 4] == 0.f) x[p][0] = x[p][1] = x[p][2] = x[p][3] = 0;
+          }
+        }
+        if (q == kBatches - 1) mbar_arrive(&bars.raw_empty[rs]);
+        // the slot's last tile, kStages / 2 of the cache's tiles ago (the last S of tile j follows the
+        // products over its keys and over the values of the tile before: of its half, where the halves
+        // take tiles in turn)
+        const int use = j - C::kStages / 2 + (values ? (two ? 2 : 1) : 0);
+        if (q == 0 && j >= C::kStages / 2) ok = wait_bar(&bars.s_full[two ? use & 1 : n_sub - 1][use % kRound], (use / kRound) & 1, v);
+        if (!ok) break;
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+          uint32_t y[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) y[2 * k] = e4m3x2_to_f16x2(x[p][k]), y[2 * k + 1] = e4m3x2_to_f16x2_hi(x[p][k]);
+          const uint32_t at = row + (q * kPasses + p) * (kPer * 128);
+          st_shared16(at + c0, make_uint4(y[0], y[1], y[2], y[3]));
+          st_shared16(at + c1, make_uint4(y[4], y[5], y[6], y[7]));
         }
       }
-      mbar_arrive(&bars.raw_empty[rs]);
-      // the slot's last tile, kStages / 2 of the cache's tiles ago (the last S of tile j follows the
-      // products over its keys and over the values of the tile before)
-      const int use = (i >> 1) - C::kStages / 2 + (values ? 1 : 0);
-      if ((i >> 1) >= C::kStages / 2 && !wait_bar(&bars.s_full[n_sub - 1][use % kRound], (use / kRound) & 1, v)) break;
-      const uint32_t row = ring_at + st * C::kSlot + to;
-#pragma unroll
-      for (int p = 0; p < kPasses; ++p) {
-        uint32_t y[8];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) y[2 * k] = e4m3x2_to_f16x2(x[p][k]), y[2 * k + 1] = e4m3x2_to_f16x2_hi(x[p][k]);
-        st_shared16(row + p * (kPer * 128) + c0, make_uint4(y[0], y[1], y[2], y[3]));
-        st_shared16(row + p * (kPer * 128) + c1, make_uint4(y[4], y[5], y[6], y[7]));
-      }
+      if (!ok) break;
       fence_proxy_async();
       mbar_arrive(&bars.full[st]);
+      rs += 2, st += 2;
+      if (rs >= n_raw) rs -= n_raw, rs_par ^= 1;
+      if (st >= C::kStages) st -= C::kStages;
     }
   } else {
     if (kWide)
       asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
     else
       asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    if (w == C::kIssuer + 1) {
+    if (w == C::kIssuer + 1 || (!kWide && w == C::kIssuer + 2)) {
       // ---------------------------------------------------------------- tiles from the cache
       // Lane g holds the page of a tile's g-th box of a page's tokens. Page ids are asked for two tiles
       // ahead and their scales one, so that no copy waits for either.
-      constexpr int kRaw = C::kRaw > 0 ? C::kRaw : 1;
+      const bool values = !kWide && w == C::kIssuer + 2;  // (codes: a warp for the keys, one for the values)
       const int log_p = v.log_page, boxes = kTok >> log_p;
       int v_exp = 127;  // exponent of the scale that those of values are relative to: the first page's
       int page0 = 0, page1 = 0, page2 = 0;
@@ -513,7 +581,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
       ask_scales();
       ask_pages(1);
       // the next tile's lists become the current ones, and its scales go to the softmax warps (far enough
-      // ahead of them that the entry of eight tiles ago has been read); a scale of 0 counts as one too
+      // ahead of them that the entry of sixteen tiles ago has been read); a scale of 0 counts as one too
       // small to matter
       auto take = [&](int j) {
         held0 = held1, page0 = page1, ks0 = ks1, vs0 = vs1;
@@ -522,7 +590,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
         if (j == 0) {
           const float ref = __shfl_sync(~0u, vs0, 0);
           if (ref > 0.f) v_exp = __float_as_int(ref) >> 23 & 255;
-          if (lane == 0) bars.v_ref = exp2_int(v_exp - 127);
+          if (lane == 0 && !values) bars.v_ref = exp2_int(v_exp - 127);
         }
         kv_scales(v, ks0, vs0);
       };
@@ -530,7 +598,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
         const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p), ks = __shfl_sync(~0u, ks0, (lane << 4) >> log_p);
         const int d = (__float_as_int(vs) >> 23) - v_exp, e = vs != 0.f ? min(max(d, -100), 100) : -100;
         if (vs != 0.f && d != e) kv_flag(v, KV_ST_SCALE);
-        if (lane < 8) bars.scale[j & 7][lane] = make_float2(ks, (float)e);
+        if (lane < 8) bars.scale[j & 15][lane] = make_float2(ks, (float)e);
         __syncwarp();
       };
       if constexpr (kWide) {
@@ -562,14 +630,12 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
             for (int k = max(0, j - kHalf); k < j; ++k) mbar_wait(&bars.full[1 + k % kHalf], (k / kHalf) & 1, kWaitLimitNs);
         }
       } else {
-        int i = 0;
-        for (; i < 2 * n; ++i) {
-          const int j = i >> 1, rs = i % kRaw;
-          const bool values = i & 1;
-          if (!values) take(j);
-          const bool ok = wait_bar(&bars.raw_empty[rs], ((i / kRaw) & 1) ^ 1, v);
+        int j = 0, rs = values;
+        uint32_t rs_par = 1;
+        for (; j < n; ++j) {
+          take(j);
+          const bool ok = wait_bar(&bars.raw_empty[rs], rs_par, v);
           if (!__all_sync(~0u, ok)) break;
-          if (!values) tell(j);
           const uint32_t held = __ballot_sync(~0u, held0);
           if (values) {
             const float vs = __shfl_sync(~0u, vs0, (lane << 4) >> log_p);
@@ -577,15 +643,20 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
             // (a group beyond kv_hi has the scale 0 too)
             const bool cut = __any_sync(~0u, lane < 8 && vs == 0.f) || begin + (j + 1) * kTok > kv_hi;
             if (lane == 0) bars.cut[rs] = cut;
+            __syncwarp();
+          } else {
+            tell(j);
           }
-          __syncwarp();
           if (lane == 0) mbar_expect_tx(&bars.raw_full[rs], (uint32_t)(__popc(held) * D) << log_p);
           __syncwarp();
           if (held0)
-            tma_tile(raw_at + rs * C::kRawSlot + ((lane * D) << log_p), values ? &mv : &mk, 0, h, page0, &bars.raw_full[rs]);
+            tma_tile(raw_slot(rs) + ((lane * D) << log_p), values ? &mv : &mk, 0, h, page0, &bars.raw_full[rs]);
+          rs += 2;
+          if (rs >= n_raw) rs -= n_raw, rs_par ^= 1;
         }
-        if (i < 2 * n)  // a wait ran out: the copies under way first (with the same limit)
-          for (int k = max(0, i - kRaw); k < i; ++k) mbar_wait(&bars.raw_full[k % kRaw], (k / kRaw) & 1, kWaitLimitNs);
+        if (j < n)  // a wait ran out: the copies under way first (with the same limit)
+          for (int k = max(0, j - n_raw / 2); k < j; ++k)
+            mbar_wait(&bars.raw_full[2 * k % n_raw + values], (2 * k / n_raw) & 1, kWaitLimitNs);
       }
     } else if (w == C::kIssuer && n > 0) {
       // ---------------------------------------------------------------- products
@@ -593,12 +664,14 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
       // addresses and descriptors stay in uniform registers: beside eight busy softmax warps every
       // instruction between two products shows. One lane, always the same, issues.
       const int n_u = __shfl_sync(~0u, n, 0), n_sub_u = __shfl_sync(~0u, n_sub, 0);
+      const bool two_u = !kWide && __shfl_sync(~0u, two, 0);
+      const int step = two_u ? 2 : 1;  // from a half's tile to its next
       auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, wait_bar(bar, parity, v)) != 0; };
       constexpr uint32_t kIdS = instr_desc(kTok, false), kIdO = instr_desc(D, true);
       const uint64_t q_desc = smem_desc(q_at, 16, 1024), k_desc = smem_desc(ring_at, 16, 1024),
                      v_desc = smem_desc(ring_at, kTok * 128, 1024);
       auto qk = [&](int t, int slot) {
-        const uint64_t q = q_desc + (uint32_t)(t * (kTileRows * D * 2 / 16)), k = k_desc + (uint32_t)(slot * (C::kSlot / 16));
+        const uint64_t q = q_desc + (uint32_t)((two_u ? 0 : t) * (kTileRows * D * 2 / 16)), k = k_desc + (uint32_t)(slot * (C::kSlot / 16));
         const uint32_t d = t * 128;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
@@ -620,25 +693,34 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
           commit(&bars.s_full[t][0]);
         }
       }
-      int vs = 1, ks = 2;
-      uint32_t v_par = 0, k_par = 0;  // parities of the slots' rounds
+      if (two_u) {
+        ok = ok && wait_all(&bars.full[2], 0);
+        fence_after();
+        if (ok && one) {
+          qk(1, 2);
+          commit(&bars.s_full[1][1]);
+        }
+      }
+      int vs = 1, ks = 2 * step % C::kStages;
+      uint32_t v_par = 0, k_par = 2 * step / C::kStages;  // parities of the slots' rounds
       for (int j = 0; ok && j < n_u; ++j) {
         ok = kWide ? wait_all(&bars.full[1 + j % (C::kStages / 2)], (j / (C::kStages / 2)) & 1) : wait_all(&bars.full[vs], v_par);
-        for (int t = 0; ok && t < n_sub_u; ++t) {
+        const int t_0 = two_u ? j & 1 : 0, t_n = two_u ? t_0 + 1 : n_sub_u;
+        for (int t = t_0; ok && t < t_n; ++t) {
           for (int half = 0; ok && half < 2; ++half) {
-            ok = wait_all(&bars.p_full[t][half], j & 1);
+            ok = wait_all(&bars.p_full[t][half], (two_u ? j >> 1 : j) & 1);
             fence_after();
-            if (ok && one) pv(t, vs, half, j > 0);
+            if (ok && one) pv(t, vs, half, j >= step);
           }
           if (!ok) break;
-          if (one && j + 1 == n_u) commit(&bars.pv_done[t]);
-          if (j + 1 < n_u) {
-            if (!kWide && t == 0) ok = wait_all(&bars.full[ks], k_par);
+          if (one && j + step >= n_u) commit(&bars.pv_done[t]);
+          if (j + step < n_u) {
+            if (!kWide && t == t_0) ok = wait_all(&bars.full[ks], k_par);
             if (!ok) break;
             if (!kWide) fence_after();
             if (one) {
               qk(t, ks);
-              commit(&bars.s_full[t][(j + 1) % kRound]);
+              commit(&bars.s_full[t][(j + step) % kRound]);
             }
           }
         }

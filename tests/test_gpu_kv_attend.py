@@ -114,6 +114,20 @@ def test_chunks_on_long_sequences(fsb, cuda, dim, window):
     run(cuda, fsb, 17, [(20000, 129)], 1, 1, dim, 128, window=window)
 
 
+@pytest.mark.parametrize("dim,page", [(128, 16), (128, 64), (128, 128), (64, 32)])
+@pytest.mark.parametrize("new,group,window", [(5, 7, 0), (5, 8, 150), (16, 8, 0), (9, 8, 1), (128, 1, 129)])
+def test_one_tile_of_rows(fsb, cuda, dim, page, new, group, window):
+    """33 to 128 rows a key head over walks of no tile of 128 tokens, one, two and more; windows under which
+    some rows see nothing of a tile; scales far apart."""
+    lens = [(l, new) for l in (128, 129, 256, 257, 300, 384, 385, 512, 640, 641, 1100, 1537)] + [(0, 0), (max(new, 9), 4), (600, 1)]
+
+    def change(d):
+        rng = np.random.default_rng(19)
+        d["v_scale"] *= np.exp2(rng.integers(-7, 8, d["v_scale"].shape)).astype(np.float32)
+
+    run(cuda, fsb, 18, lens, 8, group, dim, page, window=window, change=change)
+
+
 def test_cache_laid_out_by_token(fsb, cuda):
     run(cuda, fsb, 8, [(200, 1), (70, 3)], 4, 2, 128, 32, by_token=True)
     run(cuda, fsb, 8, [(300, 150), (70, 3)], 4, 2, 64, 32, by_token=True)
