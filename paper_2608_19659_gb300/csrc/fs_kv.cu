@@ -759,7 +759,10 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
     const int tiles = (int)((walk + want - 1) / want);
     p.chunk_split = tiles * 128;
     p.chunk_parts = (walk + tiles - 1) / tiles;
-    if (c->dim == 128 && 2 * blocks * p.chunk_parts >= sms) p.few = kMidRows;
+    // (and where most sequences have all of those rows, the others with them: no second kernel for a few
+    // that have fewer, or none)
+    if (c->dim == 128 && 2 * blocks * p.chunk_parts >= sms)
+      p.few = all <= kFewRows && 4ll * b->tokens >= 3ll * b->batch * b->max_new ? 0 : kMidRows;
     if (all <= p.few) p.chunk_tiles = 0;
   }
   if (p.chunk_tiles) {
@@ -767,9 +770,9 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
     if (p.chunk_parts > 1) p.wide_tiles = 0, p.wide_bytes = 0;
     p.chunk_floats = p.chunk_parts > 1 ? (size_t)b->batch * c->heads * p.chunk_tiles * p.chunk_parts * kKvChunkRows * (c->dim + 4) : 0;
   }
-  const int rows = (int)std::min<long long>(all, p.few);
+  const int rows = (int)std::min<long long>(all, std::max(1, p.few));
   // (every sequence has max_new new tokens: all have the same rows)
-  p.decode = !p.chunk_tiles || (long long)b->batch * b->max_new != b->tokens;
+  p.decode = !p.chunk_tiles || (p.few && (long long)b->batch * b->max_new != b->tokens);
   p.row_tile = rows <= 8 ? 8 : 16;
   p.row_blocks = (rows + p.row_tile - 1) / p.row_tile;
   const long long items = (long long)std::max(1, b->batch) * c->heads * p.row_blocks;
