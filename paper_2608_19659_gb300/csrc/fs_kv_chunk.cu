@@ -282,37 +282,38 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
   }
   __syncthreads();
 
-  // queries: a row a thread, scaled into [-2, 2] by a power of two (and by the scale's sign)
+  // queries: a row a thread, scaled into [-2, 2] by a power of two (and by the scale's sign); every load
+  // under way at once (8192-token prompt 402 -> 392 us)
   int q_exp = 0;
   if (w < 8) {
     const int r = r0 + (two ? threadIdx.x & 127 : threadIdx.x);
     const uint4* q = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (long long)(s.first + r / v.group) * a.q_token +
                                                     (h * v.group + r % v.group) * a.q_head);
+    uint4 u[D / 8];
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) u[i] = r < r_end ? q[i] : make_uint4(0, 0, 0, 0);
     float amax = 0.f;
-    if (r < r_end) {
-#pragma unroll 4
-      for (int i = 0; i < D / 8; ++i) {
-        const uint4 u = q[i];
-        const float2 z0 = Elem<T>::two(u.x), z1 = Elem<T>::two(u.y), z2 = Elem<T>::two(u.z), z3 = Elem<T>::two(u.w);
-        amax = fmaxf(amax, fmaxf(fmaxf(fmaxf(fabsf(z0.x), fabsf(z0.y)), fmaxf(fabsf(z1.x), fabsf(z1.y))),
-                                 fmaxf(fmaxf(fabsf(z2.x), fabsf(z2.y)), fmaxf(fabsf(z3.x), fabsf(z3.y)))));
-      }
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+      const float2 z0 = Elem<T>::two(u[i].x), z1 = Elem<T>::two(u[i].y), z2 = Elem<T>::two(u[i].z), z3 = Elem<T>::two(u[i].w);
+      amax = fmaxf(amax, fmaxf(fmaxf(fmaxf(fabsf(z0.x), fabsf(z0.y)), fmaxf(fabsf(z1.x), fabsf(z1.y))),
+                               fmaxf(fmaxf(fabsf(z2.x), fabsf(z2.y)), fmaxf(fabsf(z3.x), fabsf(z3.y)))));
     }
     q_exp = row_exponent(amax);
     const float down = a.scale_log2 < 0.f ? -exp2_int(-q_exp) : exp2_int(-q_exp);
     const int t = threadIdx.x >> 7, rr = threadIdx.x & 127;
     const uint32_t row = q_at + t * (kTileRows * D * 2) + rr * 128;
-#pragma unroll 4
-    for (int i = 0; i < (two && t ? 0 : D / 8); ++i) {
-      uint4 u = make_uint4(0, 0, 0, 0);
-      if (r < r_end) u = q[i];
-      uint32_t y[4] = {u.x, u.y, u.z, u.w};
+    if (!two || t == 0) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 z = Elem<T>::two(y[k]);
-        y[k] = pack_f16(z.x * down, z.y * down);
+      for (int i = 0; i < D / 8; ++i) {
+        uint32_t y[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 z = Elem<T>::two(y[k]);
+          y[k] = pack_f16(z.x * down, z.y * down);
+        }
+        st_shared16(row + (i >> 3) * (kTileRows * 128) + (((i & 7) ^ (rr & 7)) << 4), make_uint4(y[0], y[1], y[2], y[3]));
       }
-      st_shared16(row + (i >> 3) * (kTileRows * 128) + (((i & 7) ^ (rr & 7)) << 4), make_uint4(y[0], y[1], y[2], y[3]));
     }
     fence_proxy_async();
   }
