@@ -726,8 +726,8 @@ struct KvPlan {
 // Sequences with more rows (new tokens x query heads of a key head) than kFewRows go to k_kv_chunk.
 // With heads of 128, where k_kv_decode needs three passes over the codes (more than kMidRows) and
 // k_kv_chunk's blocks fill at least half of the SMs, they go there too: 40 rows over 5 sequences of up to 40000
-// tokens 106 -> 64 us, 64 rows over 48 of up to 6000 120 -> 84, 48 rows under a window of 4096 37 -> 24 (40
-// rows: 25 either way). With 32 rows it is 55 against 68, with heads of 64 54 against 62, with one long
+// tokens 106 -> 64 us, 64 rows over 48 of up to 6000 120 -> 78, 48 rows under a window of 4096 37 -> 24 (40
+// rows 25 -> 23). With 32 rows it is 55 against 68, with heads of 64 54 against 62, with one long
 // sequence (16 blocks) 33 against 46.
 constexpr int kMidRows = 32, kFewRows = 64;
 

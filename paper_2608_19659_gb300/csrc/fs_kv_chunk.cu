@@ -28,13 +28,13 @@
 //
 // Where the rows end in the first tile, the second's warps and tensor memory take every second tile of
 // the cache for the same rows, and both results are joined at the end (with the warps for keys and values:
-// 64 rows over 48 sequences of up to 6000 tokens 96 -> 80 us).
+// 64 rows over 48 sequences of up to 6000 tokens 96 -> 78 us).
 //
 // Bound by the tensor cores, 4 dim operations per (row, token), and by how fast one thread beside
 // eight busy softmax warps can issue their products and waits (a commit costs it about 200 clocks,
 // so a slot is refilled after the S that follows its products and there are only the two of S a pair
 // of tiles: 477 -> 458 us with three, 411 -> 407 with two). A prompt of 8192 tokens, 32 query heads over 4
-// key heads of 128: 404 us with the conversion (10 us), 1.36 PFLOP/s of causal work; 70 % of the bf16 rate
+// key heads of 128: 392 us with the conversion (10 us), 1.40 PFLOP/s of causal work; 72 % of the bf16 rate
 // that a library product reaches. The steps in brackets are of the same prompt, when they were taken.
 #include "fs_kv.cuh"
 

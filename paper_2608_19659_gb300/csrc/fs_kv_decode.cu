@@ -1,4 +1,4 @@
-// Attention of a few rows over the paged 8-bit cache (single tokens, proposals).
+// Attention of a few rows over the paged 8-bit cache (single tokens, few proposals).
 //
 // With at most 16 rows a key head (new tokens x query heads of its group) the call
 // is bound by reading the cache: 2 dim bytes a token and key head. The work is cut into
@@ -14,7 +14,9 @@
 //   S^T [16 tokens x rows]  = K [16 x dim] Q^T          (the codes, exact in half precision)
 //   O^T [dim x rows]       += V^T [dim x 16] P^T         (P rounded to half precision)
 // with m16n8k16 products: tokens and dimensions fill the 16 rows of the instruction, the
-// attention rows its 8 columns, so one query head costs no more padding than eight.
+// attention rows its 8 columns, so one query head costs no more padding than eight. A block takes 8
+// rows, or 16 where there are more (five proposals of 16 requests, 40 rows a key head: 25 us so, 34 with 8
+// and 36 with 24, which need all registers).
 // tcgen05 has nothing to add here: its smallest tile is 128 rows high, and its operands
 // would have to pass through shared memory once more after the conversion.
 // Three blocks an SM with two stages a warp (24 warps' rings, 192 KB an SM) read 64 sequences of up

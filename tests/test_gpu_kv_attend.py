@@ -128,6 +128,13 @@ def test_one_tile_of_rows(fsb, cuda, dim, page, new, group, window):
     run(cuda, fsb, 18, lens, 8, group, dim, page, window=window, change=change)
 
 
+@pytest.mark.parametrize("window", [0, 200])
+def test_proposals_among_single_tokens(fsb, cuda, window):
+    """Most sequences have one new token, some 33 to 64 rows: both kernels work on the batch."""
+    lens = [(700, 5), (300, 1), (1, 1), (0, 0), (257, 4), (900, 8), (128, 1), (129, 1), (40, 1), (512, 1), (1000, 5), (64, 1)]
+    run(cuda, fsb, 20, lens, 8, 8, 128, 32, window=window)
+
+
 def test_cache_laid_out_by_token(fsb, cuda):
     run(cuda, fsb, 8, [(200, 1), (70, 3)], 4, 2, 128, 32, by_token=True)
     run(cuda, fsb, 8, [(300, 150), (70, 3)], 4, 2, 64, 32, by_token=True)
