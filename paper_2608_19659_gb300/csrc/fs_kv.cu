@@ -952,7 +952,7 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   CUtensorMap mk, mv;
   if (p.chunk_tiles) {
     KvAttendArgs ca = a;
-    ca.min_rows = p.few, ca.max_rows = INT_MAX;
+    ca.min_rows = p.few, ca.max_rows = batch->max_new * (qu->q_heads / cache->heads);
     ca.split = p.chunk_split;
     ca.part = a.part + p.part_floats;
     ca.wide_tiles = p.wide_tiles;

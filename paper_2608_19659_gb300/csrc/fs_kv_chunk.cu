@@ -854,7 +854,9 @@ cudaError_t launch_all(const CUtensorMap& mk, const CUtensorMap& mv, const KvAtt
   }
   const cudaError_t e = launch<D, T, false>(mk, mv, a, tiles, parts, s);
   if (e != cudaSuccess || parts == 1) return e;
-  return launch_pdl(k_kv_chunk_join<D, T>, dim3(a.v.heads * a.v.batch, tiles, 2 * kTileRows * (D / 4) / 256), dim3(256), 0, s, a, parts);
+  // (blocks for the rows that a sequence can have, not for both of its tiles')
+  const int rows = std::min(a.max_rows, 2 * kTileRows), here = 256 / (D / 4);
+  return launch_pdl(k_kv_chunk_join<D, T>, dim3(a.v.heads * a.v.batch, tiles, (rows + here - 1) / here), dim3(256), 0, s, a, parts);
 }
 
 }  // namespace
