@@ -34,7 +34,7 @@
 // eight busy softmax warps can issue their products and waits (a commit costs it about 200 clocks,
 // so a slot is refilled after the S that follows its products and there are only the two of S a pair
 // of tiles: 477 -> 458 us with three, 411 -> 407 with two). A prompt of 8192 tokens, 32 query heads over 4
-// key heads of 128: 390 us with the conversion (10 us), 1.41 PFLOP/s of causal work, tensor cores active
+// key heads of 128: 387 us with the conversion, 1.42 PFLOP/s of causal work, tensor cores active
 // 64 % of the time; 73 % of the bf16 rate that a library product reaches. The steps in brackets are of the same prompt, when they were taken.
 #include "fs_kv.cuh"
 
@@ -791,7 +791,8 @@ __global__ void __launch_bounds__(256) k_kv_chunk_join(const KvAttendArgs a, int
 // them in: [sequence][head][tile of 128 tokens][keys, values][block of 64 dimensions][token][64].
 // Where many blocks walk over the same tokens, each tile is then converted once instead of by every
 // one of them (a prompt of 8192 tokens 455 -> 423 us). Tokens beyond a sequence's
-// and values whose scale is 0 become 0.
+// and values whose scale is 0 become 0. Bound by the latency of page, codes, store: a block for a tile's
+// keys and one for its values (one for both: ragged chunks 86 us against 82).
 template <int D>
 __global__ void __launch_bounds__(256) k_kv_expand(const KvAttendArgs a, const uint8_t* kc, const uint8_t* vc,
                                                    long long page_stride, long long head_stride, long long token_stride) {
@@ -799,39 +800,39 @@ __global__ void __launch_bounds__(256) k_kv_expand(const KvAttendArgs a, const u
   pdl_trigger();
   pdl_wait();
   const KvView& v = a.v;
-  const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x;
+  const int b = blockIdx.z, h = blockIdx.y >> 1, tile = blockIdx.x;
+  const bool values = blockIdx.y & 1;
   KvSeq s;
   if (!kv_seq(v, b, s)) return;  // (the walks' kernel reports it)
   const int rows = s.count * v.group, t0 = tile * kTok;
   const int lo = a.window ? s.len - s.count - a.window + 1 : 0;  // the first token that a row sees
   if (rows <= a.min_rows || rows > a.max_rows || t0 >= s.len || t0 + kTok <= lo || tile >= a.wide_tiles) return;
   const int cl = threadIdx.x % kLanes, tk = threadIdx.x / kLanes;
-  uint4 x[2][kPasses];
+  uint4 x[kPasses];
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) {
     const int t = t0 + p * kPer + tk;
-    x[0][p] = x[1][p] = make_uint4(0, 0, 0, 0);
+    x[p] = make_uint4(0, 0, 0, 0);
     if (t < s.len) {
       const int g = kv_page(v, b, t >> v.log_page);
       const long long at = g * page_stride + h * head_stride + (t & ((1 << v.log_page) - 1)) * token_stride + cl * 16;
-      x[0][p] = __ldg(reinterpret_cast<const uint4*>(kc + at));
-      if (v.v_scale[(long long)g * v.heads + h] != 0.f) x[1][p] = __ldg(reinterpret_cast<const uint4*>(vc + at));
+      const float scale = values ? v.v_scale[(long long)g * v.heads + h] : 1.f;  // (beside the codes' load)
+      x[p] = __ldg(reinterpret_cast<const uint4*>((values ? vc : kc) + at));
+      if (scale == 0.f) x[p] = make_uint4(0, 0, 0, 0);
     }
   }
-  char* out = a.wide + ((long long)(b * v.heads + h) * a.wide_tiles + tile) * (2 * kSlot);
+  char* out = a.wide + ((long long)(b * v.heads + h) * a.wide_tiles + tile) * (2 * kSlot) + (values ? kSlot : 0);
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
+  for (int p = 0; p < kPasses; ++p) {
+    const int tl = p * kPer + tk;
+    const uint32_t ws[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
+    uint32_t y[8];
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-      const int tl = p * kPer + tk;
-      const uint32_t ws[4] = {x[k][p].x, x[k][p].y, x[k][p].z, x[k][p].w};
-      uint32_t y[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[2 * i] = e4m3x2_to_f16x2(ws[i]), y[2 * i + 1] = e4m3x2_to_f16x2_hi(ws[i]);
-      char* row = out + k * kSlot + (cl >> 2) * (kTok * 128) + tl * 128;
-      *reinterpret_cast<uint4*>(row + ((((cl & 3) * 2) ^ (tl & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-      *reinterpret_cast<uint4*>(row + ((((cl & 3) * 2 + 1) ^ (tl & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
-    }
+    for (int i = 0; i < 4; ++i) y[2 * i] = e4m3x2_to_f16x2(ws[i]), y[2 * i + 1] = e4m3x2_to_f16x2_hi(ws[i]);
+    char* row = out + (cl >> 2) * (kTok * 128) + tl * 128;
+    *reinterpret_cast<uint4*>(row + ((((cl & 3) * 2) ^ (tl & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+    *reinterpret_cast<uint4*>(row + ((((cl & 3) * 2 + 1) ^ (tl & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+  }
 }
 
 template <int D, typename T, bool kWide>
@@ -847,7 +848,7 @@ template <int D, typename T>
 cudaError_t launch_all(const CUtensorMap& mk, const CUtensorMap& mv, const KvAttendArgs& a, const fs_kv_cache& c, int tiles,
                        int parts, cudaStream_t s) {
   if (a.wide) {
-    const cudaError_t e = launch_pdl(k_kv_expand<D>, dim3(a.wide_tiles, a.v.heads, a.v.batch), dim3(256), 0, s, a,
+    const cudaError_t e = launch_pdl(k_kv_expand<D>, dim3(a.wide_tiles, 2 * a.v.heads, a.v.batch), dim3(256), 0, s, a,
                                      static_cast<const uint8_t*>(c.k), static_cast<const uint8_t*>(c.v), (long long)c.page_stride,
                                      (long long)c.head_stride, (long long)c.token_stride);
     return e != cudaSuccess ? e : launch<D, T, true>(mk, mv, a, tiles, parts, s);
