@@ -34,7 +34,7 @@
 // eight busy softmax warps can issue their products and waits (a commit costs it about 200 clocks,
 // so a slot is refilled after the S that follows its products and there are only the two of S a pair
 // of tiles: 477 -> 458 us with three, 411 -> 407 with two). A prompt of 8192 tokens, 32 query heads over 4
-// key heads of 128: 387 us with the conversion, 1.42 PFLOP/s of causal work, tensor cores active
+// key heads of 128: 390 us with the conversion, 1.41 PFLOP/s of causal work, tensor cores active
 // 64 % of the time; 73 % of the bf16 rate that a library product reaches. The steps in brackets are of the same prompt, when they were taken.
 #include "fs_kv.cuh"
 
