@@ -287,7 +287,8 @@ __global__ void __launch_bounds__(128, 6) k_kv_append(const KvAppendArgs a) {
   const T* src = is_k ? static_cast<const T*>(a.k) + row0 * a.k_token + h * a.k_head
                       : static_cast<const T*>(a.vals) + row0 * a.v_token + h * a.v_head;
   const long long src_token = is_k ? a.k_token : a.v_token;
-  const int g = kv_page(a.v, b, pg);
+  const int g = kv_page_raw(a.v, b, pg);
+  if (!kv_page_held(a.v, g)) return;  // (all lanes of the unit)
   uint8_t* page = (is_k ? a.kc : a.vc) + g * a.page_stride + h * a.head_stride;
   float* scale_at = const_cast<float*>(is_k ? a.v.k_scale : a.v.v_scale) + (long long)g * H + h;
   const int slot0 = lo & (P - 1);
@@ -387,7 +388,8 @@ __global__ void __launch_bounds__(128, 8) k_kv_append_one(const KvAppendArgs a) 
     *reinterpret_cast<uint2*>(to + dB) = make_uint2(Elem<T>::pack(y[0], y[1]), Elem<T>::pack(y[2], y[3]));
     return;
   }
-  const int g = kv_page_ok(a.v, g_raw), slot = p & ((1 << a.v.log_page) - 1);
+  const int g = g_raw, slot = p & ((1 << a.v.log_page) - 1);
+  if (!kv_page_held(a.v, g)) return;  // (all lanes of the unit)
   float* scale_at = const_cast<float*>(is_k ? a.v.k_scale : a.v.v_scale) + (long long)g * H + h;
   const float old = slot ? *scale_at : 0.f;
   float amax = 0.f;
@@ -644,7 +646,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_kv_append_many(co
 #pragma unroll
   for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, o));
   if (threadIdx.x % 32 == 0) sm_amax[threadIdx.x / 32] = amax;
-  const int g = kv_page_ok(a.v, g_raw);
+  const int g = g_raw;
+  if (!kv_page_held(a.v, g)) return;  // (the whole block)
   float* scale_at = const_cast<float*>(is_k ? a.v.k_scale : a.v.v_scale) + (long long)g * H + h;
   const int slot0 = lo & (P - 1);
   const float old = slot0 ? *scale_at : 0.f;

@@ -70,16 +70,18 @@ __device__ __forceinline__ bool kv_seq(const KvView& v, int b, KvSeq& s) {
 
 __device__ __forceinline__ void kv_flag(const KvView& v, uint32_t bit) { atomicOr(v.status, bit); }
 
-// Page id `i` of sequence b, or 0 (flagged) where the table holds none of the cache's. The
-// check waits for the load: kv_page_raw and kv_page_ok apart let other work come between.
+// Page id `i` of sequence b. What writes to a page asks kv_page_held first and stores nothing
+// where the table holds none of the cache's pages; reads take page 0 in its place (kv_page_ok). Both
+// flag it. The check waits for the load: kv_page_raw apart lets other work come between.
 __device__ __forceinline__ int kv_page_raw(const KvView& v, int b, int i) {
   return v.page_table[(long long)b * v.table_stride + i];
 }
-__device__ __forceinline__ int kv_page_ok(const KvView& v, int g) {
-  if ((unsigned)g < (unsigned)v.pages) return g;
+__device__ __forceinline__ bool kv_page_held(const KvView& v, int g) {
+  if ((unsigned)g < (unsigned)v.pages) return true;
   kv_flag(v, KV_ST_PAGE);
-  return 0;
+  return false;
 }
+__device__ __forceinline__ int kv_page_ok(const KvView& v, int g) { return kv_page_held(v, g) ? g : 0; }
 __device__ __forceinline__ int kv_page(const KvView& v, int b, int i) { return kv_page_ok(v, kv_page_raw(v, b, i)); }
 
 // Scales are powers of two or 0, so that a code times a quotient of scales is exact in

@@ -258,3 +258,39 @@ def test_cache_beyond_32_bits(fsb, cuda):
         mag = torch.einsum("htl,lhd->thd", p, vv.abs())
         # (2^-9: probabilities 2^-11, scores, and the rest of the tolerance above with room)
         assert bool(((out.double() - want).abs() <= 2.0**-9 * mag + 2.0**-8 * want.abs()).all())
+
+
+@pytest.mark.parametrize("new", [1, 3, 20, 70])
+@pytest.mark.parametrize("bad", [-1, "pages", -(2**31), 2**31 - 1])
+@pytest.mark.parametrize("at", ["first", "last"])
+def test_a_page_outside_the_cache_is_not_written(fsb, cuda, new, bad, at):
+    """One of a sequence's page ids is none of the cache's: what belongs there is not stored anywhere (page 0 is
+    no sequence's here, but could be another request's), the rest is as with the right id, and it is reported."""
+    torch = cuda
+    rng = np.random.default_rng(31)
+    lens, page = [(new + 20, new), (45, new if new < 45 else 9), (16, 1)], 16
+    d, cache, batch, x, cos, sin, ws = setup(torch, fsb, rng, lens, 2, 4, 128, page)
+    table = batch.tensors[0]
+    spare = next(g for g in range(d["pages"]) if not (d["table"] == g).any())
+    table[table == 0] = spare
+    ct, st = torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda()
+    before = [t.clone() for t in cache.tensors]
+    q_good = torch.empty_like(x["q"])
+    fsb.fs_kv_append(cache, batch, x["k"], x["v"], ct, st, q=x["q"], q_out=q_good, workspace=ws)
+    fsb.fs_kv_check(ws)
+    want = [t.clone() for t in cache.tensors]
+    for t, b in zip(cache.tensors, before):
+        t.copy_(b)
+    col = 20 // page if at == "first" else (new + 20 - 1) // page  # of the pages that sequence 0's new tokens go to
+    true = int(table[0, col])
+    assert not torch.equal(want[2][true], before[2][true]) or not torch.equal(want[0][true], before[0][true])
+    table[0, col] = d["pages"] if bad == "pages" else bad
+    q_out = torch.empty_like(x["q"])
+    fsb.fs_kv_append(cache, batch, x["k"], x["v"], ct, st, q=x["q"], q_out=q_out, workspace=ws)
+    with pytest.raises(fsb.FleetSieveError) as ei:
+        fsb.fs_kv_check(ws)
+    assert ei.value.code == fsb.FS_EDEVICE and "page" in str(ei.value)
+    assert torch.equal(q_out, q_good)
+    for t, w, b in zip(cache.tensors, want, before):
+        w[true] = b[true]
+        assert torch.equal(t, w)
