@@ -497,7 +497,8 @@ int fs_draw_floor(int32_t mode, int32_t w, int64_t calls, int32_t reps, double *
  * paper's replica serves in FP8; the cache holds e4m3 codes with one scale per
  * (page, key head).
  *
- * Both calls take device pointers, enqueue their work on cuda_stream and return;
+ * Both calls take device pointers and a stream of the current device (the binding refuses
+ * others), enqueue their work on cuda_stream and return;
  * they allocate nothing and can be captured into a CUDA graph. fs_kv_check waits
  * and reports device-side errors.
  *

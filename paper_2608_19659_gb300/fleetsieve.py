@@ -551,7 +551,7 @@ class KvCache:
         if not k.is_cuda or any(t.device != k.device for t in (v, k_scale, v_scale)):
             raise ValueError("the cache's tensors are on one CUDA device")
         self.tensors = (k, v, k_scale, v_scale)
-        self.device, self.heads, self.dim = k.device, k.shape[1], k.shape[3]
+        self.device, self.index, self.heads, self.dim = k.device, k.device.index, k.shape[1], k.shape[3]
         self.struct = fs_kv_cache(k.shape[0], k.shape[1], k.shape[2], k.shape[3], k.data_ptr(), v.data_ptr(),
                                   k_scale.data_ptr(), v_scale.data_ptr(), k.stride(0), k.stride(1), k.stride(2))
         self.ref = C.byref(self.struct)
@@ -573,7 +573,7 @@ class KvBatch:
             if t.dtype != torch.int32 or not t.is_cuda or t.device != length.device or not t.is_contiguous():
                 raise ValueError(f"{name} is a contiguous int32 CUDA tensor, on one device with the others")
         self.tensors = (page_table, length, q_start)
-        self.device, self.tokens = length.device, int(tokens)
+        self.device, self.index, self.tokens = length.device, length.device.index, int(tokens)
         self.struct = fs_kv_batch(n, self.tokens, int(max_new), int(max_length), page_table.shape[1], 0,
                                   page_table.data_ptr(), length.data_ptr(), q_start.data_ptr())
         self.ref = C.byref(self.struct)
@@ -585,6 +585,9 @@ class KvWorkspace:
     def __init__(self, cache: KvCache, batch: KvBatch, q_heads: int):
         import torch
 
+        if not cache.index == batch.index == _current_device():
+            _kv_refuse_devices(cache, batch=batch)
+        self.index = cache.index
         n = C.c_int64()
         _check(lib().fs_kv_workspace_bytes(C.byref(cache.struct), C.byref(batch.struct), int(q_heads), C.byref(n)))
         self.tensor = torch.zeros(n.value, dtype=torch.uint8, device=cache.device)
@@ -611,15 +614,33 @@ def _kv_rows(t, name: str, dtype, cache: KvCache, tokens: int, heads: int | None
     if len(shape) != 3 or shape[0] != tokens or shape[2] != cache.dim or (heads is not None and shape[1] != heads):
         raise ValueError(f"{name} is [tokens = {tokens}, {heads or 'heads'}, {cache.dim}], not {tuple(shape)}")
     s0, s1, s2 = t.stride()
-    if t.dtype is not dtype or t.get_device() != cache.device.index or (s2 != 1 and t.numel()):
+    if t.dtype is not dtype or t.get_device() != cache.index or (s2 != 1 and t.numel()):
         raise ValueError(f"{name}: want {dtype} on {cache.device}, the last dimension contiguous")
     return t.data_ptr(), s0, s1
+
+
+def _current_device() -> int:
+    """torch's current device, as an index."""
+    global _current_device
+    import torch
+
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device  # (from the next call on)
+    return _current_device()
+
+
+def _kv_refuse_devices(cache, **others) -> None:
+    """Calls go to the current device: the cache, the batch and the workspace have to be there. (Launched on
+    another device, their addresses would be that one's, and a default stream of its own.)"""
+    for name, x in others.items():
+        if x.index != cache.index:
+            raise ValueError(f"{name} is on cuda:{x.index}, the cache on cuda:{cache.index}")
+    raise ValueError(f"cuda:{_current_device()} is current, the cache operators' tensors are on cuda:{cache.index}")
 
 
 _current_stream = None  # torch's current stream of a device index, as an address
 
 
-def _kv_stream(stream, device) -> int:
+def _kv_stream(stream, index: int) -> int:
     global _current_stream
     if stream is not None:
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
@@ -629,7 +650,7 @@ def _kv_stream(stream, device) -> int:
         # (without a torch.cuda.Stream object around the address, whose making takes 2 us of a 10 us call)
         _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda index: torch.cuda.current_stream(index).cuda_stream)
-    return _current_stream(device.index)
+    return _current_stream(index)
 
 
 # the layouts of fs_kv_new and fs_kv_query (packing is a third of the cost of filling nested structures)
@@ -641,7 +662,9 @@ def fs_kv_append(cache: KvCache, batch: KvBatch, k, v, cos=None, sin=None, q=Non
                  interleaved: bool = False, *, workspace: KvWorkspace, stream=None) -> None:
     """New keys and values [tokens, heads, dim] into the cache, the keys rotated by cos, sin
     [positions, rot / 2] (None: not rotated); q [tokens, q_heads, dim] rotated alike into q_out.
-    Enqueued on ``stream`` (default: torch's current one)."""
+    Enqueued on ``stream`` (default: torch's current one); the tensors are on the current device."""
+    if not cache.index == batch.index == workspace.index == _current_device():
+        _kv_refuse_devices(cache, batch=batch, workspace=workspace)
     dtype, tokens = k.dtype, batch.tokens
     kind = _kv_dtype(k)
     kr = _kv_rows(k, "k", dtype, cache, tokens, cache.heads)
@@ -658,7 +681,7 @@ def fs_kv_append(cache: KvCache, batch: KvBatch, k, v, cos=None, sin=None, q=Non
     if (cos is None) != (sin is None):
         raise ValueError("cos and sin go together")
     if cos is not None:
-        index, shape = cache.device.index, cos.shape
+        index, shape = cache.index, cos.shape
         if (len(shape) != 2 or sin.shape != shape or cos.element_size() != 4 or not cos.is_floating_point()
                 or sin.dtype is not cos.dtype or cos.get_device() != index or sin.get_device() != index
                 or not cos.is_contiguous() or not sin.is_contiguous()):
@@ -666,7 +689,7 @@ def fs_kv_append(cache: KvCache, batch: KvBatch, k, v, cos=None, sin=None, q=Non
         rows, rot = shape
         rot, c_at, s_at = 2 * rot, cos.data_ptr(), sin.data_ptr()
     a = _KV_NEW.pack(kind, q_heads, rot, 1 if interleaved else 0, rows, 0, *kr, *vr, *qr, *qo, c_at, s_at)
-    rc = lib().fs_kv_append(cache.ref, batch.ref, a, workspace.address, workspace.bytes, _kv_stream(stream, cache.device))
+    rc = lib().fs_kv_append(cache.ref, batch.ref, a, workspace.address, workspace.bytes, _kv_stream(stream, cache.index))
     if rc:
         _check(rc)
 
@@ -675,14 +698,16 @@ def fs_kv_attend(cache: KvCache, batch: KvBatch, q, out, scale: float, window: i
                  workspace: KvWorkspace, stream=None):
     """out [tokens, q_heads, dim] = attention of the batch's new tokens over their sequences' cached
     tokens up to their own (the last ``window`` of them; 0: all). Enqueued on ``stream`` (default:
-    torch's current one); returns out."""
+    torch's current one); the tensors are on the current device. Returns out."""
+    if not cache.index == batch.index == workspace.index == _current_device():
+        _kv_refuse_devices(cache, batch=batch, workspace=workspace)
     dtype, tokens = q.dtype, batch.tokens
     kind = _kv_dtype(q)
     qr = _kv_rows(q, "q", dtype, cache, tokens, None)
     heads = q.shape[1]
     o = _kv_rows(out, "out", dtype, cache, tokens, heads)
     a = _KV_QUERY.pack(kind, heads, scale, window, *qr, *o)
-    rc = lib().fs_kv_attend(cache.ref, batch.ref, a, workspace.address, workspace.bytes, _kv_stream(stream, cache.device))
+    rc = lib().fs_kv_attend(cache.ref, batch.ref, a, workspace.address, workspace.bytes, _kv_stream(stream, cache.index))
     if rc:
         _check(rc)
     return out
@@ -690,7 +715,9 @@ def fs_kv_attend(cache: KvCache, batch: KvBatch, q, out, scale: float, window: i
 
 def fs_kv_check(workspace: KvWorkspace, stream=None) -> None:
     """Waits for the stream and raises what the workspace's calls met on the device."""
-    _check(lib().fs_kv_check(workspace.address, _kv_stream(stream, workspace.tensor.device)))
+    if workspace.index != _current_device():
+        _kv_refuse_devices(workspace)
+    _check(lib().fs_kv_check(workspace.address, _kv_stream(stream, workspace.index)))
 
 
 def dump_dtype(K: int) -> np.dtype:
