@@ -5,14 +5,17 @@ Measuring a cell (class, TP degree, load bin) takes a replica of TP GPUs for 300
 optimistic ends of them, capacity from above and tail from below, drive the
 optimistic allocation A+. What one GPU of the replica does per decode step beside
 its matrix products, appending the new tokens to its share of the cache and
-attending to it, takes milliseconds to time on a single GPU, and no replica is
-faster than that: with R requests in flight, contexts of L tokens and N generated
-tokens a request,
+attending to it, takes milliseconds to time on a single GPU, and no replica that
+attends with these kernels is faster than that: with R requests in flight, contexts of
+L tokens and N generated tokens a request,
 
     capacity <= R / (N t_step + t_prompt)   req/s per replica (R at a time),
     tail     >= N t_step + t_prompt         s,
 
-t_step and t_prompt the rank's append and attention over all layers. :func:`tighten`
+t_step and t_prompt the rank's append and attention over all layers, on the device alone: the
+layers run in CUDA graphs, as a replica may run them, so that no host's call is counted.
+(R requests bring R prompts; one is counted, which leaves the capacity's bound on the safe
+side.) :func:`tighten`
 puts these into a model's bounds (never past the pessimistic ends), which lowers
 Gamma_t and the number of measurements wherever attention alone rules a cell out.
 """
@@ -49,7 +52,8 @@ def rank_heads(d: Decoder, tp: int) -> tuple[int, int]:
 
 class RankStep:
     """One rank's cache and buffers for `requests` requests of a decoder, and the two calls of a layer's
-    step over them. All layers of a step use the same pages here: their time does not depend on it."""
+    step over them. All layers of a step use the same pages here: a cache that fits the L2 is read faster than
+    a replica's layers read theirs, and what is timed bounds those from below all the same."""
 
     def __init__(self, d: Decoder, tp: int, requests: int, new: int = 1, seed: int = 0):
         import torch
@@ -95,22 +99,31 @@ class RankStep:
                          workspace=self.work)
         fsb.fs_kv_attend(self.cache, self.batch, self.q, self.out, self.scale, workspace=self.work)
 
-    def seconds(self, layers: int, repeats: int = 5) -> float:
-        """Time of `layers` layers on the device: the best of `repeats` runs, after an untimed one."""
+    def seconds(self, layers: int, repeats: int = 8) -> float:
+        """Time of `layers` layers on the device: what a graph of twice n layers takes longer than one of n (the best
+        of `repeats` runs of each, after an untimed one), so that neither the host nor a graph's start counts."""
         import torch
 
-        best = float("inf")
-        for i in range(repeats + 1):
-            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
-            begin.record()
-            for _ in range(layers):
-                self.layer()
-            end.record()
-            end.synchronize()
-            if i:
-                best = min(best, begin.elapsed_time(end) * 1e-3)
+        n = -(-16 // layers) * layers
+        self.layer()  # (what a first call sets up does not belong into a capture)
         fsb.fs_kv_check(self.work)
-        return best
+        graphs = {n: torch.cuda.CUDAGraph(), 2 * n: torch.cuda.CUDAGraph()}
+        for count, graph in graphs.items():
+            with torch.cuda.graph(graph):
+                for _ in range(count):
+                    self.layer()
+        best = dict.fromkeys(graphs, float("inf"))
+        for i in range(repeats + 1):
+            for count, graph in graphs.items():
+                begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+                begin.record()
+                graph.replay()
+                end.record()
+                end.synchronize()
+                if i:
+                    best[count] = min(best[count], begin.elapsed_time(end) * 1e-3)
+        fsb.fs_kv_check(self.work)
+        return (best[2 * n] - best[n]) * layers / n
 
 
 @dataclasses.dataclass
@@ -146,8 +159,10 @@ def tighten(cap_lo, cap_hi, tail_lo, tail_hi, cls: int, tp: int, b: int, p: Prob
 
 
 def main(argv=None) -> None:
-    """Probes every (TP degree, load bin) of the paper-scale grid for one class's requests and prints, as one
-    JSON line, the gap between the optimistic and the conservative allocation before and after."""
+    """Probes every (TP degree, load bin) of the paper-scale grid for one class's requests, bin b taken as 2^b
+    requests in flight (the grid's bins are ordered by load and say no more), and prints, as one JSON line, the gap
+    between the optimistic and the conservative allocation before and after, and how many of the cells' bounds
+    moved. With ordinary requests none of this grid's do; generations of 16384 tokens and more move some."""
     import argparse
     import json
 
@@ -178,8 +193,9 @@ def main(argv=None) -> None:
                 probes.append(dataclasses.asdict(p) | {"bin": b})
         fsb.fs_update_bounds(m, *bounds)
         after = fsb.fs_solve_bounds(m)
+    moved = sum(int((x != y).sum()) for x, y in zip(bounds, (w.cap_lo, w.cap_hi, w.tail_lo, w.tail_hi)))
     print(json.dumps({"class": a.cls, "decoder": dataclasses.asdict(d), "gamma_before": before[2], "gamma_after": after[2],
-                      "probes": probes}))
+                      "bounds_moved": moved, "probes": probes}))
 
 
 if __name__ == "__main__":
