@@ -536,7 +536,10 @@ typedef struct {
  * nothing. Host values: tokens = q_start[batch], max_new >= every sequence's new tokens,
  * max_length >= every length (bounds: what launches are sized by). The device arrays
  * are not checked before the call; the kernels check them, skip a sequence that breaks a
- * bound, and set status bits (fs_kv_check: FS_EDEVICE). Where a page id is none of the
+ * bound, and set status bits (fs_kv_check: FS_EDEVICE); rows before q_start[0] or from
+ * q_start[batch] on are no sequence's, and reported (a captured call that is replayed with fewer
+ * tokens gives the rest to a sequence of length 0: its rows become 0, nothing of it is
+ * appended). Where a page id is none of the
  * cache's, an append stores nothing of that page's tokens (and what belongs to other pages as
  * ever), and attention reads page 0 in its place. Limits: batch <= 65535,
  * tokens <= batch * max_new unless batch is 0, tokens * query heads <= 2^30, heads <= 1024,

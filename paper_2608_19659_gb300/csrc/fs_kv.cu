@@ -241,6 +241,7 @@ __global__ void __launch_bounds__(128, 6) k_kv_append(const KvAppendArgs a) {
     if (threadIdx.x == 0) kv_flag(a.v, KV_ST_BATCH);
     return;
   }
+  if (threadIdx.x == 0) kv_ends(a.v, b, s);
   const int P = 1 << a.v.log_page;
   const int p0 = max(s.len - s.count, 0);  // first position that is appended
   const int pg = (p0 >> a.v.log_page) + piece;
@@ -363,6 +364,7 @@ __global__ void __launch_bounds__(128, 8) k_kv_append_one(const KvAppendArgs a) 
     if (threadIdx.x == 0) kv_flag(a.v, KV_ST_BATCH);
     return;
   }
+  if (threadIdx.x == 0) kv_ends(a.v, b, s);
   const int p = s.len - 1;
   if (s.count == 0 || p < 0 || job >= 2 * H + (a.q ? a.q_heads : 0)) return;
   if (a.rot && p >= a.angle_rows) {
@@ -439,6 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_kv_append_many(co
     if (threadIdx.x == 0) kv_flag(a.v, KV_ST_BATCH);
     return;
   }
+  if (threadIdx.x == 0) kv_ends(a.v, b, s);
   const int P = 1 << a.v.log_page, H = a.v.heads;
   const int p0 = max(s.len - s.count, 0);
   const int pg = (p0 >> a.v.log_page) + piece;
@@ -774,7 +777,8 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
     p.chunk_floats = p.chunk_parts > 1 ? (size_t)b->batch * c->heads * p.chunk_tiles * p.chunk_parts * kKvChunkRows * (c->dim + 4) : 0;
   }
   const int rows = (int)std::min<long long>(all, std::max(1, p.few));
-  // (every sequence has max_new new tokens: all have the same rows)
+  // (every sequence has max_new new tokens: all have the same rows, and k_kv_chunk takes whatever a
+  // batch that breaks this has)
   p.decode = !p.chunk_tiles || (p.few && (long long)b->batch * b->max_new != b->tokens);
   p.row_tile = rows <= 8 ? 8 : 16;
   p.row_blocks = (rows + p.row_tile - 1) / p.row_tile;
@@ -955,7 +959,7 @@ extern "C" int fs_kv_attend(const fs_kv_cache* cache, const fs_kv_batch* batch, 
   CUtensorMap mk, mv;
   if (p.chunk_tiles) {
     KvAttendArgs ca = a;
-    ca.min_rows = p.few, ca.max_rows = batch->max_new * (qu->q_heads / cache->heads);
+    ca.min_rows = p.decode ? p.few : 0, ca.max_rows = batch->max_new * (qu->q_heads / cache->heads);
     ca.split = p.chunk_split;
     ca.part = a.part + p.part_floats;
     ca.wide_tiles = p.wide_tiles;

@@ -70,6 +70,11 @@ __device__ __forceinline__ bool kv_seq(const KvView& v, int b, KvSeq& s) {
 
 __device__ __forceinline__ void kv_flag(const KvView& v, uint32_t bit) { atomicOr(v.status, bit); }
 
+// Reports rows of the call that are no sequence's: before the first one's, or after the last one's.
+__device__ __forceinline__ void kv_ends(const KvView& v, int b, const KvSeq& s) {
+  if ((b == 0 && s.first != 0) || (b == v.batch - 1 && s.first + s.count != v.tokens)) kv_flag(v, KV_ST_BATCH);
+}
+
 // Page id `i` of sequence b. What writes to a page asks kv_page_held first and stores nothing
 // where the table holds none of the cache's pages; reads take page 0 in its place (kv_page_ok). Both
 // flag it. The check waits for the load: kv_page_raw apart lets other work come between.

@@ -242,6 +242,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
     if (threadIdx.x == 0 && blockIdx.y == 0) kv_flag(v, KV_ST_BATCH);
     return;
   }
+  if (threadIdx.x == 0 && blockIdx.y == 0) kv_ends(v, b, s);
   // each sequence's last rows first: theirs are its longest walks
   const int rows = s.count * v.group, part = blockIdx.z;
   const int tile = (rows + 2 * kTileRows - 1) / (2 * kTileRows) - 1 - (int)blockIdx.y, r0 = tile * (2 * kTileRows);

@@ -120,6 +120,7 @@ __global__ void __launch_bounds__(kWarps * 32, D == 128 && NT == 1 ? 3 : 1)
     if (threadIdx.x == 0 && part == 0) kv_flag(v, KV_ST_BATCH);
     return;
   }
+  if (threadIdx.x == 0 && part == 0) kv_ends(v, b, s);
   const int rows = s.count * v.group;
   const int r0 = rb * kRows;
   if (r0 >= rows || rows <= a.min_rows || rows > a.max_rows) return;
