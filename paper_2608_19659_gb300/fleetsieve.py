@@ -637,20 +637,21 @@ def _kv_refuse_devices(cache, **others) -> None:
     raise ValueError(f"cuda:{_current_device()} is current, the cache operators' tensors are on cuda:{cache.index}")
 
 
-_current_stream = None  # torch's current stream of a device index, as an address
+def _current_stream(index: int) -> int:
+    """torch's current stream of a device, as an address."""
+    global _current_stream
+    import torch
+
+    # (without a torch.cuda.Stream object around the address, whose making takes 2 us of a 10 us call)
+    _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+        lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _current_stream(index)
 
 
 def _kv_stream(stream, index: int) -> int:
-    global _current_stream
-    if stream is not None:
-        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
-    if _current_stream is None:
-        import torch
-
-        # (without a torch.cuda.Stream object around the address, whose making takes 2 us of a 10 us call)
-        _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
-            lambda index: torch.cuda.current_stream(index).cuda_stream)
-    return _current_stream(index)
+    if stream is None:
+        return _current_stream(index)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 # the layouts of fs_kv_new and fs_kv_query (packing is a third of the cost of filling nested structures)
