@@ -818,7 +818,9 @@ __global__ void __launch_bounds__(256) k_kv_expand(const KvAttendArgs a, const u
       const int g = kv_page(v, b, t >> v.log_page);
       const long long at = g * page_stride + h * head_stride + (t & ((1 << v.log_page) - 1)) * token_stride + cl * 16;
       const float scale = values ? v.v_scale[(long long)g * v.heads + h] : 1.f;  // (beside the codes' load)
-      x[p] = __ldg(reinterpret_cast<const uint4*>((values ? vc : kc) + at));
+      // (not by the path for data that nothing writes while the kernel lives: it may be resident beside an
+      // append that does)
+      x[p] = *reinterpret_cast<const uint4*>((values ? vc : kc) + at);
       if (scale == 0.f) x[p] = make_uint4(0, 0, 0, 0);
     }
   }

@@ -396,3 +396,36 @@ def test_append_and_attend_in_a_row(fsb, cuda):
 
     a, b = go(True), go(False)
     assert all(torch.equal(p, q) and bool(torch.isfinite(p.float()).all()) for p, q in zip(a, b))
+
+
+def test_a_chunk_that_rescales_pages_is_attended_to_at_once(fsb, cuda):
+    """Prompts in chunks of many rows, each louder than what is cached (its page's codes are rescaled): attention that
+    is queued right behind the append gives the bits of attention after a wait."""
+    torch = cuda
+    rng = np.random.default_rng(32)
+    B, hk, hq, D, P, n, steps = 4, 2, 16, 128, 64, 150, 4
+    pages = B * -(-n * steps // P)
+    table = torch.randperm(pages, device="cuda").view(B, -1).to(torch.int32).contiguous()
+    x = torch.from_numpy(rng.standard_normal((steps, B * n, hq + 2 * hk, D)).astype(np.float32)).to(torch.bfloat16).cuda()
+    x *= torch.tensor([1, 3, 9, 27], dtype=x.dtype, device="cuda")[:, None, None, None]
+    q_start = torch.arange(0, B * n + 1, n, dtype=torch.int32, device="cuda")
+    batches = [fsb.KvBatch(table, torch.full((B,), n * (i + 1), dtype=torch.int32, device="cuda"), q_start, B * n, n, n * steps)
+               for i in range(steps)]
+
+    def go(wait):
+        cache = fsb.KvCache(*(torch.zeros(pages, hk, P, D, dtype=torch.uint8, device="cuda") for _ in range(2)),
+                            *(torch.zeros(pages, hk, device="cuda") for _ in range(2)))
+        ws = fsb.KvWorkspace(cache, batches[-1], hq)
+        outs = [torch.empty(B * n, hq, D, dtype=x.dtype, device="cuda") for _ in range(steps)]
+        torch.cuda.synchronize()
+        for i, b in enumerate(batches):
+            fsb.fs_kv_append(cache, b, x[i][:, hq:hq + hk], x[i][:, hq + hk:], workspace=ws)
+            if wait:
+                fsb.fs_kv_check(ws)
+            fsb.fs_kv_attend(cache, b, x[i][:, :hq], outs[i], 0.02, workspace=ws)
+        fsb.fs_kv_check(ws)
+        return outs
+
+    want = go(True)
+    for _ in range(20):
+        assert all(torch.equal(a, b) for a, b in zip(want, go(False)))
