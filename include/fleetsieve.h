@@ -571,7 +571,7 @@ typedef struct {
 /*
  * The workspace of both calls: device memory of at least the bytes that
  * fs_kv_workspace_bytes gives for the largest cache, batch and q_heads that will
- * use it, 256-byte aligned, zero-filled once before its first use. It holds the
+ * use it (of caches with the same number of key heads), 256-byte aligned, zero-filled once before its first use. It holds the
  * status word and parts of results; calls that share one run one after the other.
  */
 int fs_kv_workspace_bytes(const fs_kv_cache *cache, const fs_kv_batch *batch, int32_t q_heads,

@@ -820,10 +820,11 @@ size_t part_floats_bound(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads
   // chunks: at most sms parts in all
   const long long all = (long long)std::max(1, b->max_new) * (q_heads / c->heads);
   const long long blocks = all > kMidRows ? std::max(1, b->batch) * (long long)c->heads * ((all + kKvChunkRows - 1) / kKvChunkRows) : 0;
-  // the tokens as halves: a smaller batch may have them where a larger one's are too many
+  // the tokens as halves, where a batch can have them at all: a smaller one may where a larger one's are too many
+  const bool wide = all > (kWideFrom - 1) * (long long)kKvChunkRows;
   const long long tokens = ((len + 127) / 128) * std::max(1, b->batch) * c->heads * (2ll * 128 * c->dim * 2);
   return (size_t)(decode + std::min((long long)sms, kKvFan * blocks) * kKvChunkRows * (c->dim + 4) +
-                  (blocks ? std::min(tokens, kWideBytes) / 4 + 32 : 0));
+                  (wide ? std::min(tokens, kWideBytes) / 4 + 32 : 0));
 }
 
 int device_sms(int* sms) {

@@ -429,3 +429,22 @@ def test_a_chunk_that_rescales_pages_is_attended_to_at_once(fsb, cuda):
     want = go(True)
     for _ in range(20):
         assert all(torch.equal(a, b) for a, b in zip(want, go(False)))
+
+
+def test_workspaces_hold_what_a_batch_can_use(fsb, cuda):
+    """Room for tokens as halves (up to 1 GiB) only where a batch can have the rows for that, more than 768 a key
+    head. Proposals need parts of results alone: nine parts of 16 rows an item at most, a row 130 floats."""
+    torch = cuda
+    cache = fsb.KvCache(*(torch.zeros(4, 8, 64, 128, dtype=torch.uint8, device="cuda") for _ in range(2)),
+                        *(torch.zeros(4, 8, device="cuda") for _ in range(2)))
+    table = torch.zeros(256, 512, dtype=torch.int32, device="cuda")
+    ends = torch.zeros(257, dtype=torch.int32, device="cuda")
+
+    def size(batch, new):
+        return fsb.KvWorkspace(cache, fsb.KvBatch(table[:batch], ends[:batch], ends[:batch + 1], batch * new, new, 32768), 64).bytes
+
+    assert size(16, 5) < 1 << 27
+    assert size(256, 5) <= size(256, 96) < 1 << 30
+    assert size(64, 97) >= 1 << 30  # 776 rows a key head
+    # one prompt of 8192 tokens over 32768: 256 tiles of keys and values of eight heads in halves
+    assert 256 * 8 * 2 * 128 * 256 <= size(1, 8192) < 1 << 30
