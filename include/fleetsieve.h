@@ -531,19 +531,19 @@ typedef struct {
  * of the call's arrays (none: a slot without a request, or one that only waits).
  * Token position p of sequence b is in page page_table[b * table_stride +
  * p / page_tokens], slot p mod page_tokens; entries beyond a sequence's tokens may
- * hold anything. A row whose position would be negative (more new tokens than length) is
- * not appended, its query not rotated (its row of q_out is left), and it attends to
- * nothing. Host values: tokens = q_start[batch], max_new >= every sequence's new tokens,
- * max_length >= every length (bounds: what launches are sized by). The device arrays
- * are not checked before the call; the kernels check them, skip a sequence that breaks a
- * bound, and set status bits (fs_kv_check: FS_EDEVICE); rows before q_start[0] or from
- * q_start[batch] on are no sequence's, and reported (a captured call that is replayed with fewer
- * tokens gives the rest to a sequence of length 0: its rows become 0, nothing of it is
- * appended). Where a page id is none of the
- * cache's, an append stores nothing of that page's tokens (and what belongs to other pages as
- * ever), and attention reads page 0 in its place. Limits: batch <= 65535,
- * tokens <= batch * max_new unless batch is 0, tokens * query heads <= 2^30, heads <= 1024,
- * max_length <= 2^30.
+ * hold anything, and with a window those of pages wholly before the windows of all of its
+ * new tokens (a server may free such pages). A row whose position would be negative (more
+ * new tokens than length) is not appended, its query not rotated (its row of q_out is left),
+ * and it attends to nothing. Host values: tokens = q_start[batch], max_new >= every sequence's
+ * new tokens, max_length >= every length (bounds: what launches are sized by). The device
+ * arrays are not checked before the call; the kernels check them, skip a sequence that breaks
+ * a bound, and set status bits (fs_kv_check: FS_EDEVICE); rows before q_start[0] or from
+ * q_start[batch] on are no sequence's, and reported (a captured call that is replayed with
+ * fewer tokens gives the rest to a sequence of length 0: its rows become 0, nothing of it is
+ * appended). Where a page id is none of the cache's, an append stores nothing of that page's
+ * tokens (and what belongs to other pages as ever), and attention reads page 0 in its place.
+ * Limits: batch <= 65535, tokens <= batch * max_new unless batch is 0, tokens * query heads
+ * <= 2^30, heads <= 1024, max_length <= 2^30.
  */
 typedef struct {
     int32_t batch;

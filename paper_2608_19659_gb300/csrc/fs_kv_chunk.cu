@@ -205,17 +205,18 @@ __device__ __forceinline__ float row_top(float (&x)[kTok], float c, const float2
   return top;
 }
 
-// The keys that rows [r0, r_end) of a sequence see: a walk over [begin, end), in parts of
-// a.split tokens.
+// The keys that rows [r0, r_end) of a sequence see, from `first` on: a walk over [begin, end), in
+// parts of a.split tokens.
 struct Walk {
-  int begin, end, parts;
+  int first, begin, end, parts;
 };
 __device__ __forceinline__ Walk walk_of(const KvAttendArgs& a, const KvSeq& s, int r0, int r_end) {
   const int base = s.len - s.count;
   const int pos0 = base + r0 / a.v.group, pos1 = base + (r_end - 1) / a.v.group;
   Walk w;
   w.end = max(pos1 + 1, 0);
-  w.begin = (a.window ? max(pos0 - a.window + 1, 0) : 0) & ~(kTok - 1);
+  w.first = a.window ? max(pos0 - a.window + 1, 0) : 0;
+  w.begin = w.first & ~(kTok - 1);
   w.parts = max(1, (w.end - w.begin + a.split - 1) / a.split);
   return w;
 }
@@ -561,13 +562,14 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
       // ahead and their scales one, so that no copy waits for either.
       const bool values = !kWide && w == C::kIssuer + 2;  // (codes: a warp for the keys, one for the values)
       const int log_p = v.log_page, boxes = kTok >> log_p;
-      int v_exp = 127;  // exponent of the scale that those of values are relative to: the first page's
+      int v_exp = 127;  // exponent of the scale that those of values are relative to: the first held page's
       int page0 = 0, page1 = 0, page2 = 0;
       bool held0 = false, held1 = false, held2 = false;
       float ks0 = 0.f, vs0 = 0.f, ks1 = 0.f, vs1 = 0.f;
       auto ask_pages = [&](int j) {
         const int t = begin + j * kTok + (lane << log_p);
-        held2 = j < n && lane < boxes && t < kv_hi;
+        // (pages wholly before the window: the table may hold anything there)
+        held2 = j < n && lane < boxes && t < kv_hi && t + (1 << log_p) > walk.first;
         if (held2) page2 = kv_page_raw(v, b, t >> log_p);
       };
       auto ask_scales = [&] {
@@ -590,7 +592,7 @@ __global__ void __launch_bounds__(Cfg<D, kWide>::kThreads, 1) k_kv_chunk(const _
         ask_scales();
         ask_pages(j + 2);
         if (j == 0) {
-          const float ref = __shfl_sync(~0u, vs0, 0);
+          const float ref = __shfl_sync(~0u, vs0, max(__ffs(__ballot_sync(~0u, held0)) - 1, 0));
           if (ref > 0.f) v_exp = __float_as_int(ref) >> 23 & 255;
           if (lane == 0 && !values) bars.v_ref = exp2_int(v_exp - 127);
         }
@@ -791,8 +793,8 @@ __global__ void __launch_bounds__(256) k_kv_chunk_join(const KvAttendArgs a, int
 // The codes of whole sequences as halves, in the order and swizzle that the products read
 // them in: [sequence][head][tile of 128 tokens][keys, values][block of 64 dimensions][token][64].
 // Where many blocks walk over the same tokens, each tile is then converted once instead of by every
-// one of them (a prompt of 8192 tokens 455 -> 423 us). Tokens beyond a sequence's
-// and values whose scale is 0 become 0. Bound by the latency of page, codes, store: a block for a tile's
+// one of them (a prompt of 8192 tokens 455 -> 423 us). Tokens beyond a sequence's, pages wholly before
+// its window and values whose scale is 0 become 0. Bound by the latency of page, codes, store: a block for a tile's
 // keys and one for its values (one for both: ragged chunks 86 us against 82).
 template <int D>
 __global__ void __launch_bounds__(256) k_kv_expand(const KvAttendArgs a, const uint8_t* kc, const uint8_t* vc,
@@ -814,7 +816,7 @@ __global__ void __launch_bounds__(256) k_kv_expand(const KvAttendArgs a, const u
   for (int p = 0; p < kPasses; ++p) {
     const int t = t0 + p * kPer + tk;
     x[p] = make_uint4(0, 0, 0, 0);
-    if (t < s.len) {
+    if (t < s.len && (t | ((1 << v.log_page) - 1)) >= lo) {
       const int g = kv_page(v, b, t >> v.log_page);
       const long long at = g * page_stride + h * head_stride + (t & ((1 << v.log_page) - 1)) * token_stride + cl * 16;
       const float scale = values ? v.v_scale[(long long)g * v.heads + h] : 1.f;  // (beside the codes' load)

@@ -145,13 +145,16 @@ __global__ void __launch_bounds__(kWarps * 32, D == 128 && NT == 1 ? 3 : 1)
   int pg0 = 0, pg1 = 0;
   float ks0 = 0.f, ks1 = 0.f, vs0 = 0.f, vs1 = 0.f;
   const bool half_tiles = v.log_page == 4;
+  auto before = [&](int i) { return half_tiles && c0 + (w + i * kWarps) * kTile + 16 <= kv_lo; };
   auto load_pages = [&](int i0) {
     const int i = i0 + lane;
     pg0 = pg1 = 0;
     ks0 = ks1 = vs0 = vs1 = 0.f;
     if (i < my_tiles) {
       const int t = c0 + (w + i * kWarps) * kTile;
-      pg0 = pg1 = !a.window && i0 == 0 ? kv_page_ok(v, early) : kv_page(v, b, t >> v.log_page);
+      // (a tile's first page may lie wholly before the window, where the table may hold anything: the second
+      // is taken twice, and the values' scale below says 0)
+      pg0 = pg1 = !a.window && i0 == 0 ? kv_page_ok(v, early) : kv_page(v, b, (t + (before(i) ? 16 : 0)) >> v.log_page);
       if (half_tiles && t + 16 < s.len) pg1 = kv_page(v, b, (t + 16) >> v.log_page);
     }
   };
@@ -161,6 +164,7 @@ __global__ void __launch_bounds__(kWarps * 32, D == 128 && NT == 1 ? 3 : 1)
       ks0 = v.k_scale[at0], vs0 = v.v_scale[at0];
       ks1 = ks0, vs1 = vs0;
       if (pg1 != pg0) ks1 = v.k_scale[at1], vs1 = v.v_scale[at1];
+      if (before(i0 + lane)) vs0 = 0.f;
     }
   };
   // one of a tile's copies into its stage: keys, values, and those of the second page

@@ -448,3 +448,39 @@ def test_workspaces_hold_what_a_batch_can_use(fsb, cuda):
     assert size(64, 97) >= 1 << 30  # 776 rows a key head
     # one prompt of 8192 tokens over 32768: 256 tiles of keys and values of eight heads in halves
     assert 256 * 8 * 2 * 128 * 256 <= size(1, 8192) < 1 << 30
+
+
+@pytest.mark.parametrize("dim,page", [(128, 16), (64, 16), (128, 32), (128, 64), (64, 32)])
+@pytest.mark.parametrize("new,group", [(1, 4), (5, 4), (9, 8), (70, 8), (120, 8)])
+@pytest.mark.parametrize("window", [1, 17, 50, 100])
+@pytest.mark.parametrize("freed", ["nothing", "another's"])
+def test_pages_before_the_window_may_be_freed(fsb, cuda, dim, page, new, group, window, freed):
+    """Entries of pages that lie wholly before the windows of all of a sequence's new tokens hold a number that is no
+    page, or a page of NaN codes with NaN for a scale: nothing of it shows, and nothing is reported."""
+    torch = cuda
+    rng = np.random.default_rng(33)
+    lens = [(new + x, new) for x in (0, 15, 16, 31, 33, 40, 64, 100, 127, 128, 129, 200, 257, 390, 500)] + [(0, 0), (300, 1)]
+    d = ref.make(rng, lens, 2, dim, page)
+    for b, (l, _) in enumerate(lens):  # (slots without a token hold NaN codes, as ever)
+        if l % page:
+            d["k"][d["table"][b, l // page], :, l % page:] = 0x7F
+            d["v"][d["table"][b, l // page], :, l % page:] = 0xFF
+    bad = next(g for g in range(d["pages"]) if not (d["table"] == g).any())
+    dirty = d["table"].copy()
+    n_freed = 0
+    for b, (l, n) in enumerate(lens):
+        free = max(l - n - window + 1, 0) // page if n else -(-l // page)
+        dirty[b, :free] = -7 if freed == "nothing" else bad
+        n_freed += free
+    assert n_freed > 0
+    T, hq = int(d["q_start"][-1]), 2 * group
+    cache, batch, q, ws = on_gpu(torch, fsb, d, hq, "bf16", rng.standard_normal((T, hq, dim)).astype(np.float32))
+    batch.tensors[0].copy_(torch.from_numpy(dirty))
+    for t, x in zip(cache.tensors, (0x7F, 0xFF, float("nan"), float("nan"))):
+        t[bad] = x
+    out = torch.full_like(q, float("nan"))
+    fsb.fs_kv_attend(cache, batch, q, out, 0.1, window=window, workspace=ws)
+    fsb.fs_kv_check(ws)
+    want, mag, dots = ref.attend(q.float().cpu().numpy(), d["k"], d["v"], d["k_scale"], d["v_scale"], d["table"],
+                                 d["length"], d["q_start"], 0.1, window)
+    check(out, want, mag, dots, DTYPES["bf16"])
