@@ -55,11 +55,12 @@ class RankStep:
     step over them. All layers of a step use the same pages here: a cache that fits the L2 is read faster than
     a replica's layers read theirs, and what is timed bounds those from below all the same."""
 
-    def __init__(self, d: Decoder, tp: int, requests: int, new: int = 1, seed: int = 0):
+    def __init__(self, d: Decoder, tp: int, requests: int, new: int = 1, seed: int = 0, length: int | None = None):
         import torch
 
         hq, hk = rank_heads(d, tp)
-        length = d.context if new > 1 else d.context + d.output // 2  # a prompt, or a request half way
+        if length is None:
+            length = d.context if new > 1 else d.context + d.output // 2  # a prompt, or a request half way
         g = torch.Generator(device="cuda").manual_seed(seed)
         per = -(-length // d.page)
         pages = requests * per
@@ -142,7 +143,7 @@ def probe_cell(d: Decoder, tp: int, requests: int, layers_timed: int = 4) -> Pro
     """Times one rank of TP degree tp with `requests` requests in flight (layers_timed of the decoder's
     layers, the rest counted like them)."""
     step = RankStep(d, tp, requests).seconds(layers_timed) * d.layers / layers_timed
-    prompt = RankStep(d, tp, 1, new=d.context).seconds(layers_timed) * d.layers / layers_timed
+    prompt = RankStep(d, tp, 1, new=d.context, length=d.context).seconds(layers_timed) * d.layers / layers_timed
     tail = d.output * step + prompt
     return Probe(tp, requests, step, prompt, requests / (d.output * step + prompt), tail)
 

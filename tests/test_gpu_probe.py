@@ -56,3 +56,18 @@ def test_the_command(fsb, cuda, capsys):
     r = json.loads(capsys.readouterr().out)
     assert len(r["probes"]) == 4 * 8 and r["gamma_after"] <= r["gamma_before"] and r["bounds_moved"] >= 0
     assert all(p["step_seconds"] > 0 and p["prompt_seconds"] > 0 for p in r["probes"])
+
+
+@pytest.mark.parametrize("context", [1, 2, 300])
+def test_a_prompt_is_as_long_as_the_context(fsb, cuda, monkeypatch, context):
+    """A prompt of one token too: not a step in the middle of the generation."""
+    seen = []
+
+    class Step(probe.RankStep):
+        def seconds(self, *args):
+            seen.append((self.batch.tokens, self.batch.tensors[1].tolist()))
+            return 1e-5
+
+    monkeypatch.setattr(probe, "RankStep", Step)
+    probe.probe_cell(probe.Decoder(context=context, output=64), 8, 2)
+    assert seen == [(2, [context + 32] * 2), (context, [context])]
