@@ -588,6 +588,8 @@ int fs_kv_workspace_bytes(const fs_kv_cache *cache, const fs_kv_batch *batch, in
  *              to float. Values are not rotated.
  *   q, q_out   optional [tokens][q_heads][dim] queries, rotated alike and rounded once
  *              to dtype (q_out may be q); NULL data: none.
+ * Where a page's new tokens reach beyond the tables' rows, none of the page's is appended
+ * and none of their queries rotated (a status bit).
  * The scale of a (page, head) that the call writes to becomes the larger of its old
  * one (0 if the call writes slot 0: a fresh page) and the least power of two s >=
  * 2^-126 with |x| <= 448 s for the call's finite values x there (0 if they are all 0).
@@ -619,9 +621,11 @@ int fs_kv_append(const fs_kv_cache *cache, const fs_kv_batch *batch, const fs_kv
  * tokens of its sequence up to its own position, or with window > 0 over the last
  * `window` of those. q_heads is a multiple of cache->heads; query head h reads key
  * head h / (q_heads / heads). Sums, softmax statistics and the accumulators are
- * floats; probabilities are rounded to half precision relative to the row's largest,
- * the result once to dtype. A row that sees no token becomes 0. Rows of out that
- * belong to a sequence skipped for a broken bound are left as they are.
+ * floats. Queries are rounded to half precision once a power of two has brought the row's
+ * largest magnitude into [1, 2) (values of at least 2^-14 there are exact, smaller ones are off
+ * by 2^-25 at most), probabilities to half precision relative to the row's largest, the result
+ * once to dtype; the exponential is the hardware's, to 2^-22. A row that sees no token becomes
+ * 0. Rows of out that belong to a sequence skipped for a broken bound are left as they are.
  */
 typedef struct {
     int32_t dtype;

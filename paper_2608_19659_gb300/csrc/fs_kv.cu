@@ -426,7 +426,12 @@ __global__ void __launch_bounds__(128, 8) k_kv_append_one(const KvAppendArgs a) 
 // page, as above, keeps too few loads under way: 8 prompts of 4096 tokens took 389 us with it,
 // 115 us with this one (623 MB, 5.4 TB/s, 79 % of the copy rate; issue slots 60 % busy).
 constexpr int kQHeads = 8;
-constexpr int kFewTokens = 8;  // up to so many new tokens a sequence, k_kv_append
+// Up to so many new tokens a sequence, k_kv_append. Measured on the GPU against k_kv_append_many (us, pages of 64
+// tokens): it is the faster one for many sequences of many heads (8 + 64 heads, 256 sequences of 2, 4, 8, 9 tokens: 11, 17,
+// 31, 37 against 30, 31, 35, 40; 64 of 2 and 4: 5.1 and 7.8 against 9.9 and 10.2, but 13.1 against 10.7 with 8), and the
+// slower one elsewhere (one sequence of 2, 4, 8: 4.0, 6.1, 10.6 against 3.6, 3.7, 3.8; 1 + 8 heads, 64 sequences of 8: 11.1
+// against 4.7; 64 sequences with pages of 16 of 8: 12.2 against 4.7). The rule does not look at sequences and heads.
+constexpr int kFewTokens = 8;
 
 template <int D, typename T, int kIt, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_kv_append_many(const KvAppendArgs a) {
@@ -731,14 +736,18 @@ struct KvPlan {
 
 // Sequences with more rows (new tokens x query heads of a key head) than kFewRows go to k_kv_chunk.
 // With heads of 128, where k_kv_decode needs three passes over the codes (more than kMidRows) and
-// k_kv_chunk's blocks fill at least half of the SMs, they go there too: 40 rows over 5 sequences of up to 40000
-// tokens 106 -> 64 us, 64 rows over 48 of up to 6000 120 -> 78, 48 rows under a window of 4096 37 -> 24 (40
-// rows 25 -> 23). With 32 rows it is 55 against 68, with heads of 64 54 against 62, with one long
-// sequence (16 blocks) 33 against 46.
+// k_kv_chunk's blocks fill at least half of the SMs, they go there too (us on the GPU, k_kv_decode against
+// k_kv_chunk): 40 rows over 5 sequences of up to 40000 tokens 43 against 36, 64 rows over 48 of up to 6000 80
+// against 61, 48 rows of 16 under a window of 4096 36 against 21, 40 rows 35 against 21; with one long sequence (16
+// blocks) 24 against 33. With 32 rows: 48 sequences of up to 6000 46 against 60, but 16 under the window 30 against
+// 21. Heads of 64 stay with k_kv_decode, though 40 rows over those 5 sequences take it 43 and k_kv_chunk 28.
 constexpr int kMidRows = 32, kFewRows = 64;
 
 // Where at least kWideFrom blocks can walk over a sequence's tokens, and the batch's tokens as
-// halves take no more than kWideBytes, they are converted once.
+// halves take no more than kWideBytes, they are converted once. Measured, 16 sequences of 8 key heads (us, each walk
+// converting against once): 2 blocks over 2000 tokens 80 against 107, 3 blocks 120 against 138, 4 blocks 156 against
+// 166, 6 blocks 230 against 226, 8 blocks 269 against 260; over the new tokens alone 4 blocks 49 against 47, 8 blocks
+// 100 against 90; with heads of 64 over 8000 tokens 3 blocks 296 against 306, 4 blocks 393 against 384.
 constexpr int kWideFrom = 4;
 constexpr long long kWideBytes = 1ll << 30;
 void wide_of(const fs_kv_cache* c, const fs_kv_batch* b, int tiles, int* wide_tiles, size_t* bytes) {
@@ -766,7 +775,9 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
     p.chunk_split = tiles * 128;
     p.chunk_parts = (walk + tiles - 1) / tiles;
     // (and where most sequences have all of those rows, the others with them: no second kernel for a few
-    // that have fewer, or none)
+    // that have fewer, or none. Measured, 2 key heads, five proposals for a share of 16 sequences of up to 9000
+    // tokens and one token for the rest: one kernel 28 us, two 51, at shares of tokens from 0.75 on; below, where this
+    // takes two, it is 28 to 30 against 53 to 57)
     if (c->dim == 128 && 2 * blocks * p.chunk_parts >= sms)
       p.few = all <= kFewRows && 4ll * b->tokens >= 3ll * b->batch * b->max_new ? 0 : kMidRows;
     if (all <= p.few) p.chunk_tiles = 0;
@@ -791,14 +802,17 @@ KvPlan plan_of(const fs_kv_cache* c, const fs_kv_batch* b, int q_heads, int wind
     p.splits = 1;
   } else {
     // a part for every block that is resident at once; parts for three such waves where they are
-    // few an item, because sequences differ in length (64 of up to 8192 tokens: 67 us with two)
+    // few an item, because sequences differ in length (append and attention, 64 of up to 8192 tokens: 59 us, with one
+    // wave 63, two 66, four 61)
     const long long slots = (long long)sms * (c->dim == 128 ? 3 : 6);
     const long long want = 2 * items <= slots ? slots / items : (3 * slots + items - 1) / items;
     p.split = std::clamp((int)((len + want - 1) / want + 127) / 128 * 128, kMinSplit, kMaxSplit);
     p.splits = (len + p.split - 1) / p.split;
-    // clusters where blocks are few (one token of 1000: 8.0 us without) or of few items (131072 tokens
-    // of one head: 19.9 us without, 18.8 with): elsewhere sequences' parts differ in number, and the need
-    // of free places side by side costs more (33 ragged requests 17 us without, 24 us with)
+    // clusters where blocks are few, or of few items. Measured on the GPU, one key head, tokens an item (us, with
+    // clusters against without): 1 item of 1000 5.3 against 7.2, of 16384 10.3 against 11.5, of 131072 17.5
+    // against 18.3; 8 of 4000 10.3 against 12.4. Where each item has many parts, the need of free places side by side
+    // costs more: 8 of 65536 39 against 32 (clusters all the same), 16 of 65536 66 against 52 and 33 of 16384 41 against 30
+    // (none). Between the two the rule is coarse: 12 of 4000 10.7 against 12.5, 33 of 1000 7.4 against 9.2 (none)
     if (items * p.splits <= (items <= 8 ? slots : sms))
       while (p.cluster < kKvCluster && p.cluster < p.splits) p.cluster *= 2;
     p.splits = (p.splits + p.cluster - 1) / p.cluster * p.cluster;

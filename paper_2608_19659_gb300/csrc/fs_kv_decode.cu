@@ -15,12 +15,12 @@
 //   O^T [dim x rows]       += V^T [dim x 16] P^T         (P rounded to half precision)
 // with m16n8k16 products: tokens and dimensions fill the 16 rows of the instruction, the
 // attention rows its 8 columns, so one query head costs no more padding than eight. A block takes 8
-// rows, or 16 where there are more (five proposals of 16 requests, 40 rows a key head: 25 us so, 34 with 8
-// and 36 with 24, which need all registers).
+// rows, or 16 where there are more (40 rows a key head of 16 requests, which now go to k_kv_chunk, took 25 us so,
+// 34 with 8 and 36 with 24, which need all registers).
 // tcgen05 has nothing to add here: its smallest tile is 128 rows high, and its operands
 // would have to pass through shared memory once more after the conversion.
 // Three blocks an SM with two stages a warp (24 warps' rings, 192 KB an SM) read 64 sequences of up
-// to 32768 tokens, 1.5 GB, in 243 us (6.3 TB/s, 93 % of the copy rate); two blocks with three
+// to 32768 tokens, 1.5 GB, in 244 us (6.3 TB/s, 93 % of the copy rate); two blocks with three
 // stages took 258 us.
 // The scale of a page's keys multiplies S. That of its values, a power of two relative to the
 // largest met so far (v_ref), goes into P as an addend of the exponent, and m is the largest
