@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(128, 8) k_kv_append_one(const KvAppendArgs a) 
 // tokens in registers, kIt of them a unit, so that they are read once and all at once; for
 // queries a block per page's tokens and kQHeads heads, whose rows share the angles. A unit a
 // page, as above, keeps too few loads under way: 8 prompts of 4096 tokens took 389 us with it,
-// 115 us with this one (623 MB, 5.4 TB/s, 79 % of the copy rate; issue slots 60 % busy).
+// 114 us with this one (623 MB, 5.5 TB/s, 80 % of the copy rate; issue slots 60 % busy).
 constexpr int kQHeads = 8;
 // Up to so many new tokens a sequence, k_kv_append. Measured on the GPU against k_kv_append_many (us, pages of 64
 // tokens): it is the faster one for many sequences of many heads (8 + 64 heads, 256 sequences of 2, 4, 8, 9 tokens: 11, 17,

@@ -20,7 +20,7 @@
 // tcgen05 has nothing to add here: its smallest tile is 128 rows high, and its operands
 // would have to pass through shared memory once more after the conversion.
 // Three blocks an SM with two stages a warp (24 warps' rings, 192 KB an SM) read 64 sequences of up
-// to 32768 tokens, 1.5 GB, in 244 us (6.3 TB/s, 93 % of the copy rate); two blocks with three
+// to 32768 tokens, 1.5 GB, in 244 us (6.3 TB/s, 92 % of the copy rate); two blocks with three
 // stages took 258 us.
 // The scale of a page's keys multiplies S. That of its values, a power of two relative to the
 // largest met so far (v_ref), goes into P as an addend of the exponent, and m is the largest
