@@ -644,6 +644,126 @@ int fs_kv_attend(const fs_kv_cache *cache, const fs_kv_batch *batch, const fs_kv
  * workspace's tickets. */
 int fs_kv_check(void *workspace, void *cuda_stream);
 
+/*
+ * ---- the products of a rank's layer
+ *
+ * What a rank of a replica computes beside its attention: the projections of a layer and its
+ * gated feed-forward block. With fs_kv_append and fs_kv_attend they are the whole of a rank's layer but for its
+ * norms (probe.py times them together: RankStep(..., products=True)). Types of x and W: FS_KV_BF16, FS_KV_FP16, or
+ * FS_E4M3 with a scale for each row of x and each row of W, as fs_quantise_rows writes them (any finite
+ * scales will do). Sums are floats; what the epilogue adds, multiplies and applies is float; results are
+ * rounded once. Offsets may pass 2^31.
+ *
+ * As with the cache operators: device pointers of the current device, work is enqueued on cuda_stream, nothing is
+ * allocated, calls can be captured; calls that share a workspace run one after the other. Outputs
+ * must not overlap inputs, but y may be the residual. Sizes are arbitrary (rows and out 0 to 2^24, in 1 to 2^24);
+ * what lies behind a row's end is neither used nor written.
+ *
+ * fs_mm_rows: row r begins at data + r * stride (elements); data 16-byte aligned, stride a multiple of 8 (codes: 16) and
+ * at least the row's width (of a single row it is not used; a residual's may be 0: the same row for all).
+ * scale: FS_E4M3 only, a float for each row, 16-byte aligned.
+ */
+#define FS_E4M3 2
+
+#define FS_ACT_NONE 0
+#define FS_ACT_RELU 1
+#define FS_ACT_SILU 2      /* z / (1 + e^-z) */
+#define FS_ACT_GELU 3      /* z Phi(z), Phi the normal distribution */
+#define FS_ACT_GELU_TANH 4 /* z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) */
+
+typedef struct {
+    void *data;
+    int64_t stride;
+    const float *scale;
+} fs_mm_rows;
+
+/*
+ * The workspace of the calls below: device memory of at least the bytes that fs_mm_workspace_bytes
+ * gives for the largest sizes that will use it (backward != 0: fs_gated_ff_backward too), 256-byte
+ * aligned, zero-filled once before its first use.
+ */
+int fs_mm_workspace_bytes(int32_t rows, int32_t in, int32_t out, int32_t backward, int64_t *bytes);
+
+/*
+ * fs_linear -- y [rows][out] = act(x W^T + bias) + residual.
+ *   type       of x [rows][in] and w [out][in]: FS_KV_BF16, FS_KV_FP16 or FS_E4M3 (then the product's (t, n) is
+ *              multiplied by x.scale[t] and w.scale[n])
+ *   out_type   of bias, residual and y: FS_KV_BF16 or FS_KV_FP16; type itself where that is 16-bit
+ *   activation FS_ACT_*
+ *   bias       [out], 16-byte aligned, or NULL; residual [rows][out], or NULL data
+ */
+typedef struct {
+    int32_t rows;
+    int32_t in;
+    int32_t out;
+    int32_t type;
+    int32_t out_type;
+    int32_t activation;
+    fs_mm_rows x;
+    fs_mm_rows w;
+    fs_mm_rows residual;
+    fs_mm_rows y;
+    const void *bias;
+} fs_mm_linear;
+
+int fs_linear(const fs_mm_linear *args, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/*
+ * fs_gated_ff -- y [rows][out] = act(x Wg^T) * (x Wu^T): both projections of a gated feed-forward block, the
+ * activation and the product in one kernel. w_gate, w_up [out][in]; types as in fs_linear.
+ */
+typedef struct {
+    int32_t rows;
+    int32_t in;
+    int32_t out;
+    int32_t type;
+    int32_t out_type;
+    int32_t activation;
+    fs_mm_rows x;
+    fs_mm_rows w_gate;
+    fs_mm_rows w_up;
+    fs_mm_rows y;
+} fs_mm_gated;
+
+int fs_gated_ff(const fs_mm_gated *args, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/*
+ * fs_gated_ff_backward -- the gradients of fs_gated_ff for 16-bit types, given dy [rows][out]: with g = x Wg^T,
+ * u = x Wu^T (computed again), dg = dy u act'(g) and du = dy act(g),
+ *   dx [rows][in] = dg Wg + du Wu,   dw_gate [out][in] = dg^T x,   dw_up [out][in] = du^T x.
+ * dg and du are rounded to `type` between the products (they are operands of the tensor cores), the results once.
+ * act'(0) of FS_ACT_RELU is 0. Sums over nothing (rows or out 0) are 0.
+ */
+typedef struct {
+    int32_t rows;
+    int32_t in;
+    int32_t out;
+    int32_t type;
+    int32_t activation;
+    int32_t reserved;
+    fs_mm_rows x;
+    fs_mm_rows w_gate;
+    fs_mm_rows w_up;
+    fs_mm_rows dy;
+    fs_mm_rows dx;
+    fs_mm_rows dw_gate;
+    fs_mm_rows dw_up;
+} fs_mm_gated_grad;
+
+int fs_gated_ff_backward(const fs_mm_gated_grad *args, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/*
+ * fs_quantise_rows -- 16-bit rows x [rows][in] (type FS_KV_BF16 or FS_KV_FP16) as e4m3 codes [rows][in] with a scale a row:
+ * scale[t] is the least power of two s >= 2^-126 with |x| <= 448 s for the row's finite values (0 if they are all 0), codes
+ * are x / s rounded to nearest even (0 where s is 0). What is not finite becomes a NaN code. x and codes as fs_mm_rows.
+ */
+int fs_quantise_rows(int32_t rows, int32_t in, int32_t type, const fs_mm_rows *x, const fs_mm_rows *codes, float *scale,
+                     void *cuda_stream);
+
+/* Waits for cuda_stream and reports what the calls on this workspace met since the last check
+ * (FS_ETIMEOUT); clears the status word. */
+int fs_mm_check(void *workspace, void *cuda_stream);
+
 /* Kernels this library has launched since it was loaded (all models). */
 uint64_t fs_launch_count(void);
 

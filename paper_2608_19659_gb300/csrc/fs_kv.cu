@@ -14,6 +14,28 @@ namespace fs {
 
 int record_error(int code, const char* msg);
 
+// The driver's encoder, looked up once (the library does not link libcuda).
+EncodeTiled encode_tiled() {
+  static const EncodeTiled f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+        r != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiled>(p);
+  }();
+  return f;
+}
+
+int sm_count_of(int dev) {
+  static std::atomic<int> known[64];
+  if (dev < 0 || dev >= 64) return 0;
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (!n && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess)
+    known[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
 namespace {
 
 int say(int code, const char* fmt, ...) {
@@ -694,32 +716,6 @@ cudaError_t launch_append(const KvAppendArgs& a, int pieces, bool many, cudaStre
   if (its == 4) return launch_pdl(k_kv_append_many<D, T, 4, 128>, grid, dim3(128), 0, s, a);
   if (its == 8) return launch_pdl(k_kv_append_many<D, T, 4, 256>, grid, dim3(256), 0, s, a);
   return launch_pdl(k_kv_append_many<D, T, 4, 512>, grid, dim3(512), 0, s, a);
-}
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's encoder, looked up once (the library does not link libcuda).
-EncodeTiled encode_tiled() {
-  static const EncodeTiled f = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult r;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
-        r != cudaDriverEntryPointSuccess)
-      p = nullptr;
-    return reinterpret_cast<EncodeTiled>(p);
-  }();
-  return f;
-}
-
-int sm_count_of(int dev) {
-  static std::atomic<int> known[64];
-  if (dev < 0 || dev >= 64) return 0;
-  int n = known[dev].load(std::memory_order_relaxed);
-  if (!n && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess)
-    known[dev].store(n, std::memory_order_relaxed);
-  return n;
 }
 
 // How an attend call is cut up (see k_kv_decode): rows of a (sequence, key head) in tiles

@@ -175,6 +175,12 @@ inline cudaError_t smem_limit_once(std::atomic<uint64_t>& seen, const void* kern
   return e;
 }
 
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled();  // null: the driver has none
+int sm_count_of(int dev);    // 0: not known
+
 // A tensor map of a cache tensor: [pages][heads][page tokens][dim] bytes in tiles of
 // `rows` tokens of one (page, head), its 16-byte pieces swizzled over the rows or in order.
 int kv_tensor_map(CUtensorMap* m, const fs_kv_cache& c, const void* base, int rows, bool swizzled);

@@ -29,8 +29,10 @@ EXPORTS = ("fs_load_model", "fs_update_bounds", "fs_set_floors", "fs_dump_stride
            "fs_watchdog_selftest", "fs_free_model", "fs_last_error", "fs_score_candidates_noalloc",
            "fs_timing_enable",
            "fs_timing_read", "fs_draw_floor", "fs_kv_workspace_bytes", "fs_kv_append", "fs_kv_attend",
-           "fs_kv_check")
-FS_KV_BF16, FS_KV_FP16 = 0, 1
+           "fs_kv_check", "fs_mm_workspace_bytes", "fs_linear", "fs_gated_ff", "fs_gated_ff_backward",
+           "fs_quantise_rows", "fs_mm_check")
+FS_KV_BF16, FS_KV_FP16, FS_E4M3 = 0, 1, 2
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}  # FS_ACT_*
 
 
 class FleetSieveError(RuntimeError):
@@ -96,6 +98,27 @@ class fs_kv_query(C.Structure):
                 ("window", C.c_int32), ("q", fs_kv_rows), ("out", fs_kv_rows)]
 
 
+class fs_mm_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("scale", C.c_void_p)]
+
+
+_MM_HEAD = [(n, C.c_int32) for n in ("rows", "in_", "out", "type", "out_type", "activation")]
+
+
+class fs_mm_linear(C.Structure):
+    _fields_ = _MM_HEAD + [("x", fs_mm_rows), ("w", fs_mm_rows), ("residual", fs_mm_rows), ("y", fs_mm_rows),
+                           ("bias", C.c_void_p)]
+
+
+class fs_mm_gated(C.Structure):
+    _fields_ = _MM_HEAD + [("x", fs_mm_rows), ("w_gate", fs_mm_rows), ("w_up", fs_mm_rows), ("y", fs_mm_rows)]
+
+
+class fs_mm_gated_grad(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("rows", "in_", "out", "type", "activation", "reserved")]
+                + [(n, fs_mm_rows) for n in ("x", "w_gate", "w_up", "dy", "dx", "dw_gate", "dw_up")])
+
+
 ALLOC_DTYPE = np.dtype({"names": ["t_star", "total_gpus", "has_option_mask", "ok", "floors_met",
                                   "tp", "bin", "replicas", "fulfil", "goodput"],
                         "formats": [np.float32, np.int32, np.uint64, np.int32, np.int32,
@@ -158,6 +181,11 @@ def lib():
         L.fs_kv_attend.argtypes = [C.POINTER(fs_kv_cache), C.POINTER(fs_kv_batch), C.c_void_p,
                                    C.c_void_p, C.c_int64, C.c_void_p]
         L.fs_kv_check.argtypes = [C.c_void_p, C.c_void_p]
+        L.fs_mm_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
+        for f in (L.fs_linear, L.fs_gated_ff, L.fs_gated_ff_backward):
+            f.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
+        L.fs_quantise_rows.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.fs_mm_check.argtypes = [C.c_void_p, C.c_void_p]
         L.fs_free_model.argtypes = [C.c_void_p]
         L.fs_free_model.restype = None
         L.fs_last_error.restype = C.c_char_p
@@ -719,6 +747,158 @@ def fs_kv_check(workspace: KvWorkspace, stream=None) -> None:
     if workspace.index != _current_device():
         _kv_refuse_devices(workspace)
     _check(lib().fs_kv_check(workspace.address, _kv_stream(stream, workspace.index)))
+
+
+# ---- the products of a rank's layer
+
+class MmWorkspace:
+    """Device memory of the current device for products of these sizes, or smaller ones, one after the other
+    (``backward``: for fs_gated_ff_backward too)."""
+
+    def __init__(self, rows: int, in_features: int, out_features: int, backward: bool = False):
+        import torch
+
+        n = C.c_int64()
+        _check(lib().fs_mm_workspace_bytes(int(rows), int(in_features), int(out_features), int(backward), C.byref(n)))
+        self.index = _current_device()
+        self.tensor = torch.zeros(n.value, dtype=torch.uint8, device=f"cuda:{self.index}")
+        self.address, self.bytes = self.tensor.data_ptr(), n.value
+
+
+_mm_kinds = {}  # torch dtype -> FS_KV_* or FS_E4M3
+
+
+def _mm_type(t, name: str) -> int:
+    if not _mm_kinds:
+        import torch
+
+        _mm_kinds.update({torch.bfloat16: FS_KV_BF16, torch.float16: FS_KV_FP16, torch.float8_e4m3fn: FS_E4M3})
+    kind = _mm_kinds.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{name} is {t.dtype}, not bfloat16, float16 or float8_e4m3fn")
+    return kind
+
+
+def _mm_rows(t, name: str, dtype, index: int, rows: int, width: int, scale=None) -> tuple[int, int, int]:
+    """(address, stride, address of the scales) of rows [rows, width]."""
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != rows or shape[1] != width:
+        raise ValueError(f"{name} is [{rows}, {width}], not {tuple(shape)}")
+    s0, s1 = t.stride()
+    if t.dtype is not dtype or t.get_device() != index or (s1 != 1 and width > 1 and rows):
+        raise ValueError(f"{name}: want {dtype} on cuda:{index}, the last dimension contiguous")
+    at = 0
+    if scale is not None:
+        if (scale.dim() != 1 or scale.shape[0] != rows or scale.element_size() != 4 or not scale.is_floating_point()
+                or not scale.is_contiguous() or scale.get_device() != index):
+            raise ValueError(f"{name}: scales are a contiguous float32 [{rows}] on cuda:{index}")
+        at = scale.data_ptr()
+    return t.data_ptr(), s0, at
+
+
+def _mm_act(activation: str) -> int:
+    act = ACTIVATIONS.get(activation)
+    if act is None:
+        raise ValueError(f"activation {activation!r} is none of {', '.join(ACTIVATIONS)}")
+    return act
+
+
+def _mm_here(workspace: MmWorkspace) -> int:
+    """The workspace's device, which has to be the current one: calls are launched there."""
+    index = workspace.index
+    if index != _current_device():
+        raise ValueError(f"cuda:{_current_device()} is current, the workspace is on cuda:{index}")
+    return index
+
+
+_NO_ROWS = (0, 0, 0)
+_MM_LINEAR = struct.Struct("=6i" + 4 * "Qqq" + "Q")
+_MM_GATED = struct.Struct("=6i" + 4 * "Qqq")
+_MM_GRAD = struct.Struct("=6i" + 7 * "Qqq")
+
+
+def fs_linear(x, w, y, *, bias=None, residual=None, activation: str = "none", x_scale=None, w_scale=None,
+              workspace: MmWorkspace, stream=None):
+    """y [rows, out] = act(x [rows, in] w [out, in]^T + bias) + residual, enqueued on ``stream`` (default: torch's
+    current one). x and w: both bfloat16, both float16, or both float8_e4m3fn with x_scale [rows] and w_scale [out]; bias,
+    residual and y: bfloat16 or float16 (x's type if that is 16-bit). y may be the residual. Returns y."""
+    index = _mm_here(workspace)
+    kind, out_kind, act = _mm_type(x, "x"), _mm_type(y, "y"), _mm_act(activation)
+    (rows, inner), out, dtype = x.shape, w.shape[0], y.dtype
+    xr = _mm_rows(x, "x", x.dtype, index, rows, inner, x_scale)
+    wr = _mm_rows(w, "w", x.dtype, index, out, inner, w_scale)
+    yr = _mm_rows(y, "y", dtype, index, rows, out)
+    rr = _NO_ROWS if residual is None else _mm_rows(residual, "residual", dtype, index, rows, out)
+    b = 0
+    if bias is not None:
+        if bias.dim() != 1 or bias.shape[0] != out or bias.dtype is not dtype or bias.get_device() != index or not bias.is_contiguous():
+            raise ValueError(f"bias is a contiguous {dtype} [{out}] on cuda:{index}")
+        b = bias.data_ptr()
+    a = _MM_LINEAR.pack(rows, inner, out, kind, out_kind, act, *xr, *wr, *rr, *yr, b)
+    rc = lib().fs_linear(a, workspace.address, workspace.bytes, _kv_stream(stream, index))
+    if rc:
+        _check(rc)
+    return y
+
+
+def fs_gated_ff(x, w_gate, w_up, y, *, activation: str = "silu", x_scale=None, gate_scale=None, up_scale=None,
+                workspace: MmWorkspace, stream=None):
+    """y [rows, out] = act(x w_gate^T) * (x w_up^T), types as in :func:`fs_linear`. Returns y."""
+    index = _mm_here(workspace)
+    kind, out_kind, act = _mm_type(x, "x"), _mm_type(y, "y"), _mm_act(activation)
+    (rows, inner), out = x.shape, w_gate.shape[0]
+    xr = _mm_rows(x, "x", x.dtype, index, rows, inner, x_scale)
+    gr = _mm_rows(w_gate, "w_gate", x.dtype, index, out, inner, gate_scale)
+    ur = _mm_rows(w_up, "w_up", x.dtype, index, out, inner, up_scale)
+    yr = _mm_rows(y, "y", y.dtype, index, rows, out)
+    a = _MM_GATED.pack(rows, inner, out, kind, out_kind, act, *xr, *gr, *ur, *yr)
+    rc = lib().fs_gated_ff(a, workspace.address, workspace.bytes, _kv_stream(stream, index))
+    if rc:
+        _check(rc)
+    return y
+
+
+def fs_gated_ff_backward(x, w_gate, w_up, dy, dx, dw_gate, dw_up, *, activation: str = "silu",
+                         workspace: MmWorkspace, stream=None):
+    """The gradients of :func:`fs_gated_ff` (bfloat16 or float16 throughout), given dy, into dx, dw_gate and dw_up, which
+    it returns. ``workspace`` is one made with backward=True."""
+    index = _mm_here(workspace)
+    kind, act, dtype = _mm_type(x, "x"), _mm_act(activation), x.dtype
+    (rows, inner), out = x.shape, w_gate.shape[0]
+    parts = [_mm_rows(t, name, dtype, index, n, width) for t, name, n, width in (
+        (x, "x", rows, inner), (w_gate, "w_gate", out, inner), (w_up, "w_up", out, inner), (dy, "dy", rows, out),
+        (dx, "dx", rows, inner), (dw_gate, "dw_gate", out, inner), (dw_up, "dw_up", out, inner))]
+    a = _MM_GRAD.pack(rows, inner, out, kind, act, 0, *(v for p in parts for v in p))
+    rc = lib().fs_gated_ff_backward(a, workspace.address, workspace.bytes, _kv_stream(stream, index))
+    if rc:
+        _check(rc)
+    return dx, dw_gate, dw_up
+
+
+_MM_ROWS = struct.Struct("=Qqq")
+
+
+def fs_quantise_rows(x, codes, scale, *, stream=None):
+    """Rows x [rows, in] (bfloat16 or float16) as codes [rows, in] (float8_e4m3fn or its bytes, uint8) with a power-of-two
+    scale [rows] (float32) each, what :func:`fs_linear` and :func:`fs_gated_ff` take. Returns (codes, scale)."""
+    index, kind = x.get_device(), _mm_type(x, "x")
+    if index < 0 or index != _current_device():
+        raise ValueError(f"x is on {x.device}, cuda:{_current_device()} is current")
+    rows, inner = x.shape
+    if codes.element_size() != 1:
+        raise ValueError(f"codes are {codes.dtype}, not float8_e4m3fn or uint8")
+    xr = _mm_rows(x, "x", x.dtype, index, rows, inner)
+    cr = _mm_rows(codes, "codes", codes.dtype, index, rows, inner, scale)
+    rc = lib().fs_quantise_rows(rows, inner, kind, _MM_ROWS.pack(*xr), _MM_ROWS.pack(cr[0], cr[1], 0), cr[2], _kv_stream(stream, index))
+    if rc:
+        _check(rc)
+    return codes, scale
+
+
+def fs_mm_check(workspace: MmWorkspace, stream=None) -> None:
+    """Waits for the stream and raises what the workspace's calls met on the device."""
+    index = _mm_here(workspace)
+    _check(lib().fs_mm_check(workspace.address, _kv_stream(stream, index)))
 
 
 def dump_dtype(K: int) -> np.dtype:
