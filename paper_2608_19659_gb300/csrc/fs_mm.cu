@@ -72,6 +72,39 @@ int check_workspace(const void* ws, int64_t bytes, int64_t need) {
   return FS_OK;
 }
 
+// Rows of an operand as boxes of `box_rows` rows and 128 bytes of them, swizzled.
+int rows_map(CUtensorMap* m, const void* base, int n, int width, long long stride, int type, int box_rows) {
+  const EncodeTiled enc = encode_tiled();
+  if (!enc) return say(FS_ECUDA, "the driver has no cuTensorMapEncodeTiled");
+  const int size = type == FS_E4M3 ? 1 : 2;
+  const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)n}, strides[1] = {(cuuint64_t)stride * size};
+  const cuuint32_t box[2] = {(cuuint32_t)(kMmBlock / size), (cuuint32_t)box_rows}, step[2] = {1, 1};
+  const CUresult r = enc(m, size == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(base), dims, strides, box,
+                         step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? FS_OK : say(FS_ECUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+}
+
+// act(x W^T + bias) + residual, or with `up` the gated product, of few rows.
+int few_product(const fs_mm_rows& x, const fs_mm_rows& w, const fs_mm_rows* up, const MmEpilogue& e, int in, int type, int out_type,
+                uint32_t* status, cudaStream_t s, const char* what) {
+  int dev = 0;
+  const cudaError_t d = cudaGetDevice(&dev);
+  if (d != cudaSuccess) return cuda_say(d, "cudaGetDevice");
+  const int sms = sm_count_of(dev);
+  if (!sms) return say(FS_ECUDA, "device query failed");
+  const int per = kMmBlock / (type == FS_E4M3 ? 1 : 2), blocks = (in + per - 1) / per;
+  const MmFewPlan p = mm_few_plan(e.rows, e.cols, blocks, up, sms);
+  const int w_box = up ? p.w_rows / 2 : p.w_rows;
+  CUtensorMap mx, mw, mu;
+  if (int rc = rows_map(&mx, x.data, e.rows, in, x.stride, type, p.tokens)) return rc;
+  if (int rc = rows_map(&mw, w.data, e.cols, in, w.stride, type, w_box)) return rc;
+  if (up)
+    if (int rc = rows_map(&mu, up->data, e.cols, in, up->stride, type, w_box)) return rc;
+  const cudaError_t r = launch_mm_few(mx, mw, up ? &mu : nullptr, e, p, blocks, type, out_type, status, s);
+  return r == cudaSuccess ? FS_OK : cuda_say(r, what);
+}
+
 // ---------------------------------------------------------------- products
 
 // An operand: element (i, k) at data + i * i_step + k * k_step.
@@ -236,6 +269,9 @@ extern "C" int fs_linear(const fs_mm_linear* args, void* workspace, int64_t work
   p.a[0] = {g.x.data, g.x.stride, 1}, p.b[0] = {g.w.data, g.w.stride, 1};
   p.inner[0] = g.in, p.type = g.type;
   p.e = {g.rows, g.out, g.activation, g.x.scale, {g.w.scale, nullptr}, g.bias, g.residual.data, g.residual.stride, {g.y.data, nullptr}, g.y.stride};
+  if (g.rows <= 1024)
+    return few_product(g.x, g.w, nullptr, p.e, g.in, g.type, g.out_type, static_cast<uint32_t*>(workspace), static_cast<cudaStream_t>(cuda_stream),
+                       "launch (fs_linear)");
   const cudaError_t e = launch_mm<MM_LINEAR>(p, g.out_type, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? FS_OK : cuda_say(e, "launch (fs_linear)");
 }
@@ -255,6 +291,9 @@ extern "C" int fs_gated_ff(const fs_mm_gated* args, void* workspace, int64_t wor
   p.a[0] = {g.x.data, g.x.stride, 1}, p.b[0] = {g.w_gate.data, g.w_gate.stride, 1}, p.b[1] = {g.w_up.data, g.w_up.stride, 1};
   p.inner[0] = g.in, p.type = g.type;
   p.e = {g.rows, g.out, g.activation, g.x.scale, {g.w_gate.scale, g.w_up.scale}, nullptr, nullptr, 0, {g.y.data, nullptr}, g.y.stride};
+  if (g.rows <= 1024)
+    return few_product(g.x, g.w_gate, &g.w_up, p.e, g.in, g.type, g.out_type, static_cast<uint32_t*>(workspace),
+                       static_cast<cudaStream_t>(cuda_stream), "launch (fs_gated_ff)");
   const cudaError_t e = launch_mm<MM_GATED>(p, g.out_type, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? FS_OK : cuda_say(e, "launch (fs_gated_ff)");
 }

@@ -1,7 +1,10 @@
 // Shared parts of the products of a rank's layer (fs_mm.cu and its kernels).
 #pragma once
 
+#include <type_traits>
+
 #include "fs_kv.cuh"
+#include "fs_tc.cuh"
 
 namespace fs {
 
@@ -62,6 +65,52 @@ __device__ __forceinline__ float mm_act_slope(float z, float& slope) {
   return z;
 }
 
+// Four neighbouring values of a row, n of them inside it (all when n >= 4: then 8 bytes at once).
+template <typename T>
+__device__ __forceinline__ float4 mm_load4(const T* p, int n) {
+  if (n >= 4) {
+    const uint2 w = *reinterpret_cast<const uint2*>(p);
+    const float2 a = Elem<T>::two(w.x), b = Elem<T>::two(w.y);
+    return make_float4(a.x, a.y, b.x, b.y);
+  }
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (n > 0) v.x = (float)p[0];
+  if (n > 1) v.y = (float)p[1];
+  if (n > 2) v.z = (float)p[2];
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ void mm_store4(T* p, float4 v, int n) {
+  if (n >= 4) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(Elem<T>::pack(v.x, v.y), Elem<T>::pack(v.z, v.w));
+    return;
+  }
+  if (n > 0) p[0] = (T)v.x;
+  if (n > 1) p[1] = (T)v.y;
+  if (n > 2) p[2] = (T)v.z;
+}
+__device__ __forceinline__ float4 mm_load4(const float* p, int n) {
+  if (n >= 4) return *reinterpret_cast<const float4*>(p);
+  return make_float4(n > 0 ? p[0] : 0.f, n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, 0.f);
+}
+__device__ __forceinline__ float4 operator*(float4 a, float4 b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); }
+__device__ __forceinline__ float4 operator+(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+__device__ __forceinline__ float4 operator*(float4 a, float b) { return make_float4(a.x * b, a.y * b, a.z * b, a.w * b); }
+
+// A box of rows into shared memory: from element `x` of row `y` on.
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* m, int x, int y, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+               "l"(m), "r"(x), "r"(y), "r"(smem_u32(bar))
+               : "memory");
+}
+
+// A wait that says so when it runs out; the caller leaves its loop.
+__device__ __forceinline__ bool mm_wait(uint64_t* bar, uint32_t parity, uint32_t* status) {
+  if (mbar_wait(bar, parity, kWaitLimitNs)) return true;
+  atomicOr(status, ST_TIMEOUT);
+  return false;
+}
+
 // f with the activation as a constant.
 template <typename F>
 __device__ __forceinline__ void mm_with_act(int act, F&& f) {
@@ -73,5 +122,21 @@ __device__ __forceinline__ void mm_with_act(int act, F&& f) {
     default: f(std::integral_constant<int, FS_ACT_NONE>());
   }
 }
+
+constexpr int kMmBlock = 128;  // bytes of a row in one block of a sum
+
+// A product for k_mm_few: sums over blocks_k blocks of x rows and W rows.
+struct MmFewPlan {
+  int w_rows;     // rows of W a tile: 32, 64 or 128 (gated: half of them gate's, half up's)
+  int tokens;     // rows of x a tile: a multiple of 16, up to 128
+  int token_tiles, w_tiles;
+  int cluster;    // blocks that share a tile's sum
+  int stages;
+  size_t smem;
+};
+MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms);
+// x and one or two W, each in boxes of one block and the plan's rows.
+cudaError_t launch_mm_few(const CUtensorMap& x, const CUtensorMap& w, const CUtensorMap* up, const MmEpilogue& e, const MmFewPlan& p,
+                          int blocks_k, int type, int out_type, uint32_t* status, cudaStream_t s);
 
 }  // namespace fs

@@ -45,4 +45,46 @@ __device__ __forceinline__ void tmem_ld16(uint32_t (&r)[16], uint32_t a) {
       : "memory");
 }
 
+// Instruction descriptor of products into floats: m rows and n columns; `format` of both operands (kind::f16: 0 half, 1 bfloat16;
+// kind::f8f6f4: 0 e4m3); a_mn, b_mn: the operand's rows are contiguous, not its sums' terms.
+__host__ __device__ constexpr uint32_t mm_instr(int m, int n, int format, bool a_mn = false, bool b_mn = false) {
+  return 1u << 4 | (uint32_t)format << 7 | (uint32_t)format << 10 | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) |
+         (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
+}
+
+// All blocks of the cluster.
+__device__ __forceinline__ void cluster_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// The address in block `rank` of what this block has at a.
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t a, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  return r;
+}
+
+// Launch of clusters of `cluster` blocks, beside the end of the kernel ahead (launch_pdl).
+template <typename... KArgs, typename... Args>
+cudaError_t launch_clusters(void (*kernel)(KArgs...), dim3 grid, dim3 block, int cluster, size_t smem, cudaStream_t s, Args&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {(unsigned)cluster, 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  note_launch();
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<Args&&>(args)...);
+}
+
 }  // namespace fs
