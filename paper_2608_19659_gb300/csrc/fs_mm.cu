@@ -85,117 +85,56 @@ int rows_map(CUtensorMap* m, const void* base, int n, int width, long long strid
   return r == CUDA_SUCCESS ? FS_OK : say(FS_ECUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }
 
-// act(x W^T + bias) + residual, or with `up` the gated product, of few rows.
-int few_product(const fs_mm_rows& x, const fs_mm_rows& w, const fs_mm_rows* up, const MmEpilogue& e, int in, int type, int out_type,
-                uint32_t* status, cudaStream_t s, const char* what) {
+// What every product needs of its call.
+struct MmCall {
+  int in, type, out_type, sms;
+  uint32_t* status;
+  cudaStream_t stream;
+  const char* what;  // for errors
+  int blocks() const { return (in + per() - 1) / per(); }
+  int per() const { return kMmBlock / (type == FS_E4M3 ? 1 : 2); }
+};
+
+int device_sms(int* sms) {
   int dev = 0;
-  const cudaError_t d = cudaGetDevice(&dev);
-  if (d != cudaSuccess) return cuda_say(d, "cudaGetDevice");
-  const int sms = sm_count_of(dev);
-  if (!sms) return say(FS_ECUDA, "device query failed");
-  const int per = kMmBlock / (type == FS_E4M3 ? 1 : 2), blocks = (in + per - 1) / per;
-  const MmFewPlan p = mm_few_plan(e.rows, e.cols, blocks, up, sms);
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_say(e, "cudaGetDevice");
+  *sms = sm_count_of(dev);
+  return *sms ? FS_OK : say(FS_ECUDA, "device query failed");
+}
+
+// act(x W^T + bias) + residual, or with `up` the gated product, of few rows.
+int few_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const fs_mm_rows* up, const MmEpilogue& e) {
+  const MmFewPlan p = mm_few_plan(e.rows, e.cols, c.blocks(), up, c.sms);
   const int w_box = up ? p.w_rows / 2 : p.w_rows;
   CUtensorMap mx, mw, mu;
-  if (int rc = rows_map(&mx, x.data, e.rows, in, x.stride, type, p.tokens)) return rc;
-  if (int rc = rows_map(&mw, w.data, e.cols, in, w.stride, type, w_box)) return rc;
+  if (int rc = rows_map(&mx, x.data, e.rows, c.in, x.stride, c.type, p.tokens)) return rc;
+  if (int rc = rows_map(&mw, w.data, e.cols, c.in, w.stride, c.type, w_box)) return rc;
   if (up)
-    if (int rc = rows_map(&mu, up->data, e.cols, in, up->stride, type, w_box)) return rc;
-  const cudaError_t r = launch_mm_few(mx, mw, up ? &mu : nullptr, e, p, blocks, type, out_type, status, s);
-  return r == cudaSuccess ? FS_OK : cuda_say(r, what);
+    if (int rc = rows_map(&mu, up->data, e.cols, c.in, up->stride, c.type, w_box)) return rc;
+  const cudaError_t r = launch_mm_few(mx, mw, up ? &mu : nullptr, e, p, c.blocks(), c.type, c.out_type, c.status, c.stream);
+  return r == cudaSuccess ? FS_OK : cuda_say(r, c.what);
 }
 
-// ---------------------------------------------------------------- products
-
-// An operand: element (i, k) at data + i * i_step + k * k_step.
-struct MmOperand {
-  const void* data;
-  long long i_step, k_step;
-};
-
-enum { MM_LINEAR, MM_GATED, MM_BACK };
-
-struct MmArgs {
-  MmOperand a[2], b[2];  // sums of MM_LINEAR run over a[0] b[0], then a[1] b[1]; MM_GATED, MM_BACK: a[0] with each b
-  int inner[2];          // (of MM_LINEAR's second sum: 0 is none)
-  int type;
-  MmEpilogue e;
-};
-
-__device__ __forceinline__ float load_any(const MmOperand& o, int type, long long i, int k) {
-  const long long at = i * o.i_step + k * o.k_step;
-  if (type == FS_KV_BF16) return __uint_as_float((uint32_t) static_cast<const uint16_t*>(o.data)[at] << 16);
-  if (type == FS_KV_FP16) return __half2float(static_cast<const __half*>(o.data)[at]);
-  const uint32_t c = static_cast<const uint8_t*>(o.data)[at];
-  const uint32_t h = e4m3x2_to_f16x2(c);
-  return __half2float(__ushort_as_half((unsigned short)h));
+// The same of many rows; with e.out[1] the first product of a backward pass.
+int wide_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const fs_mm_rows* up, const MmEpilogue& e) {
+  MmWideArgs a{};
+  if (int rc = rows_map(&a.maps[0], x.data, e.rows, c.in, x.stride, c.type, 128)) return rc;
+  if (int rc = rows_map(&a.maps[1], w.data, e.cols, c.in, w.stride, c.type, 128)) return rc;
+  if (up)
+    if (int rc = rows_map(&a.maps[2], up->data, e.cols, c.in, up->stride, c.type, 128)) return rc;
+  a.product[0] = {e, {0, 0}, {1, 2}, {c.blocks(), 0}, false, false, 0};
+  a.products = 1;
+  a.status = c.status;
+  const cudaError_t r = launch_mm_wide(a, e.out[1] ? MM_BACK : up ? MM_GATED : MM_LINEAR, c.type, c.out_type, c.sms, c.stream);
+  return r == cudaSuccess ? FS_OK : cuda_say(r, c.what);
 }
 
-// A tile of 64 x 64 results a block, 16 sums (of each product) a thread.
-template <typename T, int kMode>
-__global__ void __launch_bounds__(256) k_mm_simple(const MmArgs p) {
-  constexpr int kB = kMode == MM_LINEAR ? 1 : 2;
-  __shared__ float as[16][65], bs[kB][16][65];
-  pdl_trigger();
-  pdl_wait();
-  const MmEpilogue& e = p.e;
-  const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[kB][4][4] = {};
-  for (int part = 0; part < (kMode == MM_LINEAR ? 2 : 1); ++part) {
-    for (int k0 = 0; k0 < p.inner[part]; k0 += 16) {
-      for (int i = threadIdx.x; i < 1024; i += 256) {
-        const int r = i >> 4, k = i & 15;
-        const bool in = k0 + k < p.inner[part];
-        as[k][r] = in && m0 + r < e.rows ? load_any(p.a[part], p.type, m0 + r, k0 + k) : 0.f;
-#pragma unroll
-        for (int b = 0; b < kB; ++b) bs[b][k][r] = in && n0 + r < e.cols ? load_any(p.b[part + b], p.type, n0 + r, k0 + k) : 0.f;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < 16; ++k)
-#pragma unroll
-        for (int b = 0; b < kB; ++b)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[b][i][j] = fmaf(as[k][ty * 4 + i], bs[b][k][tx * 4 + j], acc[b][i][j]);
-      __syncthreads();
-    }
-  }
-  mm_with_act(e.act, [&](auto act) {
-    constexpr int kAct = decltype(act)::value;
-    for (int i = 0; i < 4; ++i)
-      for (int j = 0; j < 4; ++j) {
-        const int m = m0 + ty * 4 + i, n = n0 + tx * 4 + j;
-        if (m >= e.rows || n >= e.cols) continue;
-        float z[2] = {acc[0][i][j], acc[kB - 1][i][j]};
-        if (e.x_scale)
-          for (int b = 0; b < kB; ++b) z[b] = z[b] * e.x_scale[m] * e.w_scale[b][n];
-        T* out = static_cast<T*>(e.out[0]) + m * e.out_stride + n;
-        const T* in = e.in ? static_cast<const T*>(e.in) + m * e.in_stride + n : nullptr;
-        if (kMode == MM_LINEAR) {
-          float y = z[0];
-          if (e.bias) y += (float)static_cast<const T*>(e.bias)[n];
-          y = mm_act<kAct>(y);
-          if (in) y += (float)*in;
-          *out = (T)y;
-        } else if (kMode == MM_GATED) {
-          *out = (T)(mm_act<kAct>(z[0]) * z[1]);
-        } else {
-          float slope;
-          const float a = mm_act_slope<kAct>(z[0], slope), dy = (float)*in;
-          *out = (T)(dy * z[1] * slope);
-          static_cast<T*>(e.out[1])[m * e.out_stride + n] = (T)(dy * a);
-        }
-      }
-  });
-}
-
-template <int kMode>
-cudaError_t launch_mm(const MmArgs& p, int out_type, cudaStream_t s) {
-  const dim3 grid((p.e.cols + 63) / 64, (p.e.rows + 63) / 64);
-  return out_type == FS_KV_FP16 ? launch_pdl(k_mm_simple<__half, kMode>, grid, dim3(256), 0, s, p)
-                                : launch_pdl(k_mm_simple<__nv_bfloat16, kMode>, grid, dim3(256), 0, s, p);
+int product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const fs_mm_rows* up, const MmEpilogue& e) {
+  // pairs of SMs where their tiles are enough for half of them
+  const long long tiles = (long long)((e.rows + 255) / 256) * ((e.cols + (up ? 127 : 255)) / (up ? 128 : 256));
+  const bool few = e.rows <= 128 || (e.rows <= 1024 && tiles < c.sms / 4);
+  return few ? few_product(c, x, w, up, e) : wide_product(c, x, w, up, e);
 }
 
 // ---------------------------------------------------------------- rows to e4m3
@@ -265,15 +204,10 @@ extern "C" int fs_linear(const fs_mm_linear* args, void* workspace, int64_t work
   if (g.residual.data)
     if (int rc = check_rows(g.residual, "residual", g.rows, g.out, g.out_type, true)) return rc;
   if (!aligned(g.bias, 16)) return say(FS_EINVAL, "bias is not 16-byte aligned");
-  MmArgs p{};
-  p.a[0] = {g.x.data, g.x.stride, 1}, p.b[0] = {g.w.data, g.w.stride, 1};
-  p.inner[0] = g.in, p.type = g.type;
-  p.e = {g.rows, g.out, g.activation, g.x.scale, {g.w.scale, nullptr}, g.bias, g.residual.data, g.residual.stride, {g.y.data, nullptr}, g.y.stride};
-  if (g.rows <= 1024)
-    return few_product(g.x, g.w, nullptr, p.e, g.in, g.type, g.out_type, static_cast<uint32_t*>(workspace), static_cast<cudaStream_t>(cuda_stream),
-                       "launch (fs_linear)");
-  const cudaError_t e = launch_mm<MM_LINEAR>(p, g.out_type, static_cast<cudaStream_t>(cuda_stream));
-  return e == cudaSuccess ? FS_OK : cuda_say(e, "launch (fs_linear)");
+  MmCall c{g.in, g.type, g.out_type, 0, static_cast<uint32_t*>(workspace), static_cast<cudaStream_t>(cuda_stream), "launch (fs_linear)"};
+  if (int rc = device_sms(&c.sms)) return rc;
+  return product(c, g.x, g.w, nullptr,
+                 {g.rows, g.out, g.activation, g.x.scale, {g.w.scale, nullptr}, g.bias, g.residual.data, g.residual.stride, {g.y.data, nullptr}, g.y.stride});
 }
 
 extern "C" int fs_gated_ff(const fs_mm_gated* args, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
@@ -287,15 +221,10 @@ extern "C" int fs_gated_ff(const fs_mm_gated* args, void* workspace, int64_t wor
   if (int rc = check_rows(g.w_gate, "w_gate", g.out, g.in, g.type)) return rc;
   if (int rc = check_rows(g.w_up, "w_up", g.out, g.in, g.type)) return rc;
   if (int rc = check_rows(g.y, "y", g.rows, g.out, g.out_type)) return rc;
-  MmArgs p{};
-  p.a[0] = {g.x.data, g.x.stride, 1}, p.b[0] = {g.w_gate.data, g.w_gate.stride, 1}, p.b[1] = {g.w_up.data, g.w_up.stride, 1};
-  p.inner[0] = g.in, p.type = g.type;
-  p.e = {g.rows, g.out, g.activation, g.x.scale, {g.w_gate.scale, g.w_up.scale}, nullptr, nullptr, 0, {g.y.data, nullptr}, g.y.stride};
-  if (g.rows <= 1024)
-    return few_product(g.x, g.w_gate, &g.w_up, p.e, g.in, g.type, g.out_type, static_cast<uint32_t*>(workspace),
-                       static_cast<cudaStream_t>(cuda_stream), "launch (fs_gated_ff)");
-  const cudaError_t e = launch_mm<MM_GATED>(p, g.out_type, static_cast<cudaStream_t>(cuda_stream));
-  return e == cudaSuccess ? FS_OK : cuda_say(e, "launch (fs_gated_ff)");
+  MmCall c{g.in, g.type, g.out_type, 0, static_cast<uint32_t*>(workspace), static_cast<cudaStream_t>(cuda_stream), "launch (fs_gated_ff)"};
+  if (int rc = device_sms(&c.sms)) return rc;
+  return product(c, g.x, g.w_gate, &g.w_up,
+                 {g.rows, g.out, g.activation, g.x.scale, {g.w_gate.scale, g.w_up.scale}, nullptr, nullptr, 0, {g.y.data, nullptr}, g.y.stride});
 }
 
 extern "C" int fs_gated_ff_backward(const fs_mm_gated_grad* args, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
@@ -311,37 +240,41 @@ extern "C" int fs_gated_ff_backward(const fs_mm_gated_grad* args, void* workspac
   if (int rc = check_rows(g.dx, "dx", g.rows, g.in, g.type)) return rc;
   if (int rc = check_rows(g.dw_gate, "dw_gate", g.out, g.in, g.type)) return rc;
   if (int rc = check_rows(g.dw_up, "dw_up", g.out, g.in, g.type)) return rc;
-  const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  cudaError_t e = cudaSuccess;
+  MmCall c{g.in, g.type, g.type, 0, static_cast<uint32_t*>(workspace), static_cast<cudaStream_t>(cuda_stream), "launch (fs_gated_ff_backward)"};
   if (g.rows == 0 || g.out == 0) {  // sums over nothing
+    cudaError_t e = cudaSuccess;
     auto clear = [&](const fs_mm_rows& r, int n) {
-      if (n && e == cudaSuccess) e = cudaMemset2DAsync(r.data, 2 * r.stride, 0, 2 * (size_t)g.in, n, s);
+      if (n && e == cudaSuccess) e = cudaMemset2DAsync(r.data, 2 * r.stride, 0, 2 * (size_t)g.in, n, c.stream);
     };
     clear(g.dx, g.rows), clear(g.dw_gate, g.out), clear(g.dw_up, g.out);
     return e == cudaSuccess ? FS_OK : cuda_say(e, "clear (fs_gated_ff_backward)");
   }
+  if (int rc = device_sms(&c.sms)) return rc;
+  // dg and du, then everything that is made of them in one launch
   const long long ld = padded(g.out);
   char* dg = static_cast<char*>(workspace) + kMmPartAt;
   char* du = dg + 2 * g.rows * ld;
-  MmArgs p{};
-  p.a[0] = {g.x.data, g.x.stride, 1}, p.b[0] = {g.w_gate.data, g.w_gate.stride, 1}, p.b[1] = {g.w_up.data, g.w_up.stride, 1};
-  p.inner[0] = g.in, p.type = g.type;
-  p.e = {g.rows, g.out, g.activation, nullptr, {}, nullptr, g.dy.data, g.dy.stride, {dg, du}, ld};
-  e = launch_mm<MM_BACK>(p, g.type, s);
-  if (e == cudaSuccess) {
-    p.a[0] = {dg, ld, 1}, p.a[1] = {du, ld, 1}, p.b[0] = {g.w_gate.data, 1, g.w_gate.stride}, p.b[1] = {g.w_up.data, 1, g.w_up.stride};
-    p.inner[0] = p.inner[1] = g.out;
-    p.e = {g.rows, g.in, FS_ACT_NONE, nullptr, {}, nullptr, nullptr, 0, {g.dx.data, nullptr}, g.dx.stride};
-    e = launch_mm<MM_LINEAR>(p, g.type, s);
-  }
-  for (int i = 0; i < 2 && e == cudaSuccess; ++i) {
-    const fs_mm_rows& dw = i ? g.dw_up : g.dw_gate;
-    p.a[0] = {i ? du : dg, 1, ld}, p.b[0] = {g.x.data, 1, g.x.stride};
-    p.inner[0] = g.rows, p.inner[1] = 0;
-    p.e = {g.out, g.in, FS_ACT_NONE, nullptr, {}, nullptr, nullptr, 0, {dw.data, nullptr}, dw.stride};
-    e = launch_mm<MM_LINEAR>(p, g.type, s);
-  }
-  return e == cudaSuccess ? FS_OK : cuda_say(e, "launch (fs_gated_ff_backward)");
+  if (int rc = wide_product(c, g.x, g.w_gate, &g.w_up,
+                            {g.rows, g.out, g.activation, nullptr, {}, nullptr, g.dy.data, g.dy.stride, {dg, du}, ld}))
+    return rc;
+  MmWideArgs a{};
+  enum { DG, DU, WG_T, WU_T, DG_T, DU_T, X_T };
+  if (int rc = rows_map(&a.maps[DG], dg, g.rows, g.out, ld, g.type, 128)) return rc;
+  if (int rc = rows_map(&a.maps[DU], du, g.rows, g.out, ld, g.type, 128)) return rc;
+  if (int rc = rows_map(&a.maps[WG_T], g.w_gate.data, g.out, g.in, g.w_gate.stride, g.type, 64)) return rc;
+  if (int rc = rows_map(&a.maps[WU_T], g.w_up.data, g.out, g.in, g.w_up.stride, g.type, 64)) return rc;
+  if (int rc = rows_map(&a.maps[DG_T], dg, g.rows, g.out, ld, g.type, 64)) return rc;
+  if (int rc = rows_map(&a.maps[DU_T], du, g.rows, g.out, ld, g.type, 64)) return rc;
+  if (int rc = rows_map(&a.maps[X_T], g.x.data, g.rows, g.in, g.x.stride, g.type, 64)) return rc;
+  auto to = [&](const fs_mm_rows& r, int n) { return MmEpilogue{n, g.in, FS_ACT_NONE, nullptr, {}, nullptr, nullptr, 0, {r.data, nullptr}, r.stride}; };
+  const int out_blocks = (g.out + 63) / 64, row_blocks = (g.rows + 63) / 64;
+  a.product[0] = {to(g.dx, g.rows), {DG, DU}, {WG_T, WU_T}, {out_blocks, out_blocks}, false, true, 0};
+  a.product[1] = {to(g.dw_gate, g.out), {DG_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, 0};
+  a.product[2] = {to(g.dw_up, g.out), {DU_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, 0};
+  a.products = 3;
+  a.status = c.status;
+  const cudaError_t e = launch_mm_wide(a, MM_LINEAR, g.type, g.type, c.sms, c.stream);
+  return e == cudaSuccess ? FS_OK : cuda_say(e, c.what);
 }
 
 extern "C" int fs_quantise_rows(int32_t rows, int32_t in, int32_t type, const fs_mm_rows* x, const fs_mm_rows* codes, float* scale,

@@ -97,6 +97,9 @@ __device__ __forceinline__ float4 operator*(float4 a, float4 b) { return make_fl
 __device__ __forceinline__ float4 operator+(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 __device__ __forceinline__ float4 operator*(float4 a, float b) { return make_float4(a.x * b, a.y * b, a.z * b, a.w * b); }
 
+// What kernels ahead stored, for the copies of this thread.
+__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
 // A box of rows into shared memory: from element `x` of row `y` on.
 __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* m, int x, int y, uint64_t* bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
@@ -138,5 +141,25 @@ MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms);
 // x and one or two W, each in boxes of one block and the plan's rows.
 cudaError_t launch_mm_few(const CUtensorMap& x, const CUtensorMap& w, const CUtensorMap* up, const MmEpilogue& e, const MmFewPlan& p,
                           int blocks_k, int type, int out_type, uint32_t* status, cudaStream_t s);
+
+enum { MM_LINEAR, MM_GATED, MM_BACK };
+
+// One product of a launch of k_mm_wide: e.rows x e.cols results, sums over blocks[0] blocks of maps a[0] and b[0], then over blocks[1]
+// of a[1] and b[1] (MM_GATED, MM_BACK: a[0] with b[0] for gate and b[1] for up). Maps have boxes of 128 rows and one block, or, of an
+// operand whose rows are contiguous (a_mn, b_mn), of 64 of them and 64 terms of the sum.
+struct MmProduct {
+  MmEpilogue e;
+  int a[2], b[2], blocks[2];
+  bool a_mn, b_mn;
+  long long tiles;  // (launch_mm_wide's)
+};
+struct MmWideArgs {
+  CUtensorMap maps[8];
+  MmProduct product[3];
+  int products, eight, format;
+  long long tiles;
+  uint32_t* status;
+};
+cudaError_t launch_mm_wide(MmWideArgs& a, int mode, int type, int out_type, int sms, cudaStream_t s);
 
 }  // namespace fs

@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
 
   if (w == 0 && lane == 0) {
     // ---------------------------------------------------------------- copies
+    fence_proxy_async_all();
     const int step = a.eight ? kMmBlock : kMmBlock / 2;
     int st = 0, k = k0;
     uint32_t par = 1;

@@ -1,0 +1,328 @@
+// Products of many rows: pairs of SMs on tiles of 256 x 256, tcgen05.
+//
+// A cluster of two blocks holds a tile: each block loads its 128 rows of A and its 128 of B (half of what one SM
+// alone would read for a tile of that shape), one thread of the first issues the products of both
+// (cta_group::2), and each block has its 128 rows' 256 sums in its tensor memory, twice: while four warps finish a tile and store
+// it, the next one's sums are under way. Blocks stay for the whole launch and walk over the tiles, eight tiles of rows wide,
+// so that what is resident at a time shares its rows of W through the L2.
+// A launch holds up to three products (the backward pass: dx and both dW), whose sums may have two parts (dx: over gate
+// and up) and whose operands may lie either way (dx reads W, dW reads both, across their rows).
+// Of a gated block the first SM of a pair loads gate's rows and the second up's, so that a thread has both sums of a result.
+#include <algorithm>
+#include <atomic>
+
+#include "fs_mm.cuh"
+
+namespace fs {
+namespace {
+
+constexpr int kStages = 7, kHalf = 128 * kMmBlock, kStage = 2 * kHalf;
+constexpr int kTile = 256;
+constexpr int kGroup = 8;  // tiles of rows that are walked over together
+
+struct WideBars {
+  uint64_t full[kStages], empty[kStages], sum_full[2], sum_empty[2];
+  uint32_t tmem;
+};
+// All of an SM's shared memory: no block with tensor memory of its own fits beside one of these, which
+// take all of it. (One that held some while it waits for its cluster, and this pair for each other: none would go on.)
+constexpr size_t kSmem = 1024 + kStages * kStage + sizeof(WideBars);
+static_assert(kSmem > 220 * 1024 && kSmem <= 227 * 1024, "an SM's shared memory, all of it");
+
+// One tile: of product `p`, rows from m0 and columns (gated: results) from n0.
+struct Tile {
+  const MmProduct* p;
+  int m0, n0;
+};
+
+template <int kMode>
+__device__ __forceinline__ Tile tile_of(const MmWideArgs& a, long long i) {
+  int q = 0;
+  while (q + 1 < a.products && i >= a.product[q].tiles) i -= a.product[q++].tiles;
+  const MmProduct& p = a.product[q];
+  const int tm = (p.e.rows + kTile - 1) / kTile;
+  const int tn = (int)(p.tiles / tm);
+  const long long per = (long long)kGroup * tn;
+  const int g = (int)(i / per), r = (int)(i - g * per), high = min(kGroup, tm - g * kGroup);
+  return {&p, (g * kGroup + r % high) * kTile, r / high * (kMode == MM_LINEAR ? kTile : kTile / 2)};
+}
+
+__device__ __forceinline__ void tma_pair(uint32_t dst, const CUtensorMap* m, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(m), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add, bool eight) {
+  if (eight)
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+// Arrives on both blocks' barrier once the products issued so far are done.
+__device__ __forceinline__ void commit_pair(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+               "h"((uint16_t)3)
+               : "memory");
+}
+__device__ __forceinline__ void arrive_at(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// Eight neighbouring values of a row, n of them inside it.
+template <typename T>
+__device__ __forceinline__ void load8(float (&v)[8], const T* p, int n) {
+  if (n >= 8) {
+    const uint4 w = *reinterpret_cast<const uint4*>(p);
+    const float2 a = Elem<T>::two(w.x), b = Elem<T>::two(w.y), c = Elem<T>::two(w.z), d = Elem<T>::two(w.w);
+    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.f;
+}
+__device__ __forceinline__ void load8(float (&v)[8], const float* p, int n) {
+  if (n >= 8) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8], int n) {
+  if (n >= 8) {
+    *reinterpret_cast<uint4*>(p) =
+        make_uint4(Elem<T>::pack(v[0], v[1]), Elem<T>::pack(v[2], v[3]), Elem<T>::pack(v[4], v[5]), Elem<T>::pack(v[6], v[7]));
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) p[i] = (T)v[i];
+}
+
+template <typename T, int kMode>
+__global__ void __launch_bounds__(256, 1) k_mm_wide(const __grid_constant__ MmWideArgs a) {
+  extern __shared__ unsigned char raw[];
+  const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
+  WideBars& bars = *reinterpret_cast<WideBars*>(raw + (smem - smem_u32(raw)) + kStages * kStage);
+  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const long long first = blockIdx.x >> 1, step = gridDim.x >> 1;
+
+  pdl_trigger();
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) mbar_init(&bars.full[i], 1), mbar_init(&bars.empty[i], 1);
+    for (int i = 0; i < 2; ++i) mbar_init(&bars.sum_full[i], 1), mbar_init(&bars.sum_empty[i], 8);
+  }
+  if (w == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  }
+  pdl_wait();
+  __syncwarp();
+  fence_before();
+  cluster_all();
+  fence_after();
+  const uint32_t tmem = bars.tmem;
+
+  if (w == 0 && lane == 0) {
+    // ---------------------------------------------------------------- copies
+    fence_proxy_async_all();
+    const int per = a.eight ? kMmBlock : kMmBlock / 2;
+    int st = 0;
+    long long count = 0;
+    uint32_t par = 1;
+    bool ok = true;
+    for (long long i = first; ok && i < a.tiles; i += step) {
+      const Tile t = tile_of<kMode>(a, i);
+      const MmProduct& p = *t.p;
+      const int am = t.m0 + rank * 128, bn = kMode == MM_LINEAR ? t.n0 + rank * 128 : t.n0;
+      for (int part = 0; ok && part < (kMode == MM_LINEAR ? 2 : 1); ++part) {
+        const CUtensorMap* ma = &a.maps[p.a[part]];
+        const CUtensorMap* mb = &a.maps[p.b[kMode == MM_LINEAR ? part : rank]];
+        for (int k = 0; k < p.blocks[part]; ++k) {
+          ok = mm_wait(&bars.empty[st], par, a.status);
+          if (!ok) break;
+          const uint32_t at = smem + st * kStage, bar = cluster_addr(smem_u32(&bars.full[st]), 0);
+          if (rank == 0) mbar_expect_tx(&bars.full[st], 2 * kStage);
+          if (p.a_mn) {
+            tma_pair(at, ma, am, k * per, bar);
+            tma_pair(at + kHalf / 2, ma, am + 64, k * per, bar);
+          } else {
+            tma_pair(at, ma, k * per, am, bar);
+          }
+          if (p.b_mn) {
+            tma_pair(at + kHalf, mb, bn, k * per, bar);
+            tma_pair(at + kHalf + kHalf / 2, mb, bn + 64, k * per, bar);
+          } else {
+            tma_pair(at + kHalf, mb, k * per, bn, bar);
+          }
+          ++count;
+          if (++st == kStages) st = 0, par ^= 1;
+        }
+      }
+    }
+    if (ok) {
+      // every slot's last products are done, and their arrivals here have come
+      for (int j = 0; j < kStages && j < count; ++j) {
+        if (--st < 0) st = kStages - 1, par ^= 1;
+        mm_wait(&bars.empty[st], par ^ 1, a.status);
+      }
+    } else {
+      // a wait ran out: the copies under way end within microseconds
+      const uint64_t t0 = global_ns();
+      for (int j = 0; j < (1 << 20) && global_ns() - t0 < 1000000; ++j) {
+      }
+    }
+  } else if (w == 1 && lane == 0 && rank == 0) {
+    // ---------------------------------------------------------------- products of both blocks
+    int st = 0, n = 0;
+    uint32_t par = 0;
+    bool ok = true;
+    for (long long i = first; ok && i < a.tiles; i += step, ++n) {
+      const MmProduct& p = *tile_of<kMode>(a, i).p;
+      const uint32_t d = tmem + (n & 1) * kTile, idesc = mm_instr(kTile, kTile, a.format, p.a_mn, p.b_mn);
+      const uint32_t a_lead = p.a_mn ? kHalf / 2 : 16, b_lead = p.b_mn ? kHalf / 2 : 16, a_step = p.a_mn ? 128 : 2, b_step = p.b_mn ? 128 : 2;
+      const int blocks = p.blocks[0] + (kMode == MM_LINEAR ? p.blocks[1] : 0);
+      ok = mm_wait(&bars.sum_empty[n & 1], (n >> 1 & 1) ^ 1, a.status);
+      fence_after();
+      for (int k = 0; ok && k < blocks; ++k) {
+        ok = mm_wait(&bars.full[st], par, a.status);
+        if (!ok) break;
+        fence_after();
+        const uint32_t at = smem + st * kStage;
+        const uint64_t ad = smem_desc(at, a_lead, 1024), bd = smem_desc(at + kHalf, b_lead, 1024);
+#pragma unroll
+        for (int j = 0; j < kMmBlock / 32; ++j) mma_pair(d, ad + j * a_step, bd + j * b_step, idesc, k > 0 || j > 0, a.eight);
+        commit_pair(&bars.empty[st]);
+        if (++st == kStages) st = 0, par ^= 1;
+      }
+      if (ok) commit_pair(&bars.sum_full[n & 1]);
+    }
+  } else if (w >= 4) {
+    // ---------------------------------------------------------------- results, a row a thread
+    const uint32_t lanes = (uint32_t)(w & 3) << 21;
+    int n = 0;
+    for (long long i = first; i < a.tiles; i += step, ++n) {
+      const Tile t = tile_of<kMode>(a, i);
+      const MmEpilogue& e = t.p->e;
+      const long long m = t.m0 + rank * 128 + (w & 3) * 32 + lane;
+      const bool row = m < e.rows;
+      const bool ok = mm_wait(&bars.sum_full[n & 1], n >> 1 & 1, a.status);
+      if (!__all_sync(~0u, ok)) break;
+      fence_after();
+      const uint32_t at = tmem + lanes + (n & 1) * kTile;
+      const float xs = e.x_scale && row ? e.x_scale[m] : 1.f;
+      mm_with_act(kMode == MM_LINEAR && !e.act ? FS_ACT_NONE : e.act, [&](auto act) {
+        constexpr int kAct = decltype(act)::value;
+        constexpr int kChunks = kMode == MM_LINEAR ? kTile / 32 : kTile / 64;
+#pragma unroll 1
+        for (int c = 0; c < kChunks; ++c) {
+          const int n0 = t.n0 + 32 * c;
+          if (n0 >= e.cols) break;
+          __syncwarp();
+          uint32_t z[32], u[32];
+          tmem_ld32(z, at + 32 * c);
+          if (kMode != MM_LINEAR) tmem_ld32(u, at + kTile / 2 + 32 * c);
+          wait_ld();
+          if (!row) continue;
+          T* out = static_cast<T*>(e.out[0]) + m * e.out_stride + n0;
+          const T* in = static_cast<const T*>(e.in) + m * e.in_stride + n0;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int left = e.cols - n0 - 8 * g;
+            if (left <= 0) break;
+            float v[8], s[8], r[8], second[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(z[8 * g + j]), second[j] = kMode != MM_LINEAR ? __uint_as_float(u[8 * g + j]) : 0.f;
+            if (kMode != MM_BACK && e.x_scale) {
+              load8(s, e.w_scale[0] + n0 + 8 * g, left);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = v[j] * xs * s[j];
+              if (kMode == MM_GATED) {
+                load8(s, e.w_scale[1] + n0 + 8 * g, left);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) second[j] = second[j] * xs * s[j];
+              }
+            }
+            if (kMode == MM_LINEAR) {
+              if (e.bias) {
+                load8(s, static_cast<const T*>(e.bias) + n0 + 8 * g, left);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += s[j];
+              }
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = mm_act<kAct>(v[j]);
+              if (e.in) {
+                load8(r, in + 8 * g, left);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += r[j];
+              }
+            } else if (kMode == MM_GATED) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = mm_act<kAct>(v[j]) * second[j];
+            } else {
+              load8(r, in + 8 * g, left);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                float slope;
+                const float y = mm_act_slope<kAct>(v[j], slope);
+                v[j] = r[j] * second[j] * slope;
+                second[j] = r[j] * y;
+              }
+              store8(static_cast<T*>(e.out[1]) + m * e.out_stride + n0 + 8 * g, second, left);
+            }
+            store8(out + 8 * g, v, left);
+          }
+        }
+      });
+      fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_at(cluster_addr(smem_u32(&bars.sum_empty[n & 1]), 0));
+    }
+  }
+  __syncwarp();
+  fence_before();
+  cluster_all();
+  fence_after();
+  if (w == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+
+template <typename T, int kMode>
+cudaError_t launch(const MmWideArgs& a, int sms, cudaStream_t s) {
+  static std::atomic<uint64_t> seen{0};
+  const cudaError_t limit = smem_limit_once(seen, reinterpret_cast<const void*>(k_mm_wide<T, kMode>), kSmem);
+  if (limit != cudaSuccess) return limit;
+  const int pairs = (int)std::min<long long>(a.tiles, std::max(1, sms / 2));
+  return launch_clusters(k_mm_wide<T, kMode>, dim3(2 * pairs), dim3(256), 2, kSmem, s, a);
+}
+
+template <typename T>
+cudaError_t launch_mode(const MmWideArgs& a, int mode, int sms, cudaStream_t s) {
+  return mode == MM_LINEAR ? launch<T, MM_LINEAR>(a, sms, s) : mode == MM_GATED ? launch<T, MM_GATED>(a, sms, s) : launch<T, MM_BACK>(a, sms, s);
+}
+
+}  // namespace
+
+cudaError_t launch_mm_wide(MmWideArgs& a, int mode, int type, int out_type, int sms, cudaStream_t s) {
+  a.eight = type == FS_E4M3;
+  a.format = type == FS_KV_BF16 ? 1 : 0;
+  a.tiles = 0;
+  const int width = mode == MM_LINEAR ? kTile : kTile / 2;
+  for (int i = 0; i < a.products; ++i) {
+    MmProduct& p = a.product[i];
+    p.tiles = (long long)((p.e.rows + kTile - 1) / kTile) * ((p.e.cols + width - 1) / width);
+    a.tiles += p.tiles;
+  }
+  return out_type == FS_KV_FP16 ? launch_mode<__half>(a, mode, sms, s) : launch_mode<__nv_bfloat16>(a, mode, sms, s);
+}
+
+}  // namespace fs
