@@ -53,8 +53,9 @@ __device__ __forceinline__ void tma_pair(uint32_t dst, const CUtensorMap* m, int
       "l"(m), "r"(x), "r"(y), "r"(bar)
       : "memory");
 }
-__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add, bool eight) {
-  if (eight)
+template <bool kEight>
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  if constexpr (kEight)
     asm volatile(
         "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d),
         "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
@@ -131,12 +132,16 @@ __global__ void __launch_bounds__(256, 1) k_mm_wide(const __grid_constant__ MmWi
   fence_before();
   cluster_all();
   fence_after();
-  const uint32_t tmem = bars.tmem;
+  constexpr uint32_t tmem = 0;  // (all of tensor memory is this block's: its columns begin at 0)
 
-  if (w == 0 && lane == 0) {
+  // Copies and products: the whole warp walks, with values that are the same in every lane, so that addresses and descriptors stay
+  // in uniform registers; one lane, always the same, issues.
+  if (w == 0) {
     // ---------------------------------------------------------------- copies
-    fence_proxy_async_all();
+    const bool one = elect_one();
+    if (one) fence_proxy_async_all();
     const int per = a.eight ? kMmBlock : kMmBlock / 2;
+    const uint32_t leader = cluster_addr(smem_u32(&bars.full[0]), 0);
     int st = 0;
     long long count = 0;
     uint32_t par = 1;
@@ -149,21 +154,23 @@ __global__ void __launch_bounds__(256, 1) k_mm_wide(const __grid_constant__ MmWi
         const CUtensorMap* ma = &a.maps[p.a[part]];
         const CUtensorMap* mb = &a.maps[p.b[kMode == MM_LINEAR ? part : rank]];
         for (int k = 0; k < p.blocks[part]; ++k) {
-          ok = mm_wait(&bars.empty[st], par, a.status);
+          ok = __all_sync(~0u, mm_wait(&bars.empty[st], par, a.status));
           if (!ok) break;
-          const uint32_t at = smem + st * kStage, bar = cluster_addr(smem_u32(&bars.full[st]), 0);
-          if (rank == 0) mbar_expect_tx(&bars.full[st], 2 * kStage);
-          if (p.a_mn) {
-            tma_pair(at, ma, am, k * per, bar);
-            tma_pair(at + kHalf / 2, ma, am + 64, k * per, bar);
-          } else {
-            tma_pair(at, ma, k * per, am, bar);
-          }
-          if (p.b_mn) {
-            tma_pair(at + kHalf, mb, bn, k * per, bar);
-            tma_pair(at + kHalf + kHalf / 2, mb, bn + 64, k * per, bar);
-          } else {
-            tma_pair(at + kHalf, mb, k * per, bn, bar);
+          if (one) {
+            const uint32_t at = smem + st * kStage, bar = leader + st * 8;
+            if (rank == 0) mbar_expect_tx(&bars.full[st], 2 * kStage);
+            if (p.a_mn) {
+              tma_pair(at, ma, am, k * per, bar);
+              tma_pair(at + kHalf / 2, ma, am + 64, k * per, bar);
+            } else {
+              tma_pair(at, ma, k * per, am, bar);
+            }
+            if (p.b_mn) {
+              tma_pair(at + kHalf, mb, bn, k * per, bar);
+              tma_pair(at + kHalf + kHalf / 2, mb, bn + 64, k * per, bar);
+            } else {
+              tma_pair(at + kHalf, mb, k * per, bn, bar);
+            }
           }
           ++count;
           if (++st == kStages) st = 0, par ^= 1;
@@ -182,31 +189,39 @@ __global__ void __launch_bounds__(256, 1) k_mm_wide(const __grid_constant__ MmWi
       for (int j = 0; j < (1 << 20) && global_ns() - t0 < 1000000; ++j) {
       }
     }
-  } else if (w == 1 && lane == 0 && rank == 0) {
+  } else if (w == 1 && rank == 0) {
     // ---------------------------------------------------------------- products of both blocks
-    int st = 0, n = 0;
-    uint32_t par = 0;
-    bool ok = true;
-    for (long long i = first; ok && i < a.tiles; i += step, ++n) {
-      const MmProduct& p = *tile_of<kMode>(a, i).p;
-      const uint32_t d = tmem + (n & 1) * kTile, idesc = mm_instr(kTile, kTile, a.format, p.a_mn, p.b_mn);
-      const uint32_t a_lead = p.a_mn ? kHalf / 2 : 16, b_lead = p.b_mn ? kHalf / 2 : 16, a_step = p.a_mn ? 128 : 2, b_step = p.b_mn ? 128 : 2;
-      const int blocks = p.blocks[0] + (kMode == MM_LINEAR ? p.blocks[1] : 0);
-      ok = mm_wait(&bars.sum_empty[n & 1], (n >> 1 & 1) ^ 1, a.status);
-      fence_after();
-      for (int k = 0; ok && k < blocks; ++k) {
-        ok = mm_wait(&bars.full[st], par, a.status);
-        if (!ok) break;
+    const bool one = elect_one();
+    auto walk = [&](auto eight) {
+      int st = 0, n = 0;
+      uint32_t par = 0;
+      for (long long i = first; i < a.tiles; i += step, ++n) {
+        const MmProduct& p = *tile_of<kMode>(a, i).p;
+        const uint32_t d = (n & 1) * kTile, idesc = mm_instr(kTile, kTile, a.format, p.a_mn, p.b_mn);
+        const uint32_t a_step = p.a_mn ? 128 : 2, b_step = p.b_mn ? 128 : 2;
+        const uint64_t a_desc = smem_desc(smem, p.a_mn ? kHalf / 2 : 16, 1024), b_desc = smem_desc(smem + kHalf, p.b_mn ? kHalf / 2 : 16, 1024);
+        const int blocks = p.blocks[0] + (kMode == MM_LINEAR ? p.blocks[1] : 0);
+        if (!__all_sync(~0u, mm_wait(&bars.sum_empty[n & 1], (n >> 1 & 1) ^ 1, a.status))) return;
         fence_after();
-        const uint32_t at = smem + st * kStage;
-        const uint64_t ad = smem_desc(at, a_lead, 1024), bd = smem_desc(at + kHalf, b_lead, 1024);
+        for (int k = 0; k < blocks; ++k) {
+          if (!__all_sync(~0u, mm_wait(&bars.full[st], par, a.status))) return;
+          fence_after();
+          if (one) {
+            const uint64_t ad = a_desc + (uint32_t)(st * (kStage / 16)), bd = b_desc + (uint32_t)(st * (kStage / 16));
 #pragma unroll
-        for (int j = 0; j < kMmBlock / 32; ++j) mma_pair(d, ad + j * a_step, bd + j * b_step, idesc, k > 0 || j > 0, a.eight);
-        commit_pair(&bars.empty[st]);
-        if (++st == kStages) st = 0, par ^= 1;
+            for (int j = 0; j < kMmBlock / 32; ++j)
+              mma_pair<decltype(eight)::value>(d, ad + j * a_step, bd + j * b_step, idesc, k > 0 || j > 0);
+            commit_pair(&bars.empty[st]);
+          }
+          if (++st == kStages) st = 0, par ^= 1;
+        }
+        if (one) commit_pair(&bars.sum_full[n & 1]);
       }
-      if (ok) commit_pair(&bars.sum_full[n & 1]);
-    }
+    };
+    if (a.eight)
+      walk(std::true_type());
+    else
+      walk(std::false_type());
   } else if (w >= 4) {
     // ---------------------------------------------------------------- results, a row a thread
     const uint32_t lanes = (uint32_t)(w & 3) << 21;
