@@ -31,8 +31,9 @@ struct MmFewArgs {
   uint32_t* status;
 };
 
-__device__ __forceinline__ void mma_few(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add, bool eight) {
-  if (eight)
+template <bool kEight>
+__device__ __forceinline__ void mma_few(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  if constexpr (kEight)
     asm volatile(
         "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d),
         "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
@@ -92,38 +93,52 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
   fence_after();
   const uint32_t tmem = bars.tmem;
 
-  if (w == 0 && lane == 0) {
+  // (whole warps, with values that are the same in every lane; one lane, always the same, issues)
+  if (w == 0) {
     // ---------------------------------------------------------------- copies
-    fence_proxy_async_all();
+    const bool one = elect_one();
+    if (one) fence_proxy_async_all();
     const int step = a.eight ? kMmBlock : kMmBlock / 2;
     int st = 0, k = k0;
     uint32_t par = 1;
     for (; k < k1; ++k) {
-      if (!mm_wait(&bars.empty[st], par, a.status)) break;
-      const uint32_t at = smem + st * slot;
-      mbar_expect_tx(&bars.full[st], slot);
-      tma_rows(at, &mw, k * step, n0, &bars.full[st]);
-      if (kGated) tma_rows(at + w_bytes / 2, &mu, k * step, n0, &bars.full[st]);
-      tma_rows(at + w_bytes, &mx, k * step, t0, &bars.full[st]);
+      if (!__all_sync(~0u, mm_wait(&bars.empty[st], par, a.status))) break;
+      if (one) {
+        const uint32_t at = smem + st * slot;
+        mbar_expect_tx(&bars.full[st], slot);
+        tma_rows(at, &mw, k * step, n0, &bars.full[st]);
+        if (kGated) tma_rows(at + w_bytes / 2, &mu, k * step, n0, &bars.full[st]);
+        tma_rows(at + w_bytes, &mx, k * step, t0, &bars.full[st]);
+      }
       if (++st == p.stages) st = 0, par ^= 1;
     }
     if (k < k1)  // a wait ran out: the copies under way first (with the same limit)
       for (int j = max(k0, k - p.stages); j < k; ++j) mbar_wait(&bars.full[(j - k0) % p.stages], ((j - k0) / p.stages) & 1, kWaitLimitNs);
-  } else if (w == 1 && lane == 0) {
+  } else if (w == 1) {
     // ---------------------------------------------------------------- products
-    int st = 0;
-    uint32_t par = 0;
-    for (int k = k0; k < k1; ++k) {
-      if (!mm_wait(&bars.full[st], par, a.status)) break;
-      fence_after();
-      const uint32_t at = smem + st * slot;
-      const uint64_t wd = smem_desc(at, 16, 1024), xd = smem_desc(at + w_bytes, 16, 1024);
+    const bool one = elect_one();
+    const uint32_t d = __shfl_sync(~0u, tmem, 0);
+    auto walk = [&](auto eight) {
+      int st = 0;
+      uint32_t par = 0;
+      for (int k = k0; k < k1; ++k) {
+        if (!__all_sync(~0u, mm_wait(&bars.full[st], par, a.status))) break;
+        fence_after();
+        if (one) {
+          const uint32_t at = smem + st * slot;
+          const uint64_t wd = smem_desc(at, 16, 1024), xd = smem_desc(at + w_bytes, 16, 1024);
 #pragma unroll
-      for (int i = 0; i < kMmBlock / 32; ++i) mma_few(tmem, wd + 2 * i, xd + 2 * i, a.idesc, k > k0 || i > 0, a.eight);
-      commit(&bars.empty[st]);
-      if (++st == p.stages) st = 0, par ^= 1;
-    }
-    commit(&bars.done);
+          for (int i = 0; i < kMmBlock / 32; ++i) mma_few<decltype(eight)::value>(d, wd + 2 * i, xd + 2 * i, a.idesc, k > k0 || i > 0);
+          commit(&bars.empty[st]);
+        }
+        if (++st == p.stages) st = 0, par ^= 1;
+      }
+      if (one) commit(&bars.done);
+    };
+    if (a.eight)
+      walk(std::true_type());
+    else
+      walk(std::false_type());
   }
   __syncwarp();
   const bool ok = mm_wait(&bars.done, 0, a.status);
