@@ -118,12 +118,13 @@ int few_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const
 
 // The same of many rows; with e.out[1] the first product of a backward pass.
 int wide_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const fs_mm_rows* up, const MmEpilogue& e) {
+  const int tile = 256;
   MmWideArgs a{};
   if (int rc = rows_map(&a.maps[0], x.data, e.rows, c.in, x.stride, c.type, 128)) return rc;
-  if (int rc = rows_map(&a.maps[1], w.data, e.cols, c.in, w.stride, c.type, 128)) return rc;
+  if (int rc = rows_map(&a.maps[1], w.data, e.cols, c.in, w.stride, c.type, tile / 2)) return rc;
   if (up)
-    if (int rc = rows_map(&a.maps[2], up->data, e.cols, c.in, up->stride, c.type, 128)) return rc;
-  a.product[0] = {e, {0, 0}, {1, 2}, {c.blocks(), 0}, false, false, 0};
+    if (int rc = rows_map(&a.maps[2], up->data, e.cols, c.in, up->stride, c.type, tile / 2)) return rc;
+  a.product[0] = {e, {0, 0}, {1, 2}, {c.blocks(), 0}, false, false, tile, 0};
   a.products = 1;
   a.status = c.status;
   const cudaError_t r = launch_mm_wide(a, e.out[1] ? MM_BACK : up ? MM_GATED : MM_LINEAR, c.type, c.out_type, c.sms, c.stream);
@@ -153,29 +154,82 @@ __device__ __forceinline__ float scale_for(float amax) {
   return exp2_int(max(e - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0), -126));  // 448 = 1.75 * 2^8
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_quantise_rows(int in, const T* x, long long x_stride, uint8_t* codes, long long c_stride, float* scale) {
+// A row a group of kGroup threads, eight values a thread at a time, held in registers between the maximum and the
+// codes where the row has no more than kHeld such pieces a thread (and read again otherwise).
+template <typename T, int kGroup, int kHeld>
+__global__ void __launch_bounds__(256) k_quantise_rows(int rows, int in, const T* x, long long x_stride, uint8_t* codes, long long c_stride, float* scale) {
   __shared__ float top[8];
   pdl_trigger();
   pdl_wait();
-  const long long row = blockIdx.x;
+  const long long row = (long long)blockIdx.x * (256 / kGroup) + threadIdx.x / kGroup;
+  if (kGroup < 256 && row >= rows) return;
+  const int id = threadIdx.x % kGroup, pieces = (in + 7) / 8;
   const T* xr = x + row * x_stride;
   uint8_t* cr = codes + row * c_stride;
+  auto piece = [&](int p) {
+    const uint16_t* at = reinterpret_cast<const uint16_t*>(xr) + 8 * p;
+    if (8 * p + 8 <= in) return *reinterpret_cast<const uint4*>(at);
+    uint32_t w[4] = {0, 0, 0, 0};
+    for (int i = 0; 8 * p + i < in; ++i) w[i >> 1] |= (uint32_t)at[i] << (16 * (i & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  };
   float amax = 0.f;
-  for (int k = threadIdx.x; k < in; k += 256) {
-    const float v = fabsf((float)xr[k]);
-    if (v < INFINITY) amax = fmaxf(amax, v);
-  }
+  auto look = [&](uint4 u) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = Elem<T>::two(w[i]);
+      const float a = fabsf(v.x), b = fabsf(v.y);
+      amax = fmaxf(amax, fmaxf(a < INFINITY ? a : 0.f, b < INFINITY ? b : 0.f));
+    }
+  };
+  uint4 held[kHeld];
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) held[j] = id + j * kGroup < pieces ? piece(id + j * kGroup) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) look(held[j]);
+  for (int p = id + kHeld * kGroup; p < pieces; p += kGroup) look(piece(p));
+#pragma unroll
   for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, o));
-  if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = amax;
-  __syncthreads();
-  for (int i = 0; i < 8; ++i) amax = fmaxf(amax, top[i]);
-  const float s = scale_for(amax), inv = s > 0.f ? 1.f / s : 0.f;
-  for (int k = threadIdx.x; k < in; k += 256) {
-    const float v = (float)xr[k];
-    cr[k] = fabsf(v) < INFINITY ? (uint8_t)e4m3x2(v * inv, 0.f) : 0x7f;
+  if (kGroup == 256) {
+    if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, top[i]);
   }
-  if (threadIdx.x == 0) scale[row] = s;
+  const float s = scale_for(amax), inv = s > 0.f ? 1.f / s : 0.f;  // (a power of two: exact; 2^126 at most)
+  auto store = [&](int p, uint4 u) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    uint32_t y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = Elem<T>::two(w[i]);
+      y[i] = e4m3x2(v.x * inv, v.y * inv);
+      if (!(fabsf(v.x) < INFINITY)) y[i] = (y[i] & 0xff00u) | 0x7fu;
+      if (!(fabsf(v.y) < INFINITY)) y[i] = (y[i] & 0xffu) | 0x7f00u;
+    }
+    const uint2 c = make_uint2(y[0] | y[1] << 16, y[2] | y[3] << 16);
+    if (8 * p + 8 <= in) {
+      *reinterpret_cast<uint2*>(cr + 8 * p) = c;
+    } else {
+      for (int i = 0; 8 * p + i < in; ++i) cr[8 * p + i] = (uint8_t)((i < 4 ? c.x >> (8 * i) : c.y >> (8 * (i - 4))) & 255u);
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (id + j * kGroup < pieces) store(id + j * kGroup, held[j]);
+  for (int p = id + kHeld * kGroup; p < pieces; p += kGroup) store(p, piece(p));
+  if (id == 0) scale[row] = s;
+}
+
+template <typename T>
+cudaError_t launch_quantise(int rows, int in, const fs_mm_rows& x, const fs_mm_rows& codes, float* scale, cudaStream_t s) {
+  const T* xd = static_cast<const T*>(x.data);
+  uint8_t* cd = static_cast<uint8_t*>(codes.data);
+  const long long xs = x.stride, cs = codes.stride;
+  if (in <= 2048) return launch_pdl(k_quantise_rows<T, 32, 8>, dim3((rows + 7) / 8), dim3(256), 0, s, rows, in, xd, xs, cd, cs, scale);
+  if (in <= 8192) return launch_pdl(k_quantise_rows<T, 256, 4>, dim3(rows), dim3(256), 0, s, rows, in, xd, xs, cd, cs, scale);
+  return launch_pdl(k_quantise_rows<T, 256, 8>, dim3(rows), dim3(256), 0, s, rows, in, xd, xs, cd, cs, scale);
 }
 
 }  // namespace
@@ -268,9 +322,9 @@ extern "C" int fs_gated_ff_backward(const fs_mm_gated_grad* args, void* workspac
   if (int rc = rows_map(&a.maps[X_T], g.x.data, g.rows, g.in, g.x.stride, g.type, 64)) return rc;
   auto to = [&](const fs_mm_rows& r, int n) { return MmEpilogue{n, g.in, FS_ACT_NONE, nullptr, {}, nullptr, nullptr, 0, {r.data, nullptr}, r.stride}; };
   const int out_blocks = (g.out + 63) / 64, row_blocks = (g.rows + 63) / 64;
-  a.product[0] = {to(g.dx, g.rows), {DG, DU}, {WG_T, WU_T}, {out_blocks, out_blocks}, false, true, 0};
-  a.product[1] = {to(g.dw_gate, g.out), {DG_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, 0};
-  a.product[2] = {to(g.dw_up, g.out), {DU_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, 0};
+  a.product[0] = {to(g.dx, g.rows), {DG, DU}, {WG_T, WU_T}, {out_blocks, out_blocks}, false, true, 256, 0};
+  a.product[1] = {to(g.dw_gate, g.out), {DG_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, 256, 0};
+  a.product[2] = {to(g.dw_up, g.out), {DU_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, 256, 0};
   a.products = 3;
   a.status = c.status;
   const cudaError_t e = launch_mm_wide(a, MM_LINEAR, g.type, g.type, c.sms, c.stream);
@@ -289,11 +343,7 @@ extern "C" int fs_quantise_rows(int32_t rows, int32_t in, int32_t type, const fs
   if (int rc = check_rows(xr, "x", rows, in, type)) return rc;
   if (int rc = check_rows(cr, "codes", rows, in, FS_E4M3)) return rc;
   const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = type == FS_KV_FP16
-                            ? launch_pdl(k_quantise_rows<__half>, dim3(rows), dim3(256), 0, s, in, static_cast<const __half*>(xr.data),
-                                         (long long)xr.stride, static_cast<uint8_t*>(cr.data), (long long)cr.stride, scale)
-                            : launch_pdl(k_quantise_rows<__nv_bfloat16>, dim3(rows), dim3(256), 0, s, in, static_cast<const __nv_bfloat16*>(xr.data),
-                                         (long long)xr.stride, static_cast<uint8_t*>(cr.data), (long long)cr.stride, scale);
+  const cudaError_t e = type == FS_KV_FP16 ? launch_quantise<__half>(rows, in, xr, cr, scale, s) : launch_quantise<__nv_bfloat16>(rows, in, xr, cr, scale, s);
   return e == cudaSuccess ? FS_OK : cuda_say(e, "launch (fs_quantise_rows)");
 }
 

@@ -145,12 +145,13 @@ cudaError_t launch_mm_few(const CUtensorMap& x, const CUtensorMap& w, const CUte
 enum { MM_LINEAR, MM_GATED, MM_BACK };
 
 // One product of a launch of k_mm_wide: e.rows x e.cols results, sums over blocks[0] blocks of maps a[0] and b[0], then over blocks[1]
-// of a[1] and b[1] (MM_GATED, MM_BACK: a[0] with b[0] for gate and b[1] for up). Maps have boxes of 128 rows and one block, or, of an
-// operand whose rows are contiguous (a_mn, b_mn), of 64 of them and 64 terms of the sum.
+// of a[1] and b[1] (MM_GATED, MM_BACK: a[0] with b[0] for gate and b[1] for up). Maps have boxes of 128 rows (B: half a
+// tile's columns) and one block, or, of an operand whose rows are contiguous (a_mn, b_mn), of 64 of them and 64 terms of the sum.
 struct MmProduct {
   MmEpilogue e;
   int a[2], b[2], blocks[2];
   bool a_mn, b_mn;
+  int tile;         // columns of a tile (gated: of gate and of up together): a multiple of 64 up to 256
   long long tiles;  // (launch_mm_wide's)
 };
 struct MmWideArgs {

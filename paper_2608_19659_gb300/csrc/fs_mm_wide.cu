@@ -17,12 +17,15 @@ namespace fs {
 namespace {
 
 constexpr int kStages = 7, kHalf = 128 * kMmBlock, kStage = 2 * kHalf;
-constexpr int kTile = 256;
+constexpr int kTile = 256;                  // rows of a tile; its columns at most
+constexpr int kThreads = 12 * 32, kEnders = 8;  // (warps that finish tiles: two for each of the four groups of 32 rows)
 constexpr int kGroup = 8;  // tiles of rows that are walked over together
 
 struct WideBars {
   uint64_t full[kStages], empty[kStages], sum_full[2], sum_empty[2];
   uint32_t tmem;
+  alignas(16) float scale[kTile];  // of a tile's columns of W (gated: gate's, then up's)
+  uint16_t bias[kTile];
 };
 // All of an SM's shared memory: no block with tensor memory of its own fits beside one of these, which
 // take all of it. (One that held some while it waits for its cluster, and this pair for each other: none would go on.)
@@ -44,7 +47,7 @@ __device__ __forceinline__ Tile tile_of(const MmWideArgs& a, long long i) {
   const int tn = (int)(p.tiles / tm);
   const long long per = (long long)kGroup * tn;
   const int g = (int)(i / per), r = (int)(i - g * per), high = min(kGroup, tm - g * kGroup);
-  return {&p, (g * kGroup + r % high) * kTile, r / high * (kMode == MM_LINEAR ? kTile : kTile / 2)};
+  return {&p, (g * kGroup + r % high) * kTile, r / high * (kMode == MM_LINEAR ? p.tile : p.tile / 2)};
 }
 
 __device__ __forceinline__ void tma_pair(uint32_t dst, const CUtensorMap* m, int x, int y, uint32_t bar) {
@@ -76,29 +79,19 @@ __device__ __forceinline__ void arrive_at(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// Eight neighbouring values of a row, n of them inside it.
-template <typename T>
-__device__ __forceinline__ void load8(float (&v)[8], const T* p, int n) {
-  if (n >= 8) {
-    const uint4 w = *reinterpret_cast<const uint4*>(p);
-    const float2 a = Elem<T>::two(w.x), b = Elem<T>::two(w.y), c = Elem<T>::two(w.z), d = Elem<T>::two(w.w);
-    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
-    return;
-  }
+// Eight neighbouring 16-bit values of a row, n of them inside it (others 0).
+__device__ __forceinline__ uint4 load8(const void* row, long long at, int n) {
+  const uint16_t* p = static_cast<const uint16_t*>(row) + at;
+  if (n >= 8) return *reinterpret_cast<const uint4*>(p);
+  uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.f;
-}
-__device__ __forceinline__ void load8(float (&v)[8], const float* p, int n) {
-  if (n >= 8) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+  for (int i = 0; i < 8; ++i)
+    if (i < n) w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <typename T>
-__device__ __forceinline__ void store8(T* p, const float (&v)[8], int n) {
+__device__ __forceinline__ void store8(void* row, long long at, const float (&v)[8], int n) {
+  T* p = static_cast<T*>(row) + at;
   if (n >= 8) {
     *reinterpret_cast<uint4*>(p) =
         make_uint4(Elem<T>::pack(v[0], v[1]), Elem<T>::pack(v[2], v[3]), Elem<T>::pack(v[4], v[5]), Elem<T>::pack(v[6], v[7]));
@@ -108,9 +101,18 @@ __device__ __forceinline__ void store8(T* p, const float (&v)[8], int n) {
   for (int i = 0; i < 8; ++i)
     if (i < n) p[i] = (T)v[i];
 }
+template <typename T>
+__device__ __forceinline__ void floats8(float (&v)[8], uint4 w) {
+  const float2 a = Elem<T>::two(w.x), b = Elem<T>::two(w.y), c = Elem<T>::two(w.z), d = Elem<T>::two(w.w);
+  v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
+}
+__device__ __forceinline__ void floats8(float (&v)[8], const float* p) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
 
 template <typename T, int kMode>
-__global__ void __launch_bounds__(256, 1) k_mm_wide(const __grid_constant__ MmWideArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__ MmWideArgs a) {
   extern __shared__ unsigned char raw[];
   const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
   WideBars& bars = *reinterpret_cast<WideBars*>(raw + (smem - smem_u32(raw)) + kStages * kStage);
@@ -121,7 +123,7 @@ __global__ void __launch_bounds__(256, 1) k_mm_wide(const __grid_constant__ MmWi
   pdl_trigger();
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) mbar_init(&bars.full[i], 1), mbar_init(&bars.empty[i], 1);
-    for (int i = 0; i < 2; ++i) mbar_init(&bars.sum_full[i], 1), mbar_init(&bars.sum_empty[i], 8);
+    for (int i = 0; i < 2; ++i) mbar_init(&bars.sum_full[i], 1), mbar_init(&bars.sum_empty[i], 2 * kEnders);
   }
   if (w == 2) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars.tmem)) : "memory");
@@ -149,7 +151,8 @@ __global__ void __launch_bounds__(256, 1) k_mm_wide(const __grid_constant__ MmWi
     for (long long i = first; ok && i < a.tiles; i += step) {
       const Tile t = tile_of<kMode>(a, i);
       const MmProduct& p = *t.p;
-      const int am = t.m0 + rank * 128, bn = kMode == MM_LINEAR ? t.n0 + rank * 128 : t.n0;
+      const int am = t.m0 + rank * 128, bn = kMode == MM_LINEAR ? t.n0 + rank * (p.tile / 2) : t.n0;
+      const uint32_t bytes = 2 * kHalf + p.tile * kMmBlock;  // of both blocks
       for (int part = 0; ok && part < (kMode == MM_LINEAR ? 2 : 1); ++part) {
         const CUtensorMap* ma = &a.maps[p.a[part]];
         const CUtensorMap* mb = &a.maps[p.b[kMode == MM_LINEAR ? part : rank]];
@@ -158,7 +161,7 @@ __global__ void __launch_bounds__(256, 1) k_mm_wide(const __grid_constant__ MmWi
           if (!ok) break;
           if (one) {
             const uint32_t at = smem + st * kStage, bar = leader + st * 8;
-            if (rank == 0) mbar_expect_tx(&bars.full[st], 2 * kStage);
+            if (rank == 0) mbar_expect_tx(&bars.full[st], bytes);
             if (p.a_mn) {
               tma_pair(at, ma, am, k * per, bar);
               tma_pair(at + kHalf / 2, ma, am + 64, k * per, bar);
@@ -197,7 +200,7 @@ __global__ void __launch_bounds__(256, 1) k_mm_wide(const __grid_constant__ MmWi
       uint32_t par = 0;
       for (long long i = first; i < a.tiles; i += step, ++n) {
         const MmProduct& p = *tile_of<kMode>(a, i).p;
-        const uint32_t d = (n & 1) * kTile, idesc = mm_instr(kTile, kTile, a.format, p.a_mn, p.b_mn);
+        const uint32_t d = (n & 1) * kTile, idesc = mm_instr(kTile, p.tile, a.format, p.a_mn, p.b_mn);
         const uint32_t a_step = p.a_mn ? 128 : 2, b_step = p.b_mn ? 128 : 2;
         const uint64_t a_desc = smem_desc(smem, p.a_mn ? kHalf / 2 : 16, 1024), b_desc = smem_desc(smem + kHalf, p.b_mn ? kHalf / 2 : 16, 1024);
         const int blocks = p.blocks[0] + (kMode == MM_LINEAR ? p.blocks[1] : 0);
@@ -223,79 +226,104 @@ __global__ void __launch_bounds__(256, 1) k_mm_wide(const __grid_constant__ MmWi
     else
       walk(std::false_type());
   } else if (w >= 4) {
-    // ---------------------------------------------------------------- results, a row a thread
+    // ---------------------------------------------------------------- results, a row a thread, 32 columns at a time
     const uint32_t lanes = (uint32_t)(w & 3) << 21;
+    const int id = threadIdx.x - 128, half = id >> 7;
     int n = 0;
     for (long long i = first; i < a.tiles; i += step, ++n) {
       const Tile t = tile_of<kMode>(a, i);
       const MmEpilogue& e = t.p->e;
       const long long m = t.m0 + rank * 128 + (w & 3) * 32 + lane;
       const bool row = m < e.rows;
+      const int width = kMode == MM_LINEAR ? t.p->tile : t.p->tile / 2;  // results of a row
+      // what the columns share goes to shared memory, and a row's own first part is asked for, while the sums are made
+      if (kMode != MM_BACK && (e.x_scale || e.bias)) {
+        const int c = kMode == MM_LINEAR || id < width ? id : id - width, col = t.n0 + c;
+        const float* from = kMode == MM_LINEAR || id < width ? e.w_scale[0] : e.w_scale[1];
+        const bool in = id < t.p->tile && col < e.cols;
+        const float sc = in && e.x_scale ? from[col] : 0.f;
+        const uint16_t b = in && e.bias ? static_cast<const uint16_t*>(e.bias)[col] : 0;
+        asm volatile("bar.sync 1, 256;" ::: "memory");  // (the tile before has been finished with the old ones)
+        bars.scale[id] = sc, bars.bias[id] = b;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+      }
+      const float xs = e.x_scale && row ? e.x_scale[m] : 1.f;
+      uint4 next[4];
+      auto ask = [&](int c) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int col = t.n0 + 32 * c + 8 * g;
+          next[g] = row && col < e.cols && 32 * c < width ? load8(e.in, m * e.in_stride + col, e.cols - col) : make_uint4(0, 0, 0, 0);
+        }
+      };
+      if (e.in) ask(half);
       const bool ok = mm_wait(&bars.sum_full[n & 1], n >> 1 & 1, a.status);
       if (!__all_sync(~0u, ok)) break;
       fence_after();
       const uint32_t at = tmem + lanes + (n & 1) * kTile;
-      const float xs = e.x_scale && row ? e.x_scale[m] : 1.f;
-      mm_with_act(kMode == MM_LINEAR && !e.act ? FS_ACT_NONE : e.act, [&](auto act) {
+      mm_with_act(e.act, [&](auto act) {
         constexpr int kAct = decltype(act)::value;
-        constexpr int kChunks = kMode == MM_LINEAR ? kTile / 32 : kTile / 64;
 #pragma unroll 1
-        for (int c = 0; c < kChunks; ++c) {
+        for (int c = half; 32 * c < width; c += 2) {
           const int n0 = t.n0 + 32 * c;
           if (n0 >= e.cols) break;
           __syncwarp();
           uint32_t z[32], u[32];
           tmem_ld32(z, at + 32 * c);
-          if (kMode != MM_LINEAR) tmem_ld32(u, at + kTile / 2 + 32 * c);
+          if (kMode != MM_LINEAR) tmem_ld32(u, at + width + 32 * c);
+          uint4 own[4];
+          if (e.in) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) own[g] = next[g];
+            ask(c + 2);
+          }
           wait_ld();
           if (!row) continue;
-          T* out = static_cast<T*>(e.out[0]) + m * e.out_stride + n0;
-          const T* in = static_cast<const T*>(e.in) + m * e.in_stride + n0;
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const int left = e.cols - n0 - 8 * g;
-            if (left <= 0) break;
-            float v[8], s[8], r[8], second[8];
+            const int col = n0 + 8 * g, in_tile = 32 * c + 8 * g;
+            if (col >= e.cols) break;
+            float v[8], s[8], second[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(z[8 * g + j]), second[j] = kMode != MM_LINEAR ? __uint_as_float(u[8 * g + j]) : 0.f;
             if (kMode != MM_BACK && e.x_scale) {
-              load8(s, e.w_scale[0] + n0 + 8 * g, left);
+              floats8(s, bars.scale + in_tile);
 #pragma unroll
               for (int j = 0; j < 8; ++j) v[j] = v[j] * xs * s[j];
               if (kMode == MM_GATED) {
-                load8(s, e.w_scale[1] + n0 + 8 * g, left);
+                floats8(s, bars.scale + width + in_tile);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) second[j] = second[j] * xs * s[j];
               }
             }
             if (kMode == MM_LINEAR) {
               if (e.bias) {
-                load8(s, static_cast<const T*>(e.bias) + n0 + 8 * g, left);
+                floats8<T>(s, *reinterpret_cast<const uint4*>(bars.bias + in_tile));
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] += s[j];
               }
 #pragma unroll
               for (int j = 0; j < 8; ++j) v[j] = mm_act<kAct>(v[j]);
               if (e.in) {
-                load8(r, in + 8 * g, left);
+                floats8<T>(s, own[g]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += r[j];
+                for (int j = 0; j < 8; ++j) v[j] += s[j];
               }
             } else if (kMode == MM_GATED) {
 #pragma unroll
               for (int j = 0; j < 8; ++j) v[j] = mm_act<kAct>(v[j]) * second[j];
             } else {
-              load8(r, in + 8 * g, left);
+              floats8<T>(s, own[g]);
 #pragma unroll
               for (int j = 0; j < 8; ++j) {
                 float slope;
                 const float y = mm_act_slope<kAct>(v[j], slope);
-                v[j] = r[j] * second[j] * slope;
-                second[j] = r[j] * y;
+                v[j] = s[j] * second[j] * slope;
+                second[j] = s[j] * y;
               }
-              store8(static_cast<T*>(e.out[1]) + m * e.out_stride + n0 + 8 * g, second, left);
+              store8<T>(e.out[1], m * e.out_stride + col, second, e.cols - col);
             }
-            store8(out + 8 * g, v, left);
+            store8<T>(e.out[0], m * e.out_stride + col, v, e.cols - col);
           }
         }
       });
@@ -317,7 +345,7 @@ cudaError_t launch(const MmWideArgs& a, int sms, cudaStream_t s) {
   const cudaError_t limit = smem_limit_once(seen, reinterpret_cast<const void*>(k_mm_wide<T, kMode>), kSmem);
   if (limit != cudaSuccess) return limit;
   const int pairs = (int)std::min<long long>(a.tiles, std::max(1, sms / 2));
-  return launch_clusters(k_mm_wide<T, kMode>, dim3(2 * pairs), dim3(256), 2, kSmem, s, a);
+  return launch_clusters(k_mm_wide<T, kMode>, dim3(2 * pairs), dim3(kThreads), 2, kSmem, s, a);
 }
 
 template <typename T>
@@ -331,9 +359,9 @@ cudaError_t launch_mm_wide(MmWideArgs& a, int mode, int type, int out_type, int 
   a.eight = type == FS_E4M3;
   a.format = type == FS_KV_BF16 ? 1 : 0;
   a.tiles = 0;
-  const int width = mode == MM_LINEAR ? kTile : kTile / 2;
   for (int i = 0; i < a.products; ++i) {
     MmProduct& p = a.product[i];
+    const int width = mode == MM_LINEAR ? p.tile : p.tile / 2;
     p.tiles = (long long)((p.e.rows + kTile - 1) / kTile) * ((p.e.cols + width - 1) / width);
     a.tiles += p.tiles;
   }
