@@ -65,19 +65,19 @@ __device__ __forceinline__ float mm_act_slope(float z, float& slope) {
   return z;
 }
 
-// Four neighbouring values of a row, n of them inside it (all when n >= 4: then 8 bytes at once).
-template <typename T>
-__device__ __forceinline__ float4 mm_load4(const T* p, int n) {
-  if (n >= 4) {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
-    const float2 a = Elem<T>::two(w.x), b = Elem<T>::two(w.y);
-    return make_float4(a.x, a.y, b.x, b.y);
-  }
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (n > 0) v.x = (float)p[0];
-  if (n > 1) v.y = (float)p[1];
-  if (n > 2) v.z = (float)p[2];
+// Four neighbouring 16-bit values of a row, n of them inside it (others 0; all when n >= 4: then 8 bytes at once).
+__device__ __forceinline__ uint2 mm_raw4(const uint16_t* p, int n) {
+  if (n >= 4) return *reinterpret_cast<const uint2*>(p);
+  uint2 v = make_uint2(0, 0);
+  if (n > 0) v.x = p[0];
+  if (n > 1) v.x |= (uint32_t)p[1] << 16;
+  if (n > 2) v.y = p[2];
   return v;
+}
+template <typename T>
+__device__ __forceinline__ float4 mm_floats4(uint2 w) {
+  const float2 a = Elem<T>::two(w.x), b = Elem<T>::two(w.y);
+  return make_float4(a.x, a.y, b.x, b.y);
 }
 template <typename T>
 __device__ __forceinline__ void mm_store4(T* p, float4 v, int n) {

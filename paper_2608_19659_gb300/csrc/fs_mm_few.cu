@@ -2,9 +2,9 @@
 //
 // A tile is w_rows rows of W (the 128 rows of a tensor-core product; with fewer, its other rows are garbage that nothing
 // reads) times up to 128 tokens (its columns), so that one token costs no more than 16 of padding in shared memory and
-// nothing in bandwidth. Its sum is split over the blocks of a cluster, each of which leaves its share in its
-// shared memory; every block then adds up and finishes a share of the tile's results, in the order of the ranks, so
-// that bits repeat. Of a gated block a tile has as many rows of gate as of up.
+// nothing in bandwidth. Its sum is split over the blocks of a cluster. Each of them finishes some of the tile's tokens: the
+// others store their sums of those in its shared memory, and after the cluster's one barrier it adds them up, in the order of
+// the ranks, so that bits repeat. (Sums left where they were made and read from there: 64 rows of 8-bit 20.0 us.) Of a gated block a tile has as many rows of gate as of up.
 // One lane keeps copies on their way, one issues products, all four warps take part in the end.
 // Bound by reading W.
 #include <algorithm>
@@ -26,7 +26,7 @@ struct FewBars {
 struct MmFewArgs {
   MmEpilogue e;
   MmFewPlan p;
-  int blocks_k, eight, part_at;
+  int blocks_k, eight, bars_at, sums_at;
   uint32_t idesc;
   uint32_t* status;
 };
@@ -45,16 +45,16 @@ __device__ __forceinline__ void mma_few(uint32_t d, uint64_t a, uint64_t b, uint
         : "memory");
 }
 
-// The sum over the cluster's blocks of four floats at address a of their shared memory, in the order of the ranks.
-__device__ __forceinline__ float4 cluster_sum4(uint32_t a, int cluster) {
+__device__ __forceinline__ void st_cluster(uint32_t a, uint32_t x) {
+  asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(a), "r"(x) : "memory");
+}
+
+// The sum of four floats of every block of the cluster, `step` bytes apart in this one's shared memory, in the order of the ranks.
+__device__ __forceinline__ float4 sum4(uint32_t a, int step, int cluster) {
   float4 v[kMaxCluster];
 #pragma unroll
   for (int i = 0; i < kMaxCluster; ++i)
-    if (i < cluster)
-      asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                   : "=f"(v[i].x), "=f"(v[i].y), "=f"(v[i].z), "=f"(v[i].w)
-                   : "r"(cluster_addr(a, i))
-                   : "memory");
+    if (i < cluster) asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i].x), "=f"(v[i].y), "=f"(v[i].z), "=f"(v[i].w) : "r"(a + i * step));
   float4 s = v[0];
 #pragma unroll
   for (int i = 1; i < kMaxCluster; ++i)
@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
   const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
   const MmFewPlan& p = a.p;
   const int slot = (p.w_rows + p.tokens) * kMmBlock, w_bytes = p.w_rows * kMmBlock;
-  FewBars& bars = *reinterpret_cast<FewBars*>(raw + (smem - smem_u32(raw)) + a.part_at);
+  FewBars& bars = *reinterpret_cast<FewBars*>(raw + (smem - smem_u32(raw)) + a.bars_at);
   const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = blockIdx.x % p.cluster, tile = blockIdx.x / p.cluster;
   const int width = kGated ? p.w_rows / 2 : p.w_rows;  // columns of y a tile
@@ -92,6 +92,22 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
   __syncthreads();
   fence_after();
   const uint32_t tmem = bars.tmem;
+
+  // What this thread's four columns of results share, asked for while the sums are made. Block `o` of the cluster finishes the
+  // tokens [o share, (o + 1) share) of the tile, each 128 / quads-th of them (128 is a multiple of quads) by this thread.
+  const MmEpilogue& e = a.e;
+  const int quads = width / 4, valid = min(p.tokens, e.rows - t0), share = (valid + p.cluster - 1) / p.cluster;
+  const int first = rank * share, mine = max(0, min(valid - first, share));
+  const int n = n0 + 4 * (threadIdx.x % quads), left = e.cols - n, t_step = 128 / quads;
+  float4 scale0{}, scale1{};
+  uint2 bias{};
+  if (left > 0 && mine > 0) {
+    if (e.x_scale) {
+      scale0 = mm_load4(e.w_scale[0] + n, left);
+      if (kGated) scale1 = mm_load4(e.w_scale[1] + n, left);
+    }
+    if (!kGated && e.bias) bias = mm_raw4(static_cast<const uint16_t*>(e.bias) + n, left);
+  }
 
   // (whole warps, with values that are the same in every lane; one lane, always the same, issues)
   if (w == 0) {
@@ -144,51 +160,72 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
   const bool ok = mm_wait(&bars.done, 0, a.status);
   fence_after();
 
-  // ---------------------------------------------------------------- this block's share of the sums, [token][row of W]
-  const int ld = p.w_rows + 4;
+  // ---------------------------------------------------------------- sums to where they are added up, [rank][token][row of W]
+  const int ld = 4 * p.w_rows;
+  const uint32_t sums = smem + a.sums_at;
   if (32 * w < p.w_rows && ok) {
-    const uint32_t to = smem + (32 * w + lane) * 4;
-    for (int c = 0; c < p.tokens; c += 16) {
+    const uint32_t to = sums + rank * share * ld + (32 * w + lane) * 4;
+    for (int c = 0, o = 0, rest = share; c < valid; c += 16) {
       uint32_t x[16];
       tmem_ld16(x, tmem + ((uint32_t)(32 * w) << 16) + c);
       wait_ld();
 #pragma unroll
-      for (int i = 0; i < 16; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + (c + i) * ld * 4), "r"(x[i]) : "memory");
+      for (int i = 0; i < 16; ++i) {
+        if (c + i < valid) st_cluster(cluster_addr(to + (share - rest) * ld, o), x[i]);
+        if (--rest == 0) rest = share, ++o;
+      }
     }
   }
+  // what a token adds, some tokens at a time: the first of them while the sums are on their way
+  constexpr int kAtOnce = 4;
+  float xs[kAtOnce];
+  uint2 extra[kAtOnce];
+  int t = threadIdx.x / quads;
+  auto ask = [&] {
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int ti = t + i * t_step;
+      const long long m = t0 + first + ti;
+      const bool in = ti < mine && left > 0;
+      xs[i] = in && e.x_scale ? e.x_scale[m] : 1.f;
+      if (!kGated) extra[i] = in && e.in ? mm_raw4(static_cast<const uint16_t*>(e.in) + m * e.in_stride + n, left) : uint2{};
+    }
+  };
+  ask();
+  __syncwarp();
   fence_before();
   if (p.cluster > 1)
-    cluster_all();
+    cluster_all();  // (the last that any block does with another's shared memory)
   else
     __syncthreads();
   fence_after();
   if (w == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols));
 
   // ---------------------------------------------------------------- results, four neighbours of a row at a time
-  const MmEpilogue& e = a.e;
-  const int quads = width / 4, items = min(p.tokens, e.rows - t0) * quads;
+  if (left <= 0) return;
   mm_with_act(e.act, [&](auto act) {
     constexpr int kAct = decltype(act)::value;
-    for (int i = rank * 128 + threadIdx.x; i < items; i += p.cluster * 128) {
-      const int t = i / quads, q = 4 * (i % quads), n = n0 + q, left = e.cols - n;
-      const long long m = t0 + t;
-      if (left <= 0) continue;
-      const uint32_t at = smem + (t * ld + q) * 4;
-      float4 z = cluster_sum4(at, p.cluster), u = z;
-      if (kGated) u = cluster_sum4(at + width * 4, p.cluster);
-      if (e.x_scale) {
-        const float xs = e.x_scale[m];
-        z = z * xs * mm_load4(e.w_scale[0] + n, left);
-        if (kGated) u = u * xs * mm_load4(e.w_scale[1] + n, left);
+    while (t < mine) {
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int ti = t + i * t_step;
+        if (ti >= mine) break;
+        const uint32_t at = sums + ti * ld + 16 * (threadIdx.x % quads);
+        float4 z = sum4(at, share * ld, p.cluster), u = z;
+        if (kGated) u = sum4(at + width * 4, share * ld, p.cluster);
+        if (e.x_scale) {
+          z = z * xs[i] * scale0;
+          if (kGated) u = u * xs[i] * scale1;
+        }
+        if (!kGated) z = z + mm_floats4<T>(bias);
+        z = make_float4(mm_act<kAct>(z.x), mm_act<kAct>(z.y), mm_act<kAct>(z.z), mm_act<kAct>(z.w));
+        z = kGated ? z * u : z + mm_floats4<T>(extra[i]);
+        mm_store4(static_cast<T*>(e.out[0]) + (t0 + first + ti) * e.out_stride + n, z, left);
       }
-      if (!kGated && e.bias) z = z + mm_load4(static_cast<const T*>(e.bias) + n, left);
-      z = make_float4(mm_act<kAct>(z.x), mm_act<kAct>(z.y), mm_act<kAct>(z.z), mm_act<kAct>(z.w));
-      if (kGated) z = z * u;
-      if (!kGated && e.in) z = z + mm_load4(static_cast<const T*>(e.in) + m * e.in_stride + n, left);
-      mm_store4(static_cast<T*>(e.out[0]) + m * e.out_stride + n, z, left);
+      t += kAtOnce * t_step;
+      if (t < mine) ask();
     }
   });
-  if (p.cluster > 1) cluster_all();  // no block leaves while another reads its shared memory
 }
 
 template <typename T, bool kGated>
@@ -199,39 +236,59 @@ cudaError_t launch(const CUtensorMap& x, const CUtensorMap& w, const CUtensorMap
   return launch_clusters(k_mm_few<T, kGated>, dim3(a.p.w_tiles * a.p.cluster, a.p.token_tiles), dim3(128), a.p.cluster, a.p.smem, s, x, w, u, a);
 }
 
-int part_at(const MmFewPlan& p) {
+int ring_bytes(const MmFewPlan& p) {
   const int slot = (p.w_rows + p.tokens) * kMmBlock;
   // (the last stage's products read 128 rows, whatever a tile has)
-  const int ring = std::max(p.stages * slot, (p.stages - 1) * slot + 128 * kMmBlock);
-  return std::max(ring, (p.w_rows + 4) * p.tokens * 4);
+  return std::max(p.stages * slot, (p.stages - 1) * slot + 128 * kMmBlock);
 }
+// A cluster's sums come while a block's own products may still read its ring; those of a single block do not.
+int sums_bytes(const MmFewPlan& p) { return (p.tokens + p.cluster - 1) / p.cluster * p.cluster * p.w_rows * 4; }
+int sums_at(const MmFewPlan& p) { return p.cluster > 1 ? ring_bytes(p) : 0; }
+int bars_at(const MmFewPlan& p) { return std::max(ring_bytes(p), sums_at(p) + sums_bytes(p)); }
 
 }  // namespace
 
+// The tile and the cluster by an estimate of the time. What it goes by, and what the other choice cost where it decides (us, in
+// graphs): memory at 6.6 TB/s; a block takes 100 bytes a ns, half of that beside another on its SM, and 165 ns a step at
+// least (64 rows of 8-bit over 10240 rows of W: 240 blocks 18.7, 160 21.0, 80 20.8; one row of 8192 over 2 x 1792 gated, tiles of
+// 128 in clusters of 6 12.1, of 32 without 24.5); a quarter of the lesser of both, as they do not overlap in whole; a cluster's exchange
+// 0.8 us and 50 bytes a ns (333 rows of 1001 over 777, tiles of 64 6.4, of 128 6.7); blocks beyond what is resident wait for
+// a place (100 rows of 4096 over 2560, 120 blocks 9.8, 160 15.9).
 MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
-  MmFewPlan p{};
-  p.token_tiles = (rows + 127) / 128;
-  p.tokens = ((rows + p.token_tiles - 1) / p.token_tiles + 15) / 16 * 16;
-  for (p.w_rows = 128;; p.w_rows /= 2) {
-    const int width = gated ? p.w_rows / 2 : p.w_rows;
-    p.w_tiles = (cols + width - 1) / width;
-    const long long tiles = (long long)p.w_tiles * p.token_tiles;
-    p.cluster = (int)std::clamp<long long>(2 * sms / tiles, 1, std::min(kMaxCluster, blocks_k));
-    if (tiles * p.cluster >= sms || p.w_rows == 32) break;
-  }
-  const int slot = (p.w_rows + p.tokens) * kMmBlock, depth = (blocks_k + p.cluster - 1) / p.cluster;
-  // two blocks an SM; and shared memory in proportion to the tensor memory, so that blocks that are resident
-  // together never wait for each other's
-  p.stages = std::clamp(108 * 1024 / slot, 2, std::min(kMaxStages, std::max(2, depth)));
+  MmFewPlan best{};
+  float least = 0.f;
+  for (int w_rows = 128; w_rows >= 32; w_rows /= 2)
+    for (int cluster = 1; cluster <= std::min(kMaxCluster, blocks_k); ++cluster) {
+      MmFewPlan p{};
+      p.w_rows = w_rows, p.cluster = cluster;
+      p.token_tiles = (rows + 127) / 128;
+      p.tokens = ((rows + p.token_tiles - 1) / p.token_tiles + 15) / 16 * 16;
+      const int width = gated ? w_rows / 2 : w_rows, slot = (w_rows + p.tokens) * kMmBlock, depth = (blocks_k + cluster - 1) / cluster;
+      p.w_tiles = (cols + width - 1) / width;
+      const int sums = cluster > 1 ? sums_bytes(p) : 0;
+      // one block an SM if all of them find a place so, else two where each has three stages of its own. Clusters find theirs
+      // in groups of about 18 SMs
+      const int groups = std::max(1, sms / 18);
+      const long long blocks = (long long)p.w_tiles * p.token_tiles * cluster, one = 18 / cluster * cluster * groups;
+      const bool two = blocks > one && (110 * 1024 - sums) / slot >= std::min(3, depth);
+      p.stages = std::clamp(((two ? 110 : 216) * 1024 - sums) / slot, 2, std::min(kMaxStages, std::max(2, depth)));
+      const long long places = two ? 36 / cluster * cluster * groups : one;
+      const float waves = (float)((blocks + places - 1) / places), rate = two ? 50.f : 100.f;
+      const float memory = (float)blocks_k * kMmBlock * cols * (gated ? 2 : 1) / 6600.f, steps = waves * depth * std::max(slot / rate, 165.f);
+      const float read = std::max(memory, steps) + 0.25f * std::min(memory, steps);
+      const float exchange = cluster > 1 ? 800.f + std::min(rows, p.tokens) * w_rows * 4 * (cluster - 1) / (50.f * cluster) : 0.f;
+      if (best.w_rows == 0 || read + waves * exchange < least) best = p, least = read + waves * exchange;
+    }
+  // shared memory in proportion to the tensor memory, so that blocks that are resident together never wait for each other's
   int columns = 32;
-  while (columns < p.tokens) columns *= 2;
-  p.smem = std::max<size_t>(1024 + part_at(p) + sizeof(FewBars), columns * 456);
-  return p;
+  while (columns < best.tokens) columns *= 2;
+  best.smem = std::max<size_t>(1024 + bars_at(best) + sizeof(FewBars), columns * 456);
+  return best;
 }
 
 cudaError_t launch_mm_few(const CUtensorMap& x, const CUtensorMap& w, const CUtensorMap* up, const MmEpilogue& e, const MmFewPlan& p,
                           int blocks_k, int type, int out_type, uint32_t* status, cudaStream_t s) {
-  const MmFewArgs a{e, p, blocks_k, type == FS_E4M3, part_at(p), mm_instr(128, p.tokens, type == FS_KV_BF16 ? 1 : 0), status};
+  const MmFewArgs a{e, p, blocks_k, type == FS_E4M3, bars_at(p), sums_at(p), mm_instr(128, p.tokens, type == FS_KV_BF16 ? 1 : 0), status};
   const bool h = out_type == FS_KV_FP16;
   if (up) return h ? launch<__half, true>(x, w, *up, a, s) : launch<__nv_bfloat16, true>(x, w, *up, a, s);
   return h ? launch<__half, false>(x, w, w, a, s) : launch<__nv_bfloat16, false>(x, w, w, a, s);
