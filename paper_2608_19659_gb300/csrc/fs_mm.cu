@@ -85,6 +85,8 @@ int rows_map(CUtensorMap* m, const void* base, int n, int width, long long strid
   return r == CUDA_SUCCESS ? FS_OK : say(FS_ECUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }
 
+constexpr int kFewRowsMost = 1024;  // (beyond, W would be read nine times and more)
+
 // What every product needs of its call.
 struct MmCall {
   int in, type, out_type, sms;
@@ -104,8 +106,7 @@ int device_sms(int* sms) {
 }
 
 // act(x W^T + bias) + residual, or with `up` the gated product, of few rows.
-int few_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const fs_mm_rows* up, const MmEpilogue& e) {
-  const MmFewPlan p = mm_few_plan(e.rows, e.cols, c.blocks(), up, c.sms);
+int few_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const fs_mm_rows* up, const MmEpilogue& e, const MmFewPlan& p) {
   const int w_box = up ? p.w_rows / 2 : p.w_rows;
   CUtensorMap mx, mw, mu;
   if (int rc = rows_map(&mx, x.data, e.rows, c.in, x.stride, c.type, p.tokens)) return rc;
@@ -117,8 +118,7 @@ int few_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const
 }
 
 // The same of many rows; with e.out[1] the first product of a backward pass.
-int wide_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const fs_mm_rows* up, const MmEpilogue& e) {
-  const int tile = 256;
+int wide_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const fs_mm_rows* up, const MmEpilogue& e, int tile) {
   MmWideArgs a{};
   if (int rc = rows_map(&a.maps[0], x.data, e.rows, c.in, x.stride, c.type, 128)) return rc;
   if (int rc = rows_map(&a.maps[1], w.data, e.cols, c.in, w.stride, c.type, tile / 2)) return rc;
@@ -131,11 +131,15 @@ int wide_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, cons
   return r == cudaSuccess ? FS_OK : cuda_say(r, c.what);
 }
 
+// By the kernel that the estimates say is faster.
 int product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const fs_mm_rows* up, const MmEpilogue& e) {
-  // pairs of SMs where their tiles are enough for half of them
-  const long long tiles = (long long)((e.rows + 255) / 256) * ((e.cols + (up ? 127 : 255)) / (up ? 128 : 256));
-  const bool few = e.rows <= 128 || (e.rows <= 1024 && tiles < c.sms / 4);
-  return few ? few_product(c, x, w, up, e) : wide_product(c, x, w, up, e);
+  float ns = 0.f;
+  const int tile = mm_wide_tile(e.rows, e.cols, c.blocks(), up, c.sms, &ns);
+  if (e.rows <= kFewRowsMost) {
+    const MmFewPlan p = mm_few_plan(e.rows, e.cols, c.blocks(), up, c.sms);
+    if (p.ns < ns) return few_product(c, x, w, up, e, p);
+  }
+  return wide_product(c, x, w, up, e, tile);
 }
 
 // ---------------------------------------------------------------- rows to e4m3
@@ -308,8 +312,9 @@ extern "C" int fs_gated_ff_backward(const fs_mm_gated_grad* args, void* workspac
   const long long ld = padded(g.out);
   char* dg = static_cast<char*>(workspace) + kMmPartAt;
   char* du = dg + 2 * g.rows * ld;
-  if (int rc = wide_product(c, g.x, g.w_gate, &g.w_up,
-                            {g.rows, g.out, g.activation, nullptr, {}, nullptr, g.dy.data, g.dy.stride, {dg, du}, ld}))
+  float ns = 0.f;
+  if (int rc = wide_product(c, g.x, g.w_gate, &g.w_up, {g.rows, g.out, g.activation, nullptr, {}, nullptr, g.dy.data, g.dy.stride, {dg, du}, ld},
+                            mm_wide_tile(g.rows, g.out, c.blocks(), true, c.sms, &ns)))
     return rc;
   MmWideArgs a{};
   enum { DG, DU, WG_T, WU_T, DG_T, DU_T, X_T };

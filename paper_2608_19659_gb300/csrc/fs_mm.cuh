@@ -136,6 +136,7 @@ struct MmFewPlan {
   int cluster;    // blocks that share a tile's sum
   int stages;
   size_t smem;
+  float ns;       // what it takes, by estimate
 };
 MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms);
 // x and one or two W, each in boxes of one block and the plan's rows.
@@ -161,6 +162,7 @@ struct MmWideArgs {
   long long tiles;
   uint32_t* status;
 };
+int mm_wide_tile(int rows, int cols, int blocks, bool gated, int sms, float* ns);
 cudaError_t launch_mm_wide(MmWideArgs& a, int mode, int type, int out_type, int sms, cudaStream_t s);
 
 }  // namespace fs

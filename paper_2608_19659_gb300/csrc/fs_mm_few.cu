@@ -256,7 +256,6 @@ int bars_at(const MmFewPlan& p) { return std::max(ring_bytes(p), sums_at(p) + su
 // a place (100 rows of 4096 over 2560, 120 blocks 9.8, 160 15.9).
 MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
   MmFewPlan best{};
-  float least = 0.f;
   for (int w_rows = 128; w_rows >= 32; w_rows /= 2)
     for (int cluster = 1; cluster <= std::min(kMaxCluster, blocks_k); ++cluster) {
       MmFewPlan p{};
@@ -267,17 +266,19 @@ MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
       p.w_tiles = (cols + width - 1) / width;
       const int sums = cluster > 1 ? sums_bytes(p) : 0;
       // one block an SM if all of them find a place so, else two where each has three stages of its own. Clusters find theirs
-      // in groups of about 18 SMs
+      // in groups of about 18 SMs, of which some are smaller (one row of 8192 over 2 x 1792 gated, tiles of 64, 280 blocks in clusters of 5: 14.4)
       const int groups = std::max(1, sms / 18);
-      const long long blocks = (long long)p.w_tiles * p.token_tiles * cluster, one = 18 / cluster * cluster * groups;
+      const long long blocks = (long long)p.w_tiles * p.token_tiles * cluster, one = cluster == 1 ? sms : 18 / cluster * cluster * groups;
       const bool two = blocks > one && (110 * 1024 - sums) / slot >= std::min(3, depth);
       p.stages = std::clamp(((two ? 110 : 216) * 1024 - sums) / slot, 2, std::min(kMaxStages, std::max(2, depth)));
-      const long long places = two ? 36 / cluster * cluster * groups : one;
+      const long long places = !two ? one : cluster == 1 ? 2 * sms : 34 / cluster * cluster * groups;
       const float waves = (float)((blocks + places - 1) / places), rate = two ? 50.f : 100.f;
       const float memory = (float)blocks_k * kMmBlock * cols * (gated ? 2 : 1) / 6600.f, steps = waves * depth * std::max(slot / rate, 165.f);
       const float read = std::max(memory, steps) + 0.25f * std::min(memory, steps);
       const float exchange = cluster > 1 ? 800.f + std::min(rows, p.tokens) * w_rows * 4 * (cluster - 1) / (50.f * cluster) : 0.f;
-      if (best.w_rows == 0 || read + waves * exchange < least) best = p, least = read + waves * exchange;
+      // (and a block's last part, 25 ns a token of 128 rows of W; and 350 ns for each further tile of tokens)
+      p.ns = 2900.f + 350.f * (p.token_tiles - 1) + read + waves * (exchange + 25.f * ((std::min(rows, p.tokens) + cluster - 1) / cluster) * w_rows / 128);
+      if (best.w_rows == 0 || p.ns < best.ns) best = p;
     }
   // shared memory in proportion to the tensor memory, so that blocks that are resident together never wait for each other's
   int columns = 32;

@@ -138,51 +138,47 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
 
   // Copies and products: the whole warp walks, with values that are the same in every lane, so that addresses and descriptors stay
   // in uniform registers; one lane, always the same, issues.
-  if (w == 0) {
-    // ---------------------------------------------------------------- copies
-    const bool one = elect_one();
+  if (w == 0 || w == 2) {
+    // ---------------------------------------------------------------- copies: a warp for A, one for B
+    // (one for both took 435 clocks a block, where its products take 512 of a tile 256 wide, and fewer of a narrower one)
+    const bool of_b = w == 2, one = elect_one();
     if (one) fence_proxy_async_all();
     const int per = a.eight ? kMmBlock : kMmBlock / 2;
-    const uint32_t leader = cluster_addr(smem_u32(&bars.full[0]), 0);
-    int st = 0;
-    long long count = 0;
+    const uint32_t leader = cluster_addr(smem_u32(&bars.full[0]), 0), ring = smem + (of_b ? kHalf : 0);
+    int st = 0, count = 0;
     uint32_t par = 1;
     bool ok = true;
     for (long long i = first; ok && i < a.tiles; i += step) {
       const Tile t = tile_of<kMode>(a, i);
       const MmProduct& p = *t.p;
-      const int am = t.m0 + rank * 128, bn = kMode == MM_LINEAR ? t.n0 + rank * (p.tile / 2) : t.n0;
+      const int row = !of_b ? t.m0 + rank * 128 : kMode == MM_LINEAR ? t.n0 + rank * (p.tile / 2) : t.n0;
+      const bool mn = of_b ? p.b_mn : p.a_mn;
       const uint32_t bytes = 2 * kHalf + p.tile * kMmBlock;  // of both blocks
       for (int part = 0; ok && part < (kMode == MM_LINEAR ? 2 : 1); ++part) {
-        const CUtensorMap* ma = &a.maps[p.a[part]];
-        const CUtensorMap* mb = &a.maps[p.b[kMode == MM_LINEAR ? part : rank]];
-        for (int k = 0; k < p.blocks[part]; ++k) {
+        const CUtensorMap* map = &a.maps[of_b ? p.b[kMode == MM_LINEAR ? part : rank] : p.a[part]];
+        const int blocks = p.blocks[part];
+        for (int k = 0, x = 0; k < blocks; ++k, x += per) {
           ok = __all_sync(~0u, mm_wait(&bars.empty[st], par, a.status));
           if (!ok) break;
           if (one) {
-            const uint32_t at = smem + st * kStage, bar = leader + st * 8;
-            if (rank == 0) mbar_expect_tx(&bars.full[st], bytes);
-            if (p.a_mn) {
-              tma_pair(at, ma, am, k * per, bar);
-              tma_pair(at + kHalf / 2, ma, am + 64, k * per, bar);
+            const uint32_t at = ring + st * kStage, bar = leader + st * 8;
+            // (B's bytes may be counted before they are expected: the arrival that goes with that is still to come)
+            if (!of_b && rank == 0) mbar_expect_tx(&bars.full[st], bytes);
+            if (mn) {
+              tma_pair(at, map, row, x, bar);
+              tma_pair(at + kHalf / 2, map, row + 64, x, bar);
             } else {
-              tma_pair(at, ma, k * per, am, bar);
-            }
-            if (p.b_mn) {
-              tma_pair(at + kHalf, mb, bn, k * per, bar);
-              tma_pair(at + kHalf + kHalf / 2, mb, bn + 64, k * per, bar);
-            } else {
-              tma_pair(at + kHalf, mb, k * per, bn, bar);
+              tma_pair(at, map, x, row, bar);
             }
           }
-          ++count;
+          count = min(count + 1, kStages);
           if (++st == kStages) st = 0, par ^= 1;
         }
       }
     }
     if (ok) {
       // every slot's last products are done, and their arrivals here have come
-      for (int j = 0; j < kStages && j < count; ++j) {
+      for (int j = 0; j < count; ++j) {
         if (--st < 0) st = kStages - 1, par ^= 1;
         mm_wait(&bars.empty[st], par ^ 1, a.status);
       }
@@ -354,6 +350,24 @@ cudaError_t launch_mode(const MmWideArgs& a, int mode, int sms, cudaStream_t s) 
 }
 
 }  // namespace
+
+// The width of a tile by an estimate of the time (in ns): a block of a sum takes as long as its products, 1.09 ns a column, and 172 ns
+// at least (one warp's wait, products and commit; 8192 terms over one tile: 256 wide 40.9 us, 192 31.8, 128 27.7, 64 26.9), and
+// the longer the work the more what narrow tiles read again costs (8192 rows over 10240: 256 699 us, 192 816; 512 rows 256 79, 192 64,
+// 160 59). W is read at 6.6 TB/s, and a quarter of the lesser of both comes on top (32 rows over 10240 of 8192, 160: 35.3).
+int mm_wide_tile(int rows, int cols, int blocks, bool gated, int sms, float* ns) {
+  int best = 0;
+  for (int tile = kTile; tile >= 64; tile -= gated ? 64 : 32) {
+    const int width = gated ? tile / 2 : tile;
+    const long long tiles = (long long)((rows + kTile - 1) / kTile) * ((cols + width - 1) / width);
+    const float waves = (float)((tiles + sms / 2 - 1) / std::max(1, sms / 2));
+    const float again = 1.f + 0.08f * (256.f / tile - 1.f) * std::min(waves, 4.f);
+    const float sums = waves * blocks * std::max(1.09f * tile, 172.f) * again, memory = (float)blocks * kMmBlock * cols * (gated ? 2 : 1) / 6600.f;
+    const float t = std::max(sums, memory) + 0.25f * std::min(sums, memory) + 4200.f + 8.f * tile;
+    if (!best || t < *ns) best = tile, *ns = t;
+  }
+  return best;
+}
 
 cudaError_t launch_mm_wide(MmWideArgs& a, int mode, int type, int out_type, int sms, cudaStream_t s) {
   a.eight = type == FS_E4M3;
