@@ -250,9 +250,9 @@ int bars_at(const MmFewPlan& p) { return std::max(ring_bytes(p), sums_at(p) + su
 
 // The tile and the cluster by an estimate of the time. What it goes by, and what the other choice cost where it decides (us, in
 // graphs): memory at 6.6 TB/s; a block takes 100 bytes a ns, half of that beside another on its SM, and 165 ns a step at
-// least (64 rows of 8-bit over 10240 rows of W: 240 blocks 18.7, 160 21.0, 80 20.8; one row of 8192 over 2 x 1792 gated, tiles of
+// least, more with fewer rows of W (one row of 1024 8-bit over 8192, tiles of 32 6.0, of 64 5.6, of 128 5.5 and in clusters of three 5.2; 64 rows of 8-bit over 10240 rows of W: 240 blocks 18.7, 160 21.0, 80 20.8; one row of 8192 over 2 x 1792 gated, tiles of
 // 128 in clusters of 6 12.1, of 32 without 24.5); a quarter of the lesser of both, as they do not overlap in whole; a cluster's exchange
-// 0.8 us and 50 bytes a ns (333 rows of 1001 over 777, tiles of 64 6.4, of 128 6.7); blocks beyond what is resident wait for
+// 0.55 us and 50 bytes a ns (333 rows of 1001 over 777, tiles of 64 6.4, of 128 6.7); blocks beyond what is resident wait for
 // a place (100 rows of 4096 over 2560, 120 blocks 9.8, 160 15.9).
 MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
   MmFewPlan best{};
@@ -273,9 +273,9 @@ MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
       p.stages = std::clamp(((two ? 110 : 216) * 1024 - sums) / slot, 2, std::min(kMaxStages, std::max(2, depth)));
       const long long places = !two ? one : cluster == 1 ? 2 * sms : 34 / cluster * cluster * groups;
       const float waves = (float)((blocks + places - 1) / places), rate = two ? 50.f : 100.f;
-      const float memory = (float)blocks_k * kMmBlock * cols * (gated ? 2 : 1) / 6600.f, steps = waves * depth * std::max(slot / rate, 165.f);
+      const float memory = (float)blocks_k * kMmBlock * cols * (gated ? 2 : 1) / 6600.f, steps = waves * depth * std::max(slot / rate, w_rows == 32 ? 230.f : w_rows == 64 ? 185.f : 165.f);
       const float read = std::max(memory, steps) + 0.25f * std::min(memory, steps);
-      const float exchange = cluster > 1 ? 800.f + std::min(rows, p.tokens) * w_rows * 4 * (cluster - 1) / (50.f * cluster) : 0.f;
+      const float exchange = cluster > 1 ? 550.f + std::min(rows, p.tokens) * w_rows * 4 * (cluster - 1) / (50.f * cluster) : 0.f;
       // (and a block's last part, 25 ns a token of 128 rows of W; and 350 ns for each further tile of tokens)
       p.ns = 2900.f + 350.f * (p.token_tiles - 1) + read + waves * (exchange + 25.f * ((std::min(rows, p.tokens) + cluster - 1) / cluster) * w_rows / 128);
       if (best.w_rows == 0 || p.ns < best.ns) best = p;
