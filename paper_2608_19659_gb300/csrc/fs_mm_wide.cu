@@ -101,6 +101,8 @@ __device__ __forceinline__ void store8(void* row, long long at, const float (&v)
   for (int i = 0; i < 8; ++i)
     if (i < n) p[i] = (T)v[i];
 }
+__device__ __forceinline__ void tmem_ld(uint32_t (&r)[32], uint32_t a) { tmem_ld32(r, a); }
+__device__ __forceinline__ void tmem_ld(uint32_t (&r)[16], uint32_t a) { tmem_ld16(r, a); }
 template <typename T>
 __device__ __forceinline__ void floats8(float (&v)[8], uint4 w) {
   const float2 a = Elem<T>::two(w.x), b = Elem<T>::two(w.y), c = Elem<T>::two(w.z), d = Elem<T>::two(w.w);
@@ -166,7 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
             if (!of_b && rank == 0) mbar_expect_tx(&bars.full[st], bytes);
             if (mn) {
               tma_pair(at, map, row, x, bar);
-              tma_pair(at + kHalf / 2, map, row + 64, x, bar);
+              if (!of_b || p.tile > 128) tma_pair(at + kHalf / 2, map, row + 64, x, bar);
             } else {
               tma_pair(at, map, x, row, bar);
             }
@@ -222,7 +224,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
     else
       walk(std::false_type());
   } else if (w >= 4) {
-    // ---------------------------------------------------------------- results, a row a thread, 32 columns at a time
+    // ---------------------------------------------------------------- results, a row a thread, 32 columns at a time (16 with two results each: registers)
+    constexpr int kCols = kMode == MM_BACK ? 16 : 32;
     const uint32_t lanes = (uint32_t)(w & 3) << 21;
     const int id = threadIdx.x - 128, half = id >> 7;
     int n = 0;
@@ -244,12 +247,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
         asm volatile("bar.sync 1, 256;" ::: "memory");
       }
       const float xs = e.x_scale && row ? e.x_scale[m] : 1.f;
-      uint4 next[4];
+      uint4 next[kCols / 8];
       auto ask = [&](int c) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int col = t.n0 + 32 * c + 8 * g;
-          next[g] = row && col < e.cols && 32 * c < width ? load8(e.in, m * e.in_stride + col, e.cols - col) : make_uint4(0, 0, 0, 0);
+        for (int g = 0; g < kCols / 8; ++g) {
+          const int col = t.n0 + kCols * c + 8 * g;
+          next[g] = row && col < e.cols && kCols * c < width ? load8(e.in, m * e.in_stride + col, e.cols - col) : make_uint4(0, 0, 0, 0);
         }
       };
       if (e.in) ask(half);
@@ -260,24 +263,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
       mm_with_act(e.act, [&](auto act) {
         constexpr int kAct = decltype(act)::value;
 #pragma unroll 1
-        for (int c = half; 32 * c < width; c += 2) {
-          const int n0 = t.n0 + 32 * c;
+        for (int c = half; kCols * c < width; c += 2) {
+          const int n0 = t.n0 + kCols * c;
           if (n0 >= e.cols) break;
           __syncwarp();
-          uint32_t z[32], u[32];
-          tmem_ld32(z, at + 32 * c);
-          if (kMode != MM_LINEAR) tmem_ld32(u, at + width + 32 * c);
-          uint4 own[4];
+          uint32_t z[kCols], u[kCols];
+          tmem_ld(z, at + kCols * c);
+          if (kMode != MM_LINEAR) tmem_ld(u, at + width + kCols * c);
+          uint4 own[kCols / 8];
           if (e.in) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) own[g] = next[g];
+            for (int g = 0; g < kCols / 8; ++g) own[g] = next[g];
             ask(c + 2);
           }
           wait_ld();
           if (!row) continue;
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int col = n0 + 8 * g, in_tile = 32 * c + 8 * g;
+          for (int g = 0; g < kCols / 8; ++g) {
+            const int col = n0 + 8 * g, in_tile = kCols * c + 8 * g;
             if (col >= e.cols) break;
             float v[8], s[8], second[8];
 #pragma unroll
