@@ -16,21 +16,23 @@
 namespace fs {
 namespace {
 
-constexpr int kStages = 7, kHalf = 128 * kMmBlock, kStage = 2 * kHalf;
+constexpr int kStages = 6, kHalf = 128 * kMmBlock, kStage = 2 * kHalf;
 constexpr int kTile = 256;                  // rows of a tile; its columns at most
-constexpr int kThreads = 12 * 32, kEnders = 8;  // (warps that finish tiles: two for each of the four groups of 32 rows)
 constexpr int kGroup = 8;  // tiles of rows that are walked over together
+
+constexpr int kThreads = 12 * 32, kEnders = 8;  // (warps that finish tiles: two for each of the four groups of 32 rows)
 
 struct WideBars {
   uint64_t full[kStages], empty[kStages], sum_full[2], sum_empty[2];
   uint32_t tmem;
   alignas(16) float scale[kTile];  // of a tile's columns of W (gated: gate's, then up's)
   uint16_t bias[kTile];
+  alignas(16) uint4 pass[kEnders][32 * 4];  // of each warp that finishes tiles: 32 rows' 64 bytes, on their way from or to memory
 };
 // All of an SM's shared memory: no block with tensor memory of its own fits beside one of these, which
 // take all of it. (One that held some while it waits for its cluster, and this pair for each other: none would go on.)
-constexpr size_t kSmem = 1024 + kStages * kStage + sizeof(WideBars);
-static_assert(kSmem > 220 * 1024 && kSmem <= 227 * 1024, "an SM's shared memory, all of it");
+constexpr size_t kSmem = 226 * 1024;
+static_assert(kSmem >= 1024 + kStages * kStage + sizeof(WideBars), "a block's shared memory");
 
 // One tile: of product `p`, rows from m0 and columns (gated: results) from n0.
 struct Tile {
@@ -89,17 +91,20 @@ __device__ __forceinline__ uint4 load8(const void* row, long long at, int n) {
     if (i < n) w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-template <typename T>
-__device__ __forceinline__ void store8(void* row, long long at, const float (&v)[8], int n) {
-  T* p = static_cast<T*>(row) + at;
+__device__ __forceinline__ void store8(void* row, long long at, uint4 v, int n) {
+  uint16_t* p = static_cast<uint16_t*>(row) + at;
   if (n >= 8) {
-    *reinterpret_cast<uint4*>(p) =
-        make_uint4(Elem<T>::pack(v[0], v[1]), Elem<T>::pack(v[2], v[3]), Elem<T>::pack(v[4], v[5]), Elem<T>::pack(v[6], v[7]));
+    *reinterpret_cast<uint4*>(p) = v;
     return;
   }
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (i < n) p[i] = (T)v[i];
+    if (i < n) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
+  return make_uint4(Elem<T>::pack(v[0], v[1]), Elem<T>::pack(v[2], v[3]), Elem<T>::pack(v[4], v[5]), Elem<T>::pack(v[6], v[7]));
 }
 __device__ __forceinline__ void tmem_ld(uint32_t (&r)[32], uint32_t a) { tmem_ld32(r, a); }
 __device__ __forceinline__ void tmem_ld(uint32_t (&r)[16], uint32_t a) { tmem_ld16(r, a); }
@@ -224,15 +229,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
     else
       walk(std::false_type());
   } else if (w >= 4) {
-    // ---------------------------------------------------------------- results, a row a thread, 32 columns at a time (16 with two results each: registers)
-    constexpr int kCols = kMode == MM_BACK ? 16 : 32;
+    // ---------------------------------------------------------------- results, a row a thread, 32 columns at a time (16 with two
+    // results each: registers). Between threads and memory they pass through shared memory, so that a warp's access covers
+    // whole sectors of 8 rows, not 16 bytes of 32 (4096 rows of 1024 8-bit terms over 8192 columns, with a residual: 89 us)
+    constexpr int kCols = kMode == MM_BACK ? 16 : 32, kPieces = kCols / 8;
     const uint32_t lanes = (uint32_t)(w & 3) << 21;
     const int id = threadIdx.x - 128, half = id >> 7;
+    uint4* pass = bars.pass[w - 4];
+    // the 16-byte piece `piece` of row `r` there
+    auto at_piece = [](int r, int piece) { return 4 * r + (piece ^ (r >> 1 & 3)); };
     int n = 0;
     for (long long i = first; i < a.tiles; i += step, ++n) {
       const Tile t = tile_of<kMode>(a, i);
       const MmEpilogue& e = t.p->e;
-      const long long m = t.m0 + rank * 128 + (w & 3) * 32 + lane;
+      const long long m0 = t.m0 + rank * 128 + (w & 3) * 32, m = m0 + lane;
       const bool row = m < e.rows;
       const int width = kMode == MM_LINEAR ? t.p->tile : t.p->tile / 2;  // results of a row
       // what the columns share goes to shared memory, and a row's own first part is asked for, while the sums are made
@@ -247,12 +257,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
         asm volatile("bar.sync 1, 256;" ::: "memory");
       }
       const float xs = e.x_scale && row ? e.x_scale[m] : 1.f;
-      uint4 next[kCols / 8];
+      uint4 next[kPieces];
       auto ask = [&](int c) {
 #pragma unroll
-        for (int g = 0; g < kCols / 8; ++g) {
-          const int col = t.n0 + kCols * c + 8 * g;
-          next[g] = row && col < e.cols && kCols * c < width ? load8(e.in, m * e.in_stride + col, e.cols - col) : make_uint4(0, 0, 0, 0);
+        for (int g = 0; g < kPieces; ++g) {
+          const int r = g * (32 / kPieces) + lane / kPieces, col = t.n0 + kCols * c + 8 * (lane % kPieces);
+          next[g] = m0 + r < e.rows && col < e.cols && kCols * c < width ? load8(e.in, (m0 + r) * e.in_stride + col, e.cols - col) : make_uint4(0, 0, 0, 0);
         }
       };
       if (e.in) ask(half);
@@ -270,18 +280,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
           uint32_t z[kCols], u[kCols];
           tmem_ld(z, at + kCols * c);
           if (kMode != MM_LINEAR) tmem_ld(u, at + width + kCols * c);
-          uint4 own[kCols / 8];
           if (e.in) {
 #pragma unroll
-            for (int g = 0; g < kCols / 8; ++g) own[g] = next[g];
+            for (int g = 0; g < kPieces; ++g) pass[at_piece(g * (32 / kPieces) + lane / kPieces, lane % kPieces)] = next[g];
             ask(c + 2);
+            __syncwarp();
           }
           wait_ld();
-          if (!row) continue;
 #pragma unroll
-          for (int g = 0; g < kCols / 8; ++g) {
-            const int col = n0 + 8 * g, in_tile = kCols * c + 8 * g;
-            if (col >= e.cols) break;
+          for (int g = 0; g < kPieces; ++g) {
+            const int in_tile = kCols * c + 8 * g;
             float v[8], s[8], second[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(z[8 * g + j]), second[j] = kMode != MM_LINEAR ? __uint_as_float(u[8 * g + j]) : 0.f;
@@ -304,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
 #pragma unroll
               for (int j = 0; j < 8; ++j) v[j] = mm_act<kAct>(v[j]);
               if (e.in) {
-                floats8<T>(s, own[g]);
+                floats8<T>(s, pass[at_piece(lane, g)]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] += s[j];
               }
@@ -312,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
 #pragma unroll
               for (int j = 0; j < 8; ++j) v[j] = mm_act<kAct>(v[j]) * second[j];
             } else {
-              floats8<T>(s, own[g]);
+              floats8<T>(s, pass[at_piece(lane, g)]);
 #pragma unroll
               for (int j = 0; j < 8; ++j) {
                 float slope;
@@ -320,9 +328,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
                 v[j] = s[j] * second[j] * slope;
                 second[j] = s[j] * y;
               }
-              store8<T>(e.out[1], m * e.out_stride + col, second, e.cols - col);
+              pass[at_piece(lane, 2 + g)] = pack8<T>(second);
             }
-            store8<T>(e.out[0], m * e.out_stride + col, v, e.cols - col);
+            pass[at_piece(lane, g)] = pack8<T>(v);  // (where its own addend was)
+          }
+          __syncwarp();
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int r = 8 * g + lane / 4, piece = lane % 4, col = n0 + 8 * (piece % kPieces);
+            if (m0 + r < e.rows && col < e.cols)
+              store8(kMode == MM_BACK && piece >= kPieces ? e.out[1] : e.out[0], (m0 + r) * e.out_stride + col, pass[at_piece(r, piece)], e.cols - col);
           }
         }
       });
