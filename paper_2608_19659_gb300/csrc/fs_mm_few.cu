@@ -269,8 +269,10 @@ MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
       // in groups of about 18 SMs, of which some are smaller (one row of 8192 over 2 x 1792 gated, tiles of 64, 280 blocks in clusters of 5: 14.4)
       const int groups = std::max(1, sms / 18);
       const long long blocks = (long long)p.w_tiles * p.token_tiles * cluster, one = cluster == 1 ? sms : 18 / cluster * cluster * groups;
-      const bool two = blocks > one && (110 * 1024 - sums) / slot >= std::min(3, depth);
-      p.stages = std::clamp(((two ? 110 : 216) * 1024 - sums) / slot, 2, std::min(kMaxStages, std::max(2, depth)));
+      const int half = (110 * 1024 - sums) / slot;  // stages of half an SM's shared memory
+      const bool two = blocks > one && half >= std::min(3, depth);
+      // (where half is enough, a block of the next kernel finds room beside this one: a one-token layer of 9 calls 62.5 us without)
+      p.stages = std::clamp(two || half >= 5 ? half : (216 * 1024 - sums) / slot, 2, std::min(kMaxStages, std::max(2, depth)));
       const long long places = !two ? one : cluster == 1 ? 2 * sms : 34 / cluster * cluster * groups;
       const float waves = (float)((blocks + places - 1) / places), rate = two ? 50.f : 100.f;
       const float memory = (float)blocks_k * kMmBlock * cols * (gated ? 2 : 1) / 6600.f, steps = waves * depth * std::max(slot / rate, w_rows == 32 ? 230.f : w_rows == 64 ? 185.f : 165.f);

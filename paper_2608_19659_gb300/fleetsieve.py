@@ -779,21 +779,19 @@ def _mm_type(t, name: str) -> int:
     return kind
 
 
-def _mm_rows(t, name: str, dtype, index: int, rows: int, width: int, scale=None) -> tuple[int, int, int]:
-    """(address, stride, address of the scales) of rows [rows, width]."""
-    shape = t.shape
-    if len(shape) != 2 or shape[0] != rows or shape[1] != width:
-        raise ValueError(f"{name} is [{rows}, {width}], not {tuple(shape)}")
+def _mm_rows(t, name: str, dtype, index: int, size: tuple[int, int], scale=None) -> tuple[int, int, int]:
+    """(address, stride, address of the scales) of rows of that size."""
+    if t.shape != size:
+        raise ValueError(f"{name} is {list(size)}, not {list(t.shape)}")
     s0, s1 = t.stride()
-    if t.dtype is not dtype or t.get_device() != index or (s1 != 1 and width > 1 and rows):
+    if t.dtype is not dtype or t.get_device() != index or (s1 != 1 and size[1] > 1 and size[0]):
         raise ValueError(f"{name}: want {dtype} on cuda:{index}, the last dimension contiguous")
-    at = 0
-    if scale is not None:
-        if (scale.dim() != 1 or scale.shape[0] != rows or scale.element_size() != 4 or not scale.is_floating_point()
-                or not scale.is_contiguous() or scale.get_device() != index):
-            raise ValueError(f"{name}: scales are a contiguous float32 [{rows}] on cuda:{index}")
-        at = scale.data_ptr()
-    return t.data_ptr(), s0, at
+    if scale is None:
+        return t.data_ptr(), s0, 0
+    if (scale.shape != size[:1] or scale.element_size() != 4 or not scale.is_floating_point()
+            or not scale.is_contiguous() or scale.get_device() != index):
+        raise ValueError(f"{name}: scales are a contiguous float32 [{size[0]}] on cuda:{index}")
+    return t.data_ptr(), s0, scale.data_ptr()
 
 
 def _mm_act(activation: str) -> int:
@@ -824,14 +822,15 @@ def fs_linear(x, w, y, *, bias=None, residual=None, activation: str = "none", x_
     residual and y: bfloat16 or float16 (x's type if that is 16-bit). y may be the residual. Returns y."""
     index = _mm_here(workspace)
     kind, out_kind, act = _mm_type(x, "x"), _mm_type(y, "y"), _mm_act(activation)
-    (rows, inner), out, dtype = x.shape, w.shape[0], y.dtype
-    xr = _mm_rows(x, "x", x.dtype, index, rows, inner, x_scale)
-    wr = _mm_rows(w, "w", x.dtype, index, out, inner, w_scale)
-    yr = _mm_rows(y, "y", dtype, index, rows, out)
-    rr = _NO_ROWS if residual is None else _mm_rows(residual, "residual", dtype, index, rows, out)
+    (rows, inner), out, dtype, of_x = x.shape, w.shape[0], y.dtype, x.dtype
+    size = (rows, out)
+    xr = _mm_rows(x, "x", of_x, index, (rows, inner), x_scale)
+    wr = _mm_rows(w, "w", of_x, index, (out, inner), w_scale)
+    yr = _mm_rows(y, "y", dtype, index, size)
+    rr = _NO_ROWS if residual is None else _mm_rows(residual, "residual", dtype, index, size)
     b = 0
     if bias is not None:
-        if bias.dim() != 1 or bias.shape[0] != out or bias.dtype is not dtype or bias.get_device() != index or not bias.is_contiguous():
+        if bias.shape != (out,) or bias.dtype is not dtype or bias.get_device() != index or not bias.is_contiguous():
             raise ValueError(f"bias is a contiguous {dtype} [{out}] on cuda:{index}")
         b = bias.data_ptr()
     a = _MM_LINEAR.pack(rows, inner, out, kind, out_kind, act, *xr, *wr, *rr, *yr, b)
@@ -846,11 +845,12 @@ def fs_gated_ff(x, w_gate, w_up, y, *, activation: str = "silu", x_scale=None, g
     """y [rows, out] = act(x w_gate^T) * (x w_up^T), types as in :func:`fs_linear`. Returns y."""
     index = _mm_here(workspace)
     kind, out_kind, act = _mm_type(x, "x"), _mm_type(y, "y"), _mm_act(activation)
-    (rows, inner), out = x.shape, w_gate.shape[0]
-    xr = _mm_rows(x, "x", x.dtype, index, rows, inner, x_scale)
-    gr = _mm_rows(w_gate, "w_gate", x.dtype, index, out, inner, gate_scale)
-    ur = _mm_rows(w_up, "w_up", x.dtype, index, out, inner, up_scale)
-    yr = _mm_rows(y, "y", y.dtype, index, rows, out)
+    (rows, inner), out, of_x = x.shape, w_gate.shape[0], x.dtype
+    size = (out, inner)
+    xr = _mm_rows(x, "x", of_x, index, (rows, inner), x_scale)
+    gr = _mm_rows(w_gate, "w_gate", of_x, index, size, gate_scale)
+    ur = _mm_rows(w_up, "w_up", of_x, index, size, up_scale)
+    yr = _mm_rows(y, "y", y.dtype, index, (rows, out))
     a = _MM_GATED.pack(rows, inner, out, kind, out_kind, act, *xr, *gr, *ur, *yr)
     rc = lib().fs_gated_ff(a, workspace.address, workspace.bytes, _kv_stream(stream, index))
     if rc:
@@ -865,9 +865,10 @@ def fs_gated_ff_backward(x, w_gate, w_up, dy, dx, dw_gate, dw_up, *, activation:
     index = _mm_here(workspace)
     kind, act, dtype = _mm_type(x, "x"), _mm_act(activation), x.dtype
     (rows, inner), out = x.shape, w_gate.shape[0]
-    parts = [_mm_rows(t, name, dtype, index, n, width) for t, name, n, width in (
-        (x, "x", rows, inner), (w_gate, "w_gate", out, inner), (w_up, "w_up", out, inner), (dy, "dy", rows, out),
-        (dx, "dx", rows, inner), (dw_gate, "dw_gate", out, inner), (dw_up, "dw_up", out, inner))]
+    of_x, of_w = (rows, inner), (out, inner)
+    parts = [_mm_rows(t, name, dtype, index, size) for t, name, size in (
+        (x, "x", of_x), (w_gate, "w_gate", of_w), (w_up, "w_up", of_w), (dy, "dy", (rows, out)),
+        (dx, "dx", of_x), (dw_gate, "dw_gate", of_w), (dw_up, "dw_up", of_w))]
     a = _MM_GRAD.pack(rows, inner, out, kind, act, 0, *(v for p in parts for v in p))
     rc = lib().fs_gated_ff_backward(a, workspace.address, workspace.bytes, _kv_stream(stream, index))
     if rc:
@@ -884,12 +885,12 @@ def fs_quantise_rows(x, codes, scale, *, stream=None):
     index, kind = x.get_device(), _mm_type(x, "x")
     if index < 0 or index != _current_device():
         raise ValueError(f"x is on {x.device}, cuda:{_current_device()} is current")
-    rows, inner = x.shape
+    rows, inner = size = x.shape
     if codes.element_size() != 1:
         raise ValueError(f"codes are {codes.dtype}, not float8_e4m3fn or uint8")
-    xr = _mm_rows(x, "x", x.dtype, index, rows, inner)
-    cr = _mm_rows(codes, "codes", codes.dtype, index, rows, inner, scale)
-    rc = lib().fs_quantise_rows(rows, inner, kind, _MM_ROWS.pack(*xr), _MM_ROWS.pack(cr[0], cr[1], 0), cr[2], _kv_stream(stream, index))
+    xr = _mm_rows(x, "x", x.dtype, index, size)
+    c_at, c_stride, s_at = _mm_rows(codes, "codes", codes.dtype, index, size, scale)
+    rc = lib().fs_quantise_rows(rows, inner, kind, _MM_ROWS.pack(*xr), _MM_ROWS.pack(c_at, c_stride, 0), s_at, _kv_stream(stream, index))
     if rc:
         _check(rc)
     return codes, scale
