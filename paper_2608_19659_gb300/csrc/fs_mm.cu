@@ -58,6 +58,28 @@ int check_rows(fs_mm_rows& r, const char* name, int n, int width, int type, bool
   return FS_OK;
 }
 
+// Whether two operands' rows share a byte, as far as that can be told: exact where rows are equally far apart or one operand has a
+// single row; others are taken for disjoint.
+struct Span {
+  const fs_mm_rows* r;
+  int n, width, size;  // rows, elements of a row, bytes of an element
+};
+bool overlap(const Span& a, const Span& b) {
+  if (!a.n || !b.n || !a.r->data || !b.r->data) return false;
+  const int64_t pa = reinterpret_cast<int64_t>(a.r->data), pb = reinterpret_cast<int64_t>(b.r->data);
+  const int64_t sa = a.n > 1 ? a.r->stride * a.size : 0, sb = b.n > 1 ? b.r->stride * b.size : 0, wa = (int64_t)a.width * a.size, wb = (int64_t)b.width * b.size;
+  if (pa + (a.n - 1) * sa + wa <= pb || pb + (b.n - 1) * sb + wb <= pa) return false;
+  if (sa == 0 && sb == 0) return true;
+  if (sa && sb && sa != sb) return pa == pb;
+  const int64_t s = sa ? sa : sb, d = ((pb - pa) % s + s) % s;
+  return d < wa || s - d < wb;
+}
+
+// Outputs share nothing with inputs and each other.
+int check_apart(const Span& out, const char* out_name, const Span& in, const char* in_name) {
+  return overlap(out, in) ? say(FS_EINVAL, "%s and %s overlap", out_name, in_name) : FS_OK;
+}
+
 constexpr int64_t kMmPartAt = 256;  // the status word, then dg and du of a backward pass
 
 long long padded(int n) { return ((long long)n + 63) & ~63ll; }
@@ -312,6 +334,14 @@ extern "C" int fs_linear(const fs_mm_linear* args, void* workspace, int64_t work
   if (g.residual.data)
     if (int rc = check_rows(g.residual, "residual", g.rows, g.out, g.out_type, true)) return rc;
   if (!aligned(g.bias, 16)) return say(FS_EINVAL, "bias is not 16-byte aligned");
+  const int size = g.type == FS_E4M3 ? 1 : 2;
+  const Span y{&g.y, g.rows, g.out, 2}, r{&g.residual, g.rows, g.out, 2};
+  const fs_mm_rows bias{const_cast<void*>(g.bias), 0, nullptr};
+  if (int rc = check_apart(y, "y", {&g.x, g.rows, g.in, size}, "x")) return rc;
+  if (int rc = check_apart(y, "y", {&g.w, g.out, g.in, size}, "w")) return rc;
+  if (int rc = check_apart(y, "y", {&bias, 1, g.out, 2}, "bias")) return rc;
+  if (g.residual.data != g.y.data || g.residual.stride != g.y.stride)
+    if (int rc = check_apart(y, "y", r, "residual")) return rc;
   MmCall c{g.in, g.type, g.out_type, 0, static_cast<uint32_t*>(workspace), static_cast<cudaStream_t>(cuda_stream), "launch (fs_linear)"};
   if (int rc = device_sms(&c.sms)) return rc;
   return product(c, g.x, g.w, nullptr,
@@ -329,6 +359,11 @@ extern "C" int fs_gated_ff(const fs_mm_gated* args, void* workspace, int64_t wor
   if (int rc = check_rows(g.w_gate, "w_gate", g.out, g.in, g.type)) return rc;
   if (int rc = check_rows(g.w_up, "w_up", g.out, g.in, g.type)) return rc;
   if (int rc = check_rows(g.y, "y", g.rows, g.out, g.out_type)) return rc;
+  const int size = g.type == FS_E4M3 ? 1 : 2;
+  const Span y{&g.y, g.rows, g.out, 2};
+  if (int rc = check_apart(y, "y", {&g.x, g.rows, g.in, size}, "x")) return rc;
+  if (int rc = check_apart(y, "y", {&g.w_gate, g.out, g.in, size}, "w_gate")) return rc;
+  if (int rc = check_apart(y, "y", {&g.w_up, g.out, g.in, size}, "w_up")) return rc;
   MmCall c{g.in, g.type, g.out_type, 0, static_cast<uint32_t*>(workspace), static_cast<cudaStream_t>(cuda_stream), "launch (fs_gated_ff)"};
   if (int rc = device_sms(&c.sms)) return rc;
   return product(c, g.x, g.w_gate, &g.w_up,
@@ -348,6 +383,12 @@ extern "C" int fs_gated_ff_backward(const fs_mm_gated_grad* args, void* workspac
   if (int rc = check_rows(g.dx, "dx", g.rows, g.in, g.type)) return rc;
   if (int rc = check_rows(g.dw_gate, "dw_gate", g.out, g.in, g.type)) return rc;
   if (int rc = check_rows(g.dw_up, "dw_up", g.out, g.in, g.type)) return rc;
+  const Span all[] = {{&g.dx, g.rows, g.in, 2}, {&g.dw_gate, g.out, g.in, 2}, {&g.dw_up, g.out, g.in, 2}, {&g.x, g.rows, g.in, 2},
+                      {&g.w_gate, g.out, g.in, 2}, {&g.w_up, g.out, g.in, 2}, {&g.dy, g.rows, g.out, 2}};
+  const char* const names[] = {"dx", "dw_gate", "dw_up", "x", "w_gate", "w_up", "dy"};
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 7; ++j)
+      if (int rc = check_apart(all[i], names[i], all[j], names[j])) return rc;
   MmCall c{g.in, g.type, g.type, 0, static_cast<uint32_t*>(workspace), static_cast<cudaStream_t>(cuda_stream), "launch (fs_gated_ff_backward)"};
   if (g.rows == 0 || g.out == 0) {  // sums over nothing
     cudaError_t e = cudaSuccess;
@@ -400,6 +441,7 @@ extern "C" int fs_quantise_rows(int32_t rows, int32_t in, int32_t type, const fs
   if (!scale) return say(FS_EINVAL, "scale is NULL");
   if (int rc = check_rows(xr, "x", rows, in, type)) return rc;
   if (int rc = check_rows(cr, "codes", rows, in, FS_E4M3)) return rc;
+  if (int rc = check_apart({&cr, rows, in, 1}, "codes", {&xr, rows, in, 2}, "x")) return rc;
   const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = type == FS_KV_FP16 ? launch_quantise<__half>(rows, in, xr, cr, scale, s) : launch_quantise<__nv_bfloat16>(rows, in, xr, cr, scale, s);
   return e == cudaSuccess ? FS_OK : cuda_say(e, "launch (fs_quantise_rows)");

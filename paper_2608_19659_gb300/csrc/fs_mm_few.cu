@@ -6,6 +6,8 @@
 // others store their sums of those in its shared memory, and after the cluster's one barrier it adds them up, in the order of
 // the ranks, so that bits repeat. (Sums left where they were made and read from there: 64 rows of 8-bit 20.0 us.) Of a gated block a tile has as many rows of gate as of up.
 // One lane keeps copies on their way, one issues products, all four warps take part in the end.
+// Tensor memory is asked for only when the kernels ahead have ended (one of them may still ask for all of it), and given back
+// before the block waits for its cluster: no block that holds some waits for another.
 // Bound by reading W.
 #include <algorithm>
 #include <atomic>
@@ -83,15 +85,10 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
     for (int i = 0; i < p.stages; ++i) mbar_init(&bars.full[i], 1), mbar_init(&bars.empty[i], 1);
     mbar_init(&bars.done, 1);
   }
-  if (w == 2) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(cols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-  }
-  pdl_wait();
-  fence_before();
   __syncthreads();
-  fence_after();
-  const uint32_t tmem = bars.tmem;
+  if (p.cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // (this block has started)
+  pdl_wait();
+  __syncwarp();
 
   // What this thread's four columns of results share, asked for while the sums are made. Block `o` of the cluster finishes the
   // tokens [o share, (o + 1) share) of the tile, each 128 / quads-th of them (128 is a multiple of quads) by this thread.
@@ -130,10 +127,17 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
     }
     if (k < k1)  // a wait ran out: the copies under way first (with the same limit)
       for (int j = max(k0, k - p.stages); j < k; ++j) mbar_wait(&bars.full[(j - k0) % p.stages], ((j - k0) / p.stages) & 1, kWaitLimitNs);
+  } else if (w == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    fence_before();
+    asm volatile("bar.sync 1, 64;" ::: "memory");
   } else if (w == 1) {
     // ---------------------------------------------------------------- products
+    asm volatile("bar.sync 1, 64;" ::: "memory");
+    fence_after();
     const bool one = elect_one();
-    const uint32_t d = __shfl_sync(~0u, tmem, 0);
+    const uint32_t d = __shfl_sync(~0u, bars.tmem, 0);
     auto walk = [&](auto eight) {
       int st = 0;
       uint32_t par = 0;
@@ -159,10 +163,13 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
   __syncwarp();
   const bool ok = mm_wait(&bars.done, 0, a.status);
   fence_after();
+  const uint32_t tmem = bars.tmem;  // (warp 1 has waited for it)
 
   // ---------------------------------------------------------------- sums to where they are added up, [rank][token][row of W]
   const int ld = 4 * p.w_rows;
   const uint32_t sums = smem + a.sums_at;
+  __syncwarp();
+  if (p.cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (all of them have started)
   if (32 * w < p.w_rows && ok) {
     const uint32_t to = sums + rank * share * ld + (32 * w + lane) * 4;
     for (int c = 0, o = 0, rest = share; c < valid; c += 16) {
@@ -194,12 +201,11 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
   ask();
   __syncwarp();
   fence_before();
-  if (p.cluster > 1)
-    cluster_all();  // (the last that any block does with another's shared memory)
-  else
-    __syncthreads();
+  __syncthreads();
   fence_after();
   if (w == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols));
+  __syncwarp();
+  if (p.cluster > 1) cluster_all();  // (the last that any block does with another's shared memory)
 
   // ---------------------------------------------------------------- results, four neighbours of a row at a time
   if (left <= 0) return;
@@ -282,10 +288,7 @@ MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
       p.ns = 2900.f + 350.f * (p.token_tiles - 1) + read + waves * (exchange + 25.f * ((std::min(rows, p.tokens) + cluster - 1) / cluster) * w_rows / 128);
       if (best.w_rows == 0 || p.ns < best.ns) best = p;
     }
-  // shared memory in proportion to the tensor memory, so that blocks that are resident together never wait for each other's
-  int columns = 32;
-  while (columns < best.tokens) columns *= 2;
-  best.smem = std::max<size_t>(1024 + bars_at(best) + sizeof(FewBars), columns * 456);
+  best.smem = 1024 + bars_at(best) + sizeof(FewBars);
   return best;
 }
 

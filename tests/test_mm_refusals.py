@@ -14,15 +14,17 @@ def refused(fsb, rc):
 
 
 def good(fsb, type_=0):
-    """Sizes 3 x 20 x 10, rows of 32."""
+    """Sizes 3 x 20 x 10, rows of 32, each operand at an address of its own."""
+    at = iter(range(P16, 1 << 20, P16))
+
     def rows(codes):
-        return fsb.fs_mm_rows(P16, 32, P16 if codes else None)
+        return fsb.fs_mm_rows(next(at), 32, P16 if codes else None)
 
     head = dict(rows=3, in_=20, out=10, type=type_, activation=0)
-    e, h = rows(type_ == 2), rows(False)
-    linear = fsb.fs_mm_linear(**head, out_type=0, x=e, w=e, residual=h, y=h, bias=P16)
-    gated = fsb.fs_mm_gated(**head, out_type=0, x=e, w_gate=e, w_up=e, y=h)
-    grad = fsb.fs_mm_gated_grad(**head, x=h, w_gate=h, w_up=h, dy=h, dx=h, dw_gate=h, dw_up=h)
+    e = type_ == 2
+    linear = fsb.fs_mm_linear(**head, out_type=0, x=rows(e), w=rows(e), residual=rows(0), y=rows(0), bias=1 << 20)
+    gated = fsb.fs_mm_gated(**head, out_type=0, x=rows(e), w_gate=rows(e), w_up=rows(e), y=rows(0))
+    grad = fsb.fs_mm_gated_grad(**head, x=rows(0), w_gate=rows(0), w_up=rows(0), dy=rows(0), dx=rows(0), dw_gate=rows(0), dw_up=rows(0))
     return {"fs_linear": linear, "fs_gated_ff": gated, "fs_gated_ff_backward": grad}
 
 
@@ -89,6 +91,38 @@ def test_workspace_bias_and_null_structs(fsb):
     for sizes in ((-1, 1, 1, 0), (1, 0, 1, 0), (1, 1, -1, 0), (1, 1, 1, 2)):
         refused(fsb, L.fs_mm_workspace_bytes(*sizes, C.byref(need)))
     refused(fsb, L.fs_mm_workspace_bytes(1, 1, 1, 0, None))
+
+
+OUTPUTS = [("fs_linear", "y", ("x", "w")), ("fs_gated_ff", "y", ("x", "w_gate", "w_up"))] + [
+    ("fs_gated_ff_backward", o, ("x", "w_gate", "w_up", "dy") + tuple(p for p in ("dx", "dw_gate", "dw_up") if p != o)) for o in ("dx", "dw_gate", "dw_up")]
+
+
+@pytest.mark.parametrize("name,out,others", OUTPUTS)
+def test_outputs_that_overlap(fsb, name, out, others):
+    """The same place; the same columns of later rows; columns that meet; a row's end inside another's."""
+    for other in others:
+        for off in (0, 64, 16, -16, 2 * 64 + 16):
+            a = good(fsb)[name]
+            getattr(a, out).data = getattr(a, other).data + off
+            refused(fsb, call(fsb, name, a))
+            assert b"overlap" in fsb.lib().fs_last_error()
+
+
+def test_residual_and_bias_that_overlap(fsb):
+    for off in (64, 16, -16):
+        a = good(fsb)["fs_linear"]
+        a.residual.data = a.y.data + off
+        refused(fsb, call(fsb, "fs_linear", a))
+    a = good(fsb)["fs_linear"]
+    a.residual.data, a.residual.stride = a.y.data, 0  # one of y's rows for all
+    refused(fsb, call(fsb, "fs_linear", a))
+    a = good(fsb)["fs_linear"]
+    a.bias = a.y.data + 64
+    refused(fsb, call(fsb, "fs_linear", a))
+    x = fsb.fs_mm_rows(P16, 32, None)
+    for off, stride in ((0, 64), (0, 32), (64, 64), (16, 64), (-16, 64)):
+        c = fsb.fs_mm_rows(P16 + off, stride, None)
+        refused(fsb, fsb.lib().fs_quantise_rows(3, 20, 0, C.byref(x), C.byref(c), 1 << 20, None))
 
 
 def test_the_workspace_grows_with_every_size(fsb):
