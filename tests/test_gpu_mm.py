@@ -1,5 +1,8 @@
 """The products of a rank's layer against 64 bits (tests/mm_reference.py has the bounds)."""
 
+import math
+import random
+
 import pytest
 
 import mm_reference as ref
@@ -82,6 +85,50 @@ def test_gated(fsb, cuda, T, K, N, kind):
     ref.near(y, ref.gated(x, *w, dt, act, xs, *ws))
     untouched(torch, buf, T, N)
     fsb.fs_mm_check(work)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_sizes_at_random(fsb, cuda, seed):
+    """Sizes, types and activations as they come, every value and what lies around them."""
+    torch = cuda
+    rng = random.Random(seed)
+    size = lambda lo, hi: max(lo, int(math.exp(rng.uniform(math.log(lo), math.log(hi)))) // rng.choice((1, 1, 8, 64)) * rng.choice((1, 8)))  # noqa: E731
+    for _ in range(4):
+        T, K, N, kind = min(size(1, 1600), 2500), min(size(1, 3000), 4000), min(size(1, 3000), 4000), rng.choice(KINDS)
+        act, bias, residual = rng.choice(list(fsb.ACTIVATIONS)), rng.random() < 0.5, rng.random() < 0.5
+        x, w, xs, ws, dt = operands(torch, kind, T, K, N, 2, seed, 16)
+        y, buf = rows(torch, T, N, dt, 0, extra=8)
+        work = fsb.MmWorkspace(T, K, N)
+        b = rows(torch, 1, N, dt, 7)[0][0] if bias else None
+        r = rows(torch, T, N, dt, 8)[0] if residual else None
+        fsb.fs_linear(x, w[0], y, bias=b, residual=r, activation=act, x_scale=xs, w_scale=ws[0], workspace=work)
+        ref.near(y, ref.linear(x, w[0], dt, b, r, act, xs, ws[0]))
+        untouched(torch, buf, T, N)
+        fsb.fs_gated_ff(x, *w, y, activation=act, x_scale=xs, gate_scale=ws[0], up_scale=ws[1], workspace=work)
+        ref.near(y, ref.gated(x, *w, dt, act, xs, *ws))
+        untouched(torch, buf, T, N)
+        fsb.fs_mm_check(work)
+
+
+def test_another_stream(fsb, cuda):
+    """Calls go to the stream that is asked for, or to torch's current one, after what was put there before."""
+    torch = cuda
+    other = torch.cuda.Stream()
+    for T in (3, 500):
+        x, (w,), _, _, dt = operands(torch, "bfloat16", T, 300, 200, 1, 3)
+        late = rows(torch, T, 300, dt, 9)[0]
+        y, z = (rows(torch, T, 200, dt, 0)[0] for _ in range(2))
+        work, more = fsb.MmWorkspace(T, 300, 200), fsb.MmWorkspace(T, 300, 200)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            torch.cuda._sleep(20_000_000)
+            x.copy_(late)
+            fsb.fs_linear(x, w, y, workspace=work)
+        fsb.fs_linear(x, w, z, workspace=more, stream=other)
+        fsb.fs_mm_check(work, stream=other)
+        fsb.fs_mm_check(more, stream=other)
+        ref.near(y, ref.linear(late, w, dt))
+        assert torch.equal(y, z)
 
 
 BACK = [(1, 64, 16), (1, 1, 1), (2, 7, 3), (77, 520, 1003), (128, 128, 128), (129, 65, 257), (300, 1000, 64), (513, 264, 520), (64, 2050, 300),
@@ -211,7 +258,8 @@ def test_strides(fsb, cuda, T):
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
-@pytest.mark.parametrize("T,K", [(1, 1), (1, 8), (3, 7), (64, 8192), (5, 8193), (300, 257), (2, 16384), (3, 20001), (1000, 128), (7, 70000)])
+@pytest.mark.parametrize("T,K", [(1, 1), (1, 8), (3, 7), (64, 8192), (5, 8193), (300, 257), (2, 16384), (3, 20001), (1000, 128), (7, 70000),
+                                 (257, 2049), (300, 8200), (260, 24000), (270, 24001), (256, 8192), (40, 8193)])
 def test_quantise(fsb, cuda, T, K, dtype):
     torch = cuda
     dt = getattr(torch, dtype)
@@ -231,16 +279,17 @@ def test_quantise(fsb, cuda, T, K, dtype):
     assert bool((buf[T:] == 5).all()) and bool((buf[:T, K:] == 5).all())
 
 
-def test_quantise_not_finite_and_tiny(fsb, cuda):
+@pytest.mark.parametrize("T,K", [(6, 200), (6, 5003), (6, 9001), (6, 25003), (300, 4001)])
+def test_quantise_not_finite_and_tiny(fsb, cuda, T, K):
     torch = cuda
     for dt in (torch.bfloat16, torch.float16):
-        x = torch.randn(6, 200, device="cuda").to(dt)
-        x[0, 3], x[1, 199], x[2, 0] = float("nan"), float("inf"), float("-inf")
+        x = rows(torch, T, K, dt, 1)[0]
+        x[0, 3], x[1, K - 1], x[2, 0] = float("nan"), float("inf"), float("-inf")
         x[3] = float("inf")
         x[4] = 0
         x[4, 7] = torch.finfo(dt).smallest_normal / (4 if dt == torch.float16 else 1)
         x[5] *= 2.0**-14
-        c, s = torch.empty(6, 208, dtype=torch.uint8, device="cuda")[:, :200], torch.empty(6, device="cuda")
+        c, s = torch.empty(T, -(-K // 16) * 16, dtype=torch.uint8, device="cuda")[:, :K], torch.empty(T, device="cuda")
         fsb.fs_quantise_rows(x, c, s)
         want, scale = ref.quantise(x)
         assert torch.equal(s.double(), scale)
