@@ -23,6 +23,7 @@ constexpr int kMaxCluster = 8;
 struct FewBars {
   uint64_t full[kMaxStages], empty[kMaxStages], done;
   uint32_t tmem;
+  float x_scale[128];  // of the tokens that this block finishes
 };
 
 struct MmFewArgs {
@@ -49,6 +50,11 @@ __device__ __forceinline__ void mma_few(uint32_t d, uint64_t a, uint64_t b, uint
 
 __device__ __forceinline__ void st_cluster(uint32_t a, uint32_t x) {
   asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(a), "r"(x) : "memory");
+}
+
+// Tokens of a tile that a block of the cluster finishes: eights, as they come out of tensor memory, or all of fewer.
+__host__ __device__ __forceinline__ int tokens_each(int valid, int cluster) {
+  return valid < 8 ? valid : ((valid + cluster - 1) / cluster + 7) / 8 * 8;
 }
 
 // The sum of four floats of every block of the cluster, `step` bytes apart in this one's shared memory, in the order of the ranks.
@@ -93,11 +99,12 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
   // What this thread's four columns of results share, asked for while the sums are made. Block `o` of the cluster finishes the
   // tokens [o share, (o + 1) share) of the tile, each 128 / quads-th of them (128 is a multiple of quads) by this thread.
   const MmEpilogue& e = a.e;
-  const int quads = width / 4, valid = min(p.tokens, e.rows - t0), share = (valid + p.cluster - 1) / p.cluster;
+  const int quads = width / 4, valid = min(p.tokens, e.rows - t0), share = tokens_each(valid, p.cluster);
   const int first = rank * share, mine = max(0, min(valid - first, share));
   const int n = n0 + 4 * (threadIdx.x % quads), left = e.cols - n, t_step = 128 / quads;
   float4 scale0{}, scale1{};
   uint2 bias{};
+  if (e.x_scale && (int)threadIdx.x < mine) bars.x_scale[threadIdx.x] = e.x_scale[t0 + first + threadIdx.x];
   if (left > 0 && mine > 0) {
     if (e.x_scale) {
       scale0 = mm_load4(e.w_scale[0] + n, left);
@@ -171,34 +178,40 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
   __syncwarp();
   if (p.cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (all of them have started)
   if (32 * w < p.w_rows && ok) {
-    const uint32_t to = sums + rank * share * ld + (32 * w + lane) * 4;
-    for (int c = 0, o = 0, rest = share; c < valid; c += 16) {
-      uint32_t x[16];
-      tmem_ld16(x, tmem + ((uint32_t)(32 * w) << 16) + c);
+    const uint32_t to = sums + rank * share * ld + (32 * w + lane) * 4, from = tmem + ((uint32_t)(32 * w) << 16);
+    if (valid < 8) {  // all of them the first block's
+      uint32_t x[8];
+      tmem_ld8(x, from);
       wait_ld();
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (c + i < valid) st_cluster(cluster_addr(to + (share - rest) * ld, o), x[i]);
-        if (--rest == 0) rest = share, ++o;
+      for (int i = 0; i < 8; ++i)
+        if (i < valid) st_cluster(cluster_addr(to + i * ld, 0), x[i]);
+    } else {
+      for (int o = 0; o * share < valid; ++o) {
+        const uint32_t there = cluster_addr(to, o);
+        for (int c = 0; c < share && o * share + c < valid; c += 8) {
+          uint32_t x[8];
+          tmem_ld8(x, from + o * share + c);
+          wait_ld();
+          if (o == rank) {  // (its own by the short way)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + (c + i) * ld), "r"(x[i]) : "memory");
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) st_cluster(there + (c + i) * ld, x[i]);
+          }
+        }
       }
     }
   }
-  // what a token adds, some tokens at a time: the first of them while the sums are on their way
-  constexpr int kAtOnce = 4;
-  float xs[kAtOnce];
-  uint2 extra[kAtOnce];
+  // what a token adds, a token ahead: the first while the sums are on their way
   int t = threadIdx.x / quads;
-  auto ask = [&] {
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      const int ti = t + i * t_step;
-      const long long m = t0 + first + ti;
-      const bool in = ti < mine && left > 0;
-      xs[i] = in && e.x_scale ? e.x_scale[m] : 1.f;
-      if (!kGated) extra[i] = in && e.in ? mm_raw4(static_cast<const uint16_t*>(e.in) + m * e.in_stride + n, left) : uint2{};
-    }
+  auto ask = [&](int ti) {
+    return !kGated && e.in && ti < mine && left > 0
+               ? mm_raw4(static_cast<const uint16_t*>(e.in) + (long long)(t0 + first + ti) * e.in_stride + n, left)
+               : uint2{};
   };
-  ask();
+  uint2 extra = ask(t);
   __syncwarp();
   fence_before();
   __syncthreads();
@@ -211,25 +224,22 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
   if (left <= 0) return;
   mm_with_act(e.act, [&](auto act) {
     constexpr int kAct = decltype(act)::value;
-    while (t < mine) {
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        const int ti = t + i * t_step;
-        if (ti >= mine) break;
-        const uint32_t at = sums + ti * ld + 16 * (threadIdx.x % quads);
-        float4 z = sum4(at, share * ld, p.cluster), u = z;
-        if (kGated) u = sum4(at + width * 4, share * ld, p.cluster);
-        if (e.x_scale) {
-          z = z * xs[i] * scale0;
-          if (kGated) u = u * xs[i] * scale1;
-        }
-        if (!kGated) z = z + mm_floats4<T>(bias);
-        z = make_float4(mm_act<kAct>(z.x), mm_act<kAct>(z.y), mm_act<kAct>(z.z), mm_act<kAct>(z.w));
-        z = kGated ? z * u : z + mm_floats4<T>(extra[i]);
-        mm_store4(static_cast<T*>(e.out[0]) + (t0 + first + ti) * e.out_stride + n, z, left);
+#pragma unroll 1
+    for (; t < mine; t += t_step) {  // (a small loop: its code is fetched once, while nothing else goes on)
+      const uint2 own = extra;
+      extra = ask(t + t_step);
+      const uint32_t at = sums + t * ld + 16 * (threadIdx.x % quads);
+      float4 z = sum4(at, share * ld, p.cluster), u = z;
+      if (kGated) u = sum4(at + width * 4, share * ld, p.cluster);
+      if (e.x_scale) {
+        const float xs = bars.x_scale[t];
+        z = z * xs * scale0;
+        if (kGated) u = u * xs * scale1;
       }
-      t += kAtOnce * t_step;
-      if (t < mine) ask();
+      if (!kGated) z = z + mm_floats4<T>(bias);
+      z = make_float4(mm_act<kAct>(z.x), mm_act<kAct>(z.y), mm_act<kAct>(z.z), mm_act<kAct>(z.w));
+      z = kGated ? z * u : z + mm_floats4<T>(own);
+      mm_store4(static_cast<T*>(e.out[0]) + (t0 + first + t) * e.out_stride + n, z, left);
     }
   });
 }
@@ -248,9 +258,9 @@ int ring_bytes(const MmFewPlan& p) {
   return std::max(p.stages * slot, (p.stages - 1) * slot + 128 * kMmBlock);
 }
 // A cluster's sums come while a block's own products may still read its ring; those of a single block do not.
-int sums_bytes(const MmFewPlan& p) { return (p.tokens + p.cluster - 1) / p.cluster * p.cluster * p.w_rows * 4; }
+int sums_bytes(const MmFewPlan& p, int rows) { return tokens_each(std::min(p.tokens, rows), p.cluster) * p.cluster * p.w_rows * 4; }
 int sums_at(const MmFewPlan& p) { return p.cluster > 1 ? ring_bytes(p) : 0; }
-int bars_at(const MmFewPlan& p) { return std::max(ring_bytes(p), sums_at(p) + sums_bytes(p)); }
+int bars_at(const MmFewPlan& p, int rows) { return std::max(ring_bytes(p), sums_at(p) + sums_bytes(p, rows)); }
 
 }  // namespace
 
@@ -270,12 +280,12 @@ MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
       p.tokens = ((rows + p.token_tiles - 1) / p.token_tiles + 15) / 16 * 16;
       const int width = gated ? w_rows / 2 : w_rows, slot = (w_rows + p.tokens) * kMmBlock, depth = (blocks_k + cluster - 1) / cluster;
       p.w_tiles = (cols + width - 1) / width;
-      const int sums = cluster > 1 ? sums_bytes(p) : 0;
+      const int sums = cluster > 1 ? sums_bytes(p, rows) : 0;
       // one block an SM if all of them find a place so, else two where each has three stages of its own. Clusters find theirs
       // in groups of about 18 SMs, of which some are smaller (one row of 8192 over 2 x 1792 gated, tiles of 64, 280 blocks in clusters of 5: 14.4)
       const int groups = std::max(1, sms / 18);
       const long long blocks = (long long)p.w_tiles * p.token_tiles * cluster, one = cluster == 1 ? sms : 18 / cluster * cluster * groups;
-      const int half = (110 * 1024 - sums) / slot;  // stages of half an SM's shared memory
+      const int half = (111 * 1024 - sums) / slot;  // stages of half an SM's shared memory
       const bool two = blocks > one && half >= std::min(3, depth);
       // (where half is enough, a block of the next kernel finds room beside this one: a one-token layer of 9 calls 62.5 us without)
       p.stages = std::clamp(two || half >= 5 ? half : (216 * 1024 - sums) / slot, 2, std::min(kMaxStages, std::max(2, depth)));
@@ -285,16 +295,16 @@ MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
       const float read = std::max(memory, steps) + 0.25f * std::min(memory, steps);
       const float exchange = cluster > 1 ? 550.f + std::min(rows, p.tokens) * w_rows * 4 * (cluster - 1) / (50.f * cluster) : 0.f;
       // (and a block's last part, 25 ns a token of 128 rows of W; and 350 ns for each further tile of tokens)
-      p.ns = 2900.f + 350.f * (p.token_tiles - 1) + read + waves * (exchange + 25.f * ((std::min(rows, p.tokens) + cluster - 1) / cluster) * w_rows / 128);
+      p.ns = 2900.f + 350.f * (p.token_tiles - 1) + read + waves * (exchange + 25.f * tokens_each(std::min(rows, p.tokens), cluster) * w_rows / 128);
       if (best.w_rows == 0 || p.ns < best.ns) best = p;
     }
-  best.smem = 1024 + bars_at(best) + sizeof(FewBars);
+  best.smem = 1024 + bars_at(best, rows) + sizeof(FewBars);
   return best;
 }
 
 cudaError_t launch_mm_few(const CUtensorMap& x, const CUtensorMap& w, const CUtensorMap* up, const MmEpilogue& e, const MmFewPlan& p,
                           int blocks_k, int type, int out_type, uint32_t* status, cudaStream_t s) {
-  const MmFewArgs a{e, p, blocks_k, type == FS_E4M3, bars_at(p), sums_at(p), mm_instr(128, p.tokens, type == FS_KV_BF16 ? 1 : 0), status};
+  const MmFewArgs a{e, p, blocks_k, type == FS_E4M3, bars_at(p, e.rows), sums_at(p), mm_instr(128, p.tokens, type == FS_KV_BF16 ? 1 : 0), status};
   const bool h = out_type == FS_KV_FP16;
   if (up) return h ? launch<__half, true>(x, w, *up, a, s) : launch<__nv_bfloat16, true>(x, w, *up, a, s);
   return h ? launch<__half, false>(x, w, w, a, s) : launch<__nv_bfloat16, false>(x, w, w, a, s);

@@ -36,6 +36,12 @@ __device__ __forceinline__ void tmem_ld32(uint32_t (&r)[32], uint32_t a) {
       : "r"(a)
       : "memory");
 }
+__device__ __forceinline__ void tmem_ld8(uint32_t (&r)[8], uint32_t a) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(a)
+               : "memory");
+}
 __device__ __forceinline__ void tmem_ld16(uint32_t (&r)[16], uint32_t a) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
