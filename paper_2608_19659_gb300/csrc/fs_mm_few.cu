@@ -5,7 +5,7 @@
 // nothing in bandwidth. Its sum is split over the blocks of a cluster. Each of them finishes some of the tile's tokens: the
 // others store their sums of those in its shared memory, and after the cluster's one barrier it adds them up, in the order of
 // the ranks, so that bits repeat. (Sums left where they were made and read from there: 64 rows of 8-bit 20.0 us.) Of a gated block a tile has as many rows of gate as of up.
-// One lane keeps copies on their way, one issues products, all four warps take part in the end.
+// One warp keeps copies on their way, one issues products, all eight take part in the end.
 // Tensor memory is asked for only when the kernels ahead have ended (one of them may still ask for all of it), and given back
 // before the block waits for its cluster: no block that holds some waits for another.
 // Bound by reading W.
@@ -19,6 +19,7 @@ namespace {
 
 constexpr int kMaxStages = 12;
 constexpr int kMaxCluster = 8;
+constexpr int kThreads = 256;
 
 struct FewBars {
   uint64_t full[kMaxStages], empty[kMaxStages], done;
@@ -71,7 +72,7 @@ __device__ __forceinline__ float4 sum4(uint32_t a, int step, int cluster) {
 }
 
 template <typename T, bool kGated>
-__global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw,
+__global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw,
                                                 const __grid_constant__ CUtensorMap mu, const MmFewArgs a) {
   extern __shared__ unsigned char raw[];
   const uint32_t smem = (smem_u32(raw) + 1023) & ~1023u;
@@ -97,11 +98,11 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
   __syncwarp();
 
   // What this thread's four columns of results share, asked for while the sums are made. Block `o` of the cluster finishes the
-  // tokens [o share, (o + 1) share) of the tile, each 128 / quads-th of them (128 is a multiple of quads) by this thread.
+  // tokens [o share, (o + 1) share) of the tile, each kThreads / quads-th of them (kThreads is a multiple of quads) by this thread.
   const MmEpilogue& e = a.e;
   const int quads = width / 4, valid = min(p.tokens, e.rows - t0), share = tokens_each(valid, p.cluster);
   const int first = rank * share, mine = max(0, min(valid - first, share));
-  const int n = n0 + 4 * (threadIdx.x % quads), left = e.cols - n, t_step = 128 / quads;
+  const int n = n0 + 4 * (threadIdx.x % quads), left = e.cols - n, t_step = kThreads / quads;
   float4 scale0{}, scale1{};
   uint2 bias{};
   if (e.x_scale && (int)threadIdx.x < mine) bars.x_scale[threadIdx.x] = e.x_scale[t0 + first + threadIdx.x];
@@ -177,19 +178,22 @@ __global__ void __launch_bounds__(128) k_mm_few(const __grid_constant__ CUtensor
   const uint32_t sums = smem + a.sums_at;
   __syncwarp();
   if (p.cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (all of them have started)
-  if (32 * w < p.w_rows && ok) {
-    const uint32_t to = sums + rank * share * ld + (32 * w + lane) * 4, from = tmem + ((uint32_t)(32 * w) << 16);
+  const int group = 32 * (w & 3);  // rows of W that this warp reaches; of two such warps one takes every second eight tokens
+  if (group < p.w_rows && ok) {
+    const uint32_t to = sums + rank * share * ld + (group + lane) * 4, from = tmem + ((uint32_t)group << 16);
     if (valid < 8) {  // all of them the first block's
+      if (w < 4) {
       uint32_t x[8];
       tmem_ld8(x, from);
       wait_ld();
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if (i < valid) st_cluster(cluster_addr(to + i * ld, 0), x[i]);
+      }
     } else {
       for (int o = 0; o * share < valid; ++o) {
         const uint32_t there = cluster_addr(to, o);
-        for (int c = 0; c < share && o * share + c < valid; c += 8) {
+        for (int c = 8 * (w >> 2); c < share && o * share + c < valid; c += 16) {
           uint32_t x[8];
           tmem_ld8(x, from + o * share + c);
           wait_ld();
@@ -249,7 +253,7 @@ cudaError_t launch(const CUtensorMap& x, const CUtensorMap& w, const CUtensorMap
   static std::atomic<uint64_t> seen{0};
   const cudaError_t limit = smem_limit_once(seen, reinterpret_cast<const void*>(k_mm_few<T, kGated>), 227 * 1024);
   if (limit != cudaSuccess) return limit;
-  return launch_clusters(k_mm_few<T, kGated>, dim3(a.p.w_tiles * a.p.cluster, a.p.token_tiles), dim3(128), a.p.cluster, a.p.smem, s, x, w, u, a);
+  return launch_clusters(k_mm_few<T, kGated>, dim3(a.p.w_tiles * a.p.cluster, a.p.token_tiles), dim3(kThreads), a.p.cluster, a.p.smem, s, x, w, u, a);
 }
 
 int ring_bytes(const MmFewPlan& p) {
@@ -265,15 +269,17 @@ int bars_at(const MmFewPlan& p, int rows) { return std::max(ring_bytes(p), sums_
 }  // namespace
 
 // The tile and the cluster by an estimate of the time. What it goes by, and what the other choice cost where it decides (us, in
-// graphs): memory at 6.6 TB/s; a block takes 100 bytes a ns, half of that beside another on its SM, and 165 ns a step at
-// least, more with fewer rows of W (one row of 1024 8-bit over 8192, tiles of 32 6.0, of 64 5.6, of 128 5.5 and in clusters of three 5.2; 64 rows of 8-bit over 10240 rows of W: 240 blocks 18.7, 160 21.0, 80 20.8; one row of 8192 over 2 x 1792 gated, tiles of
-// 128 in clusters of 6 12.1, of 32 without 24.5); a quarter of the lesser of both, as they do not overlap in whole; a cluster's exchange
-// 0.55 us and 50 bytes a ns (333 rows of 1001 over 777, tiles of 64 6.4, of 128 6.7); blocks beyond what is resident wait for
-// a place (100 rows of 4096 over 2560, 120 blocks 9.8, 160 15.9).
+// graphs): memory at 6.6 TB/s; a block takes 100 bytes a ns, half of that beside another on its SM, 65 alone with
+// half of its shared memory, and 165 ns a step at
+// least, more with fewer rows of W (one row of 1024 8-bit over 8192, tiles of 32 6.0, of 64 5.6, of 128 5.5; 64 rows of 8192 8-bit over
+// 10240, 240 blocks 18.7, 160 21.0, 80 20.8; one row of 8192 over 2 x 1792 gated, tiles of 128 in clusters of 6 12.1, of 32
+// without 24.5); a quarter of the lesser of both, as they do not overlap in whole; a cluster's exchange 0.55 us and 50 bytes a ns
+// (333 rows of 1001 over 777, tiles of 64 in clusters of three 5.8, of six 7.3); blocks beyond what is resident wait for a place (100 rows of
+// 4096 over 2560, 120 blocks 9.8, 160 15.9).
 MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
   MmFewPlan best{};
   for (int w_rows = 128; w_rows >= 32; w_rows /= 2)
-    for (int cluster = 1; cluster <= std::min(kMaxCluster, blocks_k); ++cluster) {
+    for (int cluster = std::min(kMaxCluster, blocks_k); cluster >= 1; --cluster) {
       MmFewPlan p{};
       p.w_rows = w_rows, p.cluster = cluster;
       p.token_tiles = (rows + 127) / 128;
@@ -287,16 +293,20 @@ MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
       const long long blocks = (long long)p.w_tiles * p.token_tiles * cluster, one = cluster == 1 ? sms : 18 / cluster * cluster * groups;
       const int half = (111 * 1024 - sums) / slot;  // stages of half an SM's shared memory
       const bool two = blocks > one && half >= std::min(3, depth);
-      // (where half is enough, a block of the next kernel finds room beside this one: a one-token layer of 9 calls 62.5 us without)
-      p.stages = std::clamp(two || half >= 5 ? half : (216 * 1024 - sums) / slot, 2, std::min(kMaxStages, std::max(2, depth)));
+      // (where half is enough, for short sums, a block of the next kernel finds room beside this one: a one-token layer of 9 calls 62.5
+      // us without, 54.3 with it; 48 rows of 8192 8-bit over 2 x 7168 gated, 64 steps, 23.4 with it and 22.1 without)
+      const bool less = !two && half >= 5 && depth <= 32;
+      p.stages = std::clamp(two || less ? half : (216 * 1024 - sums) / slot, 2, std::min(kMaxStages, std::max(2, depth)));
       const long long places = !two ? one : cluster == 1 ? 2 * sms : 34 / cluster * cluster * groups;
-      const float waves = (float)((blocks + places - 1) / places), rate = two ? 50.f : 100.f;
+      const float waves = (float)((blocks + places - 1) / places), rate = two ? 50.f : less ? 65.f : 100.f;
       const float memory = (float)blocks_k * kMmBlock * cols * (gated ? 2 : 1) / 6600.f, steps = waves * depth * std::max(slot / rate, w_rows == 32 ? 230.f : w_rows == 64 ? 185.f : 165.f);
       const float read = std::max(memory, steps) + 0.25f * std::min(memory, steps);
-      const float exchange = cluster > 1 ? 550.f + std::min(rows, p.tokens) * w_rows * 4 * (cluster - 1) / (50.f * cluster) : 0.f;
-      // (and a block's last part, 25 ns a token of 128 rows of W; and 350 ns for each further tile of tokens)
-      p.ns = 2900.f + 350.f * (p.token_tiles - 1) + read + waves * (exchange + 25.f * tokens_each(std::min(rows, p.tokens), cluster) * w_rows / 128);
-      if (best.w_rows == 0 || p.ns < best.ns) best = p;
+      // what comes after the sums, a third longer beside another block: a cluster's exchange; 4 ns a token, 8 more for those that
+      // go to other blocks, 15 for those that it finishes (of 128 rows of W). 150 ns for each further tile of tokens
+      const float tokens = (float)std::min(rows, p.tokens), gone = (float)(cluster - 1) / cluster;
+      const float after = (cluster > 1 ? 550.f : 0.f) + tokens * (4.f + gone * (8.f + w_rows / 12.5f)) + 15.f * tokens_each((int)tokens, cluster) * w_rows / 128;
+      p.ns = 2600.f + 150.f * (p.token_tiles - 1) + read + waves * after * (two ? 1.3f : 1.f);
+      if (best.w_rows == 0 || p.ns < 0.995f * best.ns) best = p;
     }
   best.smem = 1024 + bars_at(best, rows) + sizeof(FewBars);
   return best;

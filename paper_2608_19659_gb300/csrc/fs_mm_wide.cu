@@ -381,7 +381,7 @@ int mm_wide_tile(int rows, int cols, int blocks, bool gated, int sms, float* ns)
     const float waves = (float)((tiles + sms / 2 - 1) / std::max(1, sms / 2));
     const float again = 1.f + 0.08f * (256.f / tile - 1.f) * std::min(waves, 4.f);
     const float sums = waves * blocks * std::max(1.09f * tile, 172.f) * again, memory = (float)blocks * kMmBlock * cols * (gated ? 2 : 1) / 6600.f;
-    const float t = std::max(sums, memory) + 0.25f * std::min(sums, memory) + 4200.f + 8.f * tile;
+    const float t = std::max(sums, memory) + 0.25f * std::min(sums, memory) + 4000.f + 8.f * tile;
     if (!best || t < *ns) best = tile, *ns = t;
   }
   return best;
