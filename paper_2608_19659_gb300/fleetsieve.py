@@ -762,20 +762,25 @@ class MmWorkspace:
         _check(lib().fs_mm_workspace_bytes(int(rows), int(in_features), int(out_features), int(backward), C.byref(n)))
         self.index = _current_device()
         self.tensor = torch.zeros(n.value, dtype=torch.uint8, device=f"cuda:{self.index}")
+        _mm_known()
         self.address, self.bytes = self.tensor.data_ptr(), n.value
 
 
 _mm_kinds = {}  # torch dtype -> FS_KV_* or FS_E4M3
 
 
-def _mm_type(t, name: str) -> int:
+def _mm_known() -> dict:
     if not _mm_kinds:
         import torch
 
         _mm_kinds.update({torch.bfloat16: FS_KV_BF16, torch.float16: FS_KV_FP16, torch.float8_e4m3fn: FS_E4M3})
-    kind = _mm_kinds.get(t.dtype)
+    return _mm_kinds
+
+
+def _mm_type(dtype, name: str) -> int:
+    kind = _mm_known().get(dtype)
     if kind is None:
-        raise ValueError(f"{name} is {t.dtype}, not bfloat16, float16 or float8_e4m3fn")
+        raise ValueError(f"{name} is {dtype}, not bfloat16, float16 or float8_e4m3fn")
     return kind
 
 
@@ -794,19 +799,18 @@ def _mm_rows(t, name: str, dtype, index: int, size: tuple[int, int], scale=None)
     return t.data_ptr(), s0, scale.data_ptr()
 
 
-def _mm_act(activation: str) -> int:
-    act = ACTIVATIONS.get(activation)
-    if act is None:
-        raise ValueError(f"activation {activation!r} is none of {', '.join(ACTIVATIONS)}")
-    return act
-
-
-def _mm_here(workspace: MmWorkspace) -> int:
-    """The workspace's device, which has to be the current one: calls are launched there."""
+def _mm_head(workspace: MmWorkspace, x, y, activation: str) -> tuple[int, int, int, int]:
+    """(device, type of x, type of y, activation) of a call; the workspace's device has to be the current one: calls are launched
+    there."""
     index = workspace.index
     if index != _current_device():
         raise ValueError(f"cuda:{_current_device()} is current, the workspace is on cuda:{index}")
-    return index
+    kind, out_kind, act = _mm_kinds.get(x.dtype), _mm_kinds.get(y.dtype), ACTIVATIONS.get(activation)
+    if kind is None or out_kind is None:
+        kind, out_kind = _mm_type(x.dtype, "x"), _mm_type(y.dtype, "y")
+    if act is None:
+        raise ValueError(f"activation {activation!r} is none of {', '.join(ACTIVATIONS)}")
+    return index, kind, out_kind, act
 
 
 _NO_ROWS = (0, 0, 0)
@@ -820,8 +824,7 @@ def fs_linear(x, w, y, *, bias=None, residual=None, activation: str = "none", x_
     """y [rows, out] = act(x [rows, in] w [out, in]^T + bias) + residual, enqueued on ``stream`` (default: torch's
     current one). x and w: both bfloat16, both float16, or both float8_e4m3fn with x_scale [rows] and w_scale [out]; bias,
     residual and y: bfloat16 or float16 (x's type if that is 16-bit). y may be the residual. Returns y."""
-    index = _mm_here(workspace)
-    kind, out_kind, act = _mm_type(x, "x"), _mm_type(y, "y"), _mm_act(activation)
+    index, kind, out_kind, act = _mm_head(workspace, x, y, activation)
     (rows, inner), out, dtype, of_x = x.shape, w.shape[0], y.dtype, x.dtype
     size = (rows, out)
     xr = _mm_rows(x, "x", of_x, index, (rows, inner), x_scale)
@@ -843,8 +846,7 @@ def fs_linear(x, w, y, *, bias=None, residual=None, activation: str = "none", x_
 def fs_gated_ff(x, w_gate, w_up, y, *, activation: str = "silu", x_scale=None, gate_scale=None, up_scale=None,
                 workspace: MmWorkspace, stream=None):
     """y [rows, out] = act(x w_gate^T) * (x w_up^T), types as in :func:`fs_linear`. Returns y."""
-    index = _mm_here(workspace)
-    kind, out_kind, act = _mm_type(x, "x"), _mm_type(y, "y"), _mm_act(activation)
+    index, kind, out_kind, act = _mm_head(workspace, x, y, activation)
     (rows, inner), out, of_x = x.shape, w_gate.shape[0], x.dtype
     size = (out, inner)
     xr = _mm_rows(x, "x", of_x, index, (rows, inner), x_scale)
@@ -862,9 +864,8 @@ def fs_gated_ff_backward(x, w_gate, w_up, dy, dx, dw_gate, dw_up, *, activation:
                          workspace: MmWorkspace, stream=None):
     """The gradients of :func:`fs_gated_ff` (bfloat16 or float16 throughout), given dy, into dx, dw_gate and dw_up, which
     it returns. ``workspace`` is one made with backward=True."""
-    index = _mm_here(workspace)
-    kind, act, dtype = _mm_type(x, "x"), _mm_act(activation), x.dtype
-    (rows, inner), out = x.shape, w_gate.shape[0]
+    index, kind, _, act = _mm_head(workspace, x, x, activation)
+    (rows, inner), out, dtype = x.shape, w_gate.shape[0], x.dtype
     of_x, of_w = (rows, inner), (out, inner)
     parts = [_mm_rows(t, name, dtype, index, size) for t, name, size in (
         (x, "x", of_x), (w_gate, "w_gate", of_w), (w_up, "w_up", of_w), (dy, "dy", (rows, out)),
@@ -882,13 +883,14 @@ _MM_ROWS = struct.Struct("=Qqq")
 def fs_quantise_rows(x, codes, scale, *, stream=None):
     """Rows x [rows, in] (bfloat16 or float16) as codes [rows, in] (float8_e4m3fn or its bytes, uint8) with a power-of-two
     scale [rows] (float32) each, what :func:`fs_linear` and :func:`fs_gated_ff` take. Returns (codes, scale)."""
-    index, kind = x.get_device(), _mm_type(x, "x")
+    index, dtype = x.get_device(), x.dtype
+    kind = _mm_type(dtype, "x")
     if index < 0 or index != _current_device():
         raise ValueError(f"x is on {x.device}, cuda:{_current_device()} is current")
     rows, inner = size = x.shape
     if codes.element_size() != 1:
         raise ValueError(f"codes are {codes.dtype}, not float8_e4m3fn or uint8")
-    xr = _mm_rows(x, "x", x.dtype, index, size)
+    xr = _mm_rows(x, "x", dtype, index, size)
     c_at, c_stride, s_at = _mm_rows(codes, "codes", codes.dtype, index, size, scale)
     rc = lib().fs_quantise_rows(rows, inner, kind, _MM_ROWS.pack(*xr), _MM_ROWS.pack(c_at, c_stride, 0), s_at, _kv_stream(stream, index))
     if rc:
@@ -898,7 +900,9 @@ def fs_quantise_rows(x, codes, scale, *, stream=None):
 
 def fs_mm_check(workspace: MmWorkspace, stream=None) -> None:
     """Waits for the stream and raises what the workspace's calls met on the device."""
-    index = _mm_here(workspace)
+    index = workspace.index
+    if index != _current_device():
+        raise ValueError(f"cuda:{_current_device()} is current, the workspace is on cuda:{index}")
     _check(lib().fs_mm_check(workspace.address, _kv_stream(stream, index)))
 
 
