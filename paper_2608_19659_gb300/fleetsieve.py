@@ -791,12 +791,15 @@ def _mm_rows(t, name: str, dtype, index: int, size: tuple[int, int], scale=None)
     s0, s1 = t.stride()
     if t.dtype is not dtype or t.get_device() != index or (s1 != 1 and size[1] > 1 and size[0]):
         raise ValueError(f"{name}: want {dtype} on cuda:{index}, the last dimension contiguous")
-    if scale is None:
-        return t.data_ptr(), s0, 0
-    if (scale.shape != size[:1] or scale.element_size() != 4 or not scale.is_floating_point()
-            or not scale.is_contiguous() or scale.get_device() != index):
-        raise ValueError(f"{name}: scales are a contiguous float32 [{size[0]}] on cuda:{index}")
-    return t.data_ptr(), s0, scale.data_ptr()
+    return t.data_ptr(), s0, 0 if scale is None else _mm_scale(scale, name, index, size[0])
+
+
+def _mm_scale(scale, name: str, index: int, rows: int) -> int:
+    """The address of the scales of that many rows."""
+    if (scale.shape != (rows,) or scale.element_size() != 4 or not scale.is_floating_point() or not scale.is_contiguous()
+            or scale.get_device() != index):
+        raise ValueError(f"{name}: scales are a contiguous float32 [{rows}] on cuda:{index}")
+    return scale.data_ptr()
 
 
 def _mm_head(workspace: MmWorkspace, x, y, activation: str) -> tuple[int, int, int, int]:
@@ -824,12 +827,23 @@ def fs_linear(x, w, y, *, bias=None, residual=None, activation: str = "none", x_
     """y [rows, out] = act(x [rows, in] w [out, in]^T + bias) + residual, enqueued on ``stream`` (default: torch's
     current one). x and w: both bfloat16, both float16, or both float8_e4m3fn with x_scale [rows] and w_scale [out]; bias,
     residual and y: bfloat16 or float16 (x's type if that is 16-bit). y may be the residual. Returns y."""
-    index, kind, out_kind, act = _mm_head(workspace, x, y, activation)
-    (rows, inner), out, dtype, of_x = x.shape, w.shape[0], y.dtype, x.dtype
+    index, of_x, dtype = workspace.index, x.dtype, y.dtype
+    kind, out_kind, act = _mm_kinds.get(of_x), _mm_kinds.get(dtype), ACTIVATIONS.get(activation)
+    (rows, inner), out = x.shape, w.shape[0]
     size = (rows, out)
-    xr = _mm_rows(x, "x", of_x, index, (rows, inner), x_scale)
-    wr = _mm_rows(w, "w", of_x, index, (out, inner), w_scale)
-    yr = _mm_rows(y, "y", dtype, index, size)
+    (x0, x1), (w0, w1), (y0, y1) = x.stride(), w.stride(), y.stride()
+    # (what is not as usual goes through the checks one by one, which say what is wrong)
+    if (x1 == w1 == y1 == 1 and w.shape == (out, inner) and y.shape == size and w.dtype is of_x and kind is not None
+            and out_kind is not None and act is not None
+            and x.get_device() == w.get_device() == y.get_device() == index == _current_device()):
+        xr = x.data_ptr(), x0, 0 if x_scale is None else _mm_scale(x_scale, "x", index, rows)
+        wr = w.data_ptr(), w0, 0 if w_scale is None else _mm_scale(w_scale, "w", index, out)
+        yr = y.data_ptr(), y0, 0
+    else:
+        index, kind, out_kind, act = _mm_head(workspace, x, y, activation)
+        xr = _mm_rows(x, "x", of_x, index, (rows, inner), x_scale)
+        wr = _mm_rows(w, "w", of_x, index, (out, inner), w_scale)
+        yr = _mm_rows(y, "y", dtype, index, size)
     rr = _NO_ROWS if residual is None else _mm_rows(residual, "residual", dtype, index, size)
     b = 0
     if bias is not None:
@@ -837,7 +851,7 @@ def fs_linear(x, w, y, *, bias=None, residual=None, activation: str = "none", x_
             raise ValueError(f"bias is a contiguous {dtype} [{out}] on cuda:{index}")
         b = bias.data_ptr()
     a = _MM_LINEAR.pack(rows, inner, out, kind, out_kind, act, *xr, *wr, *rr, *yr, b)
-    rc = lib().fs_linear(a, workspace.address, workspace.bytes, _kv_stream(stream, index))
+    rc = lib().fs_linear(a, workspace.address, workspace.bytes, _current_stream(index) if stream is None else _kv_stream(stream, index))
     if rc:
         _check(rc)
     return y
@@ -846,15 +860,26 @@ def fs_linear(x, w, y, *, bias=None, residual=None, activation: str = "none", x_
 def fs_gated_ff(x, w_gate, w_up, y, *, activation: str = "silu", x_scale=None, gate_scale=None, up_scale=None,
                 workspace: MmWorkspace, stream=None):
     """y [rows, out] = act(x w_gate^T) * (x w_up^T), types as in :func:`fs_linear`. Returns y."""
-    index, kind, out_kind, act = _mm_head(workspace, x, y, activation)
-    (rows, inner), out, of_x = x.shape, w_gate.shape[0], x.dtype
+    index, of_x, dtype = workspace.index, x.dtype, y.dtype
+    kind, out_kind, act = _mm_kinds.get(of_x), _mm_kinds.get(dtype), ACTIVATIONS.get(activation)
+    (rows, inner), out = x.shape, w_gate.shape[0]
     size = (out, inner)
-    xr = _mm_rows(x, "x", of_x, index, (rows, inner), x_scale)
-    gr = _mm_rows(w_gate, "w_gate", of_x, index, size, gate_scale)
-    ur = _mm_rows(w_up, "w_up", of_x, index, size, up_scale)
-    yr = _mm_rows(y, "y", y.dtype, index, (rows, out))
+    (x0, x1), (g0, g1), (u0, u1), (y0, y1) = x.stride(), w_gate.stride(), w_up.stride(), y.stride()
+    if (x1 == g1 == u1 == y1 == 1 and w_gate.shape == size and w_up.shape == size and y.shape == (rows, out) and w_gate.dtype is of_x
+            and w_up.dtype is of_x and kind is not None and out_kind is not None and act is not None
+            and x.get_device() == w_gate.get_device() == w_up.get_device() == y.get_device() == index == _current_device()):
+        xr = x.data_ptr(), x0, 0 if x_scale is None else _mm_scale(x_scale, "x", index, rows)
+        gr = w_gate.data_ptr(), g0, 0 if gate_scale is None else _mm_scale(gate_scale, "w_gate", index, out)
+        ur = w_up.data_ptr(), u0, 0 if up_scale is None else _mm_scale(up_scale, "w_up", index, out)
+        yr = y.data_ptr(), y0, 0
+    else:
+        index, kind, out_kind, act = _mm_head(workspace, x, y, activation)
+        xr = _mm_rows(x, "x", of_x, index, (rows, inner), x_scale)
+        gr = _mm_rows(w_gate, "w_gate", of_x, index, size, gate_scale)
+        ur = _mm_rows(w_up, "w_up", of_x, index, size, up_scale)
+        yr = _mm_rows(y, "y", dtype, index, (rows, out))
     a = _MM_GATED.pack(rows, inner, out, kind, out_kind, act, *xr, *gr, *ur, *yr)
-    rc = lib().fs_gated_ff(a, workspace.address, workspace.bytes, _kv_stream(stream, index))
+    rc = lib().fs_gated_ff(a, workspace.address, workspace.bytes, _current_stream(index) if stream is None else _kv_stream(stream, index))
     if rc:
         _check(rc)
     return y
@@ -883,16 +908,22 @@ _MM_ROWS = struct.Struct("=Qqq")
 def fs_quantise_rows(x, codes, scale, *, stream=None):
     """Rows x [rows, in] (bfloat16 or float16) as codes [rows, in] (float8_e4m3fn or its bytes, uint8) with a power-of-two
     scale [rows] (float32) each, what :func:`fs_linear` and :func:`fs_gated_ff` take. Returns (codes, scale)."""
-    index, dtype = x.get_device(), x.dtype
-    kind = _mm_type(dtype, "x")
+    index, dtype, size = x.get_device(), x.dtype, x.shape
     if index < 0 or index != _current_device():
         raise ValueError(f"x is on {x.device}, cuda:{_current_device()} is current")
-    rows, inner = size = x.shape
+    kind = _mm_type(dtype, "x")
+    rows, inner = size
+    (x0, x1), (c0, c1) = x.stride(), codes.stride()
     if codes.element_size() != 1:
         raise ValueError(f"codes are {codes.dtype}, not float8_e4m3fn or uint8")
-    xr = _mm_rows(x, "x", dtype, index, size)
-    c_at, c_stride, s_at = _mm_rows(codes, "codes", codes.dtype, index, size, scale)
-    rc = lib().fs_quantise_rows(rows, inner, kind, _MM_ROWS.pack(*xr), _MM_ROWS.pack(c_at, c_stride, 0), s_at, _kv_stream(stream, index))
+    if x1 == c1 == 1 and codes.shape == size and codes.get_device() == index:
+        xr, c_at, c_stride = (x.data_ptr(), x0, 0), codes.data_ptr(), c0
+    else:
+        xr = _mm_rows(x, "x", dtype, index, size)
+        c_at, c_stride, _ = _mm_rows(codes, "codes", codes.dtype, index, size)
+    s_at = _mm_scale(scale, "codes", index, rows)
+    rc = lib().fs_quantise_rows(rows, inner, kind, _MM_ROWS.pack(*xr), _MM_ROWS.pack(c_at, c_stride, 0), s_at,
+                                _current_stream(index) if stream is None else _kv_stream(stream, index))
     if rc:
         _check(rc)
     return codes, scale
