@@ -426,7 +426,7 @@ extern "C" int fs_gated_ff_backward(const fs_mm_gated_grad* args, void* workspac
   a.product[2] = {to(g.dw_up, g.out), {DU_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, tile, 0};
   a.products = 3;
   a.status = c.status;
-  const cudaError_t e = launch_mm_wide(a, MM_LINEAR, g.type, g.type, c.sms, c.stream);
+  const cudaError_t e = launch_mm_wide(a, MM_GRAD, g.type, g.type, c.sms, c.stream);
   return e == cudaSuccess ? FS_OK : cuda_say(e, c.what);
 }
 

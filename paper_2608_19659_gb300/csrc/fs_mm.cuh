@@ -143,11 +143,12 @@ MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms);
 cudaError_t launch_mm_few(const CUtensorMap& x, const CUtensorMap& w, const CUtensorMap* up, const MmEpilogue& e, const MmFewPlan& p,
                           int blocks_k, int type, int out_type, uint32_t* status, cudaStream_t s);
 
-enum { MM_LINEAR, MM_GATED, MM_BACK };
+enum { MM_LINEAR, MM_GATED, MM_BACK, MM_GRAD };
 
-// One product of a launch of k_mm_wide: e.rows x e.cols results, sums over blocks[0] blocks of maps a[0] and b[0], then over blocks[1]
-// of a[1] and b[1] (MM_GATED, MM_BACK: a[0] with b[0] for gate and b[1] for up). Maps have boxes of 128 rows (B: half a
-// tile's columns) and one block, or, of an operand whose rows are contiguous (a_mn, b_mn), of 64 of them and 64 terms of the sum.
+// One product of a launch of k_mm_wide: e.rows x e.cols results, sums over blocks[0] blocks of maps a[0] and b[0] (MM_GATED, MM_BACK: b[0]
+// for gate and b[1] for up). Maps have boxes of 128 rows (B: half a tile's columns) and one block. MM_GRAD: up to three products,
+// whose sums go on over blocks[1] blocks of a[1] and b[1], and whose operands may lie the other way (a_mn, b_mn: the rows are
+// contiguous, boxes are of 64 of them and 64 terms of the sum); results are stored as they are.
 struct MmProduct {
   MmEpilogue e;
   int a[2], b[2], blocks[2];
@@ -159,6 +160,7 @@ struct MmWideArgs {
   CUtensorMap maps[8];
   MmProduct product[3];
   int products, eight, format;
+  int stages, stage, sub;  // (launch_mm_wide's: stages of the ring, their bytes, and blocks of the sum)
   long long tiles;
   uint32_t* status;
 };
