@@ -418,12 +418,9 @@ extern "C" int fs_gated_ff_backward(const fs_mm_gated_grad* args, void* workspac
   if (int rc = rows_map(&a.maps[X_T], g.x.data, g.rows, g.in, g.x.stride, g.type, 64)) return rc;
   auto to = [&](const fs_mm_rows& r, int n) { return MmEpilogue{n, g.in, FS_ACT_NONE, nullptr, {}, nullptr, nullptr, 0, {r.data, nullptr}, r.stride}; };
   const int out_blocks = (g.out + 63) / 64, row_blocks = (g.rows + 63) / 64;
-  // half the width where all of its tiles find a pair of SMs at once
-  const long long high = (g.rows + 255) / 256 + 2ll * ((g.out + 255) / 256);
-  const int tile = high * ((g.in + 127) / 128) <= c.sms / 2 ? 128 : 256;
-  a.product[0] = {to(g.dx, g.rows), {DG, DU}, {WG_T, WU_T}, {out_blocks, out_blocks}, false, true, tile, 0};
-  a.product[1] = {to(g.dw_gate, g.out), {DG_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, tile, 0};
-  a.product[2] = {to(g.dw_up, g.out), {DU_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, tile, 0};
+  a.product[0] = {to(g.dx, g.rows), {DG, DU}, {WG_T, WU_T}, {out_blocks, out_blocks}, false, true, 0, 0};
+  a.product[1] = {to(g.dw_gate, g.out), {DG_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, 0, 0};
+  a.product[2] = {to(g.dw_up, g.out), {DU_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, 0, 0};
   a.products = 3;
   a.status = c.status;
   const cudaError_t e = launch_mm_wide(a, MM_GRAD, g.type, g.type, c.sms, c.stream);

@@ -153,13 +153,14 @@ struct MmProduct {
   MmEpilogue e;
   int a[2], b[2], blocks[2];
   bool a_mn, b_mn;
-  int tile;         // columns of a tile (gated: of gate and of up together): a multiple of 64 up to 256
+  int tile;         // (MM_GRAD: launch_mm_wide's) columns of a tile (gated: of gate and of up together): a multiple of 64 up to 256
   long long tiles;  // (launch_mm_wide's)
 };
 struct MmWideArgs {
   CUtensorMap maps[8];
   MmProduct product[3];
   int products, eight, format;
+  int lead, rounds;        // (launch_mm_wide's: pairs that start with one of the longest tiles, and how many others that takes as long as)
   int stages, stage, sub;  // (launch_mm_wide's: stages of the ring, their bytes, and blocks of the sum)
   long long tiles;
   uint32_t* status;

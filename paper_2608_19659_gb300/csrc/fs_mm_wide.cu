@@ -13,6 +13,7 @@
 // are bound by their end (4096 rows of 1024 8-bit terms over 8192 columns 55 us, 76 with a residual; the products alone 16).
 #include <algorithm>
 #include <atomic>
+#include <utility>
 
 #include "fs_mm.cuh"
 
@@ -132,7 +133,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
   WideBars& bars = *reinterpret_cast<WideBars*>(raw + (smem - smem_u32(raw)) + kRing);
   const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
+  // This pair's tiles: every `step`-th. Of gradients whose longest tiles are fewer than there are pairs, those pairs start with one of them, as
+  // long as `rounds` of the others, which the other pairs take meanwhile: then `next` is the k-th tile.
   const long long first = blockIdx.x >> 1, step = gridDim.x >> 1;
+  auto next = [&](long long i, int k) -> long long {
+    if (kMode != MM_GRAD || !a.lead) return i + step;
+    const int mine = first < a.lead ? 1 : a.rounds;
+    const long long others = step - a.lead;
+    if (k < mine) return a.lead + k * others + (first - a.lead);
+    return a.lead + a.rounds * others + (k - mine) * step + first;
+  };
 
   pdl_trigger();
   if (threadIdx.x == 0) {
@@ -188,7 +198,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
         if (++st == stages) st = 0, par ^= 1, at = ring;
       }
     };
-    for (long long i = first; ok && i < a.tiles; i += step) {
+    int n = 0;
+    for (long long i = first; ok && i < a.tiles; i = next(i, ++n)) {
       const Tile t = tile_of<kMode>(a, i);
       const MmProduct& p = *t.p;
       const int row = !of_b ? t.m0 + rank * 128 : one_sum(kMode) ? t.n0 + rank * (p.tile / 2) : t.n0;
@@ -224,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
       const uint32_t stage = a.stage >> 4;
       int st = 0, n = 0;
       uint32_t par = 0, at = 0;
-      for (long long i = first; i < a.tiles; i += step, ++n) {
+      for (long long i = first; i < a.tiles; i = next(i, ++n)) {
         const MmProduct& p = *tile_of<kMode>(a, i).p;
         const bool a_mn = kMode == MM_GRAD && p.a_mn, b_mn = kMode == MM_GRAD && p.b_mn;
         const uint32_t d = (n & 1) * kTile, idesc = mm_instr(kTile, p.tile, a.format, a_mn, b_mn);
@@ -270,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
     // the 16-byte piece `piece` of row `r` there
     auto at_piece = [](int r, int piece) { return 4 * r + (piece ^ (r >> 1 & 3)); };
     int n = 0;
-    for (long long i = first; i < a.tiles; i += step, ++n) {
+    for (long long i = first; i < a.tiles; i = next(i, ++n)) {
       const Tile t = tile_of<kMode>(a, i);
       const MmEpilogue& e = t.p->e;
       const long long m0 = t.m0 + rank * 128 + (w & 3) * 32, m = m0 + lane;
@@ -407,10 +418,13 @@ cudaError_t launch_mode(const MmWideArgs& a, int mode, int sms, cudaStream_t s) 
 
 }  // namespace
 
-// The width of a tile by an estimate of the time (in ns): a block of a sum takes as long as its products, 1.09 ns a column, and 172 ns
-// at least (one warp's wait, products and commit; 8192 terms over one tile: 256 wide 40.9 us, 192 31.8, 128 27.7, 64 26.9), and
-// the longer the work the more what narrow tiles read again costs (8192 rows over 10240: 256 699 us, 192 816; 512 rows 256 79, 192 64,
-// 160 59). W is read at 6.6 TB/s, and a quarter of the lesser of both comes on top (32 rows over 10240 of 8192, 160: 35.3).
+// What a block of 128 bytes of a sum takes over a tile of that width, in ns: the products of a wide one, one thread's wait, products
+// and commit of a narrow one (8192 terms over one tile: 256 wide 42 us, 192 33.7, 160 29.3, 128 26.6, 96 25.7, 64 24.4).
+float mm_wide_block(int tile) { return tile <= 128 ? 140.f + 0.22f * tile : 8.f + 1.13f * tile; }
+
+// The width of a tile by an estimate of the time (in ns): of its sums, or of its end, 17 ns a column, where that is longer
+// (2048 rows of 512 over 512: 256 wide 9.6 us, 64 wide 5.3); and the longer the work the more what narrow tiles read again costs (8192 rows over
+// 10240: 256 699 us, 192 816). W is read at 6.6 TB/s, and a quarter of the lesser of both comes on top (32 rows over 10240 of 8192, 160: 35.3).
 int mm_wide_tile(int rows, int cols, int blocks, bool gated, int sms, float* ns) {
   int best = 0;
   for (int tile = kTile; tile >= 64; tile -= gated ? 64 : 32) {
@@ -418,17 +432,42 @@ int mm_wide_tile(int rows, int cols, int blocks, bool gated, int sms, float* ns)
     const long long tiles = (long long)((rows + kTile - 1) / kTile) * ((cols + width - 1) / width);
     const float waves = (float)((tiles + sms / 2 - 1) / std::max(1, sms / 2));
     const float again = 1.f + 0.08f * (256.f / tile - 1.f) * std::min(waves, 4.f);
-    const float sums = waves * blocks * std::max(1.09f * tile, 172.f) * again, memory = (float)blocks * kMmBlock * cols * (gated ? 2 : 1) / 6600.f;
-    const float t = std::max(sums, memory) + 0.25f * std::min(sums, memory) + 4000.f + 8.f * tile;
+    const float one = blocks * mm_wide_block(tile), end = 17.f * tile;
+    const float sums = ((waves - 1.f) * std::max(one, end) + one) * again, memory = (float)blocks * kMmBlock * cols * (gated ? 2 : 1) / 6600.f;
+    const float t = std::max(sums, memory) + 0.25f * std::min(sums, memory) + 2900.f + end;
     if (!best || t < *ns) best = tile, *ns = t;
   }
   return best;
+}
+
+// The order of gradients, the product with the longest tiles first, and the width of all their tiles: few long ones set the pace
+// (1362 rows, 704 and 3848, dx's 18 tiles of 121 blocks: 256 wide 69 us, 128 wide 52). Pairs that have one of those get others
+// only when it is done.
+void grad_plan(MmWideArgs& a, int sms) {
+  const int pairs = std::max(1, sms / 2);
+  auto blocks = [](const MmProduct& p) { return p.blocks[0] + p.blocks[1]; };
+  if (blocks(a.product[0]) < blocks(a.product[1])) std::swap(a.product[0], a.product[2]);  // dx comes in first, dW of gate and up behind it
+  const int longest = a.product[0].blocks[1] ? 1 : 2;
+  float least = 0.f;
+  for (int tile = kTile; tile >= 128; tile -= 128) {
+    auto tiles = [&](int i) { return (long long)((a.product[i].e.rows + kTile - 1) / kTile) * ((a.product[i].e.cols + tile - 1) / tile); };
+    auto ns = [&](int i) { return std::max(blocks(a.product[i]) * mm_wide_block(tile), 17.f * tile); };
+    const long long lead = longest == 1 ? tiles(0) : 2 * tiles(0), rest = longest == 1 ? 2 * tiles(2) : tiles(2);
+    const float all = (lead * ns(0) + rest * ns(2)) / pairs * (tile == kTile ? 1.f : 1.08f), t = std::max(ns(0), all) + ns(2) + 17.f * tile;
+    if (tile < kTile && t >= least) break;
+    least = t;
+    for (int i = 0; i < a.products; ++i) a.product[i].tile = tile;
+    a.lead = lead < pairs && lead + rest > pairs ? (int)lead : 0;
+    a.rounds = std::max(1, (int)(ns(0) / ns(2) + 0.5f));
+  }
 }
 
 cudaError_t launch_mm_wide(MmWideArgs& a, int mode, int type, int out_type, int sms, cudaStream_t s) {
   a.eight = type == FS_E4M3;
   a.format = type == FS_KV_BF16 ? 1 : 0;
   a.tiles = 0;
+  a.lead = 0;
+  if (mode == MM_GRAD) grad_plan(a, sms);
   int widest = 0;
   for (int i = 0; i < a.products; ++i) widest = std::max(widest, a.product[i].tile);
   // narrow tiles take two blocks a stage: their products are done before one thread's wait, products and commit for a single block are
