@@ -889,13 +889,21 @@ def fs_gated_ff_backward(x, w_gate, w_up, dy, dx, dw_gate, dw_up, *, activation:
                          workspace: MmWorkspace, stream=None):
     """The gradients of :func:`fs_gated_ff` (bfloat16 or float16 throughout), given dy, into dx, dw_gate and dw_up, which
     it returns. ``workspace`` is one made with backward=True."""
-    index, kind, _, act = _mm_head(workspace, x, x, activation)
-    (rows, inner), out, dtype = x.shape, w_gate.shape[0], x.dtype
+    index, dtype = workspace.index, x.dtype
+    kind, act = _mm_kinds.get(dtype), ACTIVATIONS.get(activation)
+    (rows, inner), out = x.shape, w_gate.shape[0]
     of_x, of_w = (rows, inner), (out, inner)
-    parts = [_mm_rows(t, name, dtype, index, size) for t, name, size in (
-        (x, "x", of_x), (w_gate, "w_gate", of_w), (w_up, "w_up", of_w), (dy, "dy", (rows, out)),
-        (dx, "dx", of_x), (dw_gate, "dw_gate", of_w), (dw_up, "dw_up", of_w))]
-    a = _MM_GRAD.pack(rows, inner, out, kind, act, 0, *(v for p in parts for v in p))
+    parts, usual = [], kind is not None and act is not None and index == _current_device()
+    for t, size in ((x, of_x), (w_gate, of_w), (w_up, of_w), (dy, (rows, out)), (dx, of_x), (dw_gate, of_w), (dw_up, of_w)):
+        s0, s1 = t.stride()
+        usual = usual and s1 == 1 and t.shape == size and t.dtype is dtype and t.get_device() == index
+        parts += (t.data_ptr(), s0, 0)
+    if not usual:
+        index, kind, _, act = _mm_head(workspace, x, x, activation)
+        parts = [v for t, name, size in (
+            (x, "x", of_x), (w_gate, "w_gate", of_w), (w_up, "w_up", of_w), (dy, "dy", (rows, out)),
+            (dx, "dx", of_x), (dw_gate, "dw_gate", of_w), (dw_up, "dw_up", of_w)) for v in _mm_rows(t, name, dtype, index, size)]
+    a = _MM_GRAD.pack(rows, inner, out, kind, act, 0, *parts)
     rc = lib().fs_gated_ff_backward(a, workspace.address, workspace.bytes, _kv_stream(stream, index))
     if rc:
         _check(rc)
