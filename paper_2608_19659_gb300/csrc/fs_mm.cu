@@ -79,6 +79,11 @@ bool overlap(const Span& a, const Span& b) {
 int check_apart(const Span& out, const char* out_name, const Span& in, const char* in_name) {
   return overlap(out, in) ? say(FS_EINVAL, "%s and %s overlap", out_name, in_name) : FS_OK;
 }
+int check_apart(const Span& out, const char* out_name, const float* scales, int n, const char* in_name) {
+  if (!scales) return FS_OK;
+  const fs_mm_rows r{const_cast<float*>(scales), 0, nullptr};
+  return overlap(out, {&r, 1, n, 4}) ? say(FS_EINVAL, "%s and the scales of %s overlap", out_name, in_name) : FS_OK;
+}
 
 constexpr int64_t kMmPartAt = 256;  // the status word, then dg and du of a backward pass
 
@@ -339,6 +344,8 @@ extern "C" int fs_linear(const fs_mm_linear* args, void* workspace, int64_t work
   const fs_mm_rows bias{const_cast<void*>(g.bias), 0, nullptr};
   if (int rc = check_apart(y, "y", {&g.x, g.rows, g.in, size}, "x")) return rc;
   if (int rc = check_apart(y, "y", {&g.w, g.out, g.in, size}, "w")) return rc;
+  if (int rc = check_apart(y, "y", g.x.scale, g.rows, "x")) return rc;
+  if (int rc = check_apart(y, "y", g.w.scale, g.out, "w")) return rc;
   if (int rc = check_apart(y, "y", {&bias, 1, g.out, 2}, "bias")) return rc;
   if (g.residual.data != g.y.data || g.residual.stride != g.y.stride)
     if (int rc = check_apart(y, "y", r, "residual")) return rc;
@@ -364,6 +371,9 @@ extern "C" int fs_gated_ff(const fs_mm_gated* args, void* workspace, int64_t wor
   if (int rc = check_apart(y, "y", {&g.x, g.rows, g.in, size}, "x")) return rc;
   if (int rc = check_apart(y, "y", {&g.w_gate, g.out, g.in, size}, "w_gate")) return rc;
   if (int rc = check_apart(y, "y", {&g.w_up, g.out, g.in, size}, "w_up")) return rc;
+  if (int rc = check_apart(y, "y", g.x.scale, g.rows, "x")) return rc;
+  if (int rc = check_apart(y, "y", g.w_gate.scale, g.out, "w_gate")) return rc;
+  if (int rc = check_apart(y, "y", g.w_up.scale, g.out, "w_up")) return rc;
   MmCall c{g.in, g.type, g.out_type, 0, static_cast<uint32_t*>(workspace), static_cast<cudaStream_t>(cuda_stream), "launch (fs_gated_ff)"};
   if (int rc = device_sms(&c.sms)) return rc;
   return product(c, g.x, g.w_gate, &g.w_up,
@@ -439,6 +449,8 @@ extern "C" int fs_quantise_rows(int32_t rows, int32_t in, int32_t type, const fs
   if (int rc = check_rows(xr, "x", rows, in, type)) return rc;
   if (int rc = check_rows(cr, "codes", rows, in, FS_E4M3)) return rc;
   if (int rc = check_apart({&cr, rows, in, 1}, "codes", {&xr, rows, in, 2}, "x")) return rc;
+  if (int rc = check_apart({&cr, rows, in, 1}, "codes", scale, rows, "codes")) return rc;
+  if (int rc = check_apart({&xr, rows, in, 2}, "x", scale, rows, "codes")) return rc;
   const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = type == FS_KV_FP16 ? launch_quantise<__half>(rows, in, xr, cr, scale, s) : launch_quantise<__nv_bfloat16>(rows, in, xr, cr, scale, s);
   return e == cudaSuccess ? FS_OK : cuda_say(e, "launch (fs_quantise_rows)");

@@ -185,12 +185,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
     const uint32_t to = sums + rank * share * ld + (group + lane) * 4, from = tmem + ((uint32_t)group << 16);
     if (valid < 8) {  // all of them the first block's
       if (w < 4) {
-      uint32_t x[8];
-      tmem_ld8(x, from);
-      wait_ld();
+        uint32_t x[8];
+        tmem_ld8(x, from);
+        wait_ld();
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < valid) st_cluster(cluster_addr(to + i * ld, 0), x[i]);
+        for (int i = 0; i < 8; ++i)
+          if (i < valid) st_cluster(cluster_addr(to + i * ld, 0), x[i]);
       }
     } else {
       for (int o = 0; o * share < valid; ++o) {
@@ -272,11 +272,11 @@ int bars_at(const MmFewPlan& p, int rows) { return std::max(ring_bytes(p), sums_
 
 // The tile and the cluster by an estimate of the time. What it goes by, and what the other choice cost where it decides (us, in
 // graphs): memory at 6.6 TB/s; a block takes 100 bytes a ns, half of that beside another on its SM, and 165 ns a step at
-// least, 60 more for three copies, and more with fewer rows of W (one row of 1024 8-bit over 8192, tiles of 32 6.0, of 64 5.6, of 128 5.5; 64 rows of 8192 8-bit over
-// 10240, 240 blocks 18.7, 160 21.0, 80 20.8; one row of 8192 over 2 x 1792 gated, tiles of 128 in clusters of 6 12.1, of 32
-// without 24.5); a quarter of the lesser of both, as they do not overlap in whole; a cluster's exchange 0.55 us and 50 bytes a ns
-// (333 rows of 1001 over 777, tiles of 64 in clusters of three 5.8, of six 7.3); blocks beyond what is resident wait for a place (100 rows of
-// 4096 over 2560, 120 blocks 9.8, 160 15.9).
+// least, more with fewer rows of W, 60 more for a gated one's three copies (one row of 1024 8-bit over 8192, tiles of 32 6.0, of
+// 64 5.6, of 128 5.5; 64 rows of 8192 8-bit over 10240, 240 blocks 18.7, 160 21.0, 80 20.8; one row of 8192 over 2 x 1792 gated, tiles of
+// 128 in clusters of 8 11.9, of 6 12.1, of 32 without 24.5); a quarter of the lesser of both, as they do not overlap in whole; a
+// cluster's exchange 0.55 us and 50 bytes a ns (333 rows of 1001 over 777, tiles of 64 in clusters of three 5.8, of six 7.3); blocks
+// beyond what is resident wait for a place (100 rows of 4096 over 2560, 120 blocks 9.8, 160 15.9).
 MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
   MmFewPlan best{};
   for (int w_rows = 128; w_rows >= 32; w_rows /= 2)
@@ -301,7 +301,8 @@ MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
       p.stages = std::clamp(two || less ? half : (216 * 1024 - sums) / slot, 2, std::min(kMaxStages, std::max(2, depth)));
       const long long places = !two ? one : cluster == 1 ? 2 * sms : 34 / cluster * cluster * groups;
       const float waves = (float)((blocks + places - 1) / places), rate = two ? 50.f : 100.f;
-      const float memory = (float)blocks_k * kMmBlock * cols * (gated ? 2 : 1) / 6600.f, steps = waves * depth * std::max(slot / rate, (w_rows == 32 ? 230.f : w_rows == 64 ? 185.f : 165.f) + (gated ? 60.f : 0.f));
+      const float step = std::max(slot / rate, (w_rows == 32 ? 230.f : w_rows == 64 ? 185.f : 165.f) + (gated ? 60.f : 0.f));
+      const float memory = (float)blocks_k * kMmBlock * cols * (gated ? 2 : 1) / 6600.f, steps = waves * depth * step;
       const float read = std::max(memory, steps) + 0.25f * std::min(memory, steps);
       // what comes after the sums, a third longer beside another block: a cluster's exchange; 4 ns a token, 8 more for those that
       // go to other blocks, 15 for those that it finishes (of 128 rows of W). 150 ns for each further tile of tokens

@@ -278,6 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
     const uint32_t lanes = (uint32_t)(w & 3) << 21;
     const int id = threadIdx.x - 128, half = id >> 7;
     uint4* pass = bars.pass[w - 4];
+    bool ok = true;  // (a warp whose wait ran out keeps coming to the barriers of the eight)
     // the 16-byte piece `piece` of row `r` there
     auto at_piece = [](int r, int piece) { return 4 * r + (piece ^ (r >> 1 & 3)); };
     int n = 0;
@@ -308,9 +309,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
           next[g] = m0 + r < e.rows && col < e.cols && kCols * c < width ? load8(e.in, (m0 + r) * e.in_stride + col, e.cols - col) : make_uint4(0, 0, 0, 0);
         }
       };
+      if (!ok) continue;
       if (adds) ask(half);
-      const bool ok = mm_wait(&bars.sum_full[n & 1], n >> 1 & 1, a.status);
-      if (!__all_sync(~0u, ok)) break;
+      ok = __all_sync(~0u, mm_wait(&bars.sum_full[n & 1], n >> 1 & 1, a.status));
+      if (!ok) continue;
       fence_after();
       const uint32_t at = tmem + lanes + (n & 1) * kTile;
       mm_with_act(kMode == MM_GRAD ? FS_ACT_NONE : e.act, [&](auto act) {

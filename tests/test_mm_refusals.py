@@ -256,3 +256,17 @@ def test_scales_activations_and_rows_to_quantise(binding):
                     (Rows((3, 20), torch.float32), c, f), (Rows((3, 20), index=1), c, f), (t.x, Rows((3, 20), torch.uint8, 1), f)):
         with pytest.raises(ValueError):
             fsb.fs_quantise_rows(x, y, s)
+
+
+def test_scales_that_overlap(fsb):
+    for name, scaled in (("fs_linear", ("x", "w")), ("fs_gated_ff", ("x", "w_gate", "w_up"))):
+        for rows in scaled:
+            for off in (0, 16, 2 * 64 + 16, -16 if rows != "x" else 0):  # (10 rows' scales, or 3: 40 and 12 bytes)
+                a = good(fsb, 2)[name]
+                getattr(a, rows).scale = a.y.data + off
+                refused(fsb, call(fsb, name, a))
+                assert b"overlap" in fsb.lib().fs_last_error()
+    x, c = fsb.fs_mm_rows(P16, 32, None), fsb.fs_mm_rows(4 * P16, 32, None)
+    for scale in (P16, P16 + 32, 4 * P16, 4 * P16 + 64):
+        refused(fsb, fsb.lib().fs_quantise_rows(3, 20, 0, C.byref(x), C.byref(c), scale, None))
+        assert b"overlap" in fsb.lib().fs_last_error()
