@@ -153,7 +153,7 @@ struct MmProduct {
   MmEpilogue e;
   int a[2], b[2], blocks[2];
   bool a_mn, b_mn;
-  int tile;         // (MM_GRAD: launch_mm_wide's) columns of a tile (gated: of gate and of up together): a multiple of 64 up to 256
+  int tile;         // (MM_GRAD: launch_mm_wide's) columns of a tile (gated: of gate and of up together): a multiple of 32 (gated: 64) up to 256
   long long tiles;  // (launch_mm_wide's)
 };
 struct MmWideArgs {

@@ -8,9 +8,10 @@
 // A launch holds up to three products (the backward pass: dx and both dW), whose sums may have two parts (dx: over gate
 // and up) and whose operands may lie either way (dx reads W, dW reads both, across their rows).
 // Of a gated block the first SM of a pair loads gate's rows and the second up's, so that a thread has both sums of a result.
-// Bound by the tensor cores, and they by power: 8192 rows of 8192 bf16 over 10240 692 us in a burst (1.99 PFLOP/s), 780 in a row; 4096
-// rows of 7168 8-bit over 8192 133 us (3.6); the tensor pipe is active 87 to 90 % of the time with full waves. Tiles of short sums
-// are bound by their end (4096 rows of 1024 8-bit terms over 8192 columns 55 us, 76 with a residual; the products alone 16).
+// Bound by the tensor cores, and they by power: 8192 rows of 8192 bf16 over 10240 677 to 690 us in a burst (2.0 PFLOP/s), 750 to 790 in a
+// row; 4096 rows of 7168 8-bit over 8192 131 us (3.7); the tensor pipe is active 87 to 90 % of the time with full waves. Tiles of short
+// sums are bound by their end (4096 rows of 1024 8-bit terms over 8192 columns 55 us, with a residual 67 and from memory 81; the products
+// alone 16).
 #include <algorithm>
 #include <atomic>
 #include <utility>
