@@ -816,10 +816,9 @@ def _mm_head(workspace: MmWorkspace, x, y, activation: str) -> tuple[int, int, i
     return index, kind, out_kind, act
 
 
-_NO_ROWS = (0, 0, 0)
-_MM_LINEAR = struct.Struct("=6i" + 4 * "Qqq" + "Q")
-_MM_GATED = struct.Struct("=6i" + 4 * "Qqq")
-_MM_GRAD = struct.Struct("=6i" + 7 * "Qqq")
+_mm_pack_linear = struct.Struct("=6i" + 4 * "Qqq" + "Q").pack
+_mm_pack_gated = struct.Struct("=6i" + 4 * "Qqq").pack
+_mm_pack_grad = struct.Struct("=6i" + 7 * "Qqq").pack
 
 
 def fs_linear(x, w, y, *, bias=None, residual=None, activation: str = "none", x_scale=None, w_scale=None,
@@ -836,21 +835,26 @@ def fs_linear(x, w, y, *, bias=None, residual=None, activation: str = "none", x_
     if (x1 == w1 == y1 == 1 and w.shape == (out, inner) and y.shape == size and w.dtype is of_x and kind is not None
             and out_kind is not None and act is not None
             and x.get_device() == w.get_device() == y.get_device() == index == _current_device()):
-        xr = x.data_ptr(), x0, 0 if x_scale is None else _mm_scale(x_scale, "x", index, rows)
-        wr = w.data_ptr(), w0, 0 if w_scale is None else _mm_scale(w_scale, "w", index, out)
-        yr = y.data_ptr(), y0, 0
+        xs = 0 if x_scale is None else _mm_scale(x_scale, "x", index, rows)
+        ws = 0 if w_scale is None else _mm_scale(w_scale, "w", index, out)
+        xp, wp, yp = x.data_ptr(), w.data_ptr(), y.data_ptr()
     else:
         index, kind, out_kind, act = _mm_head(workspace, x, y, activation)
-        xr = _mm_rows(x, "x", of_x, index, (rows, inner), x_scale)
-        wr = _mm_rows(w, "w", of_x, index, (out, inner), w_scale)
-        yr = _mm_rows(y, "y", dtype, index, size)
-    rr = _NO_ROWS if residual is None else _mm_rows(residual, "residual", dtype, index, size)
-    b = 0
+        xp, x0, xs = _mm_rows(x, "x", of_x, index, (rows, inner), x_scale)
+        wp, w0, ws = _mm_rows(w, "w", of_x, index, (out, inner), w_scale)
+        yp, y0, _ = _mm_rows(y, "y", dtype, index, size)
+    rp = r0 = bp = 0
+    if residual is not None:
+        r0, r1 = residual.stride()
+        if r1 == 1 and residual.shape == size and residual.dtype is dtype and residual.get_device() == index:
+            rp = residual.data_ptr()
+        else:
+            rp, r0, _ = _mm_rows(residual, "residual", dtype, index, size)
     if bias is not None:
         if bias.shape != (out,) or bias.dtype is not dtype or bias.get_device() != index or not bias.is_contiguous():
             raise ValueError(f"bias is a contiguous {dtype} [{out}] on cuda:{index}")
-        b = bias.data_ptr()
-    a = _MM_LINEAR.pack(rows, inner, out, kind, out_kind, act, *xr, *wr, *rr, *yr, b)
+        bp = bias.data_ptr()
+    a = _mm_pack_linear(rows, inner, out, kind, out_kind, act, xp, x0, xs, wp, w0, ws, rp, r0, 0, yp, y0, 0, bp)
     rc = lib().fs_linear(a, workspace.address, workspace.bytes, _current_stream(index) if stream is None else _kv_stream(stream, index))
     if rc:
         _check(rc)
@@ -868,17 +872,17 @@ def fs_gated_ff(x, w_gate, w_up, y, *, activation: str = "silu", x_scale=None, g
     if (x1 == g1 == u1 == y1 == 1 and w_gate.shape == size and w_up.shape == size and y.shape == (rows, out) and w_gate.dtype is of_x
             and w_up.dtype is of_x and kind is not None and out_kind is not None and act is not None
             and x.get_device() == w_gate.get_device() == w_up.get_device() == y.get_device() == index == _current_device()):
-        xr = x.data_ptr(), x0, 0 if x_scale is None else _mm_scale(x_scale, "x", index, rows)
-        gr = w_gate.data_ptr(), g0, 0 if gate_scale is None else _mm_scale(gate_scale, "w_gate", index, out)
-        ur = w_up.data_ptr(), u0, 0 if up_scale is None else _mm_scale(up_scale, "w_up", index, out)
-        yr = y.data_ptr(), y0, 0
+        xs = 0 if x_scale is None else _mm_scale(x_scale, "x", index, rows)
+        gs = 0 if gate_scale is None else _mm_scale(gate_scale, "w_gate", index, out)
+        us = 0 if up_scale is None else _mm_scale(up_scale, "w_up", index, out)
+        xp, gp, up, yp = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), y.data_ptr()
     else:
         index, kind, out_kind, act = _mm_head(workspace, x, y, activation)
-        xr = _mm_rows(x, "x", of_x, index, (rows, inner), x_scale)
-        gr = _mm_rows(w_gate, "w_gate", of_x, index, size, gate_scale)
-        ur = _mm_rows(w_up, "w_up", of_x, index, size, up_scale)
-        yr = _mm_rows(y, "y", dtype, index, (rows, out))
-    a = _MM_GATED.pack(rows, inner, out, kind, out_kind, act, *xr, *gr, *ur, *yr)
+        xp, x0, xs = _mm_rows(x, "x", of_x, index, (rows, inner), x_scale)
+        gp, g0, gs = _mm_rows(w_gate, "w_gate", of_x, index, size, gate_scale)
+        up, u0, us = _mm_rows(w_up, "w_up", of_x, index, size, up_scale)
+        yp, y0, _ = _mm_rows(y, "y", dtype, index, (rows, out))
+    a = _mm_pack_gated(rows, inner, out, kind, out_kind, act, xp, x0, xs, gp, g0, gs, up, u0, us, yp, y0, 0)
     rc = lib().fs_gated_ff(a, workspace.address, workspace.bytes, _current_stream(index) if stream is None else _kv_stream(stream, index))
     if rc:
         _check(rc)
@@ -903,14 +907,14 @@ def fs_gated_ff_backward(x, w_gate, w_up, dy, dx, dw_gate, dw_up, *, activation:
         parts = [v for t, name, size in (
             (x, "x", of_x), (w_gate, "w_gate", of_w), (w_up, "w_up", of_w), (dy, "dy", (rows, out)),
             (dx, "dx", of_x), (dw_gate, "dw_gate", of_w), (dw_up, "dw_up", of_w)) for v in _mm_rows(t, name, dtype, index, size)]
-    a = _MM_GRAD.pack(rows, inner, out, kind, act, 0, *parts)
+    a = _mm_pack_grad(rows, inner, out, kind, act, 0, *parts)
     rc = lib().fs_gated_ff_backward(a, workspace.address, workspace.bytes, _kv_stream(stream, index))
     if rc:
         _check(rc)
     return dx, dw_gate, dw_up
 
 
-_MM_ROWS = struct.Struct("=Qqq")
+_mm_pack_rows = struct.Struct("=Qqq").pack
 
 
 def fs_quantise_rows(x, codes, scale, *, stream=None):
@@ -925,12 +929,12 @@ def fs_quantise_rows(x, codes, scale, *, stream=None):
     if codes.element_size() != 1:
         raise ValueError(f"codes are {codes.dtype}, not float8_e4m3fn or uint8")
     if x1 == c1 == 1 and codes.shape == size and codes.get_device() == index:
-        xr, c_at, c_stride = (x.data_ptr(), x0, 0), codes.data_ptr(), c0
+        xp, cp = x.data_ptr(), codes.data_ptr()
     else:
-        xr = _mm_rows(x, "x", dtype, index, size)
-        c_at, c_stride, _ = _mm_rows(codes, "codes", codes.dtype, index, size)
-    s_at = _mm_scale(scale, "codes", index, rows)
-    rc = lib().fs_quantise_rows(rows, inner, kind, _MM_ROWS.pack(*xr), _MM_ROWS.pack(c_at, c_stride, 0), s_at,
+        xp, x0, _ = _mm_rows(x, "x", dtype, index, size)
+        cp, c0, _ = _mm_rows(codes, "codes", codes.dtype, index, size)
+    sp = _mm_scale(scale, "codes", index, rows)
+    rc = lib().fs_quantise_rows(rows, inner, kind, _mm_pack_rows(xp, x0, 0), _mm_pack_rows(cp, c0, 0), sp,
                                 _current_stream(index) if stream is None else _kv_stream(stream, index))
     if rc:
         _check(rc)
