@@ -42,11 +42,15 @@ static_assert(kSmem >= 1024 + kRing + sizeof(WideBars), "a block's shared memory
 // Whether a tile's columns are W's rows (and not gate's and up's).
 __host__ __device__ constexpr bool one_sum(int mode) { return mode == MM_LINEAR || mode == MM_GRAD; }
 
-// One tile: of product `p`, rows from m0 and columns (gated: results) from n0.
+// One tile: of product q, rows from m0 and columns (gated: results) from n0.
 struct Tile {
-  const MmProduct* p;
-  int m0, n0;
+  int q, m0, n0;
 };
+// (never by a pointer: what a kernel's arguments hold is read by its index, or for a single product as constants)
+template <int kMode>
+__device__ __forceinline__ const MmProduct& product_of(const MmWideArgs& a, const Tile& t) {
+  return a.product[kMode == MM_GRAD ? t.q : 0];
+}
 
 template <int kMode>
 __device__ __forceinline__ Tile tile_of(const MmWideArgs& a, long long i) {
@@ -58,7 +62,7 @@ __device__ __forceinline__ Tile tile_of(const MmWideArgs& a, long long i) {
   const int tn = (int)(p.tiles / tm);
   const long long per = (long long)kGroup * tn;
   const int g = (int)(i / per), r = (int)(i - g * per), high = min(kGroup, tm - g * kGroup);
-  return {&p, (g * kGroup + r % high) * kTile, r / high * (one_sum(kMode) ? p.tile : p.tile / 2)};
+  return {q, (g * kGroup + r % high) * kTile, r / high * (one_sum(kMode) ? p.tile : p.tile / 2)};
 }
 
 __device__ __forceinline__ void tma_pair(uint32_t dst, const CUtensorMap* m, int x, int y, uint32_t bar) {
@@ -202,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
     int n = 0;
     for (long long i = first; ok && i < a.tiles; i = next(i, ++n)) {
       const Tile t = tile_of<kMode>(a, i);
-      const MmProduct& p = *t.p;
+      const MmProduct& p = product_of<kMode>(a, t);
       const int row = !of_b ? t.m0 + rank * 128 : one_sum(kMode) ? t.n0 + rank * (p.tile / 2) : t.n0;
       const uint32_t part_bytes = of_b ? p.tile / 2 * kMmBlock : kHalf, bytes = a.sub * (2 * kHalf + p.tile * kMmBlock);  // a block's; both SMs' stage
       const bool high = !of_b || p.tile > 128;
@@ -237,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
       int st = 0, n = 0;
       uint32_t par = 0, at = 0;
       for (long long i = first; i < a.tiles; i = next(i, ++n)) {
-        const MmProduct& p = *tile_of<kMode>(a, i).p;
+        const MmProduct& p = product_of<kMode>(a, tile_of<kMode>(a, i));
         const bool a_mn = kMode == MM_GRAD && p.a_mn, b_mn = kMode == MM_GRAD && p.b_mn;
         const uint32_t d = (n & 1) * kTile, idesc = mm_instr(kTile, p.tile, a.format, a_mn, b_mn);
         const uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;
@@ -282,45 +286,83 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
     bool ok = true;  // (a warp whose wait ran out keeps coming to the barriers of the eight)
     // the 16-byte piece `piece` of row `r` there
     auto at_piece = [](int r, int piece) { return 4 * r + (piece ^ (r >> 1 & 3)); };
-    int n = 0;
-    for (long long i = first; i < a.tiles; i = next(i, ++n)) {
-      const Tile t = tile_of<kMode>(a, i);
-      const MmEpilogue& e = t.p->e;
-      const long long m0 = t.m0 + rank * 128 + (w & 3) * 32, m = m0 + lane;
-      const bool row = m < e.rows;
-      const int width = one_sum(kMode) ? t.p->tile : t.p->tile / 2;  // results of a row
-      // what the columns share goes to shared memory, and a row's own first part is asked for, while the sums are made
+    // What a tile's columns share and its rows' own factors, asked for a tile ahead.
+    struct Ahead {
+      float scale = 0.f, x_scale = 1.f;
+      uint16_t bias = 0;
+    };
+    auto look = [&](const Tile& t) {
+      Ahead v;
+      const MmProduct& p = product_of<kMode>(a, t);
+      const MmEpilogue& e = p.e;
+      const int width = one_sum(kMode) ? p.tile : p.tile / 2;
       if (kScaled && (e.x_scale || e.bias)) {
-        const int c = one_sum(kMode) || id < width ? id : id - width, col = t.n0 + c;
-        const float* from = one_sum(kMode) || id < width ? e.w_scale[0] : e.w_scale[1];
-        const bool in = id < t.p->tile && col < e.cols;
-        const float sc = in && e.x_scale ? from[col] : 0.f;
-        const uint16_t b = in && e.bias ? static_cast<const uint16_t*>(e.bias)[col] : 0;
-        asm volatile("bar.sync 1, 256;" ::: "memory");  // (the tile before has been finished with the old ones)
-        bars.scale[id] = sc, bars.bias[id] = b;
-        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const bool first_w = one_sum(kMode) || id < width;
+        const int col = t.n0 + (first_w ? id : id - width);
+        const bool in = id < p.tile && col < e.cols;
+        if (in && e.x_scale) v.scale = e.w_scale[first_w ? 0 : 1][col];
+        if (in && e.bias) v.bias = static_cast<const uint16_t*>(e.bias)[col];
+        const long long m = t.m0 + rank * 128 + (w & 3) * 32 + lane;
+        if (e.x_scale && m < e.rows) v.x_scale = e.x_scale[m];
       }
-      const float xs = kScaled && e.x_scale && row ? e.x_scale[m] : 1.f;
+      // (what is added comes from memory: into the L2, lines of 128 bytes, two threads a row)
+      if (kMode != MM_GRAD && e.in) {
+        const long long m = t.m0 + rank * 128 + (id >> 1);
+        if (m < e.rows)
+          for (int c = 64 * (id & 1); c < width && t.n0 + c < e.cols; c += 128)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint16_t*>(e.in) + m * e.in_stride + t.n0 + c));
+      }
+      return v;
+    };
+    int n = 0;
+    Tile t{};
+    Ahead own;
+    if (first < a.tiles) t = tile_of<kMode>(a, first), own = look(t);
+    for (long long i = first; i < a.tiles;) {
+      const Tile here = t;
+      const MmProduct& p = product_of<kMode>(a, here);
+      const MmEpilogue& e = p.e;
+      const long long m0 = here.m0 + rank * 128 + (w & 3) * 32;
+      const int width = one_sum(kMode) ? p.tile : p.tile / 2;  // results of a row
       const bool adds = kMode != MM_GRAD && e.in;
-      uint4 next[kPieces];
+      uint4 added[kPieces];
+      // (where all 32 rows and a chunk's columns are inside, its accesses go out together: one by one 434 cycles for four stores)
+      const bool rows_in = m0 + 32 <= e.rows;
+      const int r_in = lane / kPieces, c_in = 8 * (lane % kPieces);
       auto ask = [&](int c) {
+        const int col = here.n0 + kCols * c + c_in;
+        if (rows_in && here.n0 + kCols * (c + 1) <= e.cols && kCols * c < width) {
+          const uint16_t* from = static_cast<const uint16_t*>(e.in) + (m0 + r_in) * e.in_stride + col;
 #pragma unroll
-        for (int g = 0; g < kPieces; ++g) {
-          const int r = g * (32 / kPieces) + lane / kPieces, col = t.n0 + kCols * c + 8 * (lane % kPieces);
-          next[g] = m0 + r < e.rows && col < e.cols && kCols * c < width ? load8(e.in, (m0 + r) * e.in_stride + col, e.cols - col) : make_uint4(0, 0, 0, 0);
+          for (int g = 0; g < kPieces; ++g) added[g] = *reinterpret_cast<const uint4*>(from + g * (32 / kPieces) * e.in_stride);
+        } else {
+#pragma unroll
+          for (int g = 0; g < kPieces; ++g) {
+            const int r = g * (32 / kPieces) + r_in;
+            added[g] = m0 + r < e.rows && col < e.cols && kCols * c < width ? load8(e.in, (m0 + r) * e.in_stride + col, e.cols - col) : make_uint4(0, 0, 0, 0);
+          }
         }
       };
-      if (!ok) continue;
       if (adds) ask(half);
-      ok = __all_sync(~0u, mm_wait(&bars.sum_full[n & 1], n >> 1 & 1, a.status));
+      if (kScaled && (e.x_scale || e.bias)) {
+        asm volatile("bar.sync 1, 256;" ::: "memory");  // (the tile before has been finished with the old ones)
+        bars.scale[id] = own.scale, bars.bias[id] = own.bias;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+      }
+      const float xs = own.x_scale;
+      const long long then = next(i, n + 1);
+      if (then < a.tiles) t = tile_of<kMode>(a, then), own = look(t);
+      const int k = n++;
+      i = then;
+      ok = ok && __all_sync(~0u, mm_wait(&bars.sum_full[k & 1], k >> 1 & 1, a.status));
       if (!ok) continue;
       fence_after();
-      const uint32_t at = tmem + lanes + (n & 1) * kTile;
+      const uint32_t at = tmem + lanes + (k & 1) * kTile;
       mm_with_act(kMode == MM_GRAD ? FS_ACT_NONE : e.act, [&](auto act) {
         constexpr int kAct = decltype(act)::value;
 #pragma unroll 1
         for (int c = half; kCols * c < width; c += 2) {
-          const int n0 = t.n0 + kCols * c;
+          const int n0 = here.n0 + kCols * c;
           if (n0 >= e.cols) break;
           __syncwarp();
           uint32_t z[kCols], u[kCols];
@@ -328,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
           if (!one_sum(kMode)) tmem_ld(u, at + width + kCols * c);
           if (adds) {
 #pragma unroll
-            for (int g = 0; g < kPieces; ++g) pass[at_piece(g * (32 / kPieces) + lane / kPieces, lane % kPieces)] = next[g];
+            for (int g = 0; g < kPieces; ++g) pass[at_piece(g * (32 / kPieces) + lane / kPieces, lane % kPieces)] = added[g];
             ask(c + 2);
             __syncwarp();
           }
@@ -380,17 +422,27 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
             pass[at_piece(lane, g)] = pack8<T>(v);  // (where its own addend was)
           }
           __syncwarp();
+          const int piece = lane % 4, col = n0 + 8 * (piece % kPieces);
+          void* const out = kMode == MM_BACK && piece >= kPieces ? e.out[1] : e.out[0];
+          if (rows_in && n0 + kCols <= e.cols) {
+            uint16_t* to = static_cast<uint16_t*>(out) + (m0 + lane / 4) * e.out_stride + col;
+            uint4 y[4];
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int r = 8 * g + lane / 4, piece = lane % 4, col = n0 + 8 * (piece % kPieces);
-            if (m0 + r < e.rows && col < e.cols)
-              store8(kMode == MM_BACK && piece >= kPieces ? e.out[1] : e.out[0], (m0 + r) * e.out_stride + col, pass[at_piece(r, piece)], e.cols - col);
+            for (int g = 0; g < 4; ++g) y[g] = pass[at_piece(8 * g + lane / 4, piece)];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) *reinterpret_cast<uint4*>(to + 8 * g * e.out_stride) = y[g];
+          } else {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const int r = 8 * g + lane / 4;
+              if (m0 + r < e.rows && col < e.cols) store8(out, (m0 + r) * e.out_stride + col, pass[at_piece(r, piece)], e.cols - col);
+            }
           }
         }
       });
       fence_before();
       __syncwarp();
-      if (lane == 0) arrive_at(cluster_addr(smem_u32(&bars.sum_empty[n & 1]), 0));
+      if (lane == 0) arrive_at(cluster_addr(smem_u32(&bars.sum_empty[k & 1]), 0));
     }
   }
   __syncwarp();
