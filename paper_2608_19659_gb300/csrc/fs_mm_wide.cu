@@ -305,8 +305,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
         const long long m = t.m0 + rank * 128 + (w & 3) * 32 + lane;
         if (e.x_scale && m < e.rows) v.x_scale = e.x_scale[m];
       }
-      // (what is added comes from memory: into the L2, lines of 128 bytes, two threads a row)
-      if (kMode != MM_GRAD && e.in) {
+      // (what is added comes from memory: where a tile's sum takes no longer than its end it comes too late, so into the L2, lines of 128
+      // bytes, two threads a row)
+      if (kMode != MM_GRAD && e.in && p.blocks[0] <= 16) {
         const long long m = t.m0 + rank * 128 + (id >> 1);
         if (m < e.rows)
           for (int c = 64 * (id & 1); c < width && t.n0 + c < e.cols; c += 128)
@@ -375,6 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
             __syncwarp();
           }
           wait_ld();
+          uint4 y[(kMode == MM_BACK ? 2 : 1) * kPieces];
 #pragma unroll
           for (int g = 0; g < kPieces; ++g) {
             const int in_tile = kCols * c + 8 * g;
@@ -417,16 +419,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
                 v[j] = s[j] * second[j] * slope;
                 second[j] = s[j] * y;
               }
-              pass[at_piece(lane, 2 + g)] = pack8<T>(second);
+              y[kPieces + g] = pack8<T>(second);
             }
-            pass[at_piece(lane, g)] = pack8<T>(v);  // (where its own addend was)
+            y[g] = pack8<T>(v);
           }
+          // (after all that is read of shared memory, which a store between would hold up; where a row's own addend was)
+#pragma unroll
+          for (int g = 0; g < (kMode == MM_BACK ? 2 : 1) * kPieces; ++g) pass[at_piece(lane, g)] = y[g];
           __syncwarp();
           const int piece = lane % 4, col = n0 + 8 * (piece % kPieces);
           void* const out = kMode == MM_BACK && piece >= kPieces ? e.out[1] : e.out[0];
           if (rows_in && n0 + kCols <= e.cols) {
             uint16_t* to = static_cast<uint16_t*>(out) + (m0 + lane / 4) * e.out_stride + col;
-            uint4 y[4];
 #pragma unroll
             for (int g = 0; g < 4; ++g) y[g] = pass[at_piece(8 * g + lane / 4, piece)];
 #pragma unroll
