@@ -1,4 +1,5 @@
 // The products of a rank's layer: entry points, and rows to e4m3.
+#include <algorithm>
 #include <cuda_runtime.h>
 
 #include <cstdarg>
@@ -27,11 +28,14 @@ int cuda_say(cudaError_t e, const char* what) { return say(FS_ECUDA, "%s: %s", w
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 constexpr int kMaxSize = 1 << 24;
+constexpr int64_t kMaxElements = 1ll << 40;
 
 int check_sizes(int rows, int in, int out) {
   if (rows < 0 || rows > kMaxSize) return say(FS_EINVAL, "rows = %d outside [0, 2^24]", rows);
   if (in < 1 || in > kMaxSize) return say(FS_EINVAL, "in = %d outside [1, 2^24]", in);
   if (out < 0 || out > kMaxSize) return say(FS_EINVAL, "out = %d outside [0, 2^24]", out);
+  if (std::max({(int64_t)rows * in, (int64_t)rows * out, (int64_t)out * in}) >= kMaxElements)
+    return say(FS_EINVAL, "rows = %d, in = %d, out = %d: an operand of 2^40 elements or more", rows, in, out);
   return FS_OK;
 }
 
@@ -151,7 +155,7 @@ int wide_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, cons
   if (int rc = rows_map(&a.maps[1], w.data, e.cols, c.in, w.stride, c.type, tile / 2)) return rc;
   if (up)
     if (int rc = rows_map(&a.maps[2], up->data, e.cols, c.in, up->stride, c.type, tile / 2)) return rc;
-  a.product[0] = {e, {0, 0}, {1, 2}, {c.blocks(), 0}, false, false, tile, 0};
+  a.product[0] = {e, {0, 0}, {1, 2}, {c.blocks(), 0}, false, false, tile};
   a.products = 1;
   a.status = c.status;
   const cudaError_t r = launch_mm_wide(a, e.out[1] ? MM_BACK : up ? MM_GATED : MM_LINEAR, c.type, c.out_type, c.sms, c.stream);
@@ -428,9 +432,9 @@ extern "C" int fs_gated_ff_backward(const fs_mm_gated_grad* args, void* workspac
   if (int rc = rows_map(&a.maps[X_T], g.x.data, g.rows, g.in, g.x.stride, g.type, 64)) return rc;
   auto to = [&](const fs_mm_rows& r, int n) { return MmEpilogue{n, g.in, FS_ACT_NONE, nullptr, {}, nullptr, nullptr, 0, {r.data, nullptr}, r.stride}; };
   const int out_blocks = (g.out + 63) / 64, row_blocks = (g.rows + 63) / 64;
-  a.product[0] = {to(g.dx, g.rows), {DG, DU}, {WG_T, WU_T}, {out_blocks, out_blocks}, false, true, 0, 0};
-  a.product[1] = {to(g.dw_gate, g.out), {DG_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, 0, 0};
-  a.product[2] = {to(g.dw_up, g.out), {DU_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true, 0, 0};
+  a.product[0] = {to(g.dx, g.rows), {DG, DU}, {WG_T, WU_T}, {out_blocks, out_blocks}, false, true};
+  a.product[1] = {to(g.dw_gate, g.out), {DG_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true};
+  a.product[2] = {to(g.dw_up, g.out), {DU_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true};
   a.products = 3;
   a.status = c.status;
   const cudaError_t e = launch_mm_wide(a, MM_GRAD, g.type, g.type, c.sms, c.stream);

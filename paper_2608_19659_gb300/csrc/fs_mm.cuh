@@ -154,7 +154,9 @@ struct MmProduct {
   int a[2], b[2], blocks[2];
   bool a_mn, b_mn;
   int tile;         // (MM_GRAD: launch_mm_wide's) columns of a tile (gated: of gate and of up together): a multiple of 32 (gated: 64) up to 256
-  long long tiles;  // (launch_mm_wide's)
+  // launch_mm_wide's: tiles of rows, tiles in all, and of a group of rows' tiles that are walked over together. (Under 2^31: no operand
+  // has 2^40 elements)
+  int row_tiles, tiles, group;
 };
 struct MmWideArgs {
   CUtensorMap maps[8];
@@ -162,7 +164,7 @@ struct MmWideArgs {
   int products, eight, format;
   int lead, rounds;        // (launch_mm_wide's: pairs that start with one of the longest tiles, and how many others that takes as long as)
   int stages, stage, sub;  // (launch_mm_wide's: stages of the ring, their bytes, and blocks of the sum)
-  long long tiles;
+  int tiles;
   uint32_t* status;
 };
 int mm_wide_tile(int rows, int cols, int blocks, bool gated, int sms, float* ns);

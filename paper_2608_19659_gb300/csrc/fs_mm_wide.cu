@@ -53,16 +53,16 @@ __device__ __forceinline__ const MmProduct& product_of(const MmWideArgs& a, cons
 }
 
 template <int kMode>
-__device__ __forceinline__ Tile tile_of(const MmWideArgs& a, long long i) {
-  int q = 0;
+__device__ __forceinline__ Tile tile_of(const MmWideArgs& a, int i) {
+  Tile t{};
   if (kMode == MM_GRAD)
-    while (q + 1 < a.products && i >= a.product[q].tiles) i -= a.product[q++].tiles;
-  const MmProduct& p = a.product[q];
-  const int tm = (p.e.rows + kTile - 1) / kTile;
-  const int tn = (int)(p.tiles / tm);
-  const long long per = (long long)kGroup * tn;
-  const int g = (int)(i / per), r = (int)(i - g * per), high = min(kGroup, tm - g * kGroup);
-  return {q, (g * kGroup + r % high) * kTile, r / high * (one_sum(kMode) ? p.tile : p.tile / 2)};
+    while (t.q + 1 < a.products && i >= a.product[t.q].tiles) i -= a.product[t.q++].tiles;
+  const MmProduct& p = product_of<kMode>(a, t);
+  const int g = (int)((unsigned)i / (unsigned)p.group), r = i - g * p.group, high = min(kGroup, p.row_tiles - g * kGroup);
+  const int across = high == kGroup ? r / kGroup : (int)((unsigned)r / (unsigned)high);
+  t.m0 = (g * kGroup + r - across * high) * kTile;
+  t.n0 = across * (one_sum(kMode) ? p.tile : p.tile / 2);
+  return t;
 }
 
 __device__ __forceinline__ void tma_pair(uint32_t dst, const CUtensorMap* m, int x, int y, uint32_t bar) {
@@ -140,11 +140,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
   const uint32_t rank = cluster_rank();
   // This pair's tiles: every `step`-th. Of gradients whose longest tiles are fewer than there are pairs, those pairs start with one of them, as
   // long as `rounds` of the others, which the other pairs take meanwhile: then `next` is the k-th tile.
-  const long long first = blockIdx.x >> 1, step = gridDim.x >> 1;
-  auto next = [&](long long i, int k) -> long long {
+  const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
+  auto next = [&](int i, int k) {
     if (kMode != MM_GRAD || !a.lead) return i + step;
-    const int mine = first < a.lead ? 1 : a.rounds;
-    const long long others = step - a.lead;
+    const int mine = first < a.lead ? 1 : a.rounds, others = step - a.lead;
     if (k < mine) return a.lead + k * others + (first - a.lead);
     return a.lead + a.rounds * others + (k - mine) * step + first;
   };
@@ -204,7 +203,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
       }
     };
     int n = 0;
-    for (long long i = first; ok && i < a.tiles; i = next(i, ++n)) {
+    for (int i = first; ok && i < a.tiles; i = next(i, ++n)) {
       const Tile t = tile_of<kMode>(a, i);
       const MmProduct& p = product_of<kMode>(a, t);
       const int row = !of_b ? t.m0 + rank * 128 : one_sum(kMode) ? t.n0 + rank * (p.tile / 2) : t.n0;
@@ -240,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
       const uint32_t stage = a.stage >> 4;
       int st = 0, n = 0;
       uint32_t par = 0, at = 0;
-      for (long long i = first; i < a.tiles; i = next(i, ++n)) {
+      for (int i = first; i < a.tiles; i = next(i, ++n)) {
         const MmProduct& p = product_of<kMode>(a, tile_of<kMode>(a, i));
         const bool a_mn = kMode == MM_GRAD && p.a_mn, b_mn = kMode == MM_GRAD && p.b_mn;
         const uint32_t d = (n & 1) * kTile, idesc = mm_instr(kTile, p.tile, a.format, a_mn, b_mn);
@@ -319,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
     Tile t{};
     Ahead own;
     if (first < a.tiles) t = tile_of<kMode>(a, first), own = look(t);
-    for (long long i = first; i < a.tiles;) {
+    for (int i = first; i < a.tiles;) {
       const Tile here = t;
       const MmProduct& p = product_of<kMode>(a, here);
       const MmEpilogue& e = p.e;
@@ -351,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
         asm volatile("bar.sync 1, 256;" ::: "memory");
       }
       const float xs = own.x_scale;
-      const long long then = next(i, n + 1);
+      const int then = next(i, n + 1);
       if (then < a.tiles) t = tile_of<kMode>(a, then), own = look(t);
       const int k = n++;
       i = then;
@@ -461,7 +460,7 @@ cudaError_t launch(const MmWideArgs& a, int sms, cudaStream_t s) {
   static std::atomic<uint64_t> seen{0};
   const cudaError_t limit = smem_limit_once(seen, reinterpret_cast<const void*>(k_mm_wide<T, kMode>), kSmem);
   if (limit != cudaSuccess) return limit;
-  const int pairs = (int)std::min<long long>(a.tiles, std::max(1, sms / 2));
+  const int pairs = std::min(a.tiles, std::max(1, sms / 2));
   return launch_clusters(k_mm_wide<T, kMode>, dim3(2 * pairs), dim3(kThreads), 2, kSmem, s, a);
 }
 
@@ -537,7 +536,9 @@ cudaError_t launch_mm_wide(MmWideArgs& a, int mode, int type, int out_type, int 
   for (int i = 0; i < a.products; ++i) {
     MmProduct& p = a.product[i];
     const int width = one_sum(mode) ? p.tile : p.tile / 2;
-    p.tiles = (long long)((p.e.rows + kTile - 1) / kTile) * ((p.e.cols + width - 1) / width);
+    p.row_tiles = (p.e.rows + kTile - 1) / kTile;
+    p.group = kGroup * ((p.e.cols + width - 1) / width);
+    p.tiles = p.row_tiles * (p.group / kGroup);
     a.tiles += p.tiles;
   }
   return out_type == FS_KV_FP16 ? launch_mode<__half>(a, mode, sms, s) : launch_mode<__nv_bfloat16>(a, mode, sms, s);

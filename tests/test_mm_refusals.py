@@ -270,3 +270,12 @@ def test_scales_that_overlap(fsb):
     for scale in (P16, P16 + 32, 4 * P16, 4 * P16 + 64):
         refused(fsb, fsb.lib().fs_quantise_rows(3, 20, 0, C.byref(x), C.byref(c), scale, None))
         assert b"overlap" in fsb.lib().fs_last_error()
+
+
+@pytest.mark.parametrize("name", CALLS)
+@pytest.mark.parametrize("sizes", [(1 << 20, 1 << 20, 1), (1 << 24, 1, 1 << 16), (1, 1 << 24, 1 << 16)])
+def test_operands_beyond_any_memory(fsb, name, sizes):
+    a = good(fsb)[name]
+    a.rows, a.in_, a.out = sizes
+    refused(fsb, call(fsb, name, a, n=1 << 62))
+    assert b"2^40" in fsb.lib().fs_last_error()
