@@ -26,8 +26,23 @@ __device__ __forceinline__ float mm_logistic(float z, float e) { return __fdivid
 
 constexpr float kLog2e = 1.44269504f, kTanhC = 0.7978845608f, kTanhD = 0.044715f;
 
-// Phi(z) by the complementary error function: no cancellation in the lower tail.
-__device__ __forceinline__ float mm_phi(float z) { return 0.5f * erfcf(-0.70710678f * z); }
+// Phi(z): without cancellation in the lower tail, as e^(-z^2 / 2) t P(t), t = 1 / (1 + 0.45 |z| / sqrt 2). t P(t) stands for half of
+// e^(x^2) erfc(x), x = |z| / sqrt 2, which falls as t does; P is of degree 7, fitted to it over x <= 10.5 for the least largest relative
+// error (Lawson's reweighted least squares): 3.2e-7, 7e-7 with the roundings, of the exponential z^2 2^-24 besides. (4096 rows of 512
+// over 4096 columns: 53 us by the library's erfcf, whose instructions were five times these.)
+__device__ __forceinline__ float mm_phi(float z) {
+  const float t = __fdividef(1.f, 1.f + 0.31819806f * fabsf(z));
+  float p = 0.03364478f;
+  p = p * t - 0.12102614f;
+  p = p * t + 0.10597738f;
+  p = p * t + 0.018687509f;
+  p = p * t + 0.09511253f;
+  p = p * t + 0.113793775f;
+  p = p * t + 0.12685856f;
+  p = p * t + 0.12695177f;
+  p *= t * ex2(-0.5f * kLog2e * z * z);
+  return z < 0.f ? p : 1.f - p;
+}
 
 template <int kAct>
 __device__ __forceinline__ float mm_act(float z) {
