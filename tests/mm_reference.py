@@ -27,13 +27,18 @@ def values(x, scale=None):
     return x.double() if scale is None else x.view(torch.float8_e4m3fn).double() * scale.double()[:, None]
 
 
+def _phi(z):
+    """The normal distribution (torch.special.ndtr loses the lower tail to cancellation: 0 at -9, not 1.1e-19)."""
+    return 0.5 * torch.special.erfc(-z / math.sqrt(2))
+
+
 def act(z, name):
     if name == "relu":
         return torch.where(z < 0, torch.zeros_like(z), z)
     if name == "silu":
         return z * torch.sigmoid(z)
     if name == "gelu":
-        return z * torch.special.ndtr(z)
+        return z * _phi(z)
     if name == "gelu_tanh":
         return z * torch.sigmoid(math.sqrt(8 / math.pi) * (z + 0.044715 * z**3))
     return z
@@ -46,7 +51,7 @@ def slope(z, name):
         s = torch.sigmoid(z)
         return s + z * s * (1 - s)
     if name == "gelu":
-        return torch.special.ndtr(z) + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+        return _phi(z) + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
     if name == "gelu_tanh":
         c = math.sqrt(8 / math.pi)
         s = torch.sigmoid(c * (z + 0.044715 * z**3))

@@ -442,3 +442,27 @@ def test_offsets_beyond_32_bits(fsb, cuda):
     c, s = big.view(torch.uint8).as_strided((T, K), (2 * ld, 1), 16384), torch.empty(T, device="cuda")
     fsb.fs_quantise_rows(x, c, s)
     assert torch.equal(c.view(torch.float8_e4m3fn).double(), ref.quantise(x)[0])
+
+
+@pytest.mark.parametrize("T", [90, 2500])
+@pytest.mark.parametrize("kind", KINDS[:2])
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu", "gelu_tanh"])
+def test_activations_over_their_range(fsb, cuda, act, kind, T):
+    """One term a sum, so that z is what x holds and the activation's own bound is all there is but the rounding."""
+    torch = cuda
+    dt = getattr(torch, kind)
+    z = torch.cat([torch.linspace(-16, 16, T // 2), torch.logspace(-7, 4, T - T // 2 - 2) * (1 - 2 * (torch.arange(T - T // 2 - 2) % 2)), torch.zeros(2)])
+    x, w = torch.zeros(T, 24, dtype=dt, device="cuda"), torch.zeros(40, 24, dtype=dt, device="cuda")
+    x[:, 3], w[:, 3] = z.cuda().to(dt), 1
+    y, work = torch.empty(T, 40, dtype=dt, device="cuda"), fsb.MmWorkspace(T, 24, 40)
+    fsb.fs_linear(x, w, y, activation=act, workspace=work)
+    at = x[:, 3:4].double().expand(T, 40)
+    want = ref._rounded(*ref._act(at, torch.zeros_like(at), act), dt)
+    ref.near(y, want)
+    fsb.fs_gated_ff(x, w, w, y, activation=act, workspace=work)  # act(z) z, where that is in the type's range
+    a, e = ref._act(at, torch.zeros_like(at), act)
+    a, e = a * at, e * at.abs() + ref.U * (a * at).abs()
+    inside = a.abs() < 60000
+    assert bool(inside.any())
+    got, (v, bound) = y, ref._rounded(a, e, dt)
+    ref.near(got[inside], (v[inside], bound[inside]))
