@@ -73,7 +73,8 @@ __device__ __forceinline__ float mm_act_slope(float z, float& slope) {
   }
   if (kAct == FS_ACT_GELU_TANH) {
     const float s = mm_logistic(1.f, 2.f * kLog2e * kTanhC * (z + kTanhD * z * z * z));
-    slope = s + z * s * (1.f - s) * 2.f * kTanhC * (1.f + 3.f * kTanhD * z * z);
+    // (beyond |z| = 20 s is 0 or 1, and z^2 may overflow)
+    slope = s + z * s * (1.f - s) * 2.f * kTanhC * (1.f + 3.f * kTanhD * fminf(z * z, 400.f));
     return z * s;
   }
   slope = 1.f;

@@ -466,3 +466,27 @@ def test_activations_over_their_range(fsb, cuda, act, kind, T):
     assert bool(inside.any())
     got, (v, bound) = y, ref._rounded(a, e, dt)
     ref.near(got[inside], (v[inside], bound[inside]))
+
+
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu", "gelu_tanh", "none"])
+@pytest.mark.parametrize("size", [1e3, 1e19, 1e24])
+def test_gradients_of_large_gates(fsb, cuda, act, size):
+    """A gate's values far out, where squares and cubes pass a float's range: the slope is 1 or 0 there (none: 1)."""
+    torch = cuda
+    T, K, N = 40, 8, 24
+    dt = torch.bfloat16
+    half = size**0.5
+    x, wg, wu, dy = (torch.zeros(n, m, dtype=dt, device="cuda") for n, m in ((T, K), (N, K), (N, K), (T, N)))
+    x[:, 0], wg[:, 0], wu[:, 0], dy[:] = half, half, 1 / half, 1 / size
+    wg[::2, 0] = -half
+    outs = [torch.full((n, K), float("nan"), dtype=dt, device="cuda") for n in (T, N, N)]
+    fsb.fs_gated_ff_backward(x, wg, wu, dy, *outs, activation=act, workspace=fsb.MmWorkspace(T, K, N, backward=True))
+    on = torch.tensor([1.0 if act == "none" or n % 2 else 0.0 for n in range(N)], device="cuda", dtype=torch.float64)
+    sign = torch.tensor([1.0 if n % 2 else -1.0 for n in range(N)], device="cuda", dtype=torch.float64)
+    # dg = on / size, du = on sign: dx = sum on sign (half / size + 1 / half), dw_gate = T on half / size, dw_up = T on sign half
+    want = [(on * sign).sum() * 2 / half, T * on * half / size, T * on * sign * half]
+    for o, w in zip(outs, want):
+        # half a step, 2^-8, each: half twice (x and w_gate) and once in dx's or dw's other factor, 1 / half and 1 / size or what stands for
+        # them, dg or du, the result: six in every product, and their products with each other
+        bound = 6.2 * 2.0**-8 * (w.abs() if w.dim() else 2 * N / half)
+        assert bool(((o[:, 0].double() - w).abs() <= bound).all()) and not bool(o[:, 1:].any())
