@@ -10,8 +10,8 @@
 // Of a gated block the first SM of a pair loads gate's rows and the second up's, so that a thread has both sums of a result.
 // Bound by the tensor cores, and they by power: 8192 rows of 8192 bf16 over 10240 677 to 690 us in a burst (2.0 PFLOP/s), 750 to 790 in a
 // row; 4096 rows of 7168 8-bit over 8192 131 us (3.7); the tensor pipe is active 87 to 90 % of the time with full waves. Tiles of short
-// sums are bound by their end (4096 rows of 1024 8-bit terms over 8192 columns 55 us, with a residual 67 and from memory 81; the products
-// alone 16).
+// sums are bound by their end (4096 rows of 1024 8-bit terms over 8192 columns 33 us, with a residual 48; the products alone 16): a tile's
+// takes 2.5 us, of a residual and an activation up to 5.5.
 #include <algorithm>
 #include <atomic>
 #include <utility>
@@ -480,8 +480,8 @@ cudaError_t launch_mode(const MmWideArgs& a, int mode, int sms, cudaStream_t s) 
 // and commit of a narrow one (8192 terms over one tile: 256 wide 42 us, 192 33.7, 160 29.3, 128 26.6, 96 25.7, 64 24.4).
 float mm_wide_block(int tile) { return tile <= 128 ? 140.f + 0.22f * tile : 8.f + 1.13f * tile; }
 
-// The width of a tile by an estimate of the time (in ns): of its sums, or of its end, 17 ns a column, where that is longer
-// (2048 rows of 512 over 512: 256 wide 9.6 us, 64 wide 5.3); and the longer the work the more what narrow tiles read again costs (8192 rows over
+// The width of a tile by an estimate of the time (in ns): of its sums, or of its end, 17 ns a column (with an activation; 10 without; a
+// choice by 12 comes out the same), where that is longer (2048 rows of 512 over 512: 256 wide 9.6 us, 64 wide 5.3); and the longer the work the more what narrow tiles read again costs (8192 rows over
 // 10240: 256 699 us, 192 816). W is read at 6.6 TB/s, and a quarter of the lesser of both comes on top (32 rows over 10240 of 8192, 160: 35.3).
 int mm_wide_tile(int rows, int cols, int blocks, bool gated, int sms, float* ns) {
   int best = 0;
