@@ -896,19 +896,23 @@ def fs_gated_ff_backward(x, w_gate, w_up, dy, dx, dw_gate, dw_up, *, activation:
     index, dtype = workspace.index, x.dtype
     kind, act = _mm_kinds.get(dtype), ACTIVATIONS.get(activation)
     (rows, inner), out = x.shape, w_gate.shape[0]
-    of_x, of_w = (rows, inner), (out, inner)
-    parts, usual = [], kind is not None and act is not None and index == _current_device()
-    for t, size in ((x, of_x), (w_gate, of_w), (w_up, of_w), (dy, (rows, out)), (dx, of_x), (dw_gate, of_w), (dw_up, of_w)):
-        s0, s1 = t.stride()
-        usual = usual and s1 == 1 and t.shape == size and t.dtype is dtype and t.get_device() == index
-        parts += (t.data_ptr(), s0, 0)
-    if not usual:
+    of_x, of_w, of_y = (rows, inner), (out, inner), (rows, out)
+    (x0, x1), (g0, g1), (u0, u1), (y0, y1) = x.stride(), w_gate.stride(), w_up.stride(), dy.stride()
+    (a0, a1), (b0, b1), (c0, c1) = dx.stride(), dw_gate.stride(), dw_up.stride()
+    if (x1 == g1 == u1 == y1 == a1 == b1 == c1 == 1 and w_gate.shape == w_up.shape == dw_gate.shape == dw_up.shape == of_w
+            and dx.shape == of_x and dy.shape == of_y and kind is not None and act is not None
+            and w_gate.dtype is w_up.dtype is dy.dtype is dx.dtype is dw_gate.dtype is dw_up.dtype is dtype
+            and x.get_device() == w_gate.get_device() == w_up.get_device() == dy.get_device() == dx.get_device()
+            == dw_gate.get_device() == dw_up.get_device() == index == _current_device()):
+        a = _mm_pack_grad(rows, inner, out, kind, act, 0, x.data_ptr(), x0, 0, w_gate.data_ptr(), g0, 0, w_up.data_ptr(), u0, 0, dy.data_ptr(), y0, 0,
+                          dx.data_ptr(), a0, 0, dw_gate.data_ptr(), b0, 0, dw_up.data_ptr(), c0, 0)
+    else:
         index, kind, _, act = _mm_head(workspace, x, x, activation)
-        parts = [v for t, name, size in (
-            (x, "x", of_x), (w_gate, "w_gate", of_w), (w_up, "w_up", of_w), (dy, "dy", (rows, out)),
-            (dx, "dx", of_x), (dw_gate, "dw_gate", of_w), (dw_up, "dw_up", of_w)) for v in _mm_rows(t, name, dtype, index, size)]
-    a = _mm_pack_grad(rows, inner, out, kind, act, 0, *parts)
-    rc = lib().fs_gated_ff_backward(a, workspace.address, workspace.bytes, _kv_stream(stream, index))
+        a = _mm_pack_grad(rows, inner, out, kind, act, 0, *(v for t, name, size in (
+            (x, "x", of_x), (w_gate, "w_gate", of_w), (w_up, "w_up", of_w), (dy, "dy", of_y), (dx, "dx", of_x),
+            (dw_gate, "dw_gate", of_w), (dw_up, "dw_up", of_w)) for v in _mm_rows(t, name, dtype, index, size)))
+    rc = lib().fs_gated_ff_backward(a, workspace.address, workspace.bytes,
+                                    _current_stream(index) if stream is None else _kv_stream(stream, index))
     if rc:
         _check(rc)
     return dx, dw_gate, dw_up
