@@ -767,12 +767,15 @@ class MmWorkspace:
 
 
 _mm_kinds = {}  # torch dtype -> FS_KV_* or FS_E4M3
+_float32 = None  # torch's
 
 
 def _mm_known() -> dict:
+    global _float32
     if not _mm_kinds:
         import torch
 
+        _float32 = torch.float32
         _mm_kinds.update({torch.bfloat16: FS_KV_BF16, torch.float16: FS_KV_FP16, torch.float8_e4m3fn: FS_E4M3})
     return _mm_kinds
 
@@ -796,8 +799,7 @@ def _mm_rows(t, name: str, dtype, index: int, size: tuple[int, int], scale=None)
 
 def _mm_scale(scale, name: str, index: int, rows: int) -> int:
     """The address of the scales of that many rows."""
-    if (scale.shape != (rows,) or scale.element_size() != 4 or not scale.is_floating_point() or not scale.is_contiguous()
-            or scale.get_device() != index):
+    if scale.shape != (rows,) or scale.dtype is not _float32 or not scale.is_contiguous() or scale.get_device() != index:
         raise ValueError(f"{name}: scales are a contiguous float32 [{rows}] on cuda:{index}")
     return scale.data_ptr()
 
@@ -927,7 +929,9 @@ def fs_quantise_rows(x, codes, scale, *, stream=None):
     index, dtype, size = x.get_device(), x.dtype, x.shape
     if index < 0 or index != _current_device():
         raise ValueError(f"x is on {x.device}, cuda:{_current_device()} is current")
-    kind = _mm_type(dtype, "x")
+    kind = _mm_kinds.get(dtype)
+    if kind is None:
+        kind = _mm_type(dtype, "x")
     rows, inner = size
     (x0, x1), (c0, c1) = x.stride(), codes.stride()
     if codes.element_size() != 1:
