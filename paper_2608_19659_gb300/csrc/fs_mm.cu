@@ -189,18 +189,19 @@ __device__ __forceinline__ float scale_for(float amax) {
   return exp2_int(max(e - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0), -126));  // 448 = 1.75 * 2^8
 }
 
-// A row a group of kGroup threads, eight values a thread at a time. Between the maximum and the codes a row is held: in registers,
+// A row a group of kGroup threads (a warp of a block, or a block), eight values a thread at a time. Between the maximum and the codes a row is held: in registers,
 // kHeld pieces a thread, or (kHeld = 0) in shared memory, where more rows an SM are under way at once; what it does not hold is read
 // again. Bound by memory with many rows (8192 of 14336 bf16 54.6 us, 6.45 TB/s; with floats compared and every value looked at for
 // what is not finite 72.7), by latency with few.
 template <typename T, int kGroup, int kHeld>
-__global__ void __launch_bounds__(256) k_quantise_rows(int rows, int in, const T* x, long long x_stride, uint8_t* codes, long long c_stride, float* scale) {
+__global__ void __launch_bounds__(kGroup == 32 ? 256 : kGroup) k_quantise_rows(int rows, int in, const T* x, long long x_stride, uint8_t* codes, long long c_stride, float* scale) {
   extern __shared__ uint4 row_at[];
+  constexpr int kBlock = kGroup == 32 ? 256 : kGroup;
   __shared__ uint32_t top[8];
   pdl_trigger();
   pdl_wait();
-  const long long row = (long long)blockIdx.x * (256 / kGroup) + threadIdx.x / kGroup;
-  if (kGroup < 256 && row >= rows) return;
+  const long long row = (long long)blockIdx.x * (kBlock / kGroup) + threadIdx.x / kGroup;
+  if (kGroup == 32 && row >= rows) return;
   const int id = threadIdx.x % kGroup, pieces = (in + 7) / 8;
   const T* xr = x + row * x_stride;
   uint8_t* cr = codes + row * c_stride;
@@ -231,12 +232,12 @@ __global__ void __launch_bounds__(256) k_quantise_rows(int rows, int in, const T
     uint32_t m = max(most & 0xffffu, most >> 16);
 #pragma unroll
     for (int o = 16; o; o >>= 1) m = max(m, __shfl_xor_sync(~0u, m, o));
-    if (kGroup == 256) {
+    if (kGroup > 32) {
       __syncthreads();  // (the last join's have been read)
       if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = m;
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, top[i]);
+      for (int i = 0; i < kGroup / 32; ++i) m = max(m, top[i]);
     }
     return m;
   };
@@ -309,11 +310,18 @@ cudaError_t launch_quantise(int rows, int in, const fs_mm_rows& x, const fs_mm_r
   const T* xd = static_cast<const T*>(x.data);
   uint8_t* cd = static_cast<uint8_t*>(codes.data);
   const long long xs = x.stride, cs = codes.stride;
-  if (in <= 2048) return launch_pdl(k_quantise_rows<T, 32, 8>, dim3((rows + 7) / 8), dim3(256), 0, s, rows, in, xd, xs, cd, cs, scale);
-  // few rows: registers (64 rows of 8192 2.0 us in graphs, in shared memory 2.3); else in what shared memory a block has without asking for
-  // more (8192 rows of 14336 54.6 us, in registers 75)
-  if (rows <= 256 && in <= 8192) return launch_pdl(k_quantise_rows<T, 256, 4>, dim3(rows), dim3(256), 0, s, rows, in, xd, xs, cd, cs, scale);
-  if (rows > 256 && in <= 24000) return launch_pdl(k_quantise_rows<T, 256, 0>, dim3(rows), dim3(256), (in + 7) / 8 * 16, s, rows, in, xd, xs, cd, cs, scale);
+  // Registers while all rows are under way at once, and where they hold a long row (64 rows of 8192 2.0 us in graphs, in shared memory 2.4;
+  // 1300 of 4096 5.5, in shared memory 6.2; one of 2048 1.4, by a warp 2.8)
+  if (in <= 8192 && (in > 6144 || rows <= (in <= 2048 ? 256 : 1536)))
+    return launch_pdl(k_quantise_rows<T, 256, 4>, dim3(rows), dim3(256), 0, s, rows, in, xd, xs, cd, cs, scale);
+  // many short rows: a warp each (4096 of 512 3.4, by blocks 4.6; 2048 of them 3.2 and 3.2)
+  if (in <= 2048 && rows > 2048) return launch_pdl(k_quantise_rows<T, 32, 8>, dim3((rows + 7) / 8), dim3(256), 0, s, rows, in, xd, xs, cd, cs, scale);
+  // else in what shared memory a block has without asking for more: blocks of 128 threads, so that more rows an SM are under way (8192 of 4096
+  // 18.1, 256 threads 22.9; 8192 of 8192 32.2, 256 threads in registers 31.6), of 256 for longer ones (8192 of 14336 54.0, 128 threads 58.3,
+  // in registers 65.5)
+  const size_t row = (in + 7) / 8 * 16;
+  if (in <= 6144) return launch_pdl(k_quantise_rows<T, 128, 0>, dim3(rows), dim3(128), row, s, rows, in, xd, xs, cd, cs, scale);
+  if (rows > 256 && in <= 24000) return launch_pdl(k_quantise_rows<T, 256, 0>, dim3(rows), dim3(256), row, s, rows, in, xd, xs, cd, cs, scale);
   return launch_pdl(k_quantise_rows<T, 256, 8>, dim3(rows), dim3(256), 0, s, rows, in, xd, xs, cd, cs, scale);
 }
 

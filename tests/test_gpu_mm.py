@@ -490,3 +490,21 @@ def test_gradients_of_large_gates(fsb, cuda, act, size):
         # them, dg or du, the result: six in every product, and their products with each other
         bound = 6.2 * 2.0**-8 * (w.abs() if w.dim() else 2 * N / half)
         assert bool(((o[:, 0].double() - w).abs() <= bound).all()) and not bool(o[:, 1:].any())
+
+
+@pytest.mark.parametrize("T,K", [(256, 2048), (257, 2048), (258, 1501), (2048, 130), (2049, 2048), (2100, 777), (1536, 2050), (1537, 2049), (1600, 6144),
+                                 (1600, 6145), (2500, 8192)])
+def test_quantise_many_rows(fsb, cuda, T, K):
+    """Around the sizes where rows change hands between registers, warps and shared memory, with values that are not finite."""
+    torch = cuda
+    x, _ = rows(torch, T, K, torch.bfloat16, T + K, 3.0, 8)
+    x.mul_(torch.exp2(torch.arange(T, device="cuda") % 40 - 20.0)[:, None].to(x.dtype))
+    x[1, K - 1], x[T // 2, 0], x[T - 1, K // 2], x[2] = float("inf"), float("nan"), float("-inf"), 0
+    buf = torch.full((T + 1, -(-K // 16) * 16 + 16), 5, dtype=torch.uint8, device="cuda")
+    c, s = buf[:T, :K].view(torch.float8_e4m3fn), torch.full((T + 3,), -1.0, device="cuda")
+    fsb.fs_quantise_rows(x, c, s[:T])
+    want, scale = ref.quantise(x)
+    assert torch.equal(s[:T].double(), scale) and bool((s[T:] == -1).all())
+    got = c.double()
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(), want.nan_to_num())
+    assert bool((buf[T:] == 5).all()) and bool((buf[:T, K:] == 5).all())
