@@ -680,7 +680,7 @@ typedef struct {
 /*
  * The workspace of the calls below: device memory of at least the bytes that fs_mm_workspace_bytes
  * gives for the largest sizes that will use it (backward != 0: fs_gated_ff_backward too), 256-byte
- * aligned, zero-filled once before its first use.
+ * aligned, its first 256 bytes zero-filled once, and that fill done, before its first use.
  */
 int fs_mm_workspace_bytes(int32_t rows, int32_t in, int32_t out, int32_t backward, int64_t *bytes);
 

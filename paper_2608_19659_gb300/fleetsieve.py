@@ -676,6 +676,16 @@ def _current_stream(index: int) -> int:
     return _current_stream(index)
 
 
+def _settle() -> None:
+    """Waits for torch's current stream: for what was just put there, and for those who had a workspace's memory before. Calls may go
+    to other streams at once, and a fill that came between two of a call's kernels would wipe out what they hand over. (A stream that
+    is being captured cannot be waited for; what is captured with it runs behind the fill.)"""
+    import torch
+
+    if not torch.cuda.is_current_stream_capturing():
+        torch.cuda.current_stream().synchronize()
+
+
 def _kv_stream(stream, index: int) -> int:
     if stream is None:
         return _current_stream(index)
@@ -751,9 +761,12 @@ def fs_kv_check(workspace: KvWorkspace, stream=None) -> None:
 
 # ---- the products of a rank's layer
 
+_MM_HEAD_BYTES = 256  # of a workspace: what has to be zero before its first use
+
+
 class MmWorkspace:
     """Device memory of the current device for products of these sizes, or smaller ones, one after the other
-    (``backward``: for fs_gated_ff_backward too)."""
+    (``backward``: for fs_gated_ff_backward too). Ready for calls on any stream."""
 
     def __init__(self, rows: int, in_features: int, out_features: int, backward: bool = False):
         import torch
@@ -761,7 +774,9 @@ class MmWorkspace:
         n = C.c_int64()
         _check(lib().fs_mm_workspace_bytes(int(rows), int(in_features), int(out_features), int(backward), C.byref(n)))
         self.index = _current_device()
-        self.tensor = torch.zeros(n.value, dtype=torch.uint8, device=f"cuda:{self.index}")
+        self.tensor = torch.empty(n.value, dtype=torch.uint8, device=f"cuda:{self.index}")
+        self.tensor[:_MM_HEAD_BYTES].zero_()
+        _settle()
         _mm_known()
         self.address, self.bytes = self.tensor.data_ptr(), n.value
 
