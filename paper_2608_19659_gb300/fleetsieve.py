@@ -608,7 +608,8 @@ class KvBatch:
 
 
 class KvWorkspace:
-    """Device memory for calls with this cache and batch, or smaller ones, one after the other."""
+    """Device memory for calls with this cache and batch, or smaller ones, one after the other. Ready for calls on any
+    stream."""
 
     def __init__(self, cache: KvCache, batch: KvBatch, q_heads: int):
         import torch
@@ -619,6 +620,7 @@ class KvWorkspace:
         n = C.c_int64()
         _check(lib().fs_kv_workspace_bytes(C.byref(cache.struct), C.byref(batch.struct), int(q_heads), C.byref(n)))
         self.tensor = torch.zeros(n.value, dtype=torch.uint8, device=cache.device)
+        _settle()
         self.address, self.bytes = self.tensor.data_ptr(), n.value
 
 

@@ -1,8 +1,9 @@
-"""Workspaces of the products, made on one stream and used on another."""
+"""Workspaces made on one stream and used on another."""
 
 import pytest
 
 import mm_reference as ref
+from test_gpu_kv_replays import check, setup
 from test_gpu_mm import operands, rows
 
 pytestmark = pytest.mark.gpu
@@ -46,3 +47,19 @@ def test_made_within_a_capture(fsb, cuda):
         for o, want in zip(outs, ref.gated_backward(x, *w, dy)):
             ref.near(o, want)
     fsb.fs_mm_check(work)
+
+
+def test_the_cache_operators(fsb, cuda):
+    """Tickets and parts of results of a cache that is read in parts: the fill is done when the constructor returns."""
+    torch = cuda
+    d, cache, b, q, _ = setup(torch, fsb, 1, 2, 2, 8, 128, 32, 4000)
+    out = torch.full_like(q, 7.0)
+    one, other = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(one):
+        torch.cuda._sleep(20_000_000)
+        work = fsb.KvWorkspace(cache, b, 16)
+        assert one.query()
+    fsb.fs_kv_attend(cache, b, q, out, 0.1, workspace=work, stream=other)
+    fsb.fs_kv_check(work, stream=other)
+    check(out, q, d, d["length"], d["q_start"], 0.1)

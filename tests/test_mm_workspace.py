@@ -1,6 +1,7 @@
 """A workspace is ready for calls on any stream when its constructor returns (stand-ins for CUDA: no GPU needed)."""
 
 import ctypes as C
+import types
 
 import pytest
 import torch
@@ -41,3 +42,17 @@ def test_products_within_a_capture(fsb, monkeypatch):
     d = Device(monkeypatch, fsb, True)
     fsb.MmWorkspace(300, 200, 500, backward=True)
     assert not d.seen and not d.memory[:256].any()
+
+
+def test_the_cache_operators(fsb, monkeypatch):
+    d = Device(monkeypatch, fsb, False)
+
+    def workspace_bytes(cache, batch, q_heads, n):  # (the library's asks for a device)
+        n._obj.value = 70000
+        return fsb.FS_OK
+
+    monkeypatch.setattr(fsb, "lib", lambda: types.SimpleNamespace(fs_kv_workspace_bytes=workspace_bytes))
+    on = lambda struct: types.SimpleNamespace(struct=struct, index=0, device="cuda:0")  # noqa: E731
+    work = fsb.KvWorkspace(on(fsb.fs_kv_cache()), on(fsb.fs_kv_batch()), 16)
+    assert len(d.memory) == work.bytes == 70000
+    assert len(d.seen) == 1 and not d.seen[0].any()
