@@ -123,11 +123,12 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* m, int
                : "memory");
 }
 
-// A wait that says so when it runs out; the caller leaves its loop.
+// A whole warp's wait, which says so when it runs out; the caller leaves its loop. Every thread gives up by its own clock, but the
+// answer is the warp's: what it guards are instructions of whole warps (tcgen05.ld, barriers).
 __device__ __forceinline__ bool mm_wait(uint64_t* bar, uint32_t parity, uint32_t* status) {
-  if (mbar_wait(bar, parity, kWaitLimitNs)) return true;
-  atomicOr(status, ST_TIMEOUT);
-  return false;
+  const bool ok = mbar_wait(bar, parity, kWaitLimitNs);
+  if (!ok) atomicOr(status, ST_TIMEOUT);
+  return __all_sync(~0u, ok);
 }
 
 // f with the activation as a constant.

@@ -117,6 +117,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
   }
 
   // (whole warps, with values that are the same in every lane; one lane, always the same, issues)
+  bool ok = true;  // (of the warp: none of its waits ran out)
   if (w == 0) {
     // ---------------------------------------------------------------- copies
     const bool one = elect_one();
@@ -125,7 +126,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
     int st = 0, k = k0;
     uint32_t par = 1;
     for (; k < k1; ++k) {
-      if (!__all_sync(~0u, mm_wait(&bars.empty[st], par, a.status))) break;
+      if (!mm_wait(&bars.empty[st], par, a.status)) break;
       if (one) {
         const uint32_t at = smem + st * slot;
         mbar_expect_tx(&bars.full[st], slot);
@@ -135,7 +136,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
       }
       if (++st == p.stages) st = 0, par ^= 1;
     }
-    if (k < k1)  // a wait ran out: the copies under way first (with the same limit)
+    ok = k == k1;
+    if (!ok)  // a wait ran out: the copies under way first (with the same limit)
       for (int j = max(k0, k - p.stages); j < k; ++j) mbar_wait(&bars.full[(j - k0) % p.stages], ((j - k0) / p.stages) & 1, kWaitLimitNs);
   } else if (w == 2) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(cols) : "memory");
@@ -152,7 +154,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
       int st = 0;
       uint32_t par = 0;
       for (int k = k0; k < k1; ++k) {
-        if (!__all_sync(~0u, mm_wait(&bars.full[st], par, a.status))) break;
+        ok = mm_wait(&bars.full[st], par, a.status);
+        if (!ok) break;
         fence_after();
         if (one) {
           const uint32_t at = smem + st * slot;
@@ -171,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
       walk(std::false_type());
   }
   __syncwarp();
-  const bool ok = mm_wait(&bars.done, 0, a.status);
+  ok = mm_wait(&bars.done, 0, a.status) && ok;
   fence_after();
   const uint32_t tmem = bars.tmem;  // (warp 1 has waited for it)
 
@@ -220,14 +223,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
   uint2 extra = ask(t);
   __syncwarp();
   fence_before();
-  __syncthreads();
+  const bool all = __syncthreads_and(ok);
   fence_after();
   if (w == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols));
   __syncwarp();
   if (p.cluster > 1) cluster_all();  // (the last that any block does with another's shared memory)
 
   // ---------------------------------------------------------------- results, four neighbours of a row at a time
-  if (left <= 0) return;
+  if (left <= 0 || !all) return;  // (a block whose wait ran out has no sums)
   mm_with_act(e.act, [&](auto act) {
     constexpr int kAct = decltype(act)::value;
 #pragma unroll 1

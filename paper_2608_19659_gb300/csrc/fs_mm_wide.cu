@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
         }
       };
       for (int x = 0; x < end; x += two ? 2 * per : per) {
-        ok = __all_sync(~0u, mm_wait(&bars.empty[st], par, a.status));
+        ok = mm_wait(&bars.empty[st], par, a.status);
         if (!ok) break;
         if (one) {
           const uint32_t bar = leader + st * 8;
@@ -247,10 +247,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
         const uint32_t b_block = p.tile / 2 * kMmBlock;
         const uint64_t a_desc = smem_desc(smem, a_mn ? kHalf / 2 : 16, 1024), b_desc = smem_desc(smem + a.sub * kHalf, b_mn ? kHalf / 2 : 16, 1024);
         const int steps = two ? (p.blocks[0] + 1) / 2 + (kMode == MM_GRAD ? (p.blocks[1] + 1) / 2 : 0) : p.blocks[0] + (kMode == MM_GRAD ? p.blocks[1] : 0);
-        if (!__all_sync(~0u, mm_wait(&bars.sum_empty[n & 1], (n >> 1 & 1) ^ 1, a.status))) return;
+        if (!mm_wait(&bars.sum_empty[n & 1], (n >> 1 & 1) ^ 1, a.status)) return;
         fence_after();
         for (int k = 0; k < steps; ++k) {
-          if (!__all_sync(~0u, mm_wait(&bars.full[st], par, a.status))) return;
+          if (!mm_wait(&bars.full[st], par, a.status)) return;
           fence_after();
           if (one) {
             const uint64_t ad = a_desc + at, bd = b_desc + at;
@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
       if (then < a.tiles) t = tile_of<kMode>(a, then), own = look(t);
       const int k = n++;
       i = then;
-      ok = ok && __all_sync(~0u, mm_wait(&bars.sum_full[k & 1], k >> 1 & 1, a.status));
+      ok = ok && mm_wait(&bars.sum_full[k & 1], k >> 1 & 1, a.status);
       if (!ok) continue;
       fence_after();
       const uint32_t at = tmem + lanes + (k & 1) * kTile;
