@@ -656,7 +656,7 @@ int fs_kv_check(void *workspace, void *cuda_stream);
  *
  * As with the cache operators: device pointers of the current device, work is enqueued on cuda_stream, nothing is
  * allocated, calls can be captured; calls that share a workspace run one after the other. Outputs
- * must not overlap inputs or each other (what can be told of that is refused), but y may be the residual. Sizes are arbitrary (rows and out 0 to 2^24, in 1 to 2^24, no operand of 2^40 elements);
+ * must not share a byte with inputs or each other (such calls are refused), but y may be the residual. Sizes are arbitrary (rows and out 0 to 2^24, in 1 to 2^24, no operand of 2^40 elements);
  * what lies behind a row's end is neither used nor written.
  *
  * fs_mm_rows: row r begins at data + r * stride (elements); data 16-byte aligned, stride a multiple of 8 (codes: 16) and

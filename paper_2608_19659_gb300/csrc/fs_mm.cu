@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "fs_mm.cuh"
+#include "fs_rows_overlap.h"
 
 namespace fs {
 
@@ -62,22 +63,15 @@ int check_rows(fs_mm_rows& r, const char* name, int n, int width, int type, bool
   return FS_OK;
 }
 
-// Whether two operands' rows share a byte, as far as that can be told: exact where rows are equally far apart or one operand has a
-// single row; others are taken for disjoint.
+// Whether two operands' rows share a byte.
 struct Span {
   const fs_mm_rows* r;
   int n, width, size;  // rows, elements of a row, bytes of an element
+  bool none() const { return !n || !width || !r->data; }
+  // (a residual's rows may all be the same one)
+  RowSpan rows() const { return {reinterpret_cast<int64_t>(r->data), r->stride ? n : 1, (int64_t)width * size, r->stride * size}; }
 };
-bool overlap(const Span& a, const Span& b) {
-  if (!a.n || !b.n || !a.r->data || !b.r->data) return false;
-  const int64_t pa = reinterpret_cast<int64_t>(a.r->data), pb = reinterpret_cast<int64_t>(b.r->data);
-  const int64_t sa = a.n > 1 ? a.r->stride * a.size : 0, sb = b.n > 1 ? b.r->stride * b.size : 0, wa = (int64_t)a.width * a.size, wb = (int64_t)b.width * b.size;
-  if (pa + (a.n - 1) * sa + wa <= pb || pb + (b.n - 1) * sb + wb <= pa) return false;
-  if (sa == 0 && sb == 0) return true;
-  if (sa && sb && sa != sb) return pa == pb;
-  const int64_t s = sa ? sa : sb, d = ((pb - pa) % s + s) % s;
-  return d < wa || s - d < wb;
-}
+bool overlap(const Span& a, const Span& b) { return !a.none() && !b.none() && rows_overlap(a.rows(), b.rows()); }
 
 // Outputs share nothing with inputs and each other.
 int check_apart(const Span& out, const char* out_name, const Span& in, const char* in_name) {
