@@ -14,6 +14,7 @@
 // takes 2.5 us, of a residual and an activation up to 5.5.
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 #include <utility>
 
 #include "fs_mm.cuh"
@@ -415,7 +416,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
               for (int j = 0; j < 8; ++j) {
                 float slope;
                 const float y = mm_act_slope<kAct>(v[j], slope);
-                v[j] = s[j] * second[j] * slope;
+                // (dy u beyond a float's range may be brought back by the slope, or be nothing with a slope of 0)
+                const float dy_u = s[j] * second[j];
+                v[j] = fabsf(dy_u) <= FLT_MAX ? dy_u * slope : s[j] * slope * second[j];
                 second[j] = s[j] * y;
               }
               y[kPieces + g] = pack8<T>(second);
