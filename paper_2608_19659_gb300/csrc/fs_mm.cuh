@@ -20,6 +20,30 @@ struct MmEpilogue {
   long long out_stride;
 };
 
+// A row's scale xs as near * far, for sums of e4m3 products (0, or 2^-18 to 2^42) that are multiplied by it and by a column's scale s, any
+// floats: far is 2^64 or 2^-64 where xs itself would carry a sum out of a float's range that s brings back, else 1.
+struct alignas(8) MmScale {
+  float near, far;
+};
+__device__ __forceinline__ MmScale mm_scale(float xs) {
+  const float m = fabsf(xs);
+  if (m >= 0x1p60f) return {xs * 0x1p-64f, 0x1p64f};
+  if (m <= 0x1p-60f && m > 0.f) return {xs * 0x1p64f, 0x1p-64f};  // (exact, of subnormals too)
+  return {xs, 1.f};
+}
+// v[i] = (v[i] near) s[i] far, far where it keeps what is between in range: with s if it brings that nearer to 1, else last. (The
+// second form is out of the way of the usual one: 64 rows of 8192 8-bit terms over 10240 13.4 us in graphs without it, 13.5 with it.)
+template <int n>
+__device__ __forceinline__ void mm_scaled(float (&v)[n], MmScale x, const float (&s)[n]) {
+  if (__builtin_expect(x.far == 1.f, 1)) {
+#pragma unroll
+    for (int i = 0; i < n; ++i) v[i] = v[i] * x.near * s[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < n; ++i) v[i] = (fabsf(s[i]) < 1.f) == (x.far > 1.f) ? v[i] * x.near * (s[i] * x.far) : v[i] * x.near * s[i] * x.far;
+  }
+}
+
 // z / (1 + e^-2h), 2 log2(e) h in `e`: the logistic function's share of z. The quotient is
 // off by 2 ulp, and 0 where e^-2h passes 2^126 (values under 2^-119 of z).
 __device__ __forceinline__ float mm_logistic(float z, float e) { return __fdividef(z, 1.f + ex2(-e)); }
@@ -111,7 +135,11 @@ __device__ __forceinline__ float4 mm_load4(const float* p, int n) {
 }
 __device__ __forceinline__ float4 operator*(float4 a, float4 b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); }
 __device__ __forceinline__ float4 operator+(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
-__device__ __forceinline__ float4 operator*(float4 a, float b) { return make_float4(a.x * b, a.y * b, a.z * b, a.w * b); }
+__device__ __forceinline__ float4 mm_scaled(float4 v, MmScale x, float4 s) {
+  float a[4] = {v.x, v.y, v.z, v.w};
+  mm_scaled(a, x, {s.x, s.y, s.z, s.w});
+  return make_float4(a[0], a[1], a[2], a[3]);
+}
 
 // What kernels ahead stored, for the copies of this thread.
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }

@@ -26,7 +26,7 @@ constexpr int kThreads = 256;
 struct FewBars {
   uint64_t full[kMaxStages], empty[kMaxStages], done;
   uint32_t tmem;
-  float x_scale[128];  // of the tokens that this block finishes
+  MmScale x_scale[128];  // of the tokens that this block finishes
 };
 
 struct MmFewArgs {
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
   const int n = n0 + 4 * (threadIdx.x % quads), left = e.cols - n, t_step = kThreads / quads;
   float4 scale0{}, scale1{};
   uint2 bias{};
-  if (e.x_scale && (int)threadIdx.x < mine) bars.x_scale[threadIdx.x] = e.x_scale[t0 + first + threadIdx.x];
+  if (e.x_scale && (int)threadIdx.x < mine) bars.x_scale[threadIdx.x] = mm_scale(e.x_scale[t0 + first + threadIdx.x]);
   if (left > 0 && mine > 0) {
     if (e.x_scale) {
       scale0 = mm_load4(e.w_scale[0] + n, left);
@@ -241,9 +241,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
       float4 z = sum4(at, share * ld, p.cluster), u = z;
       if (kGated) u = sum4(at + width * 4, share * ld, p.cluster);
       if (e.x_scale) {
-        const float xs = bars.x_scale[t];
-        z = z * xs * scale0;
-        if (kGated) u = u * xs * scale1;
+        const MmScale xs = bars.x_scale[t];
+        z = mm_scaled(z, xs, scale0);
+        if (kGated) u = mm_scaled(u, xs, scale1);
       }
       if (!kGated) z = z + mm_floats4<T>(bias);
       z = make_float4(mm_act<kAct>(z.x), mm_act<kAct>(z.y), mm_act<kAct>(z.z), mm_act<kAct>(z.w));

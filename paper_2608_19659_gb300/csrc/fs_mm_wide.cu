@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
         bars.scale[id] = own.scale, bars.bias[id] = own.bias;
         asm volatile("bar.sync 1, 256;" ::: "memory");
       }
-      const float xs = own.x_scale;
+      const MmScale xs = mm_scale(own.x_scale);
       const int then = next(i, n + 1);
       if (then < a.tiles) t = tile_of<kMode>(a, then), own = look(t);
       const int k = n++;
@@ -385,12 +385,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
             for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(z[8 * g + j]), second[j] = one_sum(kMode) ? 0.f : __uint_as_float(u[8 * g + j]);
             if (kScaled && e.x_scale) {
               floats8(s, bars.scale + in_tile);
-#pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] = v[j] * xs * s[j];
+              mm_scaled(v, xs, s);
               if (kMode == MM_GATED) {
                 floats8(s, bars.scale + width + in_tile);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) second[j] = second[j] * xs * s[j];
+                mm_scaled(second, xs, s);
               }
             }
             if (kMode == MM_LINEAR) {

@@ -3,6 +3,7 @@
 import pytest
 
 import mm_reference as ref
+from test_gpu_mm import operands, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +30,39 @@ def test_gradients_where_dy_u_passes_a_floats_range(fsb, cuda, act, T):
         assert bool(o.isfinite().all())
         ref.near(o, want)
     fsb.fs_mm_check(work)
+
+
+SCALES = [(2.0**119, 2.0**-126), (2.0**-126, 2.0**119), (2.0**127, 3e-38), (3e-38, 2.0**127), (2.0**-149, 2.0**127), (3.0, 2.0**-120), (1e-30, 1e30),
+          (2.0**60, 2.0**-60), (2.0**-60, 2.0**60), (2.0**100, 2.0**-20), (2.0**-100, 2.0**-40), (0.0, 2.0**127)]
+
+
+@pytest.mark.parametrize("T,K,N", [(3, 300, 200), (100, 5000, 90), (700, 300, 1000)])
+@pytest.mark.parametrize("a,b", SCALES)
+def test_scales_far_apart(fsb, cuda, T, K, N, a, b):
+    """Any finite scales: a row's may carry a sum out of a float's range that a column's brings back, in some rows and columns
+    but not in others."""
+    torch = cuda
+    x, (w, u), xs, (ws, us), dt = operands(torch, "e4m3", T, K, N, 2, 1, 16)
+    xs[::2], ws[::3], us[::5] = a, b, b
+    xs[1::4], ws[1::3] = -xs[1::4], -ws[1::3]
+    y, work = rows(torch, T, N, dt, 0)[0], fsb.MmWorkspace(T, K, N)
+    fsb.fs_linear(x, w, y, x_scale=xs, w_scale=ws, workspace=work)
+    within(torch, y, *ref.linear(x, w, dt, x_scale=xs, w_scale=ws))
+    fsb.fs_gated_ff(x, w, u, y, activation="relu", x_scale=xs, gate_scale=ws, up_scale=us, workspace=work)
+    # (gate and up are floats: where both are in a float's range)
+    z = [ref.linear(x, t, dt, x_scale=xs, w_scale=s)[0].abs() for t, s in ((w, ws), (u, us))]
+    inside = torch.stack([(t == 0) | (t > 2.0**-120) & (t < 2.0**127) for t in z]).all(0)
+    assert bool(inside.any())
+    want, e = ref.gated(x, w, u, dt, "relu", xs, ws, us)
+    within(torch, y[inside], want[inside], e[inside])
+    fsb.fs_mm_check(work)
+
+
+def within(torch, y, want, e):
+    """Within the bounds; infinite where the value is beyond the type's range for sure, and only where it may be."""
+    top = torch.finfo(y.dtype).max
+    surely, maybe = want.abs() - e > top * (1 + 2.0**-8), want.abs() + e > top
+    assert not bool(y.isnan().any())
+    assert bool((y[surely] == torch.where(want[surely] > 0, float("inf"), float("-inf")).to(y.dtype)).all())
+    assert bool((maybe | y.isfinite()).all())
+    ref.near(y[~maybe], (want[~maybe], e[~maybe]))
