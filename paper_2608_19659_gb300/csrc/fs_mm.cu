@@ -415,7 +415,9 @@ extern "C" int fs_gated_ff_backward(const fs_mm_gated_grad* args, void* workspac
     return e == cudaSuccess ? FS_OK : cuda_say(e, "clear (fs_gated_ff_backward)");
   }
   if (int rc = device_sms(&c.sms)) return rc;
-  // dg and du, then everything that is made of them in one launch
+  // dg and du, then everything that is made of them in one launch. They are rounded to the operands' type in between, as both operands of a
+  // tensor-core product have one: as floats they could be read only by products of tf32, with W and x twice as long and at half the rate. With
+  // the results' own rounding that is 1.4 times the error of one (bf16 2.3e-3 of 64 bits' results, 1.7e-3 in one rounding); a half's range bounds them.
   const long long ld = padded(g.out);
   char* dg = static_cast<char*>(workspace) + kMmPartAt;
   char* du = dg + 2 * g.rows * ld;

@@ -911,7 +911,9 @@ def fs_gated_ff(x, w_gate, w_up, y, *, activation: str = "silu", x_scale=None, g
 def fs_gated_ff_backward(x, w_gate, w_up, dy, dx, dw_gate, dw_up, *, activation: str = "silu",
                          workspace: MmWorkspace, stream=None):
     """The gradients of :func:`fs_gated_ff` (bfloat16 or float16 throughout), given dy, into dx, dw_gate and dw_up, which
-    it returns. ``workspace`` is one made with backward=True."""
+    it returns. ``workspace`` is one made with backward=True. dg = dy u act'(g) and du = dy act(g) are held in x's type: in
+    float16 they are infinite beyond 65504, and gradients that they go into are not finite; a smaller dy (all gradients are
+    linear in it) brings them back."""
     index, dtype = workspace.index, x.dtype
     kind, act = _mm_kinds.get(dtype), ACTIVATIONS.get(activation)
     (rows, inner), out = x.shape, w_gate.shape[0]

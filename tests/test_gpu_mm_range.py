@@ -66,3 +66,35 @@ def within(torch, y, want, e):
     assert bool((y[surely] == torch.where(want[surely] > 0, float("inf"), float("-inf")).to(y.dtype)).all())
     assert bool((maybe | y.isfinite()).all())
     ref.near(y[~maybe], (want[~maybe], e[~maybe]))
+
+
+@pytest.mark.parametrize("T", [40, 700])
+def test_halves_bound_what_the_gradients_are_made_of(fsb, cuda, T):
+    """dg and du beyond 65504: rows that they go into are not finite, all others are right; a smaller dy brings all of them
+    back."""
+    torch = cuda
+    K, N, dt = 48, 320, torch.float16
+    x, (wg, wu), _, _, _ = operands(torch, "float16", T, K, N, 2, 3)
+    wu *= 64
+    dy = rows(torch, T, N, dt, 4, 100.0)[0]
+    dy[::3] *= 60
+    dy[:, ::5] /= 64
+    outs = [rows(torch, n, K, dt, 0)[0] for n in (T, N, N)]
+    work = fsb.MmWorkspace(T, K, N, backward=True)
+    fsb.fs_gated_ff_backward(x, wg, wu, dy, *outs, workspace=work)
+    g, u = x.double() @ wg.double().T, x.double() @ wu.double().T
+    dg, du = (dy.double() * u * ref.slope(g, "silu")).abs(), (dy.double() * ref.act(g, "silu")).abs()
+    over = lambda v, dim, at: (v > at).any(dim)  # noqa: E731
+    want = ref.gated_backward(x, wg, wu, dy)
+    spans = [(torch.maximum(dg, du), 1), (dg, 0), (du, 0)]
+    for o, w, (v, dim) in zip(outs, want, spans):
+        beyond, inside = over(v, dim, 65504 * 1.001), ~over(v, dim, 65504 * 0.999)
+        assert not bool(o[beyond].isfinite().any())
+        within(torch, o[inside], w[0][inside], w[1][inside])
+    assert bool(over(dg, 1, 65504 * 1.001).any()) and not bool(over(dg, 0, 65504 * 0.999).all())
+    small = dy / 2**8  # (exact but for halves under 2^-6)
+    fsb.fs_gated_ff_backward(x, wg, wu, small, *outs, workspace=work)
+    for o, w in zip(outs, ref.gated_backward(x, wg, wu, small)):
+        within(torch, o, *w)  # (dw sums 700 rows: some results are beyond the range themselves)
+    assert bool(((want[0][0].abs() < 60000) & over(dg, 1, 65504 * 1.001)[:, None]).any())  # (what had been lost)
+    fsb.fs_mm_check(work)
