@@ -22,7 +22,7 @@ struct MmEpilogue {
 
 // A row's scale xs as near * far, for sums of e4m3 products (0, or 2^-18 to 2^42) that are multiplied by it and by a column's scale s, any
 // floats: far is 2^64 or 2^-64 where xs itself would carry a sum out of a float's range that s brings back, else 1.
-struct alignas(8) MmScale {
+struct MmScale {
   float near, far;
 };
 __device__ __forceinline__ MmScale mm_scale(float xs) {

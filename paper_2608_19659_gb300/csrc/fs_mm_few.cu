@@ -26,8 +26,10 @@ constexpr int kThreads = 256;
 struct FewBars {
   uint64_t full[kMaxStages], empty[kMaxStages], done;
   uint32_t tmem;
-  MmScale x_scale[128];  // of the tokens that this block finishes
+  float x_scale[128];  // of the tokens that this block finishes
 };
+// Two blocks an SM: a plan's ring and sums of 111 KB, what the ring begins on, these, and the 1 KB that the system keeps.
+static_assert(2 * (111 * 1024 + 1024 + sizeof(FewBars) + 1024) <= 228 * 1024, "half an SM's shared memory");
 
 struct MmFewArgs {
   MmEpilogue e;
@@ -107,7 +109,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
   const int n = n0 + 4 * (threadIdx.x % quads), left = e.cols - n, t_step = kThreads / quads;
   float4 scale0{}, scale1{};
   uint2 bias{};
-  if (e.x_scale && (int)threadIdx.x < mine) bars.x_scale[threadIdx.x] = mm_scale(e.x_scale[t0 + first + threadIdx.x]);
+  if (e.x_scale && (int)threadIdx.x < mine) bars.x_scale[threadIdx.x] = e.x_scale[t0 + first + threadIdx.x];
   if (left > 0 && mine > 0) {
     if (e.x_scale) {
       scale0 = mm_load4(e.w_scale[0] + n, left);
@@ -241,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
       float4 z = sum4(at, share * ld, p.cluster), u = z;
       if (kGated) u = sum4(at + width * 4, share * ld, p.cluster);
       if (e.x_scale) {
-        const MmScale xs = bars.x_scale[t];
+        const MmScale xs = mm_scale(bars.x_scale[t]);
         z = mm_scaled(z, xs, scale0);
         if (kGated) u = mm_scaled(u, xs, scale1);
       }
