@@ -22,7 +22,7 @@ LIB = os.path.join(HERE, "libfleetsieve.so")
 SOURCES = ["fs_api.cu", "fs_solve.cu", "fs_thresh.cu", "fs_score.cu", "fs_replay.cu", "fs_static.cu", "fs_lex.cu",
            "fs_kv.cu", "fs_kv_decode.cu", "fs_kv_chunk.cu", "fs_mm.cu", "fs_mm_few.cu", "fs_mm_wide.cu"]
 HEADERS = ["fs_internal.cuh", "fs_finalize.cuh", "fs_sample.cuh", "fs_rows.cuh", "fs_optional_buf.h", "fs_kv.cuh", "fs_tc.cuh", "fs_mm.cuh",
-           "fs_rows_overlap.h"]
+           "fs_mm_plan.h", "fs_rows_overlap.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-fmad=false", "-Xcompiler", "-fPIC,-O2,-ffp-contract=off",
               "-I", os.path.join(ROOT, "include")]

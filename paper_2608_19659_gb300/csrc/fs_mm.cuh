@@ -4,6 +4,7 @@
 #include <type_traits>
 
 #include "fs_kv.cuh"
+#include "fs_mm_plan.h"
 #include "fs_tc.cuh"
 
 namespace fs {
@@ -171,19 +172,6 @@ __device__ __forceinline__ void mm_with_act(int act, F&& f) {
   }
 }
 
-constexpr int kMmBlock = 128;  // bytes of a row in one block of a sum
-
-// A product for k_mm_few: sums over blocks_k blocks of x rows and W rows.
-struct MmFewPlan {
-  int w_rows;     // rows of W a tile: 32, 64 or 128 (gated: half of them gate's, half up's)
-  int tokens;     // rows of x a tile: a multiple of 16, up to 128
-  int token_tiles, w_tiles;
-  int cluster;    // blocks that share a tile's sum
-  int stages;
-  size_t smem;
-  float ns;       // what it takes, by estimate
-};
-MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms);
 // x and one or two W, each in boxes of one block and the plan's rows.
 cudaError_t launch_mm_few(const CUtensorMap& x, const CUtensorMap& w, const CUtensorMap* up, const MmEpilogue& e, const MmFewPlan& p,
                           int blocks_k, int type, int out_type, uint32_t* status, cudaStream_t s);
@@ -212,7 +200,6 @@ struct MmWideArgs {
   int tiles;
   uint32_t* status;
 };
-int mm_wide_tile(int rows, int cols, int blocks, bool gated, int sms, float* ns);
 cudaError_t launch_mm_wide(MmWideArgs& a, int mode, int type, int out_type, int sms, cudaStream_t s);
 
 }  // namespace fs

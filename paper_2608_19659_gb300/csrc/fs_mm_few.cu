@@ -19,8 +19,7 @@
 namespace fs {
 namespace {
 
-constexpr int kMaxStages = 12;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxStages = kFewStages, kMaxCluster = kFewCluster;
 constexpr int kThreads = 256;
 
 struct FewBars {
@@ -55,11 +54,6 @@ __device__ __forceinline__ void mma_few(uint32_t d, uint64_t a, uint64_t b, uint
 
 __device__ __forceinline__ void st_cluster(uint32_t a, uint32_t x) {
   asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(a), "r"(x) : "memory");
-}
-
-// Tokens of a tile that a block of the cluster finishes: eights, as they come out of tensor memory, or all of fewer.
-__host__ __device__ __forceinline__ int tokens_each(int valid, int cluster) {
-  return valid < 8 ? valid : ((valid + cluster - 1) / cluster + 7) / 8 * 8;
 }
 
 // The sum of four floats of every block of the cluster, `step` bytes apart in this one's shared memory, in the order of the ranks.
@@ -260,65 +254,10 @@ cudaError_t launch(const CUtensorMap& x, const CUtensorMap& w, const CUtensorMap
   static std::atomic<uint64_t> seen{0};
   const cudaError_t limit = smem_limit_once(seen, reinterpret_cast<const void*>(k_mm_few<T, kGated>), 227 * 1024);
   if (limit != cudaSuccess) return limit;
-  return launch_clusters(k_mm_few<T, kGated>, dim3(a.p.w_tiles * a.p.cluster, a.p.token_tiles), dim3(kThreads), a.p.cluster, a.p.smem, s, x, w, u, a);
+  return launch_clusters(k_mm_few<T, kGated>, dim3(a.p.w_tiles * a.p.cluster, a.p.token_tiles), dim3(kThreads), a.p.cluster, 1024 + a.bars_at + sizeof(FewBars), s, x, w, u, a);
 }
-
-int ring_bytes(const MmFewPlan& p) {
-  const int slot = (p.w_rows + p.tokens) * kMmBlock;
-  // (the last stage's products read 128 rows, whatever a tile has)
-  return std::max(p.stages * slot, (p.stages - 1) * slot + 128 * kMmBlock);
-}
-// A cluster's sums come while a block's own products may still read its ring; those of a single block do not.
-int sums_bytes(const MmFewPlan& p, int rows) { return tokens_each(std::min(p.tokens, rows), p.cluster) * p.cluster * p.w_rows * 4; }
-int sums_at(const MmFewPlan& p) { return p.cluster > 1 ? ring_bytes(p) : 0; }
-int bars_at(const MmFewPlan& p, int rows) { return std::max(ring_bytes(p), sums_at(p) + sums_bytes(p, rows)); }
 
 }  // namespace
-
-// The tile and the cluster by an estimate of the time. What it goes by, and what the other choice cost where it decides (us, in
-// graphs): memory at 6.6 TB/s; a block takes 100 bytes a ns, half of that beside another on its SM, and 165 ns a step at
-// least, more with fewer rows of W, 60 more for a gated one's three copies (one row of 1024 8-bit over 8192, tiles of 32 6.0, of
-// 64 5.6, of 128 5.5; 64 rows of 8192 8-bit over 10240, 240 blocks 18.7, 160 21.0, 80 20.8; one row of 8192 over 2 x 1792 gated, tiles of
-// 128 in clusters of 8 11.9, of 6 12.1, of 32 without 24.5); a quarter of the lesser of both, as they do not overlap in whole; a
-// cluster's exchange 0.55 us and 50 bytes a ns (333 rows of 1001 over 777, tiles of 64 in clusters of three 5.8, of six 7.3); blocks
-// beyond what is resident wait for a place (100 rows of 4096 over 2560, 120 blocks 9.8, 160 15.9).
-MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int sms) {
-  MmFewPlan best{};
-  for (int w_rows = 128; w_rows >= 32; w_rows /= 2)
-    for (int cluster = std::min(kMaxCluster, blocks_k); cluster >= 1; --cluster) {
-      MmFewPlan p{};
-      p.w_rows = w_rows, p.cluster = cluster;
-      p.token_tiles = (rows + 127) / 128;
-      p.tokens = ((rows + p.token_tiles - 1) / p.token_tiles + 15) / 16 * 16;
-      const int width = gated ? w_rows / 2 : w_rows, slot = (w_rows + p.tokens) * kMmBlock, depth = (blocks_k + cluster - 1) / cluster;
-      p.w_tiles = (cols + width - 1) / width;
-      const int sums = cluster > 1 ? sums_bytes(p, rows) : 0;
-      // one block an SM if all of them find a place so, else two where each has three stages of its own. Clusters find theirs
-      // in groups of about 18 SMs, of which some are smaller (one row of 8192 over 2 x 1792 gated, tiles of 64, 280 blocks in clusters of 5: 14.4)
-      const int groups = std::max(1, sms / 18);
-      const long long blocks = (long long)p.w_tiles * p.token_tiles * cluster, one = cluster == 1 ? sms : 18 / cluster * cluster * groups;
-      const int half = (111 * 1024 - sums) / slot;  // stages of half an SM's shared memory
-      const bool two = blocks > one && half >= std::min(3, depth);
-      // (where half is enough, for short sums, a block of the next kernel finds room beside this one: a one-token layer of 9 calls 62.5
-      // us without, 54.3 with it; 48 rows of 8192 8-bit over 2 x 7168 gated, 64 steps, 23.4 with it and 22.1 without, one row of 8192 over 1280, 16
-      // steps, 7.1 and 5.8)
-      const bool less = !two && half >= 5 && depth <= 12;
-      p.stages = std::clamp(two || less ? half : (216 * 1024 - sums) / slot, 2, std::min(kMaxStages, std::max(2, depth)));
-      const long long places = !two ? one : cluster == 1 ? 2 * sms : 34 / cluster * cluster * groups;
-      const float waves = (float)((blocks + places - 1) / places), rate = two ? 50.f : 100.f;
-      const float step = std::max(slot / rate, (w_rows == 32 ? 230.f : w_rows == 64 ? 185.f : 165.f) + (gated ? 60.f : 0.f));
-      const float memory = (float)blocks_k * kMmBlock * cols * (gated ? 2 : 1) / 6600.f, steps = waves * depth * step;
-      const float read = std::max(memory, steps) + 0.25f * std::min(memory, steps);
-      // what comes after the sums, a third longer beside another block: a cluster's exchange; 4 ns a token, 8 more for those that
-      // go to other blocks, 15 for those that it finishes (of 128 rows of W). 150 ns for each further tile of tokens
-      const float tokens = (float)std::min(rows, p.tokens), gone = (float)(cluster - 1) / cluster;
-      const float after = (cluster > 1 ? 550.f : 0.f) + tokens * (4.f + gone * (8.f + w_rows / 12.5f)) + 15.f * tokens_each((int)tokens, cluster) * w_rows / 128;
-      p.ns = 2600.f + 150.f * (p.token_tiles - 1) + read + waves * after * (two ? 1.3f : 1.f);
-      if (best.w_rows == 0 || p.ns < 0.995f * best.ns) best = p;
-    }
-  best.smem = 1024 + bars_at(best, rows) + sizeof(FewBars);
-  return best;
-}
 
 cudaError_t launch_mm_few(const CUtensorMap& x, const CUtensorMap& w, const CUtensorMap* up, const MmEpilogue& e, const MmFewPlan& p,
                           int blocks_k, int type, int out_type, uint32_t* status, cudaStream_t s) {

@@ -23,7 +23,7 @@ namespace fs {
 namespace {
 
 constexpr int kStages = 8, kHalf = 128 * kMmBlock, kRing = 12 * kHalf;  // (stages at most)
-constexpr int kTile = 256;                  // rows of a tile; its columns at most
+constexpr int kTile = kWideTile;            // rows of a tile; its columns at most
 constexpr int kGroup = 8;  // tiles of rows that are walked over together (4, 12 and 16 are 1 to 4 % slower)
 
 constexpr int kThreads = 12 * 32, kEnders = 8;  // (warps that finish tiles: two for each of the four groups of 32 rows)
@@ -142,12 +142,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
   // This pair's tiles: every `step`-th. Of gradients whose longest tiles are fewer than there are pairs, those pairs start with one of them, as
   // long as `rounds` of the others, which the other pairs take meanwhile: then `next` is the k-th tile.
   const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
-  auto next = [&](int i, int k) {
-    if (kMode != MM_GRAD || !a.lead) return i + step;
-    const int mine = first < a.lead ? 1 : a.rounds, others = step - a.lead;
-    if (k < mine) return a.lead + k * others + (first - a.lead);
-    return a.lead + a.rounds * others + (k - mine) * step + first;
-  };
+  auto next = [&](int i, int k) { return kMode == MM_GRAD ? mm_next_tile(i, k, first, step, a.lead, a.rounds) : i + step; };
 
   pdl_trigger();
   if (threadIdx.x == 0) {
@@ -477,56 +472,18 @@ cudaError_t launch_mode(const MmWideArgs& a, int mode, int sms, cudaStream_t s) 
 
 }  // namespace
 
-// What a block of 128 bytes of a sum takes over a tile of that width, in ns: the products of a wide one, one thread's wait, products
-// and commit of a narrow one (8192 terms over one tile: 256 wide 42 us, 192 33.7, 160 29.3, 128 26.6, 96 25.7, 64 24.4).
-float mm_wide_block(int tile) { return tile <= 128 ? 140.f + 0.22f * tile : 8.f + 1.13f * tile; }
-
-// The width of a tile by an estimate of the time (in ns): of its sums, or of its end, 17 ns a column (with an activation; 10 without; a
-// choice by 12 comes out the same), where that is longer (2048 rows of 512 over 512: 256 wide 9.6 us, 64 wide 5.3); and the longer the work the more what narrow tiles read again costs (8192 rows over
-// 10240: 256 699 us, 192 816). W is read at 6.6 TB/s, and a quarter of the lesser of both comes on top (32 rows over 10240 of 8192, 160: 35.3).
-int mm_wide_tile(int rows, int cols, int blocks, bool gated, int sms, float* ns) {
-  int best = 0;
-  for (int tile = kTile; tile >= 64; tile -= gated ? 64 : 32) {
-    const int width = gated ? tile / 2 : tile;
-    const long long tiles = (long long)((rows + kTile - 1) / kTile) * ((cols + width - 1) / width);
-    const float waves = (float)((tiles + sms / 2 - 1) / std::max(1, sms / 2));
-    const float again = 1.f + 0.08f * (256.f / tile - 1.f) * std::min(waves, 4.f);
-    const float one = blocks * mm_wide_block(tile), end = 17.f * tile;
-    const float sums = ((waves - 1.f) * std::max(one, end) + one) * again, memory = (float)blocks * kMmBlock * cols * (gated ? 2 : 1) / 6600.f;
-    const float t = std::max(sums, memory) + 0.25f * std::min(sums, memory) + 2900.f + end;
-    if (!best || t < *ns) best = tile, *ns = t;
-  }
-  return best;
-}
-
-// The order of gradients, the product with the longest tiles first, and the width of all their tiles: few long ones set the pace
-// (1362 rows, 704 and 3848, dx's 18 tiles of 121 blocks: 256 wide 69 us, 128 wide 52). Pairs that have one of those get others
-// only when it is done.
-void grad_plan(MmWideArgs& a, int sms) {
-  const int pairs = std::max(1, sms / 2);
-  auto blocks = [](const MmProduct& p) { return p.blocks[0] + p.blocks[1]; };
-  if (blocks(a.product[0]) < blocks(a.product[1])) std::swap(a.product[0], a.product[2]);  // dx comes in first, dW of gate and up behind it
-  const int longest = a.product[0].blocks[1] ? 1 : 2;
-  float least = 0.f;
-  for (int tile = kTile; tile >= 128; tile -= 128) {
-    auto tiles = [&](int i) { return (long long)((a.product[i].e.rows + kTile - 1) / kTile) * ((a.product[i].e.cols + tile - 1) / tile); };
-    auto ns = [&](int i) { return std::max(blocks(a.product[i]) * mm_wide_block(tile), 17.f * tile); };
-    const long long lead = longest == 1 ? tiles(0) : 2 * tiles(0), rest = longest == 1 ? 2 * tiles(2) : tiles(2);
-    const float all = (lead * ns(0) + rest * ns(2)) / pairs * (tile == kTile ? 1.f : 1.08f), t = std::max(ns(0), all) + ns(2) + 17.f * tile;
-    if (tile < kTile && t >= least) break;
-    least = t;
-    for (int i = 0; i < a.products; ++i) a.product[i].tile = tile;
-    a.lead = lead < pairs && lead + rest > pairs ? (int)lead : 0;
-    a.rounds = std::max(1, (int)(ns(0) / ns(2) + 0.5f));
-  }
-}
-
 cudaError_t launch_mm_wide(MmWideArgs& a, int mode, int type, int out_type, int sms, cudaStream_t s) {
   a.eight = type == FS_E4M3;
   a.format = type == FS_KV_BF16 ? 1 : 0;
   a.tiles = 0;
   a.lead = 0;
-  if (mode == MM_GRAD) grad_plan(a, sms);
+  if (mode == MM_GRAD) {  // (dx comes in first, dW of gate and up behind it)
+    const MmGradPlan p = mm_grad_plan(a.product[0].e.rows, a.product[0].e.cols, a.product[1].e.rows, sms);
+    if (p.dw_first) std::swap(a.product[0], a.product[2]);
+    for (int i = 0; i < a.products; ++i) a.product[i].tile = p.tile;
+    a.lead = p.lead;
+    a.rounds = p.rounds;
+  }
   int widest = 0;
   for (int i = 0; i < a.products; ++i) widest = std::max(widest, a.product[i].tile);
   // narrow tiles take two blocks a stage: their products are done before one thread's wait, products and commit for a single block are
