@@ -103,7 +103,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
   const int n = n0 + 4 * (threadIdx.x % quads), left = e.cols - n, t_step = kThreads / quads;
   float4 scale0{}, scale1{};
   uint2 bias{};
-  if (e.x_scale && (int)threadIdx.x < mine) bars.x_scale[threadIdx.x] = e.x_scale[t0 + first + threadIdx.x];
+  float own_scale = 1.f;  // (by the last four warps: the first two would wait for it before they copy and issue)
+  if (const int i = (int)threadIdx.x - 128; e.x_scale && i >= 0 && i < mine) bars.x_scale[i] = own_scale = e.x_scale[t0 + first + i];
   if (left > 0 && mine > 0) {
     if (e.x_scale) {
       scale0 = mm_load4(e.w_scale[0] + n, left);
@@ -219,7 +220,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
   uint2 extra = ask(t);
   __syncwarp();
   fence_before();
-  const bool all = __syncthreads_and(ok);
+  // (rare: a token's scale is far from 1, or a wait ran out)
+  const bool far = __syncthreads_or(!ok || mm_scale(own_scale).far != 1.f), all = !far || __syncthreads_and(ok);
   fence_after();
   if (w == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols));
   __syncwarp();
@@ -227,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
 
   // ---------------------------------------------------------------- results, four neighbours of a row at a time
   if (left <= 0 || !all) return;  // (a block whose wait ran out has no sums)
-  mm_with_act(e.act, [&](auto act) {
+  auto finish = [&](auto act, auto scales_far) {
     constexpr int kAct = decltype(act)::value;
 #pragma unroll 1
     for (; t < mine; t += t_step) {  // (a small loop: its code is fetched once, while nothing else goes on)
@@ -237,16 +239,26 @@ __global__ void __launch_bounds__(kThreads, 2) k_mm_few(const __grid_constant__ 
       float4 z = sum4(at, share * ld, p.cluster), u = z;
       if (kGated) u = sum4(at + width * 4, share * ld, p.cluster);
       if (e.x_scale) {
-        const MmScale xs = mm_scale(bars.x_scale[t]);
-        z = mm_scaled(z, xs, scale0);
-        if (kGated) u = mm_scaled(u, xs, scale1);
+        const float xs = bars.x_scale[t];
+        if constexpr (decltype(scales_far)::value) {
+          z = mm_scaled(z, mm_scale(xs), scale0);
+          if (kGated) u = mm_scaled(u, mm_scale(xs), scale1);
+        } else {
+          z = z * xs * scale0;
+          if (kGated) u = u * xs * scale1;
+        }
       }
       if (!kGated) z = z + mm_floats4<T>(bias);
       z = make_float4(mm_act<kAct>(z.x), mm_act<kAct>(z.y), mm_act<kAct>(z.z), mm_act<kAct>(z.w));
       z = kGated ? z * u : z + mm_floats4<T>(own);
       mm_store4(static_cast<T*>(e.out[0]) + (t0 + first + t) * e.out_stride + n, z, left);
     }
-  });
+  };
+  // (a loop of its own for scales far from 1, after the others)
+  if (!far)
+    mm_with_act(e.act, [&](auto act) { finish(act, std::false_type()); });
+  else
+    mm_with_act(e.act, [&](auto act) { finish(act, std::true_type()); });
 }
 
 template <typename T, bool kGated>

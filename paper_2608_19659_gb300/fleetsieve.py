@@ -784,15 +784,15 @@ class MmWorkspace:
 
 
 _mm_kinds = {}  # torch dtype -> FS_KV_* or FS_E4M3
-_float32 = _uint8 = None  # torch's
+_float32 = _uint8 = _e4m3 = None  # torch's
 
 
 def _mm_known() -> dict:
-    global _float32, _uint8
+    global _float32, _uint8, _e4m3
     if not _mm_kinds:
         import torch
 
-        _float32, _uint8 = torch.float32, torch.uint8
+        _float32, _uint8, _e4m3 = torch.float32, torch.uint8, torch.float8_e4m3fn
         _mm_kinds.update({torch.bfloat16: FS_KV_BF16, torch.float16: FS_KV_FP16, torch.float8_e4m3fn: FS_E4M3})
     return _mm_kinds
 
@@ -953,13 +953,14 @@ def fs_quantise_rows(x, codes, scale, *, stream=None):
         kind = _mm_type(dtype, "x")
     rows, inner = size
     (x0, x1), (c0, c1) = x.stride(), codes.stride()
-    if codes.dtype is not _uint8 and _mm_kinds.get(codes.dtype) != FS_E4M3:
-        raise ValueError(f"codes are {codes.dtype}, not float8_e4m3fn or uint8")
+    of_codes = codes.dtype
+    if of_codes is not _e4m3 and of_codes is not _uint8:
+        raise ValueError(f"codes are {of_codes}, not float8_e4m3fn or uint8")
     if x1 == c1 == 1 and codes.shape == size and codes.get_device() == index:
         xp, cp = x.data_ptr(), codes.data_ptr()
     else:
         xp, x0, _ = _mm_rows(x, "x", dtype, index, size)
-        cp, c0, _ = _mm_rows(codes, "codes", codes.dtype, index, size)
+        cp, c0, _ = _mm_rows(codes, "codes", of_codes, index, size)
     sp = _mm_scale(scale, "codes", index, rows)
     rc = lib().fs_quantise_rows(rows, inner, kind, _mm_pack_rows(xp, x0, 0), _mm_pack_rows(cp, c0, 0), sp,
                                 _current_stream(index) if stream is None else _kv_stream(stream, index))
