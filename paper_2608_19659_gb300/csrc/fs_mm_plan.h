@@ -65,9 +65,12 @@ inline MmFewPlan mm_few_plan(int rows, int cols, int blocks_k, bool gated, int s
       const long long blocks = (long long)p.w_tiles * p.token_tiles * cluster, one = cluster == 1 ? sms : 18 / cluster * cluster * groups;
       const int half = (111 * 1024 - sums) / slot;  // stages of half an SM's shared memory
       const bool two = blocks > one && half >= std::min(3, depth);
-      // (where half is enough, for short sums, a block of the next kernel finds room beside this one: a one-token layer of 9 calls 62.5
-      // us without, 54.3 with it; 48 rows of 8192 8-bit over 2 x 7168 gated, 64 steps, 23.4 with it and 22.1 without, one row of 8192 over 1280, 16
-      // steps, 7.1 and 5.8)
+      // Half of an SM's shared memory for short sums, where that holds five stages: a block of the next kernel finds room beside this one.
+      // Whole -> half (us, in graphs, weights beyond the L2, one row unless said). Up to 12 steps half is the faster in 19 of 26 shapes: 4096 8-bit over
+      // 5120 7.43 -> 6.70, 8192 8-bit over 2560 7.46 -> 6.77, 64 rows of 8192 8-bit over 1280 7.19 -> 7.04; but 6000 bf16 over 1280 6.36 -> 6.68. At 14 to 22 steps
+      // it is now the one, now the other: 12288 8-bit over 2560 9.18 -> 8.39, 8192 bf16 over 1280 7.15 -> 7.38, 64 rows of 8192 bf16 over 1280 8.56 -> 8.97. From 24
+      // on whole is: 14336 bf16 over 1280 9.19 -> 10.13, 64 rows of 12288 bf16 over 1280 10.3 -> 11.3, 8192 bf16 over 5120 16.0 -> 16.5. (A one-token layer of 9 calls
+      // on a rank of TP 8: 46.4 without, 46.1 with any bound of 8 to 24 steps.)
       const bool less = !two && half >= 5 && depth <= 12;
       p.stages = std::clamp(two || less ? half : (216 * 1024 - sums) / slot, 2, std::min(kFewStages, std::max(2, depth)));
       const long long places = !two ? one : cluster == 1 ? 2 * sms : 34 / cluster * cluster * groups;
@@ -113,7 +116,9 @@ inline int mm_wide_tile(int rows, int cols, int blocks, bool gated, int sms, flo
 
 // The order of gradients, the product with the longest tiles first, and the width of all their tiles: few long ones set the pace
 // (1362 rows, 704 and 3848, dx's 18 tiles of 121 blocks: 256 wide 69 us, 128 wide 52). Pairs that have one of those get others
-// only when it is done.
+// only when it is done. A tile's end is counted with 17 ns a column, as above, though gradients have no activation: by 10 some shapes come out
+// wider and are up to 12 % faster (1338 rows, 1462 and 4147: 81 -> 71 us; 2102, 3287 and 577: 55 -> 49), others come out narrower and lose more (382 rows, 3819
+// and 5690: 102 -> 128; 545, 2700 and 4571: 74 -> 96), and with the rounds alone changed times are the same (220, 1546 and 4401: 35.7).
 struct MmGradPlan {
   bool dw_first;     // both dW ahead of dx
   int tile;
