@@ -732,7 +732,8 @@ int fs_gated_ff(const fs_mm_gated *args, void *workspace, int64_t workspace_byte
  * u = x Wu^T (computed again), dg = dy u act'(g) and du = dy act(g),
  *   dx [rows][in] = dg Wg + du Wu,   dw_gate [out][in] = dg^T x,   dw_up [out][in] = du^T x.
  * dg and du are rounded to `type` between the products (they are operands of the tensor cores), the results once: with both,
- * results are off by about 1.4 times what their own rounding is (by up to twice for a few rows or columns).
+ * results are off by about 1.4 times what their own rounding is. Sums of few terms, over which dg's and du's roundings would not
+ * average out (dw with up to 64 rows, dx with up to 64 columns, out), take them in two terms each: a value and what its rounding left.
  * In FS_KV_FP16 that bounds them: dg or du beyond 65504 is infinite, and the row of dx and the row of dw_gate or dw_up
  * that it goes into are not finite, even where the formula's results would be. All gradients are linear in dy: given
  * 2^-k dy they come out as 2^-k times themselves.

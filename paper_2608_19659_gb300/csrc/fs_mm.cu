@@ -5,6 +5,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <type_traits>
+#include <utility>
 
 #include "fs_mm.cuh"
 #include "fs_rows_overlap.h"
@@ -83,11 +84,11 @@ int check_apart(const Span& out, const char* out_name, const float* scales, int 
   return overlap(out, {&r, 1, n, 4}) ? say(FS_EINVAL, "%s and the scales of %s overlap", out_name, in_name) : FS_OK;
 }
 
-constexpr int64_t kMmPartAt = 256;  // the status word, then dg and du of a backward pass
+constexpr int64_t kMmPartAt = 256;  // the status word, then dg and du of a backward pass, and what their rounding left
 
 long long padded(int n) { return ((long long)n + 63) & ~63ll; }
 
-int64_t workspace_of(int rows, int out, bool backward) { return kMmPartAt + (backward ? 4ll * rows * padded(out) : 0); }
+int64_t workspace_of(int rows, int out, bool backward) { return kMmPartAt + (backward ? 2 * mm_terms(rows, out) : 0); }
 
 int check_workspace(const void* ws, int64_t bytes, int64_t need) {
   if (!ws) return say(FS_EINVAL, "workspace is NULL");
@@ -142,7 +143,7 @@ int few_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const
   return r == cudaSuccess ? FS_OK : cuda_say(r, c.what);
 }
 
-// The same of many rows; with e.out[1] the first product of a backward pass.
+// The same of many rows; with e.out[1] the first product of a backward pass, with e.out[2] in two terms.
 int wide_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, const fs_mm_rows* up, const MmEpilogue& e, int tile) {
   MmWideArgs a{};
   if (int rc = rows_map(&a.maps[0], x.data, e.rows, c.in, x.stride, c.type, 128)) return rc;
@@ -152,7 +153,7 @@ int wide_product(const MmCall& c, const fs_mm_rows& x, const fs_mm_rows& w, cons
   a.product[0] = {e, {0, 0}, {1, 2}, {c.blocks(), 0}, false, false, tile};
   a.products = 1;
   a.status = c.status;
-  const cudaError_t r = launch_mm_wide(a, e.out[1] ? MM_BACK : up ? MM_GATED : MM_LINEAR, c.type, c.out_type, c.sms, c.stream);
+  const cudaError_t r = launch_mm_wide(a, e.out[2] ? MM_BACK_TWO : e.out[1] ? MM_BACK : up ? MM_GATED : MM_LINEAR, c.type, c.out_type, c.sms, c.stream);
   return r == cudaSuccess ? FS_OK : cuda_say(r, c.what);
 }
 
@@ -417,28 +418,35 @@ extern "C" int fs_gated_ff_backward(const fs_mm_gated_grad* args, void* workspac
   if (int rc = device_sms(&c.sms)) return rc;
   // dg and du, then everything that is made of them in one launch. They are rounded to the operands' type in between, as both operands of a
   // tensor-core product have one: as floats they could be read only by products of tf32, with W and x twice as long and at half the rate. With
-  // the results' own rounding that is 1.4 times the error of one (bf16 2.3e-3 of 64 bits' results, 1.7e-3 in one rounding); a half's range bounds them.
+  // the results' own rounding that is 1.4 times the error of one (bf16 2.3e-3 of 64 bits' results, 1.7e-3 in one rounding), in short sums more:
+  // those have them in two terms (mm_two_terms_dw, mm_two_terms_dx). A half's range bounds them.
   const long long ld = padded(g.out);
   char* dg = static_cast<char*>(workspace) + kMmPartAt;
   char* du = dg + 2 * g.rows * ld;
+  const bool dx_two = mm_two_terms_dx(g.out), dw_two = mm_two_terms_dw(g.rows), two = dx_two || dw_two;
+  char* dg_left = two ? du + 2 * g.rows * ld : nullptr;
+  char* du_left = two ? dg_left + 2 * g.rows * ld : nullptr;
   float ns = 0.f;
-  if (int rc = wide_product(c, g.x, g.w_gate, &g.w_up, {g.rows, g.out, g.activation, nullptr, {}, nullptr, g.dy.data, g.dy.stride, {dg, du}, ld},
+  if (int rc = wide_product(c, g.x, g.w_gate, &g.w_up, {g.rows, g.out, g.activation, nullptr, {}, nullptr, g.dy.data, g.dy.stride, {dg, du, dg_left, du_left}, ld},
                             mm_wide_tile(g.rows, g.out, c.blocks(), true, c.sms, &ns)))
     return rc;
   MmWideArgs a{};
-  enum { DG, DU, WG_T, WU_T, DG_T, DU_T, X_T };
-  if (int rc = rows_map(&a.maps[DG], dg, g.rows, g.out, ld, g.type, 128)) return rc;
-  if (int rc = rows_map(&a.maps[DU], du, g.rows, g.out, ld, g.type, 128)) return rc;
+  enum { DG, DU, DG_LEFT, DU_LEFT, WG_T, WU_T, DG_T, DU_T, DG_LEFT_T, DU_LEFT_T, X_T };
+  const std::pair<int, const char*> terms[] = {{DG, dg}, {DU, du}, {DG_LEFT, dg_left}, {DU_LEFT, du_left}};
+  for (const auto& [at, data] : terms) {
+    if (!data) continue;
+    if (int rc = rows_map(&a.maps[at], data, g.rows, g.out, ld, g.type, 128)) return rc;
+    if (int rc = rows_map(&a.maps[at + DG_T - DG], data, g.rows, g.out, ld, g.type, 64)) return rc;
+  }
   if (int rc = rows_map(&a.maps[WG_T], g.w_gate.data, g.out, g.in, g.w_gate.stride, g.type, 64)) return rc;
   if (int rc = rows_map(&a.maps[WU_T], g.w_up.data, g.out, g.in, g.w_up.stride, g.type, 64)) return rc;
-  if (int rc = rows_map(&a.maps[DG_T], dg, g.rows, g.out, ld, g.type, 64)) return rc;
-  if (int rc = rows_map(&a.maps[DU_T], du, g.rows, g.out, ld, g.type, 64)) return rc;
   if (int rc = rows_map(&a.maps[X_T], g.x.data, g.rows, g.in, g.x.stride, g.type, 64)) return rc;
   auto to = [&](const fs_mm_rows& r, int n) { return MmEpilogue{n, g.in, FS_ACT_NONE, nullptr, {}, nullptr, nullptr, 0, {r.data, nullptr}, r.stride}; };
   const int out_blocks = (g.out + 63) / 64, row_blocks = (g.rows + 63) / 64;
-  a.product[0] = {to(g.dx, g.rows), {DG, DU}, {WG_T, WU_T}, {out_blocks, out_blocks}, false, true};
-  a.product[1] = {to(g.dw_gate, g.out), {DG_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true};
-  a.product[2] = {to(g.dw_up, g.out), {DU_T, 0}, {X_T, 0}, {row_blocks, 0}, true, true};
+  const int out_left = dx_two ? out_blocks : 0, row_left = dw_two ? row_blocks : 0;
+  a.product[0] = {to(g.dx, g.rows), {DG, DU, DG_LEFT, DU_LEFT}, {WG_T, WU_T, WG_T, WU_T}, {out_blocks, out_blocks, out_left, out_left}, false, true};
+  a.product[1] = {to(g.dw_gate, g.out), {DG_T, DG_LEFT_T}, {X_T, X_T}, {row_blocks, row_left}, true, true};
+  a.product[2] = {to(g.dw_up, g.out), {DU_T, DU_LEFT_T}, {X_T, X_T}, {row_blocks, row_left}, true, true};
   a.products = 3;
   a.status = c.status;
   const cudaError_t e = launch_mm_wide(a, MM_GRAD, g.type, g.type, c.sms, c.stream);

@@ -17,7 +17,7 @@ struct MmEpilogue {
   const void* bias;
   const void* in;  // residual, or dy of the backward pass
   long long in_stride;
-  void* out[2];  // y; dg and du in the backward pass
+  void* out[4];  // y; dg and du in the backward pass, and in two terms what their rounding left
   long long out_stride;
 };
 
@@ -176,15 +176,15 @@ __device__ __forceinline__ void mm_with_act(int act, F&& f) {
 cudaError_t launch_mm_few(const CUtensorMap& x, const CUtensorMap& w, const CUtensorMap* up, const MmEpilogue& e, const MmFewPlan& p,
                           int blocks_k, int type, int out_type, uint32_t* status, cudaStream_t s);
 
-enum { MM_LINEAR, MM_GATED, MM_BACK, MM_GRAD };
+enum { MM_LINEAR, MM_GATED, MM_BACK, MM_GRAD, MM_BACK_TWO };
 
-// One product of a launch of k_mm_wide: e.rows x e.cols results, sums over blocks[0] blocks of maps a[0] and b[0] (MM_GATED, MM_BACK: b[0]
-// for gate and b[1] for up). Maps have boxes of 128 rows (B: half a tile's columns) and one block. MM_GRAD: up to three products,
-// whose sums go on over blocks[1] blocks of a[1] and b[1], and whose operands may lie the other way (a_mn, b_mn: the rows are
+// One product of a launch of k_mm_wide: e.rows x e.cols results, sums over blocks[0] blocks of maps a[0] and b[0] (MM_GATED, MM_BACK, MM_BACK_TWO:
+// b[0] for gate and b[1] for up). Maps have boxes of 128 rows (B: half a tile's columns) and one block. MM_GRAD: up to three products,
+// whose sums go on over blocks[i] blocks of a[i] and b[i], and whose operands may lie the other way (a_mn, b_mn: the rows are
 // contiguous, boxes are of 64 of them and 64 terms of the sum); results are stored as they are.
 struct MmProduct {
   MmEpilogue e;
-  int a[2], b[2], blocks[2];
+  int a[4], b[4], blocks[4];
   bool a_mn, b_mn;
   int tile;         // (MM_GRAD: launch_mm_wide's) columns of a tile (gated: of gate and of up together): a multiple of 32 (gated: 64) up to 256
   // launch_mm_wide's: tiles of rows, tiles in all, and of a group of rows' tiles that are walked over together. (Under 2^31: no operand
@@ -192,7 +192,7 @@ struct MmProduct {
   int row_tiles, tiles, group;
 };
 struct MmWideArgs {
-  CUtensorMap maps[8];
+  CUtensorMap maps[11];
   MmProduct product[3];
   int products, eight, format;
   int lead, rounds;        // (launch_mm_wide's: pairs that start with one of the longest tiles, and how many others that takes as long as)

@@ -114,6 +114,20 @@ inline int mm_wide_tile(int rows, int cols, int blocks, bool gated, int sms, flo
   return best;
 }
 
+// dg and du, rounded to operands of the gradients' products, are held in two terms each (a value, and what its rounding left) for results whose sums
+// are a block long: dW with up to 64 rows, dx with up to 64 columns. In longer sums the roundings average out to 1.41 times the error that the
+// results' own rounding makes, in these it came to 1.1 to 2.4 times; with two terms to 1.00. What it takes (us, one term -> two): 1 row of 520 over 1003 15.1 ->
+// 15.9, 16 rows of 300 over 2000 20.7 -> 21.2, 1 row of 4096 over 7168 111 -> 113, 2300 rows of 256 over 64 13.3 -> 14.0, 4096 of 4096 over 64 38.5 -> 43.2. For all sums it
+// would be twice the products of the second launch: 77 rows of 520 over 1003 15.8 -> 16.6 for dW alone, 4096 rows of 4096 over 512 64 -> 87 for dx.
+constexpr int kTwoTermRows = 64, kTwoTermColumns = 64;
+inline bool mm_two_terms_dw(int rows) { return rows <= kTwoTermRows; }
+inline bool mm_two_terms_dx(int out) { return out <= kTwoTermColumns; }
+// Elements of all terms: not fewer for larger sizes, as a workspace serves all up to its own.
+inline long long mm_terms(int rows, int out) {
+  auto both = [](long long r, long long n) { return 2 * r * ((n + 63) / 64 * 64); };
+  return std::max({both(rows, out), 2 * both(std::min(rows, kTwoTermRows), out), 2 * both(rows, std::min(out, kTwoTermColumns))});
+}
+
 // The order of gradients, the product with the longest tiles first, and the width of all their tiles: few long ones set the pace
 // (1362 rows, 704 and 3848, dx's 18 tiles of 121 blocks: 256 wide 69 us, 128 wide 52). Pairs that have one of those get others
 // only when it is done. A tile's end is counted with 17 ns a column, as above, though gradients have no activation: by 10 some shapes come out
@@ -125,7 +139,8 @@ struct MmGradPlan {
   int lead, rounds;  // pairs that start with one of the longest tiles (0: tiles in their order), and how many others that takes as long as
 };
 inline MmGradPlan mm_grad_plan(int rows, int in, int out, int sms) {
-  const int pairs = std::max(1, sms / 2), dx_blocks = 2 * ((out + 63) / 64), dw_blocks = (rows + 63) / 64;
+  const int pairs = std::max(1, sms / 2);
+  const int dx_blocks = (mm_two_terms_dx(out) ? 4 : 2) * ((out + 63) / 64), dw_blocks = (mm_two_terms_dw(rows) ? 2 : 1) * ((rows + 63) / 64);
   MmGradPlan best{};
   best.dw_first = dx_blocks < dw_blocks;
   const int longest = best.dw_first ? dw_blocks : dx_blocks, shortest = best.dw_first ? dx_blocks : dw_blocks;

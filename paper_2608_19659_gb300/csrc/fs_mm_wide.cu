@@ -40,6 +40,8 @@ struct WideBars {
 constexpr size_t kSmem = 226 * 1024;
 static_assert(kSmem >= 1024 + kRing + sizeof(WideBars), "a block's shared memory");
 
+constexpr int kParts = 4;  // of a gradient's sum, at most
+
 // Whether a tile's columns are W's rows (and not gate's and up's).
 __host__ __device__ constexpr bool one_sum(int mode) { return mode == MM_LINEAR || mode == MM_GRAD; }
 
@@ -127,6 +129,15 @@ __device__ __forceinline__ void floats8(float (&v)[8], uint4 w) {
   const float2 a = Elem<T>::two(w.x), b = Elem<T>::two(w.y), c = Elem<T>::two(w.z), d = Elem<T>::two(w.w);
   v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
 }
+// What rounding v to w left, rounded in its turn.
+template <typename T>
+__device__ __forceinline__ uint4 left8(const float (&v)[8], uint4 w) {
+  float r[8];
+  floats8<T>(r, w);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r[j] = v[j] - r[j];
+  return pack8<T>(r);
+}
 __device__ __forceinline__ void floats8(float (&v)[8], const float* p) {
   const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
   v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
@@ -205,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
       const int row = !of_b ? t.m0 + rank * 128 : one_sum(kMode) ? t.n0 + rank * (p.tile / 2) : t.n0;
       const uint32_t part_bytes = of_b ? p.tile / 2 * kMmBlock : kHalf, bytes = a.sub * (2 * kHalf + p.tile * kMmBlock);  // a block's; both SMs' stage
       const bool high = !of_b || p.tile > 128;
-      for (int part = 0; ok && part < (kMode == MM_GRAD ? 2 : 1); ++part) {
+      for (int part = 0; ok && part < (kMode == MM_GRAD ? kParts : 1); ++part) {
         const CUtensorMap* map = &a.maps[of_b ? p.b[one_sum(kMode) ? part : rank] : p.a[part]];
         const int end = p.blocks[part] * per;
         if (kMode == MM_GRAD && (of_b ? p.b_mn : p.a_mn))
@@ -242,7 +253,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
         const uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;
         const uint32_t b_block = p.tile / 2 * kMmBlock;
         const uint64_t a_desc = smem_desc(smem, a_mn ? kHalf / 2 : 16, 1024), b_desc = smem_desc(smem + a.sub * kHalf, b_mn ? kHalf / 2 : 16, 1024);
-        const int steps = two ? (p.blocks[0] + 1) / 2 + (kMode == MM_GRAD ? (p.blocks[1] + 1) / 2 : 0) : p.blocks[0] + (kMode == MM_GRAD ? p.blocks[1] : 0);
+        int steps = two ? (p.blocks[0] + 1) / 2 : p.blocks[0];
+        if (kMode == MM_GRAD)
+#pragma unroll
+          for (int part = 1; part < kParts; ++part) steps += two ? (p.blocks[part] + 1) / 2 : p.blocks[part];
         if (!mm_wait(&bars.sum_empty[n & 1], (n >> 1 & 1) ^ 1, a.status)) return;
         fence_after();
         for (int k = 0; k < steps; ++k) {
@@ -273,7 +287,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
     // ---------------------------------------------------------------- results, a row a thread, 32 columns at a time (16 with two
     // results each: registers). Between threads and memory they pass through shared memory, so that a warp's access covers
     // whole sectors of 8 rows, not 16 bytes of 32 (4096 rows of 1024 8-bit terms over 8192 columns, with a residual: 89 us)
-    constexpr int kCols = kMode == MM_BACK ? 16 : 32, kPieces = kCols / 8;
+    constexpr bool kBack = kMode == MM_BACK || kMode == MM_BACK_TWO;
+    constexpr int kCols = kBack ? 16 : 32, kPieces = kCols / 8;
     constexpr bool kScaled = kMode == MM_LINEAR || kMode == MM_GATED;  // 8-bit operands, bias
     const uint32_t lanes = (uint32_t)(w & 3) << 21;
     const int id = threadIdx.x - 128, half = id >> 7;
@@ -371,7 +386,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
             __syncwarp();
           }
           wait_ld();
-          uint4 y[(kMode == MM_BACK ? 2 : 1) * kPieces];
+          uint4 y[4];  // (of a backward pass dg, then du)
+          [[maybe_unused]] uint4 left[kMode == MM_BACK_TWO ? 4 : 1];  // what their rounding left
 #pragma unroll
           for (int g = 0; g < kPieces; ++g) {
             const int in_tile = kCols * c + 8 * g;
@@ -415,27 +431,36 @@ __global__ void __launch_bounds__(kThreads, 1) k_mm_wide(const __grid_constant__
                 second[j] = s[j] * y;
               }
               y[kPieces + g] = pack8<T>(second);
+              if constexpr (kMode == MM_BACK_TWO) left[kPieces + g] = left8<T>(second, y[kPieces + g]);
             }
             y[g] = pack8<T>(v);
+            if constexpr (kMode == MM_BACK_TWO) left[g] = left8<T>(v, y[g]);
           }
-          // (after all that is read of shared memory, which a store between would hold up; where a row's own addend was)
+          auto put = [&](uint4 (&y)[4], void* one, void* other) {
+            // (after all that is read of shared memory, which a store between would hold up; where a row's own addend was)
 #pragma unroll
-          for (int g = 0; g < (kMode == MM_BACK ? 2 : 1) * kPieces; ++g) pass[at_piece(lane, g)] = y[g];
-          __syncwarp();
-          const int piece = lane % 4, col = n0 + 8 * (piece % kPieces);
-          void* const out = kMode == MM_BACK && piece >= kPieces ? e.out[1] : e.out[0];
-          if (rows_in && n0 + kCols <= e.cols) {
-            uint16_t* to = static_cast<uint16_t*>(out) + (m0 + lane / 4) * e.out_stride + col;
+            for (int g = 0; g < 4; ++g) pass[at_piece(lane, g)] = y[g];
+            __syncwarp();
+            const int piece = lane % 4, col = n0 + 8 * (piece % kPieces);
+            void* const out = kBack && piece >= kPieces ? other : one;
+            if (rows_in && n0 + kCols <= e.cols) {
+              uint16_t* to = static_cast<uint16_t*>(out) + (m0 + lane / 4) * e.out_stride + col;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) y[g] = pass[at_piece(8 * g + lane / 4, piece)];
+              for (int g = 0; g < 4; ++g) y[g] = pass[at_piece(8 * g + lane / 4, piece)];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) *reinterpret_cast<uint4*>(to + 8 * g * e.out_stride) = y[g];
-          } else {
+              for (int g = 0; g < 4; ++g) *reinterpret_cast<uint4*>(to + 8 * g * e.out_stride) = y[g];
+            } else {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const int r = 8 * g + lane / 4;
-              if (m0 + r < e.rows && col < e.cols) store8(out, (m0 + r) * e.out_stride + col, pass[at_piece(r, piece)], e.cols - col);
+              for (int g = 0; g < 4; ++g) {
+                const int r = 8 * g + lane / 4;
+                if (m0 + r < e.rows && col < e.cols) store8(out, (m0 + r) * e.out_stride + col, pass[at_piece(r, piece)], e.cols - col);
+              }
             }
+          };
+          put(y, e.out[0], e.out[1]);
+          if constexpr (kMode == MM_BACK_TWO) {
+            __syncwarp();
+            put(left, e.out[2], e.out[3]);
           }
         }
       });
@@ -466,6 +491,7 @@ cudaError_t launch_mode(const MmWideArgs& a, int mode, int sms, cudaStream_t s) 
     case MM_LINEAR: return launch<T, MM_LINEAR>(a, sms, s);
     case MM_GATED: return launch<T, MM_GATED>(a, sms, s);
     case MM_BACK: return launch<T, MM_BACK>(a, sms, s);
+    case MM_BACK_TWO: return launch<T, MM_BACK_TWO>(a, sms, s);
     default: return launch<T, MM_GRAD>(a, sms, s);
   }
 }

@@ -26,6 +26,7 @@ extern "C" void grad(int rows, int in, int out, int sms, int* p) {
   const fs::MmGradPlan g = fs::mm_grad_plan(rows, in, out, sms);
   p[0] = g.dw_first, p[1] = g.tile, p[2] = g.lead, p[3] = g.rounds;
 }
+extern "C" long long terms(int rows, int out) { return fs::mm_terms(rows, out); }
 extern "C" int next_tile(int i, int k, int first, int step, int lead, int rounds) { return fs::mm_next_tile(i, k, first, step, lead, rounds); }
 """
 
@@ -37,7 +38,9 @@ def lib():
         with open(src, "w") as f:
             f.write(HARNESS)
         subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-Werror", "-shared", "-fPIC", "-I", _build.CSRC, src, "-o", so], check=True)
-        return C.CDLL(so)
+        loaded = C.CDLL(so)
+        loaded.terms.restype = C.c_longlong
+        return loaded
 
 
 def up(a, b):

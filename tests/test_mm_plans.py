@@ -47,3 +47,16 @@ def test_every_gradient_tile_is_taken_once(sms):
                 i = then
         assert sorted(seen) == list(range(p.tiles)), (rows, inner, out, p)
     assert sms == 2 or led > 20
+
+
+def test_the_terms_of_smaller_sizes_fit():
+    """A workspace's room for dg, du and their second terms: never less for a larger size, and enough for its own."""
+    lib = mm_plans.lib()
+    for rows, out in sizes(3, 4000, 9000, 9000):
+        most = lib.terms(rows, out)
+        two = rows <= 64 or out <= 64
+        assert most >= (4 if two else 2) * rows * mm_plans.up(out, 64) * 64
+        for r, o in sizes(rows + out, 6, rows, out):
+            assert lib.terms(r, o) <= most
+    assert [lib.terms(*s) for s in ((64, 64), (65, 64), (65, 256), (10000, 64), (10000, 65), (0, 5), (5, 0))] == [
+        4 * 64 * 64, 4 * 65 * 64, 4 * 64 * 256, 4 * 10000 * 64, 4 * 10000 * 64, 0, 0]
