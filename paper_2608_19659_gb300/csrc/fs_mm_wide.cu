@@ -5,8 +5,8 @@
 // (cta_group::2), and each block has its 128 rows' 256 sums in its tensor memory, twice: while eight warps finish a tile and store
 // it, the next one's sums are under way. Blocks stay for the whole launch and walk over the tiles, eight tiles of rows wide,
 // so that what is resident at a time shares its rows of W through the L2.
-// A launch holds up to three products (the backward pass: dx and both dW), whose sums may have two parts (dx: over gate
-// and up) and whose operands may lie either way (dx reads W, dW reads both, across their rows).
+// A launch holds up to three products (the backward pass: dx and both dW), whose sums may have up to four parts (dx: over gate
+// and up, each of one term or two) and whose operands may lie either way (dx reads W, dW reads both, across their rows).
 // Of a gated block the first SM of a pair loads gate's rows and the second up's, so that a thread has both sums of a result.
 // Bound by the tensor cores, and they by power: 8192 rows of 8192 bf16 over 10240 677 to 690 us in a burst (2.0 PFLOP/s), 750 to 790 in a
 // row; 4096 rows of 7168 8-bit over 8192 131 us (3.7); the tensor pipe is active 87 to 90 % of the time with full waves. Tiles of short
