@@ -34,8 +34,9 @@ inline bool rows_overlap(RowSpan a, RowSpan b) {
   using Wide = __int128;  // (rows that no memory holds are asked about too)
   const Wide reach = (Wide)(a.n - 1) * a.step + a.width;
   const Wide d = (Wide)a.at - b.at;  // from b's first byte to a's
+  if (d + reach <= 0 || d >= (Wide)(b.n - 1) * b.step + b.width) return false;  // (usually, and without a division)
   const Wide first = d < b.width ? 0 : (d - b.width) / b.step + 1;
-  const Wide end = d + reach <= 0 ? 0 : std::min<Wide>(b.n, (d + reach - 1) / b.step + 1);
+  const Wide end = std::min<Wide>(b.n, (d + reach - 1) / b.step + 1);
   if (first >= end) return false;
   // row j meets one where b.at + j b.step - a.at + b.width - 1, modulo a's step, is under both widths together less 1
   const int64_t both = a.width + b.width - 1;
